@@ -314,7 +314,7 @@ def _handles(s):
     if c["op"] == "packed":
         s["ws"] = B.alloc_workspace(s["prm"], s["q"].shape[1], B.TCA_OP_PACKED)
     elif c["op"] == "tree":
-        s["ws"] = B.alloc_tree_workspace(s["prm"], s["handle"].rows_total, c["T"])
+        s["ws"] = B.alloc_tree_workspace(s["prm"], c["T"])
 
 
 # ------------------------------------------------------------------ one pass
