@@ -19,8 +19,8 @@
  *     synchronises the host except the three that read a status back (tca_ws_status,
  *     tca_cache_status, tca_decode_static_status).  Outputs are valid once the stream has
  *     been synchronised.
- *   - Status words.  Word 0 of the prefill, decode, select and calibration workspaces is a
- *     STICKY status word: zero it once after allocating (a zero-filled workspace is fine); a
+ *   - Status words.  Word 0 of the prefill, packed, decode, tree, select and calibration
+ *     workspaces is a STICKY status word: zero it once after allocating (a zero-filled workspace is fine); a
  *     kernel sets it when one of its bounded device-side waits gives up (or, in the
  *     range-checked build, when an index is out of range) and nothing in the library clears
  *     it.  While it is set, the tensor-core kernels return at once without computing.  After
@@ -80,7 +80,8 @@ enum {
 
 enum {
   TCA_OP_SCORE = 0, TCA_OP_SELECT = 1, TCA_OP_COMPACT = 2,
-  TCA_OP_PREFILL = 3, TCA_OP_DECODE = 4, TCA_OP_APPEND = 5, TCA_OP_CALIB = 6, TCA_OP_SCORE_SELECT = 7
+  TCA_OP_PREFILL = 3, TCA_OP_DECODE = 4, TCA_OP_APPEND = 5, TCA_OP_CALIB = 6, TCA_OP_SCORE_SELECT = 7,
+  TCA_OP_PACKED = 8
 };
 
 /* Hyper-parameters of one attention layer (Algorithm 2, REQUIRE line). */
@@ -362,6 +363,86 @@ int tca_attn_decode(const tca_params* prm, const void* q, const tca_cache_desc* 
 int tca_cache_append(const tca_params* prm, tca_cache_desc* cache, const void* k_new,
                      const void* v_new, const void* q_cur, void* stream);
 
+/*
+ * Causal attention of whole prompts of different lengths, packed one after another (Eq. 2 with every
+ * key retained: what the method computes for a prompt no longer than the window, and for layers or
+ * prompts that are not compressed).  prm->batch is the number of sequences; sequence s owns rows
+ * [seq_start[s], seq_start[s+1]) of every buffer and its row i attends to its rows j <= i.
+ *   Q, O       DEVICE [n_q_heads, rows, head_dim]     K, V  DEVICE [n_kv_heads, rows, head_dim]
+ *   rows       rows of every buffer; rows that belong to no sequence are neither computed nor written
+ *   seq_start  DEVICE [batch + 1] int64, ascending, within [0, rows]; a sequence may be empty.  Read
+ *              on the device only, so a captured call may be replayed with other lengths.  Values
+ *              outside [0, rows] are clamped; sequences that overlap give unspecified rows of O.
+ *   strides    HOST [8], optional: element strides {head, row} of Q, K, V, O in that order, each at
+ *              least head_dim and a multiple of 16 bytes (a token-major [rows, heads, d] buffer, or
+ *              one with Q, K and V side by side).  NULL: contiguous buffers of the shapes above.
+ *   ws         DEVICE workspace, tca_workspace_bytes(prm, rows, TCA_OP_PACKED); word 0 is the sticky
+ *              status word
+ * Row i's result does not depend on any other sequence, nor on what its own later rows hold (an
+ * infinity or NaN there included).  O must not overlap Q, K or V.  prm->block, window and alpha are
+ * not used.  TCA_FLAG_PREFILL_SIMT runs bf16 on the FP32 pipes.
+ */
+int tca_attn_packed(const tca_params* prm, const void* Q, const void* K, const void* V, int64_t rows,
+                    const int64_t* seq_start, const int64_t* strides, void* O,
+                    void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Packed prompts enter the retained cache with all their tokens: sequence i of the packed K, V becomes
+ * cache sequence slots[i] (all its KV heads), exactly as tca_compact_kv with a 100 % budget would leave
+ * it: with m = floor((len - window) / block) (0 for a shorter prompt), rows [0, m*block) in the global
+ * region, the rest in the ring from slot 0.  Other cache sequences are not touched, so prompts can join
+ * a batch that is already decoding.  prm->batch is the cache's number of sequences.
+ *   K, V       DEVICE [n_kv_heads, rows, head_dim]
+ *   strides    HOST [4], optional: element strides {head, row} of K and V as in tca_attn_packed
+ *   seq_start  HOST [n_seq + 1], ascending, within [0, rows]
+ *   slots      HOST [n_seq], optional (NULL: sequence i goes to i): distinct cache sequences
+ * TCA_ERR_CAPACITY if a prompt's m*block exceeds its units' global_cap or the rest exceeds tail_cap.
+ */
+int tca_cache_load(const tca_params* prm, const void* K, const void* V, int64_t rows,
+                   const int64_t* strides, const int64_t* seq_start, const int32_t* slots,
+                   int32_t n_seq, tca_cache_desc* cache, void* stream);
+
+/* Most drafted tokens per sequence that tca_attn_tree and tca_cache_accept take. */
+#define TCA_TREE_MAX 128
+
+/*
+ * Attention of a tree of drafted tokens over the retained cache (speculative decoding: several query
+ * tokens per step, Eq. 2 each).  Drafted token t of a sequence sees the whole retained cache of each
+ * KV head (global region + ring) and the drafted tokens on its own path to the root, itself included.
+ * The cache is not changed; with n_draft = 1 this is tca_attn_decode of a token that was not appended.
+ *   q, O              DEVICE [batch, n_q_heads, n_draft, head_dim]
+ *   k_draft, v_draft  DEVICE [batch, n_kv_heads, n_draft, head_dim]
+ *   parent    DEVICE [batch, n_draft] int32: parent[t] < t, or -1 for a child of the context.  Any other
+ *             value counts as -1 (the range-checked build reports it).
+ *   n_live    DEVICE [batch] int32, optional: only drafted tokens t < n_live[s] exist; the rows of O of
+ *             the others are left as they were and their q, k, v are not used.  NULL: all n_draft.
+ *   ws        DEVICE workspace of tca_attn_tree_workspace_bytes(prm, n_draft) bytes, zeroed once after
+ *             allocating; word 0 is the sticky status word.  Calls that share one must not overlap.
+ * A drafted token outside a row's path does not influence it whatever it holds.  How the cache rows are
+ * dealt to CTAs follows from the device state words, so a captured call may be replayed after the cache
+ * has changed.  1 <= n_draft <= TCA_TREE_MAX, batch * n_kv_heads <= 65535, else TCA_ERR_UNSUPPORTED.
+ */
+int tca_attn_tree(const tca_params* prm, const void* q, const void* k_draft, const void* v_draft,
+                  int32_t n_draft, const int32_t* parent, const int32_t* n_live,
+                  const tca_cache_desc* cache, void* O, void* ws, size_t ws_bytes, void* stream);
+/* 0 for an invalid request. */
+size_t tca_attn_tree_workspace_bytes(const tca_params* prm, int32_t n_draft);
+
+/*
+ * The accepted path of a drafted tree becomes ordinary tokens of the cache: for every sequence s the
+ * call leaves the cache exactly as n_accept[s] calls of tca_cache_append would, with the rows
+ * path[s][0], path[s][1], ... of k_draft, v_draft and q_draft (compressions are scored with the queries
+ * of the token that filled the ring).
+ *   k_draft, v_draft, q_draft   as given to tca_attn_tree
+ *   path      DEVICE [batch, n_draft] int32: drafted indices in the order of their positions; an index
+ *             outside [0, n_draft) counts as the nearest one inside (the range-checked build reports it)
+ *   n_accept  HOST [batch], 0 <= n_accept[s] <= n_draft; a sequence with 0 is not touched
+ * TCA_ERR_CAPACITY if the global region of a unit would overflow; nothing has been changed then.
+ */
+int tca_cache_accept(const tca_params* prm, tca_cache_desc* cache, const void* k_draft,
+                     const void* v_draft, const void* q_draft, int32_t n_draft, const int32_t* path,
+                     const int32_t* n_accept, void* stream);
+
 /* Size of the scratch array built into the library image for tca_attn_decode_static. */
 #define TCA_DECODE_STATIC_SCRATCH_BYTES (16u << 20)
 
@@ -412,7 +493,7 @@ int tca_decode_static_status(void* stream);
  * checks record a failure in the reserved state word of the unit concerned.  This call synchronises
  * `stream`, reads the state words back and returns TCA_ERR_BOUNDS for the first unit whose word is
  * set, with detail[0] = unit, detail[1] = which check (1 selected index, 2 block count, 3 ring
- * slot, 4 cache row, 5 global region full), detail[2] = the offending value; detail HOST [3],
+ * slot, 4 cache row, 5 global region full, 6 drafted index), detail[2] = the offending value; detail HOST [3],
  * optional.  The checked kernels skip the access that failed its test, so no build touches memory
  * outside the buffers it was given.  tca_cache_init clears the words.
  */

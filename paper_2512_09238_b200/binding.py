@@ -26,7 +26,8 @@ TCA_FLAG_PREFILL_SIMT, TCA_FLAG_ENTROPY_INDEX, TCA_FLAG_RANDOM_ORDER, TCA_FLAG_F
 TCA_FLAG_PREFILL_BAND_FIRST = 16
 TCA_BUILD_DEBUG_BOUNDS = 1
 (TCA_OP_SCORE, TCA_OP_SELECT, TCA_OP_COMPACT, TCA_OP_PREFILL, TCA_OP_DECODE, TCA_OP_APPEND, TCA_OP_CALIB,
- TCA_OP_SCORE_SELECT) = range(8)
+ TCA_OP_SCORE_SELECT, TCA_OP_PACKED) = range(9)
+TCA_TREE_MAX = 128
 TCA_STATE_WORDS = 8
 
 EXPORTS = (
@@ -36,6 +37,7 @@ EXPORTS = (
     "tca_calib_colmean", "tca_calib_score", "tca_calib_choose", "tca_calib_candidates",
     "tca_decode_static_status", "tca_selftest_wait_expiry", "tca_score_select", "tca_build_info",
     "tca_cache_status", "tca_attn_prefill_gather", "tca_compact_kv_range",
+    "tca_attn_packed", "tca_cache_load", "tca_attn_tree", "tca_attn_tree_workspace_bytes", "tca_cache_accept",
 )
 
 
@@ -88,6 +90,12 @@ def load_library(path: str) -> C.CDLL:
     L.tca_attn_prefill.argtypes = [P, vp, vp, vp, i64, D, vp, vp, sz, vp]
     L.tca_attn_prefill_rows.argtypes = [P, vp, vp, vp, i64, i64, i64, D, vp, vp, sz, vp]
     L.tca_attn_prefill_gather.argtypes = [P, vp, vp, vp, i64, i64, i64, vp, vp, vp, vp, sz, vp]
+    L.tca_attn_packed.argtypes = [P, vp, vp, vp, i64, vp, vp, vp, vp, sz, vp]
+    L.tca_cache_load.argtypes = [P, vp, vp, i64, vp, vp, vp, C.c_int32, D, vp]
+    L.tca_attn_tree.argtypes = [P, vp, vp, vp, C.c_int32, vp, vp, D, vp, vp, sz, vp]
+    L.tca_attn_tree_workspace_bytes.restype = sz
+    L.tca_attn_tree_workspace_bytes.argtypes = [P, C.c_int32]
+    L.tca_cache_accept.argtypes = [P, D, vp, vp, vp, C.c_int32, vp, vp, vp]
     L.tca_calib_colmean.argtypes = [P, vp, vp, i64, vp, vp, sz, vp]
     L.tca_calib_score.argtypes = [P, vp, i64, vp, vp, vp, vp]
     L.tca_calib_choose.argtypes = [vp, vp, C.c_int, C.c_double]
@@ -101,7 +109,7 @@ def load_library(path: str) -> C.CDLL:
     L.tca_selftest_wait_expiry.argtypes = [vp, C.c_uint64, vp, vp]
     L.tca_build_info.argtypes = []
     for name in EXPORTS:
-        if name not in ("tca_strerror", "tca_workspace_bytes"):
+        if name not in ("tca_strerror", "tca_workspace_bytes", "tca_attn_tree_workspace_bytes"):
             getattr(L, name).restype = C.c_int
     return L
 
@@ -285,6 +293,94 @@ def tca_cache_append(prm, cache: "Cache", k_new, v_new, q_cur, stream=None) -> N
 
 def tca_ws_status(ws, stream=None) -> int:
     return lib().tca_ws_status(_dev(ws), _stream(stream))
+
+
+def _serving(prm, dtypes_and_shapes, where: str) -> None:
+    """Checks of the serving calls: every tensor on the current device, of the type and shape that prm and the
+    other arguments imply, with the last dimension contiguous.  Raises ValueError."""
+    here = torch.cuda.current_device() if torch.cuda.is_available() else None
+    for name, t, dtype, shape in dtypes_and_shapes:
+        if t is None:
+            continue
+        if not t.is_cuda or t.device.index != here:
+            raise ValueError(f"{where}: {name} must be a tensor on the current CUDA device")
+        if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+            raise ValueError(f"{where}: {name} must be {dtype} of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+        if t.numel() and t.stride(-1) != 1:
+            raise ValueError(f"{where}: the last dimension of {name} must be contiguous")
+
+
+def _elt(prm) -> torch.dtype:
+    return torch.bfloat16 if prm.dtype == TCA_BF16 else torch.float32
+
+
+def _strides(*tensors):
+    """HOST int64 {head, row} element strides of [heads, rows, d] views; a dimension of one element counts as
+    contiguous (torch leaves its stride unspecified)."""
+    out = []
+    for t in tensors:
+        heads, rows, d = t.shape
+        row = t.stride(1) if rows > 1 else d
+        out += [t.stride(0) if heads > 1 else max(rows, 1) * d, row]
+    return (C.c_int64 * len(out))(*out)
+
+
+def tca_attn_packed(prm, Q, K, V, rows, seq_start, O, ws, stream=None) -> None:
+    """Q, O [n_q_heads, rows, d], K, V [n_kv_heads, rows, d]: contiguous, or views with any head and row strides
+    that are multiples of 16 bytes (``x.transpose(0, 1)`` of a token-major tensor); seq_start a CUDA int64 tensor
+    of prm.batch + 1 elements."""
+    e, hq, hk, d = _elt(prm), prm.n_q_heads, prm.n_kv_heads, prm.head_dim
+    _serving(prm, (("Q", Q, e, (hq, rows, d)), ("K", K, e, (hk, rows, d)), ("V", V, e, (hk, rows, d)),
+                   ("O", O, e, (hq, rows, d)), ("seq_start", seq_start, torch.int64, (prm.batch + 1,)),
+                   ("ws", ws, torch.uint8, tuple(ws.shape))), "tca_attn_packed")
+    _check(lib().tca_attn_packed(C.byref(prm), Q.data_ptr(), K.data_ptr(), V.data_ptr(), rows, _dev(seq_start),
+                                 _strides(Q, K, V, O), O.data_ptr(), *_ws_args(ws), _stream(stream)), "tca_attn_packed")
+
+
+def tca_cache_load(prm, K, V, rows, seq_start, slots, cache: "Cache", stream=None) -> None:
+    """K, V [n_kv_heads, rows, d] as in tca_attn_packed; seq_start an int64 and slots an int32 numpy array (or None)."""
+    e, hk, d = _elt(prm), prm.n_kv_heads, prm.head_dim
+    _serving(prm, (("K", K, e, (hk, rows, d)), ("V", V, e, (hk, rows, d))), "tca_cache_load")
+    n_seq = len(seq_start) - 1
+    if slots is not None and len(slots) != n_seq:
+        raise ValueError("tca_cache_load: slots must have one entry per sequence")
+    _check(lib().tca_cache_load(C.byref(prm), K.data_ptr(), V.data_ptr(), rows, _strides(K, V),
+                                _host(seq_start, np.int64), _host(slots, np.int32), n_seq, C.byref(cache.desc),
+                                _stream(stream)), "tca_cache_load")
+
+
+def tca_attn_tree_workspace_bytes(prm, n_draft: int) -> int:
+    return int(lib().tca_attn_tree_workspace_bytes(C.byref(prm), n_draft))
+
+
+def alloc_tree_workspace(prm: tca_params, n_draft: int, device="cuda") -> torch.Tensor:
+    """A zero-filled workspace for tca_attn_tree calls of n_draft drafted tokens."""
+    n = tca_attn_tree_workspace_bytes(prm, n_draft)
+    if n == 0:
+        raise TcaError(TCA_ERR_INVALID_ARG, "tca_attn_tree_workspace_bytes")
+    return torch.zeros(n, dtype=torch.uint8, device=device)
+
+
+def tca_attn_tree(prm, q, k_draft, v_draft, n_draft, parent, n_live, cache: "Cache", O, ws, stream=None) -> None:
+    e, B, hq, hk, d = _elt(prm), prm.batch, prm.n_q_heads, prm.n_kv_heads, prm.head_dim
+    _serving(prm, (("q", q, e, (B, hq, n_draft, d)), ("k_draft", k_draft, e, (B, hk, n_draft, d)),
+                   ("v_draft", v_draft, e, (B, hk, n_draft, d)), ("O", O, e, (B, hq, n_draft, d)),
+                   ("parent", parent, torch.int32, (B, n_draft)), ("n_live", n_live, torch.int32, (B,)),
+                   ("ws", ws, torch.uint8, tuple(ws.shape))), "tca_attn_tree")
+    _check(lib().tca_attn_tree(C.byref(prm), _dev(q), _dev(k_draft), _dev(v_draft), n_draft, _dev(parent), _dev(n_live),
+                               C.byref(cache.desc), _dev(O), *_ws_args(ws), _stream(stream)), "tca_attn_tree")
+
+
+def tca_cache_accept(prm, cache: "Cache", k_draft, v_draft, q_draft, n_draft, path, n_accept, stream=None) -> None:
+    """path a CUDA int32 tensor [batch, n_draft]; n_accept an int32 numpy array of prm.batch elements."""
+    e, B, hq, hk, d = _elt(prm), prm.batch, prm.n_q_heads, prm.n_kv_heads, prm.head_dim
+    _serving(prm, (("k_draft", k_draft, e, (B, hk, n_draft, d)), ("v_draft", v_draft, e, (B, hk, n_draft, d)),
+                   ("q_draft", q_draft, e, (B, hq, n_draft, d)), ("path", path, torch.int32, (B, n_draft))),
+             "tca_cache_accept")
+    if len(n_accept) != B:
+        raise ValueError("tca_cache_accept: n_accept must have one entry per sequence")
+    _check(lib().tca_cache_accept(C.byref(prm), C.byref(cache.desc), _dev(k_draft), _dev(v_draft), _dev(q_draft), n_draft,
+                                  _dev(path), _host(n_accept, np.int32), _stream(stream)), "tca_cache_accept")
 
 
 # ----------------------------------------------------------------------------- cache descriptor holder

@@ -23,7 +23,7 @@ constexpr bool kDebugBounds = true;
 constexpr bool kDebugBounds = false;
 #endif
 enum { kBoundsSelectedIndex = 1, kBoundsBlockCount = 2, kBoundsRingSlot = 3, kBoundsCacheRow = 4,
-       kBoundsGlobalRegion = 5 };
+       kBoundsGlobalRegion = 5, kBoundsDraftIndex = 6 };
 constexpr int kMaxGroup = 8;    // query heads per KV head
 constexpr int kMaxBlock = 128;  // b
 

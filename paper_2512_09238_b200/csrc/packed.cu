@@ -1,0 +1,124 @@
+// tca_attn_packed: causal attention of prompts of different lengths packed one after another (Eq. 2
+// with every key retained), grouped query heads, strided buffers.  This file holds the entry point and
+// the FP32-pipe kernel (fp32 inputs; bf16 with TCA_FLAG_PREFILL_SIMT as a cross-check); bf16 runs on
+// the tensor-core kernel of packed_tc.cu.
+#include "flash_simt.cuh"
+#include "packed_common.cuh"
+
+namespace tca {
+
+namespace {
+
+// Query rows of a CTA are (position, head of the group) pairs, head fastest: row r is position
+// p0 + r / G, head kvh * G + r % G, so a short sequence of a wide group still fills the tile.
+template <typename T>
+struct PackedSrc {
+  const T *Q, *K, *V;
+  const PackedArgs* a;
+  PackedWork w;
+  int G;
+  __device__ __forceinline__ int n_rows() const { return min(kSimtRows / G, w.len - w.p0) * G; }
+  __device__ __forceinline__ int last_pos() const { return w.p0 + n_rows() / G - 1; }
+  __device__ __forceinline__ int n_tiles() const { return last_pos() / kSimtKeys + 1; }
+  __device__ __forceinline__ int keys(int t) const { return min(kSimtKeys, last_pos() + 1 - t * kSimtKeys); }
+  __device__ __forceinline__ const T* q(int r) const {
+    return Q + (w.kvh * G + r % G) * a->q.head + (w.row0 + w.p0 + r / G) * a->q.row;
+  }
+  __device__ __forceinline__ const T* k(int t, int r) const { return K + w.kvh * a->k.head + (w.row0 + t * kSimtKeys + r) * a->k.row; }
+  __device__ __forceinline__ const T* v(int t, int r) const { return V + w.kvh * a->v.head + (w.row0 + t * kSimtKeys + r) * a->v.row; }
+  __device__ __forceinline__ bool masked(int t) const { return (t + 1) * kSimtKeys - 1 > w.p0; }
+  __device__ __forceinline__ int last(int t, int r) const { return min(w.p0 + r / G, last_pos()) - t * kSimtKeys; }
+};
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kSimtThreads, 2)
+packed_simt_kernel(const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const __grid_constant__ PackedArgs args,
+                   float scale_log2e, T* __restrict__ O) {
+  extern __shared__ float4 packed_smem[];
+  __shared__ int found[3];
+  pdl_wait();
+  pdl_launch_dependents();
+  const int G = args.n_q_heads / args.n_kv_heads;
+  const int tile_pos = kSimtRows / G;
+  PackedSrc<T> src;
+  src.Q = Q; src.K = K; src.V = V; src.a = &args; src.G = G;
+  src.w.kvh = int(blockIdx.x) % args.n_kv_heads;
+  if (threadIdx.x < 32) {
+    int seq = -1, tile = 0;
+    if (!packed_find(args, int(blockIdx.x) / args.n_kv_heads, tile_pos, threadIdx.x, seq, tile)) seq = -1;
+    if (threadIdx.x == 0) { found[0] = seq; found[1] = tile; }
+  }
+  __syncthreads();
+  const int seq = found[0];
+  if (seq < 0) return;
+  packed_bounds(args, seq, src.w.row0, src.w.len);
+  src.w.p0 = found[1] * tile_pos;
+  float o[4][D / 16], m[4], l[4];
+  simt_flash<T, D>(src, scale_log2e, reinterpret_cast<float*>(packed_smem), o, m, l);
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = ty * 4 + i;
+    if (r >= src.n_rows()) continue;
+    T* out = O + (src.w.kvh * G + r % G) * args.o.head + (src.w.row0 + src.w.p0 + r / G) * args.o.row;
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) store_elt(out + tx * 4 + 64 * (c / 4) + c % 4, o[i][c] / l[i]);
+  }
+}
+
+template <typename T, int D>
+int launch_packed_simt(const tca_params* prm, const void* Q, const void* K, const void* V, const PackedArgs& a, void* O,
+                       cudaStream_t s) {
+  const int G = a.n_q_heads / a.n_kv_heads;
+  const int64_t n = packed_max_tiles(a.rows, a.n_seq, kSimtRows / G) * a.n_kv_heads;
+  if (n >= (int64_t(1) << 31)) return TCA_ERR_UNSUPPORTED;
+  auto kern = packed_simt_kernel<T, D>;
+  TCA_CHECK_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SimtSmem<D>::kBytes));
+  return launch_pdl(kern, dim3(unsigned(n)), dim3(kSimtThreads), size_t(SimtSmem<D>::kBytes), s,
+                    static_cast<const T*>(Q), static_cast<const T*>(K), static_cast<const T*>(V), a,
+                    prm->sm_scale * 1.4426950408889634f, static_cast<T*>(O));
+}
+
+// A buffer's strides: multiples of 16 bytes (vector loads, tensor maps), and room for a row.
+bool bad_view(const PackedView& v, const tca_params* prm) {
+  const int64_t unit = 16 / int64_t(elt_size(prm->dtype));
+  constexpr int64_t kMost = int64_t(1) << 36;   // elements: below the 2^40-byte limit of a tensor map's stride
+  return v.head < prm->head_dim || v.row < prm->head_dim || v.head % unit || v.row % unit || v.head >= kMost || v.row >= kMost;
+}
+
+}  // namespace
+}  // namespace tca
+
+using namespace tca;
+
+extern "C" int tca_attn_packed(const tca_params* prm, const void* Q, const void* K, const void* V, int64_t rows,
+                               const int64_t* seq_start, const int64_t* strides, void* O, void* ws, size_t ws_bytes,
+                               void* stream) {
+  int st = check_params(prm);
+  if (st != TCA_OK) return st;
+  TCA_CHECK_ARG(Q && K && V && seq_start && O && ws);
+  TCA_CHECK_ARG(rows >= 0 && rows < (int64_t(1) << 31));
+  TCA_CHECK_ARG(aligned(Q, 16) && aligned(K, 16) && aligned(V, 16) && aligned(O, 16) && aligned(ws, 256));
+  TCA_CHECK_ARG(aligned(seq_start, 8));
+  PackedArgs a;
+  PackedView* views[4] = {&a.q, &a.k, &a.v, &a.o};
+  for (int i = 0; i < 4; ++i) {
+    *views[i] = strides ? PackedView{strides[2 * i], strides[2 * i + 1]}
+                        : PackedView{(rows > 0 ? rows : 1) * prm->head_dim, int64_t(prm->head_dim)};
+    TCA_CHECK_ARG(!bad_view(*views[i], prm));
+  }
+  if (ws_bytes < tca_workspace_bytes(prm, rows > 0 ? rows : 1, TCA_OP_PACKED)) return TCA_ERR_WORKSPACE;
+  if (rows == 0) return TCA_OK;   // nothing to compute
+  a.rows = rows;
+  a.seq_start = seq_start;
+  a.n_seq = prm->batch;
+  a.n_q_heads = prm->n_q_heads;
+  a.n_kv_heads = prm->n_kv_heads;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (prm->dtype == TCA_F32) {
+    if (prm->head_dim == 128) return launch_packed_simt<float, 128>(prm, Q, K, V, a, O, s);
+    return launch_packed_simt<float, 64>(prm, Q, K, V, a, O, s);
+  }
+  if (prm->head_dim == 128) return launch_packed_simt<__nv_bfloat16, 128>(prm, Q, K, V, a, O, s);
+  return launch_packed_simt<__nv_bfloat16, 64>(prm, Q, K, V, a, O, s);
+}

@@ -1,0 +1,270 @@
+// tca_attn_tree: attention of a tree of drafted tokens over the retained cache (Eq. 2 for several query
+// tokens at once, speculative decoding).  Query (head, t) sees every row of its unit's cache and the
+// drafted tokens on its own path to the root.
+//
+// Two parts.  The cache is the same for all G * T query rows of a unit, so its rows are cut into slices
+// and a split kernel attends a block of query rows to one slice (this file: FP32 pipes; tree_tc.cu: tensor
+// cores).  A drafted token sees a handful of drafted tokens, so that part is no product of matrices:
+// the combine kernel, one warp per query row, walks the path to the root, attends to exactly the tokens
+// on it (a drafted token outside the path is not read, whatever it holds) and merges the slices in order.
+#include "flash_simt.cuh"
+#include "tree_common.cuh"
+
+namespace tca {
+
+TreePlan tree_plan(const tca_params* prm, int n_draft) {
+  TreePlan p;
+  const int U = prm->batch * prm->n_kv_heads;
+  p.rows = prm->n_q_heads / prm->n_kv_heads * n_draft;
+  p.row_blocks = (p.rows + kSimtRows - 1) / kSimtRows;
+  p.streams = 1;
+  // one wave of resident CTAs; with more units than slices fit that wave, two slices per unit and a
+  // wave on top, so that units of different lengths still balance
+  const int wave = 2 * sm_count() / p.row_blocks > 0 ? 2 * sm_count() / p.row_blocks : 1;
+  p.n_slots = wave >= 2 * U ? wave : wave + 2 * U;
+  return p;
+}
+
+namespace {
+
+constexpr int kStepRows = 128;    // cache rows are dealt to slices in steps of this
+constexpr int kMinSteps = 1;
+
+template <typename T, int D>
+struct TreeSrc {
+  const T *q_rows, *Kc, *Vc;      // first query row of this CTA; the cache
+  int n;                          // query rows here
+  SliceTiles tiles;
+  __device__ __forceinline__ int n_rows() const { return n; }
+  __device__ __forceinline__ int n_tiles() const { return tiles.n_tiles(); }
+  __device__ __forceinline__ int keys(int t) const { int y, c; tiles.get(t, y, c); return c; }
+  __device__ __forceinline__ const T* q(int r) const { return q_rows + int64_t(r) * D; }
+  __device__ __forceinline__ const T* k(int t, int r) const { int y, c; tiles.get(t, y, c); return Kc + int64_t(y + r) * D; }
+  __device__ __forceinline__ const T* v(int t, int r) const { int y, c; tiles.get(t, y, c); return Vc + int64_t(y + r) * D; }
+  __device__ __forceinline__ bool masked(int t) const { return keys(t) < kSimtKeys; }
+  __device__ __forceinline__ int last(int t, int) const { return keys(t) - 1; }
+};
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kSimtThreads, 2)
+tree_simt_kernel(const T* __restrict__ q, const T* __restrict__ Kc, const T* __restrict__ Vc,
+                 const int64_t* __restrict__ state, int n_units, int64_t tail_cap, TreePlan plan, float scale_log2e,
+                 TreeWs ws) {
+  extern __shared__ float4 tree_smem[];
+  __shared__ TreeSlice slice;
+  pdl_wait();
+  pdl_launch_dependents();
+  if (threadIdx.x < 32) {
+    const TreeSlice s = tree_find(state, n_units, tail_cap, plan.n_slots, kStepRows, kMinSteps, kSimtKeys,
+                                  int(blockIdx.x) / plan.row_blocks, threadIdx.x);
+    if (threadIdx.x == 0) slice = s;
+  }
+  __syncthreads();
+  if (slice.u < 0) return;
+  const int rb = int(blockIdx.x) % plan.row_blocks;
+  const int slot = slice.base + slice.part;
+  if (slice.part == 0 && rb == 0 && threadIdx.x == 0) ws.table[slice.u] = make_int2(slice.base, slice.np);
+  const int row0 = rb * kSimtRows;
+  TreeSrc<T, D> src;
+  src.n = min(kSimtRows, plan.rows - row0);
+  src.q_rows = q + (int64_t(slice.u) * plan.rows + row0) * D;
+  src.Kc = Kc;
+  src.Vc = Vc;
+  src.tiles = slice.tiles;
+  float o[4][D / 16], m[4], l[4];
+  simt_flash<T, D>(src, scale_log2e, reinterpret_cast<float*>(tree_smem), o, m, l);
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = row0 + ty * 4 + i;
+    if (r >= plan.rows) continue;
+    const size_t at = size_t(slot) * plan.rows + r;
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c)
+      *reinterpret_cast<float4*>(ws.acc + at * D + tx * 4 + 64 * c) =
+          make_float4(o[i][c * 4], o[i][c * 4 + 1], o[i][c * 4 + 2], o[i][c * 4 + 3]);
+    if (tx == 0) ws.ml[at] = make_float2(m[i], l[i]);
+  }
+}
+
+// ------------------------------------------------------------------ drafted tokens, and the merge of the slices
+constexpr int kCombineWarps = 8;
+
+template <int E>
+struct RowE {   // E = D / 32 consecutive elements per lane
+  float x[E];
+  __device__ __forceinline__ void load(const float* p) {
+    if constexpr (E == 4) { const float4 v = *reinterpret_cast<const float4*>(p); x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w; }
+    else { const float2 v = *reinterpret_cast<const float2*>(p); x[0] = v.x; x[1] = v.y; }
+  }
+  __device__ __forceinline__ void load(const __nv_bfloat16* p) {
+    if constexpr (E == 4) {
+      const uint2 v = *reinterpret_cast<const uint2*>(p);
+      x[0] = bf16_lo(v.x); x[1] = bf16_hi(v.x); x[2] = bf16_lo(v.y); x[3] = bf16_hi(v.y);
+    } else {
+      const uint32_t v = *reinterpret_cast<const uint32_t*>(p);
+      x[0] = bf16_lo(v); x[1] = bf16_hi(v);
+    }
+  }
+  __device__ __forceinline__ void store(float* p) const {
+    if constexpr (E == 4) *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+    else *reinterpret_cast<float2*>(p) = make_float2(x[0], x[1]);
+  }
+  __device__ __forceinline__ void store(__nv_bfloat16* p) const {
+#pragma unroll
+    for (int e = 0; e < E; e += 2)
+      *reinterpret_cast<__nv_bfloat162*>(p + e) = __floats2bfloat162_rn(x[e], x[e + 1]);
+  }
+};
+
+// Running softmax of one query row held by a warp: maximum and sum uniform, E outputs per lane.
+template <int E>
+struct RowState {
+  float m = -INFINITY, l = 0.f;
+  float o[E];
+  __device__ __forceinline__ RowState() {
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = 0.f;
+  }
+  // adds (l2, a) accumulated under the maximum m2
+  __device__ __forceinline__ void add(float m2, float l2, const RowE<E>& a) {
+    const float mn = fmaxf(m, m2), base = (mn == -INFINITY) ? 0.f : mn;
+    const float c = exp2f(m - base), w = exp2f(m2 - base);
+    l = fmaf(l, c, l2 * w);
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = fmaf(o[e], c, a.x[e] * w);
+    m = mn;
+  }
+};
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kCombineWarps * 32)
+tree_combine_kernel(const T* __restrict__ q, const T* __restrict__ k_draft, const T* __restrict__ v_draft, int n_draft,
+                    const int32_t* __restrict__ parent, const int32_t* __restrict__ n_live,
+                    const int64_t* __restrict__ state, int n_kv, TreePlan plan, float scale_log2e, TreeWs ws,
+                    T* __restrict__ O) {
+  constexpr int E = D / 32;
+  constexpr int kHeld = TCA_TREE_MAX / 32;
+  pdl_wait();
+  pdl_launch_dependents();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int r = blockIdx.x * kCombineWarps + warp, u = blockIdx.y, seq = u / n_kv;
+  if (r >= plan.rows) return;
+  const int t = r % n_draft;
+  if (n_live && t >= n_live[seq]) return;                   // not drafted: its row of O stays as it was
+  RowE<E> qr;
+  const size_t q_at = (size_t(u) * plan.rows + r) * D + lane * E;
+  qr.load(q + q_at);
+  // the path to the root as a bit set: parents lie in the lanes, a hop is one shuffle
+  int par[kHeld];
+  unsigned bits[kHeld];
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) {
+    par[i] = i * 32 + lane < n_draft ? parent[size_t(seq) * n_draft + i * 32 + lane] : -1;
+    bits[i] = 0;
+  }
+  for (int cur = t; cur >= 0;) {
+    int p = -1;
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i)
+      if (i == (cur >> 5)) {
+        bits[i] |= 1u << (cur & 31);
+        p = par[i];
+      }
+    p = __shfl_sync(0xffffffffu, p, cur & 31);
+    if constexpr (kDebugBounds) {
+      if (lane == 0 && (p < -1 || p >= cur)) report_bounds_ws(ws.status, kBoundsDraftIndex, p);
+    }
+    cur = p < cur ? p : -1;                                  // a parent that does not precede its child ends the path
+  }
+  RowState<E> row;
+  const T* kd = k_draft + size_t(u) * n_draft * D + lane * E;
+  const T* vd = v_draft + size_t(u) * n_draft * D + lane * E;
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i)
+    while (bits[i]) {
+      const int a = i * 32 + __ffs(bits[i]) - 1;
+      bits[i] &= bits[i] - 1;
+      RowE<E> k, v;
+      k.load(kd + size_t(a) * D);
+      v.load(vd + size_t(a) * D);
+      float x = 0.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) x = fmaf(qr.x[e], k.x[e], x);
+#pragma unroll
+      for (int off = 16; off > 0; off >>= 1) x += __shfl_xor_sync(0xffffffffu, x, off);
+      row.add(x * scale_log2e, 1.f, v);
+    }
+  // the slices of the unit, in order; a unit whose cache is empty has none
+  const int64_t* st = state + size_t(u) * TCA_STATE_WORDS;
+  const int2 where = st[TCA_ST_N_GLOBAL] + st[TCA_ST_N_TAIL] > 0 ? ws.table[u] : make_int2(0, 0);
+  const int n = where.y * plan.streams;
+  const size_t first = size_t(where.x) * plan.streams;
+#pragma unroll 4
+  for (int c = 0; c < n; ++c) {
+    const size_t at = (first + c) * plan.rows + r;
+    const float2 ml = ws.ml[at];
+    RowE<E> a;
+    a.load(ws.acc + at * D + lane * E);
+    if (ml.x != -INFINITY) row.add(ml.x, ml.y, a);           // a stream without a tile wrote no output
+  }
+  RowE<E> out;
+#pragma unroll
+  for (int e = 0; e < E; ++e) out.x[e] = row.o[e] / row.l;
+  out.store(O + q_at);
+}
+
+template <typename T, int D>
+int launch_tree(const tca_params* prm, const void* q, const void* kd, const void* vd, int n_draft, const int32_t* parent,
+                const int32_t* n_live, const tca_cache_desc* c, void* O, const TreePlan& plan, const TreeWs& ws,
+                cudaStream_t s) {
+  const int U = prm->batch * prm->n_kv_heads;
+  const float scale = prm->sm_scale * 1.4426950408889634f;
+  auto kern = tree_simt_kernel<T, D>;
+  TCA_CHECK_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SimtSmem<D>::kBytes));
+  const int64_t ctas = int64_t(plan.n_slots) * plan.row_blocks;
+  if (ctas >= (int64_t(1) << 31)) return TCA_ERR_UNSUPPORTED;
+  int st = launch_pdl(kern, dim3(unsigned(ctas)), dim3(kSimtThreads), size_t(SimtSmem<D>::kBytes), s,
+                      static_cast<const T*>(q), static_cast<const T*>(c->k), static_cast<const T*>(c->v),
+                      static_cast<const int64_t*>(c->state), U, c->tail_cap, plan, scale, ws);
+  if (st != TCA_OK) return st;
+  return launch_pdl(tree_combine_kernel<T, D>, dim3(unsigned((plan.rows + kCombineWarps - 1) / kCombineWarps), unsigned(U)),
+                    dim3(kCombineWarps * 32), size_t(0), s, static_cast<const T*>(q), static_cast<const T*>(kd),
+                    static_cast<const T*>(vd), n_draft, parent, n_live, static_cast<const int64_t*>(c->state),
+                    prm->n_kv_heads, plan, scale, ws, static_cast<T*>(O));
+}
+
+bool bad_tree_shape(const tca_params* prm, int32_t n_draft) {
+  return n_draft > TCA_TREE_MAX || int64_t(prm->batch) * prm->n_kv_heads > 65535;
+}
+
+}  // namespace
+}  // namespace tca
+
+using namespace tca;
+
+extern "C" size_t tca_attn_tree_workspace_bytes(const tca_params* prm, int32_t n_draft) {
+  if (check_params(prm) != TCA_OK || n_draft < 1 || bad_tree_shape(prm, n_draft)) return 0;
+  return tree_ws_layout(prm, tree_plan(prm, n_draft), nullptr).bytes;
+}
+
+extern "C" int tca_attn_tree(const tca_params* prm, const void* q, const void* k_draft, const void* v_draft,
+                             int32_t n_draft, const int32_t* parent, const int32_t* n_live, const tca_cache_desc* c,
+                             void* O, void* ws, size_t ws_bytes, void* stream) {
+  int st = check_params(prm);
+  if (st != TCA_OK) return st;
+  TCA_CHECK_ARG(q && k_draft && v_draft && parent && c && O && ws && n_draft >= 1);
+  TCA_CHECK_ARG(c->k && c->v && c->state);
+  TCA_CHECK_ARG(aligned(q, 16) && aligned(k_draft, 16) && aligned(v_draft, 16) && aligned(O, 16) && aligned(ws, 256));
+  TCA_CHECK_ARG(aligned(c->k, 16) && aligned(c->v, 16) && aligned(parent, 4) && aligned(n_live, 4));
+  TCA_CHECK_ARG(c->n_units == int64_t(prm->batch) * prm->n_kv_heads && c->tail_cap >= 1);
+  if (bad_tree_shape(prm, n_draft)) return TCA_ERR_UNSUPPORTED;
+  const TreePlan plan = tree_plan(prm, n_draft);
+  const TreeWs lay = tree_ws_layout(prm, plan, ws);
+  if (ws_bytes < lay.bytes) return TCA_ERR_WORKSPACE;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+#define TCA_TREE(T, D) launch_tree<T, D>(prm, q, k_draft, v_draft, n_draft, parent, n_live, c, O, plan, lay, s)
+  if (prm->dtype == TCA_F32) return prm->head_dim == 128 ? TCA_TREE(float, 128) : TCA_TREE(float, 64);
+  return prm->head_dim == 128 ? TCA_TREE(__nv_bfloat16, 128) : TCA_TREE(__nv_bfloat16, 64);
+#undef TCA_TREE
+}

@@ -1,0 +1,241 @@
+"""tca_attn_packed and tca_cache_load against the oracle: sizes, layouts, masked garbage, replays."""
+import numpy as np
+import pytest
+import torch
+
+import serving_harness as H
+from oracle import serving_oracle as S
+from paper_2512_09238_b200 import binding as B
+
+pytestmark = pytest.mark.gpu
+
+LENS = {
+    "one": [1], "empty_between": [0, 1, 0, 5, 0], "tile_edges": [127, 128, 129, 63, 64, 65],
+    "ragged": [300, 1, 33, 0, 511], "many": [3, 17, 0, 40, 1, 1, 96, 2] * 6,
+}
+
+
+def case(lens, hq, hkv, d, dtype, layout, seed, lead=3, trail=4):
+    starts = lead + np.concatenate([[0], np.cumsum(lens)])
+    rows = int(starts[-1]) + trail
+    mk = lambda i, h: H.packed_buffer(seed + i, h, rows, d, dtype, layout)  # noqa: E731
+    return H.params(len(lens), hq, hkv, d, dtype), mk(0, hq), mk(1, hkv), mk(2, hkv), starts
+
+
+def compare(prm, q, k, v, starts, o, dtype):
+    want, a, s = S.packed_attention(H.f64(q), H.f64(k), H.f64(v), starts, H.scale_of(prm.head_dim))
+    n = np.full(want.shape[:2], max(1, int(np.max(np.diff(starts)))))
+    H.check(H.f64(o), want, S.attention_tolerance(want, a, s, prm.head_dim, n, dtype), "packed")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("name", list(LENS))
+def test_lengths(name, d, dtype):
+    prm, q, k, v, starts = case(LENS[name], 4, 2, d, dtype, "heads", 10)
+    compare(prm, q, k, v, starts, H.run_packed(prm, q, k, v, starts), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("group", [1, 2, 3, 4, 5, 6, 7, 8])
+def test_groups(group, dtype):
+    prm, q, k, v, starts = case([70, 5, 260], 2 * group, 2, 128, dtype, "heads", 20)
+    compare(prm, q, k, v, starts, H.run_packed(prm, q, k, v, starts), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("layout", ["tokens", "fused"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_layouts(layout, d, dtype):
+    prm, q, k, v, starts = case([200, 31, 1], 6, 3, d, dtype, layout, 30)
+    o = H.run_packed(prm, q, k, v, starts, out=torch.full_like(q, float("nan")))
+    compare(prm, q, k, v, starts, o, dtype)
+    # the layout does not change a bit of the result
+    c = [x.contiguous() for x in (q, k, v)]
+    o2 = H.run_packed(prm, *c, starts)
+    assert torch.equal(o.nan_to_num(7.0), o2.nan_to_num(7.0))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_rows_a_query_does_not_see_have_no_influence(bad, dtype):
+    """A sequence's result is the same whatever its neighbours hold, and a row's whatever its later rows hold."""
+    prm, q, k, v, starts = case([150, 77, 140], 4, 2, 128, dtype, "heads", 40)
+    clean = H.f64(H.run_packed(prm, q, k, v, starts))
+    cut = int(starts[1]) + 30                               # row 30 of the second sequence and all behind it
+    for x in (k, v):
+        x[:, cut:] = bad
+        x[:, :int(starts[1]) - 1] = bad                      # all of the first sequence but its last row
+        x[:, int(starts[0]) - 1] = bad
+    got = H.f64(H.run_packed(prm, q, k, v, starts))
+    lo = int(starts[1])
+    assert np.array_equal(got[:, lo:cut], clean[:, lo:cut])
+    # only values, not keys: the rows that do see the bad value show it
+    prm, q, k, v, starts = case([150, 77, 140], 4, 2, 128, dtype, "heads", 41)
+    clean = H.f64(H.run_packed(prm, q, k, v, starts))
+    v[1, cut, 5] = bad
+    got = H.f64(H.run_packed(prm, q, k, v, starts))
+    same = np.ones_like(got, dtype=bool)
+    same[2:, cut:int(starts[2]), 5] = False
+    assert np.array_equal(got[same], clean[same], equal_nan=True)
+    hit = got[2:, cut:int(starts[2]), 5]
+    assert np.isnan(hit).all() if np.isnan(bad) else (hit == bad).all()
+
+
+def test_large_scores_and_the_lowest_value():
+    """Scores of thousands, and keys at the type's lowest finite value, stay finite."""
+    prm, q, k, v, starts = case([90, 200], 4, 2, 64, "bf16", "heads", 50)
+    q *= 40
+    compare(prm, q, k, v, starts, H.run_packed(prm, q, k, v, starts), "bf16")
+    k[:, 40:60] = torch.finfo(torch.bfloat16).min
+    q[:] = q.abs().clamp(max=1.0)                            # scores of -1e38 or so: weight zero next to any other key
+    out = H.f64(H.run_packed(prm, q, k, v, starts))
+    assert np.isfinite(out[:, starts[0]:starts[-1]]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_two_runs_and_another_stream_agree_bit_for_bit(dtype):
+    prm, q, k, v, starts = case([513, 64, 300], 8, 2, 128, dtype, "heads", 60)
+    a = H.run_packed(prm, q, k, v, starts)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        b = H.run_packed(prm, q, k, v, starts)
+    torch.cuda.synchronize()
+    assert torch.equal(a.nan_to_num(3.0), b.nan_to_num(3.0))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_captured_call_replays_with_other_lengths(dtype):
+    prm, q, k, v, starts = case([100, 50, 250], 4, 2, 128, dtype, "heads", 70)
+    st = torch.tensor(starts, dtype=torch.int64, device="cuda")
+    ws = B.alloc_workspace(prm, q.shape[1], B.TCA_OP_PACKED)
+    o = torch.full_like(q, float("nan"))
+    B.tca_attn_packed(prm, q, k, v, q.shape[1], st, o, ws)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        B.tca_attn_packed(prm, q, k, v, q.shape[1], st, o, ws)
+    for other in ([3, 3, 203, 403], [0, 399, 400, 407], [5, 5, 5, 5], list(starts)):
+        o.fill_(float("nan"))
+        st.copy_(torch.tensor(other, dtype=torch.int64))
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(o.nan_to_num(3.0), H.run_packed(prm, q, k, v, other).nan_to_num(3.0))
+
+
+def test_offsets_outside_the_buffers_are_clamped():
+    prm, q, k, v, _ = case([40, 60], 4, 2, 128, "bf16", "heads", 80)
+    rows = q.shape[1]
+    a = H.run_packed(prm, q, k, v, [-7, 40, rows + 1000])
+    b = H.run_packed(prm, q, k, v, [0, 40, rows])
+    assert torch.equal(a.nan_to_num(3.0), b.nan_to_num(3.0))
+    c = H.run_packed(prm, q, k, v, [50, 20, 10])             # descending: empty sequences
+    assert torch.isnan(c).all()
+
+
+def test_long_rows_sampled():
+    """One long prompt: sampled rows against the oracle (a full fp64 pass would take minutes)."""
+    L, hq, hkv, d = 20000, 4, 1, 128
+    prm = H.params(2, hq, hkv, d, "bf16")
+    q, k, v = (H.packed_buffer(90 + i, h, L + 10, d, "bf16", "heads") for i, h in enumerate((hq, hkv, hkv)))
+    o = H.f64(H.run_packed(prm, q, k, v, [0, 10, L + 10]))
+    kd, vd, qd = H.f64(k), H.f64(v), H.f64(q)
+    for i in (0, 1, 127, 128, 4096, 12345, L - 2, L - 1):
+        for h in (0, 3):
+            vis = np.ones((1, i + 1), dtype=bool)
+            want, a, s = S.masked_attention(qd[h, 10 + i][None], kd[0, 10:11 + i], vd[0, 10:11 + i], vis, H.scale_of(d))
+            H.check(o[h, 10 + i][None], want, S.attention_tolerance(want, a, s, d, np.array([i + 1]), "bf16"), f"row {i}")
+
+
+def test_tensor_cores_agree_with_the_fp32_pipes():
+    prm, q, k, v, starts = case([700, 130, 9], 8, 2, 128, "bf16", "tokens", 100)
+    a = H.f64(H.run_packed(prm, q, k, v, starts))
+    prm2 = H.params(3, 8, 2, 128, "bf16", flags=B.TCA_FLAG_PREFILL_SIMT)
+    b = H.f64(H.run_packed(prm2, q, k, v, starts))
+    want, aa, s = S.packed_attention(H.f64(q), H.f64(k), H.f64(v), starts, H.scale_of(128))
+    tol = 2 * S.attention_tolerance(want, aa, s, 128, np.full(want.shape[:2], 700), "bf16")
+    H.check(a, b, tol, "tensor cores against FP32 pipes")
+
+
+# ------------------------------------------------------------------ tca_cache_load
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("layout", ["heads", "tokens", "fused"])
+def test_load_places_every_row(layout, d, dtype):
+    lens, slots, hkv = [100, 0, 97, 1, 400], np.array([4, 0, 2, 6, 5], dtype=np.int32), 3
+    prm = H.params(7, 2 * hkv, hkv, d, dtype, block=32, window=64)
+    starts = 2 + np.concatenate([[0], np.cumsum(lens)]).astype(np.int64)
+    k, v = (H.packed_buffer(i, hkv, int(starts[-1]) + 3, d, dtype, layout) for i in (1, 2))
+    cache = H.make_cache(prm, 10, 50, 7, 60, dtype, 5, extra_cap=400)
+    before = H.clone_cache(prm, cache)
+    B.tca_cache_load(prm, k, v, k.shape[1], starts, slots, cache)
+    torch.cuda.synchronize()
+    H.mirror_equals_device(cache)
+    want = {n: getattr(before, n).clone() for n in ("k", "v", "pos")}
+    for i, n in enumerate(lens):
+        g, t = S.load_split(n, prm.window, prm.block)
+        for h in range(hkv):
+            u = int(slots[i]) * hkv + h
+            assert (cache.n_global[u], cache.n_tail[u], cache.tail_head[u], cache.seq_len[u]) == (g, t, 0, n)
+            rows = torch.from_numpy(cache.unit_rows(u)).cuda()
+            src = slice(int(starts[i]), int(starts[i]) + n)
+            want["k"][rows], want["v"][rows] = k[h, src], v[h, src]
+            want["pos"][rows] = torch.arange(n, dtype=torch.int32, device="cuda")
+    for n in ("k", "v", "pos"):
+        assert torch.equal(getattr(cache, n), want[n]), n    # sequences 1 and 3 and all unused rows as they were
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_load_equals_compaction_of_everything(dtype):
+    L, hkv, d, batch = 333, 2, 128, 2
+    prm = H.params(batch, 4, hkv, d, dtype, block=32, window=64)
+    k, v = (H.randn(i, (batch, hkv, L, d), dtype) for i in (1, 2))
+    g, t = S.load_split(L, 64, 32)
+    cap = np.full(batch * hkv, g, dtype=np.int64)
+    a, b = (B.Cache(prm, cap, 96, np.full(batch * hkv, 4, dtype=np.int64)) for _ in range(2))
+    offs = np.arange(batch * hkv + 1, dtype=np.int64) * g
+    idx = torch.arange(g, dtype=torch.int32, device="cuda").repeat(batch * hkv)
+    B.tca_compact_kv(prm, k, v, L, idx, torch.from_numpy(offs).cuda(), offs, a)
+    pk, pv = (x.transpose(0, 1).reshape(hkv, batch * L, d).contiguous() for x in (k, v))
+    B.tca_cache_load(prm, pk, pv, batch * L, np.arange(batch + 1, dtype=np.int64) * L, None, b)
+    torch.cuda.synchronize()
+    for n in ("k", "v", "pos", "state"):
+        assert torch.equal(getattr(a, n), getattr(b, n)), n
+    H.mirror_equals_device(b)
+
+
+def test_load_of_more_sequences_than_one_launch_takes():
+    batch, d = 250, 64
+    prm = H.params(batch, 1, 1, d, "bf16", block=16, window=8)
+    lens = np.arange(batch) % 37
+    starts = np.concatenate([[0], np.cumsum(lens)]).astype(np.int64)
+    k, v = (H.randn(i, (1, int(starts[-1]), d), "bf16") for i in (1, 2))
+    cache = B.Cache(prm, np.full(batch, 32, dtype=np.int64), 24, np.ones(batch, dtype=np.int64))
+    slots = np.random.default_rng(0).permutation(batch).astype(np.int32)
+    B.tca_cache_load(prm, k, v, int(starts[-1]), starts, slots, cache)
+    torch.cuda.synchronize()
+    H.mirror_equals_device(cache)
+    for i in range(batch):
+        rows = torch.from_numpy(cache.unit_rows(int(slots[i]))).cuda()
+        assert torch.equal(cache.k[rows], k[0, starts[i]:starts[i + 1]]) and torch.equal(cache.v[rows], v[0, starts[i]:starts[i + 1]])
+
+
+def test_load_refuses_without_touching_anything():
+    prm = H.params(3, 2, 1, 64, "bf16", block=32, window=64)
+    k = H.randn(1, (1, 500, 64), "bf16")
+    cache = H.make_cache(prm, 10, 5, 0, 15, "bf16", 5, extra_cap=90)
+    before = H.clone_cache(prm, cache)
+    i64, i32 = (lambda *x: np.array(x, dtype=np.int64)), (lambda *x: np.array(x, dtype=np.int32))
+    for starts, slots, status in (
+            (i64(0, 10, 20), i32(1, 1), B.TCA_ERR_INVALID_ARG), (i64(0, 10, 20), i32(0, 3), B.TCA_ERR_INVALID_ARG),
+            (i64(0, 10, 501), i32(0, 1), B.TCA_ERR_INVALID_ARG), (i64(10, 5), None, B.TCA_ERR_INVALID_ARG),
+            (i64(-1, 5), None, B.TCA_ERR_INVALID_ARG), (i64(0, 1, 2, 3, 4), None, B.TCA_ERR_INVALID_ARG),
+            (i64(0, 10, 210), i32(0, 1), B.TCA_ERR_CAPACITY)):
+        with pytest.raises(B.TcaError) as e:
+            B.tca_cache_load(prm, k, k, 500, starts, slots, cache)
+        assert e.value.status == status
+    torch.cuda.synchronize()
+    for n in ("k", "v", "pos", "state"):
+        assert torch.equal(getattr(cache, n), getattr(before, n))
+    H.mirror_equals_device(cache)

@@ -1,0 +1,258 @@
+"""tca_attn_tree and tca_cache_accept against the oracle and against one append per token."""
+import numpy as np
+import pytest
+import torch
+
+import serving_harness as H
+from paper_2512_09238_b200 import binding as B
+
+pytestmark = pytest.mark.gpu
+
+
+def drafts(prm, T, dtype, seed):
+    b, d = prm.batch, prm.head_dim
+    return (H.randn(seed, (b, prm.n_q_heads, T, d), dtype, 1.5), H.randn(seed + 1, (b, prm.n_kv_heads, T, d), dtype),
+            H.randn(seed + 2, (b, prm.n_kv_heads, T, d), dtype))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("T", [1, 2, 5, 16, 33, 64, 127, 128])
+def test_drafted_counts(T, d, dtype):
+    prm = H.params(2, 4, 2, d, dtype)
+    cache = H.make_cache(prm, [300, 0, 17, 128], [70, 95, 1, 64], [90, 3, 50, 0], 500, dtype, 1)   # the first ring wraps
+    q, kd, vd = drafts(prm, T, dtype, 10)
+    parent = np.stack([H.chain(T), H.bush(T, 3)])
+    H.check_tree(prm, q, kd, vd, parent, cache, H.run_tree(prm, q, kd, vd, parent, cache), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("group", [1, 2, 3, 4, 5, 6, 7, 8])
+def test_groups(group, dtype):
+    prm = H.params(1, 2 * group, 2, 128, dtype)
+    cache = H.make_cache(prm, [260, 40], [90, 20], [30, 90], 400, dtype, 2)
+    q, kd, vd = drafts(prm, 37, dtype, 20)
+    parent = H.bush(37, 5)[None]
+    H.check_tree(prm, q, kd, vd, parent, cache, H.run_tree(prm, q, kd, vd, parent, cache), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_empty_caches_and_live_counts(dtype):
+    """Units without a row (all, and some), and sequences that drafted fewer tokens or none."""
+    prm = H.params(3, 4, 2, 128, dtype)
+    T, live = 9, np.array([9, 0, 4])
+    q, kd, vd = drafts(prm, T, dtype, 30)
+    parent = np.stack([H.bush(T, i) for i in range(3)])
+    for n_global, n_tail in ((0, 0), ([0, 5, 0, 0, 400, 0], [0, 0, 0, 3, 96, 0])):
+        cache = H.make_cache(prm, n_global, n_tail, 0, 500, dtype, 3, tail_cap=97)
+        for x in (q, kd, vd):                                # what is not drafted is not used
+            x[1], x[2, :, 4:] = float("nan"), float("nan")
+        H.check_tree(prm, q, kd, vd, parent, cache, H.run_tree(prm, q, kd, vd, parent, cache, n_live=live), dtype, n_live=live)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_more_units_than_registers_hold_and_uneven_ones(dtype):
+    """150 units (more than are kept in registers), lengths from 0 to 700."""
+    prm = H.params(50, 3, 3, 64, dtype)
+    r = np.random.default_rng(4)
+    ng, nt = r.integers(0, 600, 150), r.integers(0, 96, 150)
+    ng[::7], nt[::7] = 0, 0
+    cache = H.make_cache(prm, ng, nt, r.integers(0, 96, 150), 800, dtype, 6)
+    q, kd, vd = drafts(prm, 3, dtype, 40)
+    parent = np.tile(H.chain(3), (50, 1))
+    H.check_tree(prm, q, kd, vd, parent, cache, H.run_tree(prm, q, kd, vd, parent, cache), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_long_cache(dtype):
+    prm = H.params(1, 8, 2, 128, dtype, block=128, window=1024)
+    cache = H.make_cache(prm, [9000, 2500], [1100, 1024], [1000, 0], 40000, dtype, 7)
+    q, kd, vd = drafts(prm, 24, dtype, 50)
+    parent = H.bush(24, 9)[None]
+    got = H.run_tree(prm, q, kd, vd, parent, cache)
+    H.check_tree(prm, q, kd, vd, parent, cache, got, dtype, heads=(0, 5))
+    assert torch.equal(got, H.run_tree(prm, q, kd, vd, parent, cache))            # the same bits every time
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        again = H.run_tree(prm, q, kd, vd, parent, cache)
+    torch.cuda.synchronize()
+    assert torch.equal(got, again)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_what_a_row_does_not_see_has_no_influence(bad, dtype):
+    """Other branches, cache rows not in use, and the other sequence's cache may hold anything."""
+    prm = H.params(2, 4, 2, 128, dtype)
+    cache = H.make_cache(prm, [70, 300, 129, 1], [90, 30, 96, 20], [50, 0, 20, 90], 500, dtype, 8, extra_cap=40, tail_cap=97)
+    T = 12
+    q, kd, vd = drafts(prm, T, dtype, 60)
+    parent = np.stack([H.chain(T), np.array([-1, -1, 0, 1, 2, 3, 0, 6, 5, -1, 4, 7], dtype=np.int32)])
+    clean = H.run_tree(prm, q, kd, vd, parent, cache)
+    used = np.zeros(cache.rows_total, dtype=bool)
+    for u in (2, 3):
+        used[cache.unit_rows(u)] = True
+    hide = torch.from_numpy(~used).cuda()
+    cache.k[hide], cache.v[hide] = bad, bad                   # everything but the second sequence's rows
+    kd[1, :, 3], vd[1, :, 3] = bad, bad                       # seen by 3, 5 and 8 only
+    got = H.run_tree(prm, q, kd, vd, parent, cache)
+    clear = [t for t in range(T) if t not in (3, 5, 8)]
+    assert torch.equal(got[1][:, clear], clean[1][:, clear])
+    assert not torch.isfinite(got[1][:, [3, 5, 8]].float()).any()
+
+
+def test_parents_that_do_not_precede_their_child_count_as_roots():
+    prm = H.params(1, 2, 1, 64, "bf16")
+    cache = H.make_cache(prm, 20, 30, 0, 50, "bf16", 9)
+    q, kd, vd = drafts(prm, 6, "bf16", 70)
+    odd = np.array([[0, 5, -9, 1, 2, 1 << 30]], dtype=np.int32)
+    root = np.array([[-1, -1, -1, 1, 2, -1]], dtype=np.int32)
+    if B.tca_build_info() == 0:
+        assert torch.equal(H.run_tree(prm, q, kd, vd, odd, cache), H.run_tree(prm, q, kd, vd, root, cache))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_one_drafted_token_equals_append_and_decode(dtype):
+    prm = H.params(2, 8, 2, 128, dtype)
+    cache = H.make_cache(prm, [200, 31, 0, 64], 60, 10, 300, dtype, 11, extra_cap=8)
+    q, kd, vd = drafts(prm, 1, dtype, 80)
+    parent = np.full((2, 1), -1, dtype=np.int32)
+    got = H.run_tree(prm, q, kd, vd, parent, cache)
+    H.check_tree(prm, q, kd, vd, parent, cache, got, dtype)
+    B.tca_cache_append(prm, cache, kd[:, :, 0].contiguous(), vd[:, :, 0].contiguous(), q[:, :, 0].contiguous())
+    out = torch.empty_like(q[:, :, 0]).contiguous()
+    B.tca_attn_decode(prm, q[:, :, 0].contiguous(), cache, out, B.alloc_workspace(prm, cache.rows_total, B.TCA_OP_DECODE))
+    diff = (out.float() - got[:, :, 0].float()).abs().max().item()
+    # each side is within half a bf16 step of P and of the result (values of size 1), or fp32 rounding
+    assert diff <= (2 * 2 * 2.0 ** -8 * 4 if dtype == "bf16" else 1e-4)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_captured_call_replays_over_a_cache_that_has_grown(dtype):
+    prm = H.params(1, 4, 2, 128, dtype, block=32, window=64)
+    cache = H.make_cache(prm, [3, 200], [20, 90], 0, 300, dtype, 12, extra_cap=2000, t_keep=32)
+    T = 8
+    q, kd, vd = drafts(prm, T, dtype, 90)
+    parent = H.bush(T, 2)[None]
+    par = torch.from_numpy(parent).cuda()
+    ws, o = B.alloc_tree_workspace(prm, T), torch.zeros_like(q)
+    B.tca_attn_tree(prm, q, kd, vd, T, par, None, cache, o, ws)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        B.tca_attn_tree(prm, q, kd, vd, T, par, None, cache, o, ws)
+    path = torch.arange(T, dtype=torch.int32, device="cuda")[None].contiguous()
+    for step in range(60):
+        B.tca_cache_accept(prm, cache, kd, vd, q, T, path, np.array([T], dtype=np.int32))
+        if step in (0, 20, 59):
+            g.replay()
+            torch.cuda.synchronize()
+            assert B.tca_ws_status(ws) == B.TCA_OK
+            H.check_tree(prm, q, kd, vd, parent, cache, o, dtype)
+
+
+# ------------------------------------------------------------------ tca_cache_accept
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("block,window,n_tail,T", [(32, 64, 60, 20), (32, 64, 95, 9), (16, 8, 23, 64), (1, 1, 1, 12),
+                                                   (1, 0, 0, 5), (128, 0, 100, 128), (8, 40, 47, 33)])
+def test_accept_equals_one_append_per_token(block, window, n_tail, T, dtype):
+    """Bit for bit, for sequences that accept different numbers of tokens (none, one, all)."""
+    prm = H.params(5, 6, 2, 64, dtype, block=block, window=window)
+    cache = H.make_cache(prm, 20, min(n_tail, window + block - 1), (window + block) // 2, 400, dtype, 13,
+                         t_keep=max(1, block // 3), extra_cap=2 * T + 200)
+    q, kd, vd = drafts(prm, T, dtype, 100)
+    r = np.random.default_rng(T)
+    n = np.array([0, 1, T, max(1, T // 2), max(1, T - 1)], dtype=np.int32)
+    path = np.stack([np.sort(r.permutation(T)) if s != 3 else r.permutation(T) for s in range(5)]).astype(np.int32)
+    ref = H.clone_cache(prm, cache)
+    B.tca_cache_accept(prm, cache, kd, vd, q, T, torch.from_numpy(path).cuda(), n)
+    torch.cuda.synchronize()
+    H.mirror_equals_device(cache)
+    assert B.tca_cache_status(cache)[0] == B.TCA_OK
+    for step in range(T + 1):
+        for s in range(5):
+            if n[s] != step:
+                continue
+            for u in (2 * s, 2 * s + 1):
+                lo = int(cache.seg_start[u])
+                seg = slice(lo, lo + int(cache.global_cap[u]) + cache.tail_cap)
+                for name in ("k", "v", "pos"):
+                    assert torch.equal(getattr(cache, name)[seg], getattr(ref, name)[seg]), (name, s)
+                w = slice(u * B.TCA_STATE_WORDS, (u + 1) * B.TCA_STATE_WORDS)
+                assert torch.equal(cache.state[w], ref.state[w])
+        if step < T:
+            tok = [int(path[s][step]) for s in range(5)]
+            pick = lambda x: torch.stack([x[s, :, tok[s]] for s in range(5)]).contiguous()  # noqa: E731
+            B.tca_cache_append(prm, ref, pick(kd), pick(vd), pick(q))
+
+
+def test_accept_takes_the_same_token_twice_and_clamps_the_path():
+    prm = H.params(1, 2, 1, 64, "bf16", block=32, window=64)
+    q, kd, vd = drafts(prm, 4, "bf16", 110)
+    a = H.make_cache(prm, 5, 10, 0, 15, "bf16", 14)
+    b = H.clone_cache(prm, a)
+    n = np.array([3], dtype=np.int32)
+    B.tca_cache_accept(prm, a, kd, vd, q, 4, torch.tensor([[2, 2, 3, 0]], dtype=torch.int32, device="cuda"), n)
+    if B.tca_build_info() == 0:
+        B.tca_cache_accept(prm, b, kd, vd, q, 4, torch.tensor([[2, 2, 99, -1]], dtype=torch.int32, device="cuda"), n)
+        torch.cuda.synchronize()
+        assert torch.equal(a.k, b.k) and torch.equal(a.pos, b.pos)
+
+
+def test_accept_refuses_without_touching_anything():
+    prm = H.params(2, 2, 1, 64, "bf16", block=32, window=64)
+    q, kd, vd = drafts(prm, 8, "bf16", 120)
+    cache = H.make_cache(prm, [5, 6], [92, 10], 0, 100, "bf16", 15, extra_cap=0)
+    before = H.clone_cache(prm, cache)
+    path = torch.zeros(2, 8, dtype=torch.int32, device="cuda")
+    for n, status in (([4, 0], B.TCA_ERR_CAPACITY), ([9, 0], B.TCA_ERR_INVALID_ARG), ([-1, 0], B.TCA_ERR_INVALID_ARG)):
+        with pytest.raises(B.TcaError) as e:
+            B.tca_cache_accept(prm, cache, kd, vd, q, 8, path, np.array(n, dtype=np.int32))
+        assert e.value.status == status
+    torch.cuda.synchronize()
+    for name in ("k", "v", "pos", "state"):
+        assert torch.equal(getattr(cache, name), getattr(before, name))
+    H.mirror_equals_device(cache)
+    B.tca_cache_accept(prm, cache, kd, vd, q, 8, path, np.array([3, 8], dtype=np.int32))    # what fits is taken
+
+
+# ------------------------------------------------------------------ the operators together
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_prompts_to_drafted_tokens_as_a_server_runs_them(dtype):
+    """Packed prompts -> attention -> cache -> drafted tree -> accepted path -> decode; a prompt joins later."""
+    from oracle import serving_oracle as S
+    hq, hkv, d, T = 4, 2, 128, 7
+    lens = [210, 33, 150]
+    prm4 = H.params(4, hq, hkv, d, dtype, block=32, window=64)
+    starts = np.concatenate([[0], np.cumsum(lens)]).astype(np.int64)
+    q, k, v = (H.packed_buffer(200 + i, h, int(starts[-1]), d, dtype, "tokens") for i, h in enumerate((hq, hkv, hkv)))
+    o = H.run_packed(H.params(3, hq, hkv, d, dtype), q, k, v, starts)
+    want, a, s = S.packed_attention(H.f64(q), H.f64(k), H.f64(v), starts, H.scale_of(d))
+    H.check(H.f64(o), want, S.attention_tolerance(want, a, s, d, np.full(want.shape[:2], 210), dtype), "prompts")
+    cache = B.Cache(prm4, np.full(8, 256, dtype=np.int64), 96, np.full(8, 8, dtype=np.int64))
+    B.tca_cache_load(prm4, k, v, int(starts[-1]), starts, np.array([2, 0, 3], dtype=np.int32), cache)
+    ws = B.alloc_tree_workspace(prm4, T)
+    dec_ws = B.alloc_workspace(prm4, cache.rows_total, B.TCA_OP_DECODE)
+    for step in range(6):
+        qd, kd, vd = drafts(prm4, T, dtype, 300 + 10 * step)
+        parent = np.stack([H.bush(T, step + i) for i in range(4)])
+        live = np.array([T, 0 if step < 3 else T, T, 3], dtype=np.int32)
+        got = H.run_tree(prm4, qd, kd, vd, parent, cache, n_live=live, ws=ws)
+        H.check_tree(prm4, qd, kd, vd, parent, cache, got, dtype, n_live=live)
+        n = np.minimum(live, [3, 2, 5, 1]).astype(np.int32)
+        path = torch.from_numpy(np.tile(np.arange(T, dtype=np.int32), (4, 1))).cuda()
+        B.tca_cache_accept(prm4, cache, kd, vd, qd, T, path, n)
+        H.mirror_equals_device(cache)
+        if step == 2:      # the idle slot gets its prompt while the others go on
+            B.tca_cache_load(prm4, k, v, int(starts[-1]), starts[1:3].copy(), np.array([1], dtype=np.int32), cache)
+    qn = H.randn(999, (4, hq, d), dtype, 1.5)
+    out = torch.empty_like(qn)
+    B.tca_attn_decode(prm4, qn, cache, out, dec_ws)
+    assert B.tca_ws_status(dec_ws) == B.TCA_OK
+    kk, vv = H.f64(cache.k), H.f64(cache.v)
+    for b in range(4):
+        for h in range(hq):
+            rows = cache.unit_rows(b * hkv + h // (hq // hkv))
+            w, a, s = S.masked_attention(H.f64(qn)[b, h][None], kk[rows], vv[rows], np.ones((1, len(rows)), dtype=bool), H.scale_of(d))
+            H.check(H.f64(out)[b, h][None], w, S.attention_tolerance(w, a, s, d, np.array([len(rows)]), dtype), "decode")
