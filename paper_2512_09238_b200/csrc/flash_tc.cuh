@@ -1,0 +1,382 @@
+// Attention of up to two blocks of 128 query rows over a stream of 128-key tiles on the 5th-generation
+// tensor cores (bf16 in, fp32 accumulators in TMEM, online softmax on the CUDA cores), shared by the packed
+// prompt kernel and the drafted-tree kernel.  A Source says what the rows, tiles and masks are and
+// what happens to a finished row.
+//
+// Two ways to use the two blocks:
+//   kShared   both blocks attend to the same key tiles: 256 query rows per K/V tile brought in
+//   !kShared  one block of query rows; the two "blocks" are two streams over alternate key tiles with a
+//             softmax state each.  With 128 query rows or fewer there is no second block, and a single
+//             stream would leave the tensor pipe idle during every softmax and the CUDA cores idle during
+//             every product.
+//
+// 384 threads in three warpgroups: warp 0 TMA producer, warp 1 MMA issuer, warps 2 and 3 clean value tiles
+// (below); warps 4-7 and 8-11 softmax of block 0 and 1, one thread per query row = TMEM lane.  The first
+// warpgroup hands registers to the others (88 / 208 of 168 at launch), so that a thread holds its row
+// of 128 scores.  TMEM: S0 | S1 | O0 | O1; the bf16 P of a tile overwrites the first half of its S and is
+// the A operand of the second product.  Products are issued PV0 S0' PV1 S1' so that one block's softmax
+// runs under the other's products; a stream step consumes one pair (V of this tile, K of the next of
+// the same stream), which shares a full and an empty barrier.  P reaches the second product in two parts
+// (96 keys, then 32).  O is rescaled only when a row maximum grew by more than 2^8 since the last time.
+// Softmax statistics and O are fp32; P is rounded to bf16 because the product takes bf16 operands (half a
+// step, 2^-8 of a weight), the row sum adds the unrounded weights.
+//
+// A masked weight is an exact zero, but zero times an infinity or NaN is not.  So before the second product
+// of a tile that holds keys some row must not see, warps 2 and 3 clean its value tile in shared memory: rows
+// nobody sees become zero, and a non-finite element of a row that some see and some do not becomes zero and
+// is noted (Source::note); the epilogue adds it back to the rows that see it.  That costs nothing on the
+// way: it runs under the tile's first product and softmax.
+//
+// Every mbarrier wait is bounded; a wait that gives up raises the status word, lets copies land, frees
+// TMEM and returns.
+#pragma once
+#include <cuda.h>
+
+#include "common.cuh"
+#include "ptx_sm100.cuh"
+#include "tensor_map.cuh"
+
+namespace tca {
+
+constexpr int kTcRows = 128, kTcKeys = 128;
+constexpr int kTcThreads = 384;
+constexpr int kTcRegsLean = 88, kTcRegsSoftmax = 208;
+static_assert(128 * kTcRegsLean + 256 * kTcRegsSoftmax <= kTcThreads * 168, "more registers than the launch allocates");
+constexpr int kTcHalfBytes = 128 * 128;        // 128 rows x 64 bf16: one swizzled box
+constexpr float kTcRescale = 8.f;
+constexpr int kTcPSplit = 6;                   // k-steps of 16 keys in the first part of P
+
+template <int D>
+struct TcLayout {
+  static constexpr int NH = D / 64;
+  static constexpr int kRing = D == 128 ? 5 : 9;          // K/V tiles in shared memory
+  static constexpr int kPairs = (kRing + 1) / 2;          // (V, next K) pairs that can be in flight
+  static constexpr int kTile = NH * kTcHalfBytes;         // a Q, K or V tile
+  static constexpr int offQ = 0;
+  static constexpr int offKV = 2 * kTile;
+  static constexpr int offBar = offKV + kRing * kTile;
+  static constexpr int kBars = 5 + 2 * kPairs + 2 + 4 + 2;
+  static constexpr int bytes = offBar + 512 + 1024;       // barriers and scalars, alignment slack
+  static_assert(bytes <= 227 * 1024, "shared memory");
+  static_assert(kBars * 8 + 128 <= 512, "barrier block");
+};
+
+// Small shared state next to the barriers.
+struct TcShared {
+  uint32_t tmem;
+  int abort;
+  uint32_t dirty[2][4];      // noted key rows of up to two tiles
+  int any_dirty;
+};
+
+// Called by all 384 threads after the Source is known and before anything else of the kernel's shared
+// memory is in use; returns after the last tile with every thread.  Source:
+//   int  tiles(h)                 shared: tiles of block h; streams: all tiles (h ignored)
+//   int  q_bytes(h)               bytes load_q(h) brings (both halves)
+//   void load_q(h, dst, bar)      issue the loads of block h's query tile
+//   void load(t, is_v, dst, bar)  issue the loads of a K or V tile (kTile bytes)
+//   int  row_key(h, row)          what last() needs of a row, worked out once
+//   int  last(key, t)             last key of tile t that the row sees (>= 127: all)
+//   int  clean(t)                 -1: nothing to clean; else rows of tile t that somebody sees
+//   bool scan()                   whether rows below clean(t) are searched for non-finite elements
+//   int  note_slot(t)             which dirty[] entry a cleaned tile uses
+//   void store(h, row, seen, m, l, read)  one finished row per thread, called by whole warps; seen: the
+//                                 block had tiles; read(c, v): columns 32 c .. of O (warp-wide)
+template <int D, bool kShared, typename Source>
+__device__ __forceinline__ void flash_tc(const Source& src, uint8_t* smem, TcShared* sh, float scale_log2e, int* status) {
+  using L = TcLayout<D>;
+  constexpr int kRing = L::kRing, kPairs = L::kPairs, kLead = kShared ? 1 : 2;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::offBar);
+  uint64_t *bar_q = bars, *bar_k0_full = bars + 1, *bar_k0_empty = bars + 2, *bar_clean = bars + 3, *bar_to_clean = bars + 4;
+  uint64_t *bar_full = bars + 5, *bar_empty = bar_full + kPairs;
+  uint64_t *bar_s = bar_empty + kPairs, *bar_p = bar_s + 2, *bar_pv = bar_p + 4;
+  volatile int* abort_flag = &sh->abort;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int n0 = src.tiles(0), n1 = kShared ? src.tiles(1) : 0;
+  const int nt = kShared ? max(n0, n1) : n0;                 // tiles brought in
+  const int lead = min(kLead, nt);
+  // first load of tile t's K, and V, in ring order: the leading K tiles, then (V_m, K_m+lead) pairs
+  auto k_load = [&](int t) { return t < kLead ? t : kLead + 2 * (t - kLead) + 1; };
+  auto v_load = [&](int t) { return kLead + 2 * t; };
+
+  if (tid == 0) {
+    ptx::mbar_init(bar_q, 1);
+    ptx::mbar_init(bar_k0_full, 1);
+    ptx::mbar_init(bar_k0_empty, 1);
+    ptx::mbar_init(bar_clean, 2);
+    ptx::mbar_init(bar_to_clean, 1);
+    for (int i = 0; i < kPairs; ++i) {
+      ptx::mbar_init(bar_full + i, 2);
+      ptx::mbar_init(bar_empty + i, 1);
+    }
+    for (int h = 0; h < 2; ++h) {
+      ptx::mbar_init(bar_s + h, 1);
+      ptx::mbar_init(bar_p + 2 * h, 4);
+      ptx::mbar_init(bar_p + 2 * h + 1, 4);
+      ptx::mbar_init(bar_pv + h, 1);
+    }
+    ptx::fence_barrier_init();
+    sh->abort = *reinterpret_cast<volatile int*>(status) != 0 ? 1 : 0;
+    for (int i = 0; i < 8; ++i) sh->dirty[i >> 2][i & 3] = 0;
+    sh->any_dirty = 0;
+  }
+  if (warp == 0) {
+    ptx::tmem_alloc(&sh->tmem, 512);
+    ptx::tmem_relinquish();
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::tc_fence_after();
+  const uint32_t tmem_base = sh->tmem;
+
+  if (warp < 4) {
+    ptx::reg_dealloc<kTcRegsLean>();
+    if (*abort_flag) {
+      // a status word that was already set: do nothing
+    } else if (warp == 0) {
+      // ------------------------------------------------------------- producer
+      if (lane == 0) {
+        ptx::mbar_arrive_expect_tx(bar_q, uint32_t(src.q_bytes(0) + (kShared && n1 > 0 ? src.q_bytes(1) : 0)));
+        src.load_q(0, smem + L::offQ, bar_q);
+        if (kShared && n1 > 0) src.load_q(1, smem + L::offQ + L::kTile, bar_q);
+        ptx::mbar_arrive_expect_tx(bar_k0_full, uint32_t(lead * L::kTile));
+        for (int t = 0; t < lead; ++t) src.load(t, false, smem + L::offKV + t * L::kTile, bar_k0_full);
+        bool ok = true;
+        for (int m = 0; m < nt && ok; ++m) {
+#pragma unroll
+          for (int is_k = 0; is_k < 2; ++is_k) {
+            const int t = is_k ? m + kLead : m, n = kLead + 2 * m + is_k;
+            if (t >= nt) {                                   // no such K tile: its barrier still expects two arrivals
+              ptx::mbar_arrive(bar_full + m % kPairs);
+              continue;
+            }
+            if (n >= kRing) {                                // the slot's previous tile must have been consumed
+              const int r = n - kRing;
+              if (r < kLead) ok = ptx::mbar_wait(bar_k0_empty, 0, abort_flag);
+              else ok = ptx::mbar_wait(bar_empty + ((r - kLead) >> 1) % kPairs, uint32_t(((r - kLead) >> 1) / kPairs) & 1u, abort_flag);
+              if (!ok) break;
+            }
+            ptx::mbar_arrive_expect_tx(bar_full + m % kPairs, uint32_t(L::kTile));
+            src.load(t, !is_k, smem + L::offKV + (n % kRing) * L::kTile, bar_full + m % kPairs);
+          }
+        }
+      }
+    } else if (warp == 1) {
+      // ------------------------------------------------------------- MMA issuer (whole warp, one elected lane issues)
+      constexpr uint32_t idesc_s = ptx::idesc_bf16(kTcRows, kTcKeys, false);
+      constexpr uint32_t idesc_pv = ptx::idesc_bf16(kTcRows, D, true);
+      const uint64_t dq = ptx::smem_desc_sw128(ptx::smem_u32(smem + L::offQ), 16, 1024);
+      const uint64_t dk = ptx::smem_desc_sw128(ptx::smem_u32(smem + L::offKV), 16, 1024);             // K: K-major B
+      const uint64_t dv = ptx::smem_desc_sw128(ptx::smem_u32(smem + L::offKV), kTcHalfBytes, 1024);   // V: MN-major B
+      auto wait = [&](uint64_t* bar, uint32_t parity) -> bool {
+        return __all_sync(0xffffffffu, ptx::mbar_wait(bar, parity, abort_flag));
+      };
+      auto issue_s = [&](int h, int n) {
+        const uint64_t a0 = dq + (kShared ? uint64_t(uint32_t(h * L::kTile) >> 4) : 0ull);
+        const uint64_t b0 = dk + uint64_t(uint32_t((n % kRing) * L::kTile) >> 4);
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk) {
+          const uint32_t off = (uint32_t(kk >> 2) * kTcHalfBytes + uint32_t(kk & 3) * 32u) >> 4;
+          ptx::umma_ss_elect(tmem_base + h * 128u, a0 + off, b0 + off, idesc_s, kk > 0);
+        }
+      };
+      auto issue_pv = [&](int h, int n, bool acc, uint32_t parity) -> bool {
+        const uint64_t b0 = dv + uint64_t(uint32_t((n % kRing) * L::kTile) >> 4);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          if (!wait(bar_p + 2 * h + c, parity)) return false;
+          ptx::tc_fence_after();
+#pragma unroll
+          for (int kk = (c == 0 ? 0 : kTcPSplit); kk < (c == 0 ? kTcPSplit : kTcKeys / 16); ++kk)
+            ptx::umma_ts_elect(tmem_base + 256u + uint32_t(h * D), tmem_base + h * 128u + uint32_t(kk * 8),
+                               b0 + uint32_t((kk * 2048) >> 4), idesc_pv, (acc || kk > 0) ? 1u : 0u);
+        }
+        return true;
+      };
+      uint32_t cleaned = 0;
+      bool ok = nt > 0 && wait(bar_q, 0) && wait(bar_k0_full, 0);
+      if (ok) {
+        ptx::tc_fence_after();
+        for (int h = 0; h < 2; ++h)
+          if (kShared ? (h == 0 ? n0 : n1) > 0 : h < nt) {
+            issue_s(h, kShared ? 0 : h);
+            ptx::umma_commit_elect(bar_s + h);
+          }
+        ptx::umma_commit_elect(bar_k0_empty);
+      }
+      for (int t = 0; t < nt && ok; ++t) {
+        ok = wait(bar_full + t % kPairs, uint32_t(t / kPairs) & 1u);
+        if (ok && src.clean(t) >= 0) {
+          if (lane == 0) ptx::mbar_arrive(bar_to_clean);
+          ok = wait(bar_clean, cleaned++ & 1u);
+        }
+        if (kShared) {
+          for (int h = 0; h < 2 && ok; ++h) {
+            const int nh = h == 0 ? n0 : n1;
+            if (t >= nh) continue;
+            ok = issue_pv(h, v_load(t), t > 0, uint32_t(t) & 1u);
+            if (!ok) break;
+            if (t + 1 < nh) issue_s(h, k_load(t + 1));
+            ptx::umma_commit_elect(t + 1 < nh ? bar_s + h : bar_pv + h);   // S ready implies PV done
+          }
+        } else {
+          const int h = t & 1;
+          if (ok) ok = issue_pv(h, v_load(t), t > 1, uint32_t(t >> 1) & 1u);
+          if (!ok) break;
+          if (t + 2 < nt) issue_s(h, k_load(t + 2));
+          ptx::umma_commit_elect(t + 2 < nt ? bar_s + h : bar_pv + h);
+        }
+        if (ok) ptx::umma_commit_elect(bar_empty + t % kPairs);
+      }
+    } else {
+      // ------------------------------------------------------------- cleaning of value tiles (warps 2 and 3: 64 rows each)
+      // They start on a tile when the issuer, having seen it arrive, says so: the issuer then waits for them,
+      // so neither can be a phase of the tile's barrier behind or ahead of the other.
+      bool ok = true;
+      uint32_t cleaned = 0;
+      for (int t = 0; t < nt && ok; ++t) {
+        const int seen = src.clean(t);
+        if (seen < 0) continue;
+        ok = __all_sync(0xffffffffu, ptx::mbar_wait(bar_to_clean, cleaned++ & 1u, abort_flag)) &&
+             __all_sync(0xffffffffu, ptx::mbar_wait(bar_full + t % kPairs, uint32_t(t / kPairs) & 1u, abort_flag));
+        if (!ok) break;
+        uint8_t* tile = smem + L::offKV + (v_load(t) % kRing) * L::kTile;
+        // 16-byte piece i of the warp's 64 rows; the swizzle only permutes the pieces within a row
+        for (int half = 0; half < L::NH; ++half)
+#pragma unroll 4
+          for (int i = lane; i < 64 * 8; i += 32) {
+            const int r = (warp - 2) * 64 + (i >> 3);
+            uint4* p = reinterpret_cast<uint4*>(tile + half * kTcHalfBytes + r * 128 + (i & 7) * 16);
+            if (r >= seen) {
+              *p = make_uint4(0, 0, 0, 0);
+            } else if (src.scan()) {
+              uint4 v = *p;
+              uint32_t* w = &v.x;
+              bool hit = false;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                if ((w[e] & 0x7f80u) == 0x7f80u) { w[e] &= 0xffff0000u; hit = true; }
+                if ((w[e] & 0x7f800000u) == 0x7f800000u) { w[e] &= 0xffffu; hit = true; }
+              }
+              if (hit) {
+                *p = v;
+                atomicOr(&sh->dirty[src.note_slot(t)][r >> 5], 1u << (r & 31));
+                sh->any_dirty = 1;
+              }
+            }
+          }
+        ptx::fence_proxy_async_smem();                       // the product reads the tile through the async proxy
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(bar_clean);
+      }
+    }
+  } else {
+    ptx::reg_alloc<kTcRegsSoftmax>();
+    // ------------------------------------------------------------- softmax, one row per thread
+    const int h = (warp - 4) >> 2;
+    const int mine = kShared ? (h == 0 ? n0 : n1) : (nt - h + 1) / 2;   // tiles of this block / stream
+    if (!*abort_flag) {
+      const int quarter = warp & 3, row = quarter * 32 + lane;
+      const uint32_t lane_addr = tmem_base + (uint32_t(quarter * 32) << 16);
+      const uint32_t s_addr = lane_addr + h * 128u, o_addr = lane_addr + 256u + uint32_t(h * D);
+      const int row_key = src.row_key(h, row);
+      float m_run = -INFINITY, m_used = -INFINITY, l = 0.f;
+      const uint64_t scale2 = ptx::pack2(scale_log2e, scale_log2e);
+      bool ok = true;
+      for (int it = 0; it < mine; ++it) {
+        const int hi = src.last(row_key, kShared ? it : 2 * it + h);
+        ok = __all_sync(0xffffffffu, ptx::mbar_wait(bar_s + h, uint32_t(it) & 1u, abort_flag));
+        if (!ok) break;
+        ptx::tc_fence_after();
+        uint32_t v[kTcKeys];
+#pragma unroll
+        for (int c = 0; c < kTcKeys / 32; ++c)
+          ptx::tmem_ld32(s_addr + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&v[c * 32]));
+        ptx::tc_wait_ld();
+        if (hi < kTcKeys - 1) {   // a masked score is -inf: it loses every max and its weight is exactly 0
+#pragma unroll
+          for (int k = 0; k < kTcKeys; ++k)
+            if (k > hi) v[k] = 0xff800000u;
+        }
+        float mx;
+        {
+          float mx8[8];
+#pragma unroll
+          for (int a = 0; a < 8; ++a) mx8[a] = fmaxf(__uint_as_float(v[2 * a]), __uint_as_float(v[2 * a + 1]));
+#pragma unroll
+          for (int k = 16; k < kTcKeys; k += 16)
+#pragma unroll
+            for (int a = 0; a < 8; ++a)
+              mx8[a] = ptx::max3(mx8[a], __uint_as_float(v[k + 2 * a]), __uint_as_float(v[k + 2 * a + 1]));
+          mx = fmaxf(fmaxf(ptx::max3(mx8[0], mx8[1], mx8[2]), ptx::max3(mx8[3], mx8[4], mx8[5])), fmaxf(mx8[6], mx8[7]));
+        }
+        m_run = fmaxf(m_run, mx * scale_log2e);
+        if (__any_sync(0xffffffffu, m_run > m_used + kTcRescale)) {   // warp-uniform: TMEM access is warp-wide
+          const float alpha = (m_used == -INFINITY) ? 0.f : ptx::fast_exp2(m_used - m_run);
+          if (it > 0) {
+#pragma unroll 1
+            for (int c = 0; c < D / 32; ++c) {
+              uint32_t o[32];
+              ptx::tmem_ld32(o_addr + c * 32, o);
+              ptx::tc_wait_ld();
+#pragma unroll
+              for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * alpha);
+              ptx::tmem_st32(o_addr + c * 32, o);
+            }
+            ptx::tc_wait_st();
+          }
+          l *= alpha;
+          m_used = m_run;
+        }
+        const float neg_m = (m_used == -INFINITY) ? 0.f : -m_used;
+        const uint64_t neg_m2 = ptx::pack2(neg_m, neg_m);
+        uint64_t sum2[2] = {0ull, 0ull};
+        // eight groups of 16 scores; a group's store is issued only after the next group's arithmetic, so it
+        // never waits for exponentials still in flight
+#pragma unroll
+        for (int g = 0; g < 8; ++g) {
+#pragma unroll
+          for (int jj = 0; jj < 8; ++jj) {
+            const int j = g * 8 + jj;
+            float xl, xh;
+            ptx::unpack2(ptx::fma2(ptx::pack2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])), scale2, neg_m2), xl, xh);
+            const float el = ptx::fast_exp2(xl), eh = ptx::fast_exp2(xh);
+            sum2[j & 1] = ptx::add2(sum2[j & 1], ptx::pack2(el, eh));
+            v[j] = ptx::pack_bf16x2(el, eh);   // entry j is never read again (j <= 2j)
+          }
+          if (g == kTcPSplit + 1) {            // the first part was stored at least one group ago
+            ptx::tc_wait_st();
+            ptx::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(bar_p + 2 * h);
+          }
+          if (g >= 1) ptx::tmem_st8(s_addr + (g - 1) * 8, &v[(g - 1) * 8]);
+        }
+        ptx::tmem_st8(s_addr + 56, &v[56]);
+        ptx::tc_wait_st();
+        ptx::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(bar_p + 2 * h + 1);
+        float s0, s1, s2, s3;
+        ptx::unpack2(sum2[0], s0, s1);
+        ptx::unpack2(sum2[1], s2, s3);
+        l += (s0 + s1) + (s2 + s3);
+      }
+      if (ok && mine > 0) ok = __all_sync(0xffffffffu, ptx::mbar_wait(bar_pv + h, 0, abort_flag));   // committed after the last PV
+      if (ok) {
+        ptx::tc_fence_after();
+        src.store(h, row, mine > 0, m_used, l, [&](int c, uint32_t (&v)[32]) {
+          ptx::tmem_ld32(o_addr + c * 32, v);
+          ptx::tc_wait_ld();
+        });
+      }
+    }
+  }
+  // ------------------------------------------------------------- teardown
+  ptx::tc_fence_before();
+  __syncthreads();
+  if (*abort_flag) ptx::abort_teardown(status, tid);   // status word, then time for copies in flight to land
+  if (warp == 0) ptx::tmem_dealloc(tmem_base, 512);
+}
+
+}  // namespace tca

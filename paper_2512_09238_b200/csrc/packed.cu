@@ -7,6 +7,10 @@
 
 namespace tca {
 
+template <int D>
+int launch_packed_tc(const tca_params* prm, const void* Q, const void* K, const void* V, const PackedArgs& a, void* O,
+                     void* ws, cudaStream_t s);
+
 namespace {
 
 // Query rows of a CTA are (position, head of the group) pairs, head fastest: row r is position
@@ -119,6 +123,8 @@ extern "C" int tca_attn_packed(const tca_params* prm, const void* Q, const void*
     if (prm->head_dim == 128) return launch_packed_simt<float, 128>(prm, Q, K, V, a, O, s);
     return launch_packed_simt<float, 64>(prm, Q, K, V, a, O, s);
   }
+  if (!(prm->flags & TCA_FLAG_PREFILL_SIMT))
+    return prm->head_dim == 128 ? launch_packed_tc<128>(prm, Q, K, V, a, O, ws, s) : launch_packed_tc<64>(prm, Q, K, V, a, O, ws, s);
   if (prm->head_dim == 128) return launch_packed_simt<__nv_bfloat16, 128>(prm, Q, K, V, a, O, s);
   return launch_packed_simt<__nv_bfloat16, 64>(prm, Q, K, V, a, O, s);
 }

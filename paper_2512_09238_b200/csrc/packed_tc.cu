@@ -1,0 +1,147 @@
+// tca_attn_packed for bf16: the tensor-core kernel.  One CTA takes 2 P consecutive positions of one
+// sequence for all G query heads of one KV head, P = 128 / G: query rows are (position, head) pairs, head
+// fastest, so the two blocks of 128 rows are full for any sequence of a few dozen tokens and every K/V
+// tile serves 256 rows.  Q comes as one box of P positions x G heads, whatever the strides.
+#include "flash_tc.cuh"
+#include "packed_common.cuh"
+
+namespace tca {
+namespace {
+
+template <int D>
+struct PackedTcSrc {
+  const CUtensorMap *mq, *mk, *mv;
+  const __nv_bfloat16* V;
+  __nv_bfloat16* O;
+  const PackedArgs* a;
+  TcShared* sh;
+  int64_t row0;
+  int len, p0, kvh, G, P;
+
+  __device__ __forceinline__ int last_pos(int h) const { return min(p0 + (h + 1) * P, len) - 1; }
+  __device__ __forceinline__ int tiles(int h) const { return p0 + h * P < len ? last_pos(h) / kTcKeys + 1 : 0; }
+  __device__ __forceinline__ int q_bytes(int) const { return D * 2 * G * P; }
+  __device__ __forceinline__ void load_q(int h, uint8_t* dst, uint64_t* bar) const {
+    for (int half = 0; half < D / 64; ++half)
+      ptx::tma_load_3d(dst + half * kTcHalfBytes, mq, half * 64, kvh * G, int(row0) + p0 + h * P, bar);
+  }
+  __device__ __forceinline__ void load(int t, bool is_v, uint8_t* dst, uint64_t* bar) const {
+    for (int half = 0; half < D / 64; ++half)
+      ptx::tma_load_3d(dst + half * kTcHalfBytes, is_v ? mv : mk, half * 64, int(row0) + t * kTcKeys, kvh, bar);
+  }
+  __device__ __forceinline__ int row_key(int h, int row) const { return min(p0 + h * P + row / G, last_pos(h)); }
+  __device__ __forceinline__ int last(int key, int t) const { return key - t * kTcKeys; }
+  // From the tile that holds p0 on, some row does not see some key (at most two tiles: 2 P <= 128, or
+  // P = 128 with p0 a multiple of 256).  Rows past the last position are nobody's: another sequence's, or none.
+  __device__ __forceinline__ int clean(int t) const {
+    return t < p0 / kTcKeys ? -1 : min(kTcKeys, min(p0 + 2 * P, len) - t * kTcKeys);
+  }
+  __device__ __forceinline__ bool scan() const { return true; }
+  __device__ __forceinline__ int note_slot(int t) const { return t - p0 / kTcKeys; }
+
+  template <typename Read>
+  __device__ __forceinline__ void store(int h, int row, bool seen, float, float l, Read read) const {
+    if (!seen) return;
+    const int pos = p0 + h * P + row / G;
+    const bool mine = row < G * P && pos < len;
+    const bool dirty = sh->any_dirty != 0;
+    const float inv = 1.f / l;
+    __nv_bfloat16* out = O + (kvh * G + row % G) * a->o.head + (row0 + pos) * a->o.row;
+#pragma unroll 1
+    for (int c = 0; c < D / 32; ++c) {
+      uint32_t v[32];
+      read(c, v);
+      if (!mine) continue;
+#pragma unroll
+      for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * inv);
+      if (dirty) {   // non-finite values of masked tiles, kept out of the product, reach the rows that see them
+        for (int w = 0; w < 8; ++w)
+          for (uint32_t bits = sh->dirty[w >> 2][w & 3]; bits; bits &= bits - 1) {
+            const int key = (p0 / kTcKeys + (w >> 2)) * kTcKeys + (w & 3) * 32 + __ffs(bits) - 1;
+            if (key > pos) break;
+            const __nv_bfloat16* src = V + kvh * a->v.head + (row0 + key) * a->v.row + c * 32;
+#pragma unroll
+            for (int k = 0; k < 32; ++k) {
+              const float x = __bfloat162float(src[k]);
+              if (!isfinite(x)) v[k] = __float_as_uint(__uint_as_float(v[k]) + x);
+            }
+          }
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        uint4 w;
+        w.x = ptx::pack_bf16x2(__uint_as_float(v[q * 8 + 0]), __uint_as_float(v[q * 8 + 1]));
+        w.y = ptx::pack_bf16x2(__uint_as_float(v[q * 8 + 2]), __uint_as_float(v[q * 8 + 3]));
+        w.z = ptx::pack_bf16x2(__uint_as_float(v[q * 8 + 4]), __uint_as_float(v[q * 8 + 5]));
+        w.w = ptx::pack_bf16x2(__uint_as_float(v[q * 8 + 6]), __uint_as_float(v[q * 8 + 7]));
+        *reinterpret_cast<uint4*>(out + c * 32 + q * 8) = w;
+      }
+    }
+  }
+};
+
+template <int D>
+__global__ void __launch_bounds__(kTcThreads, 1)
+packed_tc_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
+                 const __grid_constant__ CUtensorMap mv, const __nv_bfloat16* __restrict__ V,
+                 const __grid_constant__ PackedArgs args, int max_tiles, int unit_major, float scale_log2e,
+                 __nv_bfloat16* __restrict__ O, int* __restrict__ status) {
+  extern __shared__ uint8_t packed_tc_smem[];
+  __shared__ TcShared sh;
+  __shared__ int found[2];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(packed_tc_smem) + 1023) & ~uintptr_t(1023));
+  if (threadIdx.x == 0) {
+    ptx::tma_prefetch_desc(&mq);
+    ptx::tma_prefetch_desc(&mk);
+    ptx::tma_prefetch_desc(&mv);
+  }
+  pdl_wait();
+  pdl_launch_dependents();
+  PackedTcSrc<D> src;
+  src.G = args.n_q_heads / args.n_kv_heads;
+  src.P = kTcRows / src.G;
+  src.kvh = unit_major ? int(blockIdx.x) / max_tiles : int(blockIdx.x) % args.n_kv_heads;
+  const int item = unit_major ? int(blockIdx.x) % max_tiles : int(blockIdx.x) / args.n_kv_heads;
+  if (threadIdx.x < 32) {
+    int seq = -1, tile = 0;
+    if (!packed_find(args, item, 2 * src.P, threadIdx.x, seq, tile)) seq = -1;
+    if (threadIdx.x == 0) { found[0] = seq; found[1] = tile; }
+  }
+  __syncthreads();
+  if (found[0] < 0) return;
+  packed_bounds(args, found[0], src.row0, src.len);
+  src.p0 = found[1] * 2 * src.P;
+  src.mq = &mq; src.mk = &mk; src.mv = &mv;
+  src.V = V; src.O = O; src.a = &args; src.sh = &sh;
+  flash_tc<D, true>(src, smem, &sh, scale_log2e, status);
+}
+
+}  // namespace
+
+template <int D>
+int launch_packed_tc(const tca_params* prm, const void* Q, const void* K, const void* V, const PackedArgs& a, void* O,
+                     void* ws, cudaStream_t s) {
+  const int G = a.n_q_heads / a.n_kv_heads, P = kTcRows / G;
+  const int64_t max_tiles = packed_max_tiles(a.rows, a.n_seq, 2 * P);
+  if (max_tiles * a.n_kv_heads >= (int64_t(1) << 31)) return TCA_ERR_UNSUPPORTED;
+  CUtensorMap mq, mk, mv;
+  if (!encode_map_3d(&mq, Q, D, a.n_q_heads, a.rows, a.q.head, a.q.row, G, P) ||
+      !encode_map_3d(&mk, K, D, a.rows, a.n_kv_heads, a.k.row, a.k.head, kTcKeys, 1) ||
+      !encode_map_3d(&mv, V, D, a.rows, a.n_kv_heads, a.v.row, a.v.head, kTcKeys, 1))
+    return TCA_ERR_CUDA;
+  auto kern = packed_tc_kernel<D>;
+  TCA_CHECK_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, TcLayout<D>::bytes));
+  // Longest tiles first over all heads balances best, but then the resident CTAs read all heads' keys
+  // at once; when those do not fit the L2 the heads go one after another.
+  const int unit_major = a.rows * a.n_kv_heads * D * 4 > l2_bytes() / 2 ? 1 : 0;
+  return launch_pdl(kern, dim3(unsigned(max_tiles * a.n_kv_heads)), dim3(kTcThreads), size_t(TcLayout<D>::bytes), s, mq, mk,
+                    mv, static_cast<const __nv_bfloat16*>(V), a, int(max_tiles), unit_major,
+                    prm->sm_scale * 1.4426950408889634f, static_cast<__nv_bfloat16*>(O), static_cast<int*>(ws));
+}
+
+template int launch_packed_tc<64>(const tca_params*, const void*, const void*, const void*, const PackedArgs&, void*, void*,
+                                  cudaStream_t);
+template int launch_packed_tc<128>(const tca_params*, const void*, const void*, const void*, const PackedArgs&, void*, void*,
+                                   cudaStream_t);
+
+}  // namespace tca

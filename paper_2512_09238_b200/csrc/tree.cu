@@ -12,23 +12,33 @@
 
 namespace tca {
 
+int launch_tree_tc(const tca_params* prm, const void* q, const tca_cache_desc* c, const TreePlan& plan, const TreeWs& ws,
+                   cudaStream_t s);
+
+namespace {
+bool tree_on_tensor_cores(const tca_params* prm) { return prm->dtype == TCA_BF16 && !(prm->flags & TCA_FLAG_PREFILL_SIMT); }
+}  // namespace
+
 TreePlan tree_plan(const tca_params* prm, int n_draft) {
   TreePlan p;
   const int U = prm->batch * prm->n_kv_heads;
+  const bool tc = tree_on_tensor_cores(prm);
   p.rows = prm->n_q_heads / prm->n_kv_heads * n_draft;
-  p.row_blocks = (p.rows + kSimtRows - 1) / kSimtRows;
-  p.streams = 1;
+  // tensor cores: up to 128 rows run as two streams over alternate tiles, more as two blocks per CTA
+  p.streams = tc && p.rows <= 128 ? 2 : 1;
+  p.rows_per_cta = !tc ? kSimtRows : p.rows <= 128 ? 128 : 256;
+  p.row_blocks = (p.rows + p.rows_per_cta - 1) / p.rows_per_cta;
+  p.step_rows = 128;
+  p.min_steps = p.streams;
   // one wave of resident CTAs; with more units than slices fit that wave, two slices per unit and a
   // wave on top, so that units of different lengths still balance
-  const int wave = 2 * sm_count() / p.row_blocks > 0 ? 2 * sm_count() / p.row_blocks : 1;
+  const int resident = (tc ? 1 : 2) * sm_count();
+  const int wave = resident / p.row_blocks > 0 ? resident / p.row_blocks : 1;
   p.n_slots = wave >= 2 * U ? wave : wave + 2 * U;
   return p;
 }
 
 namespace {
-
-constexpr int kStepRows = 128;    // cache rows are dealt to slices in steps of this
-constexpr int kMinSteps = 1;
 
 template <typename T, int D>
 struct TreeSrc {
@@ -55,7 +65,7 @@ tree_simt_kernel(const T* __restrict__ q, const T* __restrict__ Kc, const T* __r
   pdl_wait();
   pdl_launch_dependents();
   if (threadIdx.x < 32) {
-    const TreeSlice s = tree_find(state, n_units, tail_cap, plan.n_slots, kStepRows, kMinSteps, kSimtKeys,
+    const TreeSlice s = tree_find(state, n_units, tail_cap, plan.n_slots, plan.step_rows, plan.min_steps, kSimtKeys,
                                   int(blockIdx.x) / plan.row_blocks, threadIdx.x);
     if (threadIdx.x == 0) slice = s;
   }
@@ -220,13 +230,18 @@ int launch_tree(const tca_params* prm, const void* q, const void* kd, const void
                 cudaStream_t s) {
   const int U = prm->batch * prm->n_kv_heads;
   const float scale = prm->sm_scale * 1.4426950408889634f;
-  auto kern = tree_simt_kernel<T, D>;
-  TCA_CHECK_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SimtSmem<D>::kBytes));
   const int64_t ctas = int64_t(plan.n_slots) * plan.row_blocks;
   if (ctas >= (int64_t(1) << 31)) return TCA_ERR_UNSUPPORTED;
-  int st = launch_pdl(kern, dim3(unsigned(ctas)), dim3(kSimtThreads), size_t(SimtSmem<D>::kBytes), s,
-                      static_cast<const T*>(q), static_cast<const T*>(c->k), static_cast<const T*>(c->v),
-                      static_cast<const int64_t*>(c->state), U, c->tail_cap, plan, scale, ws);
+  int st;
+  if (tree_on_tensor_cores(prm)) {
+    st = launch_tree_tc(prm, q, c, plan, ws, s);
+  } else {
+    auto kern = tree_simt_kernel<T, D>;
+    TCA_CHECK_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SimtSmem<D>::kBytes));
+    st = launch_pdl(kern, dim3(unsigned(ctas)), dim3(kSimtThreads), size_t(SimtSmem<D>::kBytes), s,
+                    static_cast<const T*>(q), static_cast<const T*>(c->k), static_cast<const T*>(c->v),
+                    static_cast<const int64_t*>(c->state), U, c->tail_cap, plan, scale, ws);
+  }
   if (st != TCA_OK) return st;
   return launch_pdl(tree_combine_kernel<T, D>, dim3(unsigned((plan.rows + kCombineWarps - 1) / kCombineWarps), unsigned(U)),
                     dim3(kCombineWarps * 32), size_t(0), s, static_cast<const T*>(q), static_cast<const T*>(kd),

@@ -9,9 +9,12 @@ namespace tca {
 // Rows of a unit's query block: row r = head-of-group * T + drafted token, as they lie in q.
 struct TreePlan {
   int rows;          // G * T
-  int row_blocks;    // CTAs per slice, each with rows_per_cta of them
+  int rows_per_cta;
+  int row_blocks;    // CTAs per slice
   int streams;       // partial results a CTA writes per row
   int n_slots;       // slices of all units together, at most
+  int step_rows;     // slices are multiples of this many rows ...
+  int min_steps;     // ... and at least this many steps long
 };
 TreePlan tree_plan(const tca_params* prm, int n_draft);
 
