@@ -27,6 +27,11 @@
 // is noted (Source::note); the epilogue adds it back to the rows that see it.  That costs nothing on the
 // way: it runs under the tile's first product and softmax.
 //
+// Persistent: a CTA works through several items (a query tile against its keys), and the roles run ahead of
+// one another across items.  While the softmax warps still write out an item, the next one's query tile and
+// keys are on their way and its first scores are computed, so the latencies of starting an item are paid
+// once per CTA.  The producer warp finds the items and hands them to the other roles through two slots.
+//
 // Every mbarrier wait is bounded; a wait that gives up raises the status word, lets copies land, frees
 // TMEM and returns.
 #pragma once
@@ -50,29 +55,76 @@ template <int D>
 struct TcLayout {
   static constexpr int NH = D / 64;
   static constexpr int kRing = D == 128 ? 5 : 9;          // K/V tiles in shared memory
-  static constexpr int kPairs = (kRing + 1) / 2;          // (V, next K) pairs that can be in flight
+  static constexpr int kPairs = kRing;                    // groups of loads (a V and a K tile) in flight, at least one tile each
   static constexpr int kTile = NH * kTcHalfBytes;         // a Q, K or V tile
   static constexpr int offQ = 0;
   static constexpr int offKV = 2 * kTile;
   static constexpr int offBar = offKV + kRing * kTile;
-  static constexpr int kBars = 5 + 2 * kPairs + 2 + 4 + 2;
-  static constexpr int bytes = offBar + 512 + 1024;       // barriers and scalars, alignment slack
-  static_assert(bytes <= 227 * 1024, "shared memory");
-  static_assert(kBars * 8 + 128 <= 512, "barrier block");
+  static constexpr int kBars = 8 + 2 * kPairs + 2 + 4 + 2;
+  static constexpr int bytes = offBar + 512 + 1024;       // barriers, alignment slack
+  static_assert(bytes <= 227 * 1024 - 512, "shared memory");
+  static_assert(kBars * 8 <= 512, "barrier block");
 };
 
-// Small shared state next to the barriers.
+// Small shared state.  Item: what the producer warp hands to the other roles.
+template <typename Item>
 struct TcShared {
   uint32_t tmem;
   int abort;
-  uint32_t dirty[2][4];      // noted key rows of up to two tiles
-  int any_dirty;
+  uint32_t dirty[2][2][4];   // per item slot: noted key rows of up to two tiles
+  int any_dirty[2];
+  int valid[2];
+  Item item[2];
 };
 
-// Called by all 384 threads after the Source is known and before anything else of the kernel's shared
-// memory is in use; returns after the last tile with every thread.  Source:
+constexpr int kTcItemReaders = 1 + 2 + 8;   // issuer, cleaners, softmax warps
+
+// Everything that needs no input: barriers and tensor memory.  Called by all threads before the dependency
+// wait, so that it overlaps the end of the kernel before.
+template <int D, typename Item>
+__device__ __forceinline__ void flash_tc_setup(uint8_t* smem, TcShared<Item>* sh, const int* status) {
+  using L = TcLayout<D>;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::offBar);
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 2; ++i) {
+      ptx::mbar_init(bars + i, 1);                        // query tile full, empty
+      ptx::mbar_init(bars + 4 + i, 1);                    // item full
+      ptx::mbar_init(bars + 6 + i, kTcItemReaders);       // item empty
+    }
+    ptx::mbar_init(bars + 2, 2);                          // clean
+    ptx::mbar_init(bars + 3, 1);                          // to clean
+    uint64_t* full = bars + 8;
+    for (int i = 0; i < L::kPairs; ++i) {
+      ptx::mbar_init(full + i, 2);
+      ptx::mbar_init(full + L::kPairs + i, 1);
+    }
+    uint64_t* s = full + 2 * L::kPairs;
+    for (int h = 0; h < 2; ++h) {
+      ptx::mbar_init(s + h, 1);
+      ptx::mbar_init(s + 2 + 2 * h, 4);                   // one arrival per warp
+      ptx::mbar_init(s + 3 + 2 * h, 4);
+      ptx::mbar_init(s + 6 + h, 1);
+    }
+    ptx::fence_barrier_init();
+    // the status word is the caller's and no kernel that still runs clears it: readable here
+    sh->abort = *reinterpret_cast<const volatile int*>(status) != 0 ? 1 : 0;
+  }
+  if (threadIdx.x < 32) {
+    ptx::tmem_alloc(&sh->tmem, 512);
+    ptx::tmem_relinquish();
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::tc_fence_after();
+}
+
+// Called by all 384 threads after flash_tc_setup and the dependency wait; returns with every thread after
+// the last item.  Source:
+//   struct Item                   plain data
+//   bool find(k, lane, item)      whole warp: the CTA's k-th item; false: there is none
+//   void set(item)                all that follows is about this item
 //   int  tiles(h)                 shared: tiles of block h; streams: all tiles (h ignored)
-//   int  q_bytes(h)               bytes load_q(h) brings (both halves)
+//   int  q_bytes(h)               bytes load_q(h) brings
 //   void load_q(h, dst, bar)      issue the loads of block h's query tile
 //   void load(t, is_v, dst, bar)  issue the loads of a K or V tile (kTile bytes)
 //   int  row_key(h, row)          what last() needs of a row, worked out once
@@ -80,86 +132,100 @@ struct TcShared {
 //   int  clean(t)                 -1: nothing to clean; else rows of tile t that somebody sees
 //   bool scan()                   whether rows below clean(t) are searched for non-finite elements
 //   int  note_slot(t)             which dirty[] entry a cleaned tile uses
-//   void store(h, row, seen, m, l, read)  one finished row per thread, called by whole warps; seen: the
-//                                 block had tiles; read(c, v): columns 32 c .. of O (warp-wide)
+//   void store(h, row, seen, m, l, dirty, read)  one finished row per thread, called by whole warps; seen:
+//                                 the block had tiles; dirty: noted key rows or null; read(c, v): columns
+//                                 32 c .. of O (warp-wide)
 template <int D, bool kShared, typename Source>
-__device__ __forceinline__ void flash_tc(const Source& src, uint8_t* smem, TcShared* sh, float scale_log2e, int* status) {
+__device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<typename Source::Item>* sh, float scale_log2e,
+                                         int* status) {
   using L = TcLayout<D>;
   constexpr int kRing = L::kRing, kPairs = L::kPairs, kLead = kShared ? 1 : 2;
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::offBar);
-  uint64_t *bar_q = bars, *bar_k0_full = bars + 1, *bar_k0_empty = bars + 2, *bar_clean = bars + 3, *bar_to_clean = bars + 4;
-  uint64_t *bar_full = bars + 5, *bar_empty = bar_full + kPairs;
+  uint64_t *bar_q = bars, *bar_q_empty = bars + 1, *bar_clean = bars + 2, *bar_to_clean = bars + 3;
+  uint64_t *bar_item = bars + 4, *bar_item_empty = bars + 6, *bar_full = bars + 8, *bar_empty = bar_full + kPairs;
   uint64_t *bar_s = bar_empty + kPairs, *bar_p = bar_s + 2, *bar_pv = bar_p + 4;
   volatile int* abort_flag = &sh->abort;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int n0 = src.tiles(0), n1 = kShared ? src.tiles(1) : 0;
-  const int nt = kShared ? max(n0, n1) : n0;                 // tiles brought in
-  const int lead = min(kLead, nt);
-  // first load of tile t's K, and V, in ring order: the leading K tiles, then (V_m, K_m+lead) pairs
-  auto k_load = [&](int t) { return t < kLead ? t : kLead + 2 * (t - kLead) + 1; };
-  auto v_load = [&](int t) { return kLead + 2 * t; };
-
-  if (tid == 0) {
-    ptx::mbar_init(bar_q, 1);
-    ptx::mbar_init(bar_k0_full, 1);
-    ptx::mbar_init(bar_k0_empty, 1);
-    ptx::mbar_init(bar_clean, 2);
-    ptx::mbar_init(bar_to_clean, 1);
-    for (int i = 0; i < kPairs; ++i) {
-      ptx::mbar_init(bar_full + i, 2);
-      ptx::mbar_init(bar_empty + i, 1);
-    }
-    for (int h = 0; h < 2; ++h) {
-      ptx::mbar_init(bar_s + h, 1);
-      ptx::mbar_init(bar_p + 2 * h, 4);
-      ptx::mbar_init(bar_p + 2 * h + 1, 4);
-      ptx::mbar_init(bar_pv + h, 1);
-    }
-    ptx::fence_barrier_init();
-    sh->abort = *reinterpret_cast<volatile int*>(status) != 0 ? 1 : 0;
-    for (int i = 0; i < 8; ++i) sh->dirty[i >> 2][i & 3] = 0;
-    sh->any_dirty = 0;
-  }
-  if (warp == 0) {
-    ptx::tmem_alloc(&sh->tmem, 512);
-    ptx::tmem_relinquish();
-  }
-  ptx::tc_fence_before();
-  __syncthreads();
-  ptx::tc_fence_after();
   const uint32_t tmem_base = sh->tmem;
+  // Loads of an item in ring order: the leading K tiles (1, or one per stream), then V_m and, if there is
+  // one, K_m+lead for every tile m.  Groups: the leading tiles, then one per m.
+  auto v_load = [&](int m, int nt) { const int lead = min(kLead, nt); return lead + m + min(m, nt - lead); };
+  auto k_load = [&](int t, int nt) { return t < kLead ? t : v_load(t - kLead, nt) + 1; };
+  auto warp_wait = [&](uint64_t* bar, uint32_t parity) -> bool {
+    return __all_sync(0xffffffffu, ptx::mbar_wait(bar, parity, abort_flag));
+  };
+  // The k-th item as the other roles see it; false after the last one, or if a wait gave up.
+  auto next_item = [&](int k) -> bool {
+    if (!warp_wait(bar_item + (k & 1), uint32_t(k >> 1) & 1u)) return false;
+    if (!sh->valid[k & 1]) return false;
+    src.set(sh->item[k & 1]);
+    return true;
+  };
+  auto item_done = [&](int k) {
+    __syncwarp();
+    if (lane == 0) ptx::mbar_arrive(bar_item_empty + (k & 1));
+  };
 
   if (warp < 4) {
     ptx::reg_dealloc<kTcRegsLean>();
     if (*abort_flag) {
       // a status word that was already set: do nothing
     } else if (warp == 0) {
-      // ------------------------------------------------------------- producer
-      if (lane == 0) {
-        ptx::mbar_arrive_expect_tx(bar_q, uint32_t(src.q_bytes(0) + (kShared && n1 > 0 ? src.q_bytes(1) : 0)));
-        src.load_q(0, smem + L::offQ, bar_q);
-        if (kShared && n1 > 0) src.load_q(1, smem + L::offQ + L::kTile, bar_q);
-        ptx::mbar_arrive_expect_tx(bar_k0_full, uint32_t(lead * L::kTile));
-        for (int t = 0; t < lead; ++t) src.load(t, false, smem + L::offKV + t * L::kTile, bar_k0_full);
-        bool ok = true;
-        for (int m = 0; m < nt && ok; ++m) {
+      // ------------------------------------------------------------- producer: finds the items, brings the tiles
+      int slot = 0;                   // ring slot of the next load
+      int group = 0;                  // its group, counted over all items
+      int group_of[kRing];            // group of the tile a slot holds
 #pragma unroll
-          for (int is_k = 0; is_k < 2; ++is_k) {
-            const int t = is_k ? m + kLead : m, n = kLead + 2 * m + is_k;
-            if (t >= nt) {                                   // no such K tile: its barrier still expects two arrivals
-              ptx::mbar_arrive(bar_full + m % kPairs);
-              continue;
-            }
-            if (n >= kRing) {                                // the slot's previous tile must have been consumed
-              const int r = n - kRing;
-              if (r < kLead) ok = ptx::mbar_wait(bar_k0_empty, 0, abort_flag);
-              else ok = ptx::mbar_wait(bar_empty + ((r - kLead) >> 1) % kPairs, uint32_t(((r - kLead) >> 1) / kPairs) & 1u, abort_flag);
+      for (int i = 0; i < kRing; ++i) group_of[i] = -1;
+      bool ok = true;
+      auto wait_group = [&](int g) { return ptx::mbar_wait(bar_empty + g % kPairs, uint32_t(g / kPairs) & 1u, abort_flag); };
+      for (int k = 0; ok; ++k) {
+        typename Source::Item item;
+        const bool have = src.find(k, lane, item);
+        if (k >= 2) ok = warp_wait(bar_item_empty + (k & 1), uint32_t((k >> 1) - 1) & 1u);
+        if (!ok) break;
+        if (lane == 0) {
+          sh->valid[k & 1] = have ? 1 : 0;
+          sh->item[k & 1] = item;
+          for (int i = 0; i < 8; ++i) sh->dirty[k & 1][i >> 2][i & 3] = 0;
+          sh->any_dirty[k & 1] = 0;
+          ptx::mbar_arrive(bar_item + (k & 1));
+        }
+        if (!have) break;
+        src.set(item);
+        if (lane == 0) {
+          const int n0 = src.tiles(0), n1 = kShared ? src.tiles(1) : 0, nt = kShared ? max(n0, n1) : n0;
+          const bool two = kShared && n1 > 0;
+          if (k > 0) ok = ptx::mbar_wait(bar_q_empty, uint32_t(k - 1) & 1u, abort_flag);
+          if (ok) {
+            ptx::mbar_arrive_expect_tx(bar_q, uint32_t(src.q_bytes(0) + (two ? src.q_bytes(1) : 0)));
+            src.load_q(0, smem + L::offQ, bar_q);
+            if (two) src.load_q(1, smem + L::offQ + L::kTile, bar_q);
+          }
+          for (int m = -1; m < nt && ok; ++m, ++group) {     // group m: V_m and K_m+lead; m = -1: the leading K tiles
+            if (group >= kPairs) ok = wait_group(group - kPairs);
+            uint64_t* full = bar_full + group % kPairs;
+#pragma unroll
+            for (int j = 0; j < 2 && ok; ++j) {
+              const bool is_v = m >= 0 && j == 0;
+              const int t = m < 0 ? j : is_v ? m : m + kLead;
+              if (t >= nt || (m < 0 && j >= kLead)) {        // no such tile: the barrier still expects two arrivals
+                ptx::mbar_arrive(full);
+                continue;
+              }
+              int held = -1;
+#pragma unroll
+              for (int i = 0; i < kRing; ++i)
+                if (i == slot) { held = group_of[i]; group_of[i] = group; }
+              if (held >= 0) ok = wait_group(held);          // the slot's previous tile must have been consumed
               if (!ok) break;
+              ptx::mbar_arrive_expect_tx(full, uint32_t(L::kTile));
+              src.load(t, is_v, smem + L::offKV + slot * L::kTile, full);
+              slot = slot + 1 == kRing ? 0 : slot + 1;
             }
-            ptx::mbar_arrive_expect_tx(bar_full + m % kPairs, uint32_t(L::kTile));
-            src.load(t, !is_k, smem + L::offKV + (n % kRing) * L::kTile, bar_full + m % kPairs);
           }
         }
+        ok = __all_sync(0xffffffffu, ok);
       }
     } else if (warp == 1) {
       // ------------------------------------------------------------- MMA issuer (whole warp, one elected lane issues)
@@ -168,23 +234,24 @@ __device__ __forceinline__ void flash_tc(const Source& src, uint8_t* smem, TcSha
       const uint64_t dq = ptx::smem_desc_sw128(ptx::smem_u32(smem + L::offQ), 16, 1024);
       const uint64_t dk = ptx::smem_desc_sw128(ptx::smem_u32(smem + L::offKV), 16, 1024);             // K: K-major B
       const uint64_t dv = ptx::smem_desc_sw128(ptx::smem_u32(smem + L::offKV), kTcHalfBytes, 1024);   // V: MN-major B
-      auto wait = [&](uint64_t* bar, uint32_t parity) -> bool {
-        return __all_sync(0xffffffffu, ptx::mbar_wait(bar, parity, abort_flag));
-      };
+      int base = 0, group = 0;               // first ring slot and group of the item
+      uint32_t cleaned = 0, tile_count[2] = {0, 0};
+      auto slot_of = [&](int n) { return (base + n) % kRing; };
       auto issue_s = [&](int h, int n) {
         const uint64_t a0 = dq + (kShared ? uint64_t(uint32_t(h * L::kTile) >> 4) : 0ull);
-        const uint64_t b0 = dk + uint64_t(uint32_t((n % kRing) * L::kTile) >> 4);
+        const uint64_t b0 = dk + uint64_t(uint32_t(slot_of(n) * L::kTile) >> 4);
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk) {
           const uint32_t off = (uint32_t(kk >> 2) * kTcHalfBytes + uint32_t(kk & 3) * 32u) >> 4;
           ptx::umma_ss_elect(tmem_base + h * 128u, a0 + off, b0 + off, idesc_s, kk > 0);
         }
       };
-      auto issue_pv = [&](int h, int n, bool acc, uint32_t parity) -> bool {
-        const uint64_t b0 = dv + uint64_t(uint32_t((n % kRing) * L::kTile) >> 4);
+      auto issue_pv = [&](int h, int n, bool acc) -> bool {
+        const uint64_t b0 = dv + uint64_t(uint32_t(slot_of(n) * L::kTile) >> 4);
+        const uint32_t parity = (h == 0 ? tile_count[0]++ : tile_count[1]++) & 1u;
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-          if (!wait(bar_p + 2 * h + c, parity)) return false;
+          if (!warp_wait(bar_p + 2 * h + c, parity)) return false;
           ptx::tc_fence_after();
 #pragma unroll
           for (int kk = (c == 0 ? 0 : kTcPSplit); kk < (c == 0 ? kTcPSplit : kTcKeys / 16); ++kk)
@@ -193,99 +260,117 @@ __device__ __forceinline__ void flash_tc(const Source& src, uint8_t* smem, TcSha
         }
         return true;
       };
-      uint32_t cleaned = 0;
-      bool ok = nt > 0 && wait(bar_q, 0) && wait(bar_k0_full, 0);
-      if (ok) {
+      for (int k = 0; next_item(k); ++k) {
+        const int n0 = src.tiles(0), n1 = kShared ? src.tiles(1) : 0, nt = kShared ? max(n0, n1) : n0;
+        bool ok = warp_wait(bar_q, uint32_t(k) & 1u) && warp_wait(bar_full + group % kPairs, uint32_t(group / kPairs) & 1u);
+        if (!ok) break;
         ptx::tc_fence_after();
         for (int h = 0; h < 2; ++h)
           if (kShared ? (h == 0 ? n0 : n1) > 0 : h < nt) {
             issue_s(h, kShared ? 0 : h);
             ptx::umma_commit_elect(bar_s + h);
           }
-        ptx::umma_commit_elect(bar_k0_empty);
-      }
-      for (int t = 0; t < nt && ok; ++t) {
-        ok = wait(bar_full + t % kPairs, uint32_t(t / kPairs) & 1u);
-        if (ok && src.clean(t) >= 0) {
-          if (lane == 0) ptx::mbar_arrive(bar_to_clean);
-          ok = wait(bar_clean, cleaned++ & 1u);
-        }
-        if (kShared) {
-          for (int h = 0; h < 2 && ok; ++h) {
-            const int nh = h == 0 ? n0 : n1;
-            if (t >= nh) continue;
-            ok = issue_pv(h, v_load(t), t > 0, uint32_t(t) & 1u);
-            if (!ok) break;
-            if (t + 1 < nh) issue_s(h, k_load(t + 1));
-            ptx::umma_commit_elect(t + 1 < nh ? bar_s + h : bar_pv + h);   // S ready implies PV done
+        if (nt <= kLead) ptx::umma_commit_elect(bar_q_empty);      // that was the last use of the query tile
+        ptx::umma_commit_elect(bar_empty + group % kPairs);
+        ++group;
+        for (int t = 0; t < nt && ok; ++t, ++group) {
+          ok = warp_wait(bar_full + group % kPairs, uint32_t(group / kPairs) & 1u);
+          if (ok && src.clean(t) >= 0) {
+            if (lane == 0) ptx::mbar_arrive(bar_to_clean);
+            ok = warp_wait(bar_clean, cleaned++ & 1u);
           }
-        } else {
-          const int h = t & 1;
-          if (ok) ok = issue_pv(h, v_load(t), t > 1, uint32_t(t >> 1) & 1u);
+          if (kShared) {
+            for (int h = 0; h < 2 && ok; ++h) {
+              const int nh = h == 0 ? n0 : n1;
+              if (t >= nh) continue;
+              ok = issue_pv(h, v_load(t, nt), t > 0);
+              if (!ok) break;
+              if (t + 1 < nh) issue_s(h, k_load(t + 1, nt));
+              ptx::umma_commit_elect(t + 1 < nh ? bar_s + h : bar_pv + h);   // S ready implies PV done
+            }
+          } else {
+            const int h = t & 1;
+            if (ok) ok = issue_pv(h, v_load(t, nt), t > 1);
+            if (!ok) break;
+            if (t + 2 < nt) issue_s(h, k_load(t + 2, nt));
+            ptx::umma_commit_elect(t + 2 < nt ? bar_s + h : bar_pv + h);
+          }
           if (!ok) break;
-          if (t + 2 < nt) issue_s(h, k_load(t + 2));
-          ptx::umma_commit_elect(t + 2 < nt ? bar_s + h : bar_pv + h);
+          if (t + 1 + kLead == nt) ptx::umma_commit_elect(bar_q_empty);      // the last scores have been issued
+          ptx::umma_commit_elect(bar_empty + group % kPairs);
         }
-        if (ok) ptx::umma_commit_elect(bar_empty + t % kPairs);
+        if (!ok) break;
+        base = slot_of(2 * nt);
+        item_done(k);
       }
     } else {
       // ------------------------------------------------------------- cleaning of value tiles (warps 2 and 3: 64 rows each)
       // They start on a tile when the issuer, having seen it arrive, says so: the issuer then waits for them,
       // so neither can be a phase of the tile's barrier behind or ahead of the other.
-      bool ok = true;
       uint32_t cleaned = 0;
-      for (int t = 0; t < nt && ok; ++t) {
-        const int seen = src.clean(t);
-        if (seen < 0) continue;
-        ok = __all_sync(0xffffffffu, ptx::mbar_wait(bar_to_clean, cleaned++ & 1u, abort_flag)) &&
-             __all_sync(0xffffffffu, ptx::mbar_wait(bar_full + t % kPairs, uint32_t(t / kPairs) & 1u, abort_flag));
-        if (!ok) break;
-        uint8_t* tile = smem + L::offKV + (v_load(t) % kRing) * L::kTile;
-        // 16-byte piece i of the warp's 64 rows; the swizzle only permutes the pieces within a row
-        for (int half = 0; half < L::NH; ++half)
+      int base = 0, group = 0;
+      for (int k = 0; next_item(k); ++k) {
+        const int n0 = src.tiles(0), n1 = kShared ? src.tiles(1) : 0, nt = kShared ? max(n0, n1) : n0;
+        bool ok = true;
+        for (int t = 0; t < nt && ok; ++t) {
+          const int seen = src.clean(t);
+          if (seen < 0) continue;
+          ok = warp_wait(bar_to_clean, cleaned++ & 1u) &&
+               warp_wait(bar_full + (group + 1 + t) % kPairs, uint32_t((group + 1 + t) / kPairs) & 1u);
+          if (!ok) break;
+          uint8_t* tile = smem + L::offKV + (base + v_load(t, nt)) % kRing * L::kTile;
+          // 16-byte piece i of the warp's 64 rows; the swizzle only permutes the pieces within a row
+          for (int half = 0; half < L::NH; ++half)
 #pragma unroll 4
-          for (int i = lane; i < 64 * 8; i += 32) {
-            const int r = (warp - 2) * 64 + (i >> 3);
-            uint4* p = reinterpret_cast<uint4*>(tile + half * kTcHalfBytes + r * 128 + (i & 7) * 16);
-            if (r >= seen) {
-              *p = make_uint4(0, 0, 0, 0);
-            } else if (src.scan()) {
-              uint4 v = *p;
-              uint32_t* w = &v.x;
-              bool hit = false;
+            for (int i = lane; i < 64 * 8; i += 32) {
+              const int r = (warp - 2) * 64 + (i >> 3);
+              uint4* p = reinterpret_cast<uint4*>(tile + half * kTcHalfBytes + r * 128 + (i & 7) * 16);
+              if (r >= seen) {
+                *p = make_uint4(0, 0, 0, 0);
+              } else if (src.scan()) {
+                uint4 v = *p;
+                uint32_t* w = &v.x;
+                bool hit = false;
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                if ((w[e] & 0x7f80u) == 0x7f80u) { w[e] &= 0xffff0000u; hit = true; }
-                if ((w[e] & 0x7f800000u) == 0x7f800000u) { w[e] &= 0xffffu; hit = true; }
-              }
-              if (hit) {
-                *p = v;
-                atomicOr(&sh->dirty[src.note_slot(t)][r >> 5], 1u << (r & 31));
-                sh->any_dirty = 1;
+                for (int e = 0; e < 4; ++e) {
+                  if ((w[e] & 0x7f80u) == 0x7f80u) { w[e] &= 0xffff0000u; hit = true; }
+                  if ((w[e] & 0x7f800000u) == 0x7f800000u) { w[e] &= 0xffffu; hit = true; }
+                }
+                if (hit) {
+                  *p = v;
+                  atomicOr(&sh->dirty[k & 1][src.note_slot(t)][r >> 5], 1u << (r & 31));
+                  sh->any_dirty[k & 1] = 1;
+                }
               }
             }
-          }
-        ptx::fence_proxy_async_smem();                       // the product reads the tile through the async proxy
-        __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(bar_clean);
+          ptx::fence_proxy_async_smem();                     // the product reads the tile through the async proxy
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive(bar_clean);
+        }
+        if (!ok) break;
+        base = (base + 2 * nt) % kRing;
+        group += nt + 1;
+        item_done(k);
       }
     }
   } else {
     ptx::reg_alloc<kTcRegsSoftmax>();
     // ------------------------------------------------------------- softmax, one row per thread
     const int h = (warp - 4) >> 2;
-    const int mine = kShared ? (h == 0 ? n0 : n1) : (nt - h + 1) / 2;   // tiles of this block / stream
-    if (!*abort_flag) {
-      const int quarter = warp & 3, row = quarter * 32 + lane;
-      const uint32_t lane_addr = tmem_base + (uint32_t(quarter * 32) << 16);
-      const uint32_t s_addr = lane_addr + h * 128u, o_addr = lane_addr + 256u + uint32_t(h * D);
+    const int quarter = warp & 3, row = quarter * 32 + lane;
+    const uint32_t lane_addr = tmem_base + (uint32_t(quarter * 32) << 16);
+    const uint32_t s_addr = lane_addr + h * 128u, o_addr = lane_addr + 256u + uint32_t(h * D);
+    const uint64_t scale2 = ptx::pack2(scale_log2e, scale_log2e);
+    uint32_t tile_count = 0, item_count = 0;
+    for (int k = 0; !*abort_flag && next_item(k); ++k) {
+      const int nt = src.tiles(kShared ? h : 0);
+      const int mine = kShared ? nt : (nt - h + 1) / 2;      // tiles of this block / stream
       const int row_key = src.row_key(h, row);
       float m_run = -INFINITY, m_used = -INFINITY, l = 0.f;
-      const uint64_t scale2 = ptx::pack2(scale_log2e, scale_log2e);
       bool ok = true;
       for (int it = 0; it < mine; ++it) {
         const int hi = src.last(row_key, kShared ? it : 2 * it + h);
-        ok = __all_sync(0xffffffffu, ptx::mbar_wait(bar_s + h, uint32_t(it) & 1u, abort_flag));
+        ok = warp_wait(bar_s + h, tile_count++ & 1u);
         if (!ok) break;
         ptx::tc_fence_after();
         uint32_t v[kTcKeys];
@@ -362,14 +447,16 @@ __device__ __forceinline__ void flash_tc(const Source& src, uint8_t* smem, TcSha
         ptx::unpack2(sum2[1], s2, s3);
         l += (s0 + s1) + (s2 + s3);
       }
-      if (ok && mine > 0) ok = __all_sync(0xffffffffu, ptx::mbar_wait(bar_pv + h, 0, abort_flag));   // committed after the last PV
-      if (ok) {
-        ptx::tc_fence_after();
-        src.store(h, row, mine > 0, m_used, l, [&](int c, uint32_t (&v)[32]) {
-          ptx::tmem_ld32(o_addr + c * 32, v);
-          ptx::tc_wait_ld();
-        });
-      }
+      if (ok && mine > 0) ok = warp_wait(bar_pv + h, item_count++ & 1u);   // committed after the last PV
+      if (!ok) break;
+      ptx::tc_fence_after();
+      src.store(h, row, mine > 0, m_used, l, sh->any_dirty[k & 1] ? &sh->dirty[k & 1][0][0] : nullptr,
+                [&](int c, uint32_t (&v)[32]) {
+                  ptx::tmem_ld32(o_addr + c * 32, v);
+                  ptx::tc_wait_ld();
+                });
+      ptx::tc_fence_before();       // the reads of O precede the next item's products (through the P barriers)
+      item_done(k);
     }
   }
   // ------------------------------------------------------------- teardown

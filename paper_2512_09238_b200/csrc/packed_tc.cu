@@ -8,15 +8,36 @@
 namespace tca {
 namespace {
 
+struct PackedItem {
+  int64_t row0;
+  int len, p0, kvh;
+};
+
 template <int D>
 struct PackedTcSrc {
+  using Item = PackedItem;
   const CUtensorMap *mq, *mk, *mv;
   const __nv_bfloat16* V;
   __nv_bfloat16* O;
   const PackedArgs* a;
-  TcShared* sh;
+  int G, P, wide, max_tiles, unit_major;
   int64_t row0;
-  int len, p0, kvh, G, P;
+  int len, p0, kvh;
+
+  // Items lie longest first; the CTAs take them in turn, every other round in reverse, so that the CTA that
+  // got the longest of one round gets the shortest of the next.  Two orders, see launch_packed_tc.
+  __device__ __forceinline__ bool find(int k, int lane, Item& it) const {
+    const int n = int(gridDim.x);
+    const int i = k * n + ((k & 1) ? n - 1 - int(blockIdx.x) : int(blockIdx.x));
+    if (i >= max_tiles * a->n_kv_heads) return false;
+    it.kvh = unit_major ? i / max_tiles : i % a->n_kv_heads;
+    int seq, tile;
+    if (!packed_find(*a, unit_major ? i % max_tiles : i / a->n_kv_heads, 2 * P, lane, seq, tile)) return false;
+    packed_bounds(*a, seq, it.row0, it.len);
+    it.p0 = tile * 2 * P;
+    return true;
+  }
+  __device__ __forceinline__ void set(const Item& it) { row0 = it.row0; len = it.len; p0 = it.p0; kvh = it.kvh; }
 
   __device__ __forceinline__ int last_pos(int h) const { return min(p0 + (h + 1) * P, len) - 1; }
   __device__ __forceinline__ int tiles(int h) const { return p0 + h * P < len ? last_pos(h) / kTcKeys + 1 : 0; }
@@ -40,11 +61,10 @@ struct PackedTcSrc {
   __device__ __forceinline__ int note_slot(int t) const { return t - p0 / kTcKeys; }
 
   template <typename Read>
-  __device__ __forceinline__ void store(int h, int row, bool seen, float, float l, Read read) const {
+  __device__ __forceinline__ void store(int h, int row, bool seen, float, float l, const uint32_t* dirty, Read read) const {
     if (!seen) return;
     const int pos = p0 + h * P + row / G;
     const bool mine = row < G * P && pos < len;
-    const bool dirty = sh->any_dirty != 0;
     const float inv = 1.f / l;
     __nv_bfloat16* out = O + (kvh * G + row % G) * a->o.head + (row0 + pos) * a->o.row;
 #pragma unroll 1
@@ -56,7 +76,7 @@ struct PackedTcSrc {
       for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * inv);
       if (dirty) {   // non-finite values of masked tiles, kept out of the product, reach the rows that see them
         for (int w = 0; w < 8; ++w)
-          for (uint32_t bits = sh->dirty[w >> 2][w & 3]; bits; bits &= bits - 1) {
+          for (uint32_t bits = dirty[w]; bits; bits &= bits - 1) {
             const int key = (p0 / kTcKeys + (w >> 2)) * kTcKeys + (w & 3) * 32 + __ffs(bits) - 1;
             if (key > pos) break;
             const __nv_bfloat16* src = V + kvh * a->v.head + (row0 + key) * a->v.row + c * 32;
@@ -68,13 +88,18 @@ struct PackedTcSrc {
           }
       }
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        uint4 w;
-        w.x = ptx::pack_bf16x2(__uint_as_float(v[q * 8 + 0]), __uint_as_float(v[q * 8 + 1]));
-        w.y = ptx::pack_bf16x2(__uint_as_float(v[q * 8 + 2]), __uint_as_float(v[q * 8 + 3]));
-        w.z = ptx::pack_bf16x2(__uint_as_float(v[q * 8 + 4]), __uint_as_float(v[q * 8 + 5]));
-        w.w = ptx::pack_bf16x2(__uint_as_float(v[q * 8 + 6]), __uint_as_float(v[q * 8 + 7]));
-        *reinterpret_cast<uint4*>(out + c * 32 + q * 8) = w;
+      for (int q = 0; q < 2; ++q) {
+        uint32_t w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          w[e] = ptx::pack_bf16x2(__uint_as_float(v[q * 16 + 2 * e]), __uint_as_float(v[q * 16 + 2 * e + 1]));
+        __nv_bfloat16* at = out + c * 32 + q * 16;
+        if (wide) {
+          ptx::st_global_32(at, w);
+        } else {
+          *reinterpret_cast<uint4*>(at) = make_uint4(w[0], w[1], w[2], w[3]);
+          *reinterpret_cast<uint4*>(at + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+        }
       }
     }
   }
@@ -84,35 +109,27 @@ template <int D>
 __global__ void __launch_bounds__(kTcThreads, 1)
 packed_tc_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
                  const __grid_constant__ CUtensorMap mv, const __nv_bfloat16* __restrict__ V,
-                 const __grid_constant__ PackedArgs args, int max_tiles, int unit_major, float scale_log2e,
+                 const __grid_constant__ PackedArgs args, int max_tiles, int unit_major, int wide, float scale_log2e,
                  __nv_bfloat16* __restrict__ O, int* __restrict__ status) {
   extern __shared__ uint8_t packed_tc_smem[];
-  __shared__ TcShared sh;
-  __shared__ int found[2];
+  __shared__ TcShared<PackedItem> sh;
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(packed_tc_smem) + 1023) & ~uintptr_t(1023));
   if (threadIdx.x == 0) {
     ptx::tma_prefetch_desc(&mq);
     ptx::tma_prefetch_desc(&mk);
     ptx::tma_prefetch_desc(&mv);
   }
+  flash_tc_setup<D>(smem, &sh, status);
   pdl_wait();
   pdl_launch_dependents();
   PackedTcSrc<D> src;
+  src.mq = &mq; src.mk = &mk; src.mv = &mv;
+  src.V = V; src.O = O; src.a = &args;
   src.G = args.n_q_heads / args.n_kv_heads;
   src.P = kTcRows / src.G;
-  src.kvh = unit_major ? int(blockIdx.x) / max_tiles : int(blockIdx.x) % args.n_kv_heads;
-  const int item = unit_major ? int(blockIdx.x) % max_tiles : int(blockIdx.x) / args.n_kv_heads;
-  if (threadIdx.x < 32) {
-    int seq = -1, tile = 0;
-    if (!packed_find(args, item, 2 * src.P, threadIdx.x, seq, tile)) seq = -1;
-    if (threadIdx.x == 0) { found[0] = seq; found[1] = tile; }
-  }
-  __syncthreads();
-  if (found[0] < 0) return;
-  packed_bounds(args, found[0], src.row0, src.len);
-  src.p0 = found[1] * 2 * src.P;
-  src.mq = &mq; src.mk = &mk; src.mv = &mv;
-  src.V = V; src.O = O; src.a = &args; src.sh = &sh;
+  src.wide = wide;
+  src.max_tiles = max_tiles;
+  src.unit_major = unit_major;
   flash_tc<D, true>(src, smem, &sh, scale_log2e, status);
 }
 
@@ -123,7 +140,8 @@ int launch_packed_tc(const tca_params* prm, const void* Q, const void* K, const 
                      void* ws, cudaStream_t s) {
   const int G = a.n_q_heads / a.n_kv_heads, P = kTcRows / G;
   const int64_t max_tiles = packed_max_tiles(a.rows, a.n_seq, 2 * P);
-  if (max_tiles * a.n_kv_heads >= (int64_t(1) << 31)) return TCA_ERR_UNSUPPORTED;
+  if (max_tiles * a.n_kv_heads >= (int64_t(1) << 31) - 65536)   // item numbers, one round past the end, are 32-bit
+    return TCA_ERR_UNSUPPORTED;
   CUtensorMap mq, mk, mv;
   if (!encode_map_3d(&mq, Q, D, a.n_q_heads, a.rows, a.q.head, a.q.row, G, P) ||
       !encode_map_3d(&mk, K, D, a.rows, a.n_kv_heads, a.k.row, a.k.head, kTcKeys, 1) ||
@@ -134,8 +152,10 @@ int launch_packed_tc(const tca_params* prm, const void* Q, const void* K, const 
   // Longest tiles first over all heads balances best, but then the resident CTAs read all heads' keys
   // at once; when those do not fit the L2 the heads go one after another.
   const int unit_major = a.rows * a.n_kv_heads * D * 4 > l2_bytes() / 2 ? 1 : 0;
-  return launch_pdl(kern, dim3(unsigned(max_tiles * a.n_kv_heads)), dim3(kTcThreads), size_t(TcLayout<D>::bytes), s, mq, mk,
-                    mv, static_cast<const __nv_bfloat16*>(V), a, int(max_tiles), unit_major,
+  const int wide = aligned(O, 32) && a.o.head % 16 == 0 && a.o.row % 16 == 0 ? 1 : 0;
+  const int64_t items = max_tiles * a.n_kv_heads, sms = sm_count();
+  return launch_pdl(kern, dim3(unsigned(items < sms ? items : sms)), dim3(kTcThreads), size_t(TcLayout<D>::bytes), s, mq, mk,
+                    mv, static_cast<const __nv_bfloat16*>(V), a, int(max_tiles), unit_major, wide,
                     prm->sm_scale * 1.4426950408889634f, static_cast<__nv_bfloat16*>(O), static_cast<int*>(ws));
 }
 

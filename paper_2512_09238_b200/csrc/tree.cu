@@ -127,26 +127,10 @@ struct RowE {   // E = D / 32 consecutive elements per lane
   }
 };
 
-// Running softmax of one query row held by a warp: maximum and sum uniform, E outputs per lane.
-template <int E>
-struct RowState {
-  float m = -INFINITY, l = 0.f;
-  float o[E];
-  __device__ __forceinline__ RowState() {
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = 0.f;
-  }
-  // adds (l2, a) accumulated under the maximum m2
-  __device__ __forceinline__ void add(float m2, float l2, const RowE<E>& a) {
-    const float mn = fmaxf(m, m2), base = (mn == -INFINITY) ? 0.f : mn;
-    const float c = exp2f(m - base), w = exp2f(m2 - base);
-    l = fmaf(l, c, l2 * w);
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = fmaf(o[e], c, a.x[e] * w);
-    m = mn;
-  }
-};
-
+// One warp per query row.  The drafted part comes before the dependency wait: it reads the caller's inputs
+// only, which were complete before the split kernel could start (that kernel triggers this launch after its
+// own wait), so it overlaps the split kernel's end.  Every loop issues its loads ahead of the arithmetic that
+// depends on them: with one row per warp the kernel is bound by latency.
 template <typename T, int D>
 __global__ void __launch_bounds__(kCombineWarps * 32)
 tree_combine_kernel(const T* __restrict__ q, const T* __restrict__ k_draft, const T* __restrict__ v_draft, int n_draft,
@@ -155,73 +139,130 @@ tree_combine_kernel(const T* __restrict__ q, const T* __restrict__ k_draft, cons
                     T* __restrict__ O) {
   constexpr int E = D / 32;
   constexpr int kHeld = TCA_TREE_MAX / 32;
-  pdl_wait();
-  pdl_launch_dependents();
+  constexpr int kBatch = 4;        // drafted tokens whose rows are fetched together
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int r = blockIdx.x * kCombineWarps + warp, u = blockIdx.y, seq = u / n_kv;
-  if (r >= plan.rows) return;
   const int t = r % n_draft;
-  if (n_live && t >= n_live[seq]) return;                   // not drafted: its row of O stays as it was
-  RowE<E> qr;
+  // not a row, or not drafted: its row of O stays as it was
+  const bool live = r < plan.rows && (!n_live || t < n_live[seq]);
+  RowE<E> o, qr;
+#pragma unroll
+  for (int e = 0; e < E; ++e) o.x[e] = 0.f;
+  float m = -INFINITY, l = 0.f;
   const size_t q_at = (size_t(u) * plan.rows + r) * D + lane * E;
-  qr.load(q + q_at);
-  // the path to the root as a bit set: parents lie in the lanes, a hop is one shuffle
-  int par[kHeld];
-  unsigned bits[kHeld];
+  int64_t cached = 0;
+  if (live) {
+    const int64_t* st = state + size_t(u) * TCA_STATE_WORDS;
+    cached = st[TCA_ST_N_GLOBAL] + st[TCA_ST_N_TAIL];
+    qr.load(q + q_at);
+    // the path to the root as a bit set: parents lie in the lanes, a hop is one shuffle
+    int par[kHeld];
+    unsigned bits[kHeld];
 #pragma unroll
-  for (int i = 0; i < kHeld; ++i) {
-    par[i] = i * 32 + lane < n_draft ? parent[size_t(seq) * n_draft + i * 32 + lane] : -1;
-    bits[i] = 0;
-  }
-  for (int cur = t; cur >= 0;) {
-    int p = -1;
+    for (int i = 0; i < kHeld; ++i) {
+      par[i] = i * 32 + lane < n_draft ? parent[size_t(seq) * n_draft + i * 32 + lane] : -1;
+      bits[i] = 0;
+    }
+    for (int cur = t; cur >= 0;) {
+      int p = -1;
 #pragma unroll
-    for (int i = 0; i < kHeld; ++i)
-      if (i == (cur >> 5)) {
-        bits[i] |= 1u << (cur & 31);
-        p = par[i];
+      for (int i = 0; i < kHeld; ++i)
+        if (i == (cur >> 5)) {
+          bits[i] |= 1u << (cur & 31);
+          p = par[i];
+        }
+      p = __shfl_sync(0xffffffffu, p, cur & 31);
+      if constexpr (kDebugBounds) {
+        if (lane == 0 && (p < -1 || p >= cur)) report_bounds_ws(ws.status, kBoundsDraftIndex, p);
       }
-    p = __shfl_sync(0xffffffffu, p, cur & 31);
-    if constexpr (kDebugBounds) {
-      if (lane == 0 && (p < -1 || p >= cur)) report_bounds_ws(ws.status, kBoundsDraftIndex, p);
+      cur = p < cur ? p : -1;                                // a parent that does not precede its child ends the path
     }
-    cur = p < cur ? p : -1;                                  // a parent that does not precede its child ends the path
+    const T* kd = k_draft + size_t(u) * n_draft * D + lane * E;
+    const T* vd = v_draft + size_t(u) * n_draft * D + lane * E;
+    bool more = true;
+    while (more) {
+      int a[kBatch];
+      RowE<E> k[kBatch], v[kBatch];
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) {
+        a[b] = -1;
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i)
+          if (a[b] < 0 && bits[i]) {
+            a[b] = i * 32 + __ffs(bits[i]) - 1;
+            bits[i] &= bits[i] - 1;
+          }
+        if (a[b] >= 0) {
+          k[b].load(kd + size_t(a[b]) * D);
+          v[b].load(vd + size_t(a[b]) * D);
+        }
+      }
+      more = a[kBatch - 1] >= 0;
+      float x[kBatch], mn = m;
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) {
+        x[b] = -INFINITY;
+        if (a[b] < 0) continue;                              // uniform
+        float s = 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) s = fmaf(qr.x[e], k[b].x[e], s);
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
+        x[b] = s * scale_log2e;
+        mn = fmaxf(mn, x[b]);
+      }
+      const float base = (mn == -INFINITY) ? 0.f : mn, c = exp2f(m - base);
+      l *= c;
+#pragma unroll
+      for (int e = 0; e < E; ++e) o.x[e] *= c;
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) {
+        if (a[b] < 0) continue;
+        const float w = exp2f(x[b] - base);
+        l += w;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o.x[e] = fmaf(w, v[b].x[e], o.x[e]);
+      }
+      m = mn;
+    }
   }
-  RowState<E> row;
-  const T* kd = k_draft + size_t(u) * n_draft * D + lane * E;
-  const T* vd = v_draft + size_t(u) * n_draft * D + lane * E;
-#pragma unroll
-  for (int i = 0; i < kHeld; ++i)
-    while (bits[i]) {
-      const int a = i * 32 + __ffs(bits[i]) - 1;
-      bits[i] &= bits[i] - 1;
-      RowE<E> k, v;
-      k.load(kd + size_t(a) * D);
-      v.load(vd + size_t(a) * D);
-      float x = 0.f;
-#pragma unroll
-      for (int e = 0; e < E; ++e) x = fmaf(qr.x[e], k.x[e], x);
-#pragma unroll
-      for (int off = 16; off > 0; off >>= 1) x += __shfl_xor_sync(0xffffffffu, x, off);
-      row.add(x * scale_log2e, 1.f, v);
-    }
+  pdl_wait();                 // the partial results come from the split kernel
+  pdl_launch_dependents();
+  if (!live) return;
   // the slices of the unit, in order; a unit whose cache is empty has none
-  const int64_t* st = state + size_t(u) * TCA_STATE_WORDS;
-  const int2 where = st[TCA_ST_N_GLOBAL] + st[TCA_ST_N_TAIL] > 0 ? ws.table[u] : make_int2(0, 0);
+  const int2 where = cached > 0 ? ws.table[u] : make_int2(0, 0);
   const int n = where.y * plan.streams;
   const size_t first = size_t(where.x) * plan.streams;
-#pragma unroll 4
-  for (int c = 0; c < n; ++c) {
-    const size_t at = (first + c) * plan.rows + r;
-    const float2 ml = ws.ml[at];
-    RowE<E> a;
-    a.load(ws.acc + at * D + lane * E);
-    if (ml.x != -INFINITY) row.add(ml.x, ml.y, a);           // a stream without a tile wrote no output
-  }
-  RowE<E> out;
+  for (int c0 = 0; c0 < n; c0 += 32) {                       // statistics of 32 partials at a time, one per lane
+    const int cn = min(32, n - c0);
+    const float2 ml = lane < cn ? ws.ml[(first + c0 + lane) * plan.rows + r] : make_float2(-INFINITY, 0.f);
+    float mn = ml.x;
 #pragma unroll
-  for (int e = 0; e < E; ++e) out.x[e] = row.o[e] / row.l;
-  out.store(O + q_at);
+    for (int off = 16; off > 0; off >>= 1) mn = fmaxf(mn, __shfl_xor_sync(0xffffffffu, mn, off));
+    mn = fmaxf(m, mn);
+    const float base = (mn == -INFINITY) ? 0.f : mn, keep = exp2f(m - base);
+    const bool some = ml.x != -INFINITY;                     // a stream without a tile wrote no output
+    const float w = some ? exp2f(ml.x - base) : 0.f;
+    const unsigned have = __ballot_sync(0xffffffffu, some);
+    l *= keep;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o.x[e] *= keep;
+    const float wl = some ? w * ml.y : 0.f;
+#pragma unroll 8
+    for (int c = 0; c < cn; ++c) {
+      const float wc = __shfl_sync(0xffffffffu, w, c);
+      l += __shfl_sync(0xffffffffu, wl, c);
+      if (!((have >> c) & 1u)) continue;                     // uniform
+      RowE<E> a;
+      a.load(ws.acc + ((first + c0 + c) * plan.rows + r) * D + lane * E);
+#pragma unroll
+      for (int e = 0; e < E; ++e) o.x[e] = fmaf(wc, a.x[e], o.x[e]);
+    }
+    m = mn;
+  }
+#pragma unroll
+  for (int e = 0; e < E; ++e) o.x[e] /= l;
+  o.store(O + q_at);
 }
 
 template <typename T, int D>

@@ -8,16 +8,44 @@
 namespace tca {
 namespace {
 
-template <int D, bool kShared>
-struct TreeTcSrc {
-  const CUtensorMap *mq, *mk, *mv;
+struct TreeItem {
   SliceTiles slice;
   int q_row;        // first query row of this CTA in the flattened query matrix
   int rows;         // query rows of this CTA
-  int n;            // tiles of the slice
-  float* acc;       // partial results: first row of this CTA in the first stream's block
-  float2* ml;
-  size_t stream_stride;   // rows from one stream's block to the next
+  size_t at;        // partial results: its first row in the first stream's block
+};
+
+// One item per CTA: its block of query rows against its slice.
+template <int D, bool kShared>
+struct TreeTcSrc {
+  using Item = TreeItem;
+  const CUtensorMap *mq, *mk, *mv;
+  const int64_t* state;
+  int n_units;
+  int64_t tail_cap;
+  const TreePlan* plan;
+  const TreeWs* ws;
+  SliceTiles slice;
+  int q_row, rows, n;
+  size_t at0;
+
+  __device__ __forceinline__ bool find(int k, int lane, Item& it) const {
+    if (k > 0) return false;
+    const TreeSlice s = tree_find(state, n_units, tail_cap, plan->n_slots, plan->step_rows, plan->min_steps, kTcKeys,
+                                  int(blockIdx.x) / plan->row_blocks, lane);
+    if (s.u < 0) return false;
+    const int rb = int(blockIdx.x) % plan->row_blocks, row0 = rb * plan->rows_per_cta;
+    if (s.part == 0 && rb == 0 && lane == 0) ws->table[s.u] = make_int2(s.base, s.np);
+    it.slice = s.tiles;
+    it.q_row = s.u * plan->rows + row0;
+    it.rows = min(plan->rows_per_cta, plan->rows - row0);
+    it.at = size_t(s.base + s.part) * plan->streams * plan->rows + row0;
+    return true;
+  }
+  __device__ __forceinline__ void set(const Item& it) {
+    slice = it.slice; q_row = it.q_row; rows = it.rows; at0 = it.at;
+    n = slice.n_tiles();
+  }
 
   __device__ __forceinline__ int tiles(int h) const { return kShared && h * kTcRows >= rows ? 0 : n; }
   __device__ __forceinline__ int q_bytes(int) const { return TcLayout<D>::kTile; }
@@ -47,10 +75,10 @@ struct TreeTcSrc {
   __device__ __forceinline__ int note_slot(int) const { return 0; }
 
   template <typename Read>
-  __device__ __forceinline__ void store(int h, int row, bool seen, float m, float l, Read read) const {
+  __device__ __forceinline__ void store(int h, int row, bool seen, float m, float l, const uint32_t*, Read read) const {
     const int r = kShared ? h * kTcRows + row : row;
-    const size_t at = (kShared ? 0 : size_t(h) * stream_stride) + r;
-    if (r < rows) ml[at] = seen ? make_float2(m, l) : make_float2(-INFINITY, 0.f);
+    const size_t at = at0 + (kShared ? 0 : size_t(h) * plan->rows) + r;
+    if (r < rows) ws->ml[at] = seen ? make_float2(m, l) : make_float2(-INFINITY, 0.f);
     if (!seen) return;
 #pragma unroll 1
     for (int c = 0; c < D / 32; ++c) {
@@ -58,8 +86,10 @@ struct TreeTcSrc {
       read(c, v);
       if (r < rows) {
 #pragma unroll
-        for (int k = 0; k < 32; k += 4)
-          *reinterpret_cast<uint4*>(acc + at * D + c * 32 + k) = make_uint4(v[k], v[k + 1], v[k + 2], v[k + 3]);
+        for (int k = 0; k < 32; k += 8) {
+          const uint32_t w[8] = {v[k], v[k + 1], v[k + 2], v[k + 3], v[k + 4], v[k + 5], v[k + 6], v[k + 7]};
+          ptx::st_global_32(ws->acc + at * D + c * 32 + k, w);
+        }
       }
     }
   }
@@ -69,38 +99,25 @@ template <int D, bool kShared>
 __global__ void __launch_bounds__(kTcThreads, 1)
 tree_tc_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
                const __grid_constant__ CUtensorMap mv, const int64_t* __restrict__ state, int n_units, int64_t tail_cap,
-               TreePlan plan, float scale_log2e, TreeWs ws) {
+               const __grid_constant__ TreePlan plan, float scale_log2e, const __grid_constant__ TreeWs ws) {
   extern __shared__ uint8_t tree_tc_smem[];
-  __shared__ TcShared sh;
-  __shared__ TreeSlice slice;
+  __shared__ TcShared<TreeItem> sh;
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(tree_tc_smem) + 1023) & ~uintptr_t(1023));
   if (threadIdx.x == 0) {
     ptx::tma_prefetch_desc(&mq);
     ptx::tma_prefetch_desc(&mk);
     ptx::tma_prefetch_desc(&mv);
   }
+  flash_tc_setup<D>(smem, &sh, ws.status);
   pdl_wait();
   pdl_launch_dependents();
-  if (threadIdx.x < 32) {
-    const TreeSlice s = tree_find(state, n_units, tail_cap, plan.n_slots, plan.step_rows, plan.min_steps, kTcKeys,
-                                  int(blockIdx.x) / plan.row_blocks, threadIdx.x);
-    if (threadIdx.x == 0) slice = s;
-  }
-  __syncthreads();
-  if (slice.u < 0) return;
-  const int rb = int(blockIdx.x) % plan.row_blocks;
-  if (slice.part == 0 && rb == 0 && threadIdx.x == 0) ws.table[slice.u] = make_int2(slice.base, slice.np);
   TreeTcSrc<D, kShared> src;
   src.mq = &mq; src.mk = &mk; src.mv = &mv;
-  src.slice = slice.tiles;
-  src.n = src.slice.n_tiles();
-  const int row0 = rb * plan.rows_per_cta;
-  src.q_row = slice.u * plan.rows + row0;
-  src.rows = min(plan.rows_per_cta, plan.rows - row0);
-  const size_t at = size_t(slice.base + slice.part) * plan.streams * plan.rows + row0;
-  src.acc = ws.acc + at * D;
-  src.ml = ws.ml + at;
-  src.stream_stride = size_t(plan.rows);
+  src.state = state;
+  src.n_units = n_units;
+  src.tail_cap = tail_cap;
+  src.plan = &plan;
+  src.ws = &ws;
   flash_tc<D, kShared>(src, smem, &sh, scale_log2e, ws.status);
 }
 

@@ -33,11 +33,14 @@ def f64(t):
 
 def packed_buffer(seed, heads, rows, d, dtype, layout):
     """[heads, rows, d]: contiguous ("heads"), a view of [rows, heads, d] ("tokens"), or of a wider token-major
-    buffer as a fused projection leaves it ("fused")."""
+    buffer as a fused projection leaves it ("fused"), or rows that are aligned to 16 bytes only ("odd")."""
     if layout == "heads":
         return randn(seed, (heads, rows, d), dtype)
     if layout == "tokens":
         return randn(seed, (rows, heads, d), dtype).transpose(0, 1)
+    if layout == "odd":     # rows 16 bytes longer than needed, starting 16 bytes into the buffer
+        pad = 16 // DT[dtype].itemsize
+        return randn(seed, (heads, rows, d + pad), dtype)[:, :, pad:]
     return randn(seed, (rows, heads + 3, d), dtype)[:, 2:2 + heads].transpose(0, 1)
 
 

@@ -44,11 +44,13 @@ def test_groups(group, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("layout", ["tokens", "fused"])
+@pytest.mark.parametrize("layout", ["tokens", "fused", "odd"])
 @pytest.mark.parametrize("d", [64, 128])
 def test_layouts(layout, d, dtype):
     prm, q, k, v, starts = case([200, 31, 1], 6, 3, d, dtype, layout, 30)
-    o = H.run_packed(prm, q, k, v, starts, out=torch.full_like(q, float("nan")))
+    o = H.packed_buffer(33, 6, q.shape[1], d, dtype, layout)
+    o.fill_(float("nan"))
+    o = H.run_packed(prm, q, k, v, starts, out=o)
     compare(prm, q, k, v, starts, o, dtype)
     # the layout does not change a bit of the result
     c = [x.contiguous() for x in (q, k, v)]
@@ -161,7 +163,7 @@ def test_tensor_cores_agree_with_the_fp32_pipes():
 # ------------------------------------------------------------------ tca_cache_load
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("d", [64, 128])
-@pytest.mark.parametrize("layout", ["heads", "tokens", "fused"])
+@pytest.mark.parametrize("layout", ["heads", "tokens", "fused", "odd"])
 def test_load_places_every_row(layout, d, dtype):
     lens, slots, hkv = [100, 0, 97, 1, 400], np.array([4, 0, 2, 6, 5], dtype=np.int32), 3
     prm = H.params(7, 2 * hkv, hkv, d, dtype, block=32, window=64)
