@@ -51,6 +51,50 @@ constexpr int kTcHalfBytes = 128 * 128;        // 128 rows x 64 bf16: one swizzl
 constexpr float kTcRescale = 8.f;
 constexpr int kTcPSplit = 6;                   // k-steps of 16 keys in the first part of P
 
+// Writing rows held one per lane: four lanes exchange their rows' 32-byte pieces, so that a store covers
+// 128 contiguous bytes of each of 8 rows instead of 32 bytes of each of 32 (a store takes the memory pipe a
+// cycle per row it touches: 4300 -> 1500 clocks per item for a block of 128 rows of 256 bytes).
+struct TcRowOut {
+  uint64_t row[4];       // the quad's rows; 0: not written
+  __device__ __forceinline__ explicit TcRowOut(const void* mine) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      row[r] = __shfl_sync(0xffffffffu, static_cast<unsigned long long>(reinterpret_cast<uintptr_t>(mine)), (lane & ~3) + r);
+  }
+  // 128 bytes at byte offset `at` of every row; w: this lane's row's.  Whole warp.  wide: 32-byte alignment.
+  __device__ __forceinline__ void store(uint32_t (&w)[32], int at, bool wide) const {
+    const int lane = threadIdx.x & 31;
+    const bool up2 = lane & 2, up1 = lane & 1;
+    // 4 x 4 transpose of 8-word pieces over the quad: first with the lane two away, then with the neighbour
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const uint32_t got = __shfl_xor_sync(0xffffffffu, up2 ? w[e] : w[16 + e], 2);
+      if (up2) w[e] = got; else w[16 + e] = got;
+    }
+#pragma unroll
+    for (int b = 0; b < 32; b += 16)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t got = __shfl_xor_sync(0xffffffffu, up1 ? w[b + e] : w[b + 8 + e], 1);
+        if (up1) w[b + e] = got; else w[b + 8 + e] = got;
+      }
+    at += (lane & 3) * 32;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      if (row[r] == 0) continue;
+      char* p = reinterpret_cast<char*>(row[r]) + at;
+      if (wide) {
+        const uint32_t o[8] = {w[r * 8], w[r * 8 + 1], w[r * 8 + 2], w[r * 8 + 3], w[r * 8 + 4], w[r * 8 + 5], w[r * 8 + 6], w[r * 8 + 7]};
+        ptx::st_global_32(p, o);
+      } else {
+        *reinterpret_cast<uint4*>(p) = make_uint4(w[r * 8], w[r * 8 + 1], w[r * 8 + 2], w[r * 8 + 3]);
+        *reinterpret_cast<uint4*>(p + 16) = make_uint4(w[r * 8 + 4], w[r * 8 + 5], w[r * 8 + 6], w[r * 8 + 7]);
+      }
+    }
+  }
+};
+
 template <int D>
 struct TcLayout {
   static constexpr int NH = D / 64;
@@ -121,6 +165,7 @@ __device__ __forceinline__ void flash_tc_setup(uint8_t* smem, TcShared<Item>* sh
 // Called by all 384 threads after flash_tc_setup and the dependency wait; returns with every thread after
 // the last item.  Source:
 //   struct Item                   plain data
+//   void begin(lane)              whole warp, once: what find() needs
 //   bool find(k, lane, item)      whole warp: the CTA's k-th item; false: there is none
 //   void set(item)                all that follows is about this item
 //   int  tiles(h)                 shared: tiles of block h; streams: all tiles (h ignored)
@@ -130,7 +175,7 @@ __device__ __forceinline__ void flash_tc_setup(uint8_t* smem, TcShared<Item>* sh
 //   int  row_key(h, row)          what last() needs of a row, worked out once
 //   int  last(key, t)             last key of tile t that the row sees (>= 127: all)
 //   int  clean(t)                 -1: nothing to clean; else rows of tile t that somebody sees
-//   bool scan()                   whether rows below clean(t) are searched for non-finite elements
+//   int  scan_from(t)             rows [scan_from(t), clean(t)) are searched for non-finite elements
 //   int  note_slot(t)             which dirty[] entry a cleaned tile uses
 //   void store(h, row, seen, m, l, dirty, read)  one finished row per thread, called by whole warps; seen:
 //                                 the block had tiles; dirty: noted key rows or null; read(c, v): columns
@@ -179,6 +224,7 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
       for (int i = 0; i < kRing; ++i) group_of[i] = -1;
       bool ok = true;
       auto wait_group = [&](int g) { return ptx::mbar_wait(bar_empty + g % kPairs, uint32_t(g / kPairs) & 1u, abort_flag); };
+      src.begin(lane);
       for (int k = 0; ok; ++k) {
         typename Source::Item item;
         const bool have = src.find(k, lane, item);
@@ -319,30 +365,47 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
                warp_wait(bar_full + (group + 1 + t) % kPairs, uint32_t((group + 1 + t) / kPairs) & 1u);
           if (!ok) break;
           uint8_t* tile = smem + L::offKV + (base + v_load(t, nt)) % kRing * L::kTile;
-          // 16-byte piece i of the warp's 64 rows; the swizzle only permutes the pieces within a row
-          for (int half = 0; half < L::NH; ++half)
-#pragma unroll 4
-            for (int i = lane; i < 64 * 8; i += 32) {
-              const int r = (warp - 2) * 64 + (i >> 3);
-              uint4* p = reinterpret_cast<uint4*>(tile + half * kTcHalfBytes + r * 128 + (i & 7) * 16);
-              if (r >= seen) {
-                *p = make_uint4(0, 0, 0, 0);
-              } else if (src.scan()) {
-                uint4 v = *p;
-                uint32_t* w = &v.x;
-                bool hit = false;
+          // One 16-byte piece per lane; the swizzle only permutes the pieces within a row.  The search takes
+          // the maximum of |x| over all pieces of the lane (NaN wins over everything): 2 instructions per
+          // 4 bytes, and only if that is not finite the pieces are looked at one by one.
+          constexpr int kPieces = L::NH * 8;                 // per row
+          auto piece = [&](int i) {                          // i-th piece of the rows this warp takes, rows alternate between the two
+            const int r = 2 * (i / kPieces) + (warp - 2), c = i % kPieces;
+            return reinterpret_cast<uint4*>(tile + (c >> 3) * kTcHalfBytes + r * 128 + (c & 7) * 16);
+          };
+          const int z0 = (max(seen, 0) + 1 - (warp - 2)) / 2;      // first of this warp's rows that nobody sees
+          const int s0 = (src.scan_from(t) + 1 - (warp - 2)) / 2;  // first of its rows to search
+          __nv_bfloat162 top = __floats2bfloat162_rn(0.f, 0.f);
+          for (int i0 = s0 * kPieces + lane; i0 < z0 * kPieces; i0 += 32 * 8) {
+            uint4 v[8];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  if ((w[e] & 0x7f80u) == 0x7f80u) { w[e] &= 0xffff0000u; hit = true; }
-                  if ((w[e] & 0x7f800000u) == 0x7f800000u) { w[e] &= 0xffffu; hit = true; }
-                }
-                if (hit) {
-                  *p = v;
-                  atomicOr(&sh->dirty[k & 1][src.note_slot(t)][r >> 5], 1u << (r & 31));
-                  sh->any_dirty[k & 1] = 1;
-                }
-              }
+            for (int j = 0; j < 8; ++j) v[j] = i0 + 32 * j < z0 * kPieces ? *piece(i0 + 32 * j) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const uint32_t* w = &v[j].x;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) top = __hmax2_nan(top, __habs2(reinterpret_cast<const __nv_bfloat162&>(w[e])));
             }
+          }
+          const uint32_t tw = reinterpret_cast<const uint32_t&>(top);
+          if ((tw & 0x7f80u) == 0x7f80u || (tw & 0x7f800000u) == 0x7f800000u) {
+            for (int i = s0 * kPieces + lane; i < z0 * kPieces; i += 32) {
+              uint4 v = *piece(i);
+              uint32_t* w = &v.x;
+              bool hit = false;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                if ((w[e] & 0x7f80u) == 0x7f80u) { w[e] &= 0xffff0000u; hit = true; }
+                if ((w[e] & 0x7f800000u) == 0x7f800000u) { w[e] &= 0xffffu; hit = true; }
+              }
+              if (!hit) continue;
+              *piece(i) = v;
+              const int r = 2 * (i / kPieces) + (warp - 2);
+              atomicOr(&sh->dirty[k & 1][src.note_slot(t)][r >> 5], 1u << (r & 31));
+              sh->any_dirty[k & 1] = 1;
+            }
+          }
+          for (int i = z0 * kPieces + lane; i < 64 * kPieces; i += 32) *piece(i) = make_uint4(0, 0, 0, 0);
           ptx::fence_proxy_async_smem();                     // the product reads the tile through the async proxy
           __syncwarp();
           if (lane == 0) ptx::mbar_arrive(bar_clean);
@@ -378,10 +441,17 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
         for (int c = 0; c < kTcKeys / 32; ++c)
           ptx::tmem_ld32(s_addr + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&v[c * 32]));
         ptx::tc_wait_ld();
-        if (hi < kTcKeys - 1) {   // a masked score is -inf: it loses every max and its weight is exactly 0
+        // a masked score is -inf: it loses every max and its weight is exactly 0.  Groups of 32 keys that the
+        // whole warp sees are left alone.
+        if (__any_sync(0xffffffffu, hi < kTcKeys - 1)) {
+          const int least = __reduce_min_sync(0xffffffffu, hi);
 #pragma unroll
-          for (int k = 0; k < kTcKeys; ++k)
-            if (k > hi) v[k] = 0xff800000u;
+          for (int c = 0; c < kTcKeys / 32; ++c)
+            if (least < c * 32 + 31) {
+#pragma unroll
+              for (int k = c * 32; k < c * 32 + 32; ++k)
+                if (k > hi) v[k] = 0xff800000u;
+            }
         }
         float mx;
         {

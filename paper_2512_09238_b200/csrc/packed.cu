@@ -39,24 +39,28 @@ __global__ void __launch_bounds__(kSimtThreads, 2)
 packed_simt_kernel(const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const __grid_constant__ PackedArgs args,
                    float scale_log2e, T* __restrict__ O) {
   extern __shared__ float4 packed_smem[];
-  __shared__ int found[3];
+  __shared__ PackedWork found;
   pdl_wait();
   pdl_launch_dependents();
   const int G = args.n_q_heads / args.n_kv_heads;
   const int tile_pos = kSimtRows / G;
   PackedSrc<T> src;
   src.Q = Q; src.K = K; src.V = V; src.a = &args; src.G = G;
-  src.w.kvh = int(blockIdx.x) % args.n_kv_heads;
   if (threadIdx.x < 32) {
-    int seq = -1, tile = 0;
-    if (!packed_find(args, int(blockIdx.x) / args.n_kv_heads, tile_pos, threadIdx.x, seq, tile)) seq = -1;
-    if (threadIdx.x == 0) { found[0] = seq; found[1] = tile; }
+    PackedFinder finder;
+    finder.read(args, tile_pos, threadIdx.x);
+    PackedWork w;
+    int tile = 0;
+    w.len = 0;
+    if (finder.find(args, int(blockIdx.x) / args.n_kv_heads, tile_pos, threadIdx.x, w.row0, w.len, tile)) {
+      w.p0 = tile * tile_pos;
+      w.kvh = int(blockIdx.x) % args.n_kv_heads;
+    }
+    if (threadIdx.x == 0) found = w;
   }
   __syncthreads();
-  const int seq = found[0];
-  if (seq < 0) return;
-  packed_bounds(args, seq, src.w.row0, src.w.len);
-  src.w.p0 = found[1] * tile_pos;
+  src.w = found;
+  if (src.w.len == 0) return;
   float o[4][D / 16], m[4], l[4];
   simt_flash<T, D>(src, scale_log2e, reinterpret_cast<float*>(packed_smem), o, m, l);
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;

@@ -24,6 +24,9 @@ struct PackedTcSrc {
   int64_t row0;
   int len, p0, kvh;
 
+  PackedFinder finder;      // the producer warp's
+
+  __device__ __forceinline__ void begin(int lane) { finder.read(*a, 2 * P, lane); }
   // Items lie longest first; the CTAs take them in turn, every other round in reverse, so that the CTA that
   // got the longest of one round gets the shortest of the next.  Two orders, see launch_packed_tc.
   __device__ __forceinline__ bool find(int k, int lane, Item& it) const {
@@ -31,9 +34,8 @@ struct PackedTcSrc {
     const int i = k * n + ((k & 1) ? n - 1 - int(blockIdx.x) : int(blockIdx.x));
     if (i >= max_tiles * a->n_kv_heads) return false;
     it.kvh = unit_major ? i / max_tiles : i % a->n_kv_heads;
-    int seq, tile;
-    if (!packed_find(*a, unit_major ? i % max_tiles : i / a->n_kv_heads, 2 * P, lane, seq, tile)) return false;
-    packed_bounds(*a, seq, it.row0, it.len);
+    int tile;
+    if (!finder.find(*a, unit_major ? i % max_tiles : i / a->n_kv_heads, 2 * P, lane, it.row0, it.len, tile)) return false;
     it.p0 = tile * 2 * P;
     return true;
   }
@@ -53,11 +55,12 @@ struct PackedTcSrc {
   __device__ __forceinline__ int row_key(int h, int row) const { return min(p0 + h * P + row / G, last_pos(h)); }
   __device__ __forceinline__ int last(int key, int t) const { return key - t * kTcKeys; }
   // From the tile that holds p0 on, some row does not see some key (at most two tiles: 2 P <= 128, or
-  // P = 128 with p0 a multiple of 256).  Rows past the last position are nobody's: another sequence's, or none.
+  // P = 128 with p0 a multiple of 256).  Rows past the last position are nobody's: another sequence's, or
+  // none; rows up to p0 are everybody's.
   __device__ __forceinline__ int clean(int t) const {
     return t < p0 / kTcKeys ? -1 : min(kTcKeys, min(p0 + 2 * P, len) - t * kTcKeys);
   }
-  __device__ __forceinline__ bool scan() const { return true; }
+  __device__ __forceinline__ int scan_from(int t) const { return max(0, p0 + 1 - t * kTcKeys); }
   __device__ __forceinline__ int note_slot(int t) const { return t - p0 / kTcKeys; }
 
   template <typename Read>
@@ -67,40 +70,34 @@ struct PackedTcSrc {
     const bool mine = row < G * P && pos < len;
     const float inv = 1.f / l;
     __nv_bfloat16* out = O + (kvh * G + row % G) * a->o.head + (row0 + pos) * a->o.row;
+    const TcRowOut rows_out(mine ? out : nullptr);
 #pragma unroll 1
-    for (int c = 0; c < D / 32; ++c) {
-      uint32_t v[32];
-      read(c, v);
-      if (!mine) continue;
+    for (int c = 0; c < D / 64; ++c) {     // 64 columns = 32 words of bf16 pairs
+      uint32_t w[32];
 #pragma unroll
-      for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * inv);
-      if (dirty) {   // non-finite values of masked tiles, kept out of the product, reach the rows that see them
-        for (int w = 0; w < 8; ++w)
-          for (uint32_t bits = dirty[w]; bits; bits &= bits - 1) {
-            const int key = (p0 / kTcKeys + (w >> 2)) * kTcKeys + (w & 3) * 32 + __ffs(bits) - 1;
-            if (key > pos) break;
-            const __nv_bfloat16* src = V + kvh * a->v.head + (row0 + key) * a->v.row + c * 32;
+      for (int half = 0; half < 2; ++half) {
+        uint32_t v[32];
+        read(2 * c + half, v);
 #pragma unroll
-            for (int k = 0; k < 32; ++k) {
-              const float x = __bfloat162float(src[k]);
-              if (!isfinite(x)) v[k] = __float_as_uint(__uint_as_float(v[k]) + x);
+        for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * inv);
+        if (dirty && mine) {   // non-finite values of masked tiles, kept out of the product, reach the rows that see them
+          for (int i = 0; i < 8; ++i)
+            for (uint32_t bits = dirty[i]; bits; bits &= bits - 1) {
+              const int key = (p0 / kTcKeys + (i >> 2)) * kTcKeys + (i & 3) * 32 + __ffs(bits) - 1;
+              if (key > pos) break;
+              const __nv_bfloat16* src = V + kvh * a->v.head + (row0 + key) * a->v.row + (2 * c + half) * 32;
+#pragma unroll
+              for (int k = 0; k < 32; ++k) {
+                const float x = __bfloat162float(src[k]);
+                if (!isfinite(x)) v[k] = __float_as_uint(__uint_as_float(v[k]) + x);
+              }
             }
-          }
-      }
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        uint32_t w[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          w[e] = ptx::pack_bf16x2(__uint_as_float(v[q * 16 + 2 * e]), __uint_as_float(v[q * 16 + 2 * e + 1]));
-        __nv_bfloat16* at = out + c * 32 + q * 16;
-        if (wide) {
-          ptx::st_global_32(at, w);
-        } else {
-          *reinterpret_cast<uint4*>(at) = make_uint4(w[0], w[1], w[2], w[3]);
-          *reinterpret_cast<uint4*>(at + 8) = make_uint4(w[4], w[5], w[6], w[7]);
         }
+#pragma unroll
+        for (int k = 0; k < 16; ++k)
+          w[half * 16 + k] = ptx::pack_bf16x2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1]));
       }
+      rows_out.store(w, c * 128, wide != 0);
     }
   }
 };

@@ -82,15 +82,24 @@ struct TreeSlice {
 __device__ __forceinline__ TreeSlice tree_find(const int64_t* state, int n_units, int64_t tail_cap, int n_slots, int step,
                                                int min_steps, int tile, int lin, int lane) {
   constexpr int kHeld = 4;   // units held in registers per lane; more are read again
+  const int groups = min(kHeld, (n_units + 31) / 32);
   auto steps_of = [&](int u) -> int {
     if (u >= n_units) return 0;
     const int64_t* st = state + size_t(u) * TCA_STATE_WORDS;
     return int((st[TCA_ST_N_GLOBAL] + st[TCA_ST_N_TAIL] + step - 1) / step);
   };
   int held[kHeld], most = 0, sum = 0;
+  UnitView first{};          // the view of unit `lane`, for the units most calls have
 #pragma unroll
   for (int k = 0; k < kHeld; ++k) {
-    held[k] = steps_of(k * 32 + lane);
+    held[k] = 0;
+    if (k >= groups) continue;
+    if (k == 0) {
+      if (lane < n_units) first = load_unit(state, lane, tail_cap);
+      held[0] = int((first.len() + step - 1) / step);
+    } else {
+      held[k] = steps_of(k * 32 + lane);
+    }
     most = max(most, held[k]);
     sum += held[k];
   }
@@ -104,16 +113,18 @@ __device__ __forceinline__ TreeSlice tree_find(const int64_t* state, int n_units
   auto count = [&](int per) {   // slices of at most `per` steps
     int c = 0;
 #pragma unroll
-    for (int k = 0; k < kHeld; ++k) c += (held[k] + per - 1) / per;
+    for (int k = 0; k < kHeld; ++k)
+      if (k < groups) c += (held[k] + per - 1) / per;
     for (int u = 32 * kHeld + lane; u < n_units; u += 32) c += (steps_of(u) + per - 1) / per;
     return int(__reduce_add_sync(0xffffffffu, c));
   };
-  int lo = max(min_steps, (sum + n_slots - 1) / n_slots), hi = max(most, lo);
-  if (count(lo) > n_slots)
-    while (lo < hi) {
-      const int mid = lo + (hi - lo) / 2;
-      if (count(mid) <= n_slots) hi = mid; else lo = mid + 1;
-    }
+  // count(per) <= sum / per + n_units, which bounds the search from above
+  int lo = max(min_steps, (sum + n_slots - 1) / n_slots);
+  int hi = max(lo, n_slots > n_units ? min(most, (sum + n_slots - n_units - 1) / (n_slots - n_units)) : most);
+  while (lo < hi) {
+    const int mid = lo + (hi - lo) / 2;
+    if (count(mid) <= n_slots) hi = mid; else lo = mid + 1;
+  }
   TreeSlice s;
   s.u = -1;
   int offset = 0;
@@ -142,7 +153,17 @@ __device__ __forceinline__ TreeSlice tree_find(const int64_t* state, int n_units
     offset += __shfl_sync(0xffffffffu, incl, 31);
   }
   if (s.u < 0) return s;
-  const UnitView v = load_unit(state, s.u, tail_cap);
+  UnitView v;
+  if (s.u < 32) {
+    v.seg = __shfl_sync(0xffffffffu, first.seg, s.u);
+    v.gcap = __shfl_sync(0xffffffffu, first.gcap, s.u);
+    v.n_global = __shfl_sync(0xffffffffu, first.n_global, s.u);
+    v.tail_head = __shfl_sync(0xffffffffu, first.tail_head, s.u);
+    v.n_tail = __shfl_sync(0xffffffffu, first.n_tail, s.u);
+    v.tail_cap = tail_cap;
+  } else {
+    v = load_unit(state, s.u, tail_cap);
+  }
   const int64_t len = v.len(), n_steps = (len + step - 1) / step;
   const int64_t r0 = slice_begin(n_steps, s.np, s.part) * step;
   const int64_t r1 = min(len, slice_begin(n_steps, s.np, s.part + 1) * step);

@@ -29,6 +29,7 @@ struct TreeTcSrc {
   int q_row, rows, n;
   size_t at0;
 
+  __device__ __forceinline__ void begin(int) {}
   __device__ __forceinline__ bool find(int k, int lane, Item& it) const {
     if (k > 0) return false;
     const TreeSlice s = tree_find(state, n_units, tail_cap, plan->n_slots, plan->step_rows, plan->min_steps, kTcKeys,
@@ -71,7 +72,7 @@ struct TreeTcSrc {
     slice.get(t, y, c);
     return c < kTcKeys ? c : -1;
   }
-  __device__ __forceinline__ bool scan() const { return false; }
+  __device__ __forceinline__ int scan_from(int) const { return kTcKeys; }
   __device__ __forceinline__ int note_slot(int) const { return 0; }
 
   template <typename Read>
@@ -80,17 +81,12 @@ struct TreeTcSrc {
     const size_t at = at0 + (kShared ? 0 : size_t(h) * plan->rows) + r;
     if (r < rows) ws->ml[at] = seen ? make_float2(m, l) : make_float2(-INFINITY, 0.f);
     if (!seen) return;
+    const TcRowOut rows_out(r < rows ? ws->acc + at * D : nullptr);
 #pragma unroll 1
     for (int c = 0; c < D / 32; ++c) {
       uint32_t v[32];
       read(c, v);
-      if (r < rows) {
-#pragma unroll
-        for (int k = 0; k < 32; k += 8) {
-          const uint32_t w[8] = {v[k], v[k + 1], v[k + 2], v[k + 3], v[k + 4], v[k + 5], v[k + 6], v[k + 7]};
-          ptx::st_global_32(ws->acc + at * D + c * 32 + k, w);
-        }
-      }
+      rows_out.store(v, c * 128, true);
     }
   }
 };

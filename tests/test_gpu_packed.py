@@ -11,7 +11,7 @@ pytestmark = pytest.mark.gpu
 
 LENS = {
     "one": [1], "empty_between": [0, 1, 0, 5, 0], "tile_edges": [127, 128, 129, 63, 64, 65],
-    "ragged": [300, 1, 33, 0, 511], "many": [3, 17, 0, 40, 1, 1, 96, 2] * 6,
+    "ragged": [300, 1, 33, 0, 511], "hundreds": [(7 * i) % 11 for i in range(290)] + [200], "many": [3, 17, 0, 40, 1, 1, 96, 2] * 6,
 }
 
 
