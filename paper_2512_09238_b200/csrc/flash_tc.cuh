@@ -66,19 +66,29 @@ struct TcRowOut {
   __device__ __forceinline__ void store(uint32_t (&w)[32], int at, bool wide) const {
     const int lane = threadIdx.x & 31;
     const bool up2 = lane & 2, up1 = lane & 1;
-    // 4 x 4 transpose of 8-word pieces over the quad: first with the lane two away, then with the neighbour
+    // 4 x 4 transpose of 8-word pieces over the quad: first with the lane two away, then with the neighbour.
+    // All of a step's exchanges are issued before the first result is used (one after the other they cost
+    // their latency each, 40 clocks).
+    uint32_t got[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) got[e] = up2 ? w[e] : w[16 + e];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) got[e] = __shfl_xor_sync(0xffffffffu, got[e], 2);
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      const uint32_t got = __shfl_xor_sync(0xffffffffu, up2 ? w[e] : w[16 + e], 2);
-      if (up2) w[e] = got; else w[16 + e] = got;
+      w[e] = up2 ? got[e] : w[e];
+      w[16 + e] = up2 ? w[16 + e] : got[e];
     }
 #pragma unroll
-    for (int b = 0; b < 32; b += 16)
+    for (int e = 0; e < 16; ++e) got[e] = up1 ? w[(e >> 3) * 16 + (e & 7)] : w[(e >> 3) * 16 + 8 + (e & 7)];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const uint32_t got = __shfl_xor_sync(0xffffffffu, up1 ? w[b + e] : w[b + 8 + e], 1);
-        if (up1) w[b + e] = got; else w[b + 8 + e] = got;
-      }
+    for (int e = 0; e < 16; ++e) got[e] = __shfl_xor_sync(0xffffffffu, got[e], 1);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      uint32_t &lo = w[(e >> 3) * 16 + (e & 7)], &hi = w[(e >> 3) * 16 + 8 + (e & 7)];
+      lo = up1 ? got[e] : lo;
+      hi = up1 ? hi : got[e];
+    }
     at += (lane & 3) * 32;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
@@ -104,7 +114,9 @@ struct TcLayout {
   static constexpr int offQ = 0;
   static constexpr int offKV = 2 * kTile;
   static constexpr int offBar = offKV + kRing * kTile;
-  static constexpr int kBars = 8 + 2 * kPairs + 2 + 4 + 2;
+  static constexpr int kRaw = 8;                          // barriers of value tiles on their way to the cleaners; at most
+  static_assert((kRing + 1) / 2 < kRaw, "value tiles in the ring");   // every other tile of the ring is a value tile, or all but one
+  static constexpr int kBars = 6 + kRaw + 2 * kPairs + 2 + 4 + 2;
   static constexpr int bytes = offBar + 512 + 1024;       // barriers, alignment slack
   static_assert(bytes <= 227 * 1024 - 512, "shared memory");
   static_assert(kBars * 8 <= 512, "barrier block");
@@ -132,14 +144,13 @@ __device__ __forceinline__ void flash_tc_setup(uint8_t* smem, TcShared<Item>* sh
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
       ptx::mbar_init(bars + i, 1);                        // query tile full, empty
-      ptx::mbar_init(bars + 4 + i, 1);                    // item full
-      ptx::mbar_init(bars + 6 + i, kTcItemReaders);       // item empty
+      ptx::mbar_init(bars + 2 + i, 1);                    // item full
+      ptx::mbar_init(bars + 4 + i, kTcItemReaders);       // item empty
     }
-    ptx::mbar_init(bars + 2, 2);                          // clean
-    ptx::mbar_init(bars + 3, 1);                          // to clean
-    uint64_t* full = bars + 8;
+    for (int i = 0; i < L::kRaw; ++i) ptx::mbar_init(bars + 6 + i, 1);
+    uint64_t* full = bars + 6 + L::kRaw;
     for (int i = 0; i < L::kPairs; ++i) {
-      ptx::mbar_init(full + i, 2);
+      ptx::mbar_init(full + i, 3);                        // K tile, V tile twice (the two cleaners, if it is cleaned)
       ptx::mbar_init(full + L::kPairs + i, 1);
     }
     uint64_t* s = full + 2 * L::kPairs;
@@ -172,22 +183,23 @@ __device__ __forceinline__ void flash_tc_setup(uint8_t* smem, TcShared<Item>* sh
 //   int  q_bytes(h)               bytes load_q(h) brings
 //   void load_q(h, dst, bar)      issue the loads of block h's query tile
 //   void load(t, is_v, dst, bar)  issue the loads of a K or V tile (kTile bytes)
-//   int  row_key(h, row)          what last() needs of a row, worked out once
+//   void begin_row(row)           softmax threads, once: their row
+//   int  row_key(h)               what last() needs of the row, worked out once per item
 //   int  last(key, t)             last key of tile t that the row sees (>= 127: all)
 //   int  clean(t)                 -1: nothing to clean; else rows of tile t that somebody sees
 //   int  scan_from(t)             rows [scan_from(t), clean(t)) are searched for non-finite elements
 //   int  note_slot(t)             which dirty[] entry a cleaned tile uses
-//   void store(h, row, seen, m, l, dirty, read)  one finished row per thread, called by whole warps; seen:
-//                                 the block had tiles; dirty: noted key rows or null; read(c, v): columns
-//                                 32 c .. of O (warp-wide)
+//   void store(h, seen, m, l, dirty, read)  one finished row per thread, called by whole warps; seen:
+//                                 the block had tiles; dirty: noted key rows or null; read(c, v): requests
+//                                 columns 32 c .. of O (warp-wide; tc_wait_ld() before v is used)
 template <int D, bool kShared, typename Source>
 __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<typename Source::Item>* sh, float scale_log2e,
                                          int* status) {
   using L = TcLayout<D>;
   constexpr int kRing = L::kRing, kPairs = L::kPairs, kLead = kShared ? 1 : 2;
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::offBar);
-  uint64_t *bar_q = bars, *bar_q_empty = bars + 1, *bar_clean = bars + 2, *bar_to_clean = bars + 3;
-  uint64_t *bar_item = bars + 4, *bar_item_empty = bars + 6, *bar_full = bars + 8, *bar_empty = bar_full + kPairs;
+  uint64_t *bar_q = bars, *bar_q_empty = bars + 1, *bar_item = bars + 2, *bar_item_empty = bars + 4, *bar_raw = bars + 6;
+  uint64_t *bar_full = bar_raw + L::kRaw, *bar_empty = bar_full + kPairs;
   uint64_t *bar_s = bar_empty + kPairs, *bar_p = bar_s + 2, *bar_pv = bar_p + 4;
   volatile int* abort_flag = &sh->abort;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -219,6 +231,7 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
       // ------------------------------------------------------------- producer: finds the items, brings the tiles
       int slot = 0;                   // ring slot of the next load
       int group = 0;                  // its group, counted over all items
+      uint32_t cleaned = 0;           // value tiles handed to the cleaners
       int group_of[kRing];            // group of the tile a slot holds
 #pragma unroll
       for (int i = 0; i < kRing; ++i) group_of[i] = -1;
@@ -251,11 +264,13 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
           for (int m = -1; m < nt && ok; ++m, ++group) {     // group m: V_m and K_m+lead; m = -1: the leading K tiles
             if (group >= kPairs) ok = wait_group(group - kPairs);
             uint64_t* full = bar_full + group % kPairs;
+            const bool unclean = m >= 0 && src.clean(m) >= 0;
+            if (!unclean) ptx::mbar_arrive(full);            // in the place of the second cleaner
 #pragma unroll
             for (int j = 0; j < 2 && ok; ++j) {
               const bool is_v = m >= 0 && j == 0;
               const int t = m < 0 ? j : is_v ? m : m + kLead;
-              if (t >= nt || (m < 0 && j >= kLead)) {        // no such tile: the barrier still expects two arrivals
+              if (t >= nt || (m < 0 && j >= kLead)) {        // no such tile: its arrival is still expected
                 ptx::mbar_arrive(full);
                 continue;
               }
@@ -265,8 +280,9 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
                 if (i == slot) { held = group_of[i]; group_of[i] = group; }
               if (held >= 0) ok = wait_group(held);          // the slot's previous tile must have been consumed
               if (!ok) break;
-              ptx::mbar_arrive_expect_tx(full, uint32_t(L::kTile));
-              src.load(t, is_v, smem + L::offKV + slot * L::kTile, full);
+              uint64_t* bar = is_v && unclean ? bar_raw + cleaned++ % L::kRaw : full;
+              ptx::mbar_arrive_expect_tx(bar, uint32_t(L::kTile));
+              src.load(t, is_v, smem + L::offKV + slot * L::kTile, bar);
               slot = slot + 1 == kRing ? 0 : slot + 1;
             }
           }
@@ -281,7 +297,7 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
       const uint64_t dk = ptx::smem_desc_sw128(ptx::smem_u32(smem + L::offKV), 16, 1024);             // K: K-major B
       const uint64_t dv = ptx::smem_desc_sw128(ptx::smem_u32(smem + L::offKV), kTcHalfBytes, 1024);   // V: MN-major B
       int base = 0, group = 0;               // first ring slot and group of the item
-      uint32_t cleaned = 0, tile_count[2] = {0, 0};
+      uint32_t tile_count[2] = {0, 0};
       auto slot_of = [&](int n) { return (base + n) % kRing; };
       auto issue_s = [&](int h, int n) {
         const uint64_t a0 = dq + (kShared ? uint64_t(uint32_t(h * L::kTile) >> 4) : 0ull);
@@ -321,10 +337,6 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
         ++group;
         for (int t = 0; t < nt && ok; ++t, ++group) {
           ok = warp_wait(bar_full + group % kPairs, uint32_t(group / kPairs) & 1u);
-          if (ok && src.clean(t) >= 0) {
-            if (lane == 0) ptx::mbar_arrive(bar_to_clean);
-            ok = warp_wait(bar_clean, cleaned++ & 1u);
-          }
           if (kShared) {
             for (int h = 0; h < 2 && ok; ++h) {
               const int nh = h == 0 ? n0 : n1;
@@ -351,8 +363,7 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
       }
     } else {
       // ------------------------------------------------------------- cleaning of value tiles (warps 2 and 3: 64 rows each)
-      // They start on a tile when the issuer, having seen it arrive, says so: the issuer then waits for them,
-      // so neither can be a phase of the tile's barrier behind or ahead of the other.
+      // Such a tile arrives on a barrier of its own and joins its group when both warps are done with it.
       uint32_t cleaned = 0;
       int base = 0, group = 0;
       for (int k = 0; next_item(k); ++k) {
@@ -361,9 +372,9 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
         for (int t = 0; t < nt && ok; ++t) {
           const int seen = src.clean(t);
           if (seen < 0) continue;
-          ok = warp_wait(bar_to_clean, cleaned++ & 1u) &&
-               warp_wait(bar_full + (group + 1 + t) % kPairs, uint32_t((group + 1 + t) / kPairs) & 1u);
+          ok = warp_wait(bar_raw + cleaned % L::kRaw, (cleaned / L::kRaw) & 1u);
           if (!ok) break;
+          ++cleaned;
           uint8_t* tile = smem + L::offKV + (base + v_load(t, nt)) % kRing * L::kTile;
           // One 16-byte piece per lane; the swizzle only permutes the pieces within a row.  The search takes
           // the maximum of |x| over all pieces of the lane (NaN wins over everything): 2 instructions per
@@ -408,7 +419,7 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
           for (int i = z0 * kPieces + lane; i < 64 * kPieces; i += 32) *piece(i) = make_uint4(0, 0, 0, 0);
           ptx::fence_proxy_async_smem();                     // the product reads the tile through the async proxy
           __syncwarp();
-          if (lane == 0) ptx::mbar_arrive(bar_clean);
+          if (lane == 0) ptx::mbar_arrive(bar_full + (group + 1 + t) % kPairs);
         }
         if (!ok) break;
         base = (base + 2 * nt) % kRing;
@@ -425,10 +436,11 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
     const uint32_t s_addr = lane_addr + h * 128u, o_addr = lane_addr + 256u + uint32_t(h * D);
     const uint64_t scale2 = ptx::pack2(scale_log2e, scale_log2e);
     uint32_t tile_count = 0, item_count = 0;
+    src.begin_row(row);
     for (int k = 0; !*abort_flag && next_item(k); ++k) {
       const int nt = src.tiles(kShared ? h : 0);
       const int mine = kShared ? nt : (nt - h + 1) / 2;      // tiles of this block / stream
-      const int row_key = src.row_key(h, row);
+      const int row_key = src.row_key(h);
       float m_run = -INFINITY, m_used = -INFINITY, l = 0.f;
       bool ok = true;
       for (int it = 0; it < mine; ++it) {
@@ -520,11 +532,8 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
       if (ok && mine > 0) ok = warp_wait(bar_pv + h, item_count++ & 1u);   // committed after the last PV
       if (!ok) break;
       ptx::tc_fence_after();
-      src.store(h, row, mine > 0, m_used, l, sh->any_dirty[k & 1] ? &sh->dirty[k & 1][0][0] : nullptr,
-                [&](int c, uint32_t (&v)[32]) {
-                  ptx::tmem_ld32(o_addr + c * 32, v);
-                  ptx::tc_wait_ld();
-                });
+      src.store(h, mine > 0, m_used, l, sh->any_dirty[k & 1] ? &sh->dirty[k & 1][0][0] : nullptr,
+                [&](int c, uint32_t (&v)[32]) { ptx::tmem_ld32(o_addr + c * 32, v); });
       ptx::tc_fence_before();       // the reads of O precede the next item's products (through the P barriers)
       item_done(k);
     }

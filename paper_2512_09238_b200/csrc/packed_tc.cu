@@ -52,7 +52,9 @@ struct PackedTcSrc {
     for (int half = 0; half < D / 64; ++half)
       ptx::tma_load_3d(dst + half * kTcHalfBytes, is_v ? mv : mk, half * 64, int(row0) + t * kTcKeys, kvh, bar);
   }
-  __device__ __forceinline__ int row_key(int h, int row) const { return min(p0 + h * P + row / G, last_pos(h)); }
+  int dp, g;                // this thread's row: position and head within the block
+  __device__ __forceinline__ void begin_row(int row) { dp = row / G; g = row % G; }
+  __device__ __forceinline__ int row_key(int h) const { return min(p0 + h * P + dp, last_pos(h)); }
   __device__ __forceinline__ int last(int key, int t) const { return key - t * kTcKeys; }
   // From the tile that holds p0 on, some row does not see some key (at most two tiles: 2 P <= 128, or
   // P = 128 with p0 a multiple of 256).  Rows past the last position are nobody's: another sequence's, or
@@ -64,39 +66,37 @@ struct PackedTcSrc {
   __device__ __forceinline__ int note_slot(int t) const { return t - p0 / kTcKeys; }
 
   template <typename Read>
-  __device__ __forceinline__ void store(int h, int row, bool seen, float, float l, const uint32_t* dirty, Read read) const {
+  __device__ __forceinline__ void store(int h, bool seen, float, float l, const uint32_t* dirty, Read read) const {
     if (!seen) return;
-    const int pos = p0 + h * P + row / G;
-    const bool mine = row < G * P && pos < len;
+    const int pos = p0 + h * P + dp;
+    const bool mine = dp < P && pos < len;
     const float inv = 1.f / l;
-    __nv_bfloat16* out = O + (kvh * G + row % G) * a->o.head + (row0 + pos) * a->o.row;
+    __nv_bfloat16* out = O + (kvh * G + g) * a->o.head + (row0 + pos) * a->o.row;
     const TcRowOut rows_out(mine ? out : nullptr);
 #pragma unroll 1
     for (int c = 0; c < D / 64; ++c) {     // 64 columns = 32 words of bf16 pairs
+      uint32_t v[64];
+      read(2 * c, reinterpret_cast<uint32_t(&)[32]>(v[0]));
+      read(2 * c + 1, reinterpret_cast<uint32_t(&)[32]>(v[32]));
+      ptx::tc_wait_ld();
+#pragma unroll
+      for (int k = 0; k < 64; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * inv);
+      if (dirty && mine) {   // non-finite values of masked tiles, kept out of the product, reach the rows that see them
+        for (int i = 0; i < 8; ++i)
+          for (uint32_t bits = dirty[i]; bits; bits &= bits - 1) {
+            const int key = (p0 / kTcKeys + (i >> 2)) * kTcKeys + (i & 3) * 32 + __ffs(bits) - 1;
+            if (key > pos) break;
+            const __nv_bfloat16* src = V + kvh * a->v.head + (row0 + key) * a->v.row + c * 64;
+#pragma unroll
+            for (int k = 0; k < 64; ++k) {
+              const float x = __bfloat162float(src[k]);
+              if (!isfinite(x)) v[k] = __float_as_uint(__uint_as_float(v[k]) + x);
+            }
+          }
+      }
       uint32_t w[32];
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        uint32_t v[32];
-        read(2 * c + half, v);
-#pragma unroll
-        for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * inv);
-        if (dirty && mine) {   // non-finite values of masked tiles, kept out of the product, reach the rows that see them
-          for (int i = 0; i < 8; ++i)
-            for (uint32_t bits = dirty[i]; bits; bits &= bits - 1) {
-              const int key = (p0 / kTcKeys + (i >> 2)) * kTcKeys + (i & 3) * 32 + __ffs(bits) - 1;
-              if (key > pos) break;
-              const __nv_bfloat16* src = V + kvh * a->v.head + (row0 + key) * a->v.row + (2 * c + half) * 32;
-#pragma unroll
-              for (int k = 0; k < 32; ++k) {
-                const float x = __bfloat162float(src[k]);
-                if (!isfinite(x)) v[k] = __float_as_uint(__uint_as_float(v[k]) + x);
-              }
-            }
-        }
-#pragma unroll
-        for (int k = 0; k < 16; ++k)
-          w[half * 16 + k] = ptx::pack_bf16x2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1]));
-      }
+      for (int k = 0; k < 32; ++k) w[k] = ptx::pack_bf16x2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1]));
       rows_out.store(w, c * 128, wide != 0);
     }
   }

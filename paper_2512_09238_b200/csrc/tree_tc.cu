@@ -60,7 +60,9 @@ struct TreeTcSrc {
     for (int half = 0; half < D / 64; ++half)
       ptx::tma_load_2d(dst + half * kTcHalfBytes, is_v ? mv : mk, half * 64, y, bar);
   }
-  __device__ __forceinline__ int row_key(int, int) const { return 0; }
+  int row;
+  __device__ __forceinline__ void begin_row(int r) { row = r; }
+  __device__ __forceinline__ int row_key(int) const { return 0; }
   __device__ __forceinline__ int last(int, int t) const {
     int y, c;
     slice.get(t, y, c);
@@ -76,7 +78,7 @@ struct TreeTcSrc {
   __device__ __forceinline__ int note_slot(int) const { return 0; }
 
   template <typename Read>
-  __device__ __forceinline__ void store(int h, int row, bool seen, float m, float l, const uint32_t*, Read read) const {
+  __device__ __forceinline__ void store(int h, bool seen, float m, float l, const uint32_t*, Read read) const {
     const int r = kShared ? h * kTcRows + row : row;
     const size_t at = at0 + (kShared ? 0 : size_t(h) * plan->rows) + r;
     if (r < rows) ws->ml[at] = seen ? make_float2(m, l) : make_float2(-INFINITY, 0.f);
@@ -86,6 +88,7 @@ struct TreeTcSrc {
     for (int c = 0; c < D / 32; ++c) {
       uint32_t v[32];
       read(c, v);
+      ptx::tc_wait_ld();
       rows_out.store(v, c * 128, true);
     }
   }
