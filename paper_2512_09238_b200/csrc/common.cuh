@@ -5,6 +5,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "tca.h"
 
 namespace tca {
@@ -103,6 +105,20 @@ DecodeWs decode_ws_layout(const tca_params* prm, int64_t rows_total, int64_t n_u
 // completed and its writes are visible, so it must come before the first dependent access.
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void pdl_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;"); }
+
+// Lets `kernel` use `bytes` of dynamic shared memory on the current device.  Remembered per kernel and
+// device (the driver call costs a good part of a microsecond), so a second call is free.
+template <auto kernel>
+inline int allow_smem(int bytes) {
+  static std::atomic<uint64_t> done{0};
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return TCA_ERR_CUDA;
+  const uint64_t bit = dev < 64 ? uint64_t(1) << dev : 0;
+  if (bit && (done.load(std::memory_order_relaxed) & bit)) return TCA_OK;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return TCA_ERR_CUDA;
+  done.fetch_or(bit, std::memory_order_relaxed);
+  return TCA_OK;
+}
 
 template <typename... KArgs, typename... Args>
 inline int launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, Args... args) {

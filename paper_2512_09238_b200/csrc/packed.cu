@@ -81,7 +81,7 @@ int launch_packed_simt(const tca_params* prm, const void* Q, const void* K, cons
   const int64_t n = packed_max_tiles(a.rows, a.n_seq, kSimtRows / G) * a.n_kv_heads;
   if (n >= (int64_t(1) << 31)) return TCA_ERR_UNSUPPORTED;
   auto kern = packed_simt_kernel<T, D>;
-  TCA_CHECK_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SimtSmem<D>::kBytes));
+  if (allow_smem<packed_simt_kernel<T, D>>(SimtSmem<D>::kBytes) != TCA_OK) return TCA_ERR_CUDA;
   return launch_pdl(kern, dim3(unsigned(n)), dim3(kSimtThreads), size_t(SimtSmem<D>::kBytes), s,
                     static_cast<const T*>(Q), static_cast<const T*>(K), static_cast<const T*>(V), a,
                     prm->sm_scale * 1.4426950408889634f, static_cast<T*>(O));

@@ -145,7 +145,7 @@ int launch_packed_tc(const tca_params* prm, const void* Q, const void* K, const 
       !encode_map_3d(&mv, V, D, a.rows, a.n_kv_heads, a.v.row, a.v.head, kTcKeys, 1))
     return TCA_ERR_CUDA;
   auto kern = packed_tc_kernel<D>;
-  TCA_CHECK_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, TcLayout<D>::bytes));
+  if (allow_smem<packed_tc_kernel<D>>(TcLayout<D>::bytes) != TCA_OK) return TCA_ERR_CUDA;
   // Longest tiles first over all heads balances best, but then the resident CTAs read all heads' keys
   // at once; when those do not fit the L2 the heads go one after another.
   const int unit_major = a.rows * a.n_kv_heads * D * 4 > l2_bytes() / 2 ? 1 : 0;

@@ -277,8 +277,8 @@ int launch_tree(const tca_params* prm, const void* q, const void* kd, const void
   if (tree_on_tensor_cores(prm)) {
     st = launch_tree_tc(prm, q, c, plan, ws, s);
   } else {
-    auto kern = tree_simt_kernel<T, D>;
-    TCA_CHECK_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SimtSmem<D>::kBytes));
+  auto kern = tree_simt_kernel<T, D>;
+  if (allow_smem<tree_simt_kernel<T, D>>(SimtSmem<D>::kBytes) != TCA_OK) return TCA_ERR_CUDA;
     st = launch_pdl(kern, dim3(unsigned(ctas)), dim3(kSimtThreads), size_t(SimtSmem<D>::kBytes), s,
                     static_cast<const T*>(q), static_cast<const T*>(c->k), static_cast<const T*>(c->v),
                     static_cast<const int64_t*>(c->state), U, c->tail_cap, plan, scale, ws);

@@ -129,7 +129,7 @@ int launch(const tca_params* prm, const void* q, const tca_cache_desc* c, const 
       !encode_map(&mv, c->v, D, c->rows_total, 0, 0))
     return TCA_ERR_CUDA;
   auto kern = tree_tc_kernel<D, kShared>;
-  TCA_CHECK_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, TcLayout<D>::bytes));
+  if (allow_smem<tree_tc_kernel<D, kShared>>(TcLayout<D>::bytes) != TCA_OK) return TCA_ERR_CUDA;
   return launch_pdl(kern, dim3(unsigned(plan.n_slots * plan.row_blocks)), dim3(kTcThreads), size_t(TcLayout<D>::bytes), s, mq,
                     mk, mv, static_cast<const int64_t*>(c->state), U, c->tail_cap, plan,
                     prm->sm_scale * 1.4426950408889634f, ws);
