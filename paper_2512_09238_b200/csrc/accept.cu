@@ -15,7 +15,7 @@ struct AcceptCounts {
 };
 
 template <typename T>
-__global__ void __launch_bounds__(kCompressThreads)
+__global__ void __launch_bounds__(kCompressThreads, 3)
 cache_accept_kernel(const T* __restrict__ k_draft, const T* __restrict__ v_draft, const T* __restrict__ q_draft, int n_draft,
                     const int32_t* __restrict__ path, const __grid_constant__ AcceptCounts counts, int seq0,
                     T* __restrict__ Kc, T* __restrict__ Vc, int32_t* __restrict__ pos, int64_t* __restrict__ state,

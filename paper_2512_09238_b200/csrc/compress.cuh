@@ -1,7 +1,7 @@
 // Compression of the block that leaves the window while tokens are appended (Section 4.2, "Online
 // Token Selection in Decoding Stage"), shared by the calls that append: score the b oldest keys of
 // a unit's ring with the current query group (Eq. 5 restricted to the block, fp64), keep the top
-// t_keep by the same radix select the prefill uses, and move those rows to the end of the global
+// t_keep by the order the prefill uses, and move those rows to the end of the global
 // region in ascending position.
 #pragma once
 #include "common.cuh"
@@ -10,6 +10,7 @@
 namespace tca {
 
 constexpr int kCompressThreads = 256;   // CTA size of every kernel that calls this
+static_assert(kCompressThreads == 2 * kMaxBlock, "two threads per key of a block");
 
 // Called by the whole CTA.  q_unit: query of the unit's first head, q_stride elements to the next
 // head's.  The rows must be visible to the CTA (a barrier after they were written); on return the
@@ -25,72 +26,136 @@ __device__ __forceinline__ void compress_oldest_block(const T* __restrict__ q_un
   __shared__ double xs[kMaxGroup][kMaxBlock];
   __shared__ double lse[kMaxGroup];
   __shared__ int kept_slot[kMaxBlock];
+  __shared__ unsigned long long keys[kMaxBlock];
+  __shared__ int ranks[kMaxBlock];
+  __shared__ unsigned kept_mask[kMaxBlock / 32];
+  // 16 lanes per row, D/16 adjacent elements each, added in the order of the elements and then across the
+  // lanes; four rows per 16-lane group are requested before the first product.
   const int EPL = D / 16;
-  for (int i0 = 0; i0 < b; i0 += kCompressThreads / 16) {  // uniform trip count: shuffles below need whole warps
-    const int i = min(i0 + grp, b - 1);
-    int64_t slot = tail_head + i;
-    if (slot >= tail_cap) slot -= tail_cap;
-    const T* krow = Kc + (ring + slot) * D + lane16 * EPL;
+  constexpr int kGroups = kCompressThreads / 16, kBatch = 4;
+  for (int i0 = 0; i0 < b; i0 += kGroups * kBatch) {
+    float4 kf[kBatch][2];
+#pragma unroll
+    for (int s = 0; s < kBatch; ++s) {
+      int64_t slot = tail_head + min(i0 + s * kGroups + grp, b - 1);
+      if (slot >= tail_cap) slot -= tail_cap;
+      const T* krow = Kc + (ring + slot) * D + lane16 * EPL;
+      load4(krow, kf[s][0]);
+      if (EPL == 8) load4(krow + 4, kf[s][1]);
+    }
+#pragma unroll 1
     for (int g = 0; g < G; ++g) {
       const T* qrow = q_unit + g * q_stride + lane16 * EPL;
-      double acc = 0.0;
-      for (int e = 0; e < EPL; ++e) acc = fma(double(elt_to_float(qrow[e])), double(elt_to_float(krow[e])), acc);
+      float4 qf[2];
+      load4(qrow, qf[0]);
+      if (EPL == 8) load4(qrow + 4, qf[1]);
 #pragma unroll
-      for (int off = 8; off > 0; off >>= 1) acc += shfl_xor_double(acc, off);
-      if (lane16 == 0 && i0 + grp < b) xs[g][i] = acc * sm_scale;
+      for (int s = 0; s < kBatch; ++s) {
+        double acc = 0.0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          if (h * 4 >= EPL) continue;
+          acc = fma(double(qf[h].x), double(kf[s][h].x), acc);
+          acc = fma(double(qf[h].y), double(kf[s][h].y), acc);
+          acc = fma(double(qf[h].z), double(kf[s][h].z), acc);
+          acc = fma(double(qf[h].w), double(kf[s][h].w), acc);
+        }
+#pragma unroll
+        for (int off = 8; off > 0; off >>= 1) acc += shfl_xor_double(acc, off);
+        const int i = i0 + s * kGroups + grp;
+        if (lane16 == 0 && i < b) xs[g][i] = acc * sm_scale;
+      }
     }
   }
   __syncthreads();
   if (warp < G) {  // log-sum-exp of head `warp` over the block
     double mx = -1.0e308;
+#pragma unroll 4
     for (int i = lane; i < b; i += 32) mx = fmax(mx, xs[warp][i]);
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) mx = fmax(mx, shfl_xor_double(mx, off));
     double sum = 0.0;
+#pragma unroll 4
     for (int i = lane; i < b; i += 32) sum += exp(xs[warp][i] - mx);
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) sum += shfl_xor_double(sum, off);
     if (lane == 0) lse[warp] = mx + log(sum);
   }
   __syncthreads();
-  if (warp == 0) {
-    unsigned long long key[4];
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      const int i = s * 32 + lane;
-      double score = -1.0e308;
-      if (i < b) {
-        if (G == 1) {
-          score = xs[0][i] - lse[0];
-        } else {
-          double top = -1.0e308;
-          for (int g = 0; g < G; ++g) top = fmax(top, xs[g][i] - lse[g]);
-          double sum = 0.0;
-          for (int g = 0; g < G; ++g) sum += exp(xs[g][i] - lse[g] - top);
-          score = top + log(sum);
-        }
-      }
-      key[s] = ordered_key(score);
+  if (tid < b) {   // score of key `tid`: the mean over the group, in logs (the 1/G is common to all)
+    double score;
+    if (G == 1) {
+      score = xs[0][tid] - lse[0];
+    } else {
+      double top = -1.0e308;
+      for (int g = 0; g < G; ++g) top = fmax(top, xs[g][tid] - lse[g]);
+      double sum = 0.0;
+#pragma unroll 4
+      for (int g = 0; g < G; ++g) sum += exp(xs[g][tid] - lse[g] - top);
+      score = top + log(sum);
     }
-    const unsigned keep = radix_select_top_t(key, b, t_keep, lane);
-    int before = 0;
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      const bool k = (keep >> s) & 1u;
-      const unsigned bal = __ballot_sync(0xffffffffu, k);
-      if (k) kept_slot[before + __popc(bal & ((1u << lane) - 1u))] = s * 32 + lane;
-      before += __popc(bal);
+    keys[tid] = ordered_key(score);
+  }
+  __syncthreads();
+  // Top t_keep by rank: a key's rank is the number of larger keys and of equal ones at lower indices, the
+  // set the radix select of the prefill keeps.  With one block per CTA the b^2 comparisons (two threads per
+  // key, half of them each) take a quarter of the time of its 50 or so dependent rounds.
+  {
+    const int i = tid & (kMaxBlock - 1), half = tid / kMaxBlock;
+    int rank = 0;
+    if (i < b) {
+      const unsigned long long mine = keys[i];
+      const int j0 = half * (b / 2), j1 = half == 0 ? b / 2 : b;
+#pragma unroll 8
+      for (int j = j0; j < j1; ++j) rank += (keys[j] > mine || (keys[j] == mine && j < i)) ? 1 : 0;
+    }
+    if (half == 1) ranks[i] = rank;
+    __syncthreads();
+    if (half == 0) {
+      const bool keep = i < b && rank + ranks[i] < t_keep;
+      const unsigned bal = __ballot_sync(0xffffffffu, keep);
+      if (lane == 0) kept_mask[warp] = bal;
+      __syncwarp();
+    }
+    __syncthreads();
+    if (half == 0 && ((kept_mask[warp] >> lane) & 1u)) {
+      int before = __popc(kept_mask[warp] & ((1u << lane) - 1u));
+      for (int w = 0; w < warp; ++w) before += __popc(kept_mask[w]);
+      kept_slot[before] = i;
     }
   }
   __syncthreads();
   // ---- move the kept rows to the end of the global region (ring and region are disjoint)
-  for (int i = tid; i < t_keep * D; i += kCompressThreads) {
-    const int r = i / D, e = i - r * D;
-    int64_t slot = tail_head + kept_slot[r];
+  // 16-byte pieces, four rows' worth in flight per thread
+  const int shift = 31 - __clz(D * int(sizeof(T)) / 16);
+  const int n_pieces = t_keep << shift;
+  uint4* K4 = reinterpret_cast<uint4*>(Kc);
+  uint4* V4 = reinterpret_cast<uint4*>(Vc);
+  for (int i0 = tid; i0 < n_pieces; i0 += 4 * kCompressThreads) {
+    uint4 kv[4], vv[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int i = i0 + j * kCompressThreads;
+      if (i >= n_pieces) continue;
+      int64_t slot = tail_head + kept_slot[i >> shift];
+      if (slot >= tail_cap) slot -= tail_cap;
+      const int64_t src = ((ring + slot) << shift) + (i & ((1 << shift) - 1));
+      kv[j] = K4[src];
+      vv[j] = V4[src];
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int i = i0 + j * kCompressThreads;
+      if (i >= n_pieces) continue;
+      const int64_t dst = ((seg + n_global) << shift) + i;
+      K4[dst] = kv[j];
+      V4[dst] = vv[j];
+    }
+  }
+  if (tid < t_keep) {
+    int64_t slot = tail_head + kept_slot[tid];
     if (slot >= tail_cap) slot -= tail_cap;
-    Kc[(seg + n_global + r) * D + e] = Kc[(ring + slot) * D + e];
-    Vc[(seg + n_global + r) * D + e] = Vc[(ring + slot) * D + e];
-    if (e == 0) pos[seg + n_global + r] = pos[ring + slot];
+    pos[seg + n_global + tid] = pos[ring + slot];
   }
 }
 

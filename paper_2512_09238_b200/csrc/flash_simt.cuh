@@ -24,12 +24,6 @@ struct SimtSmem {
   static constexpr int kBytes = kFloats * 4;
 };
 
-__device__ __forceinline__ void load4(const float* p, float4& v) { v = *reinterpret_cast<const float4*>(p); }
-__device__ __forceinline__ void load4(const __nv_bfloat16* p, float4& v) {
-  const uint2 w = *reinterpret_cast<const uint2*>(p);
-  v = make_float4(bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y));
-}
-
 // 64 rows of D elements into shared memory; rows >= n become zeros and are not read.
 template <typename T, int D, typename RowPtr>
 __device__ __forceinline__ void simt_load_rows(float* dst, int n, RowPtr row_ptr) {

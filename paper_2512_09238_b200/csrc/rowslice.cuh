@@ -57,6 +57,13 @@ struct RowF<float, 8> {
   }
 };
 
+// four consecutive elements as floats
+__device__ __forceinline__ void load4(const float* p, float4& v) { v = *reinterpret_cast<const float4*>(p); }
+__device__ __forceinline__ void load4(const __nv_bfloat16* p, float4& v) {
+  const uint2 w = *reinterpret_cast<const uint2*>(p);
+  v = make_float4(bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y));
+}
+
 __device__ __forceinline__ float elt_to_float(float x) { return x; }
 __device__ __forceinline__ float elt_to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ void store_elt(float* p, float x) { *p = x; }
