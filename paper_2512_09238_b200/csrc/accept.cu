@@ -15,7 +15,7 @@ struct AcceptCounts {
 };
 
 template <typename T>
-__global__ void __launch_bounds__(kCompressThreads, 3)
+__global__ void __launch_bounds__(kCompressThreads, 2)
 cache_accept_kernel(const T* __restrict__ k_draft, const T* __restrict__ v_draft, const T* __restrict__ q_draft, int n_draft,
                     const int32_t* __restrict__ path, const __grid_constant__ AcceptCounts counts, int seq0,
                     T* __restrict__ Kc, T* __restrict__ Vc, int32_t* __restrict__ pos, int64_t* __restrict__ state,
@@ -148,7 +148,7 @@ extern "C" int tca_cache_accept(const tca_params* prm, tca_cache_desc* c, const 
         const int64_t u = int64_t(s0 + i) * H + h;
         const int64_t k = compressions(u, n);
         c->n_global[u] += k * c->t_keep[u];
-        c->tail_head[u] = (c->tail_head[u] + k * prm->block) % c->tail_cap;
+        if (k > 0) c->tail_head[u] = (c->tail_head[u] + k * prm->block) % c->tail_cap;
         c->n_tail[u] += n - k * prm->block;
         c->seq_len[u] += n;
       }

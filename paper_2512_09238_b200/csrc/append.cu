@@ -13,7 +13,7 @@ namespace {
 constexpr int kThreads = kCompressThreads;
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads, 3)
+__global__ void __launch_bounds__(kThreads, 2)
 cache_append_kernel(const T* __restrict__ k_new, const T* __restrict__ v_new, const T* __restrict__ q_cur,
                     T* __restrict__ Kc, T* __restrict__ Vc, int32_t* __restrict__ pos,
                     int64_t* __restrict__ state, int64_t tail_cap, int D, int G, int b, int window,

@@ -30,41 +30,49 @@ __device__ __forceinline__ void compress_oldest_block(const T* __restrict__ q_un
   __shared__ int ranks[kMaxBlock];
   __shared__ unsigned kept_mask[kMaxBlock / 32];
   // 16 lanes per row, D/16 adjacent elements each, added in the order of the elements and then across the
-  // lanes; four rows per 16-lane group are requested before the first product.
+  // lanes.  What bounds this is the conversion to fp64 (a quarter of the FMA rate), so the queries are
+  // converted once, into shared memory, and a key once for all heads; four rows go through the reduction
+  // across the lanes together (a transposing butterfly, the same pairs in the same order as row by row).
+  // One block of 128 keys, 4 heads: 22.5 thousand clocks with a conversion per factor and a reduction per row.
+  __shared__ double qs[kMaxGroup * kMaxBlock];     // head_dim <= 128
+  static_assert(kMaxBlock >= 128, "a query per row of qs");
+  for (int i = tid; i < G * D; i += kCompressThreads) qs[i] = double(elt_to_float(q_unit[(i / D) * q_stride + i % D]));
+  __syncthreads();
   const int EPL = D / 16;
   constexpr int kGroups = kCompressThreads / 16, kBatch = 4;
   for (int i0 = 0; i0 < b; i0 += kGroups * kBatch) {
-    float4 kf[kBatch][2];
+    double kd[kBatch][8];
 #pragma unroll
     for (int s = 0; s < kBatch; ++s) {
       int64_t slot = tail_head + min(i0 + s * kGroups + grp, b - 1);
       if (slot >= tail_cap) slot -= tail_cap;
       const T* krow = Kc + (ring + slot) * D + lane16 * EPL;
-      load4(krow, kf[s][0]);
-      if (EPL == 8) load4(krow + 4, kf[s][1]);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (h * 4 < EPL) load4(krow + h * 4, f);
+        kd[s][h * 4] = f.x; kd[s][h * 4 + 1] = f.y; kd[s][h * 4 + 2] = f.z; kd[s][h * 4 + 3] = f.w;
+      }
     }
 #pragma unroll 1
     for (int g = 0; g < G; ++g) {
-      const T* qrow = q_unit + g * q_stride + lane16 * EPL;
-      float4 qf[2];
-      load4(qrow, qf[0]);
-      if (EPL == 8) load4(qrow + 4, qf[1]);
+      const double* qrow = qs + g * D + lane16 * EPL;
+      double acc[kBatch] = {0.0, 0.0, 0.0, 0.0};
 #pragma unroll
-      for (int s = 0; s < kBatch; ++s) {
-        double acc = 0.0;
+      for (int e = 0; e < 8; ++e) {
+        if (e >= EPL) continue;
+        const double qe = qrow[e];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          if (h * 4 >= EPL) continue;
-          acc = fma(double(qf[h].x), double(kf[s][h].x), acc);
-          acc = fma(double(qf[h].y), double(kf[s][h].y), acc);
-          acc = fma(double(qf[h].z), double(kf[s][h].z), acc);
-          acc = fma(double(qf[h].w), double(kf[s][h].w), acc);
-        }
-#pragma unroll
-        for (int off = 8; off > 0; off >>= 1) acc += shfl_xor_double(acc, off);
-        const int i = i0 + s * kGroups + grp;
-        if (lane16 == 0 && i < b) xs[g][i] = acc * sm_scale;
+        for (int s = 0; s < kBatch; ++s) acc[s] = fma(qe, kd[s][e], acc[s]);
       }
+      const bool up8 = lane16 & 8, up4 = lane16 & 4;
+      const double r0 = (up8 ? acc[2] : acc[0]) + shfl_xor_double(up8 ? acc[0] : acc[2], 8);
+      const double r1 = (up8 ? acc[3] : acc[1]) + shfl_xor_double(up8 ? acc[1] : acc[3], 8);
+      double r = (up4 ? r1 : r0) + shfl_xor_double(up4 ? r0 : r1, 4);
+      r += shfl_xor_double(r, 2);
+      r += shfl_xor_double(r, 1);
+      const int i = i0 + ((up8 ? 2 : 0) + (up4 ? 1 : 0)) * kGroups + grp;   // the row whose total ends up here
+      if ((lane16 & 3) == 0 && i < b) xs[g][i] = r * sm_scale;
     }
   }
   __syncthreads();
