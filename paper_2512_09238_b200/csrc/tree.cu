@@ -28,7 +28,6 @@ TreePlan tree_plan(const tca_params* prm, int n_draft) {
   p.streams = tc && p.rows <= 128 ? 2 : 1;
   p.rows_per_cta = !tc ? kSimtRows : p.rows <= 128 ? 128 : 256;
   p.row_blocks = (p.rows + p.rows_per_cta - 1) / p.rows_per_cta;
-  p.step_rows = 128;
   p.min_steps = p.streams;
   // one wave of resident CTAs; with more units than slices fit that wave, two slices per unit and a
   // wave on top, so that units of different lengths still balance
@@ -65,7 +64,7 @@ tree_simt_kernel(const T* __restrict__ q, const T* __restrict__ Kc, const T* __r
   pdl_wait();
   pdl_launch_dependents();
   if (threadIdx.x < 32) {
-    const TreeSlice s = tree_find(state, n_units, tail_cap, plan.n_slots, plan.step_rows, plan.min_steps, kSimtKeys,
+    const TreeSlice s = tree_find(state, n_units, int(tail_cap), plan.n_slots, plan.min_steps, kSimtKeys,
                                   int(blockIdx.x) / plan.row_blocks, threadIdx.x);
     if (threadIdx.x == 0) slice = s;
   }
@@ -314,6 +313,7 @@ extern "C" int tca_attn_tree(const tca_params* prm, const void* q, const void* k
   TCA_CHECK_ARG(aligned(q, 16) && aligned(k_draft, 16) && aligned(v_draft, 16) && aligned(O, 16) && aligned(ws, 256));
   TCA_CHECK_ARG(aligned(c->k, 16) && aligned(c->v, 16) && aligned(parent, 4) && aligned(n_live, 4));
   TCA_CHECK_ARG(c->n_units == int64_t(prm->batch) * prm->n_kv_heads && c->tail_cap >= 1);
+  TCA_CHECK_ARG(c->rows_total >= 1 && c->rows_total < (int64_t(1) << 31));
   if (bad_tree_shape(prm, n_draft)) return TCA_ERR_UNSUPPORTED;
   const TreePlan plan = tree_plan(prm, n_draft);
   const TreeWs lay = tree_ws_layout(prm, plan, ws);

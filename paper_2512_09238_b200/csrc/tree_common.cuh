@@ -2,7 +2,6 @@
 // of a slice, and the layout of the partial results.
 #pragma once
 #include "common.cuh"
-#include "decode_common.cuh"
 
 namespace tca {
 
@@ -13,8 +12,7 @@ struct TreePlan {
   int row_blocks;    // CTAs per slice
   int streams;       // partial results a CTA writes per row
   int n_slots;       // slices of all units together, at most
-  int step_rows;     // slices are multiples of this many rows ...
-  int min_steps;     // ... and at least this many steps long
+  int min_steps;     // shortest slice, in steps of kTreeStep rows
 };
 TreePlan tree_plan(const tca_params* prm, int n_draft);
 
@@ -75,66 +73,52 @@ struct TreeSlice {
   SliceTiles tiles;
 };
 
-// The lin-th slice over all units.  Rows are dealt in steps of `step` rows; the slice length is the
+// The lin-th slice over all units.  Rows are dealt in steps of kTreeStep rows; the slice length is the
 // smallest multiple of it for which no more than n_slots slices exist, so the slices of all units fit the
 // launch whatever the cache holds.  It is worked out from the device's state words: a captured launch
-// stays right when the cache has grown since.  Whole warp; every lane returns the same.
-__device__ __forceinline__ TreeSlice tree_find(const int64_t* state, int n_units, int64_t tail_cap, int n_slots, int step,
-                                               int min_steps, int tile, int lin, int lane) {
-  constexpr int kHeld = 4;   // units held in registers per lane; more are read again
-  const int groups = min(kHeld, (n_units + 31) / 32);
+// stays right when the cache has grown since.  Whole warp; every lane returns the same.  Everything is
+// 32-bit (a cache has fewer than 2^31 rows) and without 64-bit divisions: this stands between the launch and
+// the first load (3700 -> 1500 clocks).
+constexpr int kTreeStep = 128, kTreeStepLog = 7;
+
+__device__ __forceinline__ TreeSlice tree_find(const int64_t* state, int n_units, int tail_cap, int n_slots, int min_steps,
+                                               int tile, int lin, int lane) {
+  int n_global = 0, n_tail = 0;     // unit `lane`; units past the 32nd are read again in every pass
+  if (lane < n_units) {
+    const int64_t* st = state + size_t(lane) * TCA_STATE_WORDS;
+    n_global = int(st[TCA_ST_N_GLOBAL]);
+    n_tail = int(st[TCA_ST_N_TAIL]);
+  }
+  const int first = (n_global + n_tail + kTreeStep - 1) >> kTreeStepLog;
   auto steps_of = [&](int u) -> int {
     if (u >= n_units) return 0;
     const int64_t* st = state + size_t(u) * TCA_STATE_WORDS;
-    return int((st[TCA_ST_N_GLOBAL] + st[TCA_ST_N_TAIL] + step - 1) / step);
+    return int((st[TCA_ST_N_GLOBAL] + st[TCA_ST_N_TAIL] + kTreeStep - 1) >> kTreeStepLog);
   };
-  int held[kHeld], most = 0, sum = 0;
-  UnitView first{};          // the view of unit `lane`, for the units most calls have
-#pragma unroll
-  for (int k = 0; k < kHeld; ++k) {
-    held[k] = 0;
-    if (k >= groups) continue;
-    if (k == 0) {
-      if (lane < n_units) first = load_unit(state, lane, tail_cap);
-      held[0] = int((first.len() + step - 1) / step);
-    } else {
-      held[k] = steps_of(k * 32 + lane);
-    }
-    most = max(most, held[k]);
-    sum += held[k];
-  }
-  for (int u = 32 * kHeld + lane; u < n_units; u += 32) {
+  int most = first, sum = first;
+  for (int u = 32 + lane; u < n_units; u += 32) {
     const int n = steps_of(u);
     most = max(most, n);
     sum += n;
   }
   most = __reduce_max_sync(0xffffffffu, most);
   sum = __reduce_add_sync(0xffffffffu, sum);
-  auto count = [&](int per) {   // slices of at most `per` steps
-    int c = 0;
-#pragma unroll
-    for (int k = 0; k < kHeld; ++k)
-      if (k < groups) c += (held[k] + per - 1) / per;
-    for (int u = 32 * kHeld + lane; u < n_units; u += 32) c += (steps_of(u) + per - 1) / per;
-    return int(__reduce_add_sync(0xffffffffu, c));
-  };
-  // count(per) <= sum / per + n_units, which bounds the search from above
-  int lo = max(min_steps, (sum + n_slots - 1) / n_slots);
-  int hi = max(lo, n_slots > n_units ? min(most, (sum + n_slots - n_units - 1) / (n_slots - n_units)) : most);
+  auto parts = [](int steps, int per) { return int((unsigned(steps) + unsigned(per) - 1u) / unsigned(per)); };
+  // slices of `per` steps number at most sum / per + n_units, which bounds the search from above
+  int lo = max(min_steps, parts(sum, n_slots));
+  int hi = max(lo, n_slots > n_units ? min(most, parts(sum, n_slots - n_units)) : most);
   while (lo < hi) {
     const int mid = lo + (hi - lo) / 2;
-    if (count(mid) <= n_slots) hi = mid; else lo = mid + 1;
+    int c = parts(first, mid);
+    for (int u = 32 + lane; u < n_units; u += 32) c += parts(steps_of(u), mid);
+    if (int(__reduce_add_sync(0xffffffffu, c)) <= n_slots) hi = mid; else lo = mid + 1;
   }
   TreeSlice s;
   s.u = -1;
-  int offset = 0;
-  for (int k = 0; k * 32 < n_units; ++k) {
-    int mine = 0;
-#pragma unroll
-    for (int h = 0; h < kHeld; ++h)
-      if (h == k) mine = held[h];
-    if (k >= kHeld) mine = steps_of(k * 32 + lane);
-    const int np = (mine + lo - 1) / lo;
+  int offset = 0, steps = 0;
+  for (int u0 = 0; u0 < n_units; u0 += 32) {
+    const int mine = u0 == 0 ? first : steps_of(u0 + lane);
+    const int np = parts(mine, lo);
     int incl = np;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
@@ -144,39 +128,33 @@ __device__ __forceinline__ TreeSlice tree_find(const int64_t* state, int n_units
     const unsigned hit = __ballot_sync(0xffffffffu, lin < offset + incl);
     if (hit) {
       const int l = __ffs(hit) - 1;
-      s.u = k * 32 + l;
+      s.u = u0 + l;
       s.np = __shfl_sync(0xffffffffu, np, l);
       s.base = offset + __shfl_sync(0xffffffffu, incl - np, l);
+      steps = __shfl_sync(0xffffffffu, mine, l);
       s.part = lin - s.base;
       break;
     }
     offset += __shfl_sync(0xffffffffu, incl, 31);
   }
   if (s.u < 0) return s;
-  UnitView v;
-  if (s.u < 32) {
-    v.seg = __shfl_sync(0xffffffffu, first.seg, s.u);
-    v.gcap = __shfl_sync(0xffffffffu, first.gcap, s.u);
-    v.n_global = __shfl_sync(0xffffffffu, first.n_global, s.u);
-    v.tail_head = __shfl_sync(0xffffffffu, first.tail_head, s.u);
-    v.n_tail = __shfl_sync(0xffffffffu, first.n_tail, s.u);
-    v.tail_cap = tail_cap;
-  } else {
-    v = load_unit(state, s.u, tail_cap);
-  }
-  const int64_t len = v.len(), n_steps = (len + step - 1) / step;
-  const int64_t r0 = slice_begin(n_steps, s.np, s.part) * step;
-  const int64_t r1 = min(len, slice_begin(n_steps, s.np, s.part + 1) * step);
+  const int64_t* st = state + size_t(s.u) * TCA_STATE_WORDS;
+  const int seg = int(st[TCA_ST_SEG_START]), gcap = int(st[TCA_ST_GLOBAL_CAP]), ng = int(st[TCA_ST_N_GLOBAL]);
+  const int head = int(st[TCA_ST_TAIL_HEAD]), len = ng + int(st[TCA_ST_N_TAIL]);
+  // the unit's steps dealt evenly: the first `longer` slices have one more
+  const int each = int(unsigned(steps) / unsigned(s.np)), longer = steps - each * s.np;
+  const int r0 = (s.part * each + min(s.part, longer)) * kTreeStep;
+  const int r1 = min(len, r0 + (each + (s.part < longer ? 1 : 0)) * kTreeStep);
+  // runs: rows [r0, r1) of the global region, then of the ring up to its end, then from its start
+  const int wrap = ng + tail_cap - head;      // logical row that lies in the ring's slot 0
+  const int b1 = min(max(ng, r0), r1), b2 = min(max(wrap, r0), r1);
   s.tiles.tile = tile;
-  int64_t r = r0;
-#pragma unroll
-  for (int i = 0; i < 3; ++i) {
-    const int64_t n = r < r1 ? (r < v.n_global ? min(r1, v.n_global) - r : v.run(r, r1 - r)) : 0;
-    s.tiles.y[i] = n > 0 ? int(v.phys(r)) : 0;
-    s.tiles.n[i] = int(n);
-    r += n;
-    // a slice that begins inside the ring has no first run in the global region: the order is the same
-  }
+  s.tiles.y[0] = seg + r0;
+  s.tiles.n[0] = b1 - r0;
+  s.tiles.y[1] = seg + gcap + head + (b1 - ng);
+  s.tiles.n[1] = max(b2, b1) - b1;
+  s.tiles.y[2] = seg + gcap + (max(b2, b1) - wrap);
+  s.tiles.n[2] = r1 - max(b2, b1);
   return s;
 }
 

@@ -22,8 +22,9 @@ struct TreeTcSrc {
   const CUtensorMap *mq, *mk, *mv;
   const int64_t* state;
   int n_units;
-  int64_t tail_cap;
+  int tail_cap;
   const TreePlan* plan;
+  uint64_t stream;      // the cache streams through the L2: its lines go first
   const TreeWs* ws;
   SliceTiles slice;
   int q_row, rows, n;
@@ -32,7 +33,7 @@ struct TreeTcSrc {
   __device__ __forceinline__ void begin(int) {}
   __device__ __forceinline__ bool find(int k, int lane, Item& it) const {
     if (k > 0) return false;
-    const TreeSlice s = tree_find(state, n_units, tail_cap, plan->n_slots, plan->step_rows, plan->min_steps, kTcKeys,
+    const TreeSlice s = tree_find(state, n_units, tail_cap, plan->n_slots, plan->min_steps, kTcKeys,
                                   int(blockIdx.x) / plan->row_blocks, lane);
     if (s.u < 0) return false;
     const int rb = int(blockIdx.x) % plan->row_blocks, row0 = rb * plan->rows_per_cta;
@@ -58,7 +59,7 @@ struct TreeTcSrc {
     int y, c;
     slice.get(t, y, c);
     for (int half = 0; half < D / 64; ++half)
-      ptx::tma_load_2d(dst + half * kTcHalfBytes, is_v ? mv : mk, half * 64, y, bar);
+      ptx::tma_load_2d_hint(dst + half * kTcHalfBytes, is_v ? mv : mk, half * 64, y, bar, stream);
   }
   int row;
   __device__ __forceinline__ void begin_row(int r) { row = r; }
@@ -114,7 +115,8 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
   src.mq = &mq; src.mk = &mk; src.mv = &mv;
   src.state = state;
   src.n_units = n_units;
-  src.tail_cap = tail_cap;
+  src.tail_cap = int(tail_cap);
+  src.stream = ptx::l2_policy_evict_first();
   src.plan = &plan;
   src.ws = &ws;
   flash_tc<D, kShared>(src, smem, &sh, scale_log2e, ws.status);
