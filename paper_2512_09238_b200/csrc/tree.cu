@@ -28,12 +28,11 @@ TreePlan tree_plan(const tca_params* prm, int n_draft) {
   p.streams = tc && p.rows <= 128 ? 2 : 1;
   p.rows_per_cta = !tc ? kSimtRows : p.rows <= 128 ? 128 : 256;
   p.row_blocks = (p.rows + p.rows_per_cta - 1) / p.rows_per_cta;
-  p.min_steps = p.streams;
-  // one wave of resident CTAs; with more units than slices fit that wave, two slices per unit and a
-  // wave on top, so that units of different lengths still balance
+  p.min_share = tc ? 2 : 1;
+  p.lead = tc ? 3 : 0;
   const int resident = (tc ? 1 : 2) * sm_count();
-  const int wave = resident / p.row_blocks > 0 ? resident / p.row_blocks : 1;
-  p.n_slots = wave >= 2 * U ? wave : wave + 2 * U;
+  p.n_shares = resident / p.row_blocks > 0 ? resident / p.row_blocks : 1;
+  p.n_slots = p.n_shares + U;
   return p;
 }
 
@@ -60,39 +59,44 @@ tree_simt_kernel(const T* __restrict__ q, const T* __restrict__ Kc, const T* __r
                  const int64_t* __restrict__ state, int n_units, int64_t tail_cap, TreePlan plan, float scale_log2e,
                  TreeWs ws) {
   extern __shared__ float4 tree_smem[];
-  __shared__ TreeSlice slice;
+  __shared__ TreePiece piece;
   pdl_wait();
   pdl_launch_dependents();
-  if (threadIdx.x < 32) {
-    const TreeSlice s = tree_find(state, n_units, int(tail_cap), plan.n_slots, plan.min_steps, kSimtKeys,
-                                  int(blockIdx.x) / plan.row_blocks, threadIdx.x);
-    if (threadIdx.x == 0) slice = s;
-  }
-  __syncthreads();
-  if (slice.u < 0) return;
-  const int rb = int(blockIdx.x) % plan.row_blocks;
-  const int slot = slice.base + slice.part;
-  if (slice.part == 0 && rb == 0 && threadIdx.x == 0) ws.table[slice.u] = make_int2(slice.base, slice.np);
+  const int share = int(blockIdx.x) / plan.row_blocks, rb = int(blockIdx.x) % plan.row_blocks;
   const int row0 = rb * kSimtRows;
-  TreeSrc<T, D> src;
-  src.n = min(kSimtRows, plan.rows - row0);
-  src.q_rows = q + (int64_t(slice.u) * plan.rows + row0) * D;
-  src.Kc = Kc;
-  src.Vc = Vc;
-  src.tiles = slice.tiles;
-  float o[4][D / 16], m[4], l[4];
-  simt_flash<T, D>(src, scale_log2e, reinterpret_cast<float*>(tree_smem), o, m, l);
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  TreeFinder finder;
+  if (threadIdx.x < 32) finder.start(state, n_units, plan, share, threadIdx.x);
+  for (;;) {
+    if (threadIdx.x < 32) {
+      TreePiece p;
+      const bool more = finder.next(state, n_units, int(tail_cap), share, kSimtKeys, rb == 0, ws.table, threadIdx.x, p);
+      if (!more) p.u = -1;
+      if (threadIdx.x == 0) piece = p;
+    }
+    __syncthreads();
+    const TreePiece mine = piece;
+    __syncthreads();                       // read by all before the next one is written
+    if (mine.u < 0) return;
+    TreeSrc<T, D> src;
+    src.n = min(kSimtRows, plan.rows - row0);
+    src.q_rows = q + (int64_t(mine.u) * plan.rows + row0) * D;
+    src.Kc = Kc;
+    src.Vc = Vc;
+    src.tiles = mine.tiles;
+    float o[4][D / 16], m[4], l[4];
+    simt_flash<T, D>(src, scale_log2e, reinterpret_cast<float*>(tree_smem), o, m, l);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int r = row0 + ty * 4 + i;
-    if (r >= plan.rows) continue;
-    const size_t at = size_t(slot) * plan.rows + r;
+    for (int i = 0; i < 4; ++i) {
+      const int r = row0 + ty * 4 + i;
+      if (r >= plan.rows) continue;
+      const size_t at = size_t(mine.slot) * plan.rows + r;
 #pragma unroll
-    for (int c = 0; c < D / 64; ++c)
-      *reinterpret_cast<float4*>(ws.acc + at * D + tx * 4 + 64 * c) =
-          make_float4(o[i][c * 4], o[i][c * 4 + 1], o[i][c * 4 + 2], o[i][c * 4 + 3]);
-    if (tx == 0) ws.ml[at] = make_float2(m[i], l[i]);
+      for (int c = 0; c < D / 64; ++c)
+        *reinterpret_cast<float4*>(ws.acc + at * D + tx * 4 + 64 * c) =
+            make_float4(o[i][c * 4], o[i][c * 4 + 1], o[i][c * 4 + 2], o[i][c * 4 + 3]);
+      if (tx == 0) ws.ml[at] = make_float2(m[i], l[i]);
+    }
   }
 }
 
@@ -228,7 +232,7 @@ tree_combine_kernel(const T* __restrict__ q, const T* __restrict__ k_draft, cons
   pdl_wait();                 // the partial results come from the split kernel
   pdl_launch_dependents();
   if (!live) return;
-  // the slices of the unit, in order; a unit whose cache is empty has none
+  // the unit's partial results, in the order of its rows; a unit whose cache is empty has none
   const int2 where = cached > 0 ? ws.table[u] : make_int2(0, 0);
   const int n = where.y * plan.streams;
   const size_t first = size_t(where.x) * plan.streams;
@@ -270,7 +274,7 @@ int launch_tree(const tca_params* prm, const void* q, const void* kd, const void
                 cudaStream_t s) {
   const int U = prm->batch * prm->n_kv_heads;
   const float scale = prm->sm_scale * 1.4426950408889634f;
-  const int64_t ctas = int64_t(plan.n_slots) * plan.row_blocks;
+  const int64_t ctas = int64_t(plan.n_shares) * plan.row_blocks;
   if (ctas >= (int64_t(1) << 31)) return TCA_ERR_UNSUPPORTED;
   int st;
   if (tree_on_tensor_cores(prm)) {

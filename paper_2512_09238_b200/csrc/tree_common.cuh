@@ -9,14 +9,17 @@ namespace tca {
 struct TreePlan {
   int rows;          // G * T
   int rows_per_cta;
-  int row_blocks;    // CTAs per slice
+  int row_blocks;    // CTAs per share of the cache rows, one per rows_per_cta query rows
   int streams;       // partial results a CTA writes per row
-  int n_slots;       // slices of all units together, at most
-  int min_steps;     // shortest slice, in steps of kTreeStep rows
+  int min_share;     // steps of kTreeStep rows: a shorter share is all latency
+  int lead;          // steps that starting on a unit costs
+  int n_shares;      // shares the cache rows of all units are cut into, at most
+  int n_slots;       // slots for partial results: a share touches a run of units, so (share, unit) pairs
+                     // number at most n_shares + units
 };
 TreePlan tree_plan(const tca_params* prm, int n_draft);
 
-// Workspace: 256-byte header (word 0: sticky status), one (first slot, slices) pair per unit, the row
+// Workspace: 256-byte header (word 0: sticky status), one (first slot, slots) pair per unit, the row
 // statistics (maximum in log2 units, sum) and the unnormalised outputs of every (slot, stream, row).
 constexpr size_t kTreeHeaderBytes = 256;
 struct TreeWs {
@@ -41,7 +44,7 @@ inline TreeWs tree_ws_layout(const tca_params* prm, const TreePlan& p, void* ws)
   return w;
 }
 
-// The rows of one slice: up to three runs of physically contiguous cache rows (global region, ring up
+// The rows of one piece of a unit: up to three runs of physically contiguous cache rows (global region, ring up
 // to its end, ring from its start), walked in tiles of `tile` rows; the last tile of a run may be short.
 struct SliceTiles {
   int y[3], n[3];
@@ -65,97 +68,102 @@ struct SliceTiles {
   }
 };
 
-// A slice of a unit's rows.
-struct TreeSlice {
-  int u;             // -1: no such slice
-  int part, np;      // slice within the unit, slices of the unit
-  int base;          // slot of the unit's first slice
+// What one CTA attends to at a time: a piece of a unit's rows.
+struct TreePiece {
+  int u;
+  int slot;          // where its partial results go
   SliceTiles tiles;
 };
 
-// The lin-th slice over all units.  Rows are dealt in steps of kTreeStep rows; the slice length is the
-// smallest multiple of it for which no more than n_slots slices exist, so the slices of all units fit the
-// launch whatever the cache holds.  It is worked out from the device's state words: a captured launch
-// stays right when the cache has grown since.  Whole warp; every lane returns the same.  Everything is
-// 32-bit (a cache has fewer than 2^31 rows) and without 64-bit divisions: this stands between the launch and
-// the first load (3700 -> 1500 clocks).
+// How the cache rows of all units are dealt: laid end to end in steps of kTreeStep rows, they are cut into
+// equal shares, one per CTA (per block of query rows), wherever the cuts fall; a share that runs into
+// the next unit works on both, one after the other.  A unit counts plan.lead steps more than it has, because
+// starting on one costs about that much.  (Giving each unit a whole number of slices of its own left the
+// longest 13 % above the mean with 32 units of 65 to 142 steps.)  The pair (share i, unit u) has slot i + u:
+// pairs advance in one of the two at a time, so slots are distinct and a unit's are consecutive.
+// The cuts follow from the device's state words, not from the host's mirror: a captured launch stays right
+// when the cache has grown since.  Whole warp; every lane returns the same.  All 32-bit (a cache has
+// fewer than 2^31 rows), no 64-bit divisions: this stands between the launch and the first load.
 constexpr int kTreeStep = 128, kTreeStepLog = 7;
 
-__device__ __forceinline__ TreeSlice tree_find(const int64_t* state, int n_units, int tail_cap, int n_slots, int min_steps,
-                                               int tile, int lin, int lane) {
-  int n_global = 0, n_tail = 0;     // unit `lane`; units past the 32nd are read again in every pass
-  if (lane < n_units) {
-    const int64_t* st = state + size_t(lane) * TCA_STATE_WORDS;
-    n_global = int(st[TCA_ST_N_GLOBAL]);
-    n_tail = int(st[TCA_ST_N_TAIL]);
-  }
-  const int first = (n_global + n_tail + kTreeStep - 1) >> kTreeStepLog;
-  auto steps_of = [&](int u) -> int {
+struct TreeFinder {
+  int lead;
+  int q, longer;      // shares are q steps, the first `longer` of them q + 1
+  int begin, end;     // this CTA's share
+  int u0, offset;     // group of 32 units the walk is at, steps before it
+  unsigned done;      // units of the group that were handed out
+
+  __device__ __forceinline__ static int steps_of(const int64_t* state, int n_units, int u) {
     if (u >= n_units) return 0;
     const int64_t* st = state + size_t(u) * TCA_STATE_WORDS;
     return int((st[TCA_ST_N_GLOBAL] + st[TCA_ST_N_TAIL] + kTreeStep - 1) >> kTreeStepLog);
-  };
-  int most = first, sum = first;
-  for (int u = 32 + lane; u < n_units; u += 32) {
-    const int n = steps_of(u);
-    most = max(most, n);
-    sum += n;
   }
-  most = __reduce_max_sync(0xffffffffu, most);
-  sum = __reduce_add_sync(0xffffffffu, sum);
-  auto parts = [](int steps, int per) { return int((unsigned(steps) + unsigned(per) - 1u) / unsigned(per)); };
-  // slices of `per` steps number at most sum / per + n_units, which bounds the search from above
-  int lo = max(min_steps, parts(sum, n_slots));
-  int hi = max(lo, n_slots > n_units ? min(most, parts(sum, n_slots - n_units)) : most);
-  while (lo < hi) {
-    const int mid = lo + (hi - lo) / 2;
-    int c = parts(first, mid);
-    for (int u = 32 + lane; u < n_units; u += 32) c += parts(steps_of(u), mid);
-    if (int(__reduce_add_sync(0xffffffffu, c)) <= n_slots) hi = mid; else lo = mid + 1;
+  __device__ __forceinline__ int share_of(int x) const {   // the share that holds step x
+    const int head = longer * (q + 1);
+    return x < head ? x / (q + 1) : longer + (x - head) / q;
   }
-  TreeSlice s;
-  s.u = -1;
-  int offset = 0, steps = 0;
-  for (int u0 = 0; u0 < n_units; u0 += 32) {
-    const int mine = u0 == 0 ? first : steps_of(u0 + lane);
-    const int np = parts(mine, lo);
-    int incl = np;
+  __device__ __forceinline__ void start(const int64_t* state, int n_units, const TreePlan& plan, int share, int lane) {
+    lead = plan.lead;
+    int total = 0;
+    for (int u = lane; u < n_units; u += 32) {
+      const int n = steps_of(state, n_units, u);
+      total += n > 0 ? n + lead : 0;
+    }
+    total = __reduce_add_sync(0xffffffffu, total);
+    const int n = max(1, min(plan.n_shares, int(unsigned(total) / unsigned(plan.min_share))));
+    q = int(unsigned(total) / unsigned(n));
+    longer = total - q * n;
+    begin = share < n ? share * q + min(share, longer) : total;
+    end = share < n ? begin + q + (share < longer ? 1 : 0) : total;
+    u0 = offset = 0;
+    done = 0;
+  }
+  // The next piece of this share; false after the last.  The first piece of a unit also records where the
+  // unit's partial results lie.
+  __device__ __forceinline__ bool next(const int64_t* state, int n_units, int tail_cap, int share, int tile, bool record,
+                                       int2* table, int lane, TreePiece& p) {
+    for (; u0 < n_units && offset < end; u0 += 32, done = 0) {
+      const int steps = steps_of(state, n_units, u0 + lane);
+      const int width = steps > 0 ? steps + lead : 0;
+      int incl = width;
 #pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-      const int t = __shfl_up_sync(0xffffffffu, incl, off);
-      if (lane >= off) incl += t;
-    }
-    const unsigned hit = __ballot_sync(0xffffffffu, lin < offset + incl);
-    if (hit) {
+      for (int off = 1; off < 32; off <<= 1) {
+        const int t = __shfl_up_sync(0xffffffffu, incl, off);
+        if (lane >= off) incl += t;
+      }
+      const int at = offset + incl - steps;              // where the unit's rows begin
+      const int lo = max(at, begin), hi = min(at + steps, end);
+      const unsigned hit = __ballot_sync(0xffffffffu, hi > lo) & ~done;
+      if (hit == 0) {
+        offset += __shfl_sync(0xffffffffu, incl, 31);
+        continue;
+      }
       const int l = __ffs(hit) - 1;
-      s.u = u0 + l;
-      s.np = __shfl_sync(0xffffffffu, np, l);
-      s.base = offset + __shfl_sync(0xffffffffu, incl - np, l);
-      steps = __shfl_sync(0xffffffffu, mine, l);
-      s.part = lin - s.base;
-      break;
+      done |= 1u << l;
+      p.u = u0 + l;
+      p.slot = share + p.u;
+      const int at_l = __shfl_sync(0xffffffffu, at, l), steps_l = __shfl_sync(0xffffffffu, steps, l);
+      const int s0 = __shfl_sync(0xffffffffu, lo, l) - at_l, s1 = __shfl_sync(0xffffffffu, hi, l) - at_l;
+      if (s0 == 0 && record && lane == 0)
+        table[p.u] = make_int2(p.slot, share_of(at_l + steps_l - 1) - share + 1);
+      const int64_t* st = state + size_t(p.u) * TCA_STATE_WORDS;
+      const int seg = int(st[TCA_ST_SEG_START]), gcap = int(st[TCA_ST_GLOBAL_CAP]), ng = int(st[TCA_ST_N_GLOBAL]);
+      const int head = int(st[TCA_ST_TAIL_HEAD]), len = ng + int(st[TCA_ST_N_TAIL]);
+      const int r0 = s0 * kTreeStep, r1 = min(len, s1 * kTreeStep);
+      // runs: rows [r0, r1) of the global region, then of the ring up to its end, then from its start
+      const int wrap = ng + tail_cap - head;             // logical row that lies in the ring's slot 0
+      const int b1 = min(max(ng, r0), r1), b2 = max(min(max(wrap, r0), r1), b1);
+      p.tiles.tile = tile;
+      p.tiles.y[0] = seg + r0;
+      p.tiles.n[0] = b1 - r0;
+      p.tiles.y[1] = seg + gcap + head + (b1 - ng);
+      p.tiles.n[1] = b2 - b1;
+      p.tiles.y[2] = seg + gcap + (b2 - wrap);
+      p.tiles.n[2] = r1 - b2;
+      return true;
     }
-    offset += __shfl_sync(0xffffffffu, incl, 31);
+    return false;
   }
-  if (s.u < 0) return s;
-  const int64_t* st = state + size_t(s.u) * TCA_STATE_WORDS;
-  const int seg = int(st[TCA_ST_SEG_START]), gcap = int(st[TCA_ST_GLOBAL_CAP]), ng = int(st[TCA_ST_N_GLOBAL]);
-  const int head = int(st[TCA_ST_TAIL_HEAD]), len = ng + int(st[TCA_ST_N_TAIL]);
-  // the unit's steps dealt evenly: the first `longer` slices have one more
-  const int each = int(unsigned(steps) / unsigned(s.np)), longer = steps - each * s.np;
-  const int r0 = (s.part * each + min(s.part, longer)) * kTreeStep;
-  const int r1 = min(len, r0 + (each + (s.part < longer ? 1 : 0)) * kTreeStep);
-  // runs: rows [r0, r1) of the global region, then of the ring up to its end, then from its start
-  const int wrap = ng + tail_cap - head;      // logical row that lies in the ring's slot 0
-  const int b1 = min(max(ng, r0), r1), b2 = min(max(wrap, r0), r1);
-  s.tiles.tile = tile;
-  s.tiles.y[0] = seg + r0;
-  s.tiles.n[0] = b1 - r0;
-  s.tiles.y[1] = seg + gcap + head + (b1 - ng);
-  s.tiles.n[1] = max(b2, b1) - b1;
-  s.tiles.y[2] = seg + gcap + (max(b2, b1) - wrap);
-  s.tiles.n[2] = r1 - max(b2, b1);
-  return s;
-}
+};
 
 }  // namespace tca

@@ -1,5 +1,5 @@
 // The cache part of tca_attn_tree for bf16, on the tensor cores: a block of up to 256 query rows (G heads
-// x drafted tokens) against one slice of a unit's cache rows.  Bound by memory while the rows are few
+// x drafted tokens) against the pieces of a share of the cache rows.  Bound by memory while the rows are few
 // (every cache row is read once per 256 query rows), by the tensor pipe and the exponentials from about
 // 128 rows on.
 #include "flash_tc.cuh"
@@ -11,11 +11,10 @@ namespace {
 struct TreeItem {
   SliceTiles slice;
   int q_row;        // first query row of this CTA in the flattened query matrix
-  int rows;         // query rows of this CTA
   size_t at;        // partial results: its first row in the first stream's block
 };
 
-// One item per CTA: its block of query rows against its slice.
+// The items of a CTA: its block of query rows against the pieces of its share, one after the other.
 template <int D, bool kShared>
 struct TreeTcSrc {
   using Item = TreeItem;
@@ -26,29 +25,26 @@ struct TreeTcSrc {
   const TreePlan* plan;
   uint64_t stream;      // the cache streams through the L2: its lines go first
   const TreeWs* ws;
+  int share, rb, rows;  // rows: query rows of this CTA
   SliceTiles slice;
-  int q_row, rows, n;
+  int q_row, n;
   size_t at0;
+  TreeFinder finder;    // the producer warp's
 
-  __device__ __forceinline__ void begin(int) {}
-  __device__ __forceinline__ bool find(int k, int lane, Item& it) const {
-    if (k > 0) return false;
-    const TreeSlice s = tree_find(state, n_units, tail_cap, plan->n_slots, plan->min_steps, kTcKeys,
-                                  int(blockIdx.x) / plan->row_blocks, lane);
-    if (s.u < 0) return false;
-    const int rb = int(blockIdx.x) % plan->row_blocks, row0 = rb * plan->rows_per_cta;
-    if (s.part == 0 && rb == 0 && lane == 0) ws->table[s.u] = make_int2(s.base, s.np);
-    it.slice = s.tiles;
-    it.q_row = s.u * plan->rows + row0;
-    it.rows = min(plan->rows_per_cta, plan->rows - row0);
-    it.at = size_t(s.base + s.part) * plan->streams * plan->rows + row0;
+  __device__ __forceinline__ void begin(int lane) { finder.start(state, n_units, *plan, share, lane); }
+  __device__ __forceinline__ bool find(int, int lane, Item& it) {
+    TreePiece p;
+    if (!finder.next(state, n_units, tail_cap, share, kTcKeys, rb == 0, ws->table, lane, p)) return false;
+    const int row0 = rb * plan->rows_per_cta;
+    it.slice = p.tiles;
+    it.q_row = p.u * plan->rows + row0;
+    it.at = size_t(p.slot) * plan->streams * plan->rows + row0;
     return true;
   }
   __device__ __forceinline__ void set(const Item& it) {
-    slice = it.slice; q_row = it.q_row; rows = it.rows; at0 = it.at;
+    slice = it.slice; q_row = it.q_row; at0 = it.at;
     n = slice.n_tiles();
   }
-
   __device__ __forceinline__ int tiles(int h) const { return kShared && h * kTcRows >= rows ? 0 : n; }
   __device__ __forceinline__ int q_bytes(int) const { return TcLayout<D>::kTile; }
   __device__ __forceinline__ void load_q(int h, uint8_t* dst, uint64_t* bar) const {
@@ -119,6 +115,9 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
   src.stream = ptx::l2_policy_evict_first();
   src.plan = &plan;
   src.ws = &ws;
+  src.share = int(blockIdx.x) / plan.row_blocks;
+  src.rb = int(blockIdx.x) % plan.row_blocks;
+  src.rows = min(plan.rows_per_cta, plan.rows - src.rb * plan.rows_per_cta);
   flash_tc<D, kShared>(src, smem, &sh, scale_log2e, ws.status);
 }
 
@@ -132,7 +131,7 @@ int launch(const tca_params* prm, const void* q, const tca_cache_desc* c, const 
     return TCA_ERR_CUDA;
   auto kern = tree_tc_kernel<D, kShared>;
   if (allow_smem<tree_tc_kernel<D, kShared>>(TcLayout<D>::bytes) != TCA_OK) return TCA_ERR_CUDA;
-  return launch_pdl(kern, dim3(unsigned(plan.n_slots * plan.row_blocks)), dim3(kTcThreads), size_t(TcLayout<D>::bytes), s, mq,
+  return launch_pdl(kern, dim3(unsigned(plan.n_shares * plan.row_blocks)), dim3(kTcThreads), size_t(TcLayout<D>::bytes), s, mq,
                     mk, mv, static_cast<const int64_t*>(c->state), U, c->tail_cap, plan,
                     prm->sm_scale * 1.4426950408889634f, ws);
 }
