@@ -1,55 +1,86 @@
-// Attention of 64 query rows over a stream of 64-key tiles on the FP32 pipes, online softmax in one
+// Attention of 32 query rows over a stream of 64-key tiles on the FP32 pipes, online softmax in one
 // pass: the kernel for fp32 inputs (their tolerance rules out bf16 and tf32 products) and the slow
 // cross-check of the tensor-core kernels.  Scores, statistics and accumulators are fp32.
 //
-// 256 threads; thread (ty, tx) of the 16 x 16 grid holds scores of rows 4 ty .. 4 ty + 3 against keys
-// tx, tx + 16, tx + 32, tx + 48 and output columns 4 tx + 64 c of the same rows, so both products run
-// from shared memory with 16-byte loads: 64 FMAs per 8 loads for the scores, 32 D/16 per 4 + 4 D/64
-// for the output.  Rows are padded by 16 bytes against bank conflicts.
+// 256 threads in two groups of 128.  The groups take alternate key tiles, each with a softmax state of
+// its own, and are merged at the end: a row's keys are then two chains half as long, which is what
+// the longest row of a causal prompt, and a short cache, wait for.  Within a group thread (ty, tx) of the
+// 8 x 16 grid holds scores of rows 4 ty .. 4 ty + 3 against keys tx, tx + 16, tx + 32, tx + 48 and output columns
+// 4 tx + 64 c of the same rows, so both products run from shared memory with 16-byte loads (64 FMAs per 8
+// loads; rows are padded by 16 bytes against bank conflicts).  K and V have one buffer each: the next
+// K tile is fetched under this tile's softmax and second product, the next V tile under the next first
+// product.  Bound by the FMA pipe and its operand loads.
 #pragma once
-#include "common.cuh"
-#include "rowslice.cuh"
-
 #include <type_traits>
+
+#include "common.cuh"
+#include "ptx_sm100.cuh"
+#include "rowslice.cuh"
 
 namespace tca {
 
-constexpr int kSimtRows = 64, kSimtKeys = 64, kSimtThreads = 256;
+constexpr int kSimtRows = 32, kSimtKeys = 64, kSimtThreads = 256, kSimtGroup = 128;
 
 template <int D>
 struct SimtSmem {
   static constexpr int kStride = D + 4;            // floats per row of Q, K, V
   static constexpr int kPStride = kSimtKeys + 4;
-  static constexpr int kFloats = 3 * 64 * kStride + kSimtRows * kPStride;
+  static constexpr int kGroupFloats = 2 * kSimtKeys * kStride + kSimtRows * kPStride;   // K, V, P of a group
+  static constexpr int kFloats = kSimtRows * kStride + 2 * kGroupFloats;
   static constexpr int kBytes = kFloats * 4;
+  static constexpr int kCtasPerSm = D == 64 ? 2 : 1;
 };
 
-// 64 rows of D elements into shared memory; rows >= n become zeros and are not read.
-template <typename T, int D, typename RowPtr>
-__device__ __forceinline__ void simt_load_rows(float* dst, int n, RowPtr row_ptr) {
+__device__ __forceinline__ void simt_group_sync(int group) {
+  asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(kSimtGroup) : "memory");
+}
+// 16 bytes to shared memory, or zeros.
+__device__ __forceinline__ void cp_async_16_or_zero(float* dst, const float* src, bool take) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
+               ::"r"(ptx::smem_u32(dst)), "l"(src), "r"(take ? 16 : 0)
+               : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kPending>
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kPending) : "memory"); }
+
+// kRows rows of D elements into shared memory by kThreads threads; rows >= n become zeros and are not read.
+// fp32 rows go asynchronously (one commit group), bf16 rows are widened on the way.
+template <typename T, int D, int kRows, int kThreads, typename RowPtr>
+__device__ __forceinline__ void simt_load_rows(float* dst, int n, int tid, RowPtr row_ptr) {
+  const T* any = row_ptr(0);
 #pragma unroll 4
-  for (int i = threadIdx.x; i < 64 * (D / 4); i += kSimtThreads) {
+  for (int i = tid; i < kRows * (D / 4); i += kThreads) {
     const int r = i / (D / 4), c = (i % (D / 4)) * 4;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (r < n) load4(row_ptr(r) + c, v);
-    *reinterpret_cast<float4*>(dst + r * SimtSmem<D>::kStride + c) = v;
+    float* to = dst + r * SimtSmem<D>::kStride + c;
+    if constexpr (std::is_same<T, float>::value) {
+      cp_async_16_or_zero(to, r < n ? row_ptr(r) + c : any, r < n);
+    } else {
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (r < n) load4(row_ptr(r) + c, v);
+      *reinterpret_cast<float4*>(to) = v;
+    }
   }
+  if constexpr (std::is_same<T, float>::value) cp_async_commit();
 }
 
 // Src: n_tiles(); n_rows(); q(r) -> const T*; keys(t) -> number of keys of tile t (1..64); k(t, r), v(t, r)
 // -> const T*; last(t, r) -> index in tile t of the last key row r sees (< 0: none, never >= keys(t));
 // masked(t): whether some row does not see all 64 keys of the tile.
-// On return m, l and o hold the row maxima (in log2 units), sums and unnormalised outputs of this
-// thread's rows; m = -inf, l = 0, o = 0 for a row that saw nothing.
+// On return the threads of group 0 (threadIdx.x < 128; true is returned) hold the row maxima (in log2
+// units), sums and unnormalised outputs of rows 4 ty .. 4 ty + 3, columns 4 tx + 64 c; m = -inf, l = 0,
+// o = 0 for a row that saw nothing.
 template <typename T, int D, typename Src>
-__device__ __forceinline__ void simt_flash(const Src& src, float scale_log2e, float* smem, float (&o)[4][D / 16],
+__device__ __forceinline__ bool simt_flash(const Src& src, float scale_log2e, float* smem, float (&o)[4][D / 16],
                                            float (&m)[4], float (&l)[4]) {
-  constexpr int ST = SimtSmem<D>::kStride, PST = SimtSmem<D>::kPStride;
+  using S = SimtSmem<D>;
+  constexpr int ST = S::kStride, PST = S::kPStride;
+  const int group = threadIdx.x / kSimtGroup, tid = threadIdx.x % kSimtGroup;
   float* sQ = smem;
-  float* sK = sQ + 64 * ST;
-  float* sV = sK + 64 * ST;
-  float* sP = sV + 64 * ST;
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  float* sK = smem + kSimtRows * ST + group * S::kGroupFloats;
+  float* sV = sK + kSimtKeys * ST;
+  float* sP = sV + kSimtKeys * ST;
+  const int tx = tid & 15, ty = tid >> 4;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     m[i] = -INFINITY;
@@ -57,14 +88,24 @@ __device__ __forceinline__ void simt_flash(const Src& src, float scale_log2e, fl
 #pragma unroll
     for (int c = 0; c < D / 16; ++c) o[i][c] = 0.f;
   }
-  simt_load_rows<T, D>(sQ, src.n_rows(), [&](int r) { return src.q(r); });
   const int nt = src.n_tiles();
-  for (int t = 0; t < nt; ++t) {
-    __syncthreads();                       // the previous tile has been consumed
-    const int n = src.keys(t);
-    simt_load_rows<T, D>(sK, n, [&](int r) { return src.k(t, r); });
-    simt_load_rows<T, D>(sV, n, [&](int r) { return src.v(t, r); });
-    __syncthreads();
+  auto load_k = [&](int t) {
+    if (t < nt) simt_load_rows<T, D, kSimtKeys, kSimtGroup>(sK, src.keys(t), tid, [&](int r) { return src.k(t, r); });
+    else cp_async_commit();                // keeps the count of pending groups
+  };
+  auto load_v = [&](int t) {
+    if (t < nt) simt_load_rows<T, D, kSimtKeys, kSimtGroup>(sV, src.keys(t), tid, [&](int r) { return src.v(t, r); });
+    else cp_async_commit();
+  };
+  __syncthreads();                         // the buffers may still be read by the item before
+  simt_load_rows<T, D, kSimtRows, kSimtThreads>(sQ, src.n_rows(), threadIdx.x, [&](int r) { return src.q(r); });
+  load_k(group);
+  load_v(group);
+  cp_async_wait<2>();
+  __syncthreads();                         // Q is shared by the groups
+  for (int t = group; t < nt; t += 2) {
+    cp_async_wait<1>();                    // K of this tile; V may still be on its way
+    simt_group_sync(group);
     float s[4][4];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -83,6 +124,8 @@ __device__ __forceinline__ void simt_flash(const Src& src, float scale_log2e, fl
         for (int j = 0; j < 4; ++j)
           s[i][j] = fmaf(q[i].w, k[j].w, fmaf(q[i].z, k[j].z, fmaf(q[i].y, k[j].y, fmaf(q[i].x, k[j].x, s[i][j]))));
     }
+    simt_group_sync(group);                // K has been read
+    load_k(t + 2);
     const bool masked = src.masked(t);
     int last[4];
 #pragma unroll
@@ -113,7 +156,8 @@ __device__ __forceinline__ void simt_flash(const Src& src, float scale_log2e, fl
 #pragma unroll
       for (int c = 0; c < D / 16; ++c) o[i][c] *= corr;
     }
-    __syncwarp();                          // a row's 16 threads are half a warp: P needs no wider barrier
+    cp_async_wait<1>();                    // V of this tile; the next K may still be on its way
+    simt_group_sync(group);                // (P needs no more than a warp: a row's 16 threads are half of one)
     auto accumulate = [&](auto guarded) {
 #pragma unroll 2
       for (int kk = 0; kk < kSimtKeys; kk += 4) {
@@ -141,7 +185,46 @@ __device__ __forceinline__ void simt_flash(const Src& src, float scale_log2e, fl
       }
     };
     if (masked) accumulate(std::true_type{}); else accumulate(std::false_type{});
+    simt_group_sync(group);                // V has been read
+    load_v(t + 2);
   }
+  cp_async_wait<0>();
+  // group 1 hands its state over through group 1's own buffers
+  float* sO = smem + kSimtRows * ST + S::kGroupFloats;
+  float* sM = sO + kSimtRows * ST;
+  if (group == 1) {
+    simt_group_sync(group);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+#pragma unroll
+      for (int c = 0; c < D / 64; ++c)
+        *reinterpret_cast<float4*>(sO + (ty * 4 + i) * ST + tx * 4 + 64 * c) =
+            make_float4(o[i][c * 4], o[i][c * 4 + 1], o[i][c * 4 + 2], o[i][c * 4 + 3]);
+      if (tx == 0) {
+        sM[2 * (ty * 4 + i)] = m[i];
+        sM[2 * (ty * 4 + i) + 1] = l[i];
+      }
+    }
+  }
+  __syncthreads();
+  if (group == 1) return false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float m1 = sM[2 * (ty * 4 + i)], l1 = sM[2 * (ty * 4 + i) + 1];
+    const float mn = fmaxf(m[i], m1), base = (mn == -INFINITY) ? 0.f : mn;
+    const float w0 = exp2f(m[i] - base), w1 = exp2f(m1 - base);
+    l[i] = l[i] * w0 + l1 * w1;
+    m[i] = mn;
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c) {
+      const float4 v = *reinterpret_cast<const float4*>(sO + (ty * 4 + i) * ST + tx * 4 + 64 * c);
+      o[i][c * 4 + 0] = o[i][c * 4 + 0] * w0 + v.x * w1;
+      o[i][c * 4 + 1] = o[i][c * 4 + 1] * w0 + v.y * w1;
+      o[i][c * 4 + 2] = o[i][c * 4 + 2] * w0 + v.z * w1;
+      o[i][c * 4 + 3] = o[i][c * 4 + 3] * w0 + v.w * w1;
+    }
+  }
+  return true;
 }
 
 }  // namespace tca

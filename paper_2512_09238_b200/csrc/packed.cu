@@ -35,7 +35,7 @@ struct PackedSrc {
 };
 
 template <typename T, int D>
-__global__ void __launch_bounds__(kSimtThreads, 2)
+__global__ void __launch_bounds__(kSimtThreads, SimtSmem<D>::kCtasPerSm)
 packed_simt_kernel(const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const __grid_constant__ PackedArgs args,
                    float scale_log2e, T* __restrict__ O) {
   extern __shared__ float4 packed_smem[];
@@ -62,15 +62,16 @@ packed_simt_kernel(const T* __restrict__ Q, const T* __restrict__ K, const T* __
   src.w = found;
   if (src.w.len == 0) return;
   float o[4][D / 16], m[4], l[4];
-  simt_flash<T, D>(src, scale_log2e, reinterpret_cast<float*>(packed_smem), o, m, l);
+  if (!simt_flash<T, D>(src, scale_log2e, reinterpret_cast<float*>(packed_smem), o, m, l)) return;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int r = ty * 4 + i;
     if (r >= src.n_rows()) continue;
     T* out = O + (src.w.kvh * G + r % G) * args.o.head + (src.w.row0 + src.w.p0 + r / G) * args.o.row;
+    const float inv = 1.f / l[i];
 #pragma unroll
-    for (int c = 0; c < D / 16; ++c) store_elt(out + tx * 4 + 64 * (c / 4) + c % 4, o[i][c] / l[i]);
+    for (int c = 0; c < D / 16; ++c) store_elt(out + tx * 4 + 64 * (c / 4) + c % 4, o[i][c] * inv);
   }
 }
 

@@ -30,7 +30,7 @@ TreePlan tree_plan(const tca_params* prm, int n_draft) {
   p.row_blocks = (p.rows + p.rows_per_cta - 1) / p.rows_per_cta;
   p.min_share = tc ? 2 : 1;
   p.lead = tc ? 3 : 0;
-  const int resident = (tc ? 1 : 2) * sm_count();
+  const int resident = (tc || prm->head_dim == 128 ? 1 : 2) * sm_count();
   p.n_shares = resident / p.row_blocks > 0 ? resident / p.row_blocks : 1;
   p.n_slots = p.n_shares + U;
   return p;
@@ -54,7 +54,7 @@ struct TreeSrc {
 };
 
 template <typename T, int D>
-__global__ void __launch_bounds__(kSimtThreads, 2)
+__global__ void __launch_bounds__(kSimtThreads, SimtSmem<D>::kCtasPerSm)
 tree_simt_kernel(const T* __restrict__ q, const T* __restrict__ Kc, const T* __restrict__ Vc,
                  const int64_t* __restrict__ state, int n_units, int64_t tail_cap, TreePlan plan, float scale_log2e,
                  TreeWs ws) {
@@ -64,7 +64,7 @@ tree_simt_kernel(const T* __restrict__ q, const T* __restrict__ Kc, const T* __r
   pdl_launch_dependents();
   const int share = int(blockIdx.x) / plan.row_blocks, rb = int(blockIdx.x) % plan.row_blocks;
   const int row0 = rb * kSimtRows;
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;   // of the group that writes
   TreeFinder finder;
   if (threadIdx.x < 32) finder.start(state, n_units, plan, share, threadIdx.x);
   for (;;) {
@@ -85,9 +85,9 @@ tree_simt_kernel(const T* __restrict__ q, const T* __restrict__ Kc, const T* __r
     src.Vc = Vc;
     src.tiles = mine.tiles;
     float o[4][D / 16], m[4], l[4];
-    simt_flash<T, D>(src, scale_log2e, reinterpret_cast<float*>(tree_smem), o, m, l);
+    const bool mine_to_write = simt_flash<T, D>(src, scale_log2e, reinterpret_cast<float*>(tree_smem), o, m, l);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 4 && mine_to_write; ++i) {
       const int r = row0 + ty * 4 + i;
       if (r >= plan.rows) continue;
       const size_t at = size_t(mine.slot) * plan.rows + r;
