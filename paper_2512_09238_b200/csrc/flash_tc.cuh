@@ -12,7 +12,7 @@
 //
 // 384 threads in three warpgroups: warp 0 TMA producer, warp 1 MMA issuer, warps 2 and 3 clean value tiles
 // (below); warps 4-7 and 8-11 softmax of block 0 and 1, one thread per query row = TMEM lane.  The first
-// warpgroup hands registers to the others (88 / 208 of 168 at launch), so that a thread holds its row
+// warpgroup hands registers to the others (120 / 192 of 168 at launch), so that a thread holds its row
 // of 128 scores.  TMEM: S0 | S1 | O0 | O1; the bf16 P of a tile overwrites the first half of its S and is
 // the A operand of the second product.  Products are issued PV0 S0' PV1 S1' so that one block's softmax
 // runs under the other's products; a stream step consumes one pair (V of this tile, K of the next of
@@ -45,7 +45,7 @@ namespace tca {
 
 constexpr int kTcRows = 128, kTcKeys = 128;
 constexpr int kTcThreads = 384;
-constexpr int kTcRegsLean = 88, kTcRegsSoftmax = 208;
+constexpr int kTcRegsLean = 120, kTcRegsSoftmax = 192;
 static_assert(128 * kTcRegsLean + 256 * kTcRegsSoftmax <= kTcThreads * 168, "more registers than the launch allocates");
 constexpr int kTcHalfBytes = 128 * 128;        // 128 rows x 64 bf16: one swizzled box
 constexpr float kTcRescale = 8.f;
@@ -185,7 +185,9 @@ __device__ __forceinline__ void flash_tc_setup(uint8_t* smem, TcShared<Item>* sh
 //   void load(t, is_v, dst, bar)  issue the loads of a K or V tile (kTile bytes)
 //   void begin_row(row)           softmax threads, once: their row
 //   int  row_key(h)               what last() needs of the row, worked out once per item
-//   int  last(key, t)             last key of tile t that the row sees (>= 127: all)
+//   int  whole_tiles()            the first so many tiles are seen whole by every row
+//   int  keys(h, t)               keys of tile t that some row of block h sees (1 .. 128)
+//   int  last(key, t)             last key of tile t that the row sees (not asked for those)
 //   int  clean(t)                 -1: nothing to clean; else rows of tile t that somebody sees
 //   int  scan_from(t)             rows [scan_from(t), clean(t)) are searched for non-finite elements
 //   int  note_slot(t)             which dirty[] entry a cleaned tile uses
@@ -299,9 +301,14 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
       int base = 0, group = 0;               // first ring slot and group of the item
       uint32_t tile_count[2] = {0, 0};
       auto slot_of = [&](int n) { return (base + n) % kRing; };
+      // Tiles that every row sees whole come first, and their steps are a loop of their own: the issuer's
+      // instruction stream paces the products (with a run-time key count in one loop for all tiles a pair of
+      // tiles took 4200 clocks instead of 3270).
+      auto k_desc = [&](int n) { return dk + uint64_t(uint32_t(slot_of(n) * L::kTile) >> 4); };
+      auto v_desc = [&](int n) { return dv + uint64_t(uint32_t(slot_of(n) * L::kTile) >> 4); };
+      auto q_desc = [&](int h) { return dq + (kShared ? uint64_t(uint32_t(h * L::kTile) >> 4) : 0ull); };
       auto issue_s = [&](int h, int n) {
-        const uint64_t a0 = dq + (kShared ? uint64_t(uint32_t(h * L::kTile) >> 4) : 0ull);
-        const uint64_t b0 = dk + uint64_t(uint32_t(slot_of(n) * L::kTile) >> 4);
+        const uint64_t a0 = q_desc(h), b0 = k_desc(n);
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk) {
           const uint32_t off = (uint32_t(kk >> 2) * kTcHalfBytes + uint32_t(kk & 3) * 32u) >> 4;
@@ -309,7 +316,7 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
         }
       };
       auto issue_pv = [&](int h, int n, bool acc) -> bool {
-        const uint64_t b0 = dv + uint64_t(uint32_t(slot_of(n) * L::kTile) >> 4);
+        const uint64_t b0 = v_desc(n);
         const uint32_t parity = (h == 0 ? tile_count[0]++ : tile_count[1]++) & 1u;
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
@@ -322,39 +329,78 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
         }
         return true;
       };
+      // the same for any tile: only as many columns, and k-steps, in sixteens, as somebody sees
+      auto issue_s_part = [&](int h, int n, int t) {
+        const uint64_t a0 = q_desc(h), b0 = k_desc(n);
+        const uint32_t idesc = ptx::idesc_bf16(kTcRows, 0, false) | (uint32_t((src.keys(h, t) + 15) >> 4 << 1) << 17);
+#pragma unroll 1
+        for (int kk = 0; kk < D / 16; ++kk) {
+          const uint32_t off = (uint32_t(kk >> 2) * kTcHalfBytes + uint32_t(kk & 3) * 32u) >> 4;
+          ptx::umma_ss_elect(tmem_base + h * 128u, a0 + off, b0 + off, idesc, kk > 0);
+        }
+      };
+      auto issue_pv_part = [&](int h, int n, bool acc, int t) -> bool {
+        const uint64_t b0 = v_desc(n);
+        const uint32_t parity = (h == 0 ? tile_count[0]++ : tile_count[1]++) & 1u;
+        const int steps = (src.keys(h, t) + 15) >> 4;
+        if (!warp_wait(bar_p + 2 * h, parity) || !warp_wait(bar_p + 2 * h + 1, parity)) return false;
+        ptx::tc_fence_after();
+#pragma unroll 1
+        for (int kk = 0; kk < steps; ++kk)
+          ptx::umma_ts_elect(tmem_base + 256u + uint32_t(h * D), tmem_base + h * 128u + uint32_t(kk * 8),
+                             b0 + uint32_t((kk * 2048) >> 4), idesc_pv, (acc || kk > 0) ? 1u : 0u);
+        return true;
+      };
       for (int k = 0; next_item(k); ++k) {
         const int n0 = src.tiles(0), n1 = kShared ? src.tiles(1) : 0, nt = kShared ? max(n0, n1) : n0;
         bool ok = warp_wait(bar_q, uint32_t(k) & 1u) && warp_wait(bar_full + group % kPairs, uint32_t(group / kPairs) & 1u);
         if (!ok) break;
         ptx::tc_fence_after();
+#pragma unroll 1
         for (int h = 0; h < 2; ++h)
           if (kShared ? (h == 0 ? n0 : n1) > 0 : h < nt) {
-            issue_s(h, kShared ? 0 : h);
+            issue_s_part(h, kShared ? 0 : h, kShared ? 0 : h);
             ptx::umma_commit_elect(bar_s + h);
           }
         if (nt <= kLead) ptx::umma_commit_elect(bar_q_empty);      // that was the last use of the query tile
         ptx::umma_commit_elect(bar_empty + group % kPairs);
         ++group;
-        for (int t = 0; t < nt && ok; ++t, ++group) {
+        int t = 0;
+        for (const int fast = src.whole_tiles() - kLead; t < fast && ok; ++t, ++group) {
           ok = warp_wait(bar_full + group % kPairs, uint32_t(group / kPairs) & 1u);
           if (kShared) {
             for (int h = 0; h < 2 && ok; ++h) {
-              const int nh = h == 0 ? n0 : n1;
-              if (t >= nh) continue;
+              if (h == 1 && n1 == 0) continue;
               ok = issue_pv(h, v_load(t, nt), t > 0);
               if (!ok) break;
-              if (t + 1 < nh) issue_s(h, k_load(t + 1, nt));
-              ptx::umma_commit_elect(t + 1 < nh ? bar_s + h : bar_pv + h);   // S ready implies PV done
+              issue_s(h, k_load(t + 1, nt));
+              ptx::umma_commit_elect(bar_s + h);                   // S ready implies PV done
             }
           } else {
             const int h = t & 1;
             if (ok) ok = issue_pv(h, v_load(t, nt), t > 1);
             if (!ok) break;
-            if (t + 2 < nt) issue_s(h, k_load(t + 2, nt));
-            ptx::umma_commit_elect(t + 2 < nt ? bar_s + h : bar_pv + h);
+            issue_s(h, k_load(t + 2, nt));
+            ptx::umma_commit_elect(bar_s + h);
           }
           if (!ok) break;
           if (t + 1 + kLead == nt) ptx::umma_commit_elect(bar_q_empty);      // the last scores have been issued
+          ptx::umma_commit_elect(bar_empty + group % kPairs);
+        }
+        for (; t < nt && ok; ++t, ++group) {
+          ok = warp_wait(bar_full + group % kPairs, uint32_t(group / kPairs) & 1u);
+#pragma unroll 1
+          for (int j = 0; j < (kShared ? 2 : 1) && ok; ++j) {
+            const int h = kShared ? j : t & 1, mine = !kShared ? nt : h == 0 ? n0 : n1;   // tiles of this block / all
+            if (t >= mine) continue;
+            ok = issue_pv_part(h, v_load(t, nt), t >= kLead, t);
+            if (!ok) break;
+            const bool more = t + kLead < mine;
+            if (more) issue_s_part(h, k_load(t + kLead, nt), t + kLead);
+            ptx::umma_commit_elect(more ? bar_s + h : bar_pv + h);
+          }
+          if (!ok) break;
+          if (t + 1 + kLead == nt) ptx::umma_commit_elect(bar_q_empty);
           ptx::umma_commit_elect(bar_empty + group % kPairs);
         }
         if (!ok) break;
@@ -416,7 +462,8 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
               sh->any_dirty[k & 1] = 1;
             }
           }
-          for (int i = z0 * kPieces + lane; i < 64 * kPieces; i += 32) *piece(i) = make_uint4(0, 0, 0, 0);
+          const int z1 = (((seen + 15) & ~15) + 1 - (warp - 2)) / 2;   // the product reads whole k-steps
+          for (int i = z0 * kPieces + lane; i < z1 * kPieces; i += 32) *piece(i) = make_uint4(0, 0, 0, 0);
           ptx::fence_proxy_async_smem();                     // the product reads the tile through the async proxy
           __syncwarp();
           if (lane == 0) ptx::mbar_arrive(bar_full + (group + 1 + t) % kPairs);
@@ -443,44 +490,13 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
       const int row_key = src.row_key(h);
       float m_run = -INFINITY, m_used = -INFINITY, l = 0.f;
       bool ok = true;
-      for (int it = 0; it < mine; ++it) {
-        const int hi = src.last(row_key, kShared ? it : 2 * it + h);
-        ok = warp_wait(bar_s + h, tile_count++ & 1u);
-        if (!ok) break;
-        ptx::tc_fence_after();
-        uint32_t v[kTcKeys];
-#pragma unroll
-        for (int c = 0; c < kTcKeys / 32; ++c)
-          ptx::tmem_ld32(s_addr + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&v[c * 32]));
-        ptx::tc_wait_ld();
-        // a masked score is -inf: it loses every max and its weight is exactly 0.  Groups of 32 keys that the
-        // whole warp sees are left alone.
-        if (__any_sync(0xffffffffu, hi < kTcKeys - 1)) {
-          const int least = __reduce_min_sync(0xffffffffu, hi);
-#pragma unroll
-          for (int c = 0; c < kTcKeys / 32; ++c)
-            if (least < c * 32 + 31) {
-#pragma unroll
-              for (int k = c * 32; k < c * 32 + 32; ++k)
-                if (k > hi) v[k] = 0xff800000u;
-            }
-        }
-        float mx;
-        {
-          float mx8[8];
-#pragma unroll
-          for (int a = 0; a < 8; ++a) mx8[a] = fmaxf(__uint_as_float(v[2 * a]), __uint_as_float(v[2 * a + 1]));
-#pragma unroll
-          for (int k = 16; k < kTcKeys; k += 16)
-#pragma unroll
-            for (int a = 0; a < 8; ++a)
-              mx8[a] = ptx::max3(mx8[a], __uint_as_float(v[k + 2 * a]), __uint_as_float(v[k + 2 * a + 1]));
-          mx = fmaxf(fmaxf(ptx::max3(mx8[0], mx8[1], mx8[2]), ptx::max3(mx8[3], mx8[4], mx8[5])), fmaxf(mx8[6], mx8[7]));
-        }
+      // lazy rescale of the accumulator to a maximum that grew by more than 2^8 (warp-uniform: TMEM access
+      // is warp-wide)
+      auto rescale = [&](float mx, bool started) {
         m_run = fmaxf(m_run, mx * scale_log2e);
-        if (__any_sync(0xffffffffu, m_run > m_used + kTcRescale)) {   // warp-uniform: TMEM access is warp-wide
+        if (__any_sync(0xffffffffu, m_run > m_used + kTcRescale)) {
           const float alpha = (m_used == -INFINITY) ? 0.f : ptx::fast_exp2(m_used - m_run);
-          if (it > 0) {
+          if (started) {
 #pragma unroll 1
             for (int c = 0; c < D / 32; ++c) {
               uint32_t o[32];
@@ -495,6 +511,37 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
           l *= alpha;
           m_used = m_run;
         }
+      };
+      auto announce = [&](int part) {
+        ptx::tc_wait_st();
+        ptx::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(bar_p + 2 * h + part);
+      };
+      const int whole = kShared ? min(src.whole_tiles(), mine) : (src.whole_tiles() - h + 1) / 2;   // they come first
+      int it = 0;
+      for (; it < whole; ++it) {
+        ok = warp_wait(bar_s + h, tile_count++ & 1u);
+        if (!ok) break;
+        ptx::tc_fence_after();
+        uint32_t v[kTcKeys];
+#pragma unroll
+        for (int c = 0; c < kTcKeys / 32; ++c)
+          ptx::tmem_ld32(s_addr + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&v[c * 32]));
+        ptx::tc_wait_ld();
+        float mx;
+        {
+          float mx8[8];
+#pragma unroll
+          for (int a = 0; a < 8; ++a) mx8[a] = fmaxf(__uint_as_float(v[2 * a]), __uint_as_float(v[2 * a + 1]));
+#pragma unroll
+          for (int k = 16; k < kTcKeys; k += 16)
+#pragma unroll
+            for (int a = 0; a < 8; ++a)
+              mx8[a] = ptx::max3(mx8[a], __uint_as_float(v[k + 2 * a]), __uint_as_float(v[k + 2 * a + 1]));
+          mx = fmaxf(fmaxf(ptx::max3(mx8[0], mx8[1], mx8[2]), ptx::max3(mx8[3], mx8[4], mx8[5])), fmaxf(mx8[6], mx8[7]));
+        }
+        rescale(mx, it > 0);
         const float neg_m = (m_used == -INFINITY) ? 0.f : -m_used;
         const uint64_t neg_m2 = ptx::pack2(neg_m, neg_m);
         uint64_t sum2[2] = {0ull, 0ull};
@@ -512,22 +559,58 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
             v[j] = ptx::pack_bf16x2(el, eh);   // entry j is never read again (j <= 2j)
           }
           if (g == kTcPSplit + 1) {            // the first part was stored at least one group ago
-            ptx::tc_wait_st();
-            ptx::tc_fence_before();
-            __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(bar_p + 2 * h);
+            announce(0);
           }
           if (g >= 1) ptx::tmem_st8(s_addr + (g - 1) * 8, &v[(g - 1) * 8]);
         }
         ptx::tmem_st8(s_addr + 56, &v[56]);
-        ptx::tc_wait_st();
-        ptx::tc_fence_before();
-        __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(bar_p + 2 * h + 1);
+        announce(1);
         float s0, s1, s2, s3;
         ptx::unpack2(sum2[0], s0, s1);
         ptx::unpack2(sum2[1], s2, s3);
         l += (s0 + s1) + (s2 + s3);
+      }
+#pragma unroll 1
+      for (; it < mine && ok; ++it) {
+        const int t = kShared ? it : 2 * it + h;
+        ok = warp_wait(bar_s + h, tile_count++ & 1u);
+        if (!ok) break;
+        ptx::tc_fence_after();
+        // A tile that some row does not see all of (the diagonal, the end of a run): the 32-key groups that
+        // somebody sees, in a compact loop that reads the scores twice.
+        const int hi = src.last(row_key, t), groups = (src.keys(h, t) + 31) >> 5;
+        float mx = -INFINITY;
+#pragma unroll 1
+        for (int c = 0; c < groups; ++c) {
+          uint32_t v[32];
+          ptx::tmem_ld32(s_addr + c * 32, v);
+          ptx::tc_wait_ld();
+          const int last = hi - c * 32;
+#pragma unroll
+          for (int k = 0; k < 32; ++k)
+            if (k <= last) mx = fmaxf(mx, __uint_as_float(v[k]));
+        }
+        rescale(mx, it > 0);
+        const float neg_m = (m_used == -INFINITY) ? 0.f : -m_used;
+        float sum = 0.f;
+#pragma unroll 1
+        for (int c = 0; c < groups; ++c) {
+          uint32_t v[32];
+          ptx::tmem_ld32(s_addr + c * 32, v);
+          ptx::tc_wait_ld();
+          const int last = hi - c * 32;
+#pragma unroll
+          for (int k = 0; k < 32; k += 2) {    // a key the row does not see has weight 0, whatever its score
+            const float el = k <= last ? ptx::fast_exp2(fmaf(__uint_as_float(v[k]), scale_log2e, neg_m)) : 0.f;
+            const float eh = k + 1 <= last ? ptx::fast_exp2(fmaf(__uint_as_float(v[k + 1]), scale_log2e, neg_m)) : 0.f;
+            sum += el + eh;
+            v[k / 2] = ptx::pack_bf16x2(el, eh);
+          }
+          ptx::tmem_st16(s_addr + c * 16, v);  // over scores that have been read
+        }
+        announce(0);
+        announce(1);
+        l += sum;
       }
       if (ok && mine > 0) ok = warp_wait(bar_pv + h, item_count++ & 1u);   // committed after the last PV
       if (!ok) break;

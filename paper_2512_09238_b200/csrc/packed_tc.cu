@@ -56,6 +56,8 @@ struct PackedTcSrc {
   __device__ __forceinline__ void begin_row(int row) { dp = row / G; g = row % G; }
   __device__ __forceinline__ int row_key(int h) const { return min(p0 + h * P + dp, last_pos(h)); }
   __device__ __forceinline__ int last(int key, int t) const { return key - t * kTcKeys; }
+  __device__ __forceinline__ int whole_tiles() const { return p0 / kTcKeys; }
+  __device__ __forceinline__ int keys(int h, int t) const { return min(kTcKeys, last_pos(h) + 1 - t * kTcKeys); }
   // From the tile that holds p0 on, some row does not see some key (at most two tiles: 2 P <= 128, or
   // P = 128 with p0 a multiple of 256).  Rows past the last position are nobody's: another sequence's, or
   // none; rows up to p0 are everybody's.

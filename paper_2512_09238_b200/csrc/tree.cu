@@ -42,7 +42,7 @@ template <typename T, int D>
 struct TreeSrc {
   const T *q_rows, *Kc, *Vc;      // first query row of this CTA; the cache
   int n;                          // query rows here
-  SliceTiles tiles;
+  SliceTiles<kSimtKeys> tiles;
   __device__ __forceinline__ int n_rows() const { return n; }
   __device__ __forceinline__ int n_tiles() const { return tiles.n_tiles(); }
   __device__ __forceinline__ int keys(int t) const { int y, c; tiles.get(t, y, c); return c; }
@@ -59,7 +59,7 @@ tree_simt_kernel(const T* __restrict__ q, const T* __restrict__ Kc, const T* __r
                  const int64_t* __restrict__ state, int n_units, int64_t tail_cap, TreePlan plan, float scale_log2e,
                  TreeWs ws) {
   extern __shared__ float4 tree_smem[];
-  __shared__ TreePiece piece;
+  __shared__ TreePiece<kSimtKeys> piece;
   pdl_wait();
   pdl_launch_dependents();
   const int share = int(blockIdx.x) / plan.row_blocks, rb = int(blockIdx.x) % plan.row_blocks;
@@ -69,13 +69,13 @@ tree_simt_kernel(const T* __restrict__ q, const T* __restrict__ Kc, const T* __r
   if (threadIdx.x < 32) finder.start(state, n_units, plan, share, threadIdx.x);
   for (;;) {
     if (threadIdx.x < 32) {
-      TreePiece p;
-      const bool more = finder.next(state, n_units, int(tail_cap), share, kSimtKeys, rb == 0, ws.table, threadIdx.x, p);
+      TreePiece<kSimtKeys> p;
+      const bool more = finder.next(state, n_units, int(tail_cap), share, rb == 0, ws.table, threadIdx.x, p);
       if (!more) p.u = -1;
       if (threadIdx.x == 0) piece = p;
     }
     __syncthreads();
-    const TreePiece mine = piece;
+    const TreePiece<kSimtKeys> mine = piece;
     __syncthreads();                       // read by all before the next one is written
     if (mine.u < 0) return;
     TreeSrc<T, D> src;

@@ -44,35 +44,41 @@ inline TreeWs tree_ws_layout(const tca_params* prm, const TreePlan& p, void* ws)
   return w;
 }
 
-// The rows of one piece of a unit: up to three runs of physically contiguous cache rows (global region, ring up
-// to its end, ring from its start), walked in tiles of `tile` rows; the last tile of a run may be short.
+// The rows of one piece of a unit: up to three runs of physically contiguous cache rows (global region,
+// ring up to its end, ring from its start), in tiles of kTile rows: first the full tiles of all runs, then
+// what is left of each run that is not a multiple of it.  (The order does not matter to the attention.)
+template <int kTile>
 struct SliceTiles {
   int y[3], n[3];
-  int tile;
-  __device__ __forceinline__ int count(int i) const { return (n[i] + tile - 1) / tile; }
-  __device__ __forceinline__ int n_tiles() const { return count(0) + count(1) + count(2); }
+  __device__ __forceinline__ int full(int i) const { return int(unsigned(n[i]) / unsigned(kTile)); }
+  __device__ __forceinline__ int n_whole() const { return full(0) + full(1) + full(2); }
+  __device__ __forceinline__ int n_tiles() const {
+    return n_whole() + (n[0] % kTile != 0) + (n[1] % kTile != 0) + (n[2] % kTile != 0);
+  }
   // first cache row of tile t and the rows it holds
   __device__ __forceinline__ void get(int t, int& row, int& rows) const {
-    int i = 0;
-    if (t >= count(0)) {
-      t -= count(0);
-      i = 1;
-      if (t >= count(1)) {
-        t -= count(1);
-        i = 2;
-      }
-    }
-    const int yi = i == 0 ? y[0] : i == 1 ? y[1] : y[2], ni = i == 0 ? n[0] : i == 1 ? n[1] : n[2];
-    row = yi + t * tile;
-    rows = min(tile, ni - t * tile);
+    const int f0 = full(0), f1 = full(1), f2 = full(2);
+    rows = kTile;
+    if (t < f0) { row = y[0] + t * kTile; return; }
+    t -= f0;
+    if (t < f1) { row = y[1] + t * kTile; return; }
+    t -= f1;
+    if (t < f2) { row = y[2] + t * kTile; return; }
+    t -= f2;
+    const int r0 = n[0] - f0 * kTile, r1 = n[1] - f1 * kTile, r2 = n[2] - f2 * kTile;
+    if (r0 > 0 && t-- == 0) { row = y[0] + f0 * kTile; rows = r0; return; }
+    if (r1 > 0 && t-- == 0) { row = y[1] + f1 * kTile; rows = r1; return; }
+    row = y[2] + f2 * kTile;
+    rows = r2;
   }
 };
 
 // What one CTA attends to at a time: a piece of a unit's rows.
+template <int kTile>
 struct TreePiece {
   int u;
   int slot;          // where its partial results go
-  SliceTiles tiles;
+  SliceTiles<kTile> tiles;
 };
 
 // How the cache rows of all units are dealt: laid end to end in steps of kTreeStep rows, they are cut into
@@ -120,8 +126,9 @@ struct TreeFinder {
   }
   // The next piece of this share; false after the last.  The first piece of a unit also records where the
   // unit's partial results lie.
-  __device__ __forceinline__ bool next(const int64_t* state, int n_units, int tail_cap, int share, int tile, bool record,
-                                       int2* table, int lane, TreePiece& p) {
+  template <int kTile>
+  __device__ __forceinline__ bool next(const int64_t* state, int n_units, int tail_cap, int share, bool record, int2* table,
+                                       int lane, TreePiece<kTile>& p) {
     for (; u0 < n_units && offset < end; u0 += 32, done = 0) {
       const int steps = steps_of(state, n_units, u0 + lane);
       const int width = steps > 0 ? steps + lead : 0;
@@ -153,7 +160,6 @@ struct TreeFinder {
       // runs: rows [r0, r1) of the global region, then of the ring up to its end, then from its start
       const int wrap = ng + tail_cap - head;             // logical row that lies in the ring's slot 0
       const int b1 = min(max(ng, r0), r1), b2 = max(min(max(wrap, r0), r1), b1);
-      p.tiles.tile = tile;
       p.tiles.y[0] = seg + r0;
       p.tiles.n[0] = b1 - r0;
       p.tiles.y[1] = seg + gcap + head + (b1 - ng);

@@ -9,7 +9,7 @@ namespace tca {
 namespace {
 
 struct TreeItem {
-  SliceTiles slice;
+  SliceTiles<kTcKeys> slice;
   int q_row;        // first query row of this CTA in the flattened query matrix
   size_t at;        // partial results: its first row in the first stream's block
 };
@@ -26,15 +26,15 @@ struct TreeTcSrc {
   uint64_t stream;      // the cache streams through the L2: its lines go first
   const TreeWs* ws;
   int share, rb, rows;  // rows: query rows of this CTA
-  SliceTiles slice;
+  SliceTiles<kTcKeys> slice;
   int q_row, n;
   size_t at0;
   TreeFinder finder;    // the producer warp's
 
   __device__ __forceinline__ void begin(int lane) { finder.start(state, n_units, *plan, share, lane); }
   __device__ __forceinline__ bool find(int, int lane, Item& it) {
-    TreePiece p;
-    if (!finder.next(state, n_units, tail_cap, share, kTcKeys, rb == 0, ws->table, lane, p)) return false;
+    TreePiece<kTcKeys> p;
+    if (!finder.next(state, n_units, tail_cap, share, rb == 0, ws->table, lane, p)) return false;
     const int row0 = rb * plan->rows_per_cta;
     it.slice = p.tiles;
     it.q_row = p.u * plan->rows + row0;
@@ -65,6 +65,12 @@ struct TreeTcSrc {
     slice.get(t, y, c);
     return c - 1;
   }
+  __device__ __forceinline__ int keys(int, int t) const {
+    int y, c;
+    slice.get(t, y, c);
+    return c;
+  }
+  __device__ __forceinline__ int whole_tiles() const { return slice.n_whole(); }
   // rows behind a run's end are another unit's or not in use
   __device__ __forceinline__ int clean(int t) const {
     int y, c;
