@@ -51,9 +51,9 @@ constexpr int kTcHalfBytes = 128 * 128;        // 128 rows x 64 bf16: one swizzl
 constexpr float kTcRescale = 8.f;
 constexpr int kTcPSplit = 6;                   // k-steps of 16 keys in the first part of P
 
-// Writing rows held one per lane: four lanes exchange their rows' 32-byte pieces, so that a store covers
-// 128 contiguous bytes of each of 8 rows instead of 32 bytes of each of 32 (a store takes the memory pipe a
-// cycle per row it touches: 4300 -> 1500 clocks per item for a block of 128 rows of 256 bytes).
+// Writing rows held one per lane: four lanes exchange pieces of their rows, so that a store covers 64 or
+// 128 contiguous bytes of each of 8 rows instead of 16 or 32 bytes of each of 32 (a store takes the memory
+// pipe a cycle per row it touches).
 struct TcRowOut {
   uint64_t row[4];       // the quad's rows; 0: not written
   __device__ __forceinline__ explicit TcRowOut(const void* mine) {
@@ -62,45 +62,53 @@ struct TcRowOut {
     for (int r = 0; r < 4; ++r)
       row[r] = __shfl_sync(0xffffffffu, static_cast<unsigned long long>(reinterpret_cast<uintptr_t>(mine)), (lane & ~3) + r);
   }
-  // 128 bytes at byte offset `at` of every row; w: this lane's row's.  Whole warp.  wide: 32-byte alignment.
-  __device__ __forceinline__ void store(uint32_t (&w)[32], int at, bool wide) const {
+  // 4 x 4 transpose over the quad of kWords-word pieces: first with the lane two away, then with the
+  // neighbour.  All of a step's exchanges are issued before the first result is used (one after the other
+  // they cost their latency each, 40 clocks).  Afterwards piece r is row r's, number lane & 3 of it.
+  template <int kWords>
+  __device__ __forceinline__ void exchange(uint32_t* w) const {
     const int lane = threadIdx.x & 31;
     const bool up2 = lane & 2, up1 = lane & 1;
-    // 4 x 4 transpose of 8-word pieces over the quad: first with the lane two away, then with the neighbour.
-    // All of a step's exchanges are issued before the first result is used (one after the other they cost
-    // their latency each, 40 clocks).
-    uint32_t got[16];
+    uint32_t got[2 * kWords];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) got[e] = up2 ? w[e] : w[16 + e];
+    for (int e = 0; e < 2 * kWords; ++e) got[e] = up2 ? w[e] : w[2 * kWords + e];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) got[e] = __shfl_xor_sync(0xffffffffu, got[e], 2);
+    for (int e = 0; e < 2 * kWords; ++e) got[e] = __shfl_xor_sync(0xffffffffu, got[e], 2);
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
+    for (int e = 0; e < 2 * kWords; ++e) {
       w[e] = up2 ? got[e] : w[e];
-      w[16 + e] = up2 ? w[16 + e] : got[e];
+      w[2 * kWords + e] = up2 ? w[2 * kWords + e] : got[e];
     }
 #pragma unroll
-    for (int e = 0; e < 16; ++e) got[e] = up1 ? w[(e >> 3) * 16 + (e & 7)] : w[(e >> 3) * 16 + 8 + (e & 7)];
+    for (int e = 0; e < 2 * kWords; ++e) got[e] = up1 ? w[(e / kWords) * 2 * kWords + e % kWords] : w[(e / kWords) * 2 * kWords + kWords + e % kWords];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) got[e] = __shfl_xor_sync(0xffffffffu, got[e], 1);
+    for (int e = 0; e < 2 * kWords; ++e) got[e] = __shfl_xor_sync(0xffffffffu, got[e], 1);
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      uint32_t &lo = w[(e >> 3) * 16 + (e & 7)], &hi = w[(e >> 3) * 16 + 8 + (e & 7)];
+    for (int e = 0; e < 2 * kWords; ++e) {
+      uint32_t &lo = w[(e / kWords) * 2 * kWords + e % kWords], &hi = w[(e / kWords) * 2 * kWords + kWords + e % kWords];
       lo = up1 ? got[e] : lo;
       hi = up1 ? hi : got[e];
     }
-    at += (lane & 3) * 32;
+  }
+  // 128 bytes at byte offset `at` of every row (32-byte aligned); w: this lane's row's.  Whole warp.
+  __device__ __forceinline__ void store32(uint32_t (&w)[32], int at) const {
+    exchange<8>(w);
+    at += (threadIdx.x & 3) * 32;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       if (row[r] == 0) continue;
-      char* p = reinterpret_cast<char*>(row[r]) + at;
-      if (wide) {
-        const uint32_t o[8] = {w[r * 8], w[r * 8 + 1], w[r * 8 + 2], w[r * 8 + 3], w[r * 8 + 4], w[r * 8 + 5], w[r * 8 + 6], w[r * 8 + 7]};
-        ptx::st_global_32(p, o);
-      } else {
-        *reinterpret_cast<uint4*>(p) = make_uint4(w[r * 8], w[r * 8 + 1], w[r * 8 + 2], w[r * 8 + 3]);
-        *reinterpret_cast<uint4*>(p + 16) = make_uint4(w[r * 8 + 4], w[r * 8 + 5], w[r * 8 + 6], w[r * 8 + 7]);
-      }
+      const uint32_t o[8] = {w[r * 8], w[r * 8 + 1], w[r * 8 + 2], w[r * 8 + 3], w[r * 8 + 4], w[r * 8 + 5], w[r * 8 + 6], w[r * 8 + 7]};
+      ptx::st_global_32(reinterpret_cast<char*>(row[r]) + at, o);
+    }
+  }
+  // 64 bytes at byte offset `at` of every row (16-byte aligned), from the first 16 words of w.
+  __device__ __forceinline__ void store16(uint32_t (&w)[32], int at) const {
+    exchange<4>(w);
+    at += (threadIdx.x & 3) * 16;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      if (row[r] == 0) continue;
+      *reinterpret_cast<uint4*>(reinterpret_cast<char*>(row[r]) + at) = make_uint4(w[r * 4], w[r * 4 + 1], w[r * 4 + 2], w[r * 4 + 3]);
     }
   }
 };

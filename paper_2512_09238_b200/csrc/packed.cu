@@ -40,6 +40,7 @@ packed_simt_kernel(const T* __restrict__ Q, const T* __restrict__ K, const T* __
                    float scale_log2e, T* __restrict__ O) {
   extern __shared__ float4 packed_smem[];
   __shared__ PackedWork found;
+  __shared__ int held[PackedFinder::kHeld];
   pdl_wait();
   pdl_launch_dependents();
   const int G = args.n_q_heads / args.n_kv_heads;
@@ -48,7 +49,7 @@ packed_simt_kernel(const T* __restrict__ Q, const T* __restrict__ K, const T* __
   src.Q = Q; src.K = K; src.V = V; src.a = &args; src.G = G;
   if (threadIdx.x < 32) {
     PackedFinder finder;
-    finder.read(args, tile_pos, threadIdx.x);
+    finder.read(args, tile_pos, threadIdx.x, held);
     PackedWork w;
     int tile = 0;
     w.len = 0;

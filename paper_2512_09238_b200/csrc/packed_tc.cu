@@ -20,13 +20,14 @@ struct PackedTcSrc {
   const __nv_bfloat16* V;
   __nv_bfloat16* O;
   const PackedArgs* a;
-  int G, P, wide, max_tiles, unit_major;
+  int G, P, max_tiles, unit_major;
   int64_t row0;
   int len, p0, kvh;
 
   PackedFinder finder;      // the producer warp's
+  int* held;
 
-  __device__ __forceinline__ void begin(int lane) { finder.read(*a, 2 * P, lane); }
+  __device__ __forceinline__ void begin(int lane) { finder.read(*a, 2 * P, lane, held); }
   // Items lie longest first; the CTAs take them in turn, every other round in reverse, so that the CTA that
   // got the longest of one round gets the shortest of the next.  Two orders, see launch_packed_tc.
   __device__ __forceinline__ bool find(int k, int lane, Item& it) const {
@@ -76,30 +77,30 @@ struct PackedTcSrc {
     __nv_bfloat16* out = O + (kvh * G + g) * a->o.head + (row0 + pos) * a->o.row;
     const TcRowOut rows_out(mine ? out : nullptr);
 #pragma unroll 1
-    for (int c = 0; c < D / 64; ++c) {     // 64 columns = 32 words of bf16 pairs
-      uint32_t v[64];
-      read(2 * c, reinterpret_cast<uint32_t(&)[32]>(v[0]));
-      read(2 * c + 1, reinterpret_cast<uint32_t(&)[32]>(v[32]));
+    for (int c = 0; c < D / 32; ++c) {
+      uint32_t v[32];
+      read(c, v);
       ptx::tc_wait_ld();
 #pragma unroll
-      for (int k = 0; k < 64; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * inv);
-      if (dirty && mine) {   // non-finite values of masked tiles, kept out of the product, reach the rows that see them
-        for (int i = 0; i < 8; ++i)
-          for (uint32_t bits = dirty[i]; bits; bits &= bits - 1) {
-            const int key = (p0 / kTcKeys + (i >> 2)) * kTcKeys + (i & 3) * 32 + __ffs(bits) - 1;
-            if (key > pos) break;
-            const __nv_bfloat16* src = V + kvh * a->v.head + (row0 + key) * a->v.row + c * 64;
-#pragma unroll
-            for (int k = 0; k < 64; ++k) {
-              const float x = __bfloat162float(src[k]);
-              if (!isfinite(x)) v[k] = __float_as_uint(__uint_as_float(v[k]) + x);
-            }
+      for (int k = 0; k < 16; ++k)
+        v[k] = ptx::pack_bf16x2(__uint_as_float(v[2 * k]) * inv, __uint_as_float(v[2 * k + 1]) * inv);
+      rows_out.store16(v, c * 64);
+    }
+    if (dirty) {   // non-finite values of masked tiles, kept out of the product, are added to the rows that see them
+      __syncwarp();                       // a row has been written by the four lanes of its quad
+      if (!mine) return;
+#pragma unroll 1
+      for (int i = 0; i < 8; ++i)
+        for (uint32_t bits = dirty[i]; bits; bits &= bits - 1) {
+          const int key = (p0 / kTcKeys + (i >> 2)) * kTcKeys + (i & 3) * 32 + __ffs(bits) - 1;
+          if (key > pos) break;
+          const __nv_bfloat16* src = V + kvh * a->v.head + (row0 + key) * a->v.row;
+#pragma unroll 1
+          for (int k = 0; k < D; ++k) {
+            const float x = __bfloat162float(src[k]);
+            if (!isfinite(x)) out[k] = __float2bfloat16_rn(__bfloat162float(out[k]) + x);
           }
-      }
-      uint32_t w[32];
-#pragma unroll
-      for (int k = 0; k < 32; ++k) w[k] = ptx::pack_bf16x2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1]));
-      rows_out.store(w, c * 128, wide != 0);
+        }
     }
   }
 };
@@ -108,10 +109,11 @@ template <int D>
 __global__ void __launch_bounds__(kTcThreads, 1)
 packed_tc_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
                  const __grid_constant__ CUtensorMap mv, const __nv_bfloat16* __restrict__ V,
-                 const __grid_constant__ PackedArgs args, int max_tiles, int unit_major, int wide, float scale_log2e,
+                 const __grid_constant__ PackedArgs args, int max_tiles, int unit_major, float scale_log2e,
                  __nv_bfloat16* __restrict__ O, int* __restrict__ status) {
   extern __shared__ uint8_t packed_tc_smem[];
   __shared__ TcShared<PackedItem> sh;
+  __shared__ int held[PackedFinder::kHeld];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(packed_tc_smem) + 1023) & ~uintptr_t(1023));
   if (threadIdx.x == 0) {
     ptx::tma_prefetch_desc(&mq);
@@ -126,7 +128,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
   src.V = V; src.O = O; src.a = &args;
   src.G = args.n_q_heads / args.n_kv_heads;
   src.P = kTcRows / src.G;
-  src.wide = wide;
+  src.held = held;
   src.max_tiles = max_tiles;
   src.unit_major = unit_major;
   flash_tc<D, true>(src, smem, &sh, scale_log2e, status);
@@ -151,10 +153,9 @@ int launch_packed_tc(const tca_params* prm, const void* Q, const void* K, const 
   // Longest tiles first over all heads balances best, but then the resident CTAs read all heads' keys
   // at once; when those do not fit the L2 the heads go one after another.
   const int unit_major = a.rows * a.n_kv_heads * D * 4 > l2_bytes() / 2 ? 1 : 0;
-  const int wide = aligned(O, 32) && a.o.head % 16 == 0 && a.o.row % 16 == 0 ? 1 : 0;
   const int64_t items = max_tiles * a.n_kv_heads, sms = sm_count();
   return launch_pdl(kern, dim3(unsigned(items < sms ? items : sms)), dim3(kTcThreads), size_t(TcLayout<D>::bytes), s, mq, mk,
-                    mv, static_cast<const __nv_bfloat16*>(V), a, int(max_tiles), unit_major, wide,
+                    mv, static_cast<const __nv_bfloat16*>(V), a, int(max_tiles), unit_major,
                     prm->sm_scale * 1.4426950408889634f, static_cast<__nv_bfloat16*>(O), static_cast<int*>(ws));
 }
 

@@ -92,7 +92,7 @@ struct TreeTcSrc {
       uint32_t v[32];
       read(c, v);
       ptx::tc_wait_ld();
-      rows_out.store(v, c * 128, true);
+      rows_out.store32(v, c * 128);
     }
   }
 };
