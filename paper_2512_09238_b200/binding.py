@@ -144,7 +144,7 @@ def _host(a: Optional[np.ndarray], dtype) -> Optional[int]:
         return None
     if a.dtype != dtype or not a.flags["C_CONTIGUOUS"]:
         raise ValueError(f"host buffer must be a C-contiguous {np.dtype(dtype).name} array")
-    return a.ctypes.data
+    return a.__array_interface__["data"][0]
 
 
 # The current stream's handle without building a Stream object (0.1 us against 3.3 us per call).
@@ -303,84 +303,64 @@ def tca_ws_status(ws, stream=None) -> int:
 
 _ELT = {TCA_BF16: torch.bfloat16, TCA_F32: torch.float32}
 _I64x4, _I64x8 = C.c_int64 * 4, C.c_int64 * 8
+_I32, _I64, _U8 = torch.int32, torch.int64, torch.uint8
 
 
-def _refuse(where: str, here: int, specs) -> None:
-    """Says which argument of a serving call is wrong: specs lists (name, tensor, dtype, shape)."""
-    for name, t, dtype, shape in specs:
+def _refuse(where: str, *specs) -> None:
+    """Says which argument of a serving call is wrong: specs are (name, tensor, dtype, shape, contiguous)."""
+    here = torch.cuda.current_device() if torch.cuda.is_available() else -2
+    for name, t, dtype, shape, whole in specs:
         if t is None:
             continue
         if not isinstance(t, torch.Tensor) or t.get_device() != here:
             raise ValueError(f"{where}: {name} must be a tensor on the current CUDA device")
-        if t.dtype != dtype or t.shape != shape:
-            raise ValueError(f"{where}: {name} must be {dtype} of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+        if t.dtype != dtype or (shape is not None and t.shape != shape):
+            raise ValueError(f"{where}: {name} must be {dtype} of shape {tuple(shape or t.shape)}, got {t.dtype} {tuple(t.shape)}")
+        if (not t.is_contiguous()) if whole else (t.stride(-1) != 1 and t.numel() > 0):
+            raise ValueError(f"{where}: {name} must be contiguous" + ("" if whole else " in its last dimension"))
     raise ValueError(f"{where}: bad argument")
 
 
-def _serving(where: str, specs) -> list:
-    """Device pointers of the tensors of a serving call: each on the current device, of the type and shape that
-    prm and the other arguments imply.  Raises ValueError.  (Kept short: it runs before every launch.)"""
-    first = specs[0][1]
-    here = first.get_device()
-    if here < 0 or here != torch.cuda.current_device():
-        raise ValueError(f"{where}: {specs[0][0]} must be a tensor on the current CUDA device")
-    out = []
-    for _, t, dtype, shape in specs:
-        if t is None:
-            out.append(None)
-            continue
-        if t.dtype is not dtype or t.shape != shape or t.get_device() != here:
-            _refuse(where, here, specs)
-        out.append(t.data_ptr())
-    return out
+def _ok(t, here, dtype, shape) -> bool:
+    """A contiguous tensor of this type and shape on device `here` (or an optional one that is not given)."""
+    return t is None or (t.dtype is dtype and t.shape == shape and t.get_device() == here and t.is_contiguous())
 
 
-def _contiguous(where: str, specs) -> None:
-    for name, t, _, _ in specs:
-        if t is not None and not t.is_contiguous():
-            raise ValueError(f"{where}: {name} must be contiguous")
-
-
-def _view_strides(where: str, t: torch.Tensor, out: list) -> None:
-    """Appends the element strides {head, row} of a [heads, rows, d] view; a dimension of one element counts as
-    contiguous (torch leaves its stride unspecified)."""
-    heads, rows, d = t.shape
+def _view(t, here, dtype, shape, out: list) -> bool:
+    """The same for a [heads, rows, d] view with any strides but the last; appends its element strides {head, row}
+    (a dimension of one element counts as contiguous: torch leaves its stride unspecified)."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != here:
+        return False
     head, row, last = t.stride()
-    if last != 1 and t.numel():
-        raise ValueError(f"{where}: the last dimension must be contiguous")
-    out.append(head if heads > 1 else max(rows, 1) * d)
-    out.append(row if rows > 1 else d)
+    heads, rows, d = shape
+    out += (head if heads > 1 else max(rows, 1) * d, row if rows > 1 else d)
+    return last == 1 or rows == 0
 
 
 def tca_attn_packed(prm, Q, K, V, rows, seq_start, O, ws, stream=None) -> None:
     """Q, O [n_q_heads, rows, d], K, V [n_kv_heads, rows, d]: contiguous, or views with any head and row strides
     that are multiples of 16 bytes (``x.transpose(0, 1)`` of a token-major tensor); seq_start a CUDA int64 tensor
     of prm.batch + 1 elements."""
-    e, d = _ELT[prm.dtype], prm.head_dim
-    qs, ks = (prm.n_q_heads, rows, d), (prm.n_kv_heads, rows, d)
-    q, k, v, o, st, w = _serving("tca_attn_packed", (
-        ("Q", Q, e, qs), ("K", K, e, ks), ("V", V, e, ks), ("O", O, e, qs),
-        ("seq_start", seq_start, torch.int64, (prm.batch + 1,)), ("ws", ws, torch.uint8, ws.shape)))
-    strides = []
-    for t in (Q, K, V, O):
-        _view_strides("tca_attn_packed", t, strides)
-    if not seq_start.is_contiguous() or not ws.is_contiguous():
-        raise ValueError("tca_attn_packed: seq_start and ws must be contiguous")
-    _check(lib().tca_attn_packed(C.byref(prm), q, k, v, rows, st, _I64x8(*strides), o, w, ws.numel(), _stream(stream)),
-           "tca_attn_packed")
+    e, d, here, st = _ELT[prm.dtype], prm.head_dim, Q.get_device(), []
+    qs, ks, ss = (prm.n_q_heads, rows, d), (prm.n_kv_heads, rows, d), (prm.batch + 1,)
+    if not (here >= 0 and here == torch.cuda.current_device() and _view(Q, here, e, qs, st) and _view(K, here, e, ks, st)
+            and _view(V, here, e, ks, st) and _view(O, here, e, qs, st) and _ok(seq_start, here, _I64, ss)
+            and _ok(ws, here, _U8, ws.shape)):
+        _refuse("tca_attn_packed", ("Q", Q, e, qs, False), ("K", K, e, ks, False), ("V", V, e, ks, False),
+                ("O", O, e, qs, False), ("seq_start", seq_start, _I64, ss, True), ("ws", ws, _U8, None, True))
+    _check(lib().tca_attn_packed(C.byref(prm), Q.data_ptr(), K.data_ptr(), V.data_ptr(), rows, seq_start.data_ptr(),
+                                 _I64x8(*st), O.data_ptr(), ws.data_ptr(), ws.numel(), _stream(stream)), "tca_attn_packed")
 
 
 def tca_cache_load(prm, K, V, rows, seq_start, slots, cache: "Cache", stream=None) -> None:
     """K, V [n_kv_heads, rows, d] as in tca_attn_packed; seq_start an int64 and slots an int32 numpy array (or None)."""
-    e, ks = _ELT[prm.dtype], (prm.n_kv_heads, rows, prm.head_dim)
-    k, v = _serving("tca_cache_load", (("K", K, e, ks), ("V", V, e, ks)))
-    strides = []
-    _view_strides("tca_cache_load", K, strides)
-    _view_strides("tca_cache_load", V, strides)
+    e, here, st, ks = _ELT[prm.dtype], K.get_device(), [], (prm.n_kv_heads, rows, prm.head_dim)
+    if not (here >= 0 and here == torch.cuda.current_device() and _view(K, here, e, ks, st) and _view(V, here, e, ks, st)):
+        _refuse("tca_cache_load", ("K", K, e, ks, False), ("V", V, e, ks, False))
     n_seq = len(seq_start) - 1
     if slots is not None and len(slots) != n_seq:
         raise ValueError("tca_cache_load: slots must have one entry per sequence")
-    _check(lib().tca_cache_load(C.byref(prm), k, v, rows, _I64x4(*strides), _host(seq_start, np.int64),
+    _check(lib().tca_cache_load(C.byref(prm), K.data_ptr(), V.data_ptr(), rows, _I64x4(*st), _host(seq_start, np.int64),
                                 _host(slots, np.int32), n_seq, C.byref(cache.desc), _stream(stream)), "tca_cache_load")
 
 
@@ -397,29 +377,32 @@ def alloc_tree_workspace(prm: tca_params, n_draft: int, device="cuda") -> torch.
 
 
 def tca_attn_tree(prm, q, k_draft, v_draft, n_draft, parent, n_live, cache: "Cache", O, ws, stream=None) -> None:
-    e, B, d = _ELT[prm.dtype], prm.batch, prm.head_dim
-    qs, ks = (B, prm.n_q_heads, n_draft, d), (B, prm.n_kv_heads, n_draft, d)
-    specs = (("q", q, e, qs), ("k_draft", k_draft, e, ks), ("v_draft", v_draft, e, ks), ("O", O, e, qs),
-             ("parent", parent, torch.int32, (B, n_draft)), ("n_live", n_live, torch.int32, (B,)),
-             ("ws", ws, torch.uint8, ws.shape))
-    qp, kp, vp, op, pp, np_, wp = _serving("tca_attn_tree", specs)
-    _contiguous("tca_attn_tree", specs)
-    _check(lib().tca_attn_tree(C.byref(prm), qp, kp, vp, n_draft, pp, np_, C.byref(cache.desc), op, wp, ws.numel(),
-                               _stream(stream)), "tca_attn_tree")
+    e, B, d, here = _ELT[prm.dtype], prm.batch, prm.head_dim, q.get_device()
+    qs, ks, ps = (B, prm.n_q_heads, n_draft, d), (B, prm.n_kv_heads, n_draft, d), (B, n_draft)
+    if not (here >= 0 and here == torch.cuda.current_device() and _ok(q, here, e, qs) and _ok(k_draft, here, e, ks)
+            and _ok(v_draft, here, e, ks) and _ok(O, here, e, qs) and _ok(parent, here, _I32, ps)
+            and _ok(n_live, here, _I32, (B,)) and _ok(ws, here, _U8, ws.shape)):
+        _refuse("tca_attn_tree", ("q", q, e, qs, True), ("k_draft", k_draft, e, ks, True), ("v_draft", v_draft, e, ks, True),
+                ("O", O, e, qs, True), ("parent", parent, _I32, ps, True), ("n_live", n_live, _I32, (B,), True),
+                ("ws", ws, _U8, None, True))
+    _check(lib().tca_attn_tree(C.byref(prm), q.data_ptr(), k_draft.data_ptr(), v_draft.data_ptr(), n_draft, parent.data_ptr(),
+                               None if n_live is None else n_live.data_ptr(), C.byref(cache.desc), O.data_ptr(),
+                               ws.data_ptr(), ws.numel(), _stream(stream)), "tca_attn_tree")
 
 
 def tca_cache_accept(prm, cache: "Cache", k_draft, v_draft, q_draft, n_draft, path, n_accept, stream=None) -> None:
     """path a CUDA int32 tensor [batch, n_draft]; n_accept an int32 numpy array of prm.batch elements."""
-    e, B, d = _ELT[prm.dtype], prm.batch, prm.head_dim
-    ks = (B, prm.n_kv_heads, n_draft, d)
-    specs = (("k_draft", k_draft, e, ks), ("v_draft", v_draft, e, ks),
-             ("q_draft", q_draft, e, (B, prm.n_q_heads, n_draft, d)), ("path", path, torch.int32, (B, n_draft)))
-    kp, vp, qp, pp = _serving("tca_cache_accept", specs)
-    _contiguous("tca_cache_accept", specs)
+    e, B, d, here = _ELT[prm.dtype], prm.batch, prm.head_dim, k_draft.get_device()
+    qs, ks, ps = (B, prm.n_q_heads, n_draft, d), (B, prm.n_kv_heads, n_draft, d), (B, n_draft)
+    if not (here >= 0 and here == torch.cuda.current_device() and _ok(k_draft, here, e, ks) and _ok(v_draft, here, e, ks)
+            and _ok(q_draft, here, e, qs) and _ok(path, here, _I32, ps)):
+        _refuse("tca_cache_accept", ("k_draft", k_draft, e, ks, True), ("v_draft", v_draft, e, ks, True),
+                ("q_draft", q_draft, e, qs, True), ("path", path, _I32, ps, True))
     if len(n_accept) != B:
         raise ValueError("tca_cache_accept: n_accept must have one entry per sequence")
-    _check(lib().tca_cache_accept(C.byref(prm), C.byref(cache.desc), kp, vp, qp, n_draft, pp, _host(n_accept, np.int32),
-                                  _stream(stream)), "tca_cache_accept")
+    _check(lib().tca_cache_accept(C.byref(prm), C.byref(cache.desc), k_draft.data_ptr(), v_draft.data_ptr(),
+                                  q_draft.data_ptr(), n_draft, path.data_ptr(), _host(n_accept, np.int32), _stream(stream)),
+           "tca_cache_accept")
 
 
 # ----------------------------------------------------------------------------- cache descriptor holder

@@ -248,6 +248,7 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
       bool ok = true;
       auto wait_group = [&](int g) { return ptx::mbar_wait(bar_empty + g % kPairs, uint32_t(g / kPairs) & 1u, abort_flag); };
       src.begin(lane);
+#pragma unroll 1
       for (int k = 0; ok; ++k) {
         typename Source::Item item;
         const bool have = src.find(k, lane, item);
@@ -271,6 +272,7 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
             src.load_q(0, smem + L::offQ, bar_q);
             if (two) src.load_q(1, smem + L::offQ + L::kTile, bar_q);
           }
+#pragma unroll 1
           for (int m = -1; m < nt && ok; ++m, ++group) {     // group m: V_m and K_m+lead; m = -1: the leading K tiles
             if (group >= kPairs) ok = wait_group(group - kPairs);
             uint64_t* full = bar_full + group % kPairs;
@@ -359,6 +361,7 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
                              b0 + uint32_t((kk * 2048) >> 4), idesc_pv, (acc || kk > 0) ? 1u : 0u);
         return true;
       };
+#pragma unroll 1
       for (int k = 0; next_item(k); ++k) {
         const int n0 = src.tiles(0), n1 = kShared ? src.tiles(1) : 0, nt = kShared ? max(n0, n1) : n0;
         bool ok = warp_wait(bar_q, uint32_t(k) & 1u) && warp_wait(bar_full + group % kPairs, uint32_t(group / kPairs) & 1u);
@@ -374,6 +377,7 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
         ptx::umma_commit_elect(bar_empty + group % kPairs);
         ++group;
         int t = 0;
+#pragma unroll 1
         for (const int fast = src.whole_tiles() - kLead; t < fast && ok; ++t, ++group) {
           ok = warp_wait(bar_full + group % kPairs, uint32_t(group / kPairs) & 1u);
           if (kShared) {
@@ -395,6 +399,7 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
           if (t + 1 + kLead == nt) ptx::umma_commit_elect(bar_q_empty);      // the last scores have been issued
           ptx::umma_commit_elect(bar_empty + group % kPairs);
         }
+#pragma unroll 1
         for (; t < nt && ok; ++t, ++group) {
           ok = warp_wait(bar_full + group % kPairs, uint32_t(group / kPairs) & 1u);
 #pragma unroll 1
@@ -420,6 +425,7 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
       // Such a tile arrives on a barrier of its own and joins its group when both warps are done with it.
       uint32_t cleaned = 0;
       int base = 0, group = 0;
+#pragma unroll 1
       for (int k = 0; next_item(k); ++k) {
         const int n0 = src.tiles(0), n1 = kShared ? src.tiles(1) : 0, nt = kShared ? max(n0, n1) : n0;
         bool ok = true;
@@ -528,6 +534,7 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
       };
       const int whole = kShared ? min(src.whole_tiles(), mine) : (src.whole_tiles() - h + 1) / 2;   // they come first
       int it = 0;
+#pragma unroll 1
       for (; it < whole; ++it) {
         ok = warp_wait(bar_s + h, tile_count++ & 1u);
         if (!ok) break;

@@ -256,3 +256,38 @@ def test_prompts_to_drafted_tokens_as_a_server_runs_them(dtype):
             rows = cache.unit_rows(b * hkv + h // (hq // hkv))
             w, a, s = S.masked_attention(H.f64(qn)[b, h][None], kk[rows], vv[rows], np.ones((1, len(rows)), dtype=bool), H.scale_of(d))
             H.check(H.f64(out)[b, h][None], w, S.attention_tolerance(w, a, s, d, np.array([len(rows)]), dtype), "decode")
+
+
+def test_the_binding_refuses_wrong_tensors():
+    prm = H.params(2, 4, 2, 64, "bf16")
+    cache = H.make_cache(prm, 5, 5, 0, 20, "bf16", 16)
+    q, kd, vd = drafts(prm, 4, "bf16", 130)
+    par = torch.zeros(2, 4, dtype=torch.int32, device="cuda")
+    ws, o, n = B.alloc_tree_workspace(prm, 4), torch.zeros_like(q), np.zeros(2, dtype=np.int32)
+    good = dict(q=q, kd=kd, vd=vd, par=par, live=None, o=o, ws=ws)
+    for bad in (dict(q=q.float()), dict(q=q.cpu()), dict(kd=kd[:, :1]), dict(vd=vd.transpose(1, 2)), dict(o=o[:1]),
+                dict(par=par.long()), dict(live=torch.zeros(3, dtype=torch.int32, device="cuda")), dict(ws=ws.cpu()),
+                dict(q=q.transpose(0, 1).contiguous().transpose(0, 1)), dict(par=par.cpu())):
+        a = {**good, **bad}
+        with pytest.raises(ValueError):
+            B.tca_attn_tree(prm, a["q"], a["kd"], a["vd"], 4, a["par"], a["live"], cache, a["o"], a["ws"])
+    for bad in (dict(q=q.float()), dict(kd=kd.cpu()), dict(vd=vd[:, :, :3]), dict(par=par.long())):
+        a = {**good, **bad}
+        with pytest.raises(ValueError):
+            B.tca_cache_accept(prm, cache, a["kd"], a["vd"], a["q"], 4, a["par"], n)
+    with pytest.raises(ValueError):
+        B.tca_cache_accept(prm, cache, kd, vd, q, 4, par, np.zeros(3, dtype=np.int32))
+    with pytest.raises(ValueError):
+        B.tca_cache_accept(prm, cache, kd, vd, q, 4, par, np.zeros(2, dtype=np.int64))
+    x = H.randn(1, (2, 10, 64), "bf16")
+    st = torch.tensor([0, 5, 10], device="cuda")
+    pws = B.alloc_workspace(prm, 10, B.TCA_OP_PACKED)
+    qp = H.randn(2, (4, 10, 64), "bf16")
+    for a in ((qp, x, x, st.int(), qp.clone(), pws), (qp, x, x.float(), st, qp.clone(), pws), (qp[:, :9], x, x, st, qp.clone(), pws),
+              (qp, x, x, st[:2], qp.clone(), pws), (qp, x, x, st.cpu(), qp.clone(), pws), (qp, x, x, st, qp[:, :, ::2], pws),
+              (qp, x.transpose(1, 2).contiguous().transpose(1, 2), x, st, qp.clone(), pws)):
+        with pytest.raises(ValueError):
+            B.tca_attn_packed(prm, a[0], a[1], a[2], 10, a[3], a[4], a[5])
+    with pytest.raises(ValueError):
+        B.tca_cache_load(prm, x.cpu(), x, 10, np.array([0, 10]), None, cache)
+    torch.cuda.synchronize()
