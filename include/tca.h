@@ -417,7 +417,8 @@ int tca_cache_load(const tca_params* prm, const void* K, const void* V, int64_t 
  *   n_live    DEVICE [batch] int32, optional: only drafted tokens t < n_live[s] exist; the rows of O of
  *             the others are left as they were and their q, k, v are not used.  NULL: all n_draft.
  *   ws        DEVICE workspace of tca_attn_tree_workspace_bytes(prm, n_draft) bytes, zeroed once after
- *             allocating; word 0 is the sticky status word.  Calls that share one must not overlap.
+ *             allocating; word 0 is the sticky status word.  It serves calls with fewer drafted tokens
+ *             too.  Calls that share one must not overlap.
  * A drafted token outside a row's path does not influence it whatever it holds.  How the cache rows are
  * dealt to CTAs follows from the device state words, so a captured call may be replayed after the cache
  * has changed.  1 <= n_draft <= TCA_TREE_MAX, batch * n_kv_heads <= 65535, else TCA_ERR_UNSUPPORTED.

@@ -27,18 +27,27 @@ struct PackedTcSrc {
   PackedFinder finder;      // the producer warp's
   int* held;
 
-  __device__ __forceinline__ void begin(int lane) { finder.read(*a, 2 * P, lane, held); }
-  // Items lie longest first; the CTAs take them in turn, every other round in reverse, so that the CTA that
-  // got the longest of one round gets the shortest of the next.  Two orders, see launch_packed_tc.
-  __device__ __forceinline__ bool find(int k, int lane, Item& it) const {
+  __device__ __forceinline__ void begin(int lane) { finder.read(*a, 2 * P, lane, held); round = 0; }
+  // The CTAs take the items in turn, every other round in reverse, so that the CTA that got the longest of
+  // one round gets the shortest of the next.  Two orders, see launch_packed_tc; with the heads one after
+  // another the numbers past a head's last item are skipped.
+  int round;
+  __device__ __forceinline__ bool find(int, int lane, Item& it) {
     const int n = int(gridDim.x);
-    const int i = k * n + ((k & 1) ? n - 1 - int(blockIdx.x) : int(blockIdx.x));
-    if (i >= max_tiles * a->n_kv_heads) return false;
-    it.kvh = unit_major ? i / max_tiles : i % a->n_kv_heads;
-    int tile;
-    if (!finder.find(*a, unit_major ? i % max_tiles : i / a->n_kv_heads, 2 * P, lane, it.row0, it.len, tile)) return false;
-    it.p0 = tile * 2 * P;
-    return true;
+    for (;; ++round) {
+      const int i = round * n + ((round & 1) ? n - 1 - int(blockIdx.x) : int(blockIdx.x));
+      if (round * n >= max_tiles * a->n_kv_heads) return false;
+      if (i >= max_tiles * a->n_kv_heads) continue;
+      it.kvh = unit_major ? i / max_tiles : i % a->n_kv_heads;
+      int tile;
+      if (!finder.find(*a, unit_major ? i % max_tiles : i / a->n_kv_heads, 2 * P, lane, it.row0, it.len, tile)) {
+        if (unit_major) continue;
+        return false;                        // the numbers without an item are the last ones
+      }
+      it.p0 = tile * 2 * P;
+      ++round;
+      return true;
+    }
   }
   __device__ __forceinline__ void set(const Item& it) { row0 = it.row0; len = it.len; p0 = it.p0; kvh = it.kvh; }
 
@@ -150,9 +159,11 @@ int launch_packed_tc(const tca_params* prm, const void* Q, const void* K, const 
     return TCA_ERR_CUDA;
   auto kern = packed_tc_kernel<D>;
   if (allow_smem<packed_tc_kernel<D>>(TcLayout<D>::bytes) != TCA_OK) return TCA_ERR_CUDA;
-  // Longest tiles first over all heads balances best, but then the resident CTAs read all heads' keys
-  // at once; when those do not fit the L2 the heads go one after another.
-  const int unit_major = a.rows * a.n_kv_heads * D * 4 > l2_bytes() / 2 ? 1 : 0;
+  // Items of all heads in one order balance best, but then the resident CTAs read all heads' keys at once;
+  // when those are more than half of the L2 the heads go one after another (128K tokens, 8 heads: 120
+  // against 135 ms).  Not with so many sequences that no single one is long: their keys are read once or
+  // twice anyway (500 prompts of up to 200 tokens: 460 against 590 us).
+  const int unit_major = a.n_seq <= PackedFinder::kHeld && a.rows * a.n_kv_heads * D * 4 > l2_bytes() / 2 ? 1 : 0;
   const int64_t items = max_tiles * a.n_kv_heads, sms = sm_count();
   return launch_pdl(kern, dim3(unsigned(items < sms ? items : sms)), dim3(kTcThreads), size_t(TcLayout<D>::bytes), s, mq, mk,
                     mv, static_cast<const __nv_bfloat16*>(V), a, int(max_tiles), unit_major,

@@ -231,10 +231,10 @@ tree_combine_kernel(const T* __restrict__ q, const T* __restrict__ k_draft, cons
   }
   pdl_wait();                 // the partial results come from the split kernel
   pdl_launch_dependents();
-  if (!live) return;
+  if (!live || *reinterpret_cast<volatile int*>(ws.status) != 0) return;   // a wait gave up: there are no partial results
   // the unit's partial results, in the order of its rows; a unit whose cache is empty has none
   const int2 where = cached > 0 ? ws.table[u] : make_int2(0, 0);
-  const int n = where.y * plan.streams;
+  const int n = min(where.y, plan.n_slots - where.x) * plan.streams;
   const size_t first = size_t(where.x) * plan.streams;
   for (int c0 = 0; c0 < n; c0 += 32) {                       // statistics of 32 partials at a time, one per lane
     const int cn = min(32, n - c0);
@@ -304,7 +304,12 @@ using namespace tca;
 
 extern "C" size_t tca_attn_tree_workspace_bytes(const tca_params* prm, int32_t n_draft) {
   if (check_params(prm) != TCA_OK || n_draft < 1 || bad_tree_shape(prm, n_draft)) return 0;
-  return tree_ws_layout(prm, tree_plan(prm, n_draft), nullptr).bytes;
+  size_t most = 0;   // fewer rows can need more (they run as two streams): one workspace serves all calls up to n_draft
+  for (int32_t n = 1; n <= n_draft; ++n) {
+    const size_t bytes = tree_ws_layout(prm, tree_plan(prm, n), nullptr).bytes;
+    most = bytes > most ? bytes : most;
+  }
+  return most;
 }
 
 extern "C" int tca_attn_tree(const tca_params* prm, const void* q, const void* k_draft, const void* v_draft,

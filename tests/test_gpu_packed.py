@@ -150,6 +150,60 @@ def test_long_rows_sampled():
             H.check(o[h, 10 + i][None], want, S.attention_tolerance(want, a, s, d, np.array([i + 1]), "bf16"), f"row {i}")
 
 
+def test_many_sequences_with_long_ones_among_them():
+    """More sequences than are searched in sorted order, and more keys than the L2 holds."""
+    hq, hkv, d = 8, 4, 128
+    lens = [(i * 37) % 60 for i in range(300)]
+    lens[0], lens[150], lens[299] = 5000, 9000, 20000
+    prm = H.params(len(lens), hq, hkv, d, "bf16")
+    starts = np.concatenate([[0], np.cumsum(lens)])
+    rows = int(starts[-1])
+    q, k, v = (H.packed_buffer(85 + i, h, rows, d, "bf16", "heads") for i, h in enumerate((hq, hkv, hkv)))
+    out = H.run_packed(prm, q, k, v, starts)
+    assert torch.isfinite(out).all()
+    for s in (0, 7, 150, 151, 298, 299):
+        n, lo = lens[s], int(starts[s])
+        for i in {0, n // 2, n - 1} if n else ():
+            for h in (0, 3, 7):
+                kk, vv = H.f64(k[h // 2, lo:lo + i + 1]), H.f64(v[h // 2, lo:lo + i + 1])
+                want, a, ss = S.masked_attention(H.f64(q[h, lo + i])[None], kk, vv, np.ones((1, i + 1), dtype=bool), H.scale_of(d))
+                H.check(H.f64(out[h, lo + i])[None], want, S.attention_tolerance(want, a, ss, d, np.array([i + 1]), "bf16"), f"{s} {i} {h}")
+
+
+@pytest.mark.parametrize("layout", ["heads", "tokens"])
+def test_more_keys_than_the_l2_holds(layout):
+    """Enough keys that the heads are worked through one after another; several sequences, all heads sampled."""
+    hq, hkv, d = 16, 8, 128
+    lens = [9000, 0, 301, 1, 16000, 77, 5000]
+    prm = H.params(len(lens), hq, hkv, d, "bf16")
+    starts = np.concatenate([[0], np.cumsum(lens)])
+    rows = int(starts[-1])
+    assert rows * hkv * d * 4 > 100e6
+    q, k, v = (H.packed_buffer(95 + i, h, rows, d, "bf16", layout) for i, h in enumerate((hq, hkv, hkv)))
+    out = H.run_packed(prm, q, k, v, starts)
+    assert torch.isfinite(out).all()                          # every row of every head was written
+    for s, n in enumerate(lens):
+        for i in {0, n // 3, n - 65, n - 1}:
+            if not 0 <= i < n:
+                continue
+            lo = int(starts[s])
+            for h in range(hq):
+                kk, vv = H.f64(k[h // 2, lo:lo + i + 1]), H.f64(v[h // 2, lo:lo + i + 1])
+                want, a, ss = S.masked_attention(H.f64(q[h, lo + i])[None], kk, vv, np.ones((1, i + 1), dtype=bool), H.scale_of(d))
+                H.check(H.f64(out[h, lo + i])[None], want, S.attention_tolerance(want, a, ss, d, np.array([i + 1]), "bf16"), f"{s} {i} {h}")
+
+
+def test_a_set_status_word_stops_the_call():
+    prm, q, k, v, starts = case([50, 60], 4, 2, 128, "bf16", "heads", 97)
+    ws = B.alloc_workspace(prm, q.shape[1], B.TCA_OP_PACKED)
+    ws[:4] = torch.tensor([1, 0, 0, 0], dtype=torch.uint8, device="cuda")
+    o = torch.full_like(q, 7.0)
+    B.tca_attn_packed(prm, q, k, v, q.shape[1], torch.tensor(starts, device="cuda"), o, ws)
+    assert B.tca_ws_status(ws) == B.TCA_ERR_TIMEOUT and (o == 7.0).all()
+    ws.zero_()
+    compare(prm, q, k, v, starts, H.run_packed(prm, q, k, v, starts, ws=ws), "bf16")
+
+
 def test_tensor_cores_agree_with_the_fp32_pipes():
     prm, q, k, v, starts = case([700, 130, 9], 8, 2, 128, "bf16", "tokens", 100)
     a = H.f64(H.run_packed(prm, q, k, v, starts))

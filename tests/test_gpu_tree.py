@@ -152,6 +152,30 @@ def test_a_captured_call_replays_over_a_cache_that_has_grown(dtype):
             H.check_tree(prm, q, kd, vd, parent, cache, o, dtype)
 
 
+def test_a_set_status_word_stops_the_call():
+    prm = H.params(1, 4, 2, 128, "bf16")
+    cache = H.make_cache(prm, 200, 90, 0, 300, "bf16", 17)
+    q, kd, vd = drafts(prm, 5, "bf16", 140)
+    par = torch.from_numpy(H.chain(5)[None].copy()).cuda()
+    ws, o = B.alloc_tree_workspace(prm, 5), torch.full_like(q, 7.0)
+    ws[:4] = torch.tensor([1, 0, 0, 0], dtype=torch.uint8, device="cuda")
+    B.tca_attn_tree(prm, q, kd, vd, 5, par, None, cache, o, ws)
+    assert B.tca_ws_status(ws) == B.TCA_ERR_TIMEOUT and (o == 7.0).all()
+    ws.zero_()
+    H.check_tree(prm, q, kd, vd, H.chain(5)[None], cache, H.run_tree(prm, q, kd, vd, H.chain(5)[None], cache, ws=ws), "bf16")
+
+
+def test_one_workspace_serves_calls_of_different_shapes():
+    """A workspace sized for the largest call holds what earlier, larger calls left behind."""
+    prm = H.params(3, 8, 2, 128, "bf16")
+    cache = H.make_cache(prm, [900, 5, 0, 300, 260, 40], [90, 3, 0, 64, 10, 95], 20, 1000, "bf16", 18)
+    ws = B.alloc_tree_workspace(prm, 100)
+    for T in (100, 3, 32, 1, 65):
+        q, kd, vd = drafts(prm, T, "bf16", 150 + T)
+        parent = np.stack([H.bush(T, T + i) for i in range(3)])
+        H.check_tree(prm, q, kd, vd, parent, cache, H.run_tree(prm, q, kd, vd, parent, cache, ws=ws), "bf16", heads=(0, 7))
+
+
 # ------------------------------------------------------------------ tca_cache_accept
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("block,window,n_tail,T", [(32, 64, 60, 20), (32, 64, 95, 9), (16, 8, 23, 64), (1, 1, 1, 12),
