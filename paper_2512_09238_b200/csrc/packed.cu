@@ -15,27 +15,30 @@ namespace {
 
 // Query rows of a CTA are (position, head of the group) pairs, head fastest: row r is position
 // p0 + r / G, head kvh * G + r % G, so a short sequence of a wide group still fills the tile.
-template <typename T>
+template <typename T, typename Shape>
 struct PackedSrc {
+  static constexpr int kRows = Shape::kRows, kKeys = Shape::kKeys;
   const T *Q, *K, *V;
   const PackedArgs* a;
   PackedWork w;
   int G;
-  __device__ __forceinline__ int n_rows() const { return min(kSimtRows / G, w.len - w.p0) * G; }
+  __device__ __forceinline__ int n_rows() const { return min(kRows / G, w.len - w.p0) * G; }
   __device__ __forceinline__ int last_pos() const { return w.p0 + n_rows() / G - 1; }
-  __device__ __forceinline__ int n_tiles() const { return last_pos() / kSimtKeys + 1; }
-  __device__ __forceinline__ int keys(int t) const { return min(kSimtKeys, last_pos() + 1 - t * kSimtKeys); }
+  __device__ __forceinline__ int n_tiles() const { return last_pos() / kKeys + 1; }
+  __device__ __forceinline__ int keys(int t) const { return min(kKeys, last_pos() + 1 - t * kKeys); }
   __device__ __forceinline__ const T* q(int r) const {
     return Q + (w.kvh * G + r % G) * a->q.head + (w.row0 + w.p0 + r / G) * a->q.row;
   }
-  __device__ __forceinline__ const T* k(int t, int r) const { return K + w.kvh * a->k.head + (w.row0 + t * kSimtKeys + r) * a->k.row; }
-  __device__ __forceinline__ const T* v(int t, int r) const { return V + w.kvh * a->v.head + (w.row0 + t * kSimtKeys + r) * a->v.row; }
-  __device__ __forceinline__ bool masked(int t) const { return (t + 1) * kSimtKeys - 1 > w.p0; }
-  __device__ __forceinline__ int last(int t, int r) const { return min(w.p0 + r / G, last_pos()) - t * kSimtKeys; }
+  __device__ __forceinline__ const T* k(int t) const { return K + w.kvh * a->k.head + (w.row0 + t * kKeys) * a->k.row; }
+  __device__ __forceinline__ const T* v(int t) const { return V + w.kvh * a->v.head + (w.row0 + t * kKeys) * a->v.row; }
+  __device__ __forceinline__ int64_t k_stride() const { return a->k.row; }
+  __device__ __forceinline__ int64_t v_stride() const { return a->v.row; }
+  __device__ __forceinline__ bool masked(int t) const { return (t + 1) * kKeys - 1 > w.p0; }
+  __device__ __forceinline__ int last(int t, int r) const { return min(w.p0 + r / G, last_pos()) - t * kKeys; }
 };
 
-template <typename T, int D>
-__global__ void __launch_bounds__(kSimtThreads, SimtSmem<D>::kCtasPerSm)
+template <typename T, int D, typename Shape>
+__global__ void __launch_bounds__(kSimtThreads, SimtSmem<D, Shape>::kCtasPerSm)
 packed_simt_kernel(const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const __grid_constant__ PackedArgs args,
                    float scale_log2e, T* __restrict__ O) {
   extern __shared__ float4 packed_smem[];
@@ -44,8 +47,8 @@ packed_simt_kernel(const T* __restrict__ Q, const T* __restrict__ K, const T* __
   pdl_wait();
   pdl_launch_dependents();
   const int G = args.n_q_heads / args.n_kv_heads;
-  const int tile_pos = kSimtRows / G;
-  PackedSrc<T> src;
+  const int tile_pos = Shape::kRows / G;
+  PackedSrc<T, Shape> src;
   src.Q = Q; src.K = K; src.V = V; src.a = &args; src.G = G;
   if (threadIdx.x < 32) {
     PackedFinder finder;
@@ -62,12 +65,13 @@ packed_simt_kernel(const T* __restrict__ Q, const T* __restrict__ K, const T* __
   __syncthreads();
   src.w = found;
   if (src.w.len == 0) return;
-  float o[4][D / 16], m[4], l[4];
-  if (!simt_flash<T, D>(src, scale_log2e, reinterpret_cast<float*>(packed_smem), o, m, l)) return;
+  constexpr int RT = Shape::RT;
+  float o[RT][D / 16], m[RT], l[RT];
+  if (!simt_flash<T, D, Shape>(src, scale_log2e, reinterpret_cast<float*>(packed_smem), o, m, l)) return;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int r = ty * 4 + i;
+  for (int i = 0; i < RT; ++i) {
+    const int r = ty * RT + i;
     if (r >= src.n_rows()) continue;
     T* out = O + (src.w.kvh * G + r % G) * args.o.head + (src.w.row0 + src.w.p0 + r / G) * args.o.row;
     const float inv = 1.f / l[i];
@@ -76,17 +80,29 @@ packed_simt_kernel(const T* __restrict__ Q, const T* __restrict__ K, const T* __
   }
 }
 
+template <typename T, int D, typename Shape>
+int launch_packed_shape(const tca_params* prm, const void* Q, const void* K, const void* V, const PackedArgs& a, void* O,
+                        cudaStream_t s) {
+  using Smem = SimtSmem<D, Shape>;
+  const int64_t n = packed_max_tiles(a.rows, a.n_seq, Shape::kRows / (a.n_q_heads / a.n_kv_heads)) * a.n_kv_heads;
+  if (n >= (int64_t(1) << 31)) return TCA_ERR_UNSUPPORTED;
+  constexpr auto kern = packed_simt_kernel<T, D, Shape>;
+  if (allow_smem<kern>(Smem::kBytes) != TCA_OK) return TCA_ERR_CUDA;
+  return launch_pdl(kern, dim3(unsigned(n)), dim3(kSimtThreads), size_t(Smem::kBytes), s, static_cast<const T*>(Q),
+                    static_cast<const T*>(K), static_cast<const T*>(V), a, prm->sm_scale * 1.4426950408889634f,
+                    static_cast<T*>(O));
+}
+
+// The large tiles where they give every SM more than one CTA and are not mostly padding: prompts that
+// average four of them.
 template <typename T, int D>
 int launch_packed_simt(const tca_params* prm, const void* Q, const void* K, const void* V, const PackedArgs& a, void* O,
                        cudaStream_t s) {
-  const int G = a.n_q_heads / a.n_kv_heads;
-  const int64_t n = packed_max_tiles(a.rows, a.n_seq, kSimtRows / G) * a.n_kv_heads;
-  if (n >= (int64_t(1) << 31)) return TCA_ERR_UNSUPPORTED;
-  auto kern = packed_simt_kernel<T, D>;
-  if (allow_smem<packed_simt_kernel<T, D>>(SimtSmem<D>::kBytes) != TCA_OK) return TCA_ERR_CUDA;
-  return launch_pdl(kern, dim3(unsigned(n)), dim3(kSimtThreads), size_t(SimtSmem<D>::kBytes), s,
-                    static_cast<const T*>(Q), static_cast<const T*>(K), static_cast<const T*>(V), a,
-                    prm->sm_scale * 1.4426950408889634f, static_cast<T*>(O));
+  using Large = SimtLarge<D>;
+  const int64_t tiles = a.rows * a.n_q_heads / Large::kRows;
+  if (tiles >= sm_count() && a.rows * (a.n_q_heads / a.n_kv_heads) >= int64_t(4) * Large::kRows * a.n_seq)
+    return launch_packed_shape<T, D, Large>(prm, Q, K, V, a, O, s);
+  return launch_packed_shape<T, D, SimtSmall>(prm, Q, K, V, a, O, s);
 }
 
 // A buffer's strides: multiples of 16 bytes (vector loads, tensor maps), and room for a row.

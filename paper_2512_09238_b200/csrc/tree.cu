@@ -26,11 +26,11 @@ TreePlan tree_plan(const tca_params* prm, int n_draft) {
   p.rows = prm->n_q_heads / prm->n_kv_heads * n_draft;
   // tensor cores: up to 128 rows run as two streams over alternate tiles, more as two blocks per CTA
   p.streams = tc && p.rows <= 128 ? 2 : 1;
-  p.rows_per_cta = !tc ? kSimtRows : p.rows <= 128 ? 128 : 256;
+  p.rows_per_cta = !tc ? SimtSmall::kRows : p.rows <= 128 ? 128 : 256;
   p.row_blocks = (p.rows + p.rows_per_cta - 1) / p.rows_per_cta;
   p.min_share = tc ? 2 : 1;
   p.lead = tc ? 3 : 0;
-  const int resident = (tc || prm->head_dim == 128 ? 1 : 2) * sm_count();
+  const int resident = (tc ? 1 : prm->head_dim == 128 ? SimtSmem<128, SimtSmall>::kCtasPerSm : SimtSmem<64, SimtSmall>::kCtasPerSm) * sm_count();
   p.n_shares = resident / p.row_blocks > 0 ? resident / p.row_blocks : 1;
   p.n_slots = p.n_shares + U;
   return p;
@@ -42,50 +42,52 @@ template <typename T, int D>
 struct TreeSrc {
   const T *q_rows, *Kc, *Vc;      // first query row of this CTA; the cache
   int n;                          // query rows here
-  SliceTiles<kSimtKeys> tiles;
+  SliceTiles<SimtSmall::kKeys> tiles;
   __device__ __forceinline__ int n_rows() const { return n; }
   __device__ __forceinline__ int n_tiles() const { return tiles.n_tiles(); }
   __device__ __forceinline__ int keys(int t) const { int y, c; tiles.get(t, y, c); return c; }
   __device__ __forceinline__ const T* q(int r) const { return q_rows + int64_t(r) * D; }
-  __device__ __forceinline__ const T* k(int t, int r) const { int y, c; tiles.get(t, y, c); return Kc + int64_t(y + r) * D; }
-  __device__ __forceinline__ const T* v(int t, int r) const { int y, c; tiles.get(t, y, c); return Vc + int64_t(y + r) * D; }
-  __device__ __forceinline__ bool masked(int t) const { return keys(t) < kSimtKeys; }
+  __device__ __forceinline__ const T* k(int t) const { int y, c; tiles.get(t, y, c); return Kc + int64_t(y) * D; }
+  __device__ __forceinline__ const T* v(int t) const { int y, c; tiles.get(t, y, c); return Vc + int64_t(y) * D; }
+  __device__ __forceinline__ int k_stride() const { return D; }
+  __device__ __forceinline__ int v_stride() const { return D; }
+  __device__ __forceinline__ bool masked(int t) const { return keys(t) < SimtSmall::kKeys; }
   __device__ __forceinline__ int last(int t, int) const { return keys(t) - 1; }
 };
 
 template <typename T, int D>
-__global__ void __launch_bounds__(kSimtThreads, SimtSmem<D>::kCtasPerSm)
+__global__ void __launch_bounds__(kSimtThreads, SimtSmem<D, SimtSmall>::kCtasPerSm)
 tree_simt_kernel(const T* __restrict__ q, const T* __restrict__ Kc, const T* __restrict__ Vc,
                  const int64_t* __restrict__ state, int n_units, int64_t tail_cap, TreePlan plan, float scale_log2e,
                  TreeWs ws) {
   extern __shared__ float4 tree_smem[];
-  __shared__ TreePiece<kSimtKeys> piece;
+  __shared__ TreePiece<SimtSmall::kKeys> piece;
   pdl_wait();
   pdl_launch_dependents();
   const int share = int(blockIdx.x) / plan.row_blocks, rb = int(blockIdx.x) % plan.row_blocks;
-  const int row0 = rb * kSimtRows;
+  const int row0 = rb * SimtSmall::kRows;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;   // of the group that writes
   TreeFinder finder;
   if (threadIdx.x < 32) finder.start(state, n_units, plan, share, threadIdx.x);
   for (;;) {
     if (threadIdx.x < 32) {
-      TreePiece<kSimtKeys> p;
+      TreePiece<SimtSmall::kKeys> p;
       const bool more = finder.next(state, n_units, int(tail_cap), share, rb == 0, ws.table, threadIdx.x, p);
       if (!more) p.u = -1;
       if (threadIdx.x == 0) piece = p;
     }
     __syncthreads();
-    const TreePiece<kSimtKeys> mine = piece;
+    const TreePiece<SimtSmall::kKeys> mine = piece;
     __syncthreads();                       // read by all before the next one is written
     if (mine.u < 0) return;
     TreeSrc<T, D> src;
-    src.n = min(kSimtRows, plan.rows - row0);
+    src.n = min(SimtSmall::kRows, plan.rows - row0);
     src.q_rows = q + (int64_t(mine.u) * plan.rows + row0) * D;
     src.Kc = Kc;
     src.Vc = Vc;
     src.tiles = mine.tiles;
     float o[4][D / 16], m[4], l[4];
-    const bool mine_to_write = simt_flash<T, D>(src, scale_log2e, reinterpret_cast<float*>(tree_smem), o, m, l);
+    const bool mine_to_write = simt_flash<T, D, SimtSmall>(src, scale_log2e, reinterpret_cast<float*>(tree_smem), o, m, l);
 #pragma unroll
     for (int i = 0; i < 4 && mine_to_write; ++i) {
       const int r = row0 + ty * 4 + i;
@@ -281,8 +283,8 @@ int launch_tree(const tca_params* prm, const void* q, const void* kd, const void
     st = launch_tree_tc(prm, q, c, plan, ws, s);
   } else {
   auto kern = tree_simt_kernel<T, D>;
-  if (allow_smem<tree_simt_kernel<T, D>>(SimtSmem<D>::kBytes) != TCA_OK) return TCA_ERR_CUDA;
-    st = launch_pdl(kern, dim3(unsigned(ctas)), dim3(kSimtThreads), size_t(SimtSmem<D>::kBytes), s,
+  if (allow_smem<tree_simt_kernel<T, D>>(SimtSmem<D, SimtSmall>::kBytes) != TCA_OK) return TCA_ERR_CUDA;
+    st = launch_pdl(kern, dim3(unsigned(ctas)), dim3(kSimtThreads), size_t(SimtSmem<D, SimtSmall>::kBytes), s,
                     static_cast<const T*>(q), static_cast<const T*>(c->k), static_cast<const T*>(c->v),
                     static_cast<const int64_t*>(c->state), U, c->tail_cap, plan, scale, ws);
   }
