@@ -376,8 +376,8 @@ int tca_cache_append(const tca_params* prm, tca_cache_desc* cache, const void* k
  *   strides    HOST [8], optional: element strides {head, row} of Q, K, V, O in that order, each at
  *              least head_dim and a multiple of 16 bytes (a token-major [rows, heads, d] buffer, or
  *              one with Q, K and V side by side).  NULL: contiguous buffers of the shapes above.
- *   ws         DEVICE workspace, tca_workspace_bytes(prm, rows, TCA_OP_PACKED); word 0 is the sticky
- *              status word
+ *   ws         DEVICE workspace, tca_workspace_bytes(prm, rows, TCA_OP_PACKED), zeroed once after
+ *              allocating; word 0 is the sticky status word.  Calls that share one must not overlap.
  * Row i's result does not depend on any other sequence, nor on what its own later rows hold (an
  * infinity or NaN there included).  O must not overlap Q, K or V.  prm->block, window and alpha are
  * not used.  TCA_FLAG_PREFILL_SIMT runs bf16 on the FP32 pipes.
