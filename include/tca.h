@@ -438,7 +438,9 @@ size_t tca_attn_tree_workspace_bytes(const tca_params* prm, int32_t n_draft);
  *   path      DEVICE [batch, n_draft] int32: drafted indices in the order of their positions; an index
  *             outside [0, n_draft) counts as the nearest one inside (the range-checked build reports it)
  *   n_accept  HOST [batch], 0 <= n_accept[s] <= n_draft; a sequence with 0 is not touched
- * TCA_ERR_CAPACITY if the global region of a unit would overflow; nothing has been changed then.
+ * TCA_ERR_CAPACITY if the global region of a unit would overflow; nothing has been changed then.  As with
+ * every call that changes the cache, the counts and the host mirror are those of the call: a captured call
+ * that is replayed moves the device state on, but not the mirror.
  */
 int tca_cache_accept(const tca_params* prm, tca_cache_desc* cache, const void* k_draft,
                      const void* v_draft, const void* q_draft, int32_t n_draft, const int32_t* path,

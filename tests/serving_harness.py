@@ -115,10 +115,22 @@ def run_tree(prm, q, kd, vd, parent, cache, n_live=None, out=None, ws=None):
     return o
 
 
-def check_tree(prm, q, kd, vd, parent, cache, got, dtype, n_live=None, heads=None):
+def check_tree_rows(prm, q, kd, vd, parent, cache, got, dtype):
+    """check_tree for a cache too large to copy: only the rows in use come to the host."""
+    class Rows:
+        def __init__(self, x):
+            self.x = x
+
+        def __getitem__(self, rows):
+            return f64(self.x[torch.from_numpy(rows).cuda()])
+
+    check_tree(prm, q, kd, vd, parent, cache, got, dtype, kv=(Rows(cache.k), Rows(cache.v)))
+
+
+def check_tree(prm, q, kd, vd, parent, cache, got, dtype, n_live=None, heads=None, kv=None):
     """Compares every (or the given) query head's rows with the oracle."""
     G, T = prm.n_q_heads // prm.n_kv_heads, q.shape[2]
-    k, v = f64(cache.k), f64(cache.v)
+    k, v = kv or (f64(cache.k), f64(cache.v))
     qd, kdd, vdd, o = f64(q), f64(kd), f64(vd), f64(got)
     for s in range(prm.batch):
         n = T if n_live is None else int(n_live[s])

@@ -44,6 +44,32 @@ def test_groups(group, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("group", [1, 3, 7, 8])
+def test_groups_of_short_heads(group, dtype):
+    """head_dim 64: a longer ring of tiles; several items per CTA."""
+    prm, q, k, v, starts = case([700, 129, 1, 0, 400, 64], group * 4, 4, 64, dtype, "tokens", 25)
+    compare(prm, q, k, v, starts, H.run_packed(prm, q, k, v, starts), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_offsets_past_32_bits(dtype):
+    """Heads more than 2^31 bytes apart: element offsets need more than 32 bits."""
+    L, d, hq, hkv = 300, 64, 4, 2
+    far = (1 << 31) // H.DT[dtype].itemsize + 4096
+
+    def spread(seed, heads):
+        buf = torch.zeros(far * (heads - 1) + L * d, dtype=H.DT[dtype], device="cuda")
+        x = buf.as_strided((heads, L, d), (far, d, 1))
+        x.copy_(H.randn(seed, (heads, L, d), dtype))
+        return x
+
+    q, k, v, o = spread(1, hq), spread(2, hkv), spread(3, hkv), spread(4, hq)
+    o.fill_(float("nan"))
+    prm, starts = H.params(2, hq, hkv, d, dtype), [0, 100, L]
+    compare(prm, q, k, v, np.array(starts), H.run_packed(prm, q, k, v, starts, out=o), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("layout", ["tokens", "fused", "odd"])
 @pytest.mark.parametrize("d", [64, 128])
 def test_layouts(layout, d, dtype):
@@ -275,6 +301,24 @@ def test_load_of_more_sequences_than_one_launch_takes():
     for i in range(batch):
         rows = torch.from_numpy(cache.unit_rows(int(slots[i]))).cuda()
         assert torch.equal(cache.k[rows], k[0, starts[i]:starts[i + 1]]) and torch.equal(cache.v[rows], v[0, starts[i]:starts[i + 1]])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_load_far_into_a_large_cache(dtype):
+    """The second sequence's rows lie more than 2^31 elements behind the first's."""
+    d, far = 128, (1 << 31) // 128 // 2 + 1000
+    prm = H.params(2, 2, 2, d, dtype, block=32, window=64)
+    cache = B.Cache(prm, np.array([far, far, 512, 512]), 96, np.full(4, 4))
+    assert int(cache.seg_start[2]) * d > 1 << 31
+    k, v = (H.randn(i, (2, 500, d), dtype) for i in (1, 2))
+    B.tca_cache_load(prm, k, v, 500, np.array([20, 500], dtype=np.int64), np.array([1], dtype=np.int32), cache)
+    torch.cuda.synchronize()
+    H.mirror_equals_device(cache)
+    for h in range(2):
+        rows = torch.from_numpy(cache.unit_rows(2 + h)).cuda()
+        assert torch.equal(cache.k[rows], k[h, 20:]) and torch.equal(cache.v[rows], v[h, 20:])
+        assert torch.equal(cache.pos[rows], torch.arange(480, dtype=torch.int32, device="cuda"))
+    assert not cache.k[:1000].any() and not cache.k[-1].any()
 
 
 def test_load_refuses_without_touching_anything():

@@ -152,6 +152,43 @@ def test_a_captured_call_replays_over_a_cache_that_has_grown(dtype):
             H.check_tree(prm, q, kd, vd, parent, cache, o, dtype)
 
 
+@pytest.mark.parametrize("T", [3, 40, 128])
+def test_tensor_cores_agree_with_the_fp32_pipes(T):
+    cache_of = lambda p: H.make_cache(p, [700, 130], [90, 64], 40, 900, "bf16", 19)  # noqa: E731
+    prm, simt = H.params(1, 8, 2, 128, "bf16"), H.params(1, 8, 2, 128, "bf16", flags=B.TCA_FLAG_PREFILL_SIMT)
+    cache = cache_of(prm)
+    q, kd, vd = drafts(prm, T, "bf16", 160)
+    parent = H.bush(T, 1)[None]
+    for p in (prm, simt):
+        H.check_tree(p, q, kd, vd, parent, cache, H.run_tree(p, q, kd, vd, parent, cache), "bf16", heads=(0, 5))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_far_into_a_large_cache(dtype):
+    """A unit whose rows lie more than 2^31 elements into the cache: attended to, and appended to."""
+    d, far, T = 128, (1 << 31) // 128 + 1000, 6
+    prm = H.params(2, 2, 1, d, dtype, block=32, window=64)
+    cache = B.Cache(prm, np.array([far, 256]), 96, np.full(2, 8), init=False)
+    cache.n_global[:], cache.n_tail[:], cache.tail_head[:], cache.seq_len[:] = [0, 200], [3, 94], [0, 50], [3, 400]
+    B.tca_cache_init(prm, cache)
+    for u in range(2):
+        rows = torch.from_numpy(cache.unit_rows(u)).cuda()
+        cache.k[rows], cache.v[rows] = H.randn(u, (len(rows), d), dtype), H.randn(9 + u, (len(rows), d), dtype)
+        cache.pos[rows] = torch.arange(len(rows), dtype=torch.int32, device="cuda")
+    q, kd, vd = drafts(prm, T, dtype, 170)
+    parent = np.stack([H.chain(T), H.bush(T, 4)])
+    H.check_tree_rows(prm, q, kd, vd, parent, cache, H.run_tree(prm, q, kd, vd, parent, cache), dtype)
+    path = torch.arange(T, dtype=torch.int32, device="cuda").repeat(2, 1)
+    ng, nt, sl = int(cache.n_global[1]), int(cache.n_tail[1]), int(cache.seq_len[1])
+    B.tca_cache_accept(prm, cache, kd, vd, q, T, path, np.array([2, T], dtype=np.int32))      # the second compresses
+    torch.cuda.synchronize()
+    H.mirror_equals_device(cache)
+    assert (cache.n_global[1], cache.n_tail[1], cache.seq_len[1]) == (ng + 8, nt + T - 32, sl + T)
+    rows = torch.from_numpy(cache.unit_rows(1)).cuda()[-T:]
+    assert torch.equal(cache.k[rows], kd[1, 0]) and torch.equal(cache.v[rows], vd[1, 0])
+    assert cache.pos[rows].tolist() == list(range(sl, sl + T))
+
+
 def test_a_set_status_word_stops_the_call():
     prm = H.params(1, 4, 2, 128, "bf16")
     cache = H.make_cache(prm, 200, 90, 0, 300, "bf16", 17)
