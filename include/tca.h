@@ -8,8 +8,8 @@
  *     cache, workspace) are allocated and freed by the caller; the library calls no
  *     allocator.  What it keeps between calls is limited to: the built-in scratch array of
  *     tca_attn_decode_static (and its per-device address), a small cache of encoded TMA
- *     tensor maps keyed by buffer address and shape, and per-device constants (SM count,
- *     L2 cache size).  The bf16 decode kernel asks the L2 to keep part of the cache it reads
+ *     tensor maps keyed by buffer address and shape, per-device constants (SM count, L2 cache
+ *     size), and which kernels have been granted their shared memory on which device.  The bf16 decode kernel asks the L2 to keep part of the cache it reads
  *     (eviction-priority hints on its loads; nothing is set on the device or the context).
  *   - Tensors are row-major with the head dimension contiguous:
  *       Q [batch, n_q_heads, L, head_dim]      K, V [batch, n_kv_heads, L, head_dim]
@@ -58,8 +58,8 @@ enum { TCA_F32 = 0, TCA_BF16 = 1 };
 
 /* tca_params.flags */
 enum {
-  /* run the prefill on the FP32 pipes even for bf16 inputs (the slow reference kernel the
-   * tensor-core kernel is cross-checked against) */
+  /* run the prefill, tca_attn_packed and tca_attn_tree on the FP32 pipes even for bf16 inputs (the
+   * slow reference kernels the tensor-core kernels are cross-checked against) */
   TCA_FLAG_PREFILL_SIMT = 1,
   /* Selection variants of the paper's ablations (appendix "Ablations on Concentration Index" and
    * "Effectiveness of Local-context Redundancy Metric") and a flat top-B; at most one of the three.

