@@ -504,12 +504,15 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
       const int row_key = src.row_key(h);
       float m_run = -INFINITY, m_used = -INFINITY, l = 0.f;
       bool ok = true;
-      // lazy rescale of the accumulator to a maximum that grew by more than 2^8 (warp-uniform: TMEM access
-      // is warp-wide)
+      // lazy rescale of the accumulator to a maximum that grew by more than 2^8.  TMEM access is warp-wide, so
+      // the warp votes; but a row whose own maximum did not grow that far keeps its scale (times one is exact):
+      // otherwise its rounding would follow its neighbours' scores, and those may be another sequence's or
+      // rows of the tile that hold no query at all
       auto rescale = [&](float mx, bool started) {
         m_run = fmaxf(m_run, mx * scale_log2e);
-        if (__any_sync(0xffffffffu, m_run > m_used + kTcRescale)) {
-          const float alpha = (m_used == -INFINITY) ? 0.f : ptx::fast_exp2(m_used - m_run);
+        const bool grew = m_run > m_used + kTcRescale;
+        if (__any_sync(0xffffffffu, grew)) {
+          const float alpha = !grew ? 1.f : m_used == -INFINITY ? 0.f : ptx::fast_exp2(m_used - m_run);
           if (started) {
 #pragma unroll 1
             for (int c = 0; c < D / 32; ++c) {
@@ -523,7 +526,7 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
             ptx::tc_wait_st();
           }
           l *= alpha;
-          m_used = m_run;
+          if (grew) m_used = m_run;
         }
       };
       auto announce = [&](int part) {

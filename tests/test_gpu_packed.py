@@ -134,6 +134,28 @@ def test_two_runs_and_another_stream_agree_bit_for_bit(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("group", [1, 3, 5, 7, 8])
+def test_a_row_rounds_the_same_whatever_shares_its_tile(group, dtype):
+    """Bit for bit: a sequence's rows while the other sequences' queries, its own later queries, and the calls
+    before (whose queries stay in shared memory behind a group's last whole position) hold large ones."""
+    lens = [219, 29, 2, 140, 311, 5, 90]
+    prm, q, k, v, starts = case(lens, 2 * group, 2, 128, dtype, "heads", 65)
+    q *= 3
+    first = H.run_packed(prm, q, k, v, starts)
+    for i, n in enumerate(lens):
+        lo, hi = int(starts[i]), int(starts[i + 1])
+        loud = q * 50
+        H.run_packed(prm, loud, k, v, starts)
+        keep = lo + (n + 1) // 2
+        loud[:, lo:keep] = q[:, lo:keep]
+        got = H.run_packed(prm, loud, k, v, starts)
+        assert torch.equal(got[:, lo:keep], first[:, lo:keep]), i
+        loud[:, lo:hi] = q[:, lo:hi]
+        got = H.run_packed(prm, loud, k, v, starts)
+        assert torch.equal(got[:, lo:hi], first[:, lo:hi]), i
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_a_captured_call_replays_with_other_lengths(dtype):
     prm, q, k, v, starts = case([100, 50, 250], 4, 2, 128, dtype, "heads", 70)
     st = torch.tensor(starts, dtype=torch.int64, device="cuda")

@@ -102,6 +102,25 @@ def test_what_a_row_does_not_see_has_no_influence(bad, dtype):
     assert not torch.isfinite(got[1][:, [3, 5, 8]].float()).any()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("group", [1, 3, 5, 7, 8])
+def test_a_drafted_token_rounds_the_same_whatever_shares_its_tile(group, dtype):
+    """Bit for bit, while the other drafted tokens, those past n_live and the calls before hold large queries."""
+    prm = H.params(2, 2 * group, 2, 128, dtype)
+    cache = H.make_cache(prm, [700, 90, 260, 1500], [90, 30, 96, 20], [50, 0, 20, 90], 2000, dtype, 12)
+    T, live = 21, np.array([21, 13])
+    q, kd, vd = drafts(prm, T, dtype, 64)
+    q *= 3
+    parent = np.stack([H.bush(T, 3), H.chain(T)])
+    first = H.run_tree(prm, q, kd, vd, parent, cache, n_live=live)
+    for quiet in ([0], [1, 2, 7], list(range(10)), list(range(13))):
+        loud = q * 50
+        H.run_tree(prm, loud, kd, vd, parent, cache)
+        loud[:, :, quiet] = q[:, :, quiet]
+        got = H.run_tree(prm, loud, kd, vd, parent, cache, n_live=live)
+        assert torch.equal(got[:, :, quiet], first[:, :, quiet])
+
+
 def test_parents_that_do_not_precede_their_child_count_as_roots():
     prm = H.params(1, 2, 1, 64, "bf16")
     cache = H.make_cache(prm, 20, 30, 0, 50, "bf16", 9)
