@@ -248,7 +248,9 @@ tree_combine_kernel(const T* __restrict__ q, const T* __restrict__ k_draft, cons
     for (int off = 16; off > 0; off >>= 1) mn = fmaxf(mn, __shfl_xor_sync(0xffffffffu, mn, off));
     mn = fmaxf(m, mn);
     const float base = (mn == -INFINITY) ? 0.f : mn, keep = exp2f(m - base);
-    const bool some = ml.x != -INFINITY;                     // a stream without a tile wrote no output
+    // a stream without a tile wrote no output (maximum -inf, sum 0); one whose scores are all NaN has no maximum
+    // either, but a sum that is NaN and has to reach the result
+    const bool some = ml.x != -INFINITY || ml.y != 0.f;
     const float w = some ? exp2f(ml.x - base) : 0.f;
     const unsigned have = __ballot_sync(0xffffffffu, some);
     l *= keep;
@@ -284,8 +286,8 @@ int launch_tree(const tca_params* prm, const void* q, const void* kd, const void
   if (tree_on_tensor_cores(prm)) {
     st = launch_tree_tc(prm, q, c, plan, ws, s);
   } else {
-  auto kern = tree_simt_kernel<T, D>;
-  if (allow_smem<tree_simt_kernel<T, D>>(SimtSmem<D, SimtSmall>::kBytes) != TCA_OK) return TCA_ERR_CUDA;
+    auto kern = tree_simt_kernel<T, D>;
+    if (allow_smem<tree_simt_kernel<T, D>>(SimtSmem<D, SimtSmall>::kBytes) != TCA_OK) return TCA_ERR_CUDA;
     st = launch_pdl(kern, dim3(unsigned(ctas)), dim3(kSimtThreads), size_t(SimtSmem<D, SimtSmall>::kBytes), s,
                     static_cast<const T*>(q), static_cast<const T*>(c->k), static_cast<const T*>(c->v),
                     static_cast<const int64_t*>(c->state), U, c->tail_cap, plan, scale, ws);

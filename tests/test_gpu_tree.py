@@ -121,6 +121,23 @@ def test_a_drafted_token_rounds_the_same_whatever_shares_its_tile(group, dtype):
         assert torch.equal(got[:, :, quiet], first[:, :, quiet])
 
 
+@pytest.mark.parametrize("flags", [0, B.TCA_FLAG_PREFILL_SIMT])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [2, 70])
+def test_nan_keys_that_are_seen_show(T, dtype, flags):
+    """A unit whose cached keys are all NaN (so that no partial result has a maximum), and one with a single NaN."""
+    prm = H.params(1, 6, 3, 128, dtype, flags=flags)
+    cache = H.make_cache(prm, [700, 300, 2], [0, 50, 1], 0, 900, dtype, 13)
+    q, kd, vd = drafts(prm, T, dtype, 67)
+    parent = H.chain(T)[None]
+    clean = H.run_tree(prm, q, kd, vd, parent, cache)
+    cache.k[torch.from_numpy(cache.unit_rows(0)).cuda()] = float("nan")
+    cache.k[int(cache.unit_rows(2)[1]), 7] = float("nan")
+    got = H.run_tree(prm, q, kd, vd, parent, cache)
+    assert torch.isnan(got[:, [0, 1, 4, 5]]).all()
+    assert torch.equal(got[:, 2:4], clean[:, 2:4])
+
+
 def test_parents_that_do_not_precede_their_child_count_as_roots():
     prm = H.params(1, 2, 1, 64, "bf16")
     cache = H.make_cache(prm, 20, 30, 0, 50, "bf16", 9)
