@@ -370,6 +370,7 @@ int tca_cache_append(const tca_params* prm, tca_cache_desc* cache, const void* k
  * [seq_start[s], seq_start[s+1]) of every buffer and its row i attends to its rows j <= i.
  *   Q, O       DEVICE [n_q_heads, rows, head_dim]     K, V  DEVICE [n_kv_heads, rows, head_dim]
  *   rows       rows of every buffer; rows that belong to no sequence are neither computed nor written
+ *              (0: nothing is done, and the buffers may be null)
  *   seq_start  DEVICE [batch + 1] int64, ascending, within [0, rows]; a sequence may be empty.  Read
  *              on the device only, so a captured call may be replayed with other lengths.  Values
  *              outside [0, rows] are clamped; sequences that overlap give unspecified rows of O.
@@ -396,6 +397,7 @@ int tca_attn_packed(const tca_params* prm, const void* Q, const void* K, const v
  *   strides    HOST [4], optional: element strides {head, row} of K and V as in tca_attn_packed
  *   seq_start  HOST [n_seq + 1], ascending, within [0, rows]
  *   slots      HOST [n_seq], optional (NULL: sequence i goes to i): distinct cache sequences
+ * With rows = 0 K and V may be null: prompts without a token, whose places become empty.
  * TCA_ERR_CAPACITY if a prompt's m*block exceeds its units' global_cap or the rest exceeds tail_cap.
  */
 int tca_cache_load(const tca_params* prm, const void* K, const void* V, int64_t rows,

@@ -95,7 +95,7 @@ extern "C" int tca_cache_load(const tca_params* prm, const void* K, const void* 
                               void* stream) {
   int st = check_params(prm);
   if (st != TCA_OK) return st;
-  TCA_CHECK_ARG(K && V && seq_start && c);
+  TCA_CHECK_ARG(((K && V) || rows == 0) && seq_start && c);   // no rows: nothing that K and V would point at
   TCA_CHECK_ARG(c->k && c->v && c->pos && c->state && c->seg_start && c->global_cap && c->n_global && c->tail_head &&
                 c->n_tail && c->seq_len);
   TCA_CHECK_ARG(rows >= 0 && rows < (int64_t(1) << 31) && n_seq >= 0 && n_seq <= prm->batch);
@@ -111,14 +111,23 @@ extern "C" int tca_cache_load(const tca_params* prm, const void* K, const void* 
   auto blocks_of = [&](int64_t len) { return num_blocks(prm, len) * prm->block; };
   // everything is checked before anything is launched or any mirror changes
   for (int i = 0; i < n_seq; ++i) {
-    const int64_t len = seq_start[i + 1] - seq_start[i];
-    TCA_CHECK_ARG(seq_start[i] >= 0 && len >= 0 && seq_start[i + 1] <= rows);
+    TCA_CHECK_ARG(seq_start[i] >= 0 && seq_start[i + 1] >= seq_start[i] && seq_start[i + 1] <= rows);
     const int64_t slot = slots ? slots[i] : i;
     TCA_CHECK_ARG(slot >= 0 && slot < prm->batch);
-    for (int j = 0; j < i && slots; ++j) TCA_CHECK_ARG(slots[j] != slots[i]);   // two prompts cannot share a place
-    const int64_t ng = blocks_of(len);
+    const int64_t len = seq_start[i + 1] - seq_start[i], ng = blocks_of(len);
     for (int h = 0; h < H; ++h)
       if (ng > c->global_cap[slot * H + h] || len - ng > c->tail_cap) return TCA_ERR_CAPACITY;
+  }
+  // two prompts cannot share a place: a bit per place, so many places at a time
+  constexpr int kPlaces = 8192;
+  for (int64_t p0 = 0; slots && p0 < prm->batch; p0 += kPlaces) {
+    uint32_t taken[kPlaces / 32] = {};
+    for (int i = 0; i < n_seq; ++i) {
+      const int64_t p = slots[i] - p0;
+      if (p < 0 || p >= kPlaces) continue;
+      TCA_CHECK_ARG(!(taken[p / 32] >> (p % 32) & 1u));
+      taken[p / 32] |= 1u << (p % 32);
+    }
   }
   const int pieces = int(prm->head_dim * elt_size(prm->dtype) / 16);
   int shift = 0;

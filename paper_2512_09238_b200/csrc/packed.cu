@@ -122,7 +122,7 @@ extern "C" int tca_attn_packed(const tca_params* prm, const void* Q, const void*
                                void* stream) {
   int st = check_params(prm);
   if (st != TCA_OK) return st;
-  TCA_CHECK_ARG(Q && K && V && seq_start && O && ws);
+  TCA_CHECK_ARG(((Q && K && V && O) || rows == 0) && seq_start && ws);   // no rows: nothing that they would point at
   TCA_CHECK_ARG(rows >= 0 && rows < (int64_t(1) << 31));
   TCA_CHECK_ARG(aligned(Q, 16) && aligned(K, 16) && aligned(V, 16) && aligned(O, 16) && aligned(ws, 256));
   TCA_CHECK_ARG(aligned(seq_start, 8));

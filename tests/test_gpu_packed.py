@@ -361,3 +361,17 @@ def test_load_refuses_without_touching_anything():
     for n in ("k", "v", "pos", "state"):
         assert torch.equal(getattr(cache, n), getattr(before, n))
     H.mirror_equals_device(cache)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_batch_without_a_token(dtype):
+    prm = H.params(3, 4, 2, 64, dtype)
+    cache = H.make_cache(prm, 10, 20, 3, 30, dtype, 95)
+    q, k = H.randn(1, (4, 0, 64), dtype), H.randn(2, (2, 0, 64), dtype)
+    assert H.run_packed(prm, q, k, k, [0, 0, 0, 0]).numel() == 0
+    before = cache.state.clone()
+    B.tca_cache_load(prm, k, k, 0, np.zeros(2, dtype=np.int64), np.array([1], dtype=np.int32), cache)
+    after = cache.state.view(6, -1).cpu().numpy()
+    assert list(cache.n_tail) == [20, 20, 0, 0, 20, 20] and list(cache.n_global) == [10, 10, 0, 0, 10, 10]
+    assert np.array_equal(after[[0, 1, 4, 5]], before.view(6, -1).cpu().numpy()[[0, 1, 4, 5]])
+    H.mirror_equals_device(cache)

@@ -66,6 +66,31 @@ def test_load_refusals():
     assert load(n=0) == B.TCA_OK
 
 
+def test_no_rows_need_no_buffers():
+    assert packed(prm(), q=None, k=None, v=None, o=None, rows=0) == B.TCA_OK
+    assert packed(prm(), q=None, k=None, v=None, o=None, rows=0, start=None) == B.TCA_ERR_INVALID_ARG
+    d, one = desc(), (C.c_int64 * 1)(0)
+    assert B.lib().tca_cache_load(C.byref(prm()), None, None, 0, None, one, None, 0, C.byref(d), None) == B.TCA_OK
+    assert B.lib().tca_cache_load(C.byref(prm()), None, None, 1, None, one, None, 0, C.byref(d), None) == B.TCA_ERR_INVALID_ARG
+
+
+def test_load_finds_a_place_taken_twice_among_many():
+    n = 20000
+    d = desc(n_units=n, tail_cap=96)
+    starts = np.arange(n + 1, dtype=np.int64)
+    for a, b in ((0, n - 1), (8191, 8192), (8192, 8193), (16384, 3)):
+        slots = np.arange(n, dtype=np.int32)[::-1].copy()
+        slots[a] = slots[b]
+        assert B.lib().tca_cache_load(C.byref(prm(batch=n, n_q_heads=1, n_kv_heads=1)), A, A, n, None, starts.ctypes.data,
+                                      slots.ctypes.data, n, C.byref(d), None) == B.TCA_ERR_INVALID_ARG
+
+
+def test_load_refuses_starts_that_would_overflow():
+    d = desc()
+    starts = (C.c_int64 * 2)(1 << 62, -(1 << 62) - 1)
+    assert B.lib().tca_cache_load(C.byref(prm()), A, A, 100, None, starts, None, 1, C.byref(d), None) == B.TCA_ERR_INVALID_ARG
+
+
 def test_tree_refusals():
     def tree(p=None, q=A, kd=A, T=8, parent=A, live=None, d=None, o=A, ws=A, n=1 << 30):
         d = desc() if d is None else d
