@@ -337,6 +337,17 @@ def _view(t, here, dtype, shape, out: list) -> bool:
     return last == 1 or rows == 0
 
 
+def _fits(cache: "Cache", here, dtype, d) -> bool:
+    """The cache lies on device `here` and was made for this type and head size."""
+    return cache.k.dtype is dtype and cache.k.shape[1] == d and cache.k.get_device() == here
+
+
+def _refuse_cache(where: str, prm, cache: "Cache", *specs) -> None:
+    if not _fits(cache, torch.cuda.current_device() if torch.cuda.is_available() else -2, _ELT[prm.dtype], prm.head_dim):
+        raise ValueError(f"{where}: the cache must be on the current CUDA device and made for {_ELT[prm.dtype]} and head size {prm.head_dim}")
+    _refuse(where, *specs)
+
+
 def tca_attn_packed(prm, Q, K, V, rows, seq_start, O, ws, stream=None) -> None:
     """Q, O [n_q_heads, rows, d], K, V [n_kv_heads, rows, d]: contiguous, or views with any head and row strides
     that are multiples of 16 bytes (``x.transpose(0, 1)`` of a token-major tensor); seq_start a CUDA int64 tensor
@@ -355,8 +366,9 @@ def tca_attn_packed(prm, Q, K, V, rows, seq_start, O, ws, stream=None) -> None:
 def tca_cache_load(prm, K, V, rows, seq_start, slots, cache: "Cache", stream=None) -> None:
     """K, V [n_kv_heads, rows, d] as in tca_attn_packed; seq_start an int64 and slots an int32 numpy array (or None)."""
     e, here, st, ks = _ELT[prm.dtype], K.get_device(), [], (prm.n_kv_heads, rows, prm.head_dim)
-    if not (here >= 0 and here == torch.cuda.current_device() and _view(K, here, e, ks, st) and _view(V, here, e, ks, st)):
-        _refuse("tca_cache_load", ("K", K, e, ks, False), ("V", V, e, ks, False))
+    if not (here >= 0 and here == torch.cuda.current_device() and _view(K, here, e, ks, st) and _view(V, here, e, ks, st)
+            and _fits(cache, here, e, prm.head_dim)):
+        _refuse_cache("tca_cache_load", prm, cache, ("K", K, e, ks, False), ("V", V, e, ks, False))
     n_seq = len(seq_start) - 1
     if slots is not None and len(slots) != n_seq:
         raise ValueError("tca_cache_load: slots must have one entry per sequence")
@@ -381,8 +393,8 @@ def tca_attn_tree(prm, q, k_draft, v_draft, n_draft, parent, n_live, cache: "Cac
     qs, ks, ps = (B, prm.n_q_heads, n_draft, d), (B, prm.n_kv_heads, n_draft, d), (B, n_draft)
     if not (here >= 0 and here == torch.cuda.current_device() and _ok(q, here, e, qs) and _ok(k_draft, here, e, ks)
             and _ok(v_draft, here, e, ks) and _ok(O, here, e, qs) and _ok(parent, here, _I32, ps)
-            and _ok(n_live, here, _I32, (B,)) and _ok(ws, here, _U8, ws.shape)):
-        _refuse("tca_attn_tree", ("q", q, e, qs, True), ("k_draft", k_draft, e, ks, True), ("v_draft", v_draft, e, ks, True),
+            and _ok(n_live, here, _I32, (B,)) and _ok(ws, here, _U8, ws.shape) and _fits(cache, here, e, d)):
+        _refuse_cache("tca_attn_tree", prm, cache, ("q", q, e, qs, True), ("k_draft", k_draft, e, ks, True), ("v_draft", v_draft, e, ks, True),
                 ("O", O, e, qs, True), ("parent", parent, _I32, ps, True), ("n_live", n_live, _I32, (B,), True),
                 ("ws", ws, _U8, None, True))
     _check(lib().tca_attn_tree(C.byref(prm), q.data_ptr(), k_draft.data_ptr(), v_draft.data_ptr(), n_draft, parent.data_ptr(),
@@ -395,8 +407,8 @@ def tca_cache_accept(prm, cache: "Cache", k_draft, v_draft, q_draft, n_draft, pa
     e, B, d, here = _ELT[prm.dtype], prm.batch, prm.head_dim, k_draft.get_device()
     qs, ks, ps = (B, prm.n_q_heads, n_draft, d), (B, prm.n_kv_heads, n_draft, d), (B, n_draft)
     if not (here >= 0 and here == torch.cuda.current_device() and _ok(k_draft, here, e, ks) and _ok(v_draft, here, e, ks)
-            and _ok(q_draft, here, e, qs) and _ok(path, here, _I32, ps)):
-        _refuse("tca_cache_accept", ("k_draft", k_draft, e, ks, True), ("v_draft", v_draft, e, ks, True),
+            and _ok(q_draft, here, e, qs) and _ok(path, here, _I32, ps) and _fits(cache, here, e, d)):
+        _refuse_cache("tca_cache_accept", prm, cache, ("k_draft", k_draft, e, ks, True), ("v_draft", v_draft, e, ks, True),
                 ("q_draft", q_draft, e, qs, True), ("path", path, _I32, ps, True))
     if len(n_accept) != B:
         raise ValueError("tca_cache_accept: n_accept must have one entry per sequence")

@@ -388,3 +388,22 @@ def test_the_binding_refuses_wrong_tensors():
     with pytest.raises(ValueError):
         B.tca_cache_load(prm, x.cpu(), x, 10, np.array([0, 10]), None, cache)
     torch.cuda.synchronize()
+
+
+def test_the_binding_refuses_a_cache_made_for_something_else():
+    prm = H.params(2, 4, 2, 64, "bf16")
+    q, kd, vd = drafts(prm, 4, "bf16", 131)
+    par, n = torch.zeros(2, 4, dtype=torch.int32, device="cuda"), np.ones(2, dtype=np.int32)
+    ws, x = B.alloc_tree_workspace(prm, 4), H.randn(1, (2, 10, 64), "bf16")
+    elsewhere = B.Cache(prm, np.full(4, 20), 96, np.full(4, 4), device="cpu", init=False)
+    for cache in (H.make_cache(H.params(2, 4, 2, 64, "f32"), 5, 5, 0, 20, "f32", 17),
+                  H.make_cache(H.params(2, 4, 2, 128, "bf16"), 5, 5, 0, 20, "bf16", 17), elsewhere):
+        was = cache.k.clone()
+        with pytest.raises(ValueError, match="cache"):
+            B.tca_attn_tree(prm, q, kd, vd, 4, par, None, cache, torch.zeros_like(q), ws)
+        with pytest.raises(ValueError, match="cache"):
+            B.tca_cache_accept(prm, cache, kd, vd, q, 4, par, n)
+        with pytest.raises(ValueError, match="cache"):
+            B.tca_cache_load(prm, x, x, 10, np.array([0, 5, 10]), None, cache)
+        assert torch.equal(cache.k, was)
+    torch.cuda.synchronize()
