@@ -3,16 +3,20 @@
 // Stage"), compression of the blocks that leave the window included.  One CTA per unit.  The tokens up to
 // the next compression are written together; a compression scores its block with the queries of the token
 // that filled the ring, as appending that token would.  Without a compression a call is one launch of 3 us;
-// 512 units of which 200 compress take 24 us, bound by the fp64 products of the compression.
+// 512 units of which 200 compress take 14 us, bound by the latencies of a compression (its steps take turns: scores
+// 4 us, softmax and ranks 3, everything around them 4).
 #include "compress.cuh"
 
 namespace tca {
 namespace {
 
 // Accepted counts travel as kernel arguments: the host needs them for its mirror anyway.
-constexpr int kSeqPerLaunch = 2048;
+// The sequences that compress come first: a CTA that does runs seven times as long as one that does not, and not
+// all CTAs are resident at once (17 -> 15.5 us for 512 units).  Those that accept nothing have no CTA.
+constexpr int kSeqPerLaunch = 1024;
 struct AcceptCounts {
-  uint8_t n[kSeqPerLaunch];   // 0 .. TCA_TREE_MAX
+  uint8_t n[kSeqPerLaunch];      // 1 .. TCA_TREE_MAX
+  uint16_t seq[kSeqPerLaunch];   // which of the launch's sequences
 };
 
 template <typename T>
@@ -23,11 +27,10 @@ cache_accept_kernel(const T* __restrict__ k_draft, const T* __restrict__ v_draft
                     int64_t tail_cap, int D, int G, int n_kv, int b, int window, double sm_scale) {
   pdl_wait();
   pdl_launch_dependents();
-  const int local = int(blockIdx.x) / n_kv;
-  const int n = counts.n[local];
-  if (n == 0) return;
+  const int nth = int(blockIdx.x) / n_kv, seq = seq0 + counts.seq[nth];
+  const int n = counts.n[nth];
   const int tid = threadIdx.x;
-  const int64_t u = int64_t(seq0) * n_kv + blockIdx.x;
+  const int64_t u = int64_t(seq) * n_kv + int(blockIdx.x) % n_kv;
   int64_t* st = state + u * TCA_STATE_WORDS;
   __shared__ int s_path[TCA_TREE_MAX];
   const int64_t seg = st[TCA_ST_SEG_START], gcap = st[TCA_ST_GLOBAL_CAP];
@@ -36,7 +39,7 @@ cache_accept_kernel(const T* __restrict__ k_draft, const T* __restrict__ v_draft
   const int t_keep = int(st[TCA_ST_T_KEEP]);
   const int64_t ring = seg + gcap;
   if (tid < n) {
-    int t = path[int64_t(seq0 + local) * n_draft + tid];
+    int t = path[int64_t(seq) * n_draft + tid];
     if constexpr (kDebugBounds) {
       if (t < 0 || t >= n_draft) report_bounds_state(st, kBoundsDraftIndex, t);
     }
@@ -53,13 +56,14 @@ cache_accept_kernel(const T* __restrict__ k_draft, const T* __restrict__ v_draft
       return;
     }
   }
-  const int pieces = D * int(sizeof(T)) / 16;   // 16-byte pieces per row: a power of two
+  const int shift = 31 - __clz(D * int(sizeof(T)) / 16);   // 16-byte pieces per row: a power of two
   for (int i0 = 0; i0 < n;) {
     const int cnt = int(min(int64_t(n - i0), full - n_tail));   // >= 1: the ring never stays full
-    for (int i = tid; i < cnt * pieces; i += kCompressThreads) {
-      const int j = i / pieces, e = i - j * pieces;
-      const int64_t slot = (tail_head + n_tail + j) % tail_cap;
-      const int64_t src = (u * n_draft + s_path[i0 + j]) * pieces + e, dst = (ring + slot) * pieces + e;
+    for (int i = tid; i < cnt << shift; i += kCompressThreads) {
+      const int j = i >> shift, e = i & ((1 << shift) - 1);
+      int64_t slot = tail_head + n_tail + j;   // < 2 tail_cap: the ring has room for a full one
+      if (slot >= tail_cap) slot -= tail_cap;
+      const int64_t src = ((u * n_draft + s_path[i0 + j]) << shift) + e, dst = ((ring + slot) << shift) + e;
       reinterpret_cast<uint4*>(Kc)[dst] = reinterpret_cast<const uint4*>(k_draft)[src];
       reinterpret_cast<uint4*>(Vc)[dst] = reinterpret_cast<const uint4*>(v_draft)[src];
       if (e == 0) pos[ring + slot] = int32_t(seq_len + i0 + j);
@@ -72,7 +76,8 @@ cache_accept_kernel(const T* __restrict__ k_draft, const T* __restrict__ v_draft
                             n_global, tail_head, tail_cap, t_keep, D, G, b, sm_scale);
       __syncthreads();   // the moved rows have been read: their slots may be written again
       n_global += t_keep;
-      tail_head = (tail_head + b) % tail_cap;
+      tail_head += b;
+      if (tail_head >= tail_cap) tail_head -= tail_cap;
       n_tail -= b;
     }
   }
@@ -132,16 +137,19 @@ extern "C" int tca_cache_accept(const tca_params* prm, tca_cache_desc* c, const 
   for (int32_t s0 = 0; s0 < prm->batch; s0 += kSeqPerLaunch) {
     AcceptCounts counts;
     const int n_seq = prm->batch - s0 < kSeqPerLaunch ? prm->batch - s0 : kSeqPerLaunch;
-    int most = 0;
-    for (int i = 0; i < n_seq; ++i) {
-      counts.n[i] = uint8_t(n_accept[s0 + i]);
-      most = n_accept[s0 + i] > most ? n_accept[s0 + i] : most;
-    }
-    if (most == 0) continue;
+    int listed = 0;
+    for (int pass = 0; pass < 2; ++pass)
+      for (int i = 0; i < n_seq; ++i) {
+        const int32_t n = n_accept[s0 + i];
+        if (n == 0 || (compressions(int64_t(s0 + i) * H, n) > 0) != (pass == 0)) continue;
+        counts.n[listed] = uint8_t(n);
+        counts.seq[listed++] = uint16_t(i);
+      }
+    if (listed == 0) continue;
     cudaStream_t str = static_cast<cudaStream_t>(stream);
     st = prm->dtype == TCA_BF16
-             ? launch_accept<__nv_bfloat16>(prm, c, k_draft, v_draft, q_draft, n_draft, path, counts, s0, n_seq, str)
-             : launch_accept<float>(prm, c, k_draft, v_draft, q_draft, n_draft, path, counts, s0, n_seq, str);
+             ? launch_accept<__nv_bfloat16>(prm, c, k_draft, v_draft, q_draft, n_draft, path, counts, s0, listed, str)
+             : launch_accept<float>(prm, c, k_draft, v_draft, q_draft, n_draft, path, counts, s0, listed, str);
     if (st != TCA_OK) return st;
     for (int i = 0; i < n_seq; ++i) {
       const int64_t n = n_accept[s0 + i];

@@ -284,6 +284,60 @@ def test_accept_equals_one_append_per_token(block, window, n_tail, T, dtype):
             B.tca_cache_append(prm, ref, pick(kd), pick(vd), pick(q))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("group", [1, 2, 3, 4, 5, 8])
+@pytest.mark.parametrize("block,t_keep", [(1, 1), (2, 1), (8, 3), (32, 31), (64, 20), (128, 41), (128, 128)])
+def test_a_block_that_leaves_keeps_what_the_formula_says(block, t_keep, group, d, dtype):
+    """The kept positions against fp64, for keys that are all different, repeated (equal scores go to the earlier
+    position) and all the same."""
+    hkv, window = 3, 5
+    prm = H.params(1, group * hkv, hkv, d, dtype, block=block, window=window)
+    full = window + block
+    cache = H.make_cache(prm, 9, full - 1, full // 3, 500, dtype, 18, t_keep=t_keep, extra_cap=t_keep + 2)
+    q, kd, vd = drafts(prm, 2, dtype, 140)
+    rows = [cache.unit_rows(u)[9:9 + min(block, full - 1)] for u in range(hkv)]
+    r = np.random.default_rng(block + group)
+    cache.k[torch.from_numpy(rows[1]).cuda()] = cache.k[torch.from_numpy(r.choice(rows[1][:5], len(rows[1]))).cuda()]
+    cache.k[torch.from_numpy(rows[2]).cuda()] = cache.k[int(rows[2][0])].clone()
+    keys, first = [H.f64(cache.k[torch.from_numpy(x).cuda()]) for x in rows], 500 - (full - 1)
+    B.tca_cache_accept(prm, cache, kd, vd, q, 2, torch.ones(1, 2, dtype=torch.int32, device="cuda"), np.array([1], dtype=np.int32))
+    H.mirror_equals_device(cache)
+    pos, kk = cache.pos.cpu().numpy(), H.f64(cache.k)
+    for u in range(hkv):
+        x = H.f64(q)[0, u * group:(u + 1) * group, 1] @ keys[u].T * H.scale_of(d)
+        score = np.log(np.mean(np.exp(x - np.log(np.exp(x - x.max(1, keepdims=True)).sum(1, keepdims=True)) - x.max(1, keepdims=True)), axis=0))
+        # equal keys have equal scores; different ones differ by far more than fp64 rounds
+        kept = np.sort(np.lexsort((np.arange(len(score)), -np.round(score, 9)))[:t_keep])
+        lo = int(cache.seg_start[u]) + 9
+        assert np.array_equal(pos[lo:lo + t_keep], first + kept), u
+        assert np.array_equal(kk[lo:lo + t_keep], keys[u][kept]), u
+
+
+def test_accept_of_more_sequences_than_one_launch_takes():
+    batch, T = 1500, 2
+    prm = H.params(batch, 1, 1, 64, "bf16", block=8, window=8)
+    r = np.random.default_rng(3)
+    cache = H.make_cache(prm, 4, 0, 0, 40, "bf16", 19, t_keep=2, extra_cap=4, tail_cap=17)
+    cache.n_tail[:] = r.integers(3, 16, batch)
+    cache.seq_len[:] = 30 + cache.n_tail
+    B.tca_cache_init(prm, cache)
+    q, kd, vd = drafts(prm, T, "bf16", 150)
+    n = (r.random(batch) < 0.6).astype(np.int32)
+    n[1020:1030] = 1
+    path = r.integers(0, T, (batch, T)).astype(np.int32)
+    before, ref = H.clone_cache(prm, cache), H.clone_cache(prm, cache)
+    pick = lambda x: x[torch.arange(batch), :, torch.from_numpy(path[:, 0]).long()].contiguous()  # noqa: E731
+    B.tca_cache_append(prm, ref, pick(kd), pick(vd), pick(q))
+    B.tca_cache_accept(prm, cache, kd, vd, q, T, torch.from_numpy(path).cuda(), n)
+    H.mirror_equals_device(cache)
+    took = torch.from_numpy(n > 0).cuda()
+    per_unit = cache.rows_total // batch
+    for name in ("k", "v", "pos"):
+        a, b, c = (getattr(x, name).view(batch, per_unit, -1) for x in (cache, ref, before))
+        assert torch.equal(a, torch.where(took[:, None, None], b, c)), name
+
+
 def test_accept_takes_the_same_token_twice_and_clamps_the_path():
     prm = H.params(1, 2, 1, 64, "bf16", block=32, window=64)
     q, kd, vd = drafts(prm, 4, "bf16", 110)
