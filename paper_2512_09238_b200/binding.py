@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Optional, Sequence
 
 import numpy as np
@@ -302,8 +303,17 @@ def tca_ws_status(ws, stream=None) -> int:
 
 
 _ELT = {TCA_BF16: torch.bfloat16, TCA_F32: torch.float32}
-_I64x4, _I64x8 = C.c_int64 * 4, C.c_int64 * 8
+_pack4, _pack8 = struct.Struct("=4q").pack, struct.Struct("=8q").pack
 _I32, _I64, _U8 = torch.int32, torch.int64, torch.uint8
+
+
+# Without the lazy initialisation of torch.cuda.current_device(): asked only when a tensor is on a device.
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _stream_on(here: int, stream) -> int:
+    """_stream for a call whose tensors are on device `here`, the current one."""
+    return _raw_stream(here) if stream is None and _raw_stream is not None else _stream(stream)
 
 
 def _refuse(where: str, *specs) -> None:
@@ -326,15 +336,28 @@ def _ok(t, here, dtype, shape) -> bool:
     return t is None or (t.dtype is dtype and t.shape == shape and t.get_device() == here and t.is_contiguous())
 
 
-def _view(t, here, dtype, shape, out: list) -> bool:
-    """The same for a [heads, rows, d] view with any strides but the last; appends its element strides {head, row}
-    (a dimension of one element counts as contiguous: torch leaves its stride unspecified)."""
+def _strides(t, here, dtype, shape):
+    """Element strides (head, row) of a [heads, rows, d] view of this type and shape on device `here`, with any
+    strides but the last (a dimension of one element counts as contiguous: torch leaves its stride unspecified);
+    None if it is not one."""
     if t.dtype is not dtype or t.shape != shape or t.get_device() != here:
-        return False
+        return None
     head, row, last = t.stride()
     heads, rows, d = shape
-    out += (head if heads > 1 else max(rows, 1) * d, row if rows > 1 else d)
-    return last == 1 or rows == 0
+    if last != 1 and rows:
+        return None
+    if heads < 2 or rows < 2:
+        return (head if heads > 1 else max(rows, 1) * d, row if rows > 1 else d)
+    return head, row
+
+
+def _host_in(a: Optional[np.ndarray], dtype):
+    """The bytes of a small host array that a call only reads (a copy is cheaper than asking numpy for the address)."""
+    if a is None:
+        return None
+    if a.dtype != dtype or not a.flags.c_contiguous:
+        raise ValueError(f"host buffer must be a C-contiguous {np.dtype(dtype).name} array")
+    return a.tobytes()
 
 
 def _fits(cache: "Cache", here, dtype, d) -> bool:
@@ -352,28 +375,30 @@ def tca_attn_packed(prm, Q, K, V, rows, seq_start, O, ws, stream=None) -> None:
     """Q, O [n_q_heads, rows, d], K, V [n_kv_heads, rows, d]: contiguous, or views with any head and row strides
     that are multiples of 16 bytes (``x.transpose(0, 1)`` of a token-major tensor); seq_start a CUDA int64 tensor
     of prm.batch + 1 elements."""
-    e, d, here, st = _ELT[prm.dtype], prm.head_dim, Q.get_device(), []
+    e, d, here = _ELT[prm.dtype], prm.head_dim, Q.get_device()
     qs, ks, ss = (prm.n_q_heads, rows, d), (prm.n_kv_heads, rows, d), (prm.batch + 1,)
-    if not (here >= 0 and here == torch.cuda.current_device() and _view(Q, here, e, qs, st) and _view(K, here, e, ks, st)
-            and _view(V, here, e, ks, st) and _view(O, here, e, qs, st) and _ok(seq_start, here, _I64, ss)
+    if not (here >= 0 and here == _current_device() and (sq := _strides(Q, here, e, qs)) and (sk := _strides(K, here, e, ks))
+            and (sv := _strides(V, here, e, ks)) and (so := _strides(O, here, e, qs)) and _ok(seq_start, here, _I64, ss)
             and _ok(ws, here, _U8, ws.shape)):
         _refuse("tca_attn_packed", ("Q", Q, e, qs, False), ("K", K, e, ks, False), ("V", V, e, ks, False),
                 ("O", O, e, qs, False), ("seq_start", seq_start, _I64, ss, True), ("ws", ws, _U8, None, True))
     _check(lib().tca_attn_packed(C.byref(prm), Q.data_ptr(), K.data_ptr(), V.data_ptr(), rows, seq_start.data_ptr(),
-                                 _I64x8(*st), O.data_ptr(), ws.data_ptr(), ws.numel(), _stream(stream)), "tca_attn_packed")
+                                 _pack8(*sq, *sk, *sv, *so), O.data_ptr(), ws.data_ptr(), ws.numel(), _stream_on(here, stream)),
+           "tca_attn_packed")
 
 
 def tca_cache_load(prm, K, V, rows, seq_start, slots, cache: "Cache", stream=None) -> None:
     """K, V [n_kv_heads, rows, d] as in tca_attn_packed; seq_start an int64 and slots an int32 numpy array (or None)."""
-    e, here, st, ks = _ELT[prm.dtype], K.get_device(), [], (prm.n_kv_heads, rows, prm.head_dim)
-    if not (here >= 0 and here == torch.cuda.current_device() and _view(K, here, e, ks, st) and _view(V, here, e, ks, st)
+    e, here, ks = _ELT[prm.dtype], K.get_device(), (prm.n_kv_heads, rows, prm.head_dim)
+    if not (here >= 0 and here == _current_device() and (sk := _strides(K, here, e, ks)) and (sv := _strides(V, here, e, ks))
             and _fits(cache, here, e, prm.head_dim)):
         _refuse_cache("tca_cache_load", prm, cache, ("K", K, e, ks, False), ("V", V, e, ks, False))
     n_seq = len(seq_start) - 1
     if slots is not None and len(slots) != n_seq:
         raise ValueError("tca_cache_load: slots must have one entry per sequence")
-    _check(lib().tca_cache_load(C.byref(prm), K.data_ptr(), V.data_ptr(), rows, _I64x4(*st), _host(seq_start, np.int64),
-                                _host(slots, np.int32), n_seq, C.byref(cache.desc), _stream(stream)), "tca_cache_load")
+    _check(lib().tca_cache_load(C.byref(prm), K.data_ptr(), V.data_ptr(), rows, _pack4(*sk, *sv),
+                                _host_in(seq_start, np.int64), _host_in(slots, np.int32), n_seq, C.byref(cache.desc),
+                                _stream_on(here, stream)), "tca_cache_load")
 
 
 def tca_attn_tree_workspace_bytes(prm, n_draft: int) -> int:
@@ -391,7 +416,7 @@ def alloc_tree_workspace(prm: tca_params, n_draft: int, device="cuda") -> torch.
 def tca_attn_tree(prm, q, k_draft, v_draft, n_draft, parent, n_live, cache: "Cache", O, ws, stream=None) -> None:
     e, B, d, here = _ELT[prm.dtype], prm.batch, prm.head_dim, q.get_device()
     qs, ks, ps = (B, prm.n_q_heads, n_draft, d), (B, prm.n_kv_heads, n_draft, d), (B, n_draft)
-    if not (here >= 0 and here == torch.cuda.current_device() and _ok(q, here, e, qs) and _ok(k_draft, here, e, ks)
+    if not (here >= 0 and here == _current_device() and _ok(q, here, e, qs) and _ok(k_draft, here, e, ks)
             and _ok(v_draft, here, e, ks) and _ok(O, here, e, qs) and _ok(parent, here, _I32, ps)
             and _ok(n_live, here, _I32, (B,)) and _ok(ws, here, _U8, ws.shape) and _fits(cache, here, e, d)):
         _refuse_cache("tca_attn_tree", prm, cache, ("q", q, e, qs, True), ("k_draft", k_draft, e, ks, True), ("v_draft", v_draft, e, ks, True),
@@ -399,21 +424,21 @@ def tca_attn_tree(prm, q, k_draft, v_draft, n_draft, parent, n_live, cache: "Cac
                 ("ws", ws, _U8, None, True))
     _check(lib().tca_attn_tree(C.byref(prm), q.data_ptr(), k_draft.data_ptr(), v_draft.data_ptr(), n_draft, parent.data_ptr(),
                                None if n_live is None else n_live.data_ptr(), C.byref(cache.desc), O.data_ptr(),
-                               ws.data_ptr(), ws.numel(), _stream(stream)), "tca_attn_tree")
+                               ws.data_ptr(), ws.numel(), _stream_on(here, stream)), "tca_attn_tree")
 
 
 def tca_cache_accept(prm, cache: "Cache", k_draft, v_draft, q_draft, n_draft, path, n_accept, stream=None) -> None:
     """path a CUDA int32 tensor [batch, n_draft]; n_accept an int32 numpy array of prm.batch elements."""
     e, B, d, here = _ELT[prm.dtype], prm.batch, prm.head_dim, k_draft.get_device()
     qs, ks, ps = (B, prm.n_q_heads, n_draft, d), (B, prm.n_kv_heads, n_draft, d), (B, n_draft)
-    if not (here >= 0 and here == torch.cuda.current_device() and _ok(k_draft, here, e, ks) and _ok(v_draft, here, e, ks)
+    if not (here >= 0 and here == _current_device() and _ok(k_draft, here, e, ks) and _ok(v_draft, here, e, ks)
             and _ok(q_draft, here, e, qs) and _ok(path, here, _I32, ps) and _fits(cache, here, e, d)):
         _refuse_cache("tca_cache_accept", prm, cache, ("k_draft", k_draft, e, ks, True), ("v_draft", v_draft, e, ks, True),
                 ("q_draft", q_draft, e, qs, True), ("path", path, _I32, ps, True))
     if len(n_accept) != B:
         raise ValueError("tca_cache_accept: n_accept must have one entry per sequence")
     _check(lib().tca_cache_accept(C.byref(prm), C.byref(cache.desc), k_draft.data_ptr(), v_draft.data_ptr(),
-                                  q_draft.data_ptr(), n_draft, path.data_ptr(), _host(n_accept, np.int32), _stream(stream)),
+                                  q_draft.data_ptr(), n_draft, path.data_ptr(), _host_in(n_accept, np.int32), _stream_on(here, stream)),
            "tca_cache_accept")
 
 
