@@ -461,3 +461,42 @@ def test_the_binding_refuses_a_cache_made_for_something_else():
             B.tca_cache_load(prm, x, x, 10, np.array([0, 5, 10]), None, cache)
         assert torch.equal(cache.k, was)
     torch.cuda.synchronize()
+
+
+def test_calls_on_several_streams_at_once():
+    """Prompts of one batch while another one drafts and accepts: each with buffers and workspaces of its own."""
+    prm, pp = H.params(2, 8, 2, 128, "bf16"), H.params(3, 6, 2, 128, "bf16")
+    starts = [0, 700, 701, 1500]
+    qp, kp = H.randn(1, (6, 1500, 128), "bf16"), H.randn(2, (2, 1500, 128), "bf16")
+    T, parent = 20, np.stack([H.chain(20), H.bush(20, 4)])
+    sets, want = [], H.run_packed(pp, qp, kp, kp, starts)
+    for i in range(3):
+        cache = H.make_cache(prm, [900, 20, 700, 1], [90, 90, 3, 3], 5, 1200, "bf16", 20 + i, extra_cap=40, t_keep=3)
+        sets.append((cache, drafts(prm, T, "bf16", 160 + 3 * i), H.clone_cache(prm, cache)))
+    n, path = np.array([20, 7], dtype=np.int32), torch.arange(T, dtype=torch.int32, device="cuda").repeat(2, 1)
+    trees = []
+    for cache, (q, kd, vd), alone in sets:
+        trees.append(H.run_tree(prm, q, kd, vd, parent, alone))
+        B.tca_cache_accept(prm, alone, kd, vd, q, T, path, n)
+        trees.append(H.run_tree(prm, q, kd, vd, parent, alone))
+    par = torch.from_numpy(parent).cuda()
+    st = torch.tensor(starts, device="cuda")
+    pws, po = B.alloc_workspace(pp, 1500, B.TCA_OP_PACKED), torch.empty_like(qp)
+    tws = [B.alloc_tree_workspace(prm, T) for _ in sets]
+    out = [torch.empty_like(trees[0]) for _ in trees]
+    streams = [torch.cuda.Stream() for _ in range(4)]
+    torch.cuda.synchronize()
+    for i, (cache, (q, kd, vd), _) in enumerate(sets):
+        with torch.cuda.stream(streams[i]):
+            B.tca_attn_tree(prm, q, kd, vd, T, par, None, cache, out[2 * i], tws[i])
+            B.tca_cache_accept(prm, cache, kd, vd, q, T, path, n)
+            B.tca_attn_tree(prm, q, kd, vd, T, par, None, cache, out[2 * i + 1], tws[i])
+        with torch.cuda.stream(streams[3]):
+            B.tca_attn_packed(pp, qp, kp, kp, 1500, st, po, pws)
+    torch.cuda.synchronize()
+    for a, b in zip(out, trees):
+        assert torch.equal(a, b)
+    for cache, _, alone in sets:
+        H.mirror_equals_device(cache)
+        assert torch.equal(cache.state, alone.state) and torch.equal(cache.pos, alone.pos) and torch.equal(cache.k, alone.k)
+    assert torch.equal(po, want)
