@@ -212,9 +212,11 @@ int tca_score_select(const tca_params* prm, const void* q_last, const void* K, i
 /* REQUIRED once after filling the descriptor and before any other call that takes it:
  * uploads the host mirror of `cache` (seg_start, global_cap, n_global, tail_head, n_tail,
  * seq_len, t_keep) into cache->state and zero-fills cache->k and cache->v.  The zero-fill is
- * not optional: the attention kernels multiply rows that are not in use by an exactly zero
- * weight, which cancels only finite values, so a cache that skips this call can turn
- * uninitialised memory into NaNs in the output without any error being reported. */
+ * not optional: the bf16 prefill multiplies cache rows that a query does not see by an exactly
+ * zero weight, which cancels only finite values, so a cache that skips this call can turn
+ * uninitialised memory into NaNs in the output without any error being reported.
+ * (tca_attn_decode and tca_attn_tree read nothing into rows that are not in use, whatever an
+ * earlier sequence left there.) */
 int tca_cache_init(const tca_params* prm, tca_cache_desc* cache, void* stream);
 
 /*

@@ -234,8 +234,8 @@ int tca_cache_init(const tca_params* prm, tca_cache_desc* c, void* stream) {
     s[TCA_ST_SEQ_LEN] = c->seq_len[u];
     s[TCA_ST_T_KEEP] = c->t_keep[u];
   }
-  // Unused rows must hold finite values: the tensor-pipe kernels multiply masked-out rows by
-  // an exact zero weight, which only cancels finite numbers.
+  // Unused rows must hold finite values: the bf16 prefill multiplies masked-out rows by an exact
+  // zero weight, which only cancels finite numbers.
   const size_t cache_bytes = size_t(c->rows_total) * prm->head_dim * elt_size(prm->dtype);
   TCA_CHECK_CUDA(cudaMemsetAsync(c->k, 0, cache_bytes, static_cast<cudaStream_t>(stream)));
   TCA_CHECK_CUDA(cudaMemsetAsync(c->v, 0, cache_bytes, static_cast<cudaStream_t>(stream)));

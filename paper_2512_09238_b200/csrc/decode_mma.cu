@@ -84,6 +84,7 @@ decode_mma_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   __shared__ BulkRing<kStages> ring;
   __shared__ int abort_word;
   __shared__ SliceId slice_slot;
+  __shared__ __align__(16) uint32_t zeros[4];
   __shared__ float s_m[kMmaConsumers / 32][kMaxGroup], s_l[kMmaConsumers / 32][kMaxGroup];
   volatile int* abort_flag = &abort_word;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -91,6 +92,7 @@ decode_mma_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
   if (tid == 0) {
     ring.init(kMmaConsumers / 32);
     abort_word = 0;
+    zeros[0] = zeros[1] = zeros[2] = zeros[3] = 0u;
     ptx::tma_prefetch_desc(&map_k);
     ptx::tma_prefetch_desc(&map_v);
   }
@@ -224,11 +226,16 @@ decode_mma_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     // ---- O = O * corr + P V
     if (ok) ok = ring.wait_full(n, abort_flag);
     if (ok && my_rows > 0) {
-      const uint32_t vt = ring_base + (n % kStages) * Ring::kTileBytes;
+      // Rows behind a run's end are not in use and may hold anything (what an earlier sequence of the same place
+      // left there, or another unit's rows): their weight is an exact zero, but zero times an infinity or NaN is
+      // not.  So their lanes load from 16 bytes of zeros instead; the offset within the tile is scaled away.
+      // (Masking the loaded registers takes the step 0.5 us, zeroing the rows in shared memory 0.75 us.)
+      const uint32_t in_use = (ld_mi & 1) * 8 + ld_rr < my_rows ? 1u : 0u;
+      const uint32_t vt = in_use ? ring_base + (n % kStages) * Ring::kTileBytes : ptx::smem_u32(zeros);
 #pragma unroll
       for (int j = 0; j < ND; j += 2) {
         uint32_t b[4];
-        ldmatrix_x4_trans(b, vt + swz<D>(v_row, j + v_chunk));
+        ldmatrix_x4_trans(b, vt + in_use * uint32_t((j >> 3) * kBoxBytes) + in_use * swz<64>(v_row, (j & 7) + v_chunk));
         o[j][0] *= corr; o[j][1] *= corr;
         o[j + 1][0] *= corr; o[j + 1][1] *= corr;
         mma_bf16(o[j], pa, b[0], b[1]);

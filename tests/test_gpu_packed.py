@@ -375,3 +375,69 @@ def test_a_batch_without_a_token(dtype):
     assert list(cache.n_tail) == [20, 20, 0, 0, 20, 20] and list(cache.n_global) == [10, 10, 0, 0, 10, 10]
     assert np.array_equal(after[[0, 1, 4, 5]], before.view(6, -1).cpu().numpy()[[0, 1, 4, 5]])
     H.mirror_equals_device(cache)
+
+
+# ------------------------------------------------------------------ decode over a place that was used before
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_decode_after_a_place_is_reused(bad, d, dtype):
+    """A prompt that takes the place of one that held infinities or NaN decodes as in a cache that is new."""
+    hq, hkv = 8, 2
+    prm = H.params(3, hq, hkv, d, dtype, block=32, window=64)
+    cap, keep = np.full(6, 512, dtype=np.int64), np.full(6, 4, dtype=np.int64)
+    long = H.randn(1, (hkv, 600, d), dtype)
+    long[:] = bad
+    q, other = H.randn(2, (3, hq, d), dtype, 1.5), H.randn(3, (hkv, 150, d), dtype)
+    load = lambda c, x, n, slot: B.tca_cache_load(prm, x, x, x.shape[1], np.array([0, n], dtype=np.int64), np.array([slot], dtype=np.int32), c)  # noqa: E731
+    for n in (1, 15, 17, 100, 129, 417):
+        x = H.randn(10 + n, (hkv, n, d), dtype)
+        out = []
+        for used in (True, False):
+            cache = B.Cache(prm, cap, 96, keep)
+            if used:
+                load(cache, long, 600, 1)
+            load(cache, other, 150, 0)
+            load(cache, other, 150, 2)
+            load(cache, x, n, 1)
+            o, ws = torch.full_like(q, float("nan")), B.alloc_workspace(prm, cache.rows_total, B.TCA_OP_DECODE)
+            B.tca_attn_decode(prm, q, cache, o, ws)
+            assert B.tca_ws_status(ws) == B.TCA_OK
+            out.append(o)
+        assert torch.isfinite(out[0]).all() and torch.equal(out[0], out[1]), n
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("group", [1, 4, 8])
+def test_decode_rows_not_in_use_have_no_influence(group, dtype):
+    """Everything behind the ends of the runs, wrapped rings among them, may hold anything; with and without a workspace."""
+    prm = H.params(2, 3 * group, 3, 128, dtype)
+    cache = H.make_cache(prm, [70, 300, 129, 1, 0, 1000], [90, 30, 96, 20, 95, 11], [50, 0, 20, 90, 3, 94], 1500, dtype, 8, extra_cap=40, tail_cap=97)
+    q, ws = H.randn(7, (2, 3 * group, 128), dtype, 1.5), B.alloc_workspace(prm, cache.rows_total, B.TCA_OP_DECODE)
+
+    def both():
+        a, b = torch.full_like(q, 7.0), torch.full_like(q, 7.0)
+        B.tca_attn_decode(prm, q, cache, a, ws)
+        B.tca_attn_decode_static(prm, q, cache, b)
+        assert B.tca_ws_status(ws) == B.tca_decode_static_status() == B.TCA_OK
+        return a, b
+
+    clean = both()
+    unused = torch.ones(cache.rows_total, dtype=torch.bool, device="cuda")
+    for u in range(6):
+        unused[torch.from_numpy(cache.unit_rows(u)).cuda()] = False
+    for bad in (float("nan"), float("inf"), -float("inf")):
+        cache.k[unused], cache.v[unused] = bad, bad
+        for got, want in zip(both(), clean):
+            assert torch.isfinite(got).all() and torch.equal(got, want)
+    # nor does the other sequence, whose rows begin where the first one's ring ends
+    theirs = torch.zeros(cache.rows_total, dtype=torch.bool, device="cuda")
+    theirs[int(cache.seg_start[3]):] = True
+    keep = [x[theirs].clone() for x in (cache.k, cache.v)]
+    cache.k[theirs], cache.v[theirs] = float("nan"), float("inf")
+    for got, want in zip(both(), clean):
+        assert torch.equal(got[0], want[0])
+    cache.k[theirs], cache.v[theirs] = keep
+    # the last row in use does show
+    cache.v[int(cache.unit_rows(1)[-1]), 5] = float("inf")
+    assert torch.isinf(both()[0][0, group:2 * group, 5]).all()
