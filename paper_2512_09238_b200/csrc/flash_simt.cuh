@@ -11,9 +11,14 @@
 // tile's softmax and second product, the next V tile under the next first product.
 //
 // What bounds it is the shared-memory pipe, four clocks per warp for a 16-byte load against one clock of a
-// scheduler for an FMA: 4 x 4 scores per thread take 8 loads (32 clocks of the SM) per 64 FMAs (16), 8 x 8 take
-// 16 (64) per 256 (64).  So there are two shapes: SimtSmall for few rows and short prompts, SimtLarge where
-// there is work for all SMs in tiles of 64 rows (fp32 prompt of 2K, 8 heads of 64: 149 -> 138 us, 31 TFLOP/s).
+// scheduler for an FMA: 4 x 4 scores per thread take 8 loads (32 clocks of the SM) per 64 FMAs (16), 8 x 4 take 12
+// (48) per 128 (32).  So there are two shapes: SimtSmall for few rows and short prompts, SimtLarge where there is
+// work for all SMs in tiles of 64 rows (fp32 prompt of 2K, 8 heads of 64: 149 -> 139 us, 31 TFLOP/s).
+//
+// A row's result must not depend on which shape the batch around it led to.  So both take 64 keys at a time and
+// deal them to the groups in the same way (8 x 8 scores and 128 keys for head_dim 64 took 138 us, and 142 with
+// its keys in the order of the others), and what the compiler could contract into a multiply-add in one shape and
+// not in the other is written out.
 #pragma once
 #include <type_traits>
 
@@ -32,8 +37,8 @@ struct SimtShape {
   static constexpr int kRows = 8 * RT, kKeys = 16 * KT;
 };
 using SimtSmall = SimtShape<4, 4>;
-template <int D>
-using SimtLarge = SimtShape<8, D == 64 ? 8 : 4>;      // as many keys as shared memory has room for
+using SimtLarge = SimtShape<8, 4>;
+static_assert(SimtSmall::kKeys == SimtLarge::kKeys, "a row's keys are taken in the same order whatever the shape");
 
 template <int D, typename Shape>
 struct SimtSmem {
@@ -153,7 +158,7 @@ __device__ __forceinline__ bool simt_flash(const Src& src, float scale_log2e, fl
       float mx = -INFINITY;
 #pragma unroll
       for (int j = 0; j < KT; ++j) {
-        s[i][j] = (tx + 16 * j <= last[i]) ? s[i][j] * scale_log2e : -INFINITY;   // a masked score counts for nothing
+        s[i][j] = (tx + 16 * j <= last[i]) ? __fmul_rn(s[i][j], scale_log2e) : -INFINITY;   // a masked score counts for nothing
         mx = fmaxf(mx, s[i][j]);
       }
 #pragma unroll
@@ -168,9 +173,7 @@ __device__ __forceinline__ bool simt_flash(const Src& src, float scale_log2e, fl
         sum += s[i][j];
         sP[(ty * RT + i) * PST + tx + 16 * j] = s[i][j];
       }
-#pragma unroll
-      for (int off = 8; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
-      l[i] = l[i] * corr + sum;
+      l[i] = fmaf(l[i], corr, sum);        // of this thread's keys; the row's 16 threads are added up at the end
       m[i] = m_new;
 #pragma unroll
       for (int c = 0; c < D / 16; ++c) o[i][c] *= corr;
@@ -208,6 +211,10 @@ __device__ __forceinline__ bool simt_flash(const Src& src, float scale_log2e, fl
     load_v(t + 2);
   }
   cp_async_wait<0>();
+#pragma unroll
+  for (int i = 0; i < RT; ++i)
+#pragma unroll
+    for (int off = 8; off > 0; off >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], off);
   // group 1 hands its state over through group 1's own buffers
   float* sO = smem + kRows * ST + S::kGroupFloats;
   float* sM = sO + kRows * ST;
@@ -232,15 +239,15 @@ __device__ __forceinline__ bool simt_flash(const Src& src, float scale_log2e, fl
     const float m1 = sM[2 * (ty * RT + i)], l1 = sM[2 * (ty * RT + i) + 1];
     const float mn = fmaxf(m[i], m1), base = (mn == -INFINITY) ? 0.f : mn;
     const float w0 = exp2f(m[i] - base), w1 = exp2f(m1 - base);
-    l[i] = l[i] * w0 + l1 * w1;
+    l[i] = fmaf(l[i], w0, __fmul_rn(l1, w1));
     m[i] = mn;
 #pragma unroll
     for (int c = 0; c < D / 64; ++c) {
       const float4 v = *reinterpret_cast<const float4*>(sO + (ty * RT + i) * ST + tx * 4 + 64 * c);
-      o[i][c * 4 + 0] = o[i][c * 4 + 0] * w0 + v.x * w1;
-      o[i][c * 4 + 1] = o[i][c * 4 + 1] * w0 + v.y * w1;
-      o[i][c * 4 + 2] = o[i][c * 4 + 2] * w0 + v.z * w1;
-      o[i][c * 4 + 3] = o[i][c * 4 + 3] * w0 + v.w * w1;
+      o[i][c * 4 + 0] = fmaf(o[i][c * 4 + 0], w0, __fmul_rn(v.x, w1));
+      o[i][c * 4 + 1] = fmaf(o[i][c * 4 + 1], w0, __fmul_rn(v.y, w1));
+      o[i][c * 4 + 2] = fmaf(o[i][c * 4 + 2], w0, __fmul_rn(v.z, w1));
+      o[i][c * 4 + 3] = fmaf(o[i][c * 4 + 3], w0, __fmul_rn(v.w, w1));
     }
   }
   return true;

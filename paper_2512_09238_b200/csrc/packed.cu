@@ -98,7 +98,7 @@ int launch_packed_shape(const tca_params* prm, const void* Q, const void* K, con
 template <typename T, int D>
 int launch_packed_simt(const tca_params* prm, const void* Q, const void* K, const void* V, const PackedArgs& a, void* O,
                        cudaStream_t s) {
-  using Large = SimtLarge<D>;
+  using Large = SimtLarge;
   const int64_t tiles = a.rows * a.n_q_heads / Large::kRows;
   if (tiles >= sm_count() && a.rows * (a.n_q_heads / a.n_kv_heads) >= int64_t(4) * Large::kRows * a.n_seq)
     return launch_packed_shape<T, D, Large>(prm, Q, K, V, a, O, s);

@@ -441,3 +441,29 @@ def test_decode_rows_not_in_use_have_no_influence(group, dtype):
     # the last row in use does show
     cache.v[int(cache.unit_rows(1)[-1]), 5] = float("inf")
     assert torch.isinf(both()[0][0, group:2 * group, 5]).all()
+
+
+# ------------------------------------------------------------------ a prompt alone and in a batch
+@pytest.mark.parametrize("dtype,flags", [("f32", 0), ("bf16", 0), ("bf16", B.TCA_FLAG_PREFILL_SIMT)])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("group", [1, 4])
+def test_a_prompt_rounds_the_same_alone_and_in_any_batch(group, d, dtype, flags):
+    """Bit for bit, while the batch and the buffers around it go from a few rows to thousands (other tile shapes,
+    another order of the heads) and to more sequences than are searched in sorted order."""
+    hkv = 2
+    hq = hkv * group
+    rows = 24000 // hq + 800
+    q, k, v = (H.randn(i, (h, rows, d), dtype, 1.5) for i, h in ((1, hq), (2, hkv), (3, hkv)))
+    for n in (1, 40, 64, 65, 100, 129, 200, 333, 700):
+        def run(at, starts, total):
+            """The prompt at row `at` of buffers of `total` rows, among the given sequences."""
+            a, b, c = (torch.cat([x[:, 700:700 + at], x[:, :n], x[:, 700 + at:700 + total - n]], dim=1) for x in (q, k, v))
+            o = H.run_packed(H.params(len(starts) - 1, hq, hkv, d, dtype, flags=flags), a, b, c, starts)
+            return o[:, at:at + n]
+        alone = run(0, [0, n], n)
+        assert torch.isfinite(alone).all()
+        full = rows - 700 + n
+        assert torch.equal(run(0, [0, n], full), alone), (n, "much padding")
+        assert torch.equal(run(500, [0, 500, 500 + n, full], full), alone), (n, "between long prompts")
+        many = np.concatenate([np.arange(0, 300, 2), [300, 300 + n, full]])
+        assert torch.equal(run(300, many, full), alone), (n, "among many")
