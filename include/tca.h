@@ -23,8 +23,9 @@
  *     workspaces is a STICKY status word: zero it once after allocating (a zero-filled workspace is fine); a
  *     kernel sets it when one of its bounded device-side waits gives up (or, in the
  *     range-checked build, when an index is out of range) and nothing in the library clears
- *     it.  While it is set, the tensor-core kernels return at once without computing.  After
- *     a non-zero status, zero the whole workspace before using it again.
+ *     it.  While it is set, the tensor-core kernels return at once without computing (of
+ *     tca_attn_tree a wait that gave up stops the next calls; a failed range check is only
+ *     reported).  After a non-zero status, zero the whole workspace before using it again.
  *   - Return value: TCA_OK or a negative error.  Argument errors are detected on the
  *     host before anything is launched and leave every output untouched.  Unsupported
  *     shapes return TCA_ERR_UNSUPPORTED; nothing ever falls back to the CPU.

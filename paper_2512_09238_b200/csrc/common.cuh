@@ -146,6 +146,10 @@ struct Elt<__nv_bfloat16> {
   static constexpr int kDtype = TCA_BF16;
 };
 
+// Whether a status word stops the calls that share the mainloop of flash_tc.cuh: a wait gave up, so there is no
+// result.  A failed range check of theirs (a parent out of range) is only reported; it counts as documented.
+__device__ __forceinline__ bool stops_call(int status) { return status != 0 && status != kStatusBounds; }
+
 // Record a failed range check in a workspace header: word 0 = kStatusBounds, word 1 = which check,
 // bytes 8..15 = the offending value.  Only the first failure is kept.
 __device__ __forceinline__ void report_bounds_ws(int* status, int which, long long value) {

@@ -170,7 +170,7 @@ __device__ __forceinline__ void flash_tc_setup(uint8_t* smem, TcShared<Item>* sh
     }
     ptx::fence_barrier_init();
     // the status word is the caller's and no kernel that still runs clears it: readable here
-    sh->abort = *reinterpret_cast<const volatile int*>(status) != 0 ? 1 : 0;
+    sh->abort = stops_call(*reinterpret_cast<const volatile int*>(status)) ? 1 : 0;
   }
   if (threadIdx.x < 32) {
     ptx::tmem_alloc(&sh->tmem, 512);
@@ -642,7 +642,11 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
   // ------------------------------------------------------------- teardown
   ptx::tc_fence_before();
   __syncthreads();
-  if (*abort_flag) ptx::abort_teardown(status, tid);   // status word, then time for copies in flight to land
+  if (*abort_flag) {
+    // a wait that gave up outranks a failed range check: there is no result
+    if (kDebugBounds && tid == 0) atomicCAS(status, kStatusBounds, kStatusTimeout);
+    ptx::abort_teardown(status, tid);      // status word, then time for copies in flight to land
+  }
   if (warp == 0) ptx::tmem_dealloc(tmem_base, 512);
 }
 

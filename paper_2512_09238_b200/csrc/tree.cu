@@ -239,7 +239,7 @@ tree_combine_kernel(const T* __restrict__ q, const T* __restrict__ k_draft, cons
   // the unit's partial results, in the order of its rows; a unit whose cache is empty has none.  (Both words
   // are requested before either is looked at.)
   const int2 where = cached > 0 ? __ldcg(ws.table + u) : make_int2(0, 0);
-  if (__ldcg(ws.status) != 0) return;      // a wait gave up: there are no partial results
+  if (stops_call(__ldcg(ws.status))) return;      // a wait gave up: there are no partial results
   const int n = min(where.y, plan.n_slots - where.x) * plan.streams;
   const size_t first = size_t(where.x) * plan.streams;
   for (int c0 = 0; c0 < n; c0 += 32) {                       // statistics of 32 partials at a time, one per lane

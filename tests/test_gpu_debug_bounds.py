@@ -104,3 +104,49 @@ def test_block_count_outside_its_range_is_skipped_and_recorded(checked_library):
     B.tca_select(prm, run.logscore[:1].contiguous(), run.L, run.n_k[:1], idx, offsets, None, None, ws)
     assert B.tca_ws_status(ws) == B.TCA_ERR_BOUNDS
     assert int(idx[n_sel - 1]) == -1            # nothing was written beyond the window
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_parent_out_of_range_is_recorded_and_every_row_is_written(checked_library, dtype):
+    """One parent that does not precede its child: it counts as the root, the status word says so, and no row of any
+    sequence is left out, in this call or the next one with the same workspace."""
+    import serving_harness as S
+    B_, T = 40, 64
+    prm = S.params(B_, 8, 2, 64, dtype)
+    cache = S.make_cache(prm, 60, 50, 7, 200, dtype, 5)
+    q, kd, vd = (S.randn(i, (B_, h, T, 64), dtype) for i, h in ((1, 8), (2, 2), (3, 2)))
+    good = np.tile(S.bush(T, 3), (B_, 1))
+    good[:, 20] = -1
+    odd = good.copy()
+    odd[0, 20] = T + 5
+    want = S.run_tree(prm, q, kd, vd, good, cache)
+    ws = B.alloc_tree_workspace(prm, T)
+    for _ in range(5):
+        o = torch.full_like(q, float("nan"))
+        B.tca_attn_tree(prm, q, kd, vd, T, torch.from_numpy(odd).cuda(), None, cache, o, ws)
+        assert B.tca_ws_status(ws) == B.TCA_ERR_BOUNDS
+        assert torch.equal(o, want)
+    word = ws.cpu().numpy()[:16].view(np.int64)
+    assert word[0] == (6 << 32) + 2 and word[1] == T + 5            # check 6, the offending value
+    # a wait that gave up still stops the call
+    ws[:4] = torch.tensor([1, 0, 0, 0], dtype=torch.uint8, device="cuda")
+    o = torch.full_like(q, 7.0)
+    B.tca_attn_tree(prm, q, kd, vd, T, torch.from_numpy(good).cuda(), None, cache, o, ws)
+    assert B.tca_ws_status(ws) == B.TCA_ERR_TIMEOUT and (o == 7.0).all()
+
+
+def test_a_path_index_out_of_range_is_recorded_and_clamped(checked_library):
+    import serving_harness as S
+    prm = S.params(2, 4, 2, 64, "bf16")
+    a = S.make_cache(prm, 5, 10, 0, 15, "bf16", 14)
+    b = S.clone_cache(prm, a)
+    q, kd, vd = (S.randn(i, (2, h, 4, 64), "bf16") for i, h in ((1, 4), (2, 2), (3, 2)))
+    n = np.array([2, 3], dtype=np.int32)
+    path = lambda *x: torch.tensor([[0, 1, 2, 3], x], dtype=torch.int32, device="cuda")  # noqa: E731
+    B.tca_cache_accept(prm, a, kd, vd, q, 4, path(2, 3, 0, 0), n)
+    B.tca_cache_accept(prm, b, kd, vd, q, 4, path(2, 99, -1, 0), n)
+    assert B.tca_cache_status(a)[0] == B.TCA_OK
+    st, detail = B.tca_cache_status(b)
+    assert st == B.TCA_ERR_BOUNDS and list(detail[:2]) == [2, 6] and detail[2] in (99, (1 << 56) - 1)
+    for name in ("k", "v", "pos"):
+        assert torch.equal(getattr(a, name), getattr(b, name)), name
