@@ -146,7 +146,7 @@ constexpr int kTcItemReaders = 1 + 2 + 8;   // issuer, cleaners, softmax warps
 // Everything that needs no input: barriers and tensor memory.  Called by all threads before the dependency
 // wait, so that it overlaps the end of the kernel before.
 template <int D, typename Item>
-__device__ __forceinline__ void flash_tc_setup(uint8_t* smem, TcShared<Item>* sh, const int* status) {
+__device__ __forceinline__ void flash_tc_setup(uint8_t* smem, TcShared<Item>* sh) {
   using L = TcLayout<D>;
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::offBar);
   if (threadIdx.x == 0) {
@@ -169,8 +169,7 @@ __device__ __forceinline__ void flash_tc_setup(uint8_t* smem, TcShared<Item>* sh
       ptx::mbar_init(s + 6 + h, 1);
     }
     ptx::fence_barrier_init();
-    // the status word is the caller's and no kernel that still runs clears it: readable here
-    sh->abort = stops_call(*reinterpret_cast<const volatile int*>(status)) ? 1 : 0;
+    sh->abort = 0;
   }
   if (threadIdx.x < 32) {
     ptx::tmem_alloc(&sh->tmem, 512);
@@ -235,9 +234,7 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
 
   if (warp < 4) {
     ptx::reg_dealloc<kTcRegsLean>();
-    if (*abort_flag) {
-      // a status word that was already set: do nothing
-    } else if (warp == 0) {
+    if (warp == 0) {
       // ------------------------------------------------------------- producer: finds the items, brings the tiles
       int slot = 0;                   // ring slot of the next load
       int group = 0;                  // its group, counted over all items
@@ -247,11 +244,15 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
       for (int i = 0; i < kRing; ++i) group_of[i] = -1;
       bool ok = true;
       auto wait_group = [&](int g) { return ptx::mbar_wait(bar_empty + g % kPairs, uint32_t(g / kPairs) & 1u, abort_flag); };
+      // The status word is read here, behind the dependency wait: the kernel before may be what clears it.  Its trip
+      // to memory is that of begin()'s loads.  If it stops the call there are no items.
+      const int found_status = *reinterpret_cast<const volatile int*>(status);
       src.begin(lane);
+      const bool stopped = stops_call(found_status);
 #pragma unroll 1
       for (int k = 0; ok; ++k) {
         typename Source::Item item;
-        const bool have = src.find(k, lane, item);
+        const bool have = !stopped && src.find(k, lane, item);
         if (k >= 2) ok = warp_wait(bar_item_empty + (k & 1), uint32_t((k >> 1) - 1) & 1u);
         if (!ok) break;
         if (lane == 0) {

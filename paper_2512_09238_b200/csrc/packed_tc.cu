@@ -141,7 +141,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
     ptx::tma_prefetch_desc(&mk);
     ptx::tma_prefetch_desc(&mv);
   }
-  flash_tc_setup<D>(smem, &sh, status);
+  flash_tc_setup<D>(smem, &sh);
   pdl_wait();
   pdl_launch_dependents();
   PackedTcSrc<D> src;

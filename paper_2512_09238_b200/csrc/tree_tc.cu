@@ -111,7 +111,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
     ptx::tma_prefetch_desc(&mk);
     ptx::tma_prefetch_desc(&mv);
   }
-  flash_tc_setup<D>(smem, &sh, ws.status);
+  flash_tc_setup<D>(smem, &sh);
   pdl_wait();
   pdl_launch_dependents();
   TreeTcSrc<D, kShared> src;

@@ -252,6 +252,32 @@ def test_a_set_status_word_stops_the_call():
     compare(prm, q, k, v, starts, H.run_packed(prm, q, k, v, starts, ws=ws), "bf16")
 
 
+def test_a_workspace_cleared_by_the_kernel_before():
+    """The status word counts as it is when the call's turn comes, not as it was while the kernel before still ran."""
+    prm, q, k, v, starts = case([50, 60], 4, 2, 128, "bf16", "heads", 98)
+    want = H.run_packed(prm, q, k, v, starts)
+    cache = H.make_cache(prm, 200, 90, 0, 300, "bf16", 17)
+    par = torch.from_numpy(np.tile(H.chain(5), (2, 1))).cuda()
+    qd, kd = H.randn(1, (2, 4, 5, 128), "bf16"), H.randn(2, (2, 2, 5, 128), "bf16")
+    tree = H.run_tree(prm, qd, kd, kd, par.cpu().numpy(), cache)
+    ws, tws = B.alloc_workspace(prm, q.shape[1], B.TCA_OP_PACKED), B.alloc_tree_workspace(prm, 5)
+    st, o, ot = torch.tensor(starts, device="cuda"), torch.empty_like(q), torch.empty_like(qd)
+    rows = slice(int(starts[0]), int(starts[-1]))
+    for size in (256, 1 << 16, 1 << 22, 1 << 26):             # cleared by a kernel that takes longer and longer
+        for w, call, out, right in ((ws, lambda w: B.tca_attn_packed(prm, q, k, v, q.shape[1], st, o, w), o, want),
+                                    (tws, lambda w: B.tca_attn_tree(prm, qd, kd, kd, 5, par, None, cache, ot, w), ot, tree)):
+            big = torch.zeros(max(size, w.numel()), dtype=torch.uint8, device="cuda")
+            mine = big[:w.numel()]
+            for _ in range(20):
+                out.fill_(7.0)
+                mine[:4] = torch.tensor([1, 0, 0, 0], dtype=torch.uint8, device="cuda")
+                big.zero_()
+                call(mine)
+                assert B.tca_ws_status(mine) == B.TCA_OK
+                cut = (slice(None), rows) if out is o else slice(None)
+                assert torch.equal(out[cut], right[cut])
+
+
 def test_tensor_cores_agree_with_the_fp32_pipes():
     prm, q, k, v, starts = case([700, 130, 9], 8, 2, 128, "bf16", "tokens", 100)
     a = H.f64(H.run_packed(prm, q, k, v, starts))
