@@ -52,7 +52,8 @@ enum {
   TCA_ERR_TIMEOUT = -5,     /* a bounded device-side wait gave up (see tca_ws_status)   */
   TCA_ERR_CAPACITY = -6,    /* a cache region would overflow                            */
   TCA_ERR_SCRATCH_LIMIT = -7, /* problem larger than the built-in scratch of a *_static call */
-  TCA_ERR_BOUNDS = -8        /* range-checked build only: an index or offset was out of range  */
+  TCA_ERR_BOUNDS = -8        /* an index or offset was out of range (range-checked build), or a
+                              * replayed append or accept found no room (see tca_cache_status)  */
 };
 
 enum { TCA_F32 = 0, TCA_BF16 = 1 };
@@ -358,7 +359,9 @@ int tca_attn_decode(const tca_params* prm, const void* q, const tca_cache_desc* 
  * ring then holds window + block tokens, its oldest `block` tokens are scored with the
  * current query (Eq. 5 restricted to the block, averaged over the query group), the top
  * t_keep move to the end of the global region in ascending position and the rest are
- * dropped.  Call before tca_attn_decode of the same step.
+ * dropped.  Call before tca_attn_decode of the same step.  A captured call that is replayed moves
+ * the device state on, but not the host mirror; a unit without room then stays as it was
+ * (tca_cache_status says so).
  *   k_new, v_new  DEVICE [batch, n_kv_heads, head_dim]
  *   q_cur         DEVICE [batch, n_q_heads, head_dim]  query of the appended token
  * TCA_ERR_CAPACITY if the global region of a unit would overflow.
@@ -445,7 +448,8 @@ size_t tca_attn_tree_workspace_bytes(const tca_params* prm, int32_t n_draft);
  *   n_accept  HOST [batch], 0 <= n_accept[s] <= n_draft; a sequence with 0 is not touched
  * TCA_ERR_CAPACITY if the global region of a unit would overflow; nothing has been changed then.  As with
  * every call that changes the cache, the counts and the host mirror are those of the call: a captured call
- * that is replayed moves the device state on, but not the mirror.
+ * that is replayed moves the device state on, but not the mirror.  A unit whose global region has no room
+ * for a replayed call's tokens stays as it was, and tca_cache_status says so.
  */
 int tca_cache_accept(const tca_params* prm, tca_cache_desc* cache, const void* k_draft,
                      const void* v_draft, const void* q_draft, int32_t n_draft, const int32_t* path,
@@ -496,10 +500,10 @@ int tca_attn_decode_static(const tca_params* prm, const void* q, const tca_cache
 int tca_decode_static_status(void* stream);
 
 /*
- * Range-checked build only (tca_build_info() & TCA_BUILD_DEBUG_BOUNDS; in the normal build this
- * always returns TCA_OK).  tca_compact_kv and tca_cache_append take no workspace, so their range
- * checks record a failure in the reserved state word of the unit concerned.  This call synchronises
- * `stream`, reads the state words back and returns TCA_ERR_BOUNDS for the first unit whose word is
+ * Failed range checks of the calls that take no workspace (tca_compact_kv, tca_cache_load,
+ * tca_cache_append, tca_cache_accept): they are recorded in the reserved state word of the unit
+ * concerned.  All of them are made by the range-checked build (tca_build_info() &
+ * TCA_BUILD_DEBUG_BOUNDS), check 5 of append and accept by every build.  This call synchronises `stream`, reads the state words back and returns TCA_ERR_BOUNDS for the first unit whose word is
  * set, with detail[0] = unit, detail[1] = which check (1 selected index, 2 block count, 3 ring
  * slot, 4 cache row, 5 global region full, 6 drafted index), detail[2] = the offending value; detail HOST [3],
  * optional.  The checked kernels skip the access that failed its test, so no build touches memory

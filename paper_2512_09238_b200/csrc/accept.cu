@@ -48,13 +48,18 @@ cache_accept_kernel(const T* __restrict__ k_draft, const T* __restrict__ v_draft
   __syncthreads();   // also: every thread has read the state before it is updated
   const int64_t full = int64_t(window) + b;
   if constexpr (kDebugBounds) {
-    const int64_t over = n_tail + n - full;
-    const int64_t blocks = over >= 0 ? over / b + 1 : 0;
-    const bool bad_ring = tail_head < 0 || tail_head >= tail_cap || n_tail < 0 || n_tail >= full || full > tail_cap;
-    if (bad_ring || n_global + blocks * t_keep > gcap) {
-      if (tid == 0) report_bounds_state(st, bad_ring ? kBoundsRingSlot : kBoundsGlobalRegion, bad_ring ? tail_head : n_global);
+    if (tail_head < 0 || tail_head >= tail_cap || n_tail < 0 || n_tail >= full || full > tail_cap) {
+      if (tid == 0) report_bounds_state(st, kBoundsRingSlot, tail_head);
       return;
     }
+  }
+  // The host has checked the room for the counts of its mirror.  A captured call that is replayed moves on without
+  // the mirror, so the unit's own words decide whether the tokens go in, in every build.
+  const int over = int(n_tail + n - full);         // < n; b is a power of two
+  const int blocks = over >= 0 ? (over >> (31 - __clz(b))) + 1 : 0;
+  if (n_global + int64_t(blocks) * t_keep > gcap) {
+    if (tid == 0) report_bounds_state(st, kBoundsGlobalRegion, n_global);
+    return;
   }
   const int shift = 31 - __clz(D * int(sizeof(T)) / 16);   // 16-byte pieces per row: a power of two
   for (int i0 = 0; i0 < n;) {

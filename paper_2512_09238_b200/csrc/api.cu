@@ -116,7 +116,7 @@ const char* tca_strerror(int status) {
     case TCA_ERR_TIMEOUT: return "device-side wait timed out";
     case TCA_ERR_CAPACITY: return "cache capacity exceeded";
     case TCA_ERR_SCRATCH_LIMIT: return "problem exceeds the built-in scratch of the static entry point";
-    case TCA_ERR_BOUNDS: return "index or offset out of range (range-checked build)";
+    case TCA_ERR_BOUNDS: return "index or offset out of range";
     default: return "unknown status";
   }
 }

@@ -368,6 +368,85 @@ def test_accept_refuses_without_touching_anything():
     B.tca_cache_accept(prm, cache, kd, vd, q, 8, path, np.array([3, 8], dtype=np.int32))    # what fits is taken
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("call", ["accept", "append"])
+def test_a_replayed_call_without_room_leaves_the_unit_as_it_was(call, dtype):
+    """A captured accept or append moves the device state on at every replay. Units that run out of room stop there,
+    each as its last call with room left it; the others go on, and nothing outside their segments is written."""
+    T = 40 if call == "accept" else 1
+    prm = H.params(3, 4, 2, 64, dtype, block=8, window=16)
+    cache = H.make_cache(prm, 3, 20, 5, 60, dtype, 23, t_keep=3, extra_cap=[0, 20, 16, 47, 0, 31])
+    q, kd, vd = drafts(prm, T, dtype, 180)
+    ref = H.clone_cache(prm, cache)
+    full, n = 24, np.array([T, T - 1 if T > 1 else 1, 0 if T > 1 else 1], dtype=np.int32)
+    path = torch.arange(T, dtype=torch.int32, device="cuda").repeat(3, 1)
+    one = [x[:, :, 0].contiguous() for x in (kd, vd, q)]
+
+    def run(c, n=n):
+        if call == "accept":
+            B.tca_cache_accept(prm, c, kd, vd, q, T, path, n)
+        else:
+            B.tca_cache_append(prm, c, *one)
+
+    # the mirror allows one call for all units; made ready once so that the capture sees no first-call work
+    warm = H.make_cache(prm, 3, 20, 5, 60, dtype, 23, t_keep=3, extra_cap=600)
+    run(warm)
+    torch.cuda.synchronize()
+    if call == "accept":
+        n[0] = 3                      # unit 0 has no room for a block: few enough tokens at first, too many on replay
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        run(cache, n)
+    # what each unit's replays do, by the counts: it takes the call's tokens while there is room for their blocks
+    room, tail, glob, seq = (x.copy() for x in (ref.global_cap, ref.n_tail, ref.n_global, ref.seq_len))
+    taken = np.zeros(6, dtype=int)
+    replays = 30 if call == "accept" else 200
+    for _ in range(replays):
+        for u in range(6):
+            k = int(n[u // 2])
+            over = tail[u] + k - full
+            blocks = over // 8 + 1 if over >= 0 else 0
+            if k and glob[u] + 3 * blocks <= room[u]:
+                taken[u] += 1
+                tail[u], glob[u], seq[u] = tail[u] + k - 8 * blocks, glob[u] + 3 * blocks, seq[u] + k
+        g.replay()
+    torch.cuda.synchronize()
+    st = cache.state.view(6, -1).cpu().numpy()
+    assert np.array_equal(st[:, 2], glob) and np.array_equal(st[:, 4], tail) and np.array_equal(st[:, 5], seq)
+    assert 0 < taken.max() < replays
+    status, detail = B.tca_cache_status(cache)
+    stopped = [u for u in range(6) if n[u // 2] and taken[u] < replays]
+    assert status == B.TCA_ERR_BOUNDS and list(detail) == [stopped[0], 5, glob[stopped[0]]]
+    # the same numbers of tokens without a graph, in a cache with room, unit by unit
+    wide = H.make_cache(prm, 3, 20, 5, 60, dtype, 23, t_keep=3, extra_cap=600)
+    for u in range(6):
+        a, b = int(wide.seg_start[u]), int(ref.seg_start[u])
+        for name in ("k", "v", "pos"):
+            src, dst = getattr(ref, name), getattr(wide, name)
+            dst[a:a + 3] = src[b:b + 3]
+            dst[a + int(wide.global_cap[u]):a + int(wide.global_cap[u]) + 24] = src[b + int(ref.global_cap[u]):b + int(ref.global_cap[u]) + 24]
+    for step in range(int(taken.max()) + 1):
+        for u in range(6):
+            if taken[u] != step or n[u // 2] == 0:
+                continue
+            ng, a, b = int(glob[u]), int(wide.seg_start[u]), int(cache.seg_start[u])
+            for name in ("k", "v", "pos"):
+                x, y = getattr(wide, name), getattr(cache, name)
+                assert torch.equal(x[a:a + ng], y[b:b + ng]), (name, u)
+                slots = (int(st[u, 3]) + torch.arange(int(tail[u]), device="cuda")) % 24
+                assert torch.equal(x[a + int(wide.global_cap[u]) + slots], y[b + int(cache.global_cap[u]) + slots]), (name, u)
+                left = slice(b + ng, b + int(cache.global_cap[u]))          # free rows of the global region
+                assert torch.equal(y[left], getattr(ref, name)[left]), (name, u)
+        if step < taken.max():
+            run(wide, n)
+    # and a call by the mirror, which has not moved, is stopped by the unit's own words too
+    before = cache.state.clone()
+    if call == "append":
+        run(cache)
+        torch.cuda.synchronize()
+        assert torch.equal(cache.state.view(6, -1)[stopped], before.view(6, -1)[stopped])
+
+
 # ------------------------------------------------------------------ the operators together
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_prompts_to_drafted_tokens_as_a_server_runs_them(dtype):
