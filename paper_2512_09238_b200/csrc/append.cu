@@ -96,6 +96,7 @@ extern "C" int tca_cache_append(const tca_params* prm, tca_cache_desc* c, const 
                 c->n_tail && c->seq_len && c->t_keep);
   const int64_t U = int64_t(prm->batch) * prm->n_kv_heads;
   TCA_CHECK_ARG(c->n_units == U);
+  TCA_CHECK_ARG(aligned(c->k, 16) && aligned(c->v, 16));   // a block that leaves is read and moved in 16-byte pieces
   const int64_t full = int64_t(prm->window) + prm->block;
   if (c->tail_cap < full) return TCA_ERR_CAPACITY;
   for (int64_t u = 0; u < U; ++u) {

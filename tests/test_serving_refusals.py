@@ -124,6 +124,17 @@ def test_accept_refusals():
     assert accept(n=(0, 0)) == B.TCA_OK           # nothing accepted: nothing launched
 
 
+def test_append_refuses_a_cache_that_16_byte_accesses_cannot_serve():
+    def append(d):
+        return B.lib().tca_cache_append(C.byref(prm()), C.byref(d), A, A, A, None)
+    for off in (2, 4, 8):
+        assert append(desc(ptr=A + off)) == B.TCA_ERR_INVALID_ARG
+        for field in ("k", "v"):
+            d = desc()
+            setattr(d, field, A + off)
+            assert append(d) == B.TCA_ERR_INVALID_ARG
+
+
 # ------------------------------------------------------------------ the oracle itself
 def test_oracle_paths_of_a_hand_worked_tree():
     sees = S.tree_paths(np.array([-1, 0, 0, 1, -1, 4, 3]))
