@@ -320,7 +320,7 @@ def _refuse(where: str, *specs) -> None:
     """Says which argument of a serving call is wrong: specs are (name, tensor, dtype, shape, contiguous)."""
     here = torch.cuda.current_device() if torch.cuda.is_available() else -2
     for name, t, dtype, shape, whole in specs:
-        if t is None:
+        if t is None and name == "n_live":
             continue
         if not isinstance(t, torch.Tensor) or t.get_device() != here:
             raise ValueError(f"{where}: {name} must be a tensor on the current CUDA device")
@@ -331,9 +331,11 @@ def _refuse(where: str, *specs) -> None:
     raise ValueError(f"{where}: bad argument")
 
 
+# What is no tensor at all has none of the attributes that the checks below ask for: the calls catch that, which
+# costs nothing otherwise, and leave it to _refuse to say which argument it is.
 def _ok(t, here, dtype, shape) -> bool:
-    """A contiguous tensor of this type and shape on device `here` (or an optional one that is not given)."""
-    return t is None or (t.dtype is dtype and t.shape == shape and t.get_device() == here and t.is_contiguous())
+    """A contiguous tensor of this type and shape on device `here`."""
+    return t.dtype is dtype and t.shape == shape and t.get_device() == here and t.is_contiguous()
 
 
 def _strides(t, here, dtype, shape):
@@ -351,12 +353,11 @@ def _strides(t, here, dtype, shape):
     return head, row
 
 
-def _host_in(a: Optional[np.ndarray], dtype):
-    """The bytes of a small host array that a call only reads (a copy is cheaper than asking numpy for the address)."""
-    if a is None:
-        return None
-    if a.dtype != dtype or not a.flags.c_contiguous:
-        raise ValueError(f"host buffer must be a C-contiguous {np.dtype(dtype).name} array")
+def _host_in(where: str, name: str, a, dtype, n: int):
+    """The bytes of a host array of n elements that a call only reads (a copy is cheaper than asking numpy for the
+    address)."""
+    if not isinstance(a, np.ndarray) or a.dtype != dtype or a.shape != (n,) or not a.flags.c_contiguous:
+        raise ValueError(f"{where}: {name} must be a C-contiguous {np.dtype(dtype).name} array of {n} elements")
     return a.tobytes()
 
 
@@ -366,8 +367,9 @@ def _fits(cache: "Cache", here, dtype, d) -> bool:
 
 
 def _refuse_cache(where: str, prm, cache: "Cache", *specs) -> None:
-    if not _fits(cache, torch.cuda.current_device() if torch.cuda.is_available() else -2, _ELT[prm.dtype], prm.head_dim):
-        raise ValueError(f"{where}: the cache must be on the current CUDA device and made for {_ELT[prm.dtype]} and head size {prm.head_dim}")
+    e, here = _ELT.get(prm.dtype), torch.cuda.current_device() if torch.cuda.is_available() else -2
+    if not isinstance(cache, Cache) or not _fits(cache, here, e, prm.head_dim):
+        raise ValueError(f"{where}: the cache must be on the current CUDA device and made for {e} and head size {prm.head_dim}")
     _refuse(where, *specs)
 
 
@@ -375,11 +377,16 @@ def tca_attn_packed(prm, Q, K, V, rows, seq_start, O, ws, stream=None) -> None:
     """Q, O [n_q_heads, rows, d], K, V [n_kv_heads, rows, d]: contiguous, or views with any head and row strides
     that are multiples of 16 bytes (``x.transpose(0, 1)`` of a token-major tensor); seq_start a CUDA int64 tensor
     of prm.batch + 1 elements."""
-    e, d, here = _ELT[prm.dtype], prm.head_dim, Q.get_device()
+    e, d = _ELT.get(prm.dtype), prm.head_dim
     qs, ks, ss = (prm.n_q_heads, rows, d), (prm.n_kv_heads, rows, d), (prm.batch + 1,)
-    if not (here >= 0 and here == _current_device() and (sq := _strides(Q, here, e, qs)) and (sk := _strides(K, here, e, ks))
-            and (sv := _strides(V, here, e, ks)) and (so := _strides(O, here, e, qs)) and _ok(seq_start, here, _I64, ss)
-            and _ok(ws, here, _U8, ws.shape)):
+    try:
+        here = Q.get_device()
+        good = (here >= 0 and here == _current_device() and (sq := _strides(Q, here, e, qs)) and (sk := _strides(K, here, e, ks))
+                and (sv := _strides(V, here, e, ks)) and (so := _strides(O, here, e, qs)) and _ok(seq_start, here, _I64, ss)
+                and _ok(ws, here, _U8, ws.shape))
+    except AttributeError:
+        good = False
+    if not good:
         _refuse("tca_attn_packed", ("Q", Q, e, qs, False), ("K", K, e, ks, False), ("V", V, e, ks, False),
                 ("O", O, e, qs, False), ("seq_start", seq_start, _I64, ss, True), ("ws", ws, _U8, None, True))
     _check(lib().tca_attn_packed(C.byref(prm), Q.data_ptr(), K.data_ptr(), V.data_ptr(), rows, seq_start.data_ptr(),
@@ -389,15 +396,20 @@ def tca_attn_packed(prm, Q, K, V, rows, seq_start, O, ws, stream=None) -> None:
 
 def tca_cache_load(prm, K, V, rows, seq_start, slots, cache: "Cache", stream=None) -> None:
     """K, V [n_kv_heads, rows, d] as in tca_attn_packed; seq_start an int64 and slots an int32 numpy array (or None)."""
-    e, here, ks = _ELT[prm.dtype], K.get_device(), (prm.n_kv_heads, rows, prm.head_dim)
-    if not (here >= 0 and here == _current_device() and (sk := _strides(K, here, e, ks)) and (sv := _strides(V, here, e, ks))
-            and _fits(cache, here, e, prm.head_dim)):
+    e, ks = _ELT.get(prm.dtype), (prm.n_kv_heads, rows, prm.head_dim)
+    try:
+        here = K.get_device()
+        good = (here >= 0 and here == _current_device() and (sk := _strides(K, here, e, ks)) and (sv := _strides(V, here, e, ks))
+                and _fits(cache, here, e, prm.head_dim))
+    except AttributeError:
+        good = False
+    if not good:
         _refuse_cache("tca_cache_load", prm, cache, ("K", K, e, ks, False), ("V", V, e, ks, False))
-    n_seq = len(seq_start) - 1
-    if slots is not None and len(slots) != n_seq:
-        raise ValueError("tca_cache_load: slots must have one entry per sequence")
+    n_seq = len(seq_start) - 1 if isinstance(seq_start, np.ndarray) and seq_start.ndim == 1 else -1
+    starts = _host_in("tca_cache_load", "seq_start", seq_start, np.int64, n_seq + 1)
+    places = None if slots is None else _host_in("tca_cache_load", "slots", slots, np.int32, n_seq)
     _check(lib().tca_cache_load(C.byref(prm), K.data_ptr(), V.data_ptr(), rows, _pack4(*sk, *sv),
-                                _host_in(seq_start, np.int64), _host_in(slots, np.int32), n_seq, C.byref(cache.desc),
+                                starts, places, n_seq, C.byref(cache.desc),
                                 _stream_on(here, stream)), "tca_cache_load")
 
 
@@ -414,11 +426,16 @@ def alloc_tree_workspace(prm: tca_params, n_draft: int, device="cuda") -> torch.
 
 
 def tca_attn_tree(prm, q, k_draft, v_draft, n_draft, parent, n_live, cache: "Cache", O, ws, stream=None) -> None:
-    e, B, d, here = _ELT[prm.dtype], prm.batch, prm.head_dim, q.get_device()
+    e, B, d = _ELT.get(prm.dtype), prm.batch, prm.head_dim
     qs, ks, ps = (B, prm.n_q_heads, n_draft, d), (B, prm.n_kv_heads, n_draft, d), (B, n_draft)
-    if not (here >= 0 and here == _current_device() and _ok(q, here, e, qs) and _ok(k_draft, here, e, ks)
-            and _ok(v_draft, here, e, ks) and _ok(O, here, e, qs) and _ok(parent, here, _I32, ps)
-            and _ok(n_live, here, _I32, (B,)) and _ok(ws, here, _U8, ws.shape) and _fits(cache, here, e, d)):
+    try:
+        here = q.get_device()
+        good = (here >= 0 and here == _current_device() and _ok(q, here, e, qs) and _ok(k_draft, here, e, ks)
+                and _ok(v_draft, here, e, ks) and _ok(O, here, e, qs) and _ok(parent, here, _I32, ps)
+                and (n_live is None or _ok(n_live, here, _I32, (B,))) and _ok(ws, here, _U8, ws.shape) and _fits(cache, here, e, d))
+    except AttributeError:
+        good = False
+    if not good:
         _refuse_cache("tca_attn_tree", prm, cache, ("q", q, e, qs, True), ("k_draft", k_draft, e, ks, True), ("v_draft", v_draft, e, ks, True),
                 ("O", O, e, qs, True), ("parent", parent, _I32, ps, True), ("n_live", n_live, _I32, (B,), True),
                 ("ws", ws, _U8, None, True))
@@ -429,16 +446,20 @@ def tca_attn_tree(prm, q, k_draft, v_draft, n_draft, parent, n_live, cache: "Cac
 
 def tca_cache_accept(prm, cache: "Cache", k_draft, v_draft, q_draft, n_draft, path, n_accept, stream=None) -> None:
     """path a CUDA int32 tensor [batch, n_draft]; n_accept an int32 numpy array of prm.batch elements."""
-    e, B, d, here = _ELT[prm.dtype], prm.batch, prm.head_dim, k_draft.get_device()
+    e, B, d = _ELT.get(prm.dtype), prm.batch, prm.head_dim
     qs, ks, ps = (B, prm.n_q_heads, n_draft, d), (B, prm.n_kv_heads, n_draft, d), (B, n_draft)
-    if not (here >= 0 and here == _current_device() and _ok(k_draft, here, e, ks) and _ok(v_draft, here, e, ks)
-            and _ok(q_draft, here, e, qs) and _ok(path, here, _I32, ps) and _fits(cache, here, e, d)):
+    try:
+        here = k_draft.get_device()
+        good = (here >= 0 and here == _current_device() and _ok(k_draft, here, e, ks) and _ok(v_draft, here, e, ks)
+                and _ok(q_draft, here, e, qs) and _ok(path, here, _I32, ps) and _fits(cache, here, e, d))
+    except AttributeError:
+        good = False
+    if not good:
         _refuse_cache("tca_cache_accept", prm, cache, ("k_draft", k_draft, e, ks, True), ("v_draft", v_draft, e, ks, True),
                 ("q_draft", q_draft, e, qs, True), ("path", path, _I32, ps, True))
-    if len(n_accept) != B:
-        raise ValueError("tca_cache_accept: n_accept must have one entry per sequence")
+    counts = _host_in("tca_cache_accept", "n_accept", n_accept, np.int32, B)
     _check(lib().tca_cache_accept(C.byref(prm), C.byref(cache.desc), k_draft.data_ptr(), v_draft.data_ptr(),
-                                  q_draft.data_ptr(), n_draft, path.data_ptr(), _host_in(n_accept, np.int32), _stream_on(here, stream)),
+                                  q_draft.data_ptr(), n_draft, path.data_ptr(), counts, _stream_on(here, stream)),
            "tca_cache_accept")
 
 

@@ -3,6 +3,7 @@ import ctypes as C
 
 import numpy as np
 import pytest
+import torch
 
 from oracle import serving_oracle as S
 from paper_2512_09238_b200 import _build, binding as B
@@ -133,6 +134,60 @@ def test_append_refuses_a_cache_that_16_byte_accesses_cannot_serve():
             d = desc()
             setattr(d, field, A + off)
             assert append(d) == B.TCA_ERR_INVALID_ARG
+
+
+class OnDevice(torch.Tensor):
+    """A host tensor that says it lies on device 0: what the binding looks at before it calls the library."""
+
+    def get_device(self):
+        return 0
+
+
+def test_the_binding_names_what_is_missing_or_no_tensor(monkeypatch):
+    monkeypatch.setattr(B, "_current_device", lambda: 0)
+    monkeypatch.setattr(B, "_raw_stream", lambda d: 0)
+    monkeypatch.setattr(torch.cuda, "is_available", lambda: True)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    called = []
+
+    class Lib:
+        def __getattr__(self, name):
+            return lambda *a: called.append(name) or 0
+
+    monkeypatch.setattr(B, "_lib", Lib())
+    mk = lambda *s, t=torch.bfloat16: torch.zeros(s, dtype=t).as_subclass(OnDevice)  # noqa: E731
+    p = prm(head_dim=64)
+    cache = B.Cache(p, np.full(8, 32), 96, np.full(8, 4), device="cpu", init=False)
+    cache.k, cache.v = cache.k.as_subclass(OnDevice), cache.v.as_subclass(OnDevice)
+    i32, i64 = np.int32, np.int64
+    calls = {
+        B.tca_attn_packed: dict(Q=mk(8, 10, 64), K=mk(4, 10, 64), V=mk(4, 10, 64), rows=10, seq_start=mk(3, t=torch.int64),
+                                O=mk(8, 10, 64), ws=mk(256, t=torch.uint8)),
+        B.tca_cache_load: dict(K=mk(4, 10, 64), V=mk(4, 10, 64), rows=10, seq_start=np.array([0, 4, 10], i64),
+                               slots=np.array([1, 0], i32), cache=cache),
+        B.tca_attn_tree: dict(q=mk(2, 8, 5, 64), k_draft=mk(2, 4, 5, 64), v_draft=mk(2, 4, 5, 64), n_draft=5,
+                              parent=mk(2, 5, t=torch.int32), n_live=mk(2, t=torch.int32), cache=cache, O=mk(2, 8, 5, 64),
+                              ws=mk(4096, t=torch.uint8)),
+        B.tca_cache_accept: dict(cache=cache, k_draft=mk(2, 4, 5, 64), v_draft=mk(2, 4, 5, 64), q_draft=mk(2, 8, 5, 64), n_draft=5,
+                                 path=mk(2, 5, t=torch.int32), n_accept=np.array([1, 2], i32)),
+    }
+    for call, good in calls.items():
+        call(p, **good)                                       # the stand-in library takes it
+        for name, value in good.items():
+            if name in ("rows", "n_draft"):
+                continue
+            optional = name in ("n_live", "slots")
+            for bad in (None, [1, 2, 3], "text", 5, np.zeros((2, 2, 2))):
+                if bad is None and optional:
+                    call(p, **{**good, name: None})
+                    continue
+                n = len(called)
+                with pytest.raises(ValueError, match=name):
+                    call(p, **{**good, name: bad})
+                assert len(called) == n
+        with pytest.raises(ValueError):
+            call(prm(head_dim=64, dtype=7), **good)
+    assert len(called) == 6
 
 
 # ------------------------------------------------------------------ the oracle itself
