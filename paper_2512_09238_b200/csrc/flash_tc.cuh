@@ -248,7 +248,7 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
       // to memory is that of begin()'s loads.  If it stops the call there are no items.
       const int found_status = *reinterpret_cast<const volatile int*>(status);
       src.begin(lane);
-      const bool stopped = stops_call(found_status);
+      const bool stopped = __any_sync(0xffffffffu, stops_call(found_status));   // find() needs the whole warp
 #pragma unroll 1
       for (int k = 0; ok; ++k) {
         typename Source::Item item;
