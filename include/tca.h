@@ -20,8 +20,8 @@
  *     tca_cache_status, tca_decode_static_status).  Outputs are valid once the stream has
  *     been synchronised.
  *   - Status words.  Word 0 of the prefill, packed, decode, tree, select and calibration
- *     workspaces is a STICKY status word: zero it once after allocating (a zero-filled workspace is fine); a
- *     kernel sets it when one of its bounded device-side waits gives up (or, in the
+ *     workspaces is a STICKY status word: zero it once after allocating (a zero-filled workspace is fine;
+ *     tca_attn_packed needs its whole workspace zeroed, see there); a kernel sets it when one of its bounded device-side waits gives up (or, in the
  *     range-checked build, when an index is out of range) and nothing in the library clears
  *     it.  While it is set, the tensor-core kernels return at once without computing (of
  *     tca_attn_tree a wait that gave up stops the next calls; a failed range check is only
@@ -383,11 +383,16 @@ int tca_cache_append(const tca_params* prm, tca_cache_desc* cache, const void* k
  *   strides    HOST [8], optional: element strides {head, row} of Q, K, V, O in that order, each at
  *              least head_dim and a multiple of 16 bytes (a token-major [rows, heads, d] buffer, or
  *              one with Q, K and V side by side).  NULL: contiguous buffers of the shapes above.
- *   ws         DEVICE workspace, tca_workspace_bytes(prm, rows, TCA_OP_PACKED), zeroed once after
- *              allocating; word 0 is the sticky status word.  Calls that share one must not overlap.
+ *   ws         DEVICE workspace, tca_workspace_bytes(prm, rows, TCA_OP_PACKED), all of it zeroed once
+ *              after allocating; word 0 is the sticky status word, others count the work that is left and
+ *              are zero again when a call ends.  So it is for this call alone: if another operator has
+ *              written to it, zero it again, or rows are left out without a status.  Calls that share
+ *              one must not overlap.
  * Row i's result does not depend on any other sequence, nor on what its own later rows hold (an
  * infinity or NaN there included).  O must not overlap Q, K or V.  prm->block, window and alpha are
- * not used.  TCA_FLAG_PREFILL_SIMT runs bf16 on the FP32 pipes.
+ * not used.  TCA_FLAG_PREFILL_SIMT runs bf16 on the FP32 pipes.  On the tensor cores (here and in
+ * tca_attn_tree) the softmax weights of bf16 inputs are rounded to bf16 before they meet the values, as
+ * in the library's other bf16 attention calls; sums and accumulators are fp32.
  */
 int tca_attn_packed(const tca_params* prm, const void* Q, const void* K, const void* V, int64_t rows,
                     const int64_t* seq_start, const int64_t* strides, void* O,
@@ -418,6 +423,9 @@ int tca_cache_load(const tca_params* prm, const void* K, const void* V, int64_t 
  * tokens per step, Eq. 2 each).  Drafted token t of a sequence sees the whole retained cache of each
  * KV head (global region + ring) and the drafted tokens on its own path to the root, itself included.
  * The cache is not changed; with n_draft = 1 this is tca_attn_decode of a token that was not appended.
+ * Compression stays outside: where appending one token at a time would fill the ring and compress a block
+ * before that token attends, a drafted token still sees the whole block.  So from the token that fills
+ * the ring on, results differ from those of append and decode; tca_cache_accept then compresses as they do.
  *   q, O              DEVICE [batch, n_q_heads, n_draft, head_dim]
  *   k_draft, v_draft  DEVICE [batch, n_kv_heads, n_draft, head_dim]
  *   parent    DEVICE [batch, n_draft] int32: parent[t] < t, or -1 for a child of the context.  Any other

@@ -195,7 +195,7 @@ size_t tca_workspace_bytes(const tca_params* prm, int64_t L, int op) {
     case TCA_OP_PREFILL: return align_up(prefill_tc_ws_bytes(prm), 256);
     case TCA_OP_DECODE: return decode_ws_layout(prm, L, U, nullptr).bytes;
     case TCA_OP_APPEND: return 256;
-    case TCA_OP_PACKED: return 256;   // the status word
+    case TCA_OP_PACKED: return 256;   // status word, item counter, count of CTAs that left (packed_tc.cu)
     case TCA_OP_CALIB: return prm->dtype == TCA_BF16 ? calib_ws_bytes(prm, L) : 0;
     case TCA_OP_SCORE_SELECT:
       return align_up(score_ws_layout(prm, L, nullptr).bytes, 256) + select_ws_layout(prm, L, nullptr).bytes;

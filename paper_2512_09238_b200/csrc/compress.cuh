@@ -94,7 +94,7 @@ __device__ __forceinline__ void compress_oldest_block(const T* __restrict__ q_un
                                                       int64_t ring, int64_t n_global, int64_t tail_head,
                                                       int64_t tail_cap, int t_keep, int D, int G, int b,
                                                       double sm_scale) {
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, lane16 = tid & 15, grp = tid >> 4;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   // ---- logits of the b oldest tail tokens against the G current queries, fp64
   __shared__ double xs[kMaxGroup][kMaxBlock];
   __shared__ double lse[kMaxGroup];

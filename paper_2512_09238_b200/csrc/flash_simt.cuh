@@ -1,5 +1,5 @@
 // Attention of a block of query rows over a stream of key tiles on the FP32 pipes, online softmax in one
-// pass: the kernel for fp32 inputs (their tolerance rules out bf16 and tf32 products) and the slow
+// pass: the kernel for fp32 inputs (their tolerance rules out a single bf16 or tf32 product) and the slow
 // cross-check of the tensor-core kernels.  Scores, statistics and accumulators are fp32.
 //
 // 256 threads in two groups of 128.  The groups take alternate key tiles, each with a softmax state of

@@ -4,8 +4,9 @@
 // tile serves 256 rows.  Q comes as one box of P positions x G heads, whatever the strides.
 //
 // Bound by the chain from a tile's scores to its product (flash_tc.cuh): a prompt of 8192 tokens, 32/8 heads of
-// 128, takes 480 us (1140 TFLOP/s, 67 % of the measured burst rate), one of 128K tokens 115 ms (1220 TFLOP/s);
-// 24 prompts of 0 to 1024 tokens take 48 us, where starting and finishing an item weighs as much as its tiles.
+// 128, takes 500 us (1100 TFLOP/s, 64 % of the measured burst rate; 477 us at full clock), one of 128K tokens
+// 116 ms (1210 TFLOP/s); 24 prompts of 0 to 1024 tokens take 51 us (48 at full clock), where starting and finishing
+// an item weighs as much as its tiles.
 #include "flash_tc.cuh"
 #include "packed_common.cuh"
 
@@ -182,8 +183,9 @@ int launch_packed_tc(const tca_params* prm, const void* Q, const void* K, const 
   if (allow_smem<packed_tc_kernel<D>>(TcLayout<D>::bytes) != TCA_OK) return TCA_ERR_CUDA;
   // Items of all heads in one order balance best, but then the resident CTAs read all heads' keys at once;
   // when those are more than half of the L2 the heads go one after another (128K tokens, 8 heads: 120
-  // against 135 ms).  Not with so many sequences that no single one is long: their keys are read once or
-  // twice anyway (500 prompts of up to 200 tokens: 460 against 590 us).
+  // against 135 ms).  Not with more sequences than the finder sorts: their keys are read once or
+  // twice anyway if they are short (500 prompts of up to 200 tokens: 460 against 590 us).  A long prompt among so
+  // many pays for it: 128K tokens among 127 prompts of 20 tokens 116 ms, among 128 or more 119 to 121 ms.
   const int unit_major = a.n_seq <= PackedFinder::kHeld && a.rows * a.n_kv_heads * D * 4 > l2_bytes() / 2 ? 1 : 0;
   const int64_t items = max_tiles * a.n_kv_heads, sms = sm_count();
   return launch_pdl(kern, dim3(unsigned(items < sms ? items : sms)), dim3(kTcThreads), size_t(TcLayout<D>::bytes), s, mq, mk,
