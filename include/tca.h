@@ -463,6 +463,98 @@ int tca_cache_accept(const tca_params* prm, tca_cache_desc* cache, const void* k
                      const void* v_draft, const void* q_draft, int32_t n_draft, const int32_t* path,
                      const int32_t* n_accept, void* stream);
 
+/*
+ * Causal attention with a sliding window and a few first tokens that stay visible ("sinks"), for packed prompts:
+ * row i of a sequence attends to its rows j <= i with i - j < prm->window or j < n_sink.  Everything else is
+ * tca_attn_packed: buffers, strides, seq_start, empty sequences, rows of nobody, what a row does not see, flags, and
+ * the workspace (TCA_OP_PACKED; the two calls may use the same one in turn).  With a window as long as every prompt the
+ * result is bit for bit tca_attn_packed's.  The form for single tokens is tca_attn_paged.
+ * n_sink >= 0, else TCA_ERR_INVALID_ARG; prm->window >= 1, else TCA_ERR_UNSUPPORTED.
+ */
+int tca_attn_window(const tca_params* prm, const void* Q, const void* K, const void* V, int64_t rows,
+                    const int64_t* seq_start, const int64_t* strides, int32_t n_sink, void* O,
+                    void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * A paged KV cache: the rows of a unit (sequence, KV head) lie in pages that the caller assigns from one pool, so that
+ * units of very different lengths, per-head budgets among them, share it.  Slot j of unit u is row j % page_size of page
+ * table[u][j / page_size].  All buffers are DEVICE memory of the caller; the struct is HOST memory.  The lengths live in
+ * the device state alone: a captured call may be replayed and goes on from there.
+ *   state   [n_units][TCA_PG_STATE_WORDS] int32, 16-byte aligned, zeroed once: rows in use, position of the next token,
+ *           first failed check (tca_paged_status), a word of the library's
+ *   table   entries of slots that are not in use are not read.  Pages may be shared by units while they are only read;
+ *           a call that writes to a page (append, evict, attention that accumulates) needs it to be one unit's alone.
+ * Supported: page_size 16, 32, 64, 128 or 256; n_pages * page_size and max_pages * page_size below 2^31; up to 65535
+ * units (else TCA_ERR_UNSUPPORTED).
+ */
+typedef struct tca_paged_desc {
+  void* k;              /* DEVICE [n_pages, page_size, head_dim]                        */
+  void* v;              /* DEVICE [n_pages, page_size, head_dim]                        */
+  int32_t* pos;         /* DEVICE [n_pages, page_size]: original position of every row   */
+  float* mass;          /* DEVICE [n_pages, page_size]: attention weight it has gathered */
+  int32_t* table;       /* DEVICE [n_units, max_pages]                                  */
+  int32_t* state;       /* DEVICE [n_units, TCA_PG_STATE_WORDS]                         */
+  int64_t n_pages;
+  int64_t n_units;      /* batch * n_kv_heads                                           */
+  int32_t page_size;
+  int32_t max_pages;    /* pages a unit can have                                        */
+} tca_paged_desc;
+#define TCA_PG_STATE_WORDS 4
+enum { TCA_PG_LEN = 0, TCA_PG_NEXT = 1, TCA_PG_CHECK = 2, TCA_PG_RESERVED = 3 };
+
+/*
+ * New rows go to the end of paged sequences, whole prompts or one token each.  Sequence i of the packed K, V goes to
+ * cache sequence slots[i] (all its KV heads): row r of it to slot len + r, with position next + r and the given mass;
+ * then len and next grow by the number of rows.  prm->batch is the cache's number of sequences.
+ *   K, V, rows, strides   as in tca_cache_load
+ *   seq_start  HOST [n_seq + 1], ascending, within [0, rows]; NULL: one row per sequence, row i for sequence i
+ *              (rows >= n_seq)
+ *   slots      HOST [n_seq], optional (NULL: sequence i goes to i): distinct cache sequences
+ *   mass       DEVICE [n_kv_heads, rows], optional (NULL: zeros): attention weight that the rows already have
+ * A unit without room for its rows (max_pages * page_size) and a unit with a page outside the pool among them keep
+ * their lengths (what may have been written behind them is not in use), and tca_paged_status says so.
+ */
+int tca_paged_append(const tca_params* prm, const void* K, const void* V, int64_t rows, const int64_t* strides,
+                     const int64_t* seq_start, const int32_t* slots, int32_t n_seq, const float* mass,
+                     tca_paged_desc* cache, void* stream);
+
+/*
+ * Attention of one new token per sequence over a paged cache (Eq. 2 with a single query per head).  The query
+ * heads of a unit with len rows attend to its slots j < len with j >= len - prm->window or j < n_sink (a window of
+ * 2^31 - 1 hides nothing); the token's own row is one of them if it was appended before.  A unit without a visible
+ * slot gives zeros.
+ *   q    DEVICE [batch, n_q_heads, head_dim]     O  DEVICE out, same shape
+ *   accumulate  not 0: the mass of every visible row grows by the mean over the unit's query heads of its softmax weight
+ *   ws   DEVICE workspace of tca_attn_paged_workspace_bytes(prm, cache, accumulate) bytes, zeroed once after
+ *        allocating; word 0 is the sticky status word.  Calls that share one must not overlap.
+ * Slots that are not visible have no influence whatever they hold.  A visible slot whose page lies outside the pool
+ * counts as not visible and sets the status word to TCA_ERR_BOUNDS.  n_sink >= 0 (TCA_ERR_INVALID_ARG), prm->window >= 1
+ * (TCA_ERR_UNSUPPORTED).  prm->block, alpha and flags are not used.
+ */
+int tca_attn_paged(const tca_params* prm, const void* q, const tca_paged_desc* cache, int32_t n_sink, int32_t accumulate,
+                   void* O, void* ws, size_t ws_bytes, void* stream);
+/* 0 for an invalid request. */
+size_t tca_attn_paged_workspace_bytes(const tca_params* prm, const tca_paged_desc* cache, int32_t accumulate);
+
+/*
+ * Eviction by accumulated attention weight.  A unit with more than budget[u] rows keeps budget[u] of them: the slots
+ * below n_sink, the rows whose position is above the unit's largest position minus n_recent, and of the others
+ * those with the largest mass (a NaN counts as the largest, equal ones to the lower slot).  Kept rows in slots below the
+ * budget stay where they are; the other kept rows, in ascending order of slots, fill the evicted slots below the budget,
+ * lowest first, with K, V, position and mass.  Then len is the budget (pages behind it are free); the position of the next token stays.
+ * The order of the other rows changes, so a sliding window, which goes by slots, no longer follows the positions.
+ *   budget  DEVICE [n_units] int32
+ * A unit whose sinks and recent rows are more than its budget, or with a page outside the pool, stays as it was, and
+ * tca_paged_status says so.  n_sink, n_recent >= 0 (TCA_ERR_INVALID_ARG).
+ */
+int tca_paged_evict(const tca_params* prm, tca_paged_desc* cache, int32_t n_sink, int32_t n_recent, const int32_t* budget,
+                    void* stream);
+
+/* Synchronise `stream` and report the first unit whose append or evict failed since the state was zeroed: TCA_OK, or
+ * TCA_ERR_BOUNDS with detail[0] = unit, detail[1] = which check (1 no room, 2 page outside the pool, 3 budget smaller
+ * than sinks and recent rows); detail HOST [2], optional. */
+int tca_paged_status(const tca_paged_desc* cache, void* stream, int64_t* detail);
+
 /* Size of the scratch array built into the library image for tca_attn_decode_static. */
 #define TCA_DECODE_STATIC_SCRATCH_BYTES (16u << 20)
 

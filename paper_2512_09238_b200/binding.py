@@ -30,6 +30,8 @@ TCA_BUILD_DEBUG_BOUNDS = 1
  TCA_OP_SCORE_SELECT, TCA_OP_PACKED) = range(9)
 TCA_TREE_MAX = 128
 TCA_STATE_WORDS = 8
+TCA_PG_STATE_WORDS = 4
+TCA_PG_LEN, TCA_PG_NEXT, TCA_PG_CHECK = 0, 1, 2
 
 EXPORTS = (
     "tca_strerror", "tca_version", "tca_budget_resolve", "tca_workspace_bytes", "tca_score",
@@ -39,6 +41,8 @@ EXPORTS = (
     "tca_decode_static_status", "tca_selftest_wait_expiry", "tca_score_select", "tca_build_info",
     "tca_cache_status", "tca_attn_prefill_gather", "tca_compact_kv_range",
     "tca_attn_packed", "tca_cache_load", "tca_attn_tree", "tca_attn_tree_workspace_bytes", "tca_cache_accept",
+    "tca_attn_window", "tca_paged_append", "tca_attn_paged", "tca_attn_paged_workspace_bytes", "tca_paged_evict",
+    "tca_paged_status",
 )
 
 
@@ -61,6 +65,12 @@ class tca_cache_desc(C.Structure):
                 ("seg_start", C.c_void_p), ("global_cap", C.c_void_p), ("n_global", C.c_void_p),
                 ("tail_head", C.c_void_p), ("n_tail", C.c_void_p), ("seq_len", C.c_void_p),
                 ("t_keep", C.c_void_p)]
+
+
+class tca_paged_desc(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("pos", C.c_void_p), ("mass", C.c_void_p), ("table", C.c_void_p),
+                ("state", C.c_void_p), ("n_pages", C.c_int64), ("n_units", C.c_int64), ("page_size", C.c_int32),
+                ("max_pages", C.c_int32)]
 
 
 _lib = None
@@ -97,6 +107,14 @@ def load_library(path: str) -> C.CDLL:
     L.tca_attn_tree_workspace_bytes.restype = sz
     L.tca_attn_tree_workspace_bytes.argtypes = [P, C.c_int32]
     L.tca_cache_accept.argtypes = [P, D, vp, vp, vp, C.c_int32, vp, vp, vp]
+    G = C.POINTER(tca_paged_desc)
+    L.tca_attn_window.argtypes = [P, vp, vp, vp, i64, vp, vp, C.c_int32, vp, vp, sz, vp]
+    L.tca_paged_append.argtypes = [P, vp, vp, i64, vp, vp, vp, C.c_int32, vp, G, vp]
+    L.tca_attn_paged.argtypes = [P, vp, G, C.c_int32, C.c_int32, vp, vp, sz, vp]
+    L.tca_attn_paged_workspace_bytes.restype = sz
+    L.tca_attn_paged_workspace_bytes.argtypes = [P, G, C.c_int32]
+    L.tca_paged_evict.argtypes = [P, G, C.c_int32, C.c_int32, vp, vp]
+    L.tca_paged_status.argtypes = [G, vp, vp]
     L.tca_calib_colmean.argtypes = [P, vp, vp, i64, vp, vp, sz, vp]
     L.tca_calib_score.argtypes = [P, vp, i64, vp, vp, vp, vp]
     L.tca_calib_choose.argtypes = [vp, vp, C.c_int, C.c_double]
@@ -110,7 +128,8 @@ def load_library(path: str) -> C.CDLL:
     L.tca_selftest_wait_expiry.argtypes = [vp, C.c_uint64, vp, vp]
     L.tca_build_info.argtypes = []
     for name in EXPORTS:
-        if name not in ("tca_strerror", "tca_workspace_bytes", "tca_attn_tree_workspace_bytes"):
+        if name not in ("tca_strerror", "tca_workspace_bytes", "tca_attn_tree_workspace_bytes",
+                        "tca_attn_paged_workspace_bytes"):
             getattr(L, name).restype = C.c_int
     return L
 
@@ -304,7 +323,7 @@ def tca_ws_status(ws, stream=None) -> int:
 
 _ELT = {TCA_BF16: torch.bfloat16, TCA_F32: torch.float32}
 _pack4, _pack8 = struct.Struct("=4q").pack, struct.Struct("=8q").pack
-_I32, _I64, _U8 = torch.int32, torch.int64, torch.uint8
+_I32, _I64, _U8, _F32 = torch.int32, torch.int64, torch.uint8, torch.float32
 
 
 # Without the lazy initialisation of torch.cuda.current_device(): asked only when a tensor is on a device.
@@ -320,7 +339,7 @@ def _refuse(where: str, *specs) -> None:
     """Says which argument of a serving call is wrong: specs are (name, tensor, dtype, shape, contiguous)."""
     here = torch.cuda.current_device() if torch.cuda.is_available() else -2
     for name, t, dtype, shape, whole in specs:
-        if t is None and name == "n_live":
+        if t is None and name in ("n_live", "mass"):
             continue
         if not isinstance(t, torch.Tensor) or t.get_device() != here:
             raise ValueError(f"{where}: {name} must be a tensor on the current CUDA device")
@@ -394,6 +413,26 @@ def tca_attn_packed(prm, Q, K, V, rows, seq_start, O, ws, stream=None) -> None:
            "tca_attn_packed")
 
 
+def tca_attn_window(prm, Q, K, V, rows, seq_start, n_sink, O, ws, stream=None) -> None:
+    """tca_attn_packed with a sliding window of prm.window keys and the first n_sink keys of each sequence always
+    visible; buffers and workspace (TCA_OP_PACKED) as there."""
+    e, d = _ELT.get(prm.dtype), prm.head_dim
+    qs, ks, ss = (prm.n_q_heads, rows, d), (prm.n_kv_heads, rows, d), (prm.batch + 1,)
+    try:
+        here = Q.get_device()
+        good = (here >= 0 and here == _current_device() and (sq := _strides(Q, here, e, qs)) and (sk := _strides(K, here, e, ks))
+                and (sv := _strides(V, here, e, ks)) and (so := _strides(O, here, e, qs)) and _ok(seq_start, here, _I64, ss)
+                and _ok(ws, here, _U8, ws.shape))
+    except AttributeError:
+        good = False
+    if not good:
+        _refuse("tca_attn_window", ("Q", Q, e, qs, False), ("K", K, e, ks, False), ("V", V, e, ks, False),
+                ("O", O, e, qs, False), ("seq_start", seq_start, _I64, ss, True), ("ws", ws, _U8, None, True))
+    _check(lib().tca_attn_window(C.byref(prm), Q.data_ptr(), K.data_ptr(), V.data_ptr(), rows, seq_start.data_ptr(),
+                                 _pack8(*sq, *sk, *sv, *so), n_sink, O.data_ptr(), ws.data_ptr(), ws.numel(), _stream_on(here, stream)),
+           "tca_attn_window")
+
+
 def tca_cache_load(prm, K, V, rows, seq_start, slots, cache: "Cache", stream=None) -> None:
     """K, V [n_kv_heads, rows, d] as in tca_attn_packed; seq_start an int64 and slots an int32 numpy array (or None)."""
     e, ks = _ELT.get(prm.dtype), (prm.n_kv_heads, rows, prm.head_dim)
@@ -463,6 +502,84 @@ def tca_cache_accept(prm, cache: "Cache", k_draft, v_draft, q_draft, n_draft, pa
            "tca_cache_accept")
 
 
+def _refuse_paged(where: str, prm, cache: "PagedCache", *specs) -> None:
+    e, here = _ELT.get(prm.dtype), torch.cuda.current_device() if torch.cuda.is_available() else -2
+    if not isinstance(cache, PagedCache) or not cache.fits(here, e, prm.head_dim):
+        raise ValueError(f"{where}: the cache must be a PagedCache on the current CUDA device, made for {e} and head size {prm.head_dim}")
+    _refuse(where, *specs)
+
+
+def tca_paged_append(prm, K, V, rows, seq_start, slots, mass, cache: "PagedCache", stream=None) -> None:
+    """K, V [n_kv_heads, rows, d] as in tca_attn_packed; seq_start an int64 numpy array, or None: one row for each of
+    `rows` sequences; slots an int32 numpy array or None; mass a float32 CUDA tensor [n_kv_heads, rows] or None."""
+    e, ks, ms = _ELT.get(prm.dtype), (prm.n_kv_heads, rows, prm.head_dim), (prm.n_kv_heads, rows)
+    try:
+        here = K.get_device()
+        good = (here >= 0 and here == _current_device() and (sk := _strides(K, here, e, ks)) and (sv := _strides(V, here, e, ks))
+                and (mass is None or _ok(mass, here, _F32, ms)) and cache.fits(here, e, prm.head_dim))
+    except AttributeError:
+        good = False
+    if not good:
+        _refuse_paged("tca_paged_append", prm, cache, ("K", K, e, ks, False), ("V", V, e, ks, False), ("mass", mass, _F32, ms, True))
+    if seq_start is None:
+        n_seq, starts = rows, None
+    else:
+        n_seq = len(seq_start) - 1 if isinstance(seq_start, np.ndarray) and seq_start.ndim == 1 else -1
+        starts = _host_in("tca_paged_append", "seq_start", seq_start, np.int64, n_seq + 1)
+    places = None if slots is None else _host_in("tca_paged_append", "slots", slots, np.int32, n_seq)
+    _check(lib().tca_paged_append(C.byref(prm), K.data_ptr(), V.data_ptr(), rows, _pack4(*sk, *sv), starts, places, n_seq,
+                                  None if mass is None else mass.data_ptr(), C.byref(cache.desc), _stream_on(here, stream)),
+           "tca_paged_append")
+
+
+def tca_attn_paged_workspace_bytes(prm, cache: "PagedCache", accumulate) -> int:
+    return int(lib().tca_attn_paged_workspace_bytes(C.byref(prm), C.byref(cache.desc), int(bool(accumulate))))
+
+
+def alloc_paged_workspace(prm: tca_params, cache: "PagedCache", accumulate: bool = False) -> torch.Tensor:
+    """A zero-filled workspace for tca_attn_paged calls over this cache (with accumulate, for calls of both kinds)."""
+    n = tca_attn_paged_workspace_bytes(prm, cache, accumulate)
+    if n == 0:
+        raise TcaError(TCA_ERR_INVALID_ARG, "tca_attn_paged_workspace_bytes")
+    return torch.zeros(n, dtype=torch.uint8, device=cache.k.device)
+
+
+def tca_attn_paged(prm, q, cache: "PagedCache", n_sink, accumulate, O, ws, stream=None) -> None:
+    """q, O [batch, n_q_heads, d], contiguous."""
+    e, qs = _ELT.get(prm.dtype), (prm.batch, prm.n_q_heads, prm.head_dim)
+    try:
+        here = q.get_device()
+        good = (here >= 0 and here == _current_device() and _ok(q, here, e, qs) and _ok(O, here, e, qs) and _ok(ws, here, _U8, ws.shape)
+                and cache.fits(here, e, prm.head_dim))
+    except AttributeError:
+        good = False
+    if not good:
+        _refuse_paged("tca_attn_paged", prm, cache, ("q", q, e, qs, True), ("O", O, e, qs, True), ("ws", ws, _U8, None, True))
+    _check(lib().tca_attn_paged(C.byref(prm), q.data_ptr(), C.byref(cache.desc), n_sink, 1 if accumulate else 0, O.data_ptr(),
+                                ws.data_ptr(), ws.numel(), _stream_on(here, stream)), "tca_attn_paged")
+
+
+def tca_paged_evict(prm, cache: "PagedCache", n_sink, n_recent, budget, stream=None) -> None:
+    """budget an int32 CUDA tensor of one element per (sequence, KV head)."""
+    e, bs = _ELT.get(prm.dtype), (prm.batch * prm.n_kv_heads,)
+    try:
+        here = budget.get_device()
+        good = here >= 0 and here == _current_device() and _ok(budget, here, _I32, bs) and cache.fits(here, e, prm.head_dim)
+    except AttributeError:
+        good = False
+    if not good:
+        _refuse_paged("tca_paged_evict", prm, cache, ("budget", budget, _I32, bs, True))
+    _check(lib().tca_paged_evict(C.byref(prm), C.byref(cache.desc), n_sink, n_recent, budget.data_ptr(), _stream_on(here, stream)),
+           "tca_paged_evict")
+
+
+def tca_paged_status(cache: "PagedCache", stream=None):
+    """(status, detail) with detail = [unit, which check] when status is TCA_ERR_BOUNDS."""
+    detail = np.zeros(2, dtype=np.int64)
+    st = lib().tca_paged_status(C.byref(cache.desc), _stream(stream), detail.ctypes.data)
+    return st, detail
+
+
 # ----------------------------------------------------------------------------- cache descriptor holder
 class Cache:
     """Owns the buffers a ``tca_cache_desc`` points at (torch device tensors, numpy host
@@ -506,6 +623,75 @@ class Cache:
         ring = self.seg_start[u] + self.global_cap[u]
         t = ring + (self.tail_head[u] + np.arange(self.n_tail[u])) % self.tail_cap
         return np.concatenate([g, t]).astype(np.int64)
+
+
+class PagedCache:
+    """Owns the buffers a ``tca_paged_desc`` points at and deals the pages of the pool to units.
+
+    ``table``, ``state`` (rows, next position, first failed check, a word of the library's), ``pos`` and ``mass`` are
+    device tensors; the last three lie in one buffer, ``meta``.  ``reserve`` and ``release`` keep a host copy of the table and a
+    list of free pages, and upload the units that changed; a program with an allocator of its own writes ``table``
+    instead."""
+
+    def __init__(self, prm: tca_params, n_pages: int, page_size: int, max_pages: int, device="cuda"):
+        U = prm.batch * prm.n_kv_heads
+        n_pages, page_size, max_pages = int(n_pages), int(page_size), int(max_pages)
+        if n_pages < 1 or page_size < 1 or max_pages < 1:
+            raise ValueError("n_pages, page_size and max_pages must be positive")
+        self.prm, self.n_pages, self.page_size, self.max_pages = prm, n_pages, page_size, max_pages
+        tdt, n = _ELT[prm.dtype], n_pages * page_size
+        self.k = torch.zeros(n_pages, page_size, prm.head_dim, dtype=tdt, device=device)
+        self.v = torch.zeros(n_pages, page_size, prm.head_dim, dtype=tdt, device=device)
+        pad = -n % 4                                     # the state begins on 16 bytes
+        self.meta = torch.zeros(2 * (n + pad) + TCA_PG_STATE_WORDS * U, dtype=torch.int32, device=device)
+        self.pos = self.meta[:n].view(n_pages, page_size)
+        self.mass = self.meta[n + pad:2 * n + pad].view(torch.float32).view(n_pages, page_size)
+        self.state = self.meta[2 * (n + pad):].view(U, TCA_PG_STATE_WORDS)
+        self.table = torch.full((U, max_pages), -1, dtype=torch.int32, device=device)
+        self.table_host = np.full((U, max_pages), -1, dtype=np.int32)
+        self.n_held = np.zeros(U, dtype=np.int64)        # pages dealt to each unit
+        self.free = list(range(n_pages - 1, -1, -1))
+        self.desc = tca_paged_desc(self.k.data_ptr(), self.v.data_ptr(), self.pos.data_ptr(), self.mass.data_ptr(),
+                                   self.table.data_ptr(), self.state.data_ptr(), n_pages, U, page_size, max_pages)
+        self._kind = (self.k.get_device(), tdt, prm.head_dim)
+
+    def fits(self, here, dtype, d) -> bool:
+        """It lies on device `here` and was made for this type and head size."""
+        return self._kind == (here, dtype, d)
+
+    def reserve(self, rows: Sequence[int]) -> None:
+        """Every unit u gets the pages that rows[u] rows need, where it has fewer."""
+        want = -(-np.asarray(rows, dtype=np.int64) // self.page_size)
+        if want.shape != self.n_held.shape:
+            raise ValueError("rows must have one entry per (sequence, KV head)")
+        more = np.maximum(0, want - self.n_held)
+        if want.max(initial=0) > self.max_pages or more.sum() > len(self.free):
+            raise TcaError(TCA_ERR_CAPACITY, "PagedCache.reserve")
+        changed = np.nonzero(more)[0]
+        for u in changed:
+            n = int(more[u])
+            self.table_host[u, self.n_held[u]:want[u]] = self.free[-n:][::-1]
+            del self.free[-n:]
+            self.n_held[u] = want[u]
+        self._upload(changed)
+
+    def release(self, rows: Sequence[int]) -> None:
+        """Every unit u gives back the pages that rows[u] rows do not need (after an eviction to a budget, or with 0
+        rows when its sequence ends; its state is the caller's to clear then)."""
+        want = -(-np.asarray(rows, dtype=np.int64) // self.page_size)
+        if want.shape != self.n_held.shape:
+            raise ValueError("rows must have one entry per (sequence, KV head)")
+        changed = np.nonzero(want < self.n_held)[0]
+        for u in changed:
+            self.free.extend(self.table_host[u, want[u]:self.n_held[u]][::-1].tolist())
+            self.table_host[u, want[u]:] = -1
+            self.n_held[u] = want[u]
+        self._upload(changed)
+
+    def _upload(self, units) -> None:
+        if len(units):
+            at = torch.from_numpy(np.ascontiguousarray(units)).to(self.table.device)
+            self.table[at] = torch.from_numpy(self.table_host[units]).to(self.table.device)
 
 
 def tca_calib_colmean(prm, Q, K, L, colmean, ws, stream=None) -> None:

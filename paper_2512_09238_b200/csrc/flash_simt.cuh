@@ -87,7 +87,8 @@ __device__ __forceinline__ void simt_load_rows(float* dst, int n, int tid, RowPt
 
 // Src: n_tiles(); n_rows(); q(r) -> const T*; keys(t) -> number of keys of tile t (1..kKeys); k(t), v(t)
 // -> const T*, its first row, k_stride(), v_stride() elements to the next; last(t, r) -> index in tile t of the last key row r sees (< 0: none, never >= keys(t));
-// masked(t): whether some row does not see all kKeys keys of the tile.
+// masked(t): whether some row does not see all kKeys keys of the tile.  kGap: rows also do not see keys
+// [gap_begin(t), gap_end(t, r)) of the tile.
 // On return the threads of group 0 (threadIdx.x < 128; true is returned) hold the row maxima (in log2
 // units), sums and unnormalised outputs of rows RT ty .., columns 4 tx + 64 c; m = -inf, l = 0,
 // o = 0 for a row that saw nothing.
@@ -151,14 +152,20 @@ __device__ __forceinline__ bool simt_flash(const Src& src, float scale_log2e, fl
     simt_group_sync(group);                // K has been read
     load_k(t + 2);
     const bool masked = src.masked(t);
-    int last[RT];
+    int last[RT], gap0 = 0, gap1[Src::kGap ? RT : 1] = {};
+    if constexpr (Src::kGap) gap0 = src.gap_begin(t);
+    auto sees = [&](int key, int last_i, int gap1_i) {
+      if constexpr (Src::kGap) { if (key >= gap0 && key < gap1_i) return false; }
+      return key <= last_i;
+    };
 #pragma unroll
     for (int i = 0; i < RT; ++i) {
       last[i] = masked ? src.last(t, ty * RT + i) : kKeys - 1;
+      if constexpr (Src::kGap) gap1[i] = masked ? src.gap_end(t, ty * RT + i) : 0;
       float mx = -INFINITY;
 #pragma unroll
       for (int j = 0; j < KT; ++j) {
-        s[i][j] = (tx + 16 * j <= last[i]) ? __fmul_rn(s[i][j], scale_log2e) : -INFINITY;   // a masked score counts for nothing
+        s[i][j] = sees(tx + 16 * j, last[i], gap1[Src::kGap ? i : 0]) ? __fmul_rn(s[i][j], scale_log2e) : -INFINITY;   // a masked score counts for nothing
         mx = fmaxf(mx, s[i][j]);
       }
 #pragma unroll
@@ -195,7 +202,7 @@ __device__ __forceinline__ bool simt_flash(const Src& src, float scale_log2e, fl
             for (int i = 0; i < RT; ++i) {
               const float pe = e == 0 ? p[i].x : e == 1 ? p[i].y : e == 2 ? p[i].z : p[i].w;
               // a key the row does not see must not reach it even if its value is an infinity or a NaN
-              if (!decltype(guarded)::value || kk + e <= last[i]) {
+              if (!decltype(guarded)::value || sees(kk + e, last[i], gap1[Src::kGap ? i : 0])) {
                 o[i][c * 4 + 0] = fmaf(pe, v.x, o[i][c * 4 + 0]);
                 o[i][c * 4 + 1] = fmaf(pe, v.y, o[i][c * 4 + 1]);
                 o[i][c * 4 + 2] = fmaf(pe, v.z, o[i][c * 4 + 2]);

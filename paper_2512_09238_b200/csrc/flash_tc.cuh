@@ -131,11 +131,11 @@ struct TcLayout {
 };
 
 // Small shared state.  Item: what the producer warp hands to the other roles.
-template <typename Item>
+template <typename Item, int kNoted = 2>
 struct TcShared {
   uint32_t tmem;
   int abort;
-  uint32_t dirty[2][2][4];   // per item slot: noted key rows of up to two tiles
+  uint32_t dirty[2][kNoted][4];   // per item slot: noted key rows of up to kNoted tiles
   int any_dirty[2];
   int valid[2];
   Item item[2];
@@ -145,8 +145,8 @@ constexpr int kTcItemReaders = 1 + 2 + 8;   // issuer, cleaners, softmax warps
 
 // Everything that needs no input: barriers and tensor memory.  Called by all threads before the dependency
 // wait, so that it overlaps the end of the kernel before.
-template <int D, typename Item>
-__device__ __forceinline__ void flash_tc_setup(uint8_t* smem, TcShared<Item>* sh) {
+template <int D, typename Shared>
+__device__ __forceinline__ void flash_tc_setup(uint8_t* smem, Shared* sh) {
   using L = TcLayout<D>;
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::offBar);
   if (threadIdx.x == 0) {
@@ -183,6 +183,9 @@ __device__ __forceinline__ void flash_tc_setup(uint8_t* smem, TcShared<Item>* sh
 // Called by all 384 threads after flash_tc_setup and the dependency wait; returns with every thread after
 // the last item.  Source:
 //   struct Item                   plain data
+//   kNoted, kGap                  tiles that are cleaned, at most; whether rows have a gap:
+//                                 row_key's row does not see keys [gap_begin(t), gap_end(key, t)) of tile t
+//                                 either (asked for the tiles that last() is asked for)
 //   void begin(lane)              whole warp, once: what find() needs
 //   bool find(k, lane, item)      whole warp: the CTA's k-th item; false: there is none
 //   void set(item)                all that follows is about this item
@@ -202,7 +205,7 @@ __device__ __forceinline__ void flash_tc_setup(uint8_t* smem, TcShared<Item>* sh
 //                                 the block had tiles; dirty: noted key rows or null; read(c, v): requests
 //                                 columns 32 c .. of O (warp-wide; tc_wait_ld() before v is used)
 template <int D, bool kShared, typename Source>
-__device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<typename Source::Item>* sh, float scale_log2e,
+__device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<typename Source::Item, Source::kNoted>* sh, float scale_log2e,
                                          int* status) {
   using L = TcLayout<D>;
   constexpr int kRing = L::kRing, kPairs = L::kPairs, kLead = kShared ? 1 : 2;
@@ -258,7 +261,7 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
         if (lane == 0) {
           sh->valid[k & 1] = have ? 1 : 0;
           sh->item[k & 1] = item;
-          for (int i = 0; i < 8; ++i) sh->dirty[k & 1][i >> 2][i & 3] = 0;
+          for (int i = 0; i < 4 * Source::kNoted; ++i) sh->dirty[k & 1][i >> 2][i & 3] = 0;
           sh->any_dirty[k & 1] = 0;
           ptx::mbar_arrive(bar_item + (k & 1));
         }
@@ -598,6 +601,12 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
         // A tile that some row does not see all of (the diagonal, the end of a run): the 32-key groups that
         // somebody sees, in a compact loop that reads the scores twice.
         const int hi = src.last(row_key, t), groups = (src.keys(h, t) + 31) >> 5;
+        int gap0 = 0, gap1 = 0;
+        if constexpr (Source::kGap) { gap0 = src.gap_begin(t); gap1 = src.gap_end(row_key, t); }
+        auto hidden_of = [&](int c) -> uint32_t {          // of keys 32 c .. 32 c + 31: bits of those in the gap
+          auto below = [](int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; };
+          return Source::kGap ? below(gap1 - c * 32) & ~below(gap0 - c * 32) : 0u;
+        };
         float mx = -INFINITY;
 #pragma unroll 1
         for (int c = 0; c < groups; ++c) {
@@ -605,9 +614,10 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
           ptx::tmem_ld32(s_addr + c * 32, v);
           ptx::tc_wait_ld();
           const int last = hi - c * 32;
+          const uint32_t hidden = hidden_of(c);
 #pragma unroll
           for (int k = 0; k < 32; ++k)
-            if (k <= last) mx = fmaxf(mx, __uint_as_float(v[k]));
+            if (k <= last && !(Source::kGap && (hidden >> k) & 1u)) mx = fmaxf(mx, __uint_as_float(v[k]));
         }
         rescale(mx, it > 0);
         const float neg_m = (m_used == -INFINITY) ? 0.f : -m_used;
@@ -618,10 +628,12 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
           ptx::tmem_ld32(s_addr + c * 32, v);
           ptx::tc_wait_ld();
           const int last = hi - c * 32;
+          const uint32_t hidden = hidden_of(c);
+          auto sees = [&](int k) { return k <= last && !(Source::kGap && (hidden >> k) & 1u); };
 #pragma unroll
           for (int k = 0; k < 32; k += 2) {    // a key the row does not see has weight 0, whatever its score
-            const float el = k <= last ? ptx::fast_exp2(fmaf(__uint_as_float(v[k]), scale_log2e, neg_m)) : 0.f;
-            const float eh = k + 1 <= last ? ptx::fast_exp2(fmaf(__uint_as_float(v[k + 1]), scale_log2e, neg_m)) : 0.f;
+            const float el = sees(k) ? ptx::fast_exp2(fmaf(__uint_as_float(v[k]), scale_log2e, neg_m)) : 0.f;
+            const float eh = sees(k + 1) ? ptx::fast_exp2(fmaf(__uint_as_float(v[k + 1]), scale_log2e, neg_m)) : 0.f;
             sum += el + eh;
             v[k / 2] = ptx::pack_bf16x2(el, eh);
           }

@@ -1,5 +1,6 @@
 // tca_attn_packed: causal attention of prompts of different lengths packed one after another (Eq. 2
-// with every key retained), grouped query heads, strided buffers.  This file holds the entry point and
+// with every key retained), grouped query heads, strided buffers; tca_attn_window: the same with a sliding window
+// and sinks.  This file holds the entry points and
 // the FP32-pipe kernel (fp32 inputs; bf16 with TCA_FLAG_PREFILL_SIMT as a cross-check); bf16 runs on
 // the tensor-core kernel of packed_tc.cu.
 #include "flash_simt.cuh"
@@ -7,7 +8,7 @@
 
 namespace tca {
 
-template <int D>
+template <int D, bool kWindow>
 int launch_packed_tc(const tca_params* prm, const void* Q, const void* K, const void* V, const PackedArgs& a, void* O,
                      void* ws, cudaStream_t s);
 
@@ -15,29 +16,51 @@ namespace {
 
 // Query rows of a CTA are (position, head of the group) pairs, head fastest: row r is position
 // p0 + r / G, head kvh * G + r % G, so a short sequence of a wide group still fills the tile.
-template <typename T, typename Shape>
+//
+// With a window, tiles that no row sees are left out, in pairs: the two groups of warps take alternate tiles, and a
+// row's keys have to meet the same group whichever rows share its CTA.  (A tile that a row does not see changes
+// nothing of its state.)
+template <typename T, typename Shape, bool kWindow>
 struct PackedSrc {
   static constexpr int kRows = Shape::kRows, kKeys = Shape::kKeys;
+  static constexpr bool kGap = kWindow;
   const T *Q, *K, *V;
   const PackedArgs* a;
   PackedWork w;
   int G;
+  int n0, skip;            // window: tiles t >= n0 lie `skip` tiles further on
+  __device__ __forceinline__ void begin() {
+    n0 = skip = 0;
+    if constexpr (kWindow) {
+      const int band = max(0, w.p0 - a->window + 1) / (2 * kKeys) * 2;
+      n0 = (min(a->n_sink, w.len) + 2 * kKeys - 1) / (2 * kKeys) * 2;
+      skip = max(0, band - n0);
+    }
+  }
+  __device__ __forceinline__ int tile(int t) const { return kWindow && t >= n0 ? t + skip : t; }
   __device__ __forceinline__ int n_rows() const { return min(kRows / G, w.len - w.p0) * G; }
   __device__ __forceinline__ int last_pos() const { return w.p0 + n_rows() / G - 1; }
-  __device__ __forceinline__ int n_tiles() const { return last_pos() / kKeys + 1; }
-  __device__ __forceinline__ int keys(int t) const { return min(kKeys, last_pos() + 1 - t * kKeys); }
+  __device__ __forceinline__ int n_tiles() const { return last_pos() / kKeys + 1 - (kWindow ? skip : 0); }
+  __device__ __forceinline__ int keys(int t) const { return min(kKeys, last_pos() + 1 - tile(t) * kKeys); }
   __device__ __forceinline__ const T* q(int r) const {
     return Q + (w.kvh * G + r % G) * a->q.head + (w.row0 + w.p0 + r / G) * a->q.row;
   }
-  __device__ __forceinline__ const T* k(int t) const { return K + w.kvh * a->k.head + (w.row0 + t * kKeys) * a->k.row; }
-  __device__ __forceinline__ const T* v(int t) const { return V + w.kvh * a->v.head + (w.row0 + t * kKeys) * a->v.row; }
+  __device__ __forceinline__ const T* k(int t) const { return K + w.kvh * a->k.head + (w.row0 + tile(t) * kKeys) * a->k.row; }
+  __device__ __forceinline__ const T* v(int t) const { return V + w.kvh * a->v.head + (w.row0 + tile(t) * kKeys) * a->v.row; }
   __device__ __forceinline__ int64_t k_stride() const { return a->k.row; }
   __device__ __forceinline__ int64_t v_stride() const { return a->v.row; }
-  __device__ __forceinline__ bool masked(int t) const { return (t + 1) * kKeys - 1 > w.p0; }
-  __device__ __forceinline__ int last(int t, int r) const { return min(w.p0 + r / G, last_pos()) - t * kKeys; }
+  __device__ __forceinline__ int pos(int r) const { return min(w.p0 + r / G, last_pos()); }
+  __device__ __forceinline__ bool masked(int t) const {
+    const int k0 = tile(t) * kKeys;
+    if (kWindow && k0 + kKeys > a->n_sink && k0 <= last_pos() - a->window) return true;
+    return k0 + kKeys - 1 > w.p0;
+  }
+  __device__ __forceinline__ int last(int t, int r) const { return pos(r) - tile(t) * kKeys; }
+  __device__ __forceinline__ int gap_begin(int t) const { return a->n_sink - tile(t) * kKeys; }
+  __device__ __forceinline__ int gap_end(int t, int r) const { return pos(r) - a->window + 1 - tile(t) * kKeys; }
 };
 
-template <typename T, int D, typename Shape>
+template <typename T, int D, typename Shape, bool kWindow>
 __global__ void __launch_bounds__(kSimtThreads, SimtSmem<D, Shape>::kCtasPerSm)
 packed_simt_kernel(const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const __grid_constant__ PackedArgs args,
                    float scale_log2e, T* __restrict__ O) {
@@ -48,7 +71,7 @@ packed_simt_kernel(const T* __restrict__ Q, const T* __restrict__ K, const T* __
   pdl_launch_dependents();
   const int G = args.n_q_heads / args.n_kv_heads;
   const int tile_pos = Shape::kRows / G;
-  PackedSrc<T, Shape> src;
+  PackedSrc<T, Shape, kWindow> src;
   src.Q = Q; src.K = K; src.V = V; src.a = &args; src.G = G;
   if (threadIdx.x < 32) {
     PackedFinder finder;
@@ -65,6 +88,7 @@ packed_simt_kernel(const T* __restrict__ Q, const T* __restrict__ K, const T* __
   __syncthreads();
   src.w = found;
   if (src.w.len == 0) return;
+  src.begin();
   constexpr int RT = Shape::RT;
   float o[RT][D / 16], m[RT], l[RT];
   if (!simt_flash<T, D, Shape>(src, scale_log2e, reinterpret_cast<float*>(packed_smem), o, m, l)) return;
@@ -80,13 +104,13 @@ packed_simt_kernel(const T* __restrict__ Q, const T* __restrict__ K, const T* __
   }
 }
 
-template <typename T, int D, typename Shape>
+template <typename T, int D, typename Shape, bool kWindow>
 int launch_packed_shape(const tca_params* prm, const void* Q, const void* K, const void* V, const PackedArgs& a, void* O,
                         cudaStream_t s) {
   using Smem = SimtSmem<D, Shape>;
   const int64_t n = packed_max_tiles(a.rows, a.n_seq, Shape::kRows / (a.n_q_heads / a.n_kv_heads)) * a.n_kv_heads;
   if (n >= (int64_t(1) << 31)) return TCA_ERR_UNSUPPORTED;
-  constexpr auto kern = packed_simt_kernel<T, D, Shape>;
+  constexpr auto kern = packed_simt_kernel<T, D, Shape, kWindow>;
   if (allow_smem<kern>(Smem::kBytes) != TCA_OK) return TCA_ERR_CUDA;
   return launch_pdl(kern, dim3(unsigned(n)), dim3(kSimtThreads), size_t(Smem::kBytes), s, static_cast<const T*>(Q),
                     static_cast<const T*>(K), static_cast<const T*>(V), a, prm->sm_scale * 1.4426950408889634f,
@@ -95,14 +119,14 @@ int launch_packed_shape(const tca_params* prm, const void* Q, const void* K, con
 
 // The large tiles where they give every SM more than one CTA and are not mostly padding: prompts that
 // average four of them.
-template <typename T, int D>
+template <typename T, int D, bool kWindow>
 int launch_packed_simt(const tca_params* prm, const void* Q, const void* K, const void* V, const PackedArgs& a, void* O,
                        cudaStream_t s) {
   using Large = SimtLarge;
   const int64_t tiles = a.rows * a.n_q_heads / Large::kRows;
   if (tiles >= sm_count() && a.rows * (a.n_q_heads / a.n_kv_heads) >= int64_t(4) * Large::kRows * a.n_seq)
-    return launch_packed_shape<T, D, Large>(prm, Q, K, V, a, O, s);
-  return launch_packed_shape<T, D, SimtSmall>(prm, Q, K, V, a, O, s);
+    return launch_packed_shape<T, D, Large, kWindow>(prm, Q, K, V, a, O, s);
+  return launch_packed_shape<T, D, SimtSmall, kWindow>(prm, Q, K, V, a, O, s);
 }
 
 // A buffer's strides: multiples of 16 bytes (vector loads, tensor maps), and room for a row.
@@ -112,20 +136,20 @@ bool bad_view(const PackedView& v, const tca_params* prm) {
   return v.head < prm->head_dim || v.row < prm->head_dim || v.head % unit || v.row % unit || v.head >= kMost || v.row >= kMost;
 }
 
-}  // namespace
-}  // namespace tca
-
-using namespace tca;
-
-extern "C" int tca_attn_packed(const tca_params* prm, const void* Q, const void* K, const void* V, int64_t rows,
-                               const int64_t* seq_start, const int64_t* strides, void* O, void* ws, size_t ws_bytes,
-                               void* stream) {
+// Both calls: checks, and the kernel of the type.
+template <bool kWindow>
+int attn_packed(const tca_params* prm, const void* Q, const void* K, const void* V, int64_t rows, const int64_t* seq_start,
+                const int64_t* strides, int32_t n_sink, void* O, void* ws, size_t ws_bytes, void* stream) {
   int st = check_params(prm);
   if (st != TCA_OK) return st;
   TCA_CHECK_ARG(((Q && K && V && O) || rows == 0) && seq_start && ws);   // no rows: nothing that they would point at
   TCA_CHECK_ARG(rows >= 0 && rows < (int64_t(1) << 31));
   TCA_CHECK_ARG(aligned(Q, 16) && aligned(K, 16) && aligned(V, 16) && aligned(O, 16) && aligned(ws, 256));
   TCA_CHECK_ARG(aligned(seq_start, 8));
+  if (kWindow) {
+    TCA_CHECK_ARG(n_sink >= 0);
+    if (prm->window < 1) return TCA_ERR_UNSUPPORTED;
+  }
   PackedArgs a;
   PackedView* views[4] = {&a.q, &a.k, &a.v, &a.o};
   for (int i = 0; i < 4; ++i) {
@@ -140,13 +164,33 @@ extern "C" int tca_attn_packed(const tca_params* prm, const void* Q, const void*
   a.n_seq = prm->batch;
   a.n_q_heads = prm->n_q_heads;
   a.n_kv_heads = prm->n_kv_heads;
+  // no sequence is longer than `rows`
+  a.window = int(prm->window < rows ? prm->window : rows);
+  a.n_sink = int(n_sink < rows ? n_sink : rows);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (prm->dtype == TCA_F32) {
-    if (prm->head_dim == 128) return launch_packed_simt<float, 128>(prm, Q, K, V, a, O, s);
-    return launch_packed_simt<float, 64>(prm, Q, K, V, a, O, s);
+    if (prm->head_dim == 128) return launch_packed_simt<float, 128, kWindow>(prm, Q, K, V, a, O, s);
+    return launch_packed_simt<float, 64, kWindow>(prm, Q, K, V, a, O, s);
   }
   if (!(prm->flags & TCA_FLAG_PREFILL_SIMT))
-    return prm->head_dim == 128 ? launch_packed_tc<128>(prm, Q, K, V, a, O, ws, s) : launch_packed_tc<64>(prm, Q, K, V, a, O, ws, s);
-  if (prm->head_dim == 128) return launch_packed_simt<__nv_bfloat16, 128>(prm, Q, K, V, a, O, s);
-  return launch_packed_simt<__nv_bfloat16, 64>(prm, Q, K, V, a, O, s);
+    return prm->head_dim == 128 ? launch_packed_tc<128, kWindow>(prm, Q, K, V, a, O, ws, s) : launch_packed_tc<64, kWindow>(prm, Q, K, V, a, O, ws, s);
+  if (prm->head_dim == 128) return launch_packed_simt<__nv_bfloat16, 128, kWindow>(prm, Q, K, V, a, O, s);
+  return launch_packed_simt<__nv_bfloat16, 64, kWindow>(prm, Q, K, V, a, O, s);
+}
+
+}  // namespace
+}  // namespace tca
+
+using namespace tca;
+
+extern "C" int tca_attn_packed(const tca_params* prm, const void* Q, const void* K, const void* V, int64_t rows,
+                               const int64_t* seq_start, const int64_t* strides, void* O, void* ws, size_t ws_bytes,
+                               void* stream) {
+  return attn_packed<false>(prm, Q, K, V, rows, seq_start, strides, 0, O, ws, ws_bytes, stream);
+}
+
+extern "C" int tca_attn_window(const tca_params* prm, const void* Q, const void* K, const void* V, int64_t rows,
+                               const int64_t* seq_start, const int64_t* strides, int32_t n_sink, void* O, void* ws,
+                               size_t ws_bytes, void* stream) {
+  return attn_packed<true>(prm, Q, K, V, rows, seq_start, strides, n_sink, O, ws, ws_bytes, stream);
 }

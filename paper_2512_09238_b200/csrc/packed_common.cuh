@@ -14,6 +14,7 @@ struct PackedArgs {
   int64_t rows;                 // rows of every buffer
   const int64_t* seq_start;     // DEVICE [n_seq + 1]
   int n_seq, n_q_heads, n_kv_heads;
+  int window, n_sink;           // tca_attn_window: at most `rows` each
 };
 
 // What one CTA does: query positions [p0, p0 + n_pos) of the sequence that begins at row `row0` and

@@ -1,4 +1,4 @@
-// tca_attn_packed for bf16: the tensor-core kernel.  One CTA takes 2 P consecutive positions of one
+// tca_attn_packed and tca_attn_window for bf16: the tensor-core kernel.  One CTA takes 2 P consecutive positions of one
 // sequence for all G query heads of one KV head, P = 128 / G: query rows are (position, head) pairs, head
 // fastest, so the two blocks of 128 rows are full for any sequence of a few dozen tokens and every K/V
 // tile serves 256 rows.  Q comes as one box of P positions x G heads, whatever the strides.
@@ -17,14 +17,67 @@ namespace {
 // both zero between calls.
 constexpr int kCounterWord = 16, kLeftWord = 32;
 
+// A run of key tiles that lie one behind the other: tile t >= first begins at key 128 t + shift.
+struct KeyRun {
+  int first, shift;
+};
+
+// The key tiles of query positions p0 .. last of a sequence under a window of w keys and S sinks, in the order in which
+// they are taken: those that every row sees whole come first (flash_tc.cuh).  The band begins at key b0: the first that
+// the first row's window holds, or 0 where the sinks reach it; sinks in front of the band have tiles of their own.
+struct WindowTiles {
+  int n, whole;            // tiles; of them whole
+  KeyRun run[5];           // whole sink tiles, whole band tiles, the rest of the sinks, lower and upper edge of the band
+  int rest;                // keys of the third run's tile
+  __host__ __device__ WindowTiles() {}
+  __host__ __device__ WindowTiles(int p0, int last, int w, int sinks) {
+    const int c_lo = p0 - w + 1 > 0 ? p0 - w + 1 : 0;     // first key of the first row's window
+    const int all_lo = last - w + 1 > 0 ? last - w + 1 : 0;   // first key of every row's window
+    const bool apart = sinks < c_lo;
+    const int b0 = apart ? c_lo : 0;
+    const int n_band = (last - b0) / kTcKeys + 1;
+    const int to_diag = (p0 + 1 - b0) / kTcKeys;           // band tiles in front of the diagonal
+    const int in_sinks = apart ? 0 : sinks / kTcKeys < to_diag ? sinks / kTcKeys : to_diag;
+    const int from = (all_lo - b0 + kTcKeys - 1) / kTcKeys;
+    const int a = from > in_sinks ? from : in_sinks;       // band tiles [a, to_diag) are whole
+    const int w0 = apart ? sinks / kTcKeys : in_sinks, w1 = to_diag > a ? to_diag - a : 0;
+    rest = apart ? sinks % kTcKeys : 0;
+    const int r = rest > 0 ? 1 : 0;
+    const int low = (a < n_band ? a : n_band) - in_sinks;  // tiles [in_sinks, a): some row's window begins inside
+    const int up = to_diag > in_sinks + low ? to_diag : in_sinks + low;
+    whole = w0 + w1;
+    n = whole + r + low + (n_band - up);
+    run[0] = KeyRun{0, 0};
+    run[1] = KeyRun{w0, b0 + (a - w0) * kTcKeys};
+    run[2] = KeyRun{whole, (w0 - whole) * kTcKeys};
+    run[3] = KeyRun{whole + r, b0 + (in_sinks - whole - r) * kTcKeys};
+    run[4] = KeyRun{whole + r + low, b0 + (up - whole - r - low) * kTcKeys};
+  }
+  __host__ __device__ int key0(int t) const {
+    int shift = 0;
+    for (int i = 1; i < 5; ++i) shift = t >= run[i].first ? run[i].shift : shift;
+    return t * kTcKeys + shift;
+  }
+  __host__ __device__ bool is_rest(int t) const { return rest > 0 && t == whole; }
+};
+
+template <bool kWindow>
 struct PackedItem {
   int64_t row0;
   int len, p0, kvh;
 };
+template <>
+struct PackedItem<true> {
+  int64_t row0;
+  int len, p0, kvh;
+  WindowTiles tiles;
+};
 
-template <int D>
+template <int D, bool kWindow>
 struct PackedTcSrc {
-  using Item = PackedItem;
+  using Item = PackedItem<kWindow>;
+  static constexpr int kNoted = kWindow ? 6 : 2;
+  static constexpr bool kGap = kWindow;
   const CUtensorMap *mq, *mk, *mv;
   const __nv_bfloat16* V;
   __nv_bfloat16* O;
@@ -32,6 +85,7 @@ struct PackedTcSrc {
   int G, P, max_tiles, unit_major;
   int64_t row0;
   int len, p0, kvh;
+  WindowTiles win;          // kWindow only
 
   PackedFinder finder;      // the producer warp's
   int* held;
@@ -59,13 +113,29 @@ struct PackedTcSrc {
         return false;                        // the numbers without an item are the last ones
       }
       it.p0 = tile * 2 * P;
+      if constexpr (kWindow) it.tiles = WindowTiles(it.p0, min(it.p0 + 2 * P, it.len) - 1, a->window, a->n_sink);
       return true;
     }
   }
-  __device__ __forceinline__ void set(const Item& it) { row0 = it.row0; len = it.len; p0 = it.p0; kvh = it.kvh; }
+  __device__ __forceinline__ void set(const Item& it) {
+    row0 = it.row0; len = it.len; p0 = it.p0; kvh = it.kvh;
+    if constexpr (kWindow) win = it.tiles;
+  }
 
+  __device__ __forceinline__ int key0(int t) const {      // first key of tile t
+    if constexpr (kWindow) return win.key0(t);
+    return t * kTcKeys;
+  }
   __device__ __forceinline__ int last_pos(int h) const { return min(p0 + (h + 1) * P, len) - 1; }
-  __device__ __forceinline__ int tiles(int h) const { return p0 + h * P < len ? last_pos(h) / kTcKeys + 1 : 0; }
+  __device__ __forceinline__ int tiles(int h) const {
+    if (p0 + h * P >= len) return 0;
+    if constexpr (kWindow) {
+      int n = win.n;                       // but for those behind the block's last row, which are the last ones
+      while (n > win.whole && win.key0(n - 1) > last_pos(h)) --n;
+      return n;
+    }
+    return last_pos(h) / kTcKeys + 1;
+  }
   __device__ __forceinline__ int q_bytes(int) const { return D * 2 * G * P; }
   __device__ __forceinline__ void load_q(int h, uint8_t* dst, uint64_t* bar) const {
     for (int half = 0; half < D / 64; ++half)
@@ -73,22 +143,41 @@ struct PackedTcSrc {
   }
   __device__ __forceinline__ void load(int t, bool is_v, uint8_t* dst, uint64_t* bar) const {
     for (int half = 0; half < D / 64; ++half)
-      ptx::tma_load_3d(dst + half * kTcHalfBytes, is_v ? mv : mk, half * 64, int(row0) + t * kTcKeys, kvh, bar);
+      ptx::tma_load_3d(dst + half * kTcHalfBytes, is_v ? mv : mk, half * 64, int(row0) + key0(t), kvh, bar);
   }
   int dp, g;                // this thread's row: position and head within the block
   __device__ __forceinline__ void begin_row(int row) { dp = row / G; g = row % G; }
   __device__ __forceinline__ int row_key(int h) const { return min(p0 + h * P + dp, last_pos(h)); }
-  __device__ __forceinline__ int last(int key, int t) const { return key - t * kTcKeys; }
-  __device__ __forceinline__ int whole_tiles() const { return p0 / kTcKeys; }
-  __device__ __forceinline__ int keys(int h, int t) const { return min(kTcKeys, last_pos(h) + 1 - t * kTcKeys); }
-  // From the tile that holds p0 on, some row does not see some key (at most two tiles: 2 P <= 128, or
-  // P = 128 with p0 a multiple of 256).  Rows past the last position are nobody's: another sequence's, or
-  // none; rows up to p0 are everybody's.
-  __device__ __forceinline__ int clean(int t) const {
-    return t < p0 / kTcKeys ? -1 : min(kTcKeys, min(p0 + 2 * P, len) - t * kTcKeys);
+  __device__ __forceinline__ int last(int key, int t) const {
+    if constexpr (kWindow) { if (win.is_rest(t)) return win.rest - 1; }
+    return key - key0(t);
   }
-  __device__ __forceinline__ int scan_from(int t) const { return max(0, p0 + 1 - t * kTcKeys); }
-  __device__ __forceinline__ int note_slot(int t) const { return t - p0 / kTcKeys; }
+  __device__ __forceinline__ int gap_begin(int t) const { return a->n_sink - key0(t); }
+  __device__ __forceinline__ int gap_end(int key, int t) const { return key - a->window + 1 - key0(t); }
+  __device__ __forceinline__ int whole_tiles() const {
+    if constexpr (kWindow) return win.whole;
+    return p0 / kTcKeys;
+  }
+  __device__ __forceinline__ int keys(int h, int t) const {
+    if constexpr (kWindow) { if (win.is_rest(t)) return win.rest; }
+    return min(kTcKeys, last_pos(h) + 1 - key0(t));
+  }
+  // From the tile that holds p0 on, some row does not see some key (at most two tiles: 2 P <= 128, or
+  // P = 128 with p0 a multiple of 256; with a window at most six, counting its lower edge and the rest of the sinks).
+  // Rows past the last position are nobody's: another sequence's, or none; rows up to p0 are everybody's.
+  __device__ __forceinline__ int clean(int t) const {
+    if constexpr (kWindow) { if (win.is_rest(t)) return win.rest; }
+    return t < whole_tiles() ? -1 : min(kTcKeys, min(p0 + 2 * P, len) - key0(t));
+  }
+  __device__ __forceinline__ int scan_from(int t) const {
+    if constexpr (kWindow) {
+      if (win.is_rest(t)) return win.rest;                 // everybody sees the sinks
+      if (t < win.run[4].first) return 0;
+      if (win.key0(t) <= min(p0 + 2 * P, len) - 1 - a->window) return 0;   // a lower edge as well
+    }
+    return max(0, p0 + 1 - key0(t));
+  }
+  __device__ __forceinline__ int note_slot(int t) const { return t - whole_tiles(); }
 
   template <typename Read>
   __device__ __forceinline__ void store(int h, bool seen, float, float l, const uint32_t* dirty, Read read) const {
@@ -112,10 +201,11 @@ struct PackedTcSrc {
       __syncwarp();                       // a row has been written by the four lanes of its quad
       if (!mine) return;
 #pragma unroll 1
-      for (int i = 0; i < 8; ++i)
+      for (int i = 0; i < 4 * kNoted; ++i)
         for (uint32_t bits = dirty[i]; bits; bits &= bits - 1) {
-          const int key = (p0 / kTcKeys + (i >> 2)) * kTcKeys + (i & 3) * 32 + __ffs(bits) - 1;
+          const int key = key0(whole_tiles() + (i >> 2)) + (i & 3) * 32 + __ffs(bits) - 1;
           if (key > pos) break;
+          if (kWindow && key <= pos - a->window && key >= a->n_sink) continue;
           const __nv_bfloat16* src = V + kvh * a->v.head + (row0 + key) * a->v.row;
 #pragma unroll 1
           for (int k = 0; k < D; ++k) {
@@ -127,14 +217,14 @@ struct PackedTcSrc {
   }
 };
 
-template <int D>
+template <int D, bool kWindow>
 __global__ void __launch_bounds__(kTcThreads, 1)
 packed_tc_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
                  const __grid_constant__ CUtensorMap mv, const __nv_bfloat16* __restrict__ V,
                  const __grid_constant__ PackedArgs args, int max_tiles, int unit_major, float scale_log2e,
                  __nv_bfloat16* __restrict__ O, int* __restrict__ status) {
   extern __shared__ uint8_t packed_tc_smem[];
-  __shared__ TcShared<PackedItem> sh;
+  __shared__ TcShared<PackedItem<kWindow>, PackedTcSrc<D, kWindow>::kNoted> sh;
   __shared__ int held[PackedFinder::kHeld];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(packed_tc_smem) + 1023) & ~uintptr_t(1023));
   if (threadIdx.x == 0) {
@@ -145,7 +235,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
   flash_tc_setup<D>(smem, &sh);
   pdl_wait();
   pdl_launch_dependents();
-  PackedTcSrc<D> src;
+  PackedTcSrc<D, kWindow> src;
   src.mq = &mq; src.mk = &mk; src.mv = &mv;
   src.V = V; src.O = O; src.a = &args;
   src.G = args.n_q_heads / args.n_kv_heads;
@@ -167,7 +257,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
 
 }  // namespace
 
-template <int D>
+template <int D, bool kWindow>
 int launch_packed_tc(const tca_params* prm, const void* Q, const void* K, const void* V, const PackedArgs& a, void* O,
                      void* ws, cudaStream_t s) {
   const int G = a.n_q_heads / a.n_kv_heads, P = kTcRows / G;
@@ -179,23 +269,28 @@ int launch_packed_tc(const tca_params* prm, const void* Q, const void* K, const 
       !encode_map_3d(&mk, K, D, a.rows, a.n_kv_heads, a.k.row, a.k.head, kTcKeys, 1) ||
       !encode_map_3d(&mv, V, D, a.rows, a.n_kv_heads, a.v.row, a.v.head, kTcKeys, 1))
     return TCA_ERR_CUDA;
-  auto kern = packed_tc_kernel<D>;
-  if (allow_smem<packed_tc_kernel<D>>(TcLayout<D>::bytes) != TCA_OK) return TCA_ERR_CUDA;
+  auto kern = packed_tc_kernel<D, kWindow>;
+  if (allow_smem<packed_tc_kernel<D, kWindow>>(TcLayout<D>::bytes) != TCA_OK) return TCA_ERR_CUDA;
   // Items of all heads in one order balance best, but then the resident CTAs read all heads' keys at once;
   // when those are more than half of the L2 the heads go one after another (128K tokens, 8 heads: 120
   // against 135 ms).  Not with more sequences than the finder sorts: their keys are read once or
   // twice anyway if they are short (500 prompts of up to 200 tokens: 460 against 590 us).  A long prompt among so
   // many pays for it: 128K tokens among 127 prompts of 20 tokens 116 ms, among 128 or more 119 to 121 ms.
-  const int unit_major = a.n_seq <= PackedFinder::kHeld && a.rows * a.n_kv_heads * D * 4 > l2_bytes() / 2 ? 1 : 0;
+  // Under a window neighbouring items share their keys, so all heads at once need little of the L2.
+  const int unit_major = !kWindow && a.n_seq <= PackedFinder::kHeld && a.rows * a.n_kv_heads * D * 4 > l2_bytes() / 2 ? 1 : 0;
   const int64_t items = max_tiles * a.n_kv_heads, sms = sm_count();
   return launch_pdl(kern, dim3(unsigned(items < sms ? items : sms)), dim3(kTcThreads), size_t(TcLayout<D>::bytes), s, mq, mk,
                     mv, static_cast<const __nv_bfloat16*>(V), a, int(max_tiles), unit_major,
                     prm->sm_scale * 1.4426950408889634f, static_cast<__nv_bfloat16*>(O), static_cast<int*>(ws));
 }
 
-template int launch_packed_tc<64>(const tca_params*, const void*, const void*, const void*, const PackedArgs&, void*, void*,
-                                  cudaStream_t);
-template int launch_packed_tc<128>(const tca_params*, const void*, const void*, const void*, const PackedArgs&, void*, void*,
-                                   cudaStream_t);
+#define TCA_INSTANTIATE(D, W)                                                                                                   \
+  template int launch_packed_tc<D, W>(const tca_params*, const void*, const void*, const void*, const PackedArgs&, void*, void*, \
+                                      cudaStream_t);
+TCA_INSTANTIATE(64, false)
+TCA_INSTANTIATE(128, false)
+TCA_INSTANTIATE(64, true)
+TCA_INSTANTIATE(128, true)
+#undef TCA_INSTANTIATE
 
 }  // namespace tca

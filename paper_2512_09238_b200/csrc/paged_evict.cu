@@ -1,0 +1,354 @@
+// tca_paged_evict: a unit keeps its sinks, its recent rows and, of the others, those that gathered the most attention
+// weight; the kept rows behind the budget move into the holes in front of it.
+//
+// One cluster of CTAs per unit, each with a run of the unit's slots.  The weights become order-preserving 32-bit keys,
+// held in shared memory; the smallest kept key is found by radix selection, 8 bits at a time, on histograms that the CTAs
+// read from one another's shared memory.  The i-th hole below the budget takes the i-th kept row behind it: sources and
+// destinations are disjoint, so rows move in any order, and no more of them than have to (keeping the order of slots
+// would move all rows behind the first hole, through a staging buffer).  The pairs are put into shared memory by their
+// number, equally many per CTA, so that the copies are dealt evenly wherever the rows lie.
+// Bound by latency for short units, by memory for long ones: 8 bytes a row (weight, position) and 2 (2 d + 8) bytes and more a
+// moved row.
+#include <climits>
+
+#include <cooperative_groups.h>
+
+#include "paged_common.cuh"
+
+namespace tca {
+namespace {
+
+namespace cg = cooperative_groups;
+
+constexpr int kThreads = 512, kWarps = kThreads / 32;
+constexpr int kMaxCluster = 8;
+constexpr int kMostSlots = 1 << 22;      // slots of a unit: one bit each has to fit a cluster's shared memory
+constexpr int kHeld = 12 * 1024;         // slots of a CTA whose key and pool row are held; the others' are read again
+constexpr int kPairs = 4 * 1024;         // moves of a CTA at a time
+constexpr uint32_t kSafe = 0xFFFFFFFFu;  // key of a sink or recent row; a NaN has the one below
+
+struct EvictBuffers {
+  uint4 *K, *V;
+  int32_t* pos;
+  float* mass;
+  int shift;                             // log2 of a row's 16-byte pieces
+};
+
+__device__ __forceinline__ uint32_t mass_key(float x) {
+  if (x != x) return kSafe - 1;
+  const uint32_t u = __float_as_uint(x + 0.f);            // -0 becomes +0
+  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);      // at most that of +infinity, 0xFF800000
+}
+
+struct EvictShared {
+  int max_pos[kMaxCluster], bad[kMaxCluster], safe[kMaxCluster];   // of every CTA of the cluster, written by each
+  int2 counts[kMaxCluster];                                        // holes, kept rows behind the budget
+  int scan[kWarps][2];
+  unsigned hist[2][256];                  // this CTA's; two, so that one barrier per digit is enough
+  unsigned picked;
+  int need, equals, equal_before;         // left to find; keys equal to the threshold, those of the CTAs before
+};
+
+// Dynamic shared memory: keys [held_cap], pool rows [held_cap], moves (from, to) [pair_cap], a bit per slot: kept.
+struct EvictSizes {
+  int held_cap, pair_cap, words;
+  int bytes() const { return held_cap * 8 + pair_cap * 8 + words * 4; }
+};
+
+__device__ __forceinline__ unsigned low_bits(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; }
+
+__global__ void __launch_bounds__(kThreads)
+evict_kernel(const __grid_constant__ EvictBuffers b, const __grid_constant__ PagedArgs args, int n_sink, int n_recent,
+             const int32_t* __restrict__ budgets, EvictSizes sizes) {
+  extern __shared__ __align__(16) uint32_t evict_smem[];
+  __shared__ EvictShared sh;
+  uint32_t* keys = evict_smem;
+  int* rows = reinterpret_cast<int*>(evict_smem + sizes.held_cap);
+  int2* pairs = reinterpret_cast<int2*>(evict_smem + 2 * sizes.held_cap);
+  uint32_t* kept = evict_smem + 2 * sizes.held_cap + 2 * sizes.pair_cap;
+  cg::cluster_group cluster = cg::this_cluster();
+  const int rank = int(cluster.block_rank()), n_ctas = int(cluster.num_blocks());
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int u = int(blockIdx.x) / n_ctas;
+  pdl_wait();
+  pdl_launch_dependents();
+  int4* st = args.state + u;
+  const int len = paged_len(args, st->x), budget = budgets[u];
+  if (len <= budget) return;                              // the whole cluster alike, before any barrier
+  cluster.barrier_arrive();
+  const int per = (len + n_ctas - 1) / n_ctas;
+  const int s0 = min(len, rank * per), n = min(len, s0 + per) - s0, held = min(n, sizes.held_cap);
+
+  // ---- one pass over positions and weights
+  int top = INT_MIN;
+  bool bad = false;
+#pragma unroll 4
+  for (int i = tid; i < n; i += kThreads) {
+    const int row = paged_row(args, u, s0 + i);
+    if (row < 0) { bad = true; continue; }
+    top = max(top, b.pos[row]);
+    if (i < held) {
+      keys[i] = mass_key(b.mass[row]);
+      rows[i] = row;
+    }
+  }
+  top = __reduce_max_sync(0xffffffffu, top);
+  bad = __any_sync(0xffffffffu, bad);
+  if (lane == 0) { sh.scan[warp][0] = top; sh.scan[warp][1] = bad; }
+  sh.hist[tid >> 8][tid & 255] = 0;
+  __syncthreads();
+  cluster.barrier_wait();                                 // every CTA of the cluster runs: its memory can be written
+  if (tid < n_ctas) {
+    int t = INT_MIN, any = 0;
+    for (int w = 0; w < kWarps; ++w) { t = max(t, sh.scan[w][0]); any |= sh.scan[w][1]; }
+    EvictShared* to = cluster.map_shared_rank(&sh, tid);
+    to->max_pos[rank] = t;
+    to->bad[rank] = any;
+  }
+  cluster.sync();
+  int newest = INT_MIN, any_bad = 0;
+  for (int c = 0; c < n_ctas; ++c) { newest = max(newest, sh.max_pos[c]); any_bad |= sh.bad[c]; }
+  if (any_bad) {                                          // the whole cluster alike
+    if (rank == 0 && tid == 0) report_paged(st, kPagedBadPage);
+    return;
+  }
+  const int64_t recent_from = int64_t(newest) - n_recent; // positions above it are recent
+  auto row_of = [&](int i) { return i < held ? rows[i] : paged_row(args, u, s0 + i); };
+  auto key_of = [&](int i) -> uint32_t {                  // of slot s0 + i
+    if (i < held) return keys[i];
+    const int row = paged_row(args, u, s0 + i);
+    return s0 + i < n_sink || b.pos[row] > recent_from ? kSafe : mass_key(b.mass[row]);
+  };
+
+  // ---- safe rows get the highest key; how many are there?
+  int safe = 0;
+#pragma unroll 4
+  for (int i = tid; i < n; i += kThreads) {
+    if (i < held) {
+      const bool is = s0 + i < n_sink || b.pos[rows[i]] > recent_from;
+      if (is) keys[i] = kSafe;
+      safe += is;
+    } else {
+      safe += key_of(i) == kSafe;
+    }
+  }
+  safe = __reduce_add_sync(0xffffffffu, safe);
+  if (lane == 0) sh.scan[warp][0] = safe;
+  __syncthreads();
+  if (tid < n_ctas) {
+    int t = 0;
+    for (int w = 0; w < kWarps; ++w) t += sh.scan[w][0];
+    cluster.map_shared_rank(&sh, tid)->safe[rank] = t;
+  }
+  // ---- radix selection of the need-th largest key among the others
+  uint32_t prefix = 0;
+  int need = 0;
+  for (int digit = 0; digit < 4; ++digit) {
+    const int shift = 24 - 8 * digit;
+    unsigned* hist = sh.hist[digit & 1];
+    for (int i0 = 0; i0 < n; i0 += kThreads) {
+      const int i = i0 + tid;
+      const uint32_t k = i < n ? key_of(i) : kSafe;
+      const bool in = k != kSafe && (digit == 0 || (k >> (shift + 8)) == prefix);
+      // equal digits of a warp are counted together: weights have few different exponents
+      const unsigned active = __ballot_sync(0xffffffffu, in);
+      if (in) {
+        const unsigned d = (k >> shift) & 255u;
+        const unsigned same = __match_any_sync(active, d);
+        if (lane == __ffs(same) - 1) atomicAdd(&hist[d], unsigned(__popc(same)));
+      }
+    }
+    cluster.sync();
+    if (digit == 0) {
+      need = budget;
+      for (int c = 0; c < n_ctas; ++c) need -= sh.safe[c];
+      if (need < 0) {                                     // the whole cluster alike; nobody reads another's memory any more
+        if (rank == 0 && tid == 0) report_paged(st, kPagedBudget);
+        return;
+      }
+    }
+    // the bin at which the count from above reaches need, one bin per thread; if nothing is needed the highest, of
+    // which nothing is kept
+    unsigned total = 0, before = 0, count = 0;
+    if (tid < 256) {
+      for (int c = 0; c < n_ctas; ++c) {
+        const unsigned v = cluster.map_shared_rank(&sh, c)->hist[digit & 1][255 - tid];
+        total += v;
+        if (c < rank) before += v;
+      }
+      count = total;
+#pragma unroll
+      for (int off = 1; off < 32; off <<= 1) {
+        const unsigned t = __shfl_up_sync(0xffffffffu, count, off);
+        if (lane >= off) count += t;
+      }
+      if (lane == 31) sh.scan[warp][0] = int(count);
+    }
+    __syncthreads();
+    if (tid < 256) {
+      for (int w = 0; w < warp; ++w) count += unsigned(sh.scan[w][0]);
+      const int above = int(count - total);
+      if (need > 0 ? int(count) >= need && above < need : tid == 0) {
+        sh.picked = 255 - tid;
+        sh.need = need - above;
+        sh.equals = int(total);
+        sh.equal_before = int(before);
+      }
+      sh.hist[(digit + 1) & 1][tid] = 0;                  // its readers passed the barrier above
+    }
+    __syncthreads();
+    prefix = (prefix << 8) | sh.picked;
+    need = need > 0 ? sh.need : 0;
+  }
+
+  // ---- which slots are kept: keys above the threshold, and of those equal to it the `need` lowest slots
+  const int words = (n + 31) >> 5;
+  const bool tie = need != sh.equals;                     // the whole cluster alike
+  int equals = sh.equal_before;
+  for (int i0 = 0; i0 < n; i0 += kThreads) {
+    const int i = i0 + tid;
+    const uint32_t k = i < n ? key_of(i) : 0u;
+    bool keep = i < n && (k == kSafe || k > prefix);
+    if (!tie) {
+      keep |= i < n && need > 0 && k == prefix;
+    } else if (need > 0) {
+      const unsigned eq = __ballot_sync(0xffffffffu, i < n && k == prefix);
+      __syncthreads();                                    // the counts of the chunk before have been read
+      if (lane == 0) sh.scan[warp][0] = __popc(eq);
+      __syncthreads();
+      int mine = equals;
+      for (int w = 0; w < kWarps; ++w) {
+        if (w < warp) mine += sh.scan[w][0];
+        equals += sh.scan[w][0];
+      }
+      keep |= ((eq >> lane) & 1u) && mine + __popc(eq & low_bits(lane)) < need;
+    }
+    const unsigned word = __ballot_sync(0xffffffffu, keep);
+    if (lane == 0 && (i0 >> 5) + warp < words) kept[(i0 >> 5) + warp] = word;
+  }
+  __syncthreads();
+  // holes below the budget and kept rows behind it, of one word of 32 slots
+  auto holes_of = [&](int w) { return w < words ? ~kept[w] & low_bits(n - w * 32) & low_bits(budget - s0 - w * 32) : 0u; };
+  auto late_of = [&](int w) { return w < words ? kept[w] & ~low_bits(budget - s0 - w * 32) : 0u; };
+  int n_holes = 0, n_late = 0;
+  for (int w = tid; w < words; w += kThreads) {
+    n_holes += __popc(holes_of(w));
+    n_late += __popc(late_of(w));
+  }
+  n_holes = __reduce_add_sync(0xffffffffu, n_holes);
+  n_late = __reduce_add_sync(0xffffffffu, n_late);
+  if (lane == 0) { sh.scan[warp][0] = n_holes; sh.scan[warp][1] = n_late; }
+  __syncthreads();
+  if (tid < n_ctas) {
+    int2 t = make_int2(0, 0);
+    for (int w = 0; w < kWarps; ++w) { t.x += sh.scan[w][0]; t.y += sh.scan[w][1]; }
+    cluster.map_shared_rank(&sh, tid)->counts[rank] = t;
+  }
+  cluster.sync();
+  int hole0 = 0, late0 = 0, moves = 0;
+  for (int c = 0; c < n_ctas; ++c) {
+    if (c < rank) { hole0 += sh.counts[c].x; late0 += sh.counts[c].y; }
+    moves += sh.counts[c].x;                              // as many kept rows lie behind the budget
+  }
+  // ---- the moves, dealt evenly by their number, in rounds if there are very many
+  const int q = min(sizes.pair_cap, (moves + n_ctas - 1) / n_ctas);
+  for (int first = 0; first < moves; first += q * n_ctas) {
+    auto put = [&](int number, int i, bool to) {
+      const int at = number - first;
+      if (at < 0 || at >= q * n_ctas) return;
+      int2* p = cluster.map_shared_rank(pairs, at / q) + at % q;
+      (to ? p->y : p->x) = row_of(i);
+    };
+    int h = hole0, l = late0;                             // numbers before the 16 words at hand
+    for (int w0 = 0; w0 < words; w0 += kWarps) {
+      const int nh = lane < kWarps ? __popc(holes_of(w0 + lane)) : 0, nl = lane < kWarps ? __popc(late_of(w0 + lane)) : 0;
+      const int h_before = __reduce_add_sync(0xffffffffu, lane < warp ? nh : 0), l_before = __reduce_add_sync(0xffffffffu, lane < warp ? nl : 0);
+      const unsigned hb = holes_of(w0 + warp), lb = late_of(w0 + warp);
+      if ((hb >> lane) & 1u) put(h + h_before + __popc(hb & low_bits(lane)), (w0 + warp) * 32 + lane, true);
+      if ((lb >> lane) & 1u) put(l + l_before + __popc(lb & low_bits(lane)), (w0 + warp) * 32 + lane, false);
+      h += __reduce_add_sync(0xffffffffu, nh);
+      l += __reduce_add_sync(0xffffffffu, nl);
+    }
+    cluster.sync();
+    const int mine = min(q, moves - first - rank * q), pieces = mine > 0 ? mine << b.shift : 0;
+    for (int p0 = tid; p0 < pieces; p0 += 4 * kThreads) {
+      uint4 kv[4], vv[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int p = p0 + i * kThreads;
+        if (p < pieces) {
+          const int64_t at = (int64_t(pairs[p >> b.shift].x) << b.shift) + (p & ((1 << b.shift) - 1));
+          kv[i] = b.K[at];
+          vv[i] = b.V[at];
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int p = p0 + i * kThreads;
+        if (p < pieces) {
+          const int64_t at = (int64_t(pairs[p >> b.shift].y) << b.shift) + (p & ((1 << b.shift) - 1));
+          b.K[at] = kv[i];
+          b.V[at] = vv[i];
+        }
+      }
+    }
+    for (int p = tid; p < mine; p += kThreads) {
+      const int2 m = pairs[p];
+      b.pos[m.y] = b.pos[m.x];
+      b.mass[m.y] = b.mass[m.x];
+    }
+    cluster.sync();
+  }
+  if (rank == 0 && tid == 0) st->x = budget;
+}
+
+}  // namespace
+}  // namespace tca
+
+using namespace tca;
+
+extern "C" int tca_paged_evict(const tca_params* prm, tca_paged_desc* c, int32_t n_sink, int32_t n_recent, const int32_t* budget,
+                               void* stream) {
+  const int st = check_paged(prm, c);
+  if (st != TCA_OK) return st;
+  TCA_CHECK_ARG(budget && aligned(budget, 4) && n_sink >= 0 && n_recent >= 0);
+  const int64_t slots = int64_t(c->max_pages) * c->page_size;
+  if (slots > kMostSlots) return TCA_ERR_UNSUPPORTED;
+  // CTAs per unit: as many as leave each a thousand slots, while the units do not fill the SMs twice over (and as many as
+  // the bits of very long units need)
+  int n_ctas = 1;
+  while (n_ctas < kMaxCluster && slots > int64_t(n_ctas) * 1024 &&
+         (c->n_units * n_ctas <= sm_count() || slots > int64_t(n_ctas) * (kMostSlots / kMaxCluster)))
+    n_ctas *= 2;
+  const int per = int((slots + n_ctas - 1) / n_ctas);
+  EvictSizes sizes;
+  sizes.held_cap = ((per < kHeld ? per : kHeld) + 3) & ~3;
+  sizes.pair_cap = per / 2 + 1 < kPairs ? per / 2 + 1 : kPairs;
+  sizes.words = (per + 31) / 32;
+  EvictBuffers b;
+  b.K = static_cast<uint4*>(c->k);
+  b.V = static_cast<uint4*>(c->v);
+  b.pos = c->pos;
+  b.mass = c->mass;
+  b.shift = 0;
+  while ((16 << b.shift) < int64_t(prm->head_dim) * int64_t(elt_size(prm->dtype))) ++b.shift;
+  // what the largest call can ask for: 12K slots held, 4K moves, a bit for each of 512K slots
+  constexpr int kMostBytes = kHeld * 8 + kPairs * 8 + kMostSlots / 8 / 8;
+  static_assert(kMostBytes + int(sizeof(EvictShared)) + 1024 <= 227 * 1024, "shared memory");
+  if (allow_smem<evict_kernel>(kMostBytes) != TCA_OK) return TCA_ERR_CUDA;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(unsigned(c->n_units * n_ctas));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = size_t(sizes.bytes());
+  cfg.stream = static_cast<cudaStream_t>(stream);
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = unsigned(n_ctas);
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  TCA_CHECK_CUDA(cudaLaunchKernelEx(&cfg, evict_kernel, b, paged_args(c), int(n_sink), int(n_recent), budget, sizes));
+  return TCA_OK;
+}

@@ -45,6 +45,7 @@ namespace {
 
 template <typename T, int D>
 struct TreeSrc {
+  static constexpr bool kGap = false;
   const T *q_rows, *Kc, *Vc;      // first query row of this CTA; the cache
   int n;                          // query rows here
   SliceTiles<SimtSmall::kKeys> tiles;

@@ -19,6 +19,8 @@ struct TreeItem {
 template <int D, bool kShared>
 struct TreeTcSrc {
   using Item = TreeItem;
+  static constexpr int kNoted = 2;
+  static constexpr bool kGap = false;
   const CUtensorMap *mq, *mk, *mv;
   const int64_t* state;
   int n_units;
