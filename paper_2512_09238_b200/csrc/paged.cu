@@ -5,10 +5,11 @@
 // units are cut into one equal share per SM (paged_common.cuh); a CTA streams its share through a shared-memory ring.
 //   producer warp   reads the page table four steps ahead and brings one box per page (K or V: all columns of up to
 //                   128 rows, 128-byte swizzle; a page without a visible row is not read)
-//   8 consumer warps, each 16 rows of every step of 128 and a private online softmax.  bf16: ldmatrix and
-//                   mma.sync, the G <= 8 heads are the rows of the A tile (tcgen05 needs 64 of them).  fp32: FP32 pipes,
-//                   half a row of K per lane, then D / 32 columns of V per lane.
-// At the end of a unit's piece the eight states are merged; a piece that is the whole unit gives the result, others
+//   two teams of 4 consumer warps, which take the pieces of the share in turn; a warp has 32 rows of every step
+//                   of 128 and a private online softmax.  bf16: ldmatrix and
+//                   mma.sync, the G <= 8 heads are the columns of the products (tcgen05 needs 64 rows of queries).
+//                   fp32: FP32 pipes, a row of K per lane, then D / 32 columns of V per lane.
+// At the end of a unit's piece the four states are merged; a piece that is the whole unit gives the result, others
 // partial results that a second kernel merges in order.  Statistics and accumulators are fp32; bf16 weights are rounded
 // to bf16 before they meet the values (half a step, 2^-8 of a weight), the row sum adds the unrounded ones.
 // A slot nobody sees has no influence whatever it holds: its score is replaced, its value row is not read from the ring.
@@ -41,45 +42,72 @@ int check_paged(const tca_params* prm, const tca_paged_desc* c) {
 
 namespace {
 
-constexpr int kConsumers = 256, kThreads = kConsumers + 32, kWarps = kConsumers / 32;
-constexpr int kList = 64;
-constexpr int kMergeStates = 4;      // warp states in shared memory at a time
+constexpr int kConsumers = 128, kWarps = kConsumers / 32;   // of a team
+constexpr int kWarpRows = kPagedStep / kWarps;      // of a step
+static_assert(kWarpRows == 32, "two groups of 16 rows, one lane per row");
+constexpr int kList = 64;            // pieces of a round
+constexpr int kPageBatches = 7;      // batches of page numbers on their way
+constexpr int kGroups = kPagedStep / 16;            // groups of 16 rows of a step: none is on two pages
+__host__ __device__ constexpr int state_row(int d) { return d + 4; }   // floats per head of a warp's state in shared memory
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr double kL2Share = 0.45;
 
-PagedPlan paged_plan(const tca_params*) {
-  PagedPlan p;
-  p.n_shares = sm_count();
-  p.min_share = 1;
-  p.lead = 1;
-  return p;
-}
-
-PagedWs paged_ws_layout(const tca_params* prm, const tca_paged_desc* c, const PagedPlan& p, bool weights, void* ws) {
+PagedWs paged_ws_layout(const tca_params* prm, const tca_paged_desc* c, bool weights, void* ws) {
   PagedWs w;
-  const size_t U = size_t(c->n_units), G = size_t(prm->n_q_heads / prm->n_kv_heads), n = (p.n_shares + U) * G;
+  const size_t U = size_t(c->n_units), G = size_t(prm->n_q_heads / prm->n_kv_heads), n = (size_t(sm_count()) + U) * G;
   char* base = static_cast<char*>(ws);
   size_t at = kPagedHeaderBytes;
   w.status = reinterpret_cast<int*>(base);
-  w.table = reinterpret_cast<int2*>(base + at);
-  at += align_up(U * sizeof(int2), 256);
+  w.records = reinterpret_cast<PagedRecord*>(base + at);
+  at += align_up((U + 1) * sizeof(PagedRecord), 256);
   w.ml = reinterpret_cast<float2*>(base + at);
   at += align_up(n * sizeof(float2), 256);
   w.acc = reinterpret_cast<float*>(base + at);
   at += align_up(n * prm->head_dim * sizeof(float), 256);
-  w.score = weights ? reinterpret_cast<float*>(base + at) : nullptr;
-  if (weights) at += align_up(size_t(c->n_pages) * c->page_size * G * sizeof(float), 256);
+  w.score = nullptr;
+  w.steps = nullptr;
+  if (weights) {
+    w.score = reinterpret_cast<float*>(base + at);
+    at += align_up(size_t(c->n_pages) * c->page_size * G * sizeof(float), 256);
+    w.steps = reinterpret_cast<PagedStepRecord*>(base + at);
+    at += align_up(U * (size_t(c->max_pages) * c->page_size / kPagedStep + 2) * sizeof(PagedStepRecord), 256);
+  }
   w.bytes = at;
   return w;
 }
 
-template <typename T, int D>
+// GT: heads of the group, at most.
+template <typename T, int D, int GT>
 struct PagedRing {
   static constexpr int kBoxes = D * int(sizeof(T)) / 128;        // 128-byte column blocks of a row
   static constexpr int kStageBytes = kPagedStep * 128 * kBoxes;
-  static constexpr int kStages = (192 * 1024) / kStageBytes > 12 ? 12 : (192 * 1024) / kStageBytes;
-  static constexpr int kScratch = kMergeStates * kMaxGroup * D * 4;
-  static constexpr int kSmemBytes = kStages * kStageBytes + kScratch + 1024;
+  // Teams of consumers.  They take pieces in turn, so that one streams while the other begins and ends one (3500 clocks for
+  // a piece of one step, whose 64 KB take 2300).
+  static constexpr int kTeams = kStageBytes == 65536 && GT == 8 ? 1 : 2;
+  static constexpr int kThreads = kTeams * kConsumers + 32;
+  static constexpr int kState = kWarps * GT * state_row(D) * 4;  // a team's states
+  static constexpr int kQueryBytes = GT * D * int(sizeof(T));
+  // Queries of the pieces that the producer is ahead by: a piece has two stages or more.
+  static constexpr int queries(int stages) { return stages / 2 + 2; }
+  static constexpr int bytes(int stages) { return stages * kStageBytes + kTeams * kState + queries(stages) * kQueryBytes + 1024; }
+  static constexpr int most() {
+    int n = 2;
+    while (n < 12 && bytes(n + 1) <= 227 * 1024 - 5632) ++n;
+    return n;
+  }
+  static constexpr int kStages = most(), kQueries = queries(kStages), kSmemBytes = bytes(kStages);
 };
+
+// Barrier of a team.
+__device__ __forceinline__ void team_sync(int team) {
+  asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "n"(kConsumers) : "memory");
+}
+__device__ __forceinline__ void cp_async_4(int* smem_dst, const int* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(ptx::smem_u32(smem_dst)), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kPending>
+__device__ __forceinline__ void cp_async_pending() { asm volatile("cp.async.wait_group %0;" ::"n"(kPending) : "memory"); }
 
 // Byte offset of 16-byte piece `piece` of row r of a page box of `rows` rows.
 __device__ __forceinline__ uint32_t box_at(int rows, int r, int piece) {
@@ -95,133 +123,162 @@ __device__ __forceinline__ void ldm_x4_trans(uint32_t (&r)[4], uint32_t addr) {
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
 }
 __device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile(
+  asm(
       "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
       "{%0, %1, %2, %3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// A warp's softmax state over its 16 rows of every step.  score(): the rows' scores against the G heads and the new
-// maximum and sum; value(): the outputs.  Both get the warp's rows in the ring (base of their page box, its rows, first
-// row) and which of the 16 are visible.
+// A warp's softmax state over its 32 rows of every step.  score(): the rows' scores against the G heads and their weights;
+// value(): the outputs.  Both get where the warp's two groups of 16 rows lie in the ring (base of their page box, first row
+// in it) and which rows are visible.  The maximum that weights refer to moves only when a score is more than 2^8 above it,
+// so that a step needs one vote and no reduction; sums stay per lane until the piece is done.
+struct WarpPlace {
+  uint32_t base[2];
+  int r0[2], box_rows;
+};
+constexpr float kGrow = 8.f;
+
 template <typename T, int D, int GT>
 struct WarpRows;
 
+// bf16: S^T = K Q^T and O^T = V^T P^T, so that the A tiles are full (16 keys, 16 columns) and the 8 columns of B are the
+// heads; P^T is S^T transposed within 8 x 8 blocks.  A lane holds keys lane / 4 (+ 8) of heads 2 (lane % 4) (+ 1) of the
+// scores, columns 16 j + lane / 4 (+ 8) of the same heads of the outputs.
 template <int D, int GT>
 struct WarpRows<__nv_bfloat16, D, GT> {
-  static constexpr int ND = D / 8, KC = D / 16;
-  uint32_t qa[KC][2];
-  float o[ND][4], m, l;      // heads gq: entries 0 and 1 (the upper half of the A tile is zero)
-  float x[4], corr;          // this step: scores of keys kq, kq + 1, 8 + kq, 9 + kq, in log2 units
-  uint32_t pa[2];
-  int gq, kq, lane, G;
+  static constexpr int KC = D / 16;
+  uint32_t q[KC][2];
+  float o[KC][4], m[2], l[2];
+  float x[2][4];             // [group of rows][key, head]: in log2 units
+  uint32_t p[2][2];
+  int lane, G;
 
-  __device__ __forceinline__ void begin(const __nv_bfloat16* q, int heads, const float*) {
+  __device__ __forceinline__ void begin(const __nv_bfloat16* queries, int heads) {   // shared memory [heads][D]
     lane = threadIdx.x & 31;
-    gq = lane >> 2;
-    kq = (lane & 3) * 2;
     G = heads;
+    const int g = lane >> 2, k = (lane & 3) * 2;
 #pragma unroll
     for (int c = 0; c < KC; ++c) {
-      qa[c][0] = qa[c][1] = 0u;
-      if (gq < G) {
-        const __nv_bfloat16* p = q + size_t(gq) * D + c * 16 + kq;
-        qa[c][0] = *reinterpret_cast<const uint32_t*>(p);
-        qa[c][1] = *reinterpret_cast<const uint32_t*>(p + 8);
+      const __nv_bfloat16* at = queries + min(g, G - 1) * D + c * 16 + k;
+      q[c][0] = *reinterpret_cast<const uint32_t*>(at);
+      q[c][1] = *reinterpret_cast<const uint32_t*>(at + 8);
+      o[c][0] = o[c][1] = o[c][2] = o[c][3] = 0.f;
+    }
+    m[0] = m[1] = -INFINITY;
+    l[0] = l[1] = 0.f;
+  }
+  __device__ __forceinline__ void score(const WarpPlace& w, uint32_t stage, unsigned visible, float scale_log2e) {
+    float s[2][2][4];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[t][0][i] = s[t][1][i] = 0.f;
+    // A = 16 keys x 16 columns: matrices (keys 0-7, columns 0-7), (8-15, 0-7), (0-7, 8-15), (8-15, 8-15)
+    // (all loads first: a load waits its turn behind the product before it.  A group nobody sees is read for nothing)
+    const int r = lane & 15, piece = lane >> 4;
+    uint32_t a[2][KC][4];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int c = 0; c < KC; ++c) ldm_x4(a[t][c], w.base[t] + stage + box_at(w.box_rows, w.r0[t] + r, c * 2 + piece));
+#pragma unroll
+    for (int c = 0; c < KC; ++c)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) mma_16816(s[t][c & 1], a[t][c], q[c][0], q[c][1]);
+    float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int key = 16 * t + (lane >> 2) + (i >> 1) * 8;
+        x[t][i] = (visible >> key) & 1u ? (s[t][0][i] + s[t][1][i]) * scale_log2e : -INFINITY;
+        top[i & 1] = fmaxf(top[i & 1], x[t][i]);
+      }
+    if (__any_sync(0xffffffffu, top[0] > m[0] + kGrow || top[1] > m[1] + kGrow)) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int off = 4; off < 32; off <<= 1) top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], off));
+        if (top[h] > m[h] + kGrow) {
+          const float alpha = ptx::fast_exp2(m[h] - top[h]);
+          l[h] *= alpha;
+#pragma unroll
+          for (int c = 0; c < KC; ++c) { o[c][h] *= alpha; o[c][2 + h] *= alpha; }
+          m[h] = top[h];
+        }
       }
     }
+    const float from[2] = {m[0] == -INFINITY ? 0.f : m[0], m[1] == -INFINITY ? 0.f : m[1]};
 #pragma unroll
-    for (int j = 0; j < ND; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
-    m = -INFINITY;
-    l = 0.f;
-  }
-  __device__ __forceinline__ void score(uint32_t base, int rows, int r0, unsigned visible, float scale_log2e) {
-    float s[2][4];
+    for (int t = 0; t < 2; ++t) {
+      float e[4];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) s[t][0] = s[t][1] = s[t][2] = s[t][3] = 0.f;
-    const int row = r0 + (lane >> 4) * 8 + (lane & 7), piece = (lane >> 3) & 1;
+      for (int i = 0; i < 4; ++i) {
+        e[i] = ptx::fast_exp2(x[t][i] - from[i & 1]);
+        l[i & 1] += e[i];
+      }
 #pragma unroll
-    for (int c = 0; c < KC; ++c) {
-      uint32_t b[4];
-      ldm_x4(b, base + box_at(rows, row, c * 2 + piece));
-      const uint32_t a[4] = {qa[c][0], 0u, qa[c][1], 0u};
-      mma_16816(s[0], a, b[0], b[1]);
-      mma_16816(s[1], a, b[2], b[3]);
+      for (int k = 0; k < 2; ++k)
+        asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(p[t][k]) : "r"(ptx::pack_bf16x2(e[2 * k], e[2 * k + 1])));
     }
-    float mx = -INFINITY;
+  }
+  // 16 rows' scores, [head][16]
+  __device__ __forceinline__ void leave_scores(int t, float* out) const {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      x[i] = (visible >> ((i >> 1) * 8 + kq + (i & 1))) & 1u ? s[i >> 1][i & 1] * scale_log2e : -INFINITY;
-      mx = fmaxf(mx, x[i]);
+      const int g = (lane & 3) * 2 + (i & 1);
+      if (g < G) out[g * 16 + (lane >> 2) + (i >> 1) * 8] = x[t][i];
     }
-    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-    const float m_new = fmaxf(m, mx), from = m_new == -INFINITY ? 0.f : m_new;
-    corr = exp2f(m - from);
-    float p[4], sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { p[i] = exp2f(x[i] - from); sum += p[i]; }
-    sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-    sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-    l = l * corr + sum;
-    m = m_new;
-    pa[0] = ptx::pack_bf16x2(p[0], p[1]);
-    pa[1] = ptx::pack_bf16x2(p[2], p[3]);
-  }
-  // the 16 rows' scores, [head][16]
-  __device__ __forceinline__ void leave_scores(float* out) const {
-    if (gq >= G) return;
-    *reinterpret_cast<float2*>(out + gq * 16 + kq) = make_float2(x[0], x[1]);
-    *reinterpret_cast<float2*>(out + gq * 16 + 8 + kq) = make_float2(x[2], x[3]);
   }
   // lanes of a row nobody sees load 16 bytes of zeros instead: zero times an infinity is not zero
-  __device__ __forceinline__ void value(uint32_t base, int rows, int r0, unsigned visible, uint32_t zeros) {
-    const int r = ((lane >> 3) & 1) * 8 + (lane & 7), half = lane >> 4;
-    const uint32_t seen = (visible >> r) & 1u;
-    const uint32_t from = seen ? base : zeros;
+  __device__ __forceinline__ void value(const WarpPlace& w, uint32_t stage, unsigned visible, uint32_t zeros) {
+    // A = 16 columns x 16 keys: matrices (columns 0-7, keys 0-7), (8-15, 0-7), (0-7, 8-15), (8-15, 8-15), each stored by keys
+    const int r = (lane >> 4) * 8 + (lane & 7), piece = (lane >> 3) & 1;
+    uint32_t a[2][KC][4];
 #pragma unroll
-    for (int j = 0; j < ND; j += 2) {
-      uint32_t b[4];
-      ldm_x4_trans(b, from + seen * box_at(rows, r0 + r, j + half));
-      o[j][0] *= corr; o[j][1] *= corr;
-      o[j + 1][0] *= corr; o[j + 1][1] *= corr;
-      const uint32_t a[4] = {pa[0], 0u, pa[1], 0u};
-      mma_16816(o[j], a, b[0], b[1]);
-      mma_16816(o[j + 1], a, b[2], b[3]);
+    for (int t = 0; t < 2; ++t) {
+      const uint32_t seen = (visible >> (16 * t + r)) & 1u, base = seen ? w.base[t] + stage : zeros;
+#pragma unroll
+      for (int c = 0; c < KC; ++c) ldm_x4_trans(a[t][c], base + seen * box_at(w.box_rows, w.r0[t] + r, c * 2 + piece));
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int c = 0; c < KC; ++c) mma_16816(o[c], a[t][c], p[t][0], p[t][1]);
+  }
+  // To shared memory: outputs [G][kStateRow], maxima and sums [G].
+  __device__ __forceinline__ void leave(float* out, float* ms, float* ls) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int off = 4; off < 32; off <<= 1) l[h] += __shfl_xor_sync(0xffffffffu, l[h], off);
+      const int g = (lane & 3) * 2 + h;
+      if (g >= G) continue;
+#pragma unroll
+      for (int c = 0; c < KC; ++c) {
+        out[g * state_row(D) + c * 16 + (lane >> 2)] = o[c][h];
+        out[g * state_row(D) + c * 16 + (lane >> 2) + 8] = o[c][2 + h];
+      }
+      if (lane < 4) { ms[g] = m[h]; ls[g] = l[h]; }
     }
   }
-  // f(head, column, value): every element of the state that this lane holds
-  template <typename F>
-  __device__ __forceinline__ void each(F f) {
-    if (gq >= G) return;
-#pragma unroll
-    for (int j = 0; j < ND; ++j) {
-      f(gq, j * 8 + kq, o[j][0]);
-      f(gq, j * 8 + kq + 1, o[j][1]);
-    }
-  }
-  __device__ __forceinline__ bool stats_lane(int g) const { return g == gq && (lane & 3) == 0; }
-  __device__ __forceinline__ float& max_of(int) { return m; }
-  __device__ __forceinline__ float& sum_of(int) { return l; }
-  // heads whose statistics this lane holds
-  __device__ __forceinline__ int head0() const { return gq; }
-  __device__ __forceinline__ int head1() const { return min(gq + 1, G); }
 };
 
-// fp32: lanes 0-15 hold the first half of the 16 rows' columns for the scores, lanes 16-31 the second; for the outputs a
-// lane owns D / 32 columns.  The queries lie in shared memory.  GT: the group, up to a power of two (the heads behind it are zero).
+// fp32: a lane is a row for the scores and owns D / 32 columns of the outputs.  GT: the group, up to a power of two (the
+// heads behind it repeat the last one and are not written).
 template <int D, int GT>
 struct WarpRows<float, D, GT> {
   static constexpr int E = D / 32;
-  const float* q;            // shared memory [GT][D]
-  float o[GT][E], m[GT], l[GT], x[GT], p[GT], corr[GT];
+  const float* q;            // shared memory [heads][D]
+  float o[GT][E], m[GT], l[GT], x[GT], p[GT];
   int lane, G;
 
-  __device__ __forceinline__ void begin(const float*, int heads, const float* q_shared) {
+  __device__ __forceinline__ void begin(const float* queries, int heads) {
     lane = threadIdx.x & 31;
     G = heads;
-    q = q_shared;
+    q = queries;
 #pragma unroll
     for (int g = 0; g < GT; ++g) {
       m[g] = -INFINITY;
@@ -230,103 +287,114 @@ struct WarpRows<float, D, GT> {
       for (int e = 0; e < E; ++e) o[g][e] = 0.f;
     }
   }
-  __device__ __forceinline__ void score(uint32_t base, int rows, int r0, unsigned visible, float scale_log2e) {
-    const int r = lane & 15, half = lane >> 4;
-    float s[GT];
+  __device__ __forceinline__ void score(const WarpPlace& w, uint32_t stage, unsigned visible, float scale_log2e) {
+    const uint32_t base = (lane < 16 ? w.base[0] : w.base[1]) + stage;
+    const int row = (lane < 16 ? w.r0[0] : w.r0[1]) + (lane & 15);
+    float s[GT], s2[GT];                   // two chains each
 #pragma unroll
-    for (int g = 0; g < GT; ++g) s[g] = 0.f;
-#pragma unroll 4
-    for (int c = 0; c < D / 8; ++c) {
-      const int piece = half * (D / 8) + c;
+    for (int g = 0; g < GT; ++g) s[g] = s2[g] = 0.f;
+#pragma unroll (GT <= 2 ? 8 : 4)
+    for (int c = 0; c < D / 4; ++c) {
       float4 k;
-      asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(k.x), "=f"(k.y), "=f"(k.z), "=f"(k.w) : "r"(base + box_at(rows, r0 + r, piece)));
+      asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(k.x), "=f"(k.y), "=f"(k.z), "=f"(k.w) : "r"(base + box_at(w.box_rows, row, c)));
 #pragma unroll
       for (int g = 0; g < GT; ++g) {
-        const float4 v = *reinterpret_cast<const float4*>(q + g * D + piece * 4);
-        s[g] = fmaf(v.w, k.w, fmaf(v.z, k.z, fmaf(v.y, k.y, fmaf(v.x, k.x, s[g]))));
+        const float4 v = *reinterpret_cast<const float4*>(q + min(g, G - 1) * D + c * 4);
+        s[g] = fmaf(v.y, k.y, fmaf(v.x, k.x, s[g]));
+        s2[g] = fmaf(v.w, k.w, fmaf(v.z, k.z, s2[g]));
+      }
+    }
+    bool grew = false;
+#pragma unroll
+    for (int g = 0; g < GT; ++g) {
+      x[g] = (visible >> lane) & 1u ? (s[g] + s2[g]) * scale_log2e : -INFINITY;
+      grew |= x[g] > m[g] + kGrow;
+    }
+    if (__any_sync(0xffffffffu, grew)) {
+#pragma unroll
+      for (int g = 0; g < GT; ++g) {
+        float top = x[g];
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+        if (top > m[g] + kGrow) {
+          const float alpha = exp2f(m[g] - top);
+          l[g] *= alpha;
+#pragma unroll
+          for (int e = 0; e < E; ++e) o[g][e] *= alpha;
+          m[g] = top;
+        }
       }
     }
 #pragma unroll
     for (int g = 0; g < GT; ++g) {
-      s[g] += __shfl_xor_sync(0xffffffffu, s[g], 16);
-      x[g] = (visible >> r) & 1u ? s[g] * scale_log2e : -INFINITY;
-      float mx = x[g];
-#pragma unroll
-      for (int off = 8; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
-      const float m_new = fmaxf(m[g], mx), from = m_new == -INFINITY ? 0.f : m_new;
-      corr[g] = exp2f(m[g] - from);
-      p[g] = exp2f(x[g] - from);
-      float sum = p[g];
-#pragma unroll
-      for (int off = 8; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
-      l[g] = l[g] * corr[g] + sum;
-      m[g] = m_new;
+      p[g] = exp2f(x[g] - (m[g] == -INFINITY ? 0.f : m[g]));
+      l[g] += p[g];
     }
   }
-  __device__ __forceinline__ void leave_scores(float* out) const {
-    if (lane >= 16) return;
+  __device__ __forceinline__ void leave_scores(int t, float* out) const {
+    if (lane >> 4 != t) return;
 #pragma unroll
     for (int g = 0; g < GT; ++g)
-      if (g < G) out[g * 16 + lane] = x[g];
+      if (g < G) out[g * 16 + (lane & 15)] = x[g];
   }
-  __device__ __forceinline__ void value(uint32_t base, int rows, int r0, unsigned visible, uint32_t) {
+  __device__ __forceinline__ void value(const WarpPlace& w, uint32_t stage, unsigned visible, uint32_t zeros) {
 #pragma unroll
-    for (int g = 0; g < GT; ++g)
+    for (int t = 0; t < 2; ++t)
+#pragma unroll 8
+      for (int r = 0; r < 16; ++r) {
+        // a row nobody sees has weight 0; its values are not read
+        float v[E];
+        const uint32_t seen = (visible >> (16 * t + r)) & 1u;
+        const uint32_t from = w.base[t] + stage + box_at(w.box_rows, w.r0[t] + r, E == 4 ? lane : lane >> 1) + (E == 4 ? 0 : (lane & 1) * 8);
+        const uint32_t at = zeros + seen * (from - zeros);
+        if constexpr (E == 4)
+          asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(at));
+        else
+          asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v[0]), "=f"(v[1]) : "r"(at));
 #pragma unroll
-      for (int e = 0; e < E; ++e) o[g][e] *= corr[g];
-#pragma unroll 4
-    for (int r = 0; r < 16; ++r) {
-      if (!((visible >> r) & 1u)) continue;     // the same for the whole warp
-      float v[E];
-      const uint32_t at = base + box_at(rows, r0 + r, E == 4 ? lane : lane >> 1);
-      if constexpr (E == 4)
-        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(at));
-      else
-        asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v[0]), "=f"(v[1]) : "r"(at + (lane & 1) * 8));
+        for (int g = 0; g < GT; ++g) {
+          const float wt = __shfl_sync(0xffffffffu, p[g], 16 * t + r);
 #pragma unroll
-      for (int g = 0; g < GT; ++g) {
-        const float w = __shfl_sync(0xffffffffu, p[g], r);
-#pragma unroll
-        for (int e = 0; e < E; ++e) o[g][e] = fmaf(w, v[e], o[g][e]);
+          for (int e = 0; e < E; ++e) o[g][e] = fmaf(wt, v[e], o[g][e]);
+        }
       }
+  }
+  __device__ __forceinline__ void leave(float* out, float* ms, float* ls) {
+#pragma unroll
+    for (int g = 0; g < GT; ++g) {
+#pragma unroll
+      for (int off = 16; off > 0; off >>= 1) l[g] += __shfl_xor_sync(0xffffffffu, l[g], off);
+      if (g >= G) continue;
+#pragma unroll
+      for (int e = 0; e < E; ++e) out[g * state_row(D) + lane * E + e] = o[g][e];
+      if (lane == 0) { ms[g] = m[g]; ls[g] = l[g]; }
     }
   }
-  template <typename F>
-  __device__ __forceinline__ void each(F f) {
-#pragma unroll
-    for (int g = 0; g < GT; ++g)
-      if (g < G)
-#pragma unroll
-        for (int e = 0; e < E; ++e) f(g, lane * E + e, o[g][e]);
-  }
-  __device__ __forceinline__ bool stats_lane(int) const { return lane == 0; }
-  __device__ __forceinline__ float& max_of(int g) { return m[g]; }
-  __device__ __forceinline__ float& sum_of(int g) { return l[g]; }
-  __device__ __forceinline__ int head0() const { return 0; }
-  __device__ __forceinline__ int head1() const { return GT; }
 };
 
 template <typename T, int D, int GT>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(PagedRing<T, D, GT>::kThreads, 1)
 paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const T* __restrict__ q,
-             const __grid_constant__ PagedArgs args, int G, int window, int n_sink, float scale_log2e, PagedPlan plan, PagedWs ws,
-             T* __restrict__ O) {
-  using Ring = PagedRing<T, D>;
-  constexpr int kStages = Ring::kStages;
+             const __grid_constant__ PagedArgs args, int G, int window, int n_sink, float scale_log2e, int64_t l2_keep, PagedWs ws, T* __restrict__ O) {
+  using Ring = PagedRing<T, D, GT>;
+  constexpr int kStages = Ring::kStages, kTeams = Ring::kTeams;
   extern __shared__ uint8_t paged_smem[];
   uint8_t* ring_buf = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(paged_smem) + 1023) & ~uintptr_t(1023));
-  float* scratch = reinterpret_cast<float*>(ring_buf + kStages * Ring::kStageBytes);
+  uint8_t* states = ring_buf + kStages * Ring::kStageBytes;
+  uint8_t* query_buf = states + kTeams * Ring::kState;
   __shared__ BulkRing<kStages> ring;
-  __shared__ PagedDeal<kThreads, kList> deal;
-  __shared__ int abort_word, stop_word;
+  __shared__ PagedDeal<kTeams * kConsumers, kList> deal;
+  __shared__ int abort_word;
   __shared__ __align__(16) uint32_t zeros[4];
-  __shared__ __align__(16) float s_q[GT > 0 ? GT * D : 4];
-  __shared__ float s_m[kMergeStates][kMaxGroup], s_l[kMergeStates][kMaxGroup];
-  __shared__ int group_row[kStages][kWarps];      // a stage's pool rows / 16; -1: not a page of the pool
+  __shared__ uint64_t query_full[Ring::kQueries];
+  __shared__ int page_buf[kPageBatches + 1][32];
+  __shared__ float s_m[kTeams][kWarps][kMaxGroup], s_l[kTeams][kWarps][kMaxGroup];
+  __shared__ int group_row[kStages][kGroups];      // a stage's pool rows / 16; -1: not a page of the pool
   volatile int* abort_flag = &abort_word;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
-    ring.init(kWarps);
+    for (int i = 0; i < Ring::kQueries; ++i) ptx::mbar_init(&query_full[i], 1);
+    ring.init(kTeams * kWarps);
     abort_word = 0;
     zeros[0] = zeros[1] = zeros[2] = zeros[3] = 0u;
     ptx::tma_prefetch_desc(&map_k);
@@ -334,35 +402,69 @@ paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
   }
   pdl_wait();
   pdl_launch_dependents();
-  if (tid == 0) stop_word = stops_call(*reinterpret_cast<volatile int*>(ws.status));
+  // Looked at only where results are written: the load takes up to 2 us, and the first request does not wait for it.
+  const int found_status = *reinterpret_cast<const volatile int*>(ws.status);
   const int share = int(blockIdx.x);
   const int box_rows = min(1 << args.page_shift, kPagedStep);      // rows of a box
+  // A lane of the producer warp reads the page of one group of 16 rows: of steps 0 .. 3 of a batch, group lane % 8.  Pages
+  // come asynchronously, kPageBatches batches ahead: a trip to memory takes 2 to 3 us while everybody streams, as
+  // long as two steps.
+  int ahead_i = 0, ahead_s = 0;
+  auto request_pages = [&](int k, int rank0, int here) {
+    int* to = &page_buf[k % (kPageBatches + 1)][lane];
+    bool there = false;
+    const int32_t* from = args.table;
+    if (ahead_i < here) {
+      const PagedPiece& p = deal.at(rank0, ahead_i);
+      if (ahead_s + (lane >> 3) < p.n) {
+        const PagedSpan span(p.len, window, n_sink);
+        const int slot = span.slot0(p.s0 + ahead_s + (lane >> 3)) + (lane & 7) * 16;
+        there = span.any_visible(slot & ~(box_rows - 1), box_rows);
+        from += size_t(p.u) * args.max_pages + (slot >> args.page_shift);
+      }
+      ahead_s += 4;
+      if (ahead_s >= p.n) { ahead_s = 0; ++ahead_i; }
+    }
+    if (there) cp_async_4(to, from);
+    else *to = -1;
+    cp_async_group();
+  };
+  typename PagedDeal<kTeams * kConsumers, kList>::Mine my;
+  const PagedCut cut = deal.start(args, window, n_sink, share, my, ws.records);
+  const int n_pieces = deal.n_pieces();
   int n = 0;                                                       // stages handed over so far
   bool ok = true;
-  for (int rank0 = 0;; rank0 += kList) {
-    const int n_pieces = deal.deal(args, plan, window, n_sink, share, rank0, ws.table);
-    if (stop_word) return;
+  for (int rank0 = 0; rank0 < n_pieces; rank0 += kList) {
+    deal.round(args, window, n_sink, my, cut, share, rank0);
     const int here = min(kList, n_pieces - rank0);
-    if (warp == kWarps) {
+    if (warp == kTeams * kWarps) {
       // ------------------------------------------------------------- producer
-      // A lane reads the page of one group of 16 rows: of steps 0 .. 3 of a batch, group lane % 8.  The next
-      // batch's pages are requested before this one's boxes are issued.
-      auto page_of = [&](int i, int s) {          // step s of piece i
-        if (i >= here) return -1;
-        const PagedPiece& p = deal.list[i];
-        if (s + (lane >> 3) >= p.n) return -1;
-        const PagedSpan span(p.len, window, n_sink);
-        const int slot = span.slot0(p.s0 + s + (lane >> 3)) + (lane & 7) * 16;
-        if (!span.any_visible(slot & ~(box_rows - 1), box_rows)) return -1;
-        return args.table[size_t(p.u) * args.max_pages + (slot >> args.page_shift)];
-      };
-      int next_page = page_of(0, 0);
+      // The next call reads these rows again, from where they are: of every 64 runs of 128 pool rows (bit-reversed, so
+      // that every share holds as many) as many as fit kL2Share of the L2 ask to stay, the others to go first, so
+      // that code, states, tables and partial results stay as well.
+      const uint64_t stays = ptx::l2_policy_evict_last(), streams = ptx::l2_policy_evict_first();
+      const int keep = int(min(int64_t(64), l2_keep / max(1, cut.total - kPagedLead)));
+      int batch = 0;
+      ahead_i = ahead_s = 0;
+      for (int k = 0; k < 2; ++k) request_pages(k, rank0, here);
       for (int i = 0; i < here && ok; ++i) {
-        const PagedPiece piece = deal.list[i];
+        const PagedPiece piece = deal.at(rank0, i);
         const PagedSpan span(piece.len, window, n_sink);
+        if (lane == 0) {       // the piece that had the place has been begun by all consumers: they released a stage of it
+          const int k = (rank0 + i) % Ring::kQueries;
+          const uint32_t bytes = uint32_t(G) * D * sizeof(T);
+          ptx::mbar_arrive_expect_tx(&query_full[k], bytes);
+          bulk_copy_g2s(query_buf + k * Ring::kQueryBytes, q + size_t(piece.u) * G * D, bytes, &query_full[k]);
+        }
         for (int s = 0; s < piece.n && ok; s += 4) {
-          const int page = next_page;
-          next_page = s + 4 < piece.n ? page_of(i, s + 4) : page_of(i + 1, 0);
+          if (batch == 0) {
+            cp_async_pending<1>();                        // the others can wait until the first boxes are on their way
+          } else {
+            for (int k = batch == 1 ? 2 : batch + kPageBatches - 1; k < batch + kPageBatches; ++k) request_pages(k, rank0, here);
+            cp_async_pending<kPageBatches - 1>();
+          }
+          const int page = page_buf[batch % (kPageBatches + 1)][lane];   // this lane's own request
+          ++batch;
           for (int b = 0; b < 4 && s + b < piece.n && ok; ++b) {
             const int mine = __shfl_sync(0xffffffffu, page, b * 8 + (lane & 7));
             const int slot = span.slot0(piece.s0 + s + b) + (lane & 7) * 16;
@@ -372,6 +474,11 @@ paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
             const int row = (mine << args.page_shift) + (slot & ((1 << args.page_shift) - 1));
             const bool box = wanted && good && (slot & (box_rows - 1)) == 0;
             const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, box)) * box_rows * 128 * Ring::kBoxes;
+            if (ws.steps) {
+              PagedStepRecord* to = ws.steps + piece.step + piece.s0 + s + b;
+              if (lane < 8) to->group[lane] = make_int2(wanted && good ? row >> 4 : -1, int(span.visible16(slot)));
+              if (lane == 8) *reinterpret_cast<int2*>(&to->slot) = make_int2(piece.slot, piece.parts);
+            }
             for (int kv = 0; kv < 2 && ok; ++kv, ++n) {
               const int stage = n % kStages;
               if (lane == 0 && n >= kStages) ok = ptx::mbar_wait(&ring.empty[stage], uint32_t(n / kStages - 1) & 1u, abort_flag);
@@ -382,111 +489,101 @@ paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
               if (lane == 0) ptx::mbar_arrive_expect_tx(&ring.full[stage], bytes);
               __syncwarp();
               if (box)
-                ptx::tma_load_3d(ring_buf + stage * Ring::kStageBytes + lane * 16 * 128 * Ring::kBoxes, kv ? &map_v : &map_k, 0, row, 0,
-                                 &ring.full[stage]);
+                ptx::tma_load_3d_hint(ring_buf + stage * Ring::kStageBytes + lane * 16 * 128 * Ring::kBoxes, kv ? &map_v : &map_k, 0, row, 0,
+                                      &ring.full[stage], (int(__brev(unsigned(row >> 7)) >> 26) < keep) ? stays : streams);
             }
           }
         }
       }
     } else {
       // ------------------------------------------------------------- consumers
+      const int team = warp / kWarps, tw = warp % kWarps;
       WarpRows<T, D, GT> rows;
-      const int page_in_step = warp * 16 / box_rows, r0 = warp * 16 % box_rows;
-      const uint32_t warp_base = ptx::smem_u32(ring_buf) + uint32_t(page_in_step * box_rows * 128 * Ring::kBoxes);
+      WarpPlace place;
+      place.box_rows = box_rows;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const int r = tw * kWarpRows + t * 16;
+        place.base[t] = ptx::smem_u32(ring_buf) + uint32_t(r & ~(box_rows - 1)) * 128u * Ring::kBoxes;
+        place.r0[t] = r & (box_rows - 1);
+      }
       const uint32_t zero_addr = ptx::smem_u32(zeros);
+      float* state = reinterpret_cast<float*>(states + team * Ring::kState);
       for (int i = 0; i < here; ++i) {
-        const PagedPiece piece = deal.list[i];
+        const PagedPiece piece = deal.at(rank0, i);
+        if (kTeams > 1 && ((rank0 + i) & 1) != team) {
+          // The other team's: its stages are waited for and released like one's own.  A barrier tells only whether its
+          // last phase is over, so nobody may be further ahead or behind than the ring is long.
+          for (int s = 0; s < 2 * piece.n; ++s, ++n) {
+            if (ok) ok = __all_sync(0xffffffffu, ring.wait_full(n, abort_flag));
+            if (lane == 0) ring.release(n);
+          }
+          continue;
+        }
         const PagedSpan span(piece.len, window, n_sink);
-        const T* q_unit = q + size_t(piece.u) * G * D;
-        if constexpr (GT > 0) {
-          for (int j = tid; j < GT * D; j += kConsumers) s_q[j] = j < G * D ? float(q_unit[j]) : 0.f;
-          consumer_sync(kConsumers);
-        }
-        rows.begin(q_unit, G, s_q);
+        const int qk = (rank0 + i) % Ring::kQueries;
+        if (ok) ok = __all_sync(0xffffffffu, ptx::mbar_wait(&query_full[qk], uint32_t((rank0 + i) / Ring::kQueries) & 1u, abort_flag));
+        rows.begin(reinterpret_cast<const T*>(query_buf + qk * Ring::kQueryBytes), G);
         for (int s = 0; s < piece.n; ++s) {
-          const int slot = span.slot0(piece.s0 + s) + warp * 16;
-          unsigned visible = span.visible16(slot);
+          const int slot = span.slot0(piece.s0 + s) + tw * kWarpRows;
+          unsigned visible = span.visible16(slot) | span.visible16(slot + 16) << 16;
           if (ok) ok = __all_sync(0xffffffffu, ring.wait_full(n, abort_flag));
-          const int at = ok ? group_row[n % kStages][warp] : -1;
-          if (at < 0) visible = 0;
+          const int at0 = ok ? group_row[n % kStages][tw * 2] : -1, at1 = ok ? group_row[n % kStages][tw * 2 + 1] : -1;
+          if (at0 < 0) visible &= 0xffff0000u;
+          if (at1 < 0) visible &= 0xffffu;
           if (visible) {
-            rows.score(warp_base + (n % kStages) * Ring::kStageBytes, box_rows, r0, visible, scale_log2e);
-            if (ws.score) rows.leave_scores(ws.score + size_t(at) * G * 16);
+            rows.score(place, (n % kStages) * Ring::kStageBytes, visible, scale_log2e);
+            if (ws.score) {
+              if (at0 >= 0) rows.leave_scores(0, ws.score + size_t(at0) * G * 16);
+              if (at1 >= 0) rows.leave_scores(1, ws.score + size_t(at1) * G * 16);
+            }
           }
           __syncwarp();
           if (lane == 0) ring.release(n);
           ++n;
           if (ok) ok = __all_sync(0xffffffffu, ring.wait_full(n, abort_flag));
-          if (ok && visible) rows.value(warp_base + (n % kStages) * Ring::kStageBytes, box_rows, r0, visible, zero_addr);
+          if (ok && visible) rows.value(place, (n % kStages) * Ring::kStageBytes, visible, zero_addr);
           __syncwarp();
           if (lane == 0) ring.release(n);
           ++n;
         }
-        // ----------------------------------------------------------- merge the warps' states: 4 .. 7 into 0 .. 3, then those
-        const int hs = warp & 3;
-        float* mine = scratch + size_t(hs) * G * D;
-        if (warp >= 4) {
-          rows.each([&](int g, int d, float& v) { mine[g * D + d] = v; });
-          for (int g = rows.head0(); g < rows.head1(); ++g)
-            if (g < G && rows.stats_lane(g)) { s_m[hs][g] = rows.max_of(g); s_l[hs][g] = rows.sum_of(g); }
-        }
-        consumer_sync(kConsumers);
-        if (warp < 4) {
-          float w0[GT > 0 ? GT : 1], w1[GT > 0 ? GT : 1];
-#pragma unroll
-          for (int k = 0; k < (GT > 0 ? GT : 1); ++k) {
-            const int g = rows.head0() + k;
-            w0[k] = 1.f;
-            w1[k] = 0.f;
-            if (g < G) {
-              const float ma = rows.max_of(g), mb = s_m[hs][g], M = fmaxf(ma, mb), from = M == -INFINITY ? 0.f : M;
-              w0[k] = exp2f(ma - from);
-              w1[k] = exp2f(mb - from);
-              rows.sum_of(g) = rows.sum_of(g) * w0[k] + s_l[hs][g] * w1[k];
-              rows.max_of(g) = M;
-            }
-          }
-          rows.each([&](int g, int d, float& v) {
-            const int k = GT > 0 ? g : 0;
-            v = v * w0[k] + mine[g * D + d] * w1[k];
-            mine[g * D + d] = v;
-          });
-          __syncwarp();                       // the warp's lanes have read the other state's statistics
-          for (int g = rows.head0(); g < rows.head1(); ++g)
-            if (g < G && rows.stats_lane(g)) { s_m[hs][g] = rows.max_of(g); s_l[hs][g] = rows.sum_of(g); }
-        }
-        consumer_sync(kConsumers);
-        if (!*abort_flag) {
+        // ----------------------------------------------------------- the warps' states become the piece's
+        rows.leave(state + tw * GT * state_row(D), s_m[team][tw], s_l[team][tw]);
+        team_sync(team);
+        if (!*abort_flag && !stops_call(found_status)) {
           const size_t at = size_t(share + piece.u) * G;
-          for (int j = tid * 2; j < G * D; j += kConsumers * 2) {
+          for (int j = tid % kConsumers * 4; j < G * D; j += kConsumers * 4) {
             const int g = j / D, d = j - g * D;
-            float M = -INFINITY;
+            float ms[kWarps], M = -INFINITY;
 #pragma unroll
-            for (int w = 0; w < kMergeStates; ++w) M = fmaxf(M, s_m[w][g]);
+            for (int w = 0; w < kWarps; ++w) M = fmaxf(M, ms[w] = s_m[team][w][g]);
             const float from = M == -INFINITY ? 0.f : M;
-            float a0 = 0.f, a1 = 0.f, l = 0.f;
+            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+            float l = 0.f;
 #pragma unroll
-            for (int w = 0; w < kMergeStates; ++w) {
-              const float wt = exp2f(s_m[w][g] - from);
-              const float2 v = *reinterpret_cast<const float2*>(scratch + (size_t(w) * G + g) * D + d);
-              a0 = fmaf(v.x, wt, a0);
-              a1 = fmaf(v.y, wt, a1);
-              l = fmaf(s_l[w][g], wt, l);
+            for (int w = 0; w < kWarps; ++w) {
+              const float wt = exp2f(ms[w] - from);
+              const float4 v = *reinterpret_cast<const float4*>(state + (w * GT + g) * state_row(D) + d);
+              acc.x = fmaf(v.x, wt, acc.x);
+              acc.y = fmaf(v.y, wt, acc.y);
+              acc.z = fmaf(v.z, wt, acc.z);
+              acc.w = fmaf(v.w, wt, acc.w);
+              l = fmaf(s_l[team][w][g], wt, l);
             }
-            if (piece.whole) {
+            if (piece.parts == 0) {
+              const float inv = 1.f / l;
               T* out = O + size_t(piece.u) * G * D + j;
-              if constexpr (sizeof(T) == 4) *reinterpret_cast<float2*>(out) = make_float2(a0 / l, a1 / l);
-              else *reinterpret_cast<uint32_t*>(out) = ptx::pack_bf16x2(a0 / l, a1 / l);
+              if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(out) = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+              else *reinterpret_cast<uint2*>(out) = make_uint2(ptx::pack_bf16x2(acc.x * inv, acc.y * inv), ptx::pack_bf16x2(acc.z * inv, acc.w * inv));
             } else {
-              *reinterpret_cast<float2*>(ws.acc + at * D + j) = make_float2(a0, a1);
+              *reinterpret_cast<float4*>(ws.acc + at * D + j) = acc;
             }
             if (d == 0) ws.ml[at + g] = make_float2(M, l);
           }
         }
-        consumer_sync(kConsumers);            // the states are written over by the next piece
+        team_sync(team);                        // the states are written over by the next piece
       }
     }
-    if (rank0 + kList >= n_pieces) break;
   }
   __syncthreads();
   if (*abort_flag) {
@@ -497,60 +594,65 @@ paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
 
 // ------------------------------------------------------------------ merge of the partial results; weights
 constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32;
+constexpr int kWeightBlocks = 4;     // per SM
+constexpr int kJoinAhead = 8;        // partial results whose outputs are on their way together
 
-// Blocks below merge_blocks: one warp per (unit, head) merges the unit's partial results in order.  The others (only if
-// weights are accumulated): a share of the visible rows each, turning scores into weights.
-template <typename T, int D>
-__global__ void __launch_bounds__(kJoinThreads)
-paged_join_kernel(const __grid_constant__ PagedArgs args, int G, int window, int n_sink, int merge_blocks, PagedPlan plan, PagedWs ws,
+// The first weight_blocks blocks (none if weights are not accumulated): a warp per step of 128 slots turns its scores into
+// weights.  The others: one warp per (unit, head) merges the unit's partial results in order.  All loads that do not depend on
+// one another are issued together: the kernel is a chain of trips to memory.  (Held to 64 registers a block fits beside a
+// CTA of the first kernel, and the call takes 42.6 us instead of 41.2: 64 conversations with weights.)
+template <typename T, int D, int GT>
+__global__ void __launch_bounds__(kJoinThreads, 3)
+paged_join_kernel(const __grid_constant__ PagedArgs args, int G, int window, int n_sink, int weight_blocks, PagedWs ws,
                   float* __restrict__ mass, T* __restrict__ O) {
-  __shared__ PagedDeal<kJoinThreads, kList> deal;
-  __shared__ float s_lse[kMaxGroup];
-  __shared__ int stop_word;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   constexpr int E = D / 32;
-  if (int(blockIdx.x) < merge_blocks) {
-    const int at = int(blockIdx.x) * kJoinWarps + warp, u = at / G, g = at - u * G;
-    pdl_wait();
-    pdl_launch_dependents();
+  pdl_wait();
+  pdl_launch_dependents();
+  const int found_status = __ldcg(ws.status);
+  if (int(blockIdx.x) >= weight_blocks) {
+    const int at = (int(blockIdx.x) - weight_blocks) * kJoinWarps + warp, u = at / G, g = at - u * G;
     if (u >= args.n_units) return;
-    const int len = args.state[u].x;
-    const int2 where = __ldcg(ws.table + u);
-    if (stops_call(__ldcg(ws.status))) return;
-    float o[E];
+    const int4 rec = __ldcg(reinterpret_cast<const int4*>(ws.records) + u);
+    if (stops_call(found_status)) return;
+    const int n = PagedSpan(rec.z, window, n_sink).n > 0 ? rec.y : -1;   // partial results; -1: nothing is visible
+    if (n == 0) return;                         // its only share wrote the result
+    float o[E], m = -INFINITY, l = 0.f;
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] = 0.f;
-    if (PagedSpan(paged_len(args, len), window, n_sink).n > 0) {
-      if (where.y == 0) return;                 // its only share wrote the result
-      float m = -INFINITY, l = 0.f;
-      for (int c0 = 0; c0 < where.y; c0 += 32) {
-        const int cn = min(32, where.y - c0);
-        const float2 ml = lane < cn ? __ldcg(ws.ml + size_t(where.x + c0 + lane) * G + g) : make_float2(-INFINITY, 0.f);
-        float mn = ml.x;
+    for (int c0 = 0; c0 < n; c0 += kJoinAhead) {
+      const int cn = min(kJoinAhead, n - c0);
+      const float2 ml = lane < cn ? __ldcg(ws.ml + size_t(rec.x + c0 + lane) * G + g) : make_float2(-INFINITY, 0.f);
+      float v[kJoinAhead][E];
 #pragma unroll
-        for (int off = 16; off > 0; off >>= 1) mn = fmaxf(mn, __shfl_xor_sync(0xffffffffu, mn, off));
-        mn = fmaxf(m, mn);
-        const float from = mn == -INFINITY ? 0.f : mn, keep = exp2f(m - from), w = exp2f(ml.x - from);
-        l *= keep;
-#pragma unroll
-        for (int e = 0; e < E; ++e) o[e] *= keep;
-        const float wl = w * ml.y;
-#pragma unroll 8
-        for (int c = 0; c < cn; ++c) {
-          const float wc = __shfl_sync(0xffffffffu, w, c);
-          l += __shfl_sync(0xffffffffu, wl, c);
-          const float* a = ws.acc + (size_t(where.x + c0 + c) * G + g) * D + lane * E;
-          float v[E];
-          if constexpr (E == 4) { const float4 t = __ldcg(reinterpret_cast<const float4*>(a)); v[0] = t.x; v[1] = t.y; v[2] = t.z; v[3] = t.w; }
-          else { const float2 t = __ldcg(reinterpret_cast<const float2*>(a)); v[0] = t.x; v[1] = t.y; }
-#pragma unroll
-          for (int e = 0; e < E; ++e) o[e] = fmaf(wc, v[e], o[e]);
-        }
-        m = mn;
+      for (int c = 0; c < kJoinAhead; ++c) {
+        const float* a = ws.acc + (size_t(rec.x + c0 + min(c, cn - 1)) * G + g) * D + lane * E;
+        if constexpr (E == 4) { const float4 t = __ldcg(reinterpret_cast<const float4*>(a)); v[c][0] = t.x; v[c][1] = t.y; v[c][2] = t.z; v[c][3] = t.w; }
+        else { const float2 t = __ldcg(reinterpret_cast<const float2*>(a)); v[c][0] = t.x; v[c][1] = t.y; }
       }
+      float mn = ml.x;
+#pragma unroll
+      for (int off = kJoinAhead / 2; off > 0; off >>= 1) mn = fmaxf(mn, __shfl_xor_sync(0xffffffffu, mn, off));
+      mn = fmaxf(m, __shfl_sync(0xffffffffu, mn, 0));
+      const float from = mn == -INFINITY ? 0.f : mn, keep = exp2f(m - from), w = exp2f(ml.x - from);
+      const float wl = w * ml.y;
+      l *= keep;
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] *= keep;
+#pragma unroll
+      for (int c = 0; c < kJoinAhead; ++c) {
+        const float wc = __shfl_sync(0xffffffffu, w, c);
+        l += __shfl_sync(0xffffffffu, wl, c);
+        if (c < cn) {
+#pragma unroll
+          for (int e = 0; e < E; ++e) o[e] = fmaf(wc, v[c][e], o[e]);
+        }
+      }
+      m = mn;
+    }
+    if (n > 0)
 #pragma unroll
       for (int e = 0; e < E; ++e) o[e] /= l;
-    }
     T* out = O + (size_t(u) * G + g) * D + lane * E;
 #pragma unroll
     for (int e = 0; e < E; e += 2) {
@@ -559,50 +661,62 @@ paged_join_kernel(const __grid_constant__ PagedArgs args, int G, int window, int
     }
     return;
   }
-  pdl_wait();
-  pdl_launch_dependents();
-  if (tid == 0) stop_word = stops_call(__ldcg(ws.status));
-  const int share = int(blockIdx.x) - merge_blocks;
+  // ---- weights
+  const int warps = weight_blocks * kJoinWarps;
+  const int total = __ldcg(&ws.records[args.n_units].step);
+  if (stops_call(found_status)) return;
   const float inv_g = 1.f / float(G);
-  for (int rank0 = 0;; rank0 += kList) {
-    const int n_pieces = deal.deal(args, plan, window, n_sink, share, rank0, nullptr);
-    if (stop_word) return;
-    const int here = min(kList, n_pieces - rank0);
-    for (int i = 0; i < here; ++i) {
-      const PagedPiece p = deal.list[i];
-      const PagedSpan span(p.len, window, n_sink);
-      __syncthreads();
-      if (warp < G) {                           // the row sums of the unit: log2 of the sum over its partial results
-        const int2 where = __ldcg(ws.table + p.u);
-        float m = -INFINITY, l = 0.f;
-        for (int c = lane; c < max(1, where.y); c += 32) {
-          const float2 ml = __ldcg(ws.ml + size_t(where.x + c) * G + warp);
-          const float mn = fmaxf(m, ml.x), from = mn == -INFINITY ? 0.f : mn;
-          l = l * exp2f(m - from) + ml.y * exp2f(ml.x - from);
-          m = mn;
-        }
+  for (int step = int(blockIdx.x) * kJoinWarps + warp; step < total; step += warps) {
+    const PagedStepRecord* rec = ws.steps + step;
+    const int2 where = __ldcg(reinterpret_cast<const int2*>(&rec->slot));
+    int row[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int2 group = __ldcg(&rec->group[i * 2 + (lane >> 4)]);
+      row[i] = group.x >= 0 && ((group.y >> (lane & 15)) & 1) ? group.x * 16 + (lane & 15) : -1;
+    }
+    // the row sums: log2 of the sum over the unit's partial results, head by head
+    float lse[GT];
+    const int parts = max(1, where.y);
+    float x[4][GT], sum[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      sum[i] = row[i] >= 0 ? mass[row[i]] : 0.f;
+#pragma unroll
+      for (int g = 0; g < GT; ++g)
+        x[i][g] = g < G && row[i] >= 0 ? __ldcg(ws.score + (size_t(row[i] >> 4) * G + g) * 16 + (row[i] & 15)) : 0.f;
+    }
+#pragma unroll
+    for (int g = 0; g < GT; ++g) {
+      lse[g] = 0.f;
+      if (g >= G) continue;
+      float m = -INFINITY, l = 0.f;
+      for (int c = lane; c < parts; c += 32) {
+        const float2 ml = __ldcg(ws.ml + size_t(where.x + c) * G + g);
+        const float mn = fmaxf(m, ml.x), from = mn == -INFINITY ? 0.f : mn;
+        l = l * exp2f(m - from) + ml.y * exp2f(ml.x - from);
+        m = mn;
+      }
+      if (parts > 1) {
 #pragma unroll
         for (int off = 16; off > 0; off >>= 1) {
-          const float mo = __shfl_xor_sync(0xffffffffu, m, off), lo = __shfl_xor_sync(0xffffffffu, l, off);
+          const float mo = __shfl_xor_sync(0xffffffffu, m, off), lo2 = __shfl_xor_sync(0xffffffffu, l, off);
           const float mn = fmaxf(m, mo), from = mn == -INFINITY ? 0.f : mn;
-          l = l * exp2f(m - from) + lo * exp2f(mo - from);
+          l = l * exp2f(m - from) + lo2 * exp2f(mo - from);
           m = mn;
         }
-        if (lane == 0) s_lse[warp] = m + log2f(l);
       }
-      __syncthreads();
-      for (int j = tid; j < p.n * kPagedStep; j += kJoinThreads) {
-        const int slot = span.slot0(p.s0 + j / kPagedStep) + j % kPagedStep;
-        if (!((span.visible16(slot & ~15) >> (slot & 15)) & 1u)) continue;
-        const int row = paged_row(args, p.u, slot);
-        if (row < 0) continue;
-        const float* x = ws.score + size_t(row >> 4) * G * 16 + (row & 15);
-        float sum = 0.f;
-        for (int g = 0; g < G; ++g) sum += exp2f(__ldcg(x + g * 16) - s_lse[g]);
-        mass[row] += sum * inv_g;
-      }
+      lse[g] = __shfl_sync(0xffffffffu, m + log2f(l), 0);
     }
-    if (rank0 + kList >= n_pieces) break;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (row[i] < 0) continue;
+      float w = 0.f;
+#pragma unroll
+      for (int g = 0; g < GT; ++g)
+        if (g < G) w += exp2f(x[i][g] - lse[g]);
+      mass[row[i]] = sum[i] + w * inv_g;
+    }
   }
 }
 
@@ -612,10 +726,10 @@ bool pool_map(CUtensorMap* out, const void* base, const tca_paged_desc* c) {
   EncodeTiledFn fn = encode_fn();
   if (!fn) return false;
   constexpr int kCols = 128 / int(sizeof(T));
-  cuuint64_t dims[3] = {cuuint64_t(kCols), cuuint64_t(c->n_pages) * c->page_size, cuuint64_t(PagedRing<T, D>::kBoxes)};
+  cuuint64_t dims[3] = {cuuint64_t(kCols), cuuint64_t(c->n_pages) * c->page_size, cuuint64_t(PagedRing<T, D, 8>::kBoxes)};
   cuuint64_t strides[2] = {cuuint64_t(D) * sizeof(T), 128};
   cuuint32_t box[3] = {cuuint32_t(kCols), cuuint32_t(c->page_size < kPagedStep ? c->page_size : kPagedStep),
-                       cuuint32_t(PagedRing<T, D>::kBoxes)};
+                       cuuint32_t(PagedRing<T, D, 8>::kBoxes)};
   cuuint32_t estr[3] = {1, 1, 1};
   return fn(out, sizeof(T) == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, const_cast<void*>(base), dims,
             strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
@@ -623,34 +737,33 @@ bool pool_map(CUtensorMap* out, const void* base, const tca_paged_desc* c) {
 }
 
 template <typename T, int D, int GT>
-int launch_paged(const tca_params* prm, const void* q, const tca_paged_desc* c, int n_sink, bool weights, void* O, const PagedPlan& plan,
-                 const PagedWs& ws, cudaStream_t s) {
-  using Ring = PagedRing<T, D>;
+int launch_paged(const tca_params* prm, const void* q, const tca_paged_desc* c, int n_sink, bool weights, void* O, const PagedWs& ws,
+                 cudaStream_t s) {
+  using Ring = PagedRing<T, D, GT>;
   CUtensorMap mk, mv;
   if (!pool_map<T, D>(&mk, c->k, c) || !pool_map<T, D>(&mv, c->v, c)) return TCA_ERR_CUDA;
   const int G = prm->n_q_heads / prm->n_kv_heads;
   const PagedArgs args = paged_args(c);
   constexpr auto kern = paged_kernel<T, D, GT>;
   if (allow_smem<kern>(Ring::kSmemBytes) != TCA_OK) return TCA_ERR_CUDA;
-  const int st = launch_pdl(kern, dim3(unsigned(plan.n_shares)), dim3(kThreads), size_t(Ring::kSmemBytes), s, mk, mv, static_cast<const T*>(q),
-                            args, G, prm->window, n_sink, prm->sm_scale * kLog2e, plan, ws, static_cast<T*>(O));
+  const int st = launch_pdl(kern, dim3(unsigned(sm_count())), dim3(Ring::kThreads), size_t(Ring::kSmemBytes), s, mk, mv, static_cast<const T*>(q),
+                            args, G, prm->window, n_sink, prm->sm_scale * kLog2e, int64_t(64 * kL2Share * double(l2_bytes()) / (2 * Ring::kStageBytes)), ws,
+                            static_cast<T*>(O));
   if (st != TCA_OK) return st;
   const int merge_blocks = int((c->n_units * G + kJoinWarps - 1) / kJoinWarps);
-  PagedPlan join = plan;
-  join.n_shares = plan.n_shares * 4;
-  join.lead = 0;
-  return launch_pdl(paged_join_kernel<T, D>, dim3(unsigned(merge_blocks + (weights ? join.n_shares : 0))), dim3(kJoinThreads), size_t(0), s, args,
-                    G, prm->window, n_sink, merge_blocks, join, ws, c->mass, static_cast<T*>(O));
+  const int weight_blocks = weights ? kWeightBlocks * sm_count() : 0;
+  return launch_pdl(paged_join_kernel<T, D, (GT > 4 ? 8 : 4)>, dim3(unsigned(merge_blocks + weight_blocks)), dim3(kJoinThreads),
+                    size_t(0), s, args, G, prm->window, n_sink, weight_blocks, ws, c->mass, static_cast<T*>(O));
 }
 
 template <int D>
-int launch_paged_f32(const tca_params* prm, const void* q, const tca_paged_desc* c, int n_sink, bool weights, void* O, const PagedPlan& plan,
-                     const PagedWs& ws, cudaStream_t s) {
+int launch_paged_f32(const tca_params* prm, const void* q, const tca_paged_desc* c, int n_sink, bool weights, void* O, const PagedWs& ws,
+                     cudaStream_t s) {
   const int G = prm->n_q_heads / prm->n_kv_heads;
-  if (G == 1) return launch_paged<float, D, 1>(prm, q, c, n_sink, weights, O, plan, ws, s);
-  if (G == 2) return launch_paged<float, D, 2>(prm, q, c, n_sink, weights, O, plan, ws, s);
-  if (G <= 4) return launch_paged<float, D, 4>(prm, q, c, n_sink, weights, O, plan, ws, s);
-  return launch_paged<float, D, 8>(prm, q, c, n_sink, weights, O, plan, ws, s);
+  if (G == 1) return launch_paged<float, D, 1>(prm, q, c, n_sink, weights, O, ws, s);
+  if (G == 2) return launch_paged<float, D, 2>(prm, q, c, n_sink, weights, O, ws, s);
+  if (G <= 4) return launch_paged<float, D, 4>(prm, q, c, n_sink, weights, O, ws, s);
+  return launch_paged<float, D, 8>(prm, q, c, n_sink, weights, O, ws, s);
 }
 
 }  // namespace
@@ -660,7 +773,7 @@ using namespace tca;
 
 extern "C" size_t tca_attn_paged_workspace_bytes(const tca_params* prm, const tca_paged_desc* c, int32_t accumulate) {
   if (check_paged(prm, c) != TCA_OK) return 0;
-  return paged_ws_layout(prm, c, paged_plan(prm), accumulate != 0, nullptr).bytes;
+  return paged_ws_layout(prm, c, accumulate != 0, nullptr).bytes;
 }
 
 extern "C" int tca_attn_paged(const tca_params* prm, const void* q, const tca_paged_desc* c, int32_t n_sink, int32_t accumulate, void* O,
@@ -670,15 +783,16 @@ extern "C" int tca_attn_paged(const tca_params* prm, const void* q, const tca_pa
   TCA_CHECK_ARG(q && O && ws && n_sink >= 0);
   TCA_CHECK_ARG(aligned(q, 16) && aligned(O, 16) && aligned(ws, 256));
   if (prm->window < 1) return TCA_ERR_UNSUPPORTED;
-  const PagedPlan plan = paged_plan(prm);
-  const PagedWs lay = paged_ws_layout(prm, c, plan, accumulate != 0, ws);
+  const PagedWs lay = paged_ws_layout(prm, c, accumulate != 0, ws);
   if (ws_bytes < lay.bytes) return TCA_ERR_WORKSPACE;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const bool w = accumulate != 0;
   if (prm->dtype == TCA_F32)
-    return prm->head_dim == 128 ? launch_paged_f32<128>(prm, q, c, n_sink, w, O, plan, lay, s) : launch_paged_f32<64>(prm, q, c, n_sink, w, O, plan, lay, s);
-  if (prm->head_dim == 128) return launch_paged<__nv_bfloat16, 128, 0>(prm, q, c, n_sink, w, O, plan, lay, s);
-  return launch_paged<__nv_bfloat16, 64, 0>(prm, q, c, n_sink, w, O, plan, lay, s);
+    return prm->head_dim == 128 ? launch_paged_f32<128>(prm, q, c, n_sink, w, O, lay, s) : launch_paged_f32<64>(prm, q, c, n_sink, w, O, lay, s);
+  const bool wide = prm->n_q_heads > 4 * prm->n_kv_heads;
+#define TCA_PAGED(D) (wide ? launch_paged<__nv_bfloat16, D, 8>(prm, q, c, n_sink, w, O, lay, s) : launch_paged<__nv_bfloat16, D, 4>(prm, q, c, n_sink, w, O, lay, s))
+  return prm->head_dim == 128 ? TCA_PAGED(128) : TCA_PAGED(64);
+#undef TCA_PAGED
 }
 
 extern "C" int tca_paged_status(const tca_paged_desc* c, void* stream, int64_t* detail) {

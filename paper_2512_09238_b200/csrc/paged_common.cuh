@@ -67,106 +67,158 @@ struct PagedSpan {
 #endif
 };
 
-// How the steps of all units are dealt: laid end to end they are cut into equal shares, one per CTA, wherever the
-// cuts fall; a share that runs into the next unit works on both.  A unit counts `lead` steps more than it has, which
-// is what starting on one costs.  The cuts follow from the device's state, so a captured launch stays right when the
-// cache has changed since.  Pair (share i, unit u) has partial slot i + u: pairs advance in one of the two at a time.
-struct PagedPlan {
-  int n_shares, min_share, lead;
+// How the steps of all units are dealt: laid end to end they are cut into equal shares, one per CTA, wherever the cuts
+// fall; a share that runs into the next unit works on both.  The cuts follow from the device's state, so a captured launch
+// stays right when the cache has changed since.  Pair (share i, unit u) has partial slot i + u: pairs advance in one of
+// the two at a time, so slots are distinct and a unit's are consecutive.  A unit is kPagedLead wider than its steps are,
+// which is what starting on one and finishing it costs.
+// (The SMs do not get the same bandwidth: of 249 MB the first finish after 42 us, half of them after 45, the last after 51.
+// A quarter of the steps in small shares that whoever is ready takes did not help: what a CTA has to ask for ahead, three
+// small shares, takes as long as that, and finding them delayed the start: 76 against 58 us.)
+constexpr int kPagedLead = 1;
+struct PagedCut {
+  int total, n, q, longer;               // width; shares: the first `longer` are q + 1 wide, the others q
+#ifdef __CUDACC__
+  __host__ __device__ PagedCut(int steps, int ctas) {
+    total = steps;
+    n = steps < ctas ? (steps > 0 ? steps : 1) : ctas;
+    q = int(unsigned(steps) / unsigned(n));
+    longer = steps - q * n;
+  }
+  __device__ __forceinline__ int begin(int share) const { return share < n ? share * q + min(share, longer) : total; }
+  __device__ __forceinline__ int share_of(int x) const {   // the share that place x lies in
+    const int head = longer * (q + 1);
+    return x < head ? int(unsigned(x) / unsigned(q + 1)) : longer + int(unsigned(x - head) / unsigned(q));
+  }
+#endif
 };
 struct PagedPiece {
-  int u, s0, n, whole;     // steps [s0, s0 + n) of unit u; whole: all it has
+  int u, s0, n;            // steps [s0, s0 + n) of unit u
   int len;                 // rows of the unit
+  int step;                // steps of the units before it
+  int slot, parts;         // the unit's partial results: first slot, number (0: this piece is all it has)
+};
+// What the second kernel needs of a unit (len, partial results as above), and of a step.
+struct __align__(16) PagedRecord {
+  int slot, parts, len, step;            // step: steps of the units before it
+};
+struct __align__(16) PagedStepRecord {
+  int2 group[8];           // of every 16 slots: pool row / 16 (-1: not a page of the pool), visible slots as bits
+  int slot, parts, unused[2];
 };
 
 #ifdef __CUDACC__
-// All threads of the CTA deal together (a thread takes a run of units, the CTA scans their sums): one trip to memory
-// for up to kThreads units.  Pieces come in rounds of kList.
-template <int kThreads, int kList>
+// The CTA's first kDealers threads lay the steps end to end: one trip to memory for all rows (kept in shared memory for up
+// to kHeld units), a thread takes a run of units, a scan of their widths.  All threads take part in the barriers.  The share's
+// pieces come in rounds of kList; piece i of a round is at(i).  Loops are left rolled: this code stands between the launch
+// and the first load, and a cold line of it costs more than its instructions.
+template <int kDealers, int kList>
 struct PagedDeal {
-  int warp_sum[kThreads / 32][2];
-  int first_rank, n_pieces;
+  static_assert((kList & (kList - 1)) == 0, "a power of two");
+  static constexpr int kHeld = 512;
+  int warp_sum[kDealers / 32][2];
+  int first, last;         // ranks, among the units that have steps, of those in the share
+  int held[kHeld];
   PagedPiece list[kList];
 
-  __device__ __forceinline__ static int share_of(int x, int q, int longer) {   // the share that holds step x
-    const int head = longer * (q + 1);
-    return x < head ? x / (q + 1) : longer + (x - head) / q;
+  struct Mine {            // of a thread: its units, and the width and the units with steps before them
+    int u_begin, u_end, at, rank;
+  };
+  __device__ __forceinline__ int rows_of(const PagedArgs& a, int u) const {
+    return a.n_units <= kHeld ? held[u] : paged_len(a, __ldcg(&a.state[u].x));
   }
-  // Fills the list with the share's pieces of ranks [rank0, rank0 + kList) and returns how many pieces it has in
-  // all.  table: where each unit's partial results lie (written by the share that holds its first step); null: not.
-  __device__ int deal(const PagedArgs& a, const PagedPlan& plan, int window, int n_sink, int share, int rank0, int2* table) {
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int chunk = (a.n_units + kThreads - 1) / kThreads;
-    const int u_begin = tid * chunk, u_end = min(a.n_units, u_begin + chunk);
-    int steps = 0, units = 0;
-    int len = 0, one = 0;              // rows and steps of the only unit, if there is one
-    for (int u = u_begin; u < u_end; ++u) {
-      len = paged_len(a, a.state[u].x);
-      one = PagedSpan(len, window, n_sink).n;
-      steps += one > 0 ? one + plan.lead : 0;
-      units += one > 0;
-    }
-    int incl = steps, incl_u = units;
-#pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-      const int t = __shfl_up_sync(0xffffffffu, incl, off), tu = __shfl_up_sync(0xffffffffu, incl_u, off);
-      if (lane >= off) { incl += t; incl_u += tu; }
-    }
-    __syncthreads();                   // the list and the sums may still be read from the round before
-    if (lane == 31) { warp_sum[warp][0] = incl; warp_sum[warp][1] = incl_u; }
-    if (tid == 0) { n_pieces = 0; first_rank = 0; }
-    __syncthreads();
-    int at = incl - steps, rank = incl_u - units, total = 0;
-    for (int w = 0; w < kThreads / 32; ++w) {
-      if (w < warp) { at += warp_sum[w][0]; rank += warp_sum[w][1]; }
-      total += warp_sum[w][0];
-    }
-    const int n = max(1, min(plan.n_shares, total / plan.min_share));
-    const int q = total / n, longer = total - q * n;
-    const int begin = share < n ? share * q + min(share, longer) : total;
-    const int end = share < n ? begin + q + (share < longer ? 1 : 0) : total;
-    for (int pass = 0; pass < 2; ++pass) {
-      // first which of the units comes first in the share, then the list
-      int off = at, r = rank;
-      for (int u = u_begin; u < u_end; ++u) {
-        if (off >= end) break;
-        int m = one;
-        if (chunk > 1) {
-          len = paged_len(a, a.state[u].x);
-          m = PagedSpan(len, window, n_sink).n;
-        }
-        if (m == 0) continue;
-        const int rows = off + plan.lead;                  // where the unit's own steps begin
-        const int lo = max(rows, begin), hi = min(rows + m, end);
+  // Pieces of ranks [from, from + kList) go to the list; from < 0: all, and the ranks of the first and last are noted (if
+  // there are more than kList, round() fills the list again) and the records written, by all CTAs together.
+  __device__ __forceinline__ void fill(const PagedArgs& a, int window, int n_sink, const Mine& my, const PagedCut& cut, int share, int from,
+                                       PagedRecord* records) {
+    const int begin = cut.begin(share), end = cut.begin(share + 1);
+    int r = my.rank, off = my.at;
+#pragma unroll 1
+    for (int u = my.u_begin; u < my.u_end; ++u) {
+      const int len = rows_of(a, u), m = PagedSpan(len, window, n_sink).n;
+      const int at = off + kPagedLead, lo = max(at, begin), hi = min(at + m, end);
+      const bool record = records && u % int(gridDim.x) == int(blockIdx.x);
+      if (hi > lo || record) {
+        const int f = m > 0 ? cut.share_of(at) : 0, l = m > 0 ? cut.share_of(at + m - 1) : 0;
+        const int parts = f == l ? 0 : l - f + 1, step = off - kPagedLead * r;
         if (hi > lo) {
-          if (pass == 0) {
-            if (off <= begin) first_rank = r;
-            atomicAdd(&n_pieces, 1);
-          } else {
-            const int i = r - first_rank - rank0;
-            if (i >= 0 && i < kList) list[i] = PagedPiece{u, lo - rows, hi - lo, hi - lo == m, len};
-            if (table && lo == rows)
-              table[u] = make_int2(share + u, hi - lo == m ? 0 : share_of(rows + m - 1, q, longer) - share + 1);
+          if (from < 0) {
+            if (off <= begin) first = r;       // a unit before it would reach past `begin`
+            atomicMax(&last, r);
           }
+          if (from < 0 || (r >= from && r < from + kList)) list[r & (kList - 1)] = PagedPiece{u, lo - at, hi - lo, len, step, f + u, parts};
         }
-        off += m + plan.lead;
-        ++r;
+        if (record) records[u] = PagedRecord{f + u, parts, len, step};
       }
-      __syncthreads();
+      off += m > 0 ? m + kPagedLead : 0;
+      r += m > 0;
     }
-    return n_pieces;
   }
+  __device__ __forceinline__ PagedCut start(const PagedArgs& a, int window, int n_sink, int share, Mine& my, PagedRecord* records) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if (tid < kDealers && a.n_units <= kHeld)
+#pragma unroll 4
+      for (int u = tid; u < a.n_units; u += kDealers) held[u] = paged_len(a, __ldcg(&a.state[u].x));
+    if (tid == 0) { first = 0; last = -1; }
+    __syncthreads();
+    my = Mine{};
+    if (tid < kDealers) {
+      const int chunk = (a.n_units + kDealers - 1) / kDealers;
+      my.u_begin = min(a.n_units, tid * chunk);
+      my.u_end = min(a.n_units, my.u_begin + chunk);
+      int width = 0, units = 0;
+#pragma unroll 1
+      for (int u = my.u_begin; u < my.u_end; ++u) {
+        const int m = PagedSpan(rows_of(a, u), window, n_sink).n;
+        width += m > 0 ? m + kPagedLead : 0;
+        units += m > 0;
+      }
+      my.at = width;
+      my.rank = units;
+#pragma unroll 1
+      for (int off = 1; off < 32; off <<= 1) {
+        const int t = __shfl_up_sync(0xffffffffu, my.at, off), tu = __shfl_up_sync(0xffffffffu, my.rank, off);
+        if (lane >= off) { my.at += t; my.rank += tu; }
+      }
+      if (lane == 31) { warp_sum[warp][0] = my.at; warp_sum[warp][1] = my.rank; }
+      my.at -= width;
+      my.rank -= units;
+    }
+    __syncthreads();
+    int total = 0, units = 0;
+#pragma unroll
+    for (int w = 0; w < kDealers / 32; ++w) {
+      const int x = warp_sum[w][0], y = warp_sum[w][1];
+      if (w < warp) { my.at += x; my.rank += y; }
+      total += x;
+      units += y;
+    }
+    const PagedCut cut(total, int(gridDim.x));
+    if (tid < kDealers) fill(a, window, n_sink, my, cut, share, -1, records);
+    if (tid == 0 && blockIdx.x == 0 && records) records[a.n_units] = PagedRecord{0, 0, 0, total - kPagedLead * units};
+    __syncthreads();
+    return cut;
+  }
+  __device__ __forceinline__ int n_pieces() const { return last - first + 1; }
+  // Before round rank0 / kList, by all threads.  The first is ready if all pieces fit.
+  __device__ __forceinline__ void round(const PagedArgs& a, int window, int n_sink, const Mine& my, const PagedCut& cut, int share, int rank0) {
+    if (n_pieces() <= kList) return;
+    __syncthreads();
+    if (threadIdx.x < kDealers) fill(a, window, n_sink, my, cut, share, first + rank0, nullptr);
+    __syncthreads();
+  }
+  __device__ __forceinline__ const PagedPiece& at(int rank0, int i) const { return list[(first + rank0 + i) & (kList - 1)]; }
 };
 #endif
 
-// Workspace: 256-byte header (word 0: sticky status), where each unit's partial results lie (first slot, number; 0: its
-// only share wrote the result itself), row statistics (maximum in log2 units, sum) and unnormalised outputs of every
-// (slot, head of the group); where weights are accumulated, the scores of every pool row in groups of 16 rows:
+// Workspace: 256-byte header (word 0: sticky status), a record of each unit and one behind them (steps in all), row
+// statistics (maximum in log2 units, sum) and unnormalised outputs of every (slot, head of the group); where weights are accumulated, the scores of every pool row in groups of 16 rows:
 // [pool row / 16][head of the group][16], in log2 units.
 constexpr size_t kPagedHeaderBytes = 256;
 struct PagedWs {
   int* status;
-  int2* table;
+  PagedRecord* records;
+  PagedStepRecord* steps;
   float2* ml;
   float* acc;
   float* score;

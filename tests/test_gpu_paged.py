@@ -144,6 +144,15 @@ def test_more_pieces_than_a_round_holds():
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+def test_long_and_short_pieces_in_a_share(dtype):
+    """Shares of 25 steps and more: pieces longer than the ring of stages, short ones in between."""
+    prm = Q.params(7, 2, 1, 64, dtype)
+    c = Q.make(prm, [200000, 300, 130000, 40, 1, 140000, 900], 128, dtype, 19)
+    before, q = Q.snapshot(c), query(prm, 10, dtype)
+    Q.check(prm, q, c, Q.attend(prm, q, c, accumulate=True), 0, dtype, before)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 def test_shared_pages(dtype):
     """Two sequences read the same pages of a common beginning."""
     prm = Q.params(2, 4, 1, 64, dtype)
