@@ -467,8 +467,8 @@ int tca_cache_accept(const tca_params* prm, tca_cache_desc* cache, const void* k
  * Causal attention with a sliding window and a few first tokens that stay visible ("sinks"), for packed prompts:
  * row i of a sequence attends to its rows j <= i with i - j < prm->window or j < n_sink.  Everything else is
  * tca_attn_packed: buffers, strides, seq_start, empty sequences, rows of nobody, what a row does not see, flags, and
- * the workspace (TCA_OP_PACKED; the two calls may use the same one in turn).  With a window as long as every prompt the
- * result is bit for bit tca_attn_packed's.  The form for single tokens is tca_attn_paged.
+ * the workspace (TCA_OP_PACKED; the two calls may use the same one in turn).  With a window, or
+ * sinks, of at least `rows` the result is bit for bit tca_attn_packed's.  The form for single tokens is tca_attn_paged.
  * n_sink >= 0, else TCA_ERR_INVALID_ARG; prm->window >= 1, else TCA_ERR_UNSUPPORTED.
  */
 int tca_attn_window(const tca_params* prm, const void* Q, const void* K, const void* V, int64_t rows,
@@ -480,8 +480,9 @@ int tca_attn_window(const tca_params* prm, const void* Q, const void* K, const v
  * units of very different lengths, per-head budgets among them, share it.  Slot j of unit u is row j % page_size of page
  * table[u][j / page_size].  All buffers are DEVICE memory of the caller; the struct is HOST memory.  The lengths live in
  * the device state alone: a captured call may be replayed and goes on from there.
- *   state   [n_units][TCA_PG_STATE_WORDS] int32, 16-byte aligned, zeroed once: rows in use, position of the next token,
- *           first failed check (tca_paged_status), a word of the library's
+ *   All buffers but the table are aligned to 16 bytes.
+ *   state   [n_units][TCA_PG_STATE_WORDS] int32, zeroed once: rows in use, position of the next token, first failed check
+ *           (tca_paged_status), a word of the library's
  *   table   entries of slots that are not in use are not read.  Pages may be shared by units while they are only read;
  *           a call that writes to a page (append, evict, attention that accumulates) needs it to be one unit's alone.
  * Supported: page_size 16, 32, 64, 128 or 256; n_pages * page_size and max_pages * page_size below 2^31; up to 65535

@@ -183,9 +183,9 @@ __device__ __forceinline__ void flash_tc_setup(uint8_t* smem, Shared* sh) {
 // Called by all 384 threads after flash_tc_setup and the dependency wait; returns with every thread after
 // the last item.  Source:
 //   struct Item                   plain data
-//   kNoted, kGap                  tiles that are cleaned, at most; whether rows have a gap:
-//                                 row_key's row does not see keys [gap_begin(t), gap_end(key, t)) of tile t
-//                                 either (asked for the tiles that last() is asked for)
+//   kNoted, kBits                 tiles that are cleaned, at most; kBits: tiles are two halves of 64 keys that need not lie
+//                                 together, all of them are taken at full width, and what a row sees of one that it
+//                                 does not see whole is a bit per key
 //   void begin(lane)              whole warp, once: what find() needs
 //   bool find(k, lane, item)      whole warp: the CTA's k-th item; false: there is none
 //   void set(item)                all that follows is about this item
@@ -197,9 +197,11 @@ __device__ __forceinline__ void flash_tc_setup(uint8_t* smem, Shared* sh) {
 //   int  row_key(h)               what last() needs of the row, worked out once per item
 //   int  whole_tiles()            the first so many tiles are seen whole by every row
 //   int  keys(h, t)               keys of tile t that some row of block h sees (1 .. 128)
-//   int  last(key, t)             last key of tile t that the row sees (not asked for those)
-//   int  clean(t)                 -1: nothing to clean; else rows of tile t that somebody sees
-//   int  scan_from(t)             rows [scan_from(t), clean(t)) are searched for non-finite elements
+//   int  last(key, t)             last key of tile t that the row sees (not asked for those); kBits:
+//   uint32_t seen_bits(key, t, c) instead: which of keys 32 c .. 32 c + 31 of tile t
+//   int  clean(t)                 -1: nothing to clean; else rows of tile t that somebody sees; kBits: of half t
+//                                 (0 .. 64; -1 only for both halves of a tile)
+//   int  scan_from(t)             rows [scan_from(t), clean(t)) are searched for non-finite elements; kBits: of half t
 //   int  note_slot(t)             which dirty[] entry a cleaned tile uses
 //   void store(h, seen, m, l, dirty, read)  one finished row per thread, called by whole warps; seen:
 //                                 the block had tiles; dirty: noted key rows or null; read(c, v): requests
@@ -280,7 +282,7 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
           for (int m = -1; m < nt && ok; ++m, ++group) {     // group m: V_m and K_m+lead; m = -1: the leading K tiles
             if (group >= kPairs) ok = wait_group(group - kPairs);
             uint64_t* full = bar_full + group % kPairs;
-            const bool unclean = m >= 0 && src.clean(m) >= 0;
+            const bool unclean = m >= 0 && src.clean(Source::kBits ? 2 * m : m) >= 0;
             if (!unclean) ptx::mbar_arrive(full);            // in the place of the second cleaner
 #pragma unroll
             for (int j = 0; j < 2 && ok; ++j) {
@@ -382,7 +384,7 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
         ++group;
         int t = 0;
 #pragma unroll 1
-        for (const int fast = src.whole_tiles() - kLead; t < fast && ok; ++t, ++group) {
+        for (const int fast = (Source::kBits ? nt : src.whole_tiles()) - kLead; t < fast && ok; ++t, ++group) {
           ok = warp_wait(bar_full + group % kPairs, uint32_t(group / kPairs) & 1u);
           if (kShared) {
             for (int h = 0; h < 2 && ok; ++h) {
@@ -434,54 +436,58 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
         const int n0 = src.tiles(0), n1 = kShared ? src.tiles(1) : 0, nt = kShared ? max(n0, n1) : n0;
         bool ok = true;
         for (int t = 0; t < nt && ok; ++t) {
-          const int seen = src.clean(t);
-          if (seen < 0) continue;
+          if (src.clean(Source::kBits ? 2 * t : t) < 0) continue;
           ok = warp_wait(bar_raw + cleaned % L::kRaw, (cleaned / L::kRaw) & 1u);
           if (!ok) break;
           ++cleaned;
           uint8_t* tile = smem + L::offKV + (base + v_load(t, nt)) % kRing * L::kTile;
-          // One 16-byte piece per lane; the swizzle only permutes the pieces within a row.  The search takes
-          // the maximum of |x| over all pieces of the lane (NaN wins over everything): 2 instructions per
-          // 4 bytes, and only if that is not finite the pieces are looked at one by one.
-          constexpr int kPieces = L::NH * 8;                 // per row
-          auto piece = [&](int i) {                          // i-th piece of the rows this warp takes, rows alternate between the two
-            const int r = 2 * (i / kPieces) + (warp - 2), c = i % kPieces;
-            return reinterpret_cast<uint4*>(tile + (c >> 3) * kTcHalfBytes + r * 128 + (c & 7) * 16);
-          };
-          const int z0 = (max(seen, 0) + 1 - (warp - 2)) / 2;      // first of this warp's rows that nobody sees
-          const int s0 = (src.scan_from(t) + 1 - (warp - 2)) / 2;  // first of its rows to search
-          __nv_bfloat162 top = __floats2bfloat162_rn(0.f, 0.f);
-          for (int i0 = s0 * kPieces + lane; i0 < z0 * kPieces; i0 += 32 * 8) {
-            uint4 v[8];
+          constexpr int kPieces = L::NH * 8, kParts = Source::kBits ? 2 : 1;    // 16-byte pieces of a row; parts of a tile
+#pragma unroll 1
+          for (int p = 0; p < kParts; ++p) {
+            const int part = kParts * t + p, row0 = p * (kTcKeys / 2);          // the part's first row
+            const int seen = src.clean(part);
+            // One 16-byte piece per lane; the swizzle only permutes the pieces within a row.  The search takes
+            // the maximum of |x| over all pieces of the lane (NaN wins over everything): 2 instructions per
+            // 4 bytes, and only if that is not finite the pieces are looked at one by one.
+            auto piece = [&](int i) {                          // i-th piece of the rows this warp takes, rows alternate between the two
+              const int r = row0 + 2 * (i / kPieces) + (warp - 2), c = i % kPieces;
+              return reinterpret_cast<uint4*>(tile + (c >> 3) * kTcHalfBytes + r * 128 + (c & 7) * 16);
+            };
+            const int z0 = (max(seen, 0) + 1 - (warp - 2)) / 2;      // first of this warp's rows that nobody sees
+            const int s0 = (src.scan_from(part) + 1 - (warp - 2)) / 2;  // first of its rows to search
+            __nv_bfloat162 top = __floats2bfloat162_rn(0.f, 0.f);
+            for (int i0 = s0 * kPieces + lane; i0 < z0 * kPieces; i0 += 32 * 8) {
+              uint4 v[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = i0 + 32 * j < z0 * kPieces ? *piece(i0 + 32 * j) : make_uint4(0, 0, 0, 0);
+              for (int j = 0; j < 8; ++j) v[j] = i0 + 32 * j < z0 * kPieces ? *piece(i0 + 32 * j) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              const uint32_t* w = &v[j].x;
+              for (int j = 0; j < 8; ++j) {
+                const uint32_t* w = &v[j].x;
 #pragma unroll
-              for (int e = 0; e < 4; ++e) top = __hmax2_nan(top, __habs2(reinterpret_cast<const __nv_bfloat162&>(w[e])));
-            }
-          }
-          const uint32_t tw = reinterpret_cast<const uint32_t&>(top);
-          if ((tw & 0x7f80u) == 0x7f80u || (tw & 0x7f800000u) == 0x7f800000u) {
-            for (int i = s0 * kPieces + lane; i < z0 * kPieces; i += 32) {
-              uint4 v = *piece(i);
-              uint32_t* w = &v.x;
-              bool hit = false;
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                if ((w[e] & 0x7f80u) == 0x7f80u) { w[e] &= 0xffff0000u; hit = true; }
-                if ((w[e] & 0x7f800000u) == 0x7f800000u) { w[e] &= 0xffffu; hit = true; }
+                for (int e = 0; e < 4; ++e) top = __hmax2_nan(top, __habs2(reinterpret_cast<const __nv_bfloat162&>(w[e])));
               }
-              if (!hit) continue;
-              *piece(i) = v;
-              const int r = 2 * (i / kPieces) + (warp - 2);
-              atomicOr(&sh->dirty[k & 1][src.note_slot(t)][r >> 5], 1u << (r & 31));
-              sh->any_dirty[k & 1] = 1;
             }
+            const uint32_t tw = reinterpret_cast<const uint32_t&>(top);
+            if ((tw & 0x7f80u) == 0x7f80u || (tw & 0x7f800000u) == 0x7f800000u) {
+              for (int i = s0 * kPieces + lane; i < z0 * kPieces; i += 32) {
+                uint4 v = *piece(i);
+                uint32_t* w = &v.x;
+                bool hit = false;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  if ((w[e] & 0x7f80u) == 0x7f80u) { w[e] &= 0xffff0000u; hit = true; }
+                  if ((w[e] & 0x7f800000u) == 0x7f800000u) { w[e] &= 0xffffu; hit = true; }
+                }
+                if (!hit) continue;
+                *piece(i) = v;
+                const int r = row0 + 2 * (i / kPieces) + (warp - 2);
+                atomicOr(&sh->dirty[k & 1][src.note_slot(t)][r >> 5], 1u << (r & 31));
+                sh->any_dirty[k & 1] = 1;
+              }
+            }
+            const int z1 = ((Source::kBits ? kTcKeys / 2 : (seen + 15) & ~15) + 1 - (warp - 2)) / 2;   // the product reads whole k-steps
+            for (int i = z0 * kPieces + lane; i < z1 * kPieces; i += 32) *piece(i) = make_uint4(0, 0, 0, 0);
           }
-          const int z1 = (((seen + 15) & ~15) + 1 - (warp - 2)) / 2;   // the product reads whole k-steps
-          for (int i = z0 * kPieces + lane; i < z1 * kPieces; i += 32) *piece(i) = make_uint4(0, 0, 0, 0);
           ptx::fence_proxy_async_smem();                     // the product reads the tile through the async proxy
           __syncwarp();
           if (lane == 0) ptx::mbar_arrive(bar_full + (group + 1 + t) % kPairs);
@@ -539,7 +545,7 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(bar_p + 2 * h + part);
       };
-      const int whole = kShared ? min(src.whole_tiles(), mine) : (src.whole_tiles() - h + 1) / 2;   // they come first
+      const int whole = Source::kBits ? mine : kShared ? min(src.whole_tiles(), mine) : (src.whole_tiles() - h + 1) / 2;   // they come first
       int it = 0;
 #pragma unroll 1
       for (; it < whole; ++it) {
@@ -551,6 +557,17 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
         for (int c = 0; c < kTcKeys / 32; ++c)
           ptx::tmem_ld32(s_addr + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&v[c * 32]));
         ptx::tc_wait_ld();
+        if constexpr (Source::kBits) {
+          if (it >= src.whole_tiles()) {
+#pragma unroll
+            for (int c = 0; c < kTcKeys / 32; ++c) {
+              const uint32_t bits = src.seen_bits(row_key, it, c);
+#pragma unroll
+              for (int k = 0; k < 32; ++k)       // a key the row does not see has weight 0, whatever its score
+                if (!((bits >> k) & 1u)) v[c * 32 + k] = 0xff800000u;
+            }
+          }
+        }
         float mx;
         {
           float mx8[8];
@@ -592,6 +609,7 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
         ptx::unpack2(sum2[1], s2, s3);
         l += (s0 + s1) + (s2 + s3);
       }
+      if constexpr (!Source::kBits)
 #pragma unroll 1
       for (; it < mine && ok; ++it) {
         const int t = kShared ? it : 2 * it + h;
@@ -601,12 +619,6 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
         // A tile that some row does not see all of (the diagonal, the end of a run): the 32-key groups that
         // somebody sees, in a compact loop that reads the scores twice.
         const int hi = src.last(row_key, t), groups = (src.keys(h, t) + 31) >> 5;
-        int gap0 = 0, gap1 = 0;
-        if constexpr (Source::kGap) { gap0 = src.gap_begin(t); gap1 = src.gap_end(row_key, t); }
-        auto hidden_of = [&](int c) -> uint32_t {          // of keys 32 c .. 32 c + 31: bits of those in the gap
-          auto below = [](int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; };
-          return Source::kGap ? below(gap1 - c * 32) & ~below(gap0 - c * 32) : 0u;
-        };
         float mx = -INFINITY;
 #pragma unroll 1
         for (int c = 0; c < groups; ++c) {
@@ -614,10 +626,9 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
           ptx::tmem_ld32(s_addr + c * 32, v);
           ptx::tc_wait_ld();
           const int last = hi - c * 32;
-          const uint32_t hidden = hidden_of(c);
 #pragma unroll
           for (int k = 0; k < 32; ++k)
-            if (k <= last && !(Source::kGap && (hidden >> k) & 1u)) mx = fmaxf(mx, __uint_as_float(v[k]));
+            if (k <= last) mx = fmaxf(mx, __uint_as_float(v[k]));
         }
         rescale(mx, it > 0);
         const float neg_m = (m_used == -INFINITY) ? 0.f : -m_used;
@@ -628,12 +639,10 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
           ptx::tmem_ld32(s_addr + c * 32, v);
           ptx::tc_wait_ld();
           const int last = hi - c * 32;
-          const uint32_t hidden = hidden_of(c);
-          auto sees = [&](int k) { return k <= last && !(Source::kGap && (hidden >> k) & 1u); };
 #pragma unroll
           for (int k = 0; k < 32; k += 2) {    // a key the row does not see has weight 0, whatever its score
-            const float el = sees(k) ? ptx::fast_exp2(fmaf(__uint_as_float(v[k]), scale_log2e, neg_m)) : 0.f;
-            const float eh = sees(k + 1) ? ptx::fast_exp2(fmaf(__uint_as_float(v[k + 1]), scale_log2e, neg_m)) : 0.f;
+            const float el = k <= last ? ptx::fast_exp2(fmaf(__uint_as_float(v[k]), scale_log2e, neg_m)) : 0.f;
+            const float eh = k + 1 <= last ? ptx::fast_exp2(fmaf(__uint_as_float(v[k + 1]), scale_log2e, neg_m)) : 0.f;
             sum += el + eh;
             v[k / 2] = ptx::pack_bf16x2(el, eh);
           }

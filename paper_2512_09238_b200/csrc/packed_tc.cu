@@ -17,48 +17,75 @@ namespace {
 // both zero between calls.
 constexpr int kCounterWord = 16, kLeftWord = 32;
 
-// A run of key tiles that lie one behind the other: tile t >= first begins at key 128 t + shift.
+constexpr int kHalf = kTcKeys / 2;
+
+// A run of half tiles that lie one behind the other: half i >= first begins at key 64 i + shift.
 struct KeyRun {
   int first, shift;
 };
 
-// The key tiles of query positions p0 .. last of a sequence under a window of w keys and S sinks, in the order in which
-// they are taken: those that every row sees whole come first (flash_tc.cuh).  The band begins at key b0: the first that
-// the first row's window holds, or 0 where the sinks reach it; sinks in front of the band have tiles of their own.
+// The keys of query positions p0 .. last of a sequence under a window of w keys and S sinks, in halves of tiles (64
+// keys), in the order in which they are taken: those that every row sees whole come first (flash_tc.cuh).  The band
+// begins at key b0: the first that the first row's window holds, or 0 where the sinks reach it; sinks in front of the
+// band have halves of their own.  Halves, because the band's two edges, 2 P keys each, and the sinks then share tiles: 512
+// keys and 16 sinks for 64 positions are 5 tiles instead of 6.
 struct WindowTiles {
-  int n, whole;            // tiles; of them whole
-  KeyRun run[5];           // whole sink tiles, whole band tiles, the rest of the sinks, lower and upper edge of the band
-  int rest;                // keys of the third run's tile
+  int n, whole;            // halves; of them whole
+  KeyRun run[5];           // whole sink halves, whole band halves, the rest of the sinks, lower and upper edge of the band
+  int rest;                // keys of the third run's half
   __host__ __device__ WindowTiles() {}
   __host__ __device__ WindowTiles(int p0, int last, int w, int sinks) {
     const int c_lo = p0 - w + 1 > 0 ? p0 - w + 1 : 0;     // first key of the first row's window
     const int all_lo = last - w + 1 > 0 ? last - w + 1 : 0;   // first key of every row's window
     const bool apart = sinks < c_lo;
     const int b0 = apart ? c_lo : 0;
-    const int n_band = (last - b0) / kTcKeys + 1;
-    const int to_diag = (p0 + 1 - b0) / kTcKeys;           // band tiles in front of the diagonal
-    const int in_sinks = apart ? 0 : sinks / kTcKeys < to_diag ? sinks / kTcKeys : to_diag;
-    const int from = (all_lo - b0 + kTcKeys - 1) / kTcKeys;
-    const int a = from > in_sinks ? from : in_sinks;       // band tiles [a, to_diag) are whole
-    const int w0 = apart ? sinks / kTcKeys : in_sinks, w1 = to_diag > a ? to_diag - a : 0;
-    rest = apart ? sinks % kTcKeys : 0;
+    const int n_band = (last - b0) / kHalf + 1;
+    const int to_diag = (p0 + 1 - b0) / kHalf;             // band halves in front of the diagonal
+    const int in_sinks = apart ? 0 : sinks / kHalf < to_diag ? sinks / kHalf : to_diag;
+    const int from = (all_lo - b0 + kHalf - 1) / kHalf;
+    const int a = from > in_sinks ? from : in_sinks;       // band halves [a, to_diag) are whole
+    const int w0 = apart ? sinks / kHalf : in_sinks, w1 = to_diag > a ? to_diag - a : 0;
+    rest = apart ? sinks % kHalf : 0;
     const int r = rest > 0 ? 1 : 0;
-    const int low = (a < n_band ? a : n_band) - in_sinks;  // tiles [in_sinks, a): some row's window begins inside
+    const int low = (a < n_band ? a : n_band) - in_sinks;  // halves [in_sinks, a): some row's window begins inside
     const int up = to_diag > in_sinks + low ? to_diag : in_sinks + low;
     whole = w0 + w1;
     n = whole + r + low + (n_band - up);
     run[0] = KeyRun{0, 0};
-    run[1] = KeyRun{w0, b0 + (a - w0) * kTcKeys};
-    run[2] = KeyRun{whole, (w0 - whole) * kTcKeys};
-    run[3] = KeyRun{whole + r, b0 + (in_sinks - whole - r) * kTcKeys};
-    run[4] = KeyRun{whole + r + low, b0 + (up - whole - r - low) * kTcKeys};
+    run[1] = KeyRun{w0, b0 + (a - w0) * kHalf};
+    run[2] = KeyRun{whole, (w0 - whole) * kHalf};
+    run[3] = KeyRun{whole + r, b0 + (in_sinks - whole - r) * kHalf};
+    run[4] = KeyRun{whole + r + low, b0 + (up - whole - r - low) * kHalf};
   }
-  __host__ __device__ int key0(int t) const {
+  __host__ __device__ int key0(int half) const {           // of a half that is not there: the last one's
+    const int i = half < n ? half : n - 1;
     int shift = 0;
-    for (int i = 1; i < 5; ++i) shift = t >= run[i].first ? run[i].shift : shift;
-    return t * kTcKeys + shift;
+    for (int k = 1; k < 5; ++k) shift = i >= run[k].first ? run[k].shift : shift;
+    return i * kHalf + shift;
   }
-  __host__ __device__ bool is_rest(int t) const { return rest > 0 && t == whole; }
+  __host__ __device__ bool is_rest(int half) const { return rest > 0 && half == whole; }
+  // rows of a half that somebody sees, and from which on some row may not see one
+  __host__ __device__ int seen(int half, int last) const {
+    if (half >= n) return 0;
+    if (is_rest(half)) return rest;
+    const int k = last + 1 - key0(half);
+    return k < kHalf ? k : kHalf;
+  }
+  __host__ __device__ int scan_from(int half, int p0, int last, int w) const {
+    if (half < whole || half >= n || is_rest(half)) return kHalf;
+    const int k0 = key0(half);
+    if (half < run[4].first || k0 <= last - w) return 0;
+    return p0 + 1 > k0 ? p0 + 1 - k0 : 0;
+  }
+  // Which of keys 32 c .. 32 c + 31 of tile t the row at `pos` sees.
+  __host__ __device__ static uint32_t below(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; }
+  __host__ __device__ uint32_t seen_bits(int pos, int t, int c, int w, int sinks) const {
+    const int half = 2 * t + (c >> 1), off = (c & 1) * 32;
+    if (half >= n) return 0u;
+    if (is_rest(half)) return below(rest - off);
+    const int k0 = key0(half) + off;
+    return below(pos + 1 - k0) & ~(below(pos - w + 1 - k0) & ~below(sinks - k0));
+  }
 };
 
 template <bool kWindow>
@@ -77,7 +104,7 @@ template <int D, bool kWindow>
 struct PackedTcSrc {
   using Item = PackedItem<kWindow>;
   static constexpr int kNoted = kWindow ? 6 : 2;
-  static constexpr bool kGap = kWindow;
+  static constexpr bool kBits = kWindow;
   const CUtensorMap *mq, *mk, *mv;
   const __nv_bfloat16* V;
   __nv_bfloat16* O;
@@ -122,18 +149,10 @@ struct PackedTcSrc {
     if constexpr (kWindow) win = it.tiles;
   }
 
-  __device__ __forceinline__ int key0(int t) const {      // first key of tile t
-    if constexpr (kWindow) return win.key0(t);
-    return t * kTcKeys;
-  }
   __device__ __forceinline__ int last_pos(int h) const { return min(p0 + (h + 1) * P, len) - 1; }
   __device__ __forceinline__ int tiles(int h) const {
     if (p0 + h * P >= len) return 0;
-    if constexpr (kWindow) {
-      int n = win.n;                       // but for those behind the block's last row, which are the last ones
-      while (n > win.whole && win.key0(n - 1) > last_pos(h)) --n;
-      return n;
-    }
+    if constexpr (kWindow) return (win.n + 1) / 2;
     return last_pos(h) / kTcKeys + 1;
   }
   __device__ __forceinline__ int q_bytes(int) const { return D * 2 * G * P; }
@@ -142,40 +161,35 @@ struct PackedTcSrc {
       ptx::tma_load_3d(dst + half * kTcHalfBytes, mq, half * 64, kvh * G, int(row0) + p0 + h * P, bar);
   }
   __device__ __forceinline__ void load(int t, bool is_v, uint8_t* dst, uint64_t* bar) const {
-    for (int half = 0; half < D / 64; ++half)
-      ptx::tma_load_3d(dst + half * kTcHalfBytes, is_v ? mv : mk, half * 64, int(row0) + key0(t), kvh, bar);
+    for (int part = 0; part < (kWindow ? 2 : 1); ++part) {   // boxes of 64 rows or of 128
+      const int row = int(row0) + (kWindow ? win.key0(2 * t + part) : t * kTcKeys);
+      for (int half = 0; half < D / 64; ++half)
+        ptx::tma_load_3d(dst + half * kTcHalfBytes + part * (kTcHalfBytes / 2), is_v ? mv : mk, half * 64, row, kvh, bar);
+    }
   }
   int dp, g;                // this thread's row: position and head within the block
   __device__ __forceinline__ void begin_row(int row) { dp = row / G; g = row % G; }
   __device__ __forceinline__ int row_key(int h) const { return min(p0 + h * P + dp, last_pos(h)); }
-  __device__ __forceinline__ int last(int key, int t) const {
-    if constexpr (kWindow) { if (win.is_rest(t)) return win.rest - 1; }
-    return key - key0(t);
-  }
-  __device__ __forceinline__ int gap_begin(int t) const { return a->n_sink - key0(t); }
-  __device__ __forceinline__ int gap_end(int key, int t) const { return key - a->window + 1 - key0(t); }
+  __device__ __forceinline__ int last(int key, int t) const { return key - t * kTcKeys; }
+  __device__ __forceinline__ uint32_t seen_bits(int key, int t, int c) const { return win.seen_bits(key, t, c, a->window, a->n_sink); }
   __device__ __forceinline__ int whole_tiles() const {
-    if constexpr (kWindow) return win.whole;
+    if constexpr (kWindow) return win.whole / 2;
     return p0 / kTcKeys;
   }
   __device__ __forceinline__ int keys(int h, int t) const {
-    if constexpr (kWindow) { if (win.is_rest(t)) return win.rest; }
-    return min(kTcKeys, last_pos(h) + 1 - key0(t));
+    if constexpr (kWindow) return kTcKeys;
+    return min(kTcKeys, last_pos(h) + 1 - t * kTcKeys);
   }
   // From the tile that holds p0 on, some row does not see some key (at most two tiles: 2 P <= 128, or
-  // P = 128 with p0 a multiple of 256; with a window at most six, counting its lower edge and the rest of the sinks).
-  // Rows past the last position are nobody's: another sequence's, or none; rows up to p0 are everybody's.
-  __device__ __forceinline__ int clean(int t) const {
-    if constexpr (kWindow) { if (win.is_rest(t)) return win.rest; }
-    return t < whole_tiles() ? -1 : min(kTcKeys, min(p0 + 2 * P, len) - key0(t));
+  // P = 128 with p0 a multiple of 256; with a window at most six).  Rows past the last position are nobody's: another
+  // sequence's, or none; rows up to p0 are everybody's.
+  __device__ __forceinline__ int clean(int t) const {      // window: of half t
+    if constexpr (kWindow) return t / 2 < whole_tiles() ? -1 : win.seen(t, last_pos(1));
+    return t < whole_tiles() ? -1 : min(kTcKeys, min(p0 + 2 * P, len) - t * kTcKeys);
   }
   __device__ __forceinline__ int scan_from(int t) const {
-    if constexpr (kWindow) {
-      if (win.is_rest(t)) return win.rest;                 // everybody sees the sinks
-      if (t < win.run[4].first) return 0;
-      if (win.key0(t) <= min(p0 + 2 * P, len) - 1 - a->window) return 0;   // a lower edge as well
-    }
-    return max(0, p0 + 1 - key0(t));
+    if constexpr (kWindow) return win.scan_from(t, p0, last_pos(1), a->window);
+    return max(0, p0 + 1 - t * kTcKeys);
   }
   __device__ __forceinline__ int note_slot(int t) const { return t - whole_tiles(); }
 
@@ -203,9 +217,14 @@ struct PackedTcSrc {
 #pragma unroll 1
       for (int i = 0; i < 4 * kNoted; ++i)
         for (uint32_t bits = dirty[i]; bits; bits &= bits - 1) {
-          const int key = key0(whole_tiles() + (i >> 2)) + (i & 3) * 32 + __ffs(bits) - 1;
-          if (key > pos) break;
-          if (kWindow && key <= pos - a->window && key >= a->n_sink) continue;
+          const int bit = __ffs(bits) - 1, t = whole_tiles() + (i >> 2);
+          int key = t * kTcKeys + (i & 3) * 32 + bit;
+          if constexpr (kWindow) {
+            if (!((seen_bits(pos, t, i & 3) >> bit) & 1u)) continue;
+            key = win.key0(2 * t + ((i >> 1) & 1)) + (i & 1) * 32 + bit;
+          } else if (key > pos) {
+            break;
+          }
           const __nv_bfloat16* src = V + kvh * a->v.head + (row0 + key) * a->v.row;
 #pragma unroll 1
           for (int k = 0; k < D; ++k) {
@@ -266,8 +285,8 @@ int launch_packed_tc(const tca_params* prm, const void* Q, const void* K, const 
     return TCA_ERR_UNSUPPORTED;
   CUtensorMap mq, mk, mv;
   if (!encode_map_3d(&mq, Q, D, a.n_q_heads, a.rows, a.q.head, a.q.row, G, P) ||
-      !encode_map_3d(&mk, K, D, a.rows, a.n_kv_heads, a.k.row, a.k.head, kTcKeys, 1) ||
-      !encode_map_3d(&mv, V, D, a.rows, a.n_kv_heads, a.v.row, a.v.head, kTcKeys, 1))
+      !encode_map_3d(&mk, K, D, a.rows, a.n_kv_heads, a.k.row, a.k.head, kWindow ? kHalf : kTcKeys, 1) ||
+      !encode_map_3d(&mv, V, D, a.rows, a.n_kv_heads, a.v.row, a.v.head, kWindow ? kHalf : kTcKeys, 1))
     return TCA_ERR_CUDA;
   auto kern = packed_tc_kernel<D, kWindow>;
   if (allow_smem<packed_tc_kernel<D, kWindow>>(TcLayout<D>::bytes) != TCA_OK) return TCA_ERR_CUDA;

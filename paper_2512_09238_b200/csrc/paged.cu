@@ -29,8 +29,8 @@ int check_paged(const tca_params* prm, const tca_paged_desc* c) {
   const int st = check_params(prm);
   if (st != TCA_OK) return st;
   TCA_CHECK_ARG(c && c->k && c->v && c->pos && c->mass && c->table && c->state);
-  TCA_CHECK_ARG(aligned(c->k, 16) && aligned(c->v, 16) && aligned(c->state, 16));
-  TCA_CHECK_ARG(aligned(c->pos, 4) && aligned(c->mass, 4) && aligned(c->table, 4));
+  TCA_CHECK_ARG(aligned(c->k, 16) && aligned(c->v, 16) && aligned(c->state, 16) && aligned(c->pos, 16) && aligned(c->mass, 16));
+  TCA_CHECK_ARG(aligned(c->table, 4));
   TCA_CHECK_ARG(c->n_units == int64_t(prm->batch) * prm->n_kv_heads && c->n_pages >= 1 && c->max_pages >= 1);
   if (!is_pow2(c->page_size) || c->page_size < 16 || c->page_size > 256) return TCA_ERR_UNSUPPORTED;
   constexpr int64_t kMost = int64_t(1) << 31;

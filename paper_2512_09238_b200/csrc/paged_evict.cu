@@ -1,13 +1,14 @@
 // tca_paged_evict: a unit keeps its sinks, its recent rows and, of the others, those that gathered the most attention
 // weight; the kept rows behind the budget move into the holes in front of it.
 //
-// One cluster of CTAs per unit, each with a run of the unit's slots.  The weights become order-preserving 32-bit keys,
-// held in shared memory; the smallest kept key is found by radix selection, 8 bits at a time, on histograms that the CTAs
-// read from one another's shared memory.  The i-th hole below the budget takes the i-th kept row behind it: sources and
-// destinations are disjoint, so rows move in any order, and no more of them than have to (keeping the order of slots
-// would move all rows behind the first hole, through a staging buffer).  The pairs are put into shared memory by their
-// number, equally many per CTA, so that the copies are dealt evenly wherever the rows lie.
-// Bound by latency for short units, by memory for long ones: 8 bytes a row (weight, position) and 2 (2 d + 8) bytes and more a
+// One cluster of CTAs per unit, each with a run of the unit's slots, four of which a thread reads at a time (a page holds a
+// multiple of four).  The weights become order-preserving 32-bit keys, held in shared memory; the smallest kept key is
+// found by radix selection, 8 bits at a time, on histograms that the CTAs read from one another's shared memory.  The
+// i-th hole below the budget takes the i-th kept row behind it: sources and destinations are disjoint, so rows move in any
+// order, and no more of them than have to (keeping the order of slots would move all rows behind the first hole, through
+// a staging buffer).  The pairs are put into shared memory by their number, equally many per CTA, so that the copies are
+// dealt evenly wherever the rows lie.
+// Bound by latency for short units, by memory for long ones: 8 bytes a row (weight, position) and 2 (4 d + 8) bytes and more a
 // moved row.
 #include <climits>
 
@@ -21,9 +22,9 @@ namespace {
 namespace cg = cooperative_groups;
 
 constexpr int kThreads = 512, kWarps = kThreads / 32;
-constexpr int kMaxCluster = 8;
+constexpr int kMaxCluster = 16;          // more than 8 is not portable: evict_cluster() asks the device
 constexpr int kMostSlots = 1 << 22;      // slots of a unit: one bit each has to fit a cluster's shared memory
-constexpr int kHeld = 12 * 1024;         // slots of a CTA whose key and pool row are held; the others' are read again
+constexpr int kHeld = 8 * 1024;          // slots of a CTA whose key and position are held; the others' are read again
 constexpr int kPairs = 4 * 1024;         // moves of a CTA at a time
 constexpr uint32_t kSafe = 0xFFFFFFFFu;  // key of a sink or recent row; a NaN has the one below
 
@@ -44,12 +45,14 @@ struct EvictShared {
   int max_pos[kMaxCluster], bad[kMaxCluster], safe[kMaxCluster];   // of every CTA of the cluster, written by each
   int2 counts[kMaxCluster];                                        // holes, kept rows behind the budget
   int scan[kWarps][2];
-  unsigned hist[2][256];                  // this CTA's; two, so that one barrier per digit is enough
+  unsigned hist[256];                     // this CTA's
+  unsigned sum[2][256];                   // the cluster's, added up by all; two, so that one barrier per digit is enough
   unsigned picked;
-  int need, equals, equal_before;         // left to find; keys equal to the threshold, those of the CTAs before
+  int need, equals;                       // left to find; keys equal to the threshold
+  int equal[kMaxCluster];
 };
 
-// Dynamic shared memory: keys [held_cap], pool rows [held_cap], moves (from, to) [pair_cap], a bit per slot: kept.
+// Dynamic shared memory: keys and positions [held_cap], moves (from, to) [pair_cap], a bit per slot: kept.
 struct EvictSizes {
   int held_cap, pair_cap, words;
   int bytes() const { return held_cap * 8 + pair_cap * 8 + words * 4; }
@@ -57,13 +60,13 @@ struct EvictSizes {
 
 __device__ __forceinline__ unsigned low_bits(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; }
 
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 2)
 evict_kernel(const __grid_constant__ EvictBuffers b, const __grid_constant__ PagedArgs args, int n_sink, int n_recent,
              const int32_t* __restrict__ budgets, EvictSizes sizes) {
   extern __shared__ __align__(16) uint32_t evict_smem[];
   __shared__ EvictShared sh;
   uint32_t* keys = evict_smem;
-  int* rows = reinterpret_cast<int*>(evict_smem + sizes.held_cap);
+  int* held_pos = reinterpret_cast<int*>(evict_smem + sizes.held_cap);
   int2* pairs = reinterpret_cast<int2*>(evict_smem + 2 * sizes.held_cap);
   uint32_t* kept = evict_smem + 2 * sizes.held_cap + 2 * sizes.pair_cap;
   cg::cluster_group cluster = cg::this_cluster();
@@ -76,26 +79,33 @@ evict_kernel(const __grid_constant__ EvictBuffers b, const __grid_constant__ Pag
   const int len = paged_len(args, st->x), budget = budgets[u];
   if (len <= budget) return;                              // the whole cluster alike, before any barrier
   cluster.barrier_arrive();
-  const int per = (len + n_ctas - 1) / n_ctas;
-  const int s0 = min(len, rank * per), n = min(len, s0 + per) - s0, held = min(n, sizes.held_cap);
+  const int per = ((len + n_ctas - 1) / n_ctas + 63) & ~63;   // a multiple of four slots, and of a word of bits
+  const int s0 = min(len, rank * per), n = min(len, s0 + per) - s0, held = min((n + 3) & ~3, sizes.held_cap);
 
-  // ---- one pass over positions and weights
+  // ---- one pass over positions and weights, four slots at a time
   int top = INT_MIN;
   bool bad = false;
 #pragma unroll 4
-  for (int i = tid; i < n; i += kThreads) {
+  for (int i = tid * 4; i < n; i += kThreads * 4) {
     const int row = paged_row(args, u, s0 + i);
     if (row < 0) { bad = true; continue; }
-    top = max(top, b.pos[row]);
+    int4 pos = *reinterpret_cast<const int4*>(b.pos + row);
+    const float4 w = *reinterpret_cast<const float4*>(b.mass + row);
+    // (what lies behind the last row counts for nothing below)
+    if (i + 1 >= n) pos.y = INT_MIN;
+    if (i + 2 >= n) pos.z = INT_MIN;
+    if (i + 3 >= n) pos.w = INT_MIN;
+    top = max(max(top, max(pos.x, pos.y)), max(pos.z, pos.w));
     if (i < held) {
-      keys[i] = mass_key(b.mass[row]);
-      rows[i] = row;
+      *reinterpret_cast<uint4*>(keys + i) = make_uint4(mass_key(w.x), mass_key(w.y), mass_key(w.z), mass_key(w.w));
+      *reinterpret_cast<int4*>(held_pos + i) = pos;
     }
   }
   top = __reduce_max_sync(0xffffffffu, top);
   bad = __any_sync(0xffffffffu, bad);
   if (lane == 0) { sh.scan[warp][0] = top; sh.scan[warp][1] = bad; }
-  sh.hist[tid >> 8][tid & 255] = 0;
+  sh.sum[tid >> 8][tid & 255] = 0;
+  if (tid < 256) sh.hist[tid] = 0;
   __syncthreads();
   cluster.barrier_wait();                                 // every CTA of the cluster runs: its memory can be written
   if (tid < n_ctas) {
@@ -113,24 +123,27 @@ evict_kernel(const __grid_constant__ EvictBuffers b, const __grid_constant__ Pag
     return;
   }
   const int64_t recent_from = int64_t(newest) - n_recent; // positions above it are recent
-  auto row_of = [&](int i) { return i < held ? rows[i] : paged_row(args, u, s0 + i); };
-  auto key_of = [&](int i) -> uint32_t {                  // of slot s0 + i
-    if (i < held) return keys[i];
-    const int row = paged_row(args, u, s0 + i);
-    return s0 + i < n_sink || b.pos[row] > recent_from ? kSafe : mass_key(b.mass[row]);
+  auto row_of = [&](int i) { return paged_row(args, u, s0 + i); };
+  // Keys of slots s0 + i .. + 3 (i a multiple of four below n): a safe row has the highest.
+  auto mark = [&](uint32_t key, int pos, int i) { return s0 + i < n_sink || pos > recent_from ? kSafe : key; };
+  auto four = [&](int i) -> uint4 {
+    if (i < held) return *reinterpret_cast<const uint4*>(keys + i);
+    const int row = row_of(i);
+    const int4 pos = *reinterpret_cast<const int4*>(b.pos + row);
+    const float4 w = *reinterpret_cast<const float4*>(b.mass + row);
+    return make_uint4(mark(mass_key(w.x), pos.x, i), mark(mass_key(w.y), pos.y, i + 1), mark(mass_key(w.z), pos.z, i + 2), mark(mass_key(w.w), pos.w, i + 3));
   };
 
-  // ---- safe rows get the highest key; how many are there?
+  // ---- how many rows are safe?
   int safe = 0;
-#pragma unroll 4
-  for (int i = tid; i < n; i += kThreads) {
+  for (int i = tid * 4; i < n; i += kThreads * 4) {
+    uint4 k = four(i);
     if (i < held) {
-      const bool is = s0 + i < n_sink || b.pos[rows[i]] > recent_from;
-      if (is) keys[i] = kSafe;
-      safe += is;
-    } else {
-      safe += key_of(i) == kSafe;
+      const int4 pos = *reinterpret_cast<const int4*>(held_pos + i);
+      k = make_uint4(mark(k.x, pos.x, i), mark(k.y, pos.y, i + 1), mark(k.z, pos.z, i + 2), mark(k.w, pos.w, i + 3));
+      *reinterpret_cast<uint4*>(keys + i) = k;
     }
+    safe += (k.x == kSafe) + (i + 1 < n && k.y == kSafe) + (i + 2 < n && k.z == kSafe) + (i + 3 < n && k.w == kSafe);
   }
   safe = __reduce_add_sync(0xffffffffu, safe);
   if (lane == 0) sh.scan[warp][0] = safe;
@@ -145,18 +158,24 @@ evict_kernel(const __grid_constant__ EvictBuffers b, const __grid_constant__ Pag
   int need = 0;
   for (int digit = 0; digit < 4; ++digit) {
     const int shift = 24 - 8 * digit;
-    unsigned* hist = sh.hist[digit & 1];
-    for (int i0 = 0; i0 < n; i0 += kThreads) {
-      const int i = i0 + tid;
-      const uint32_t k = i < n ? key_of(i) : kSafe;
-      const bool in = k != kSafe && (digit == 0 || (k >> (shift + 8)) == prefix);
-      // equal digits of a warp are counted together: weights have few different exponents
-      const unsigned active = __ballot_sync(0xffffffffu, in);
-      if (in) {
-        const unsigned d = (k >> shift) & 255u;
-        const unsigned same = __match_any_sync(active, d);
-        if (lane == __ffs(same) - 1) atomicAdd(&hist[d], unsigned(__popc(same)));
+    for (int i = tid * 4; i < n; i += kThreads * 4) {
+      const uint4 k4 = four(i);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t k = e == 0 ? k4.x : e == 1 ? k4.y : e == 2 ? k4.z : k4.w;
+        const bool in = i + e < n && k != kSafe && (digit == 0 || (k >> (shift + 8)) == prefix);
+        if (in) atomicAdd(&sh.hist[(k >> shift) & 255u], 1u);   // (counting equal digits of a warp together first is slower)
       }
+    }
+    __syncthreads();
+    if (tid < 256) {
+      // every CTA adds its counts to everybody's (read from the others after the barrier they took 1.2 us more a digit)
+      const unsigned v = sh.hist[tid];
+      if (v)
+        for (int c = 0; c < n_ctas; ++c) atomicAdd(&cluster.map_shared_rank(&sh, c)->sum[digit & 1][tid], v);
+      if (digit < 3) sh.hist[tid] = 0;
+    } else {
+      sh.sum[(digit + 1) & 1][tid - 256] = 0;     // read before the last barrier, added to after the next
     }
     cluster.sync();
     if (digit == 0) {
@@ -169,14 +188,9 @@ evict_kernel(const __grid_constant__ EvictBuffers b, const __grid_constant__ Pag
     }
     // the bin at which the count from above reaches need, one bin per thread; if nothing is needed the highest, of
     // which nothing is kept
-    unsigned total = 0, before = 0, count = 0;
+    unsigned total = 0, count = 0;
     if (tid < 256) {
-      for (int c = 0; c < n_ctas; ++c) {
-        const unsigned v = cluster.map_shared_rank(&sh, c)->hist[digit & 1][255 - tid];
-        total += v;
-        if (c < rank) before += v;
-      }
-      count = total;
+      count = total = sh.sum[digit & 1][255 - tid];
 #pragma unroll
       for (int off = 1; off < 32; off <<= 1) {
         const unsigned t = __shfl_up_sync(0xffffffffu, count, off);
@@ -192,9 +206,7 @@ evict_kernel(const __grid_constant__ EvictBuffers b, const __grid_constant__ Pag
         sh.picked = 255 - tid;
         sh.need = need - above;
         sh.equals = int(total);
-        sh.equal_before = int(before);
       }
-      sh.hist[(digit + 1) & 1][tid] = 0;                  // its readers passed the barrier above
     }
     __syncthreads();
     prefix = (prefix << 8) | sh.picked;
@@ -204,34 +216,56 @@ evict_kernel(const __grid_constant__ EvictBuffers b, const __grid_constant__ Pag
   // ---- which slots are kept: keys above the threshold, and of those equal to it the `need` lowest slots
   const int words = (n + 31) >> 5;
   const bool tie = need != sh.equals;                     // the whole cluster alike
-  int equals = sh.equal_before;
-  for (int i0 = 0; i0 < n; i0 += kThreads) {
-    const int i = i0 + tid;
-    const uint32_t k = i < n ? key_of(i) : 0u;
-    bool keep = i < n && (k == kSafe || k > prefix);
+  int equals = 0;                                         // of the slots before: keys equal to the threshold
+  if (tie && need > 0) {
+    if (tid < n_ctas) cluster.map_shared_rank(&sh, tid)->equal[rank] = int(sh.hist[sh.picked]);
+    cluster.sync();
+    for (int c = 0; c < rank; ++c) equals += sh.equal[c];
+  }
+  for (int i0 = 0; i0 < n; i0 += kThreads * 4) {
+    const int i = i0 + tid * 4;
+    const uint4 k4 = i < n ? four(i) : make_uint4(0, 0, 0, 0);
+    unsigned nibble = 0, eq = 0;                          // of the four slots: kept, equal to the threshold
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t k = e == 0 ? k4.x : e == 1 ? k4.y : e == 2 ? k4.z : k4.w;
+      if (i + e >= n) continue;
+      if (k == kSafe || k > prefix) nibble |= 1u << e;
+      if (need > 0 && k == prefix) eq |= 1u << e;
+    }
     if (!tie) {
-      keep |= i < n && need > 0 && k == prefix;
+      nibble |= eq;
     } else if (need > 0) {
-      const unsigned eq = __ballot_sync(0xffffffffu, i < n && k == prefix);
+      int incl = __popc(eq);
+#pragma unroll
+      for (int off = 1; off < 32; off <<= 1) {
+        const int t = __shfl_up_sync(0xffffffffu, incl, off);
+        if (lane >= off) incl += t;
+      }
       __syncthreads();                                    // the counts of the chunk before have been read
-      if (lane == 0) sh.scan[warp][0] = __popc(eq);
+      if (lane == 31) sh.scan[warp][0] = incl;
       __syncthreads();
-      int mine = equals;
+      int mine = equals + incl - __popc(eq);
       for (int w = 0; w < kWarps; ++w) {
         if (w < warp) mine += sh.scan[w][0];
         equals += sh.scan[w][0];
       }
-      keep |= ((eq >> lane) & 1u) && mine + __popc(eq & low_bits(lane)) < need;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if ((eq >> e) & 1u) nibble |= (mine++ < need ? 1u : 0u) << e;
     }
-    const unsigned word = __ballot_sync(0xffffffffu, keep);
-    if (lane == 0 && (i0 >> 5) + warp < words) kept[(i0 >> 5) + warp] = word;
+    unsigned word = nibble << (lane & 7) * 4;             // eight lanes make a word of 32 slots
+#pragma unroll
+    for (int off = 1; off < 8; off <<= 1) word |= __shfl_xor_sync(0xffffffffu, word, off);
+    if ((lane & 7) == 0 && (i >> 5) < words) kept[i >> 5] = word;
   }
   __syncthreads();
-  // holes below the budget and kept rows behind it, of one word of 32 slots
-  auto holes_of = [&](int w) { return w < words ? ~kept[w] & low_bits(n - w * 32) & low_bits(budget - s0 - w * 32) : 0u; };
-  auto late_of = [&](int w) { return w < words ? kept[w] & ~low_bits(budget - s0 - w * 32) : 0u; };
+  // holes below the budget and kept rows behind it, of one word of 32 slots; each warp has a run of words
+  auto holes_of = [&](int w) { return ~kept[w] & low_bits(n - w * 32) & low_bits(budget - s0 - w * 32); };
+  auto late_of = [&](int w) { return kept[w] & ~low_bits(budget - s0 - w * 32); };
+  const int w_begin = words * warp / kWarps, w_end = words * (warp + 1) / kWarps;
   int n_holes = 0, n_late = 0;
-  for (int w = tid; w < words; w += kThreads) {
+  for (int w = w_begin + lane; w < w_end; w += 32) {
     n_holes += __popc(holes_of(w));
     n_late += __popc(late_of(w));
   }
@@ -245,7 +279,8 @@ evict_kernel(const __grid_constant__ EvictBuffers b, const __grid_constant__ Pag
     cluster.map_shared_rank(&sh, tid)->counts[rank] = t;
   }
   cluster.sync();
-  int hole0 = 0, late0 = 0, moves = 0;
+  int hole0 = 0, late0 = 0, moves = 0;                    // numbers before this warp's words
+  for (int w = 0; w < warp; ++w) { hole0 += sh.scan[w][0]; late0 += sh.scan[w][1]; }
   for (int c = 0; c < n_ctas; ++c) {
     if (c < rank) { hole0 += sh.counts[c].x; late0 += sh.counts[c].y; }
     moves += sh.counts[c].x;                              // as many kept rows lie behind the budget
@@ -259,15 +294,14 @@ evict_kernel(const __grid_constant__ EvictBuffers b, const __grid_constant__ Pag
       int2* p = cluster.map_shared_rank(pairs, at / q) + at % q;
       (to ? p->y : p->x) = row_of(i);
     };
-    int h = hole0, l = late0;                             // numbers before the 16 words at hand
-    for (int w0 = 0; w0 < words; w0 += kWarps) {
-      const int nh = lane < kWarps ? __popc(holes_of(w0 + lane)) : 0, nl = lane < kWarps ? __popc(late_of(w0 + lane)) : 0;
-      const int h_before = __reduce_add_sync(0xffffffffu, lane < warp ? nh : 0), l_before = __reduce_add_sync(0xffffffffu, lane < warp ? nl : 0);
-      const unsigned hb = holes_of(w0 + warp), lb = late_of(w0 + warp);
-      if ((hb >> lane) & 1u) put(h + h_before + __popc(hb & low_bits(lane)), (w0 + warp) * 32 + lane, true);
-      if ((lb >> lane) & 1u) put(l + l_before + __popc(lb & low_bits(lane)), (w0 + warp) * 32 + lane, false);
-      h += __reduce_add_sync(0xffffffffu, nh);
-      l += __reduce_add_sync(0xffffffffu, nl);
+    int h = hole0, l = late0;
+#pragma unroll 4
+    for (int w = w_begin; w < w_end; ++w) {
+      const unsigned hb = holes_of(w), lb = late_of(w);
+      if ((hb >> lane) & 1u) put(h + __popc(hb & low_bits(lane)), w * 32 + lane, true);
+      if ((lb >> lane) & 1u) put(l + __popc(lb & low_bits(lane)), w * 32 + lane, false);
+      h += __popc(hb);
+      l += __popc(lb);
     }
     cluster.sync();
     const int mine = min(q, moves - first - rank * q), pieces = mine > 0 ? mine << b.shift : 0;
@@ -307,6 +341,38 @@ evict_kernel(const __grid_constant__ EvictBuffers b, const __grid_constant__ Pag
 
 using namespace tca;
 
+namespace tca {
+namespace {
+
+// 16 if the current device can run clusters of 16 of the kernel with `bytes` of shared memory, else 8.  Asked once per device.
+int evict_cluster(int bytes) {
+  static std::atomic<uint64_t> wide{0}, narrow{0};
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev >= 64) return 8;
+  const uint64_t bit = uint64_t(1) << dev;
+  if (wide.load(std::memory_order_relaxed) & bit) return 16;
+  if (narrow.load(std::memory_order_relaxed) & bit) return 8;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(16);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = size_t(bytes);
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 16;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  int n = 0;
+  const bool can = cudaFuncSetAttribute(evict_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
+                   cudaOccupancyMaxActiveClusters(&n, evict_kernel, &cfg) == cudaSuccess && n > 0;
+  cudaGetLastError();                    // a refusal is an answer here
+  (can ? wide : narrow).fetch_or(bit, std::memory_order_relaxed);
+  return can ? 16 : 8;
+}
+
+}  // namespace
+}  // namespace tca
+
 extern "C" int tca_paged_evict(const tca_params* prm, tca_paged_desc* c, int32_t n_sink, int32_t n_recent, const int32_t* budget,
                                void* stream) {
   const int st = check_paged(prm, c);
@@ -314,17 +380,22 @@ extern "C" int tca_paged_evict(const tca_params* prm, tca_paged_desc* c, int32_t
   TCA_CHECK_ARG(budget && aligned(budget, 4) && n_sink >= 0 && n_recent >= 0);
   const int64_t slots = int64_t(c->max_pages) * c->page_size;
   if (slots > kMostSlots) return TCA_ERR_UNSUPPORTED;
-  // CTAs per unit: as many as leave each a thousand slots, while the units do not fill the SMs twice over (and as many as
-  // the bits of very long units need)
+  // what the largest call can ask for: a bit for each of 512K slots beside the rest
+  constexpr int kMostBytes = kHeld * 8 + kPairs * 8 + kMostSlots / 8 / 8;
+  static_assert(kMostBytes + int(sizeof(EvictShared)) + 1024 <= 227 * 1024, "shared memory");
+  if (allow_smem<evict_kernel>(kMostBytes) != TCA_OK) return TCA_ERR_CUDA;
+  // CTAs per unit: as many as leave each two thousand slots, while the units do not fill the SMs with two each (and as many
+  // as the bits of very long units need)
+  const int most = slots > 2048 ? evict_cluster(kMostBytes) : 1;
   int n_ctas = 1;
-  while (n_ctas < kMaxCluster && slots > int64_t(n_ctas) * 1024 &&
-         (c->n_units * n_ctas <= sm_count() || slots > int64_t(n_ctas) * (kMostSlots / kMaxCluster)))
+  while (n_ctas < most && slots > int64_t(n_ctas) * 2048 &&
+         (c->n_units * n_ctas <= 2 * sm_count() || slots > int64_t(n_ctas) * (kMostSlots / 8)))
     n_ctas *= 2;
-  const int per = int((slots + n_ctas - 1) / n_ctas);
+  const int per = int(((slots + n_ctas - 1) / n_ctas + 63) & ~int64_t(63));
   EvictSizes sizes;
-  sizes.held_cap = ((per < kHeld ? per : kHeld) + 3) & ~3;
+  sizes.held_cap = per < kHeld ? per : kHeld;
   sizes.pair_cap = per / 2 + 1 < kPairs ? per / 2 + 1 : kPairs;
-  sizes.words = (per + 31) / 32;
+  sizes.words = per / 32;
   EvictBuffers b;
   b.K = static_cast<uint4*>(c->k);
   b.V = static_cast<uint4*>(c->v);
@@ -332,10 +403,6 @@ extern "C" int tca_paged_evict(const tca_params* prm, tca_paged_desc* c, int32_t
   b.mass = c->mass;
   b.shift = 0;
   while ((16 << b.shift) < int64_t(prm->head_dim) * int64_t(elt_size(prm->dtype))) ++b.shift;
-  // what the largest call can ask for: 12K slots held, 4K moves, a bit for each of 512K slots
-  constexpr int kMostBytes = kHeld * 8 + kPairs * 8 + kMostSlots / 8 / 8;
-  static_assert(kMostBytes + int(sizeof(EvictShared)) + 1024 <= 227 * 1024, "shared memory");
-  if (allow_smem<evict_kernel>(kMostBytes) != TCA_OK) return TCA_ERR_CUDA;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(unsigned(c->n_units * n_ctas));
   cfg.blockDim = dim3(kThreads);

@@ -20,7 +20,7 @@ template <int D, bool kShared>
 struct TreeTcSrc {
   using Item = TreeItem;
   static constexpr int kNoted = 2;
-  static constexpr bool kGap = false;
+  static constexpr bool kBits = false;
   const CUtensorMap *mq, *mk, *mv;
   const int64_t* state;
   int n_units;

@@ -43,7 +43,7 @@ def test_descriptors_are_refused(name):
     call = CALLS[name]
     assert call(prm(), None) == B.TCA_ERR_INVALID_ARG
     for kw in (dict(k=None), dict(v=None), dict(pos=None), dict(mass=None), dict(table=None), dict(state=None), dict(k=A + 8), dict(v=A + 2),
-               dict(state=A + 4), dict(table=A + 2), dict(pos=A + 1), dict(mass=A + 3), dict(n_units=7), dict(n_pages=0), dict(max_pages=0)):
+               dict(state=A + 4), dict(table=A + 2), dict(pos=A + 8), dict(mass=A + 4), dict(n_units=7), dict(n_pages=0), dict(max_pages=0)):
         assert call(prm(), desc(**kw)) == B.TCA_ERR_INVALID_ARG, kw
     for kw in (dict(page_size=8), dict(page_size=48), dict(page_size=512), dict(page_size=0), dict(n_pages=1 << 26), dict(max_pages=1 << 26)):
         assert call(prm(), desc(**kw)) == B.TCA_ERR_UNSUPPORTED, kw
