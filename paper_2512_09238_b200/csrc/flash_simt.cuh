@@ -54,6 +54,12 @@ struct SimtSmem {
 __device__ __forceinline__ void simt_group_sync(int group) {
   asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(kSimtGroup) : "memory");
 }
+__device__ __forceinline__ bool simt_group_any(int group, bool p) {
+  int any;
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbar.red.or.pred q, %2, %3, p;\n\tselp.b32 %0, 1, 0, q;\n\t}"
+               : "=r"(any) : "r"(int(p)), "r"(group + 1), "n"(kSimtGroup) : "memory");
+  return any != 0;
+}
 // 16 bytes to shared memory, or zeros.
 __device__ __forceinline__ void cp_async_16_or_zero(float* dst, const float* src, bool take) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
@@ -87,8 +93,9 @@ __device__ __forceinline__ void simt_load_rows(float* dst, int n, int tid, RowPt
 
 // Src: n_tiles(); n_rows(); q(r) -> const T*; keys(t) -> number of keys of tile t (1..kKeys); k(t), v(t)
 // -> const T*, its first row, k_stride(), v_stride() elements to the next; last(t, r) -> index in tile t of the last key row r sees (< 0: none, never >= keys(t));
-// masked(t): whether some row does not see all kKeys keys of the tile.  kGap: rows also do not see keys
-// [gap_begin(t), gap_end(t, r)) of the tile.
+// masked(t): whether some row does not see all kKeys keys of the tile.  kGap: a tile's keys need not lie together (k(t, r), v(t, r)
+// -> its row r); rows also do not see keys [gap_begin(t), gap_end(t, r)) of it, and all see those from sink_begin(t) on; a
+// masked tile whose values are all finite is accumulated without looking (a masked weight is an exact zero).
 // On return the threads of group 0 (threadIdx.x < 128; true is returned) hold the row maxima (in log2
 // units), sums and unnormalised outputs of rows RT ty .., columns 4 tx + 64 c; m = -inf, l = 0,
 // o = 0 for a row that saw nothing.
@@ -113,14 +120,22 @@ __device__ __forceinline__ bool simt_flash(const Src& src, float scale_log2e, fl
   }
   const int nt = src.n_tiles();
   auto load_k = [&](int t) {
-    const T* base = t < nt ? src.k(t) : nullptr;
-    if (t < nt) simt_load_rows<T, D, kKeys, kSimtGroup>(sK, src.keys(t), tid, [&](int r) { return base + r * src.k_stride(); });
-    else cp_async_commit();                // keeps the count of pending groups
+    if (t >= nt) { cp_async_commit(); return; }   // keeps the count of pending groups
+    if constexpr (Src::kGap) {
+      simt_load_rows<T, D, kKeys, kSimtGroup>(sK, src.keys(t), tid, [&](int r) { return src.k(t, r); });
+    } else {
+      const T* base = src.k(t);
+      simt_load_rows<T, D, kKeys, kSimtGroup>(sK, src.keys(t), tid, [&](int r) { return base + r * src.k_stride(); });
+    }
   };
   auto load_v = [&](int t) {
-    const T* base = t < nt ? src.v(t) : nullptr;
-    if (t < nt) simt_load_rows<T, D, kKeys, kSimtGroup>(sV, src.keys(t), tid, [&](int r) { return base + r * src.v_stride(); });
-    else cp_async_commit();
+    if (t >= nt) { cp_async_commit(); return; }
+    if constexpr (Src::kGap) {
+      simt_load_rows<T, D, kKeys, kSimtGroup>(sV, src.keys(t), tid, [&](int r) { return src.v(t, r); });
+    } else {
+      const T* base = src.v(t);
+      simt_load_rows<T, D, kKeys, kSimtGroup>(sV, src.keys(t), tid, [&](int r) { return base + r * src.v_stride(); });
+    }
   };
   __syncthreads();                         // the buffers may still be read by the item before
   simt_load_rows<T, D, kRows, kSimtThreads>(sQ, src.n_rows(), threadIdx.x, [&](int r) { return src.q(r); });
@@ -152,10 +167,10 @@ __device__ __forceinline__ bool simt_flash(const Src& src, float scale_log2e, fl
     simt_group_sync(group);                // K has been read
     load_k(t + 2);
     const bool masked = src.masked(t);
-    int last[RT], gap0 = 0, gap1[Src::kGap ? RT : 1] = {};
-    if constexpr (Src::kGap) gap0 = src.gap_begin(t);
+    int last[RT], gap0 = 0, sink0 = kKeys, n_keys = kKeys, gap1[Src::kGap ? RT : 1] = {};
+    if constexpr (Src::kGap) { gap0 = src.gap_begin(t); sink0 = src.sink_begin(t); n_keys = src.keys(t); }
     auto sees = [&](int key, int last_i, int gap1_i) {
-      if constexpr (Src::kGap) { if (key >= gap0 && key < gap1_i) return false; }
+      if constexpr (Src::kGap) return key >= sink0 ? key < n_keys : key <= last_i && !(key >= gap0 && key < gap1_i);
       return key <= last_i;
     };
 #pragma unroll
@@ -213,7 +228,18 @@ __device__ __forceinline__ bool simt_flash(const Src& src, float scale_log2e, fl
         }
       }
     };
-    if (masked) accumulate(std::true_type{}); else accumulate(std::false_type{});
+    bool guard = masked;
+    if constexpr (Src::kGap) {
+      if (masked) {
+        int top = 0;                       // of the tile's values, without their signs: from 0x7f800000 on not finite
+        for (int i = tid * 4; i < kKeys * D; i += kSimtGroup * 4) {
+          const int4 v = *reinterpret_cast<const int4*>(sV + i / D * ST + i % D);
+          top = max(max(top, v.x & 0x7fffffff), max(v.y & 0x7fffffff, max(v.z & 0x7fffffff, v.w & 0x7fffffff)));
+        }
+        guard = simt_group_any(group, top >= 0x7f800000);
+      }
+    }
+    if (guard) accumulate(std::true_type{}); else accumulate(std::false_type{});
     simt_group_sync(group);                // V has been read
     load_v(t + 2);
   }

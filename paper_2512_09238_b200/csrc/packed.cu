@@ -17,9 +17,9 @@ namespace {
 // Query rows of a CTA are (position, head of the group) pairs, head fastest: row r is position
 // p0 + r / G, head kvh * G + r % G, so a short sequence of a wide group still fills the tile.
 //
-// With a window, tiles that no row sees are left out, in pairs: the two groups of warps take alternate tiles, and a
-// row's keys have to meet the same group whichever rows share its CTA.  (A tile that a row does not see changes
-// nothing of its state.)
+// With a window the keys are those of the rows' windows, from the first one's first to the last row, and then the sinks in
+// front of them, 64 at a time wherever they lie.  What a row's tiles are depends on the rows that share its CTA, and
+// so do its last bits; so a window's calls all have the same shape, and a position the same neighbours in any batch.
 template <typename T, typename Shape, bool kWindow>
 struct PackedSrc {
   static constexpr int kRows = Shape::kRows, kKeys = Shape::kKeys;
@@ -28,36 +28,46 @@ struct PackedSrc {
   const PackedArgs* a;
   PackedWork w;
   int G;
-  int n0, skip;            // window: tiles t >= n0 lie `skip` tiles further on
+  int b0, n_band, sinks;   // window: first key of the band, its keys, sinks in front of it
   __device__ __forceinline__ void begin() {
-    n0 = skip = 0;
     if constexpr (kWindow) {
-      const int band = max(0, w.p0 - a->window + 1) / (2 * kKeys) * 2;
-      n0 = (min(a->n_sink, w.len) + 2 * kKeys - 1) / (2 * kKeys) * 2;
-      skip = max(0, band - n0);
+      const int lo = max(0, w.p0 - a->window + 1);
+      const bool apart = a->n_sink < lo;
+      b0 = apart ? lo : 0;
+      n_band = last_pos() + 1 - b0;
+      sinks = apart ? a->n_sink : 0;
     }
   }
-  __device__ __forceinline__ int tile(int t) const { return kWindow && t >= n0 ? t + skip : t; }
   __device__ __forceinline__ int n_rows() const { return min(kRows / G, w.len - w.p0) * G; }
   __device__ __forceinline__ int last_pos() const { return w.p0 + n_rows() / G - 1; }
-  __device__ __forceinline__ int n_tiles() const { return last_pos() / kKeys + 1 - (kWindow ? skip : 0); }
-  __device__ __forceinline__ int keys(int t) const { return min(kKeys, last_pos() + 1 - tile(t) * kKeys); }
+  __device__ __forceinline__ int n_keys() const { return kWindow ? n_band + sinks : last_pos() + 1; }
+  __device__ __forceinline__ int n_tiles() const { return (n_keys() - 1) / kKeys + 1; }
+  __device__ __forceinline__ int keys(int t) const { return min(kKeys, n_keys() - t * kKeys); }
   __device__ __forceinline__ const T* q(int r) const {
     return Q + (w.kvh * G + r % G) * a->q.head + (w.row0 + w.p0 + r / G) * a->q.row;
   }
-  __device__ __forceinline__ const T* k(int t) const { return K + w.kvh * a->k.head + (w.row0 + tile(t) * kKeys) * a->k.row; }
-  __device__ __forceinline__ const T* v(int t) const { return V + w.kvh * a->v.head + (w.row0 + tile(t) * kKeys) * a->v.row; }
+  __device__ __forceinline__ const T* k(int t) const { return K + w.kvh * a->k.head + (w.row0 + t * kKeys) * a->k.row; }
+  __device__ __forceinline__ const T* v(int t) const { return V + w.kvh * a->v.head + (w.row0 + t * kKeys) * a->v.row; }
+  __device__ __forceinline__ int key(int t, int r) const {       // row r of tile t
+    const int i = t * kKeys + r;
+    return i < n_band ? b0 + i : i - n_band;
+  }
+  __device__ __forceinline__ const T* k(int t, int r) const { return K + w.kvh * a->k.head + (w.row0 + key(t, r)) * a->k.row; }
+  __device__ __forceinline__ const T* v(int t, int r) const { return V + w.kvh * a->v.head + (w.row0 + key(t, r)) * a->v.row; }
   __device__ __forceinline__ int64_t k_stride() const { return a->k.row; }
   __device__ __forceinline__ int64_t v_stride() const { return a->v.row; }
   __device__ __forceinline__ int pos(int r) const { return min(w.p0 + r / G, last_pos()); }
   __device__ __forceinline__ bool masked(int t) const {
-    const int k0 = tile(t) * kKeys;
-    if (kWindow && k0 + kKeys > a->n_sink && k0 <= last_pos() - a->window) return true;
-    return k0 + kKeys - 1 > w.p0;
+    if constexpr (kWindow) {
+      const int k0 = b0 + t * kKeys, k1 = b0 + min((t + 1) * kKeys, n_band) - 1;      // the tile's keys of the band
+      return keys(t) < kKeys || k1 > w.p0 || (k1 >= a->n_sink && k0 <= last_pos() - a->window);
+    }
+    return (t + 1) * kKeys - 1 > w.p0;
   }
-  __device__ __forceinline__ int last(int t, int r) const { return pos(r) - tile(t) * kKeys; }
-  __device__ __forceinline__ int gap_begin(int t) const { return a->n_sink - tile(t) * kKeys; }
-  __device__ __forceinline__ int gap_end(int t, int r) const { return pos(r) - a->window + 1 - tile(t) * kKeys; }
+  __device__ __forceinline__ int last(int t, int r) const { return kWindow ? pos(r) - b0 - t * kKeys : pos(r) - t * kKeys; }
+  __device__ __forceinline__ int gap_begin(int t) const { return a->n_sink - b0 - t * kKeys; }
+  __device__ __forceinline__ int gap_end(int t, int r) const { return pos(r) - a->window + 1 - b0 - t * kKeys; }
+  __device__ __forceinline__ int sink_begin(int t) const { return n_band - t * kKeys; }
 };
 
 template <typename T, int D, typename Shape, bool kWindow>
@@ -118,15 +128,16 @@ int launch_packed_shape(const tca_params* prm, const void* Q, const void* K, con
 }
 
 // The large tiles where they give every SM more than one CTA and are not mostly padding: prompts that
-// average four of them.
+// average four of them, and wherever there is a window.
 template <typename T, int D, bool kWindow>
 int launch_packed_simt(const tca_params* prm, const void* Q, const void* K, const void* V, const PackedArgs& a, void* O,
                        cudaStream_t s) {
   using Large = SimtLarge;
   const int64_t tiles = a.rows * a.n_q_heads / Large::kRows;
-  if (tiles >= sm_count() && a.rows * (a.n_q_heads / a.n_kv_heads) >= int64_t(4) * Large::kRows * a.n_seq)
+  if (kWindow || (tiles >= sm_count() && a.rows * (a.n_q_heads / a.n_kv_heads) >= int64_t(4) * Large::kRows * a.n_seq))
     return launch_packed_shape<T, D, Large, kWindow>(prm, Q, K, V, a, O, s);
-  return launch_packed_shape<T, D, SimtSmall, kWindow>(prm, Q, K, V, a, O, s);
+  if constexpr (!kWindow) return launch_packed_shape<T, D, SimtSmall, kWindow>(prm, Q, K, V, a, O, s);
+  return TCA_ERR_UNSUPPORTED;
 }
 
 // A buffer's strides: multiples of 16 bytes (vector loads, tensor maps), and room for a row.
