@@ -87,9 +87,25 @@ append_rows_kernel(const __grid_constant__ AppendBuffers b, const __grid_constan
     if (seqs.first_cta[mid] <= cta) lo = mid; else hi = mid;
   }
   const int n_new = seqs.len[lo], u = seqs.slot[lo] * b.n_kv + h;
+  const int r0 = (cta - seqs.first_cta[lo]) * kRowsPerCta, n = min(kRowsPerCta, n_new - r0);
+  const int64_t row = int64_t(seqs.row0[lo]) + r0;
+  const uint4* ks = b.K + h * b.kview.head + row * b.kview.row;
+  const uint4* vs = b.V + h * b.vview.head + row * b.vview.row;
+  uint4 kv[4], vv[4];
+  auto fetch = [&](int p0) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int p = p0 + i * kThreads;
+      if (p < (n << b.shift)) {
+        const int r = p >> b.shift, c = p & ((1 << b.shift) - 1);
+        kv[i] = __ldcs(ks + r * b.kview.row + c);
+        vv[i] = __ldcs(vs + r * b.vview.row + c);
+      }
+    }
+  };
+  fetch(tid);                             // on its way while the length and the pages are looked up
   int4* st = args.state + u;
   const int len = st->x, next = st->y;
-  const int r0 = (cta - seqs.first_cta[lo]) * kRowsPerCta, n = min(kRowsPerCta, n_new - r0);
   if (len < 0 || int64_t(len) + n_new > int64_t(args.max_pages) << args.page_shift) {   // the same for all of the unit's CTAs
     if (r0 == 0 && tid == 0) report_paged(st, kPagedNoRoom);
     return;
@@ -116,20 +132,8 @@ append_rows_kernel(const __grid_constant__ AppendBuffers b, const __grid_constan
       *count = 0;
     }
   }
-  const int64_t row = int64_t(seqs.row0[lo]) + r0;
-  const uint4* ks = b.K + h * b.kview.head + row * b.kview.row;
-  const uint4* vs = b.V + h * b.vview.head + row * b.vview.row;
   for (int p0 = tid; p0 < (n << b.shift); p0 += 4 * kThreads) {
-    uint4 kv[4], vv[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int p = p0 + i * kThreads;
-      if (p < (n << b.shift)) {
-        const int r = p >> b.shift, c = p & ((1 << b.shift) - 1);
-        kv[i] = __ldcs(ks + r * b.kview.row + c);
-        vv[i] = __ldcs(vs + r * b.vview.row + c);
-      }
-    }
+    if (p0 != tid) fetch(p0);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int p = p0 + i * kThreads;
