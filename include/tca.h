@@ -483,8 +483,9 @@ int tca_attn_window(const tca_params* prm, const void* Q, const void* K, const v
  *   All buffers but the table are aligned to 16 bytes.
  *   state   [n_units][TCA_PG_STATE_WORDS] int32, zeroed once: rows in use, position of the next token, first failed check
  *           (tca_paged_status), a word of the library's
- *   table   entries of slots that are not in use are not read.  Pages may be shared by units while they are only read;
+ *   table   entries of slots that are not in use, or that a window hides, are not read.  Pages may be shared by units while they are only read;
  *           a call that writes to a page (append, evict, attention that accumulates) needs it to be one unit's alone.
+ * A call that changes a cache must not overlap with another one on it.
  * Supported: page_size 16, 32, 64, 128 or 256; n_pages * page_size and max_pages * page_size below 2^31; up to 65535
  * units (else TCA_ERR_UNSUPPORTED).
  */
@@ -529,7 +530,8 @@ int tca_paged_append(const tca_params* prm, const void* K, const void* V, int64_
  *   ws   DEVICE workspace of tca_attn_paged_workspace_bytes(prm, cache, accumulate) bytes, zeroed once after
  *        allocating; word 0 is the sticky status word.  Calls that share one must not overlap.
  * Slots that are not visible have no influence whatever they hold.  A visible slot whose page lies outside the pool
- * counts as not visible and sets the status word to TCA_ERR_BOUNDS.  n_sink >= 0 (TCA_ERR_INVALID_ARG), prm->window >= 1
+ * counts as not visible and sets the status word to TCA_ERR_BOUNDS (a unit that has no other gives NaN); later calls go on.
+ * While a wait that gave up is in the status word, O and the masses stay as they were.  O must not overlap q.  n_sink >= 0 (TCA_ERR_INVALID_ARG), prm->window >= 1
  * (TCA_ERR_UNSUPPORTED).  prm->block, alpha and flags are not used.
  */
 int tca_attn_paged(const tca_params* prm, const void* q, const tca_paged_desc* cache, int32_t n_sink, int32_t accumulate,

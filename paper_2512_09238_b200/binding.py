@@ -661,9 +661,7 @@ class PagedCache:
 
     def reserve(self, rows: Sequence[int]) -> None:
         """Every unit u gets the pages that rows[u] rows need, where it has fewer."""
-        want = -(-np.asarray(rows, dtype=np.int64) // self.page_size)
-        if want.shape != self.n_held.shape:
-            raise ValueError("rows must have one entry per (sequence, KV head)")
+        want = self._pages(rows)
         more = np.maximum(0, want - self.n_held)
         if want.max(initial=0) > self.max_pages or more.sum() > len(self.free):
             raise TcaError(TCA_ERR_CAPACITY, "PagedCache.reserve")
@@ -678,15 +676,19 @@ class PagedCache:
     def release(self, rows: Sequence[int]) -> None:
         """Every unit u gives back the pages that rows[u] rows do not need (after an eviction to a budget, or with 0
         rows when its sequence ends; its state is the caller's to clear then)."""
-        want = -(-np.asarray(rows, dtype=np.int64) // self.page_size)
-        if want.shape != self.n_held.shape:
-            raise ValueError("rows must have one entry per (sequence, KV head)")
+        want = self._pages(rows)
         changed = np.nonzero(want < self.n_held)[0]
         for u in changed:
             self.free.extend(self.table_host[u, want[u]:self.n_held[u]][::-1].tolist())
             self.table_host[u, want[u]:] = -1
             self.n_held[u] = want[u]
         self._upload(changed)
+
+    def _pages(self, rows) -> np.ndarray:
+        rows = np.asarray(rows, dtype=np.int64)
+        if rows.shape != self.n_held.shape or rows.min(initial=0) < 0:
+            raise ValueError("rows must have one entry, not negative, per (sequence, KV head)")
+        return -(-rows // self.page_size)
 
     def _upload(self, units) -> None:
         if len(units):

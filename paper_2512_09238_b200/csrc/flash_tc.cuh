@@ -549,6 +549,12 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
       int it = 0;
 #pragma unroll 1
       for (; it < whole; ++it) {
+        uint32_t bits[Source::kBits ? kTcKeys / 32 : 1];
+        const bool masked = Source::kBits && it >= src.whole_tiles();
+        if constexpr (Source::kBits) {           // worked out while the scores are
+#pragma unroll
+          for (int c = 0; c < kTcKeys / 32; ++c) bits[c] = masked ? src.seen_bits(row_key, it, c) : 0xffffffffu;
+        }
         ok = warp_wait(bar_s + h, tile_count++ & 1u);
         if (!ok) break;
         ptx::tc_fence_after();
@@ -558,14 +564,12 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
           ptx::tmem_ld32(s_addr + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&v[c * 32]));
         ptx::tc_wait_ld();
         if constexpr (Source::kBits) {
-          if (it >= src.whole_tiles()) {
+          if (masked) {
 #pragma unroll
-            for (int c = 0; c < kTcKeys / 32; ++c) {
-              const uint32_t bits = src.seen_bits(row_key, it, c);
+            for (int c = 0; c < kTcKeys / 32; ++c)
 #pragma unroll
               for (int k = 0; k < 32; ++k)       // a key the row does not see has weight 0, whatever its score
-                if (!((bits >> k) & 1u)) v[c * 32 + k] = 0xff800000u;
-            }
+                if (!((bits[c] >> k) & 1u)) v[c * 32 + k] = 0xff800000u;
           }
         }
         float mx;

@@ -16,8 +16,6 @@
 //
 // Weights need the row sums of the whole unit, so the scores are left in the workspace (4 G bytes a row beside 4 d or 8 d)
 // and the second kernel turns them into weights.
-#include <vector>
-
 #include "bulk_ring.cuh"
 #include "paged_common.cuh"
 #include "rowslice.cuh"
@@ -796,15 +794,19 @@ extern "C" int tca_attn_paged(const tca_params* prm, const void* q, const tca_pa
 }
 
 extern "C" int tca_paged_status(const tca_paged_desc* c, void* stream, int64_t* detail) {
-  TCA_CHECK_ARG(c && c->state && c->n_units >= 1 && c->n_units < (int64_t(1) << 31));
-  std::vector<int32_t> st(size_t(c->n_units) * TCA_PG_STATE_WORDS);
+  TCA_CHECK_ARG(c && c->state && c->n_units >= 1 && c->n_units <= 65535);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  TCA_CHECK_CUDA(cudaMemcpyAsync(st.data(), c->state, st.size() * sizeof(int32_t), cudaMemcpyDeviceToHost, s));
-  TCA_CHECK_CUDA(cudaStreamSynchronize(s));
-  for (int64_t u = 0; u < c->n_units; ++u) {
-    const int32_t which = st[size_t(u) * TCA_PG_STATE_WORDS + TCA_PG_CHECK];
-    if (which != 0) {
-      if (detail) { detail[0] = u; detail[1] = which; }
+  constexpr int kUnits = 1024;             // a part of the state at a time: no allocation
+  int32_t st[kUnits * TCA_PG_STATE_WORDS];
+  for (int64_t u0 = 0; u0 < c->n_units; u0 += kUnits) {
+    const int64_t n = c->n_units - u0 < kUnits ? c->n_units - u0 : kUnits;
+    TCA_CHECK_CUDA(cudaMemcpyAsync(st, c->state + u0 * TCA_PG_STATE_WORDS, size_t(n) * TCA_PG_STATE_WORDS * sizeof(int32_t),
+                                   cudaMemcpyDeviceToHost, s));
+    TCA_CHECK_CUDA(cudaStreamSynchronize(s));
+    for (int64_t u = 0; u < n; ++u) {
+      const int32_t which = st[u * TCA_PG_STATE_WORDS + TCA_PG_CHECK];
+      if (which == 0) continue;
+      if (detail) { detail[0] = u0 + u; detail[1] = which; }
       return TCA_ERR_BOUNDS;
     }
   }

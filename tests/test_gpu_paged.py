@@ -163,6 +163,39 @@ def test_shared_pages(dtype):
     Q.check(prm, q, c, Q.attend(prm, q, c), 0, dtype)
 
 
+def test_a_status_word_that_stops_the_call_leaves_results_alone():
+    prm = Q.params(2, 8, 2, 128, "bf16")
+    c = Q.make(prm, [900, 20, 0, 4000], 64, "bf16", 21)
+    ws, q = B.alloc_paged_workspace(prm, c, True), query(prm, 11, "bf16")
+    good, before = Q.attend(prm, q, c, ws=ws), Q.snapshot(c)
+    ws[0] = 1
+    o = torch.full_like(q, 7.0)
+    B.tca_attn_paged(prm, q, c, 0, True, o, ws)
+    assert B.tca_ws_status(ws) == B.TCA_ERR_TIMEOUT and (o == 7).all()
+    Q.same(before, Q.snapshot(c))
+    ws.zero_()
+    assert torch.equal(good, Q.attend(prm, q, c, ws=ws))
+
+
+def test_calls_on_several_streams_at_once():
+    """Caches, workspaces and tensors of their own."""
+    work = []
+    for i in range(4):
+        prm = Q.params(2, 8, 2, 128, "bf16")
+        c = Q.make(prm, [700 + 300 * i, 20, 5000, 64], 32, "bf16", 80 + i)
+        q = query(prm, 90 + i, "bf16")
+        work.append((prm, c, q, torch.full_like(q, float("nan")), B.alloc_paged_workspace(prm, c), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for prm, c, q, o, ws, stream in work:
+            with torch.cuda.stream(stream):
+                B.tca_attn_paged(prm, q, c, 0, False, o, ws)
+    torch.cuda.synchronize()
+    for prm, c, q, o, ws, _ in work:
+        assert B.tca_ws_status(ws) == B.TCA_OK
+        Q.check(prm, q, c, o, 0, "bf16")
+
+
 def test_one_workspace_for_calls_of_both_kinds_and_another_stream():
     prm = Q.params(3, 8, 2, 128, "bf16")
     c = Q.make(prm, [900, 20, 0, 400, 3000, 77], 64, "bf16", 18)

@@ -136,8 +136,11 @@ def test_pages_are_dealt_and_given_back():
     c.release([0, 16, 16, 0, 0, 0, 0, 33])
     assert c.n_held.tolist() == [0, 1, 1, 0, 0, 0, 0, 3] and len(c.free) == 15 and (c.table.numpy() == c.table_host).all()
     assert (c.table_host[0] == -1).all() and sorted(c.free + c.table_host[c.table_host >= 0].tolist()) == list(range(20))
-    with pytest.raises(ValueError):
-        c.reserve([1, 2])
+    for rows in ([1, 2], [-1] + [0] * 7):
+        with pytest.raises(ValueError):
+            c.reserve(rows)
+        with pytest.raises(ValueError):
+            c.release(rows)
     with pytest.raises(ValueError):
         B.PagedCache(p, 0, 16, 4, device="cpu")
 
