@@ -73,12 +73,15 @@ evict_kernel(const __grid_constant__ EvictBuffers b, const __grid_constant__ Pag
   const int rank = int(cluster.block_rank()), n_ctas = int(cluster.num_blocks());
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int u = int(blockIdx.x) / n_ctas;
+  auto sync_all = [&] {                                   // a unit that is one CTA's needs no more than that CTA's barrier
+    if (n_ctas > 1) cluster.sync(); else __syncthreads();
+  };
   pdl_wait();
   pdl_launch_dependents();
   int4* st = args.state + u;
   const int len = paged_len(args, st->x), budget = budgets[u];
   if (len <= budget) return;                              // the whole cluster alike, before any barrier
-  cluster.barrier_arrive();
+  if (n_ctas > 1) cluster.barrier_arrive();
   const int per = ((len + n_ctas - 1) / n_ctas + 63) & ~63;   // a multiple of four slots, and of a word of bits
   const int s0 = min(len, rank * per), n = min(len, s0 + per) - s0, held = min((n + 3) & ~3, sizes.held_cap);
 
@@ -107,7 +110,7 @@ evict_kernel(const __grid_constant__ EvictBuffers b, const __grid_constant__ Pag
   sh.sum[tid >> 8][tid & 255] = 0;
   if (tid < 256) sh.hist[tid] = 0;
   __syncthreads();
-  cluster.barrier_wait();                                 // every CTA of the cluster runs: its memory can be written
+  if (n_ctas > 1) cluster.barrier_wait();                 // every CTA of the cluster runs: its memory can be written
   if (tid < n_ctas) {
     int t = INT_MIN, any = 0;
     for (int w = 0; w < kWarps; ++w) { t = max(t, sh.scan[w][0]); any |= sh.scan[w][1]; }
@@ -115,7 +118,7 @@ evict_kernel(const __grid_constant__ EvictBuffers b, const __grid_constant__ Pag
     to->max_pos[rank] = t;
     to->bad[rank] = any;
   }
-  cluster.sync();
+  sync_all();
   int newest = INT_MIN, any_bad = 0;
   for (int c = 0; c < n_ctas; ++c) { newest = max(newest, sh.max_pos[c]); any_bad |= sh.bad[c]; }
   if (any_bad) {                                          // the whole cluster alike
@@ -168,16 +171,19 @@ evict_kernel(const __grid_constant__ EvictBuffers b, const __grid_constant__ Pag
       }
     }
     __syncthreads();
-    if (tid < 256) {
-      // every CTA adds its counts to everybody's (read from the others after the barrier they took 1.2 us more a digit)
-      const unsigned v = sh.hist[tid];
-      if (v)
-        for (int c = 0; c < n_ctas; ++c) atomicAdd(&cluster.map_shared_rank(&sh, c)->sum[digit & 1][tid], v);
-      if (digit < 3) sh.hist[tid] = 0;
-    } else {
-      sh.sum[(digit + 1) & 1][tid - 256] = 0;     // read before the last barrier, added to after the next
+    const unsigned* counts = sh.hist;
+    if (n_ctas > 1) {
+      counts = sh.sum[digit & 1];
+      if (tid < 256) {
+        // every CTA adds its counts to everybody's (read from the others after the barrier they took 1.2 us more a digit)
+        const unsigned v = sh.hist[tid];
+        if (v)
+          for (int c = 0; c < n_ctas; ++c) atomicAdd(&cluster.map_shared_rank(&sh, c)->sum[digit & 1][tid], v);
+      } else {
+        sh.sum[(digit + 1) & 1][tid - 256] = 0;     // read before the last barrier, added to after the next
+      }
+      cluster.sync();
     }
-    cluster.sync();
     if (digit == 0) {
       need = budget;
       for (int c = 0; c < n_ctas; ++c) need -= sh.safe[c];
@@ -190,7 +196,7 @@ evict_kernel(const __grid_constant__ EvictBuffers b, const __grid_constant__ Pag
     // which nothing is kept
     unsigned total = 0, count = 0;
     if (tid < 256) {
-      count = total = sh.sum[digit & 1][255 - tid];
+      count = total = counts[255 - tid];
 #pragma unroll
       for (int off = 1; off < 32; off <<= 1) {
         const unsigned t = __shfl_up_sync(0xffffffffu, count, off);
@@ -207,6 +213,7 @@ evict_kernel(const __grid_constant__ EvictBuffers b, const __grid_constant__ Pag
         sh.need = need - above;
         sh.equals = int(total);
       }
+      if (digit < 3) sh.hist[255 - tid] = 0;
     }
     __syncthreads();
     prefix = (prefix << 8) | sh.picked;
@@ -219,7 +226,7 @@ evict_kernel(const __grid_constant__ EvictBuffers b, const __grid_constant__ Pag
   int equals = 0;                                         // of the slots before: keys equal to the threshold
   if (tie && need > 0) {
     if (tid < n_ctas) cluster.map_shared_rank(&sh, tid)->equal[rank] = int(sh.hist[sh.picked]);
-    cluster.sync();
+    sync_all();
     for (int c = 0; c < rank; ++c) equals += sh.equal[c];
   }
   for (int i0 = 0; i0 < n; i0 += kThreads * 4) {
@@ -278,7 +285,7 @@ evict_kernel(const __grid_constant__ EvictBuffers b, const __grid_constant__ Pag
     for (int w = 0; w < kWarps; ++w) { t.x += sh.scan[w][0]; t.y += sh.scan[w][1]; }
     cluster.map_shared_rank(&sh, tid)->counts[rank] = t;
   }
-  cluster.sync();
+  sync_all();
   int hole0 = 0, late0 = 0, moves = 0;                    // numbers before this warp's words
   for (int w = 0; w < warp; ++w) { hole0 += sh.scan[w][0]; late0 += sh.scan[w][1]; }
   for (int c = 0; c < n_ctas; ++c) {
@@ -303,7 +310,7 @@ evict_kernel(const __grid_constant__ EvictBuffers b, const __grid_constant__ Pag
       h += __popc(hb);
       l += __popc(lb);
     }
-    cluster.sync();
+    sync_all();
     const int mine = min(q, moves - first - rank * q), pieces = mine > 0 ? mine << b.shift : 0;
     for (int p0 = tid; p0 < pieces; p0 += 4 * kThreads) {
       uint4 kv[4], vv[4];
@@ -331,7 +338,7 @@ evict_kernel(const __grid_constant__ EvictBuffers b, const __grid_constant__ Pag
       b.pos[m.y] = b.pos[m.x];
       b.mass[m.y] = b.mass[m.x];
     }
-    cluster.sync();
+    sync_all();
   }
   if (rank == 0 && tid == 0) st->x = budget;
 }
