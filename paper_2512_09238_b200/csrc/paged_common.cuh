@@ -128,7 +128,7 @@ struct PagedDeal {
     return a.n_units <= kHeld ? held[u] : paged_len(a, __ldcg(&a.state[u].x));
   }
   // Pieces of ranks [from, from + kList) go to the list; from < 0: all, and the ranks of the first and last are noted (if
-  // there are more than kList, round() fills the list again) and the records written, by all CTAs together.
+  // there are more than kList, round() fills the list again) and the records written.
   __device__ __forceinline__ void fill(const PagedArgs& a, int window, int n_sink, const Mine& my, const PagedCut& cut, int share, int from,
                                        PagedRecord* records) {
     const int begin = cut.begin(share), end = cut.begin(share + 1);
@@ -137,9 +137,12 @@ struct PagedDeal {
     for (int u = my.u_begin; u < my.u_end; ++u) {
       const int len = rows_of(a, u), m = PagedSpan(len, window, n_sink).n;
       const int at = off + kPagedLead, lo = max(at, begin), hi = min(at + m, end);
-      const bool record = records && u % int(gridDim.x) == int(blockIdx.x);
+      // the record is written by the share in which the unit's width begins (the last one's end belongs to it as well)
+      const bool record = records && off >= begin && (off < end || share == cut.n - 1);
       if (hi > lo || record) {
-        const int f = m > 0 ? cut.share_of(at) : 0, l = m > 0 ? cut.share_of(at + m - 1) : 0;
+        // (divisions only for a unit that crosses the share's borders)
+        const int f = at < begin ? cut.share_of(at) : at < end ? share : share + 1;
+        const int l = at + m - 1 < end && at + m - 1 >= begin ? share : m > 0 ? cut.share_of(at + m - 1) : f;
         const int parts = f == l ? 0 : l - f + 1, step = off - kPagedLead * r;
         if (hi > lo) {
           if (from < 0) {
