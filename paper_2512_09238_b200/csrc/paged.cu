@@ -10,12 +10,13 @@
 //                   mma.sync, the G <= 8 heads are the columns of the products (tcgen05 needs 64 rows of queries).
 //                   fp32: FP32 pipes, a row of K per lane, then D / 32 columns of V per lane.
 // At the end of a unit's piece the four states are merged; a piece that is the whole unit gives the result, others
-// partial results that a second kernel merges in order.  Statistics and accumulators are fp32; bf16 weights are rounded
+// partial results, which whoever brings the unit's last one merges in order.  Statistics and accumulators are fp32; bf16 weights are rounded
 // to bf16 before they meet the values (half a step, 2^-8 of a weight), the row sum adds the unrounded ones.
 // A slot nobody sees has no influence whatever it holds: its score is replaced, its value row is not read from the ring.
 //
 // Weights need the row sums of the whole unit, so the scores are left in the workspace (4 G bytes a row beside 4 d or 8 d)
-// and the second kernel turns them into weights.
+// and a second kernel turns them into weights; it merges the partial results as well, which costs nothing there (in the
+// first kernel, 2.5 us).
 #include "bulk_ring.cuh"
 #include "paged_common.cuh"
 #include "rowslice.cuh"
@@ -44,7 +45,7 @@ constexpr int kConsumers = 128, kWarps = kConsumers / 32;   // of a team
 constexpr int kWarpRows = kPagedStep / kWarps;      // of a step
 static_assert(kWarpRows == 32, "two groups of 16 rows, one lane per row");
 constexpr int kList = 64;            // pieces of a round
-constexpr int kPageBatches = 7;      // batches of page numbers on their way
+constexpr int kPageBatches = 3;      // batches of page numbers on their way
 constexpr int kGroups = kPagedStep / 16;            // groups of 16 rows of a step: none is on two pages
 __host__ __device__ constexpr int state_row(int d) { return d + 4; }   // floats per head of a warp's state in shared memory
 constexpr float kLog2e = 1.4426950408889634f;
@@ -58,6 +59,8 @@ PagedWs paged_ws_layout(const tca_params* prm, const tca_paged_desc* c, bool wei
   w.status = reinterpret_cast<int*>(base);
   w.records = reinterpret_cast<PagedRecord*>(base + at);
   at += align_up((U + 1) * sizeof(PagedRecord), 256);
+  w.tickets = reinterpret_cast<int*>(base + at);
+  at += align_up(U * sizeof(int), 256);
   w.ml = reinterpret_cast<float2*>(base + at);
   at += align_up(n * sizeof(float2), 256);
   w.acc = reinterpret_cast<float*>(base + at);
@@ -370,6 +373,58 @@ struct WarpRows<float, D, GT> {
   }
 };
 
+constexpr int kJoinAhead = 8;        // partial results whose outputs are on their way together
+
+// One warp merges the partial results of a unit's head in order: `parts` of them from `slot` on (none: zeros).
+template <typename T, int D>
+__device__ __forceinline__ void merge_head(const PagedWs& ws, int slot, int parts, int G, int g, T* out) {
+  constexpr int E = D / 32;
+  const int lane = threadIdx.x & 31;
+  float o[E], m = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) o[e] = 0.f;
+#pragma unroll 1
+  for (int c0 = 0; c0 < parts; c0 += kJoinAhead) {
+    const int cn = min(kJoinAhead, parts - c0);
+    const float2 ml = lane < cn ? __ldcg(ws.ml + size_t(slot + c0 + lane) * G + g) : make_float2(-INFINITY, 0.f);
+    float v[kJoinAhead][E];
+#pragma unroll
+    for (int c = 0; c < kJoinAhead; ++c) {
+      const float* a = ws.acc + (size_t(slot + c0 + min(c, cn - 1)) * G + g) * D + lane * E;
+      if constexpr (E == 4) { const float4 t = __ldcg(reinterpret_cast<const float4*>(a)); v[c][0] = t.x; v[c][1] = t.y; v[c][2] = t.z; v[c][3] = t.w; }
+      else { const float2 t = __ldcg(reinterpret_cast<const float2*>(a)); v[c][0] = t.x; v[c][1] = t.y; }
+    }
+    float mn = ml.x;
+#pragma unroll
+    for (int off = kJoinAhead / 2; off > 0; off >>= 1) mn = fmaxf(mn, __shfl_xor_sync(0xffffffffu, mn, off));
+    mn = fmaxf(m, __shfl_sync(0xffffffffu, mn, 0));
+    const float from = mn == -INFINITY ? 0.f : mn, keep = exp2f(m - from), w = exp2f(ml.x - from);
+    const float wl = w * ml.y;
+    l *= keep;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] *= keep;
+#pragma unroll
+    for (int c = 0; c < kJoinAhead; ++c) {
+      const float wc = __shfl_sync(0xffffffffu, w, c);
+      l += __shfl_sync(0xffffffffu, wl, c);
+      if (c < cn) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] = fmaf(wc, v[c][e], o[e]);
+      }
+    }
+    m = mn;
+  }
+  if (parts > 0)
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] /= l;
+  T* to = out + lane * E;
+#pragma unroll
+  for (int e = 0; e < E; e += 2) {
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<float2*>(to + e) = make_float2(o[e], o[e + 1]);
+    else *reinterpret_cast<uint32_t*>(to + e) = ptx::pack_bf16x2(o[e], o[e + 1]);
+  }
+}
+
 template <typename T, int D, int GT>
 __global__ void __launch_bounds__(PagedRing<T, D, GT>::kThreads, 1)
 paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const T* __restrict__ q,
@@ -382,7 +437,7 @@ paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
   uint8_t* query_buf = states + kTeams * Ring::kState;
   __shared__ BulkRing<kStages> ring;
   __shared__ PagedDeal<kTeams * kConsumers, kList> deal;
-  __shared__ int abort_word;
+  __shared__ int abort_word, merge_here[kTeams];
   __shared__ __align__(16) uint32_t zeros[4];
   __shared__ uint64_t query_full[Ring::kQueries];
   __shared__ int page_buf[kPageBatches + 1][32];
@@ -428,7 +483,7 @@ paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
     cp_async_group();
   };
   typename PagedDeal<kTeams * kConsumers, kList>::Mine my;
-  const PagedCut cut = deal.start(args, window, n_sink, share, my, ws.records);
+  const PagedCut cut = deal.start(args, window, n_sink, share, my, ws.steps ? ws.records : nullptr);   // (records are for the second kernel)
   const int n_pieces = deal.n_pieces();
   int n = 0;                                                       // stages handed over so far
   bool ok = true;
@@ -578,10 +633,30 @@ paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
             }
             if (d == 0) ws.ml[at + g] = make_float2(M, l);
           }
+          if (piece.parts > 0 && !ws.steps) {
+            // whoever brings the unit's last partial result merges them
+            team_sync(team);
+            if (tid % kConsumers == 0) {
+              __threadfence();
+              const bool all = atomicAdd(ws.tickets + piece.u, 1) == piece.parts - 1;
+              if (all) ws.tickets[piece.u] = 0;             // for the next call
+              __threadfence();
+              merge_here[team] = all;
+            }
+            team_sync(team);
+            if (merge_here[team])
+              for (int g = tw; g < G; g += kWarps) merge_head<T, D>(ws, piece.slot, piece.parts, G, g, O + (size_t(piece.u) * G + g) * D);
+          }
         }
         team_sync(team);                        // the states are written over by the next piece
       }
     }
+  }
+  if (warp < kTeams * kWarps && !ws.steps && !stops_call(found_status)) {
+    // nobody's pieces: units without a visible slot give zeros
+    for (int u = share * kTeams * kConsumers + tid; u < args.n_units; u += int(gridDim.x) * kTeams * kConsumers)
+      if (PagedSpan(deal.rows_of(args, u), window, n_sink).n == 0)
+        for (int j = 0; j < G * D; j += 16 / int(sizeof(T))) *reinterpret_cast<uint4*>(O + size_t(u) * G * D + j) = make_uint4(0, 0, 0, 0);
   }
   __syncthreads();
   if (*abort_flag) {
@@ -590,12 +665,11 @@ paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
   }
 }
 
-// ------------------------------------------------------------------ merge of the partial results; weights
+// ------------------------------------------------------------------ weights, and the merge of the partial results beside them
 constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32;
 constexpr int kWeightBlocks = 4;     // per SM
-constexpr int kJoinAhead = 8;        // partial results whose outputs are on their way together
 
-// The first weight_blocks blocks (none if weights are not accumulated): a warp per step of 128 slots turns its scores into
+// For calls that accumulate weights.  The first weight_blocks blocks: a warp per step of 128 slots turns its scores into
 // weights.  The others: one warp per (unit, head) merges the unit's partial results in order.  All loads that do not depend on
 // one another are issued together: the kernel is a chain of trips to memory.  (Held to 64 registers a block fits beside a
 // CTA of the first kernel, and the call takes 42.6 us instead of 41.2: 64 conversations with weights.)
@@ -604,7 +678,6 @@ __global__ void __launch_bounds__(kJoinThreads, 3)
 paged_join_kernel(const __grid_constant__ PagedArgs args, int G, int window, int n_sink, int weight_blocks, PagedWs ws,
                   float* __restrict__ mass, T* __restrict__ O) {
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  constexpr int E = D / 32;
   pdl_wait();
   pdl_launch_dependents();
   const int found_status = __ldcg(ws.status);
@@ -613,50 +686,8 @@ paged_join_kernel(const __grid_constant__ PagedArgs args, int G, int window, int
     if (u >= args.n_units) return;
     const int4 rec = __ldcg(reinterpret_cast<const int4*>(ws.records) + u);
     if (stops_call(found_status)) return;
-    const int n = PagedSpan(rec.z, window, n_sink).n > 0 ? rec.y : -1;   // partial results; -1: nothing is visible
-    if (n == 0) return;                         // its only share wrote the result
-    float o[E], m = -INFINITY, l = 0.f;
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = 0.f;
-    for (int c0 = 0; c0 < n; c0 += kJoinAhead) {
-      const int cn = min(kJoinAhead, n - c0);
-      const float2 ml = lane < cn ? __ldcg(ws.ml + size_t(rec.x + c0 + lane) * G + g) : make_float2(-INFINITY, 0.f);
-      float v[kJoinAhead][E];
-#pragma unroll
-      for (int c = 0; c < kJoinAhead; ++c) {
-        const float* a = ws.acc + (size_t(rec.x + c0 + min(c, cn - 1)) * G + g) * D + lane * E;
-        if constexpr (E == 4) { const float4 t = __ldcg(reinterpret_cast<const float4*>(a)); v[c][0] = t.x; v[c][1] = t.y; v[c][2] = t.z; v[c][3] = t.w; }
-        else { const float2 t = __ldcg(reinterpret_cast<const float2*>(a)); v[c][0] = t.x; v[c][1] = t.y; }
-      }
-      float mn = ml.x;
-#pragma unroll
-      for (int off = kJoinAhead / 2; off > 0; off >>= 1) mn = fmaxf(mn, __shfl_xor_sync(0xffffffffu, mn, off));
-      mn = fmaxf(m, __shfl_sync(0xffffffffu, mn, 0));
-      const float from = mn == -INFINITY ? 0.f : mn, keep = exp2f(m - from), w = exp2f(ml.x - from);
-      const float wl = w * ml.y;
-      l *= keep;
-#pragma unroll
-      for (int e = 0; e < E; ++e) o[e] *= keep;
-#pragma unroll
-      for (int c = 0; c < kJoinAhead; ++c) {
-        const float wc = __shfl_sync(0xffffffffu, w, c);
-        l += __shfl_sync(0xffffffffu, wl, c);
-        if (c < cn) {
-#pragma unroll
-          for (int e = 0; e < E; ++e) o[e] = fmaf(wc, v[c][e], o[e]);
-        }
-      }
-      m = mn;
-    }
-    if (n > 0)
-#pragma unroll
-      for (int e = 0; e < E; ++e) o[e] /= l;
-    T* out = O + (size_t(u) * G + g) * D + lane * E;
-#pragma unroll
-    for (int e = 0; e < E; e += 2) {
-      if constexpr (sizeof(T) == 4) *reinterpret_cast<float2*>(out + e) = make_float2(o[e], o[e + 1]);
-      else *reinterpret_cast<uint32_t*>(out + e) = ptx::pack_bf16x2(o[e], o[e + 1]);
-    }
+    const int parts = PagedSpan(rec.z, window, n_sink).n > 0 ? rec.y : -1;   // -1: nothing is visible
+    if (parts != 0) merge_head<T, D>(ws, rec.x, parts, G, g, O + (size_t(u) * G + g) * D);   // (0: its only share wrote the result)
     return;
   }
   // ---- weights
@@ -747,9 +778,9 @@ int launch_paged(const tca_params* prm, const void* q, const tca_paged_desc* c, 
   const int st = launch_pdl(kern, dim3(unsigned(sm_count())), dim3(Ring::kThreads), size_t(Ring::kSmemBytes), s, mk, mv, static_cast<const T*>(q),
                             args, G, prm->window, n_sink, prm->sm_scale * kLog2e, int64_t(64 * kL2Share * double(l2_bytes()) / (2 * Ring::kStageBytes)), ws,
                             static_cast<T*>(O));
-  if (st != TCA_OK) return st;
+  if (st != TCA_OK || !weights) return st;
   const int merge_blocks = int((c->n_units * G + kJoinWarps - 1) / kJoinWarps);
-  const int weight_blocks = weights ? kWeightBlocks * sm_count() : 0;
+  const int weight_blocks = kWeightBlocks * sm_count();
   return launch_pdl(paged_join_kernel<T, D, (GT > 4 ? 8 : 4)>, dim3(unsigned(merge_blocks + weight_blocks)), dim3(kJoinThreads),
                     size_t(0), s, args, G, prm->window, n_sink, weight_blocks, ws, c->mass, static_cast<T*>(O));
 }

@@ -214,13 +214,15 @@ struct PagedDeal {
 };
 #endif
 
-// Workspace: 256-byte header (word 0: sticky status), a record of each unit and one behind them (steps in all), row
+// Workspace: 256-byte header (word 0: sticky status), a record of each unit and one behind them (steps in all), number of
+// each unit's partial results that are there (zero between calls), row
 // statistics (maximum in log2 units, sum) and unnormalised outputs of every (slot, head of the group); where weights are accumulated, the scores of every pool row in groups of 16 rows:
 // [pool row / 16][head of the group][16], in log2 units.
 constexpr size_t kPagedHeaderBytes = 256;
 struct PagedWs {
   int* status;
   PagedRecord* records;
+  int* tickets;
   PagedStepRecord* steps;
   float2* ml;
   float* acc;
