@@ -9,22 +9,22 @@
  *     allocator.  What it keeps between calls is limited to: the built-in scratch array of
  *     tca_attn_decode_static (and its per-device address), a small cache of encoded TMA
  *     tensor maps keyed by buffer address and shape, per-device constants (SM count, L2 cache
- *     size), and which kernels have been granted their shared memory on which device.  The bf16 decode kernel asks the L2 to keep part of the cache it reads
- *     (eviction-priority hints on its loads; nothing is set on the device or the context).
+ *     size, whether clusters of 16 run), and which kernels have been granted their shared memory on which device.  The bf16 decode kernel and tca_attn_paged ask the L2 to keep part of the
+ *     cache they read (eviction-priority hints on their loads; nothing is set on the device or the context).
  *   - Tensors are row-major with the head dimension contiguous:
  *       Q [batch, n_q_heads, L, head_dim]      K, V [batch, n_kv_heads, L, head_dim]
  *     A "unit" is one (sequence, KV head) pair, u = seq * n_kv_heads + kv_head; the G =
  *     n_q_heads / n_kv_heads query heads kv_head*G .. kv_head*G+G-1 share it.
  *   - Device work is enqueued on `stream` (a cudaStream_t passed as void*); no call
- *     synchronises the host except the three that read a status back (tca_ws_status,
- *     tca_cache_status, tca_decode_static_status).  Outputs are valid once the stream has
+ *     synchronises the host except the four that read a status back (tca_ws_status,
+ *     tca_cache_status, tca_decode_static_status, tca_paged_status).  Outputs are valid once the stream has
  *     been synchronised.
- *   - Status words.  Word 0 of the prefill, packed, decode, tree, select and calibration
+ *   - Status words.  Word 0 of the prefill, packed, window, decode, paged, tree, select and calibration
  *     workspaces is a STICKY status word: zero it once after allocating (a zero-filled workspace is fine;
  *     tca_attn_packed needs its whole workspace zeroed, see there); a kernel sets it when one of its bounded device-side waits gives up (or, in the
  *     range-checked build, when an index is out of range) and nothing in the library clears
  *     it.  While it is set, the tensor-core kernels return at once without computing (of
- *     tca_attn_tree a wait that gave up stops the next calls; a failed range check is only
+ *     tca_attn_tree and tca_attn_paged a wait that gave up stops the next calls; a failed range check is only
  *     reported).  After a non-zero status, zero the whole workspace before using it again.
  *   - Return value: TCA_OK or a negative error.  Argument errors are detected on the
  *     host before anything is launched and leave every output untouched.  Unsupported
