@@ -37,6 +37,8 @@
 #pragma once
 #include <cuda.h>
 
+#include <type_traits>
+
 #include "common.cuh"
 #include "ptx_sm100.cuh"
 #include "tensor_map.cuh"
@@ -545,32 +547,31 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(bar_p + 2 * h + part);
       };
-      const int whole = Source::kBits ? mine : kShared ? min(src.whole_tiles(), mine) : (src.whole_tiles() - h + 1) / 2;   // they come first
+      const int whole = kShared ? min(src.whole_tiles(), mine) : (src.whole_tiles() - h + 1) / 2;   // they come first
       int it = 0;
-#pragma unroll 1
-      for (; it < whole; ++it) {
-        uint32_t bits[Source::kBits ? kTcKeys / 32 : 1];
-        const bool masked = Source::kBits && it >= src.whole_tiles();
-        if constexpr (Source::kBits) {           // worked out while the scores are
+      // One tile at full width; masked: with a bit per key, worked out while the scores are.  Two bodies: the test of
+      // a flag in one took 1 to 2 % of a long window.
+      auto full_tile = [&](auto masked, auto& from) {
+        constexpr bool kMasked = decltype(masked)::value;
+        uint32_t bits[kMasked ? kTcKeys / 32 : 1];
+        if constexpr (kMasked) {
 #pragma unroll
-          for (int c = 0; c < kTcKeys / 32; ++c) bits[c] = masked ? src.seen_bits(row_key, it, c) : 0xffffffffu;
+          for (int c = 0; c < kTcKeys / 32; ++c) bits[c] = from.seen_bits(row_key, it, c);
         }
         ok = warp_wait(bar_s + h, tile_count++ & 1u);
-        if (!ok) break;
+        if (!ok) return;
         ptx::tc_fence_after();
         uint32_t v[kTcKeys];
 #pragma unroll
         for (int c = 0; c < kTcKeys / 32; ++c)
           ptx::tmem_ld32(s_addr + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&v[c * 32]));
         ptx::tc_wait_ld();
-        if constexpr (Source::kBits) {
-          if (masked) {
+        if constexpr (kMasked) {
 #pragma unroll
-            for (int c = 0; c < kTcKeys / 32; ++c)
+          for (int c = 0; c < kTcKeys / 32; ++c)
 #pragma unroll
-              for (int k = 0; k < 32; ++k)       // a key the row does not see has weight 0, whatever its score
-                if (!((bits[c] >> k) & 1u)) v[c * 32 + k] = 0xff800000u;
-          }
+            for (int k = 0; k < 32; ++k)         // a key the row does not see has weight 0, whatever its score
+              if (!((bits[c] >> k) & 1u)) v[c * 32 + k] = 0xff800000u;
         }
         float mx;
         {
@@ -612,8 +613,13 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
         ptx::unpack2(sum2[0], s0, s1);
         ptx::unpack2(sum2[1], s2, s3);
         l += (s0 + s1) + (s2 + s3);
-      }
-      if constexpr (!Source::kBits)
+      };
+#pragma unroll 1
+      for (; it < whole && ok; ++it) full_tile(std::false_type{}, src);
+      if constexpr (Source::kBits) {
+#pragma unroll 1
+        for (; it < mine && ok; ++it) full_tile(std::true_type{}, src);
+      } else
 #pragma unroll 1
       for (; it < mine && ok; ++it) {
         const int t = kShared ? it : 2 * it + h;
