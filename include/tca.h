@@ -528,7 +528,8 @@ int tca_paged_append(const tca_params* prm, const void* K, const void* V, int64_
  *   q    DEVICE [batch, n_q_heads, head_dim]     O  DEVICE out, same shape
  *   accumulate  not 0: the mass of every visible row grows by the mean over the unit's query heads of its softmax weight
  *   ws   DEVICE workspace of tca_attn_paged_workspace_bytes(prm, cache, accumulate) bytes, zeroed once after
- *        allocating; word 0 is the sticky status word.  Calls that share one must not overlap.
+ *        allocating; word 0 is the sticky status word.  Calls that share one must not overlap; they may be over
+ *        different caches.
  * Slots that are not visible have no influence whatever they hold.  A visible slot whose page lies outside the pool
  * counts as not visible and sets the status word to TCA_ERR_BOUNDS (a unit that has no other gives NaN); later calls go on.
  * While a wait that gave up is in the status word, O and the masses stay as they were.  O must not overlap q.  n_sink >= 0 (TCA_ERR_INVALID_ARG), prm->window >= 1

@@ -537,7 +537,8 @@ def tca_attn_paged_workspace_bytes(prm, cache: "PagedCache", accumulate) -> int:
 
 
 def alloc_paged_workspace(prm: tca_params, cache: "PagedCache", accumulate: bool = False) -> torch.Tensor:
-    """A zero-filled workspace for tca_attn_paged calls over this cache (with accumulate, for calls of both kinds)."""
+    """A zero-filled workspace for tca_attn_paged calls over this cache (with accumulate, for calls of both kinds), or
+    over any that need no more."""
     n = tca_attn_paged_workspace_bytes(prm, cache, accumulate)
     if n == 0:
         raise TcaError(TCA_ERR_INVALID_ARG, "tca_attn_paged_workspace_bytes")

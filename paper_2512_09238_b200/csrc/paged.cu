@@ -57,10 +57,10 @@ PagedWs paged_ws_layout(const tca_params* prm, const tca_paged_desc* c, bool wei
   char* base = static_cast<char*>(ws);
   size_t at = kPagedHeaderBytes;
   w.status = reinterpret_cast<int*>(base);
+  w.tickets = reinterpret_cast<int*>(base + at);
+  at += align_up(size_t(sm_count()) * sizeof(int), 256);
   w.records = reinterpret_cast<PagedRecord*>(base + at);
   at += align_up((U + 1) * sizeof(PagedRecord), 256);
-  w.tickets = reinterpret_cast<int*>(base + at);
-  at += align_up(U * sizeof(int), 256);
   w.ml = reinterpret_cast<float2*>(base + at);
   at += align_up(n * sizeof(float2), 256);
   w.acc = reinterpret_cast<float*>(base + at);
@@ -638,8 +638,9 @@ paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
             team_sync(team);
             if (tid % kConsumers == 0) {
               __threadfence();
-              const bool all = atomicAdd(ws.tickets + piece.u, 1) == piece.parts - 1;
-              if (all) ws.tickets[piece.u] = 0;             // for the next call
+              int* ticket = ws.tickets + (piece.slot - piece.u);
+              const bool all = atomicAdd(ticket, 1) == piece.parts - 1;
+              if (all) *ticket = 0;                         // for the next call
               __threadfence();
               merge_here[team] = all;
             }

@@ -214,15 +214,16 @@ struct PagedDeal {
 };
 #endif
 
-// Workspace: 256-byte header (word 0: sticky status), a record of each unit and one behind them (steps in all), number of
-// each unit's partial results that are there (zero between calls), row
-// statistics (maximum in log2 units, sum) and unnormalised outputs of every (slot, head of the group); where weights are accumulated, the scores of every pool row in groups of 16 rows:
-// [pool row / 16][head of the group][16], in log2 units.
+// Workspace: 256-byte header (word 0: sticky status); per share, how many partial results are there of the unit that
+// runs from it into the next (zero between calls, and where they are whatever the cache, so that caches of any sizes can use
+// one workspace in turn); a record of each unit and one behind them (steps in all); row statistics (maximum in log2
+// units, sum) and unnormalised outputs of every (slot, head of the group); where weights are accumulated, the scores of every
+// pool row in groups of 16 rows: [pool row / 16][head of the group][16], in log2 units.
 constexpr size_t kPagedHeaderBytes = 256;
 struct PagedWs {
   int* status;
-  PagedRecord* records;
   int* tickets;
+  PagedRecord* records;
   PagedStepRecord* steps;
   float2* ml;
   float* acc;

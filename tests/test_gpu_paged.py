@@ -209,6 +209,22 @@ def test_one_workspace_for_calls_of_both_kinds_and_another_stream():
     assert torch.equal(first, second) and torch.equal(first, Q.attend(prm, q, c, ws=ws))
 
 
+def test_one_workspace_for_caches_of_different_sizes():
+    """Many units beside few, so that whatever the layout depends on lies elsewhere."""
+    calls = []
+    for i, (batch, hq, hkv, d, dtype, lens) in enumerate([(3, 8, 2, 128, "bf16", [9000, 20, 0, 400, 3000, 77]),
+                                                          (150, 16, 4, 128, "bf16", [1 + 13 * u % 900 for u in range(600)]),
+                                                          (2, 2, 2, 64, "f32", [2000, 5, 130, 700])]):
+        prm = Q.params(batch, hq, hkv, d, dtype)
+        calls.append((prm, Q.make(prm, lens, 32, dtype, 100 + i), query(prm, 110 + i, dtype), dtype))
+    n = max(B.tca_attn_paged_workspace_bytes(prm, c, True) for prm, c, _, _ in calls)
+    ws = torch.zeros(n, dtype=torch.uint8, device="cuda")
+    for accumulate in (False, True, False):
+        for prm, c, q, dtype in calls + calls[::-1]:
+            before = Q.snapshot(c)
+            Q.check(prm, q, c, Q.attend(prm, q, c, accumulate=accumulate, ws=ws), 0, dtype, before if accumulate else None)
+
+
 # ------------------------------------------------------------------ append
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("layout", ["heads", "tokens", "fused", "odd"])
