@@ -25,7 +25,7 @@ constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kMaxCluster = 16;          // more than 8 is not portable: evict_cluster() asks the device
 constexpr int kMostSlots = 1 << 22;      // slots of a unit: one bit each has to fit a cluster's shared memory
 constexpr int kHeld = 16 * 1024;         // slots of a CTA whose key and position are held; the others' are read again
-constexpr int kPairs = 3 * 1024;         // moves of a CTA at a time
+constexpr int kPairs = 2 * 1024;         // moves of a CTA at a time
 constexpr uint32_t kSafe = 0xFFFFFFFFu;  // key of a sink or recent row; a NaN has the one below
 
 struct EvictBuffers {
