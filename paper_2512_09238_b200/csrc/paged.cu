@@ -60,7 +60,7 @@ PagedWs paged_ws_layout(const tca_params* prm, const tca_paged_desc* c, bool wei
   w.tickets = reinterpret_cast<int*>(base + at);
   at += align_up(size_t(sm_count()) * sizeof(int), 256);
   w.records = reinterpret_cast<PagedRecord*>(base + at);
-  at += align_up((U + 1) * sizeof(PagedRecord), 256);
+  at += align_up(size_t(sm_count()) * sizeof(PagedRecord), 256);
   w.ml = reinterpret_cast<float2*>(base + at);
   at += align_up(n * sizeof(float2), 256);
   w.acc = reinterpret_cast<float*>(base + at);
@@ -375,7 +375,7 @@ struct WarpRows<float, D, GT> {
 
 constexpr int kJoinAhead = 8;        // partial results whose outputs are on their way together
 
-// One warp merges the partial results of a unit's head in order: `parts` of them from `slot` on (none: zeros).
+// One warp merges the partial results of a unit's head in order: `parts` of them from `slot` on.
 template <typename T, int D>
 __device__ __forceinline__ void merge_head(const PagedWs& ws, int slot, int parts, int G, int g, T* out) {
   constexpr int E = D / 32;
@@ -414,9 +414,8 @@ __device__ __forceinline__ void merge_head(const PagedWs& ws, int slot, int part
     }
     m = mn;
   }
-  if (parts > 0)
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[e] /= l;
+  for (int e = 0; e < E; ++e) o[e] /= l;
   T* to = out + lane * E;
 #pragma unroll
   for (int e = 0; e < E; e += 2) {
@@ -483,8 +482,9 @@ paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
     cp_async_group();
   };
   typename PagedDeal<kTeams * kConsumers, kList>::Mine my;
-  const PagedCut cut = deal.start(args, window, n_sink, share, my, ws.steps ? ws.records : nullptr);   // (records are for the second kernel)
+  const PagedCut cut = deal.start(args, window, n_sink, share, my);
   const int n_pieces = deal.n_pieces();
+  if (ws.steps && tid == 0) ws.records[share] = deal.record;       // for the second kernel
   int n = 0;                                                       // stages handed over so far
   bool ok = true;
   for (int rank0 = 0; rank0 < n_pieces; rank0 += kList) {
@@ -653,7 +653,7 @@ paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       }
     }
   }
-  if (warp < kTeams * kWarps && !ws.steps && !stops_call(found_status)) {
+  if (warp < kTeams * kWarps && !stops_call(found_status)) {
     // nobody's pieces: units without a visible slot give zeros
     for (int u = share * kTeams * kConsumers + tid; u < args.n_units; u += int(gridDim.x) * kTeams * kConsumers)
       if (PagedSpan(deal.rows_of(args, u), window, n_sink).n == 0)
@@ -668,43 +668,46 @@ paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
 
 // ------------------------------------------------------------------ weights, and the merge of the partial results beside them
 constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32;
-constexpr int kWeightBlocks = 4;     // per SM
+constexpr int kWeightBlocks = 3;     // per SM
 
 // For calls that accumulate weights.  The first weight_blocks blocks: a warp per step of 128 slots turns its scores into
-// weights.  The others: one warp per (unit, head) merges the unit's partial results in order.  All loads that do not depend on
-// one another are issued together: the kernel is a chain of trips to memory.  (Held to 64 registers a block fits beside a
-// CTA of the first kernel, and the call takes 42.6 us instead of 41.2: 64 conversations with weights.)
+// weights.  The others: one warp per (share, head) merges the partial results of the unit that begins there and runs on.  All
+// loads that do not depend on one another are issued together: the kernel is a chain of trips to memory.
 template <typename T, int D, int GT>
-__global__ void __launch_bounds__(kJoinThreads, 3)
-paged_join_kernel(const __grid_constant__ PagedArgs args, int G, int window, int n_sink, int weight_blocks, PagedWs ws,
-                  float* __restrict__ mass, T* __restrict__ O) {
+__global__ void __launch_bounds__(kJoinThreads, kWeightBlocks)
+paged_join_kernel(int G, int n_shares, int weight_blocks, PagedWs ws, float* __restrict__ mass, T* __restrict__ O) {
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   pdl_wait();
   pdl_launch_dependents();
   const int found_status = __ldcg(ws.status);
   if (int(blockIdx.x) >= weight_blocks) {
-    const int at = (int(blockIdx.x) - weight_blocks) * kJoinWarps + warp, u = at / G, g = at - u * G;
-    if (u >= args.n_units) return;
-    const int4 rec = __ldcg(reinterpret_cast<const int4*>(ws.records) + u);
+    const int at = (int(blockIdx.x) - weight_blocks) * kJoinWarps + warp, share = at / G, g = at - share * G;
+    if (share >= n_shares) return;
+    const int4 rec = __ldcg(reinterpret_cast<const int4*>(ws.records) + share);
     if (stops_call(found_status)) return;
-    const int parts = PagedSpan(rec.z, window, n_sink).n > 0 ? rec.y : -1;   // -1: nothing is visible
-    if (parts != 0) merge_head<T, D>(ws, rec.x, parts, G, g, O + (size_t(u) * G + g) * D);   // (0: its only share wrote the result)
+    if (rec.z > 0) merge_head<T, D>(ws, rec.y, rec.z, G, g, O + (size_t(rec.x) * G + g) * D);
     return;
   }
   // ---- weights
   const int warps = weight_blocks * kJoinWarps;
-  const int total = __ldcg(&ws.records[args.n_units].step);
+  const int total = __ldcg(&ws.records[0].steps);
   if (stops_call(found_status)) return;
   const float inv_g = 1.f / float(G);
-  for (int step = int(blockIdx.x) * kJoinWarps + warp; step < total; step += warps) {
+  int2 where, next_where, group[4];
+  auto fetch = [&](int step) {               // the record of the step after this one is on its way during this one
     const PagedStepRecord* rec = ws.steps + step;
-    const int2 where = __ldcg(reinterpret_cast<const int2*>(&rec->slot));
+    next_where = __ldcg(reinterpret_cast<const int2*>(&rec->slot));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) group[i] = __ldcg(&rec->group[i * 2 + (lane >> 4)]);
+  };
+  int step = int(blockIdx.x) * kJoinWarps + warp;
+  if (step < total) fetch(step);
+  for (; step < total; step += warps) {
+    where = next_where;
     int row[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int2 group = __ldcg(&rec->group[i * 2 + (lane >> 4)]);
-      row[i] = group.x >= 0 && ((group.y >> (lane & 15)) & 1) ? group.x * 16 + (lane & 15) : -1;
-    }
+    for (int i = 0; i < 4; ++i) row[i] = group[i].x >= 0 && ((group[i].y >> (lane & 15)) & 1) ? group[i].x * 16 + (lane & 15) : -1;
+    if (step + warps < total) fetch(step + warps);
     // the row sums: log2 of the sum over the unit's partial results, head by head
     float lse[GT];
     const int parts = max(1, where.y);
@@ -780,10 +783,10 @@ int launch_paged(const tca_params* prm, const void* q, const tca_paged_desc* c, 
                             args, G, prm->window, n_sink, prm->sm_scale * kLog2e, int64_t(64 * kL2Share * double(l2_bytes()) / (2 * Ring::kStageBytes)), ws,
                             static_cast<T*>(O));
   if (st != TCA_OK || !weights) return st;
-  const int merge_blocks = int((c->n_units * G + kJoinWarps - 1) / kJoinWarps);
+  const int merge_blocks = (sm_count() * G + kJoinWarps - 1) / kJoinWarps;
   const int weight_blocks = kWeightBlocks * sm_count();
   return launch_pdl(paged_join_kernel<T, D, (GT > 4 ? 8 : 4)>, dim3(unsigned(merge_blocks + weight_blocks)), dim3(kJoinThreads),
-                    size_t(0), s, args, G, prm->window, n_sink, weight_blocks, ws, c->mass, static_cast<T*>(O));
+                    size_t(0), s, G, sm_count(), weight_blocks, ws, c->mass, static_cast<T*>(O));
 }
 
 template <int D>

@@ -98,9 +98,10 @@ struct PagedPiece {
   int step;                // steps of the units before it
   int slot, parts;         // the unit's partial results: first slot, number (0: this piece is all it has)
 };
-// What the second kernel needs of a unit (len, partial results as above), and of a step.
+// What the second kernel needs of a share, and of a step.
 struct __align__(16) PagedRecord {
-  int slot, parts, len, step;            // step: steps of the units before it
+  int u, slot, parts;      // the unit that runs from the share into the next, its partial results; parts 0: there is none
+  int steps;               // of all units
 };
 struct __align__(16) PagedStepRecord {
   int2 group[8];           // of every 16 slots: pool row / 16 (-1: not a page of the pool), visible slots as bits
@@ -118,6 +119,7 @@ struct PagedDeal {
   static constexpr int kHeld = 512;
   int warp_sum[kDealers / 32][2];
   int first, last;         // ranks, among the units that have steps, of those in the share
+  PagedRecord record;
   int held[kHeld];
   PagedPiece list[kList];
 
@@ -127,42 +129,37 @@ struct PagedDeal {
   __device__ __forceinline__ int rows_of(const PagedArgs& a, int u) const {
     return a.n_units <= kHeld ? held[u] : paged_len(a, __ldcg(&a.state[u].x));
   }
-  // Pieces of ranks [from, from + kList) go to the list; from < 0: all, and the ranks of the first and last are noted (if
-  // there are more than kList, round() fills the list again) and the records written.
-  __device__ __forceinline__ void fill(const PagedArgs& a, int window, int n_sink, const Mine& my, const PagedCut& cut, int share, int from,
-                                       PagedRecord* records) {
+  // Pieces of ranks [from, from + kList) go to the list; from < 0: all, and the ranks of the first and last and the record
+  // are noted (if there are more than kList, round() fills the list again).
+  __device__ __forceinline__ void fill(const PagedArgs& a, int window, int n_sink, const Mine& my, const PagedCut& cut, int share, int from) {
     const int begin = cut.begin(share), end = cut.begin(share + 1);
     int r = my.rank, off = my.at;
 #pragma unroll 1
     for (int u = my.u_begin; u < my.u_end; ++u) {
       const int len = rows_of(a, u), m = PagedSpan(len, window, n_sink).n;
       const int at = off + kPagedLead, lo = max(at, begin), hi = min(at + m, end);
-      // the record is written by the share in which the unit's width begins (the last one's end belongs to it as well)
-      const bool record = records && off >= begin && (off < end || share == cut.n - 1);
-      if (hi > lo || record) {
+      if (hi > lo) {
         // (divisions only for a unit that crosses the share's borders)
-        const int f = at < begin ? cut.share_of(at) : at < end ? share : share + 1;
-        const int l = at + m - 1 < end && at + m - 1 >= begin ? share : m > 0 ? cut.share_of(at + m - 1) : f;
+        const int f = at < begin ? cut.share_of(at) : share;
+        const int l = at + m <= end ? share : cut.share_of(at + m - 1);
         const int parts = f == l ? 0 : l - f + 1, step = off - kPagedLead * r;
-        if (hi > lo) {
-          if (from < 0) {
-            if (off <= begin) first = r;       // a unit before it would reach past `begin`
-            atomicMax(&last, r);
-          }
-          if (from < 0 || (r >= from && r < from + kList)) list[r & (kList - 1)] = PagedPiece{u, lo - at, hi - lo, len, step, f + u, parts};
+        if (from < 0) {
+          if (off <= begin) first = r;         // a unit before it would reach past `begin`
+          atomicMax(&last, r);
+          if (parts > 0 && f == share) { record.u = u; record.slot = f + u; record.parts = parts; }
         }
-        if (record) records[u] = PagedRecord{f + u, parts, len, step};
+        if (from < 0 || (r >= from && r < from + kList)) list[r & (kList - 1)] = PagedPiece{u, lo - at, hi - lo, len, step, f + u, parts};
       }
       off += m > 0 ? m + kPagedLead : 0;
       r += m > 0;
     }
   }
-  __device__ __forceinline__ PagedCut start(const PagedArgs& a, int window, int n_sink, int share, Mine& my, PagedRecord* records) {
+  __device__ __forceinline__ PagedCut start(const PagedArgs& a, int window, int n_sink, int share, Mine& my) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     if (tid < kDealers && a.n_units <= kHeld)
 #pragma unroll 4
       for (int u = tid; u < a.n_units; u += kDealers) held[u] = paged_len(a, __ldcg(&a.state[u].x));
-    if (tid == 0) { first = 0; last = -1; }
+    if (tid == 0) { first = 0; last = -1; record.parts = 0; }
     __syncthreads();
     my = Mine{};
     if (tid < kDealers) {
@@ -197,8 +194,8 @@ struct PagedDeal {
       units += y;
     }
     const PagedCut cut(total, int(gridDim.x));
-    if (tid < kDealers) fill(a, window, n_sink, my, cut, share, -1, records);
-    if (tid == 0 && blockIdx.x == 0 && records) records[a.n_units] = PagedRecord{0, 0, 0, total - kPagedLead * units};
+    if (tid == 0) record.steps = total - kPagedLead * units;
+    if (tid < kDealers) fill(a, window, n_sink, my, cut, share, -1);
     __syncthreads();
     return cut;
   }
@@ -207,7 +204,7 @@ struct PagedDeal {
   __device__ __forceinline__ void round(const PagedArgs& a, int window, int n_sink, const Mine& my, const PagedCut& cut, int share, int rank0) {
     if (n_pieces() <= kList) return;
     __syncthreads();
-    if (threadIdx.x < kDealers) fill(a, window, n_sink, my, cut, share, first + rank0, nullptr);
+    if (threadIdx.x < kDealers) fill(a, window, n_sink, my, cut, share, first + rank0);
     __syncthreads();
   }
   __device__ __forceinline__ const PagedPiece& at(int rank0, int i) const { return list[(first + rank0 + i) & (kList - 1)]; }
@@ -216,9 +213,9 @@ struct PagedDeal {
 
 // Workspace: 256-byte header (word 0: sticky status); per share, how many partial results are there of the unit that
 // runs from it into the next (zero between calls, and where they are whatever the cache, so that caches of any sizes can use
-// one workspace in turn); a record of each unit and one behind them (steps in all); row statistics (maximum in log2
-// units, sum) and unnormalised outputs of every (slot, head of the group); where weights are accumulated, the scores of every
-// pool row in groups of 16 rows: [pool row / 16][head of the group][16], in log2 units.
+// one workspace in turn) and its record; row statistics (maximum in log2 units, sum) and unnormalised outputs of every
+// (slot, head of the group); where weights are accumulated, the scores of every pool row in groups of 16 rows: [pool row / 16]
+// [head of the group][16], in log2 units, and the records of the steps.
 constexpr size_t kPagedHeaderBytes = 256;
 struct PagedWs {
   int* status;
