@@ -44,7 +44,7 @@ namespace {
 constexpr int kConsumers = 128, kWarps = kConsumers / 32;   // of a team
 constexpr int kWarpRows = kPagedStep / kWarps;      // of a step
 static_assert(kWarpRows == 32, "two groups of 16 rows, one lane per row");
-constexpr int kList = 64;            // pieces of a round
+constexpr int kList = 128;           // pieces of a round
 constexpr int kPageBatches = 3;      // batches of page numbers on their way
 constexpr int kGroups = kPagedStep / 16;            // groups of 16 rows of a step: none is on two pages
 __host__ __device__ constexpr int state_row(int d) { return d + 4; }   // floats per head of a warp's state in shared memory
@@ -481,8 +481,12 @@ paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
     else *to = -1;
     cp_async_group();
   };
+  // The rows of all units are held in memory that has another use later: of 512 units the teams' states, of more the ring, which
+  // takes a fence (0.3 us of a short call).
+  static_assert(kTeams * Ring::kState >= (512 + 512 / 32) * 4, "rows of 512 units");
+  const bool few = args.n_units <= 512, hold = args.n_units + (args.n_units >> 5) <= kStages * Ring::kStageBytes / 4;
   typename PagedDeal<kTeams * kConsumers, kList>::Mine my;
-  const PagedCut cut = deal.start(args, window, n_sink, share, my);
+  const PagedCut cut = deal.start(args, window, n_sink, share, my, hold ? reinterpret_cast<int*>(few ? states : ring_buf) : nullptr, hold && !few);
   const int n_pieces = deal.n_pieces();
   if (ws.steps && tid == 0) ws.records[share] = deal.record;       // for the second kernel
   int n = 0;                                                       // stages handed over so far
@@ -655,8 +659,9 @@ paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
   }
   if (warp < kTeams * kWarps && !stops_call(found_status)) {
     // nobody's pieces: units without a visible slot give zeros
-    for (int u = share * kTeams * kConsumers + tid; u < args.n_units; u += int(gridDim.x) * kTeams * kConsumers)
-      if (PagedSpan(deal.rows_of(args, u), window, n_sink).n == 0)
+    constexpr int kDealers = kTeams * kConsumers;
+    for (int u = share * kDealers + tid; u < args.n_units; u += int(gridDim.x) * kDealers)
+      if (PagedSpan(u == share * kDealers + tid ? my.tail : deal.rows_of(args, nullptr, u), window, n_sink).n == 0)
         for (int j = 0; j < G * D; j += 16 / int(sizeof(T))) *reinterpret_cast<uint4*>(O + size_t(u) * G * D + j) = make_uint4(0, 0, 0, 0);
   }
   __syncthreads();

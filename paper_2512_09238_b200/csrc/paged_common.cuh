@@ -2,6 +2,7 @@
 // the partial results of tca_attn_paged.
 #pragma once
 #include "common.cuh"
+#include "ptx_sm100.cuh"
 
 namespace tca {
 
@@ -109,34 +110,35 @@ struct __align__(16) PagedStepRecord {
 };
 
 #ifdef __CUDACC__
-// The CTA's first kDealers threads lay the steps end to end: one trip to memory for all rows (kept in shared memory for up
-// to kHeld units), a thread takes a run of units, a scan of their widths.  All threads take part in the barriers.  The share's
+// The CTA's first kDealers threads lay the steps end to end: one trip to memory for all rows (kept meanwhile in shared
+// memory that the caller needs only later; copied_over: for bulk copies), a thread takes a run of units, a scan of their widths.  All threads take part in the barriers.  The share's
 // pieces come in rounds of kList; piece i of a round is at(i).  Loops are left rolled: this code stands between the launch
 // and the first load, and a cold line of it costs more than its instructions.
 template <int kDealers, int kList>
 struct PagedDeal {
   static_assert((kList & (kList - 1)) == 0, "a power of two");
-  static constexpr int kHeld = 512;
   int warp_sum[kDealers / 32][2];
   int first, last;         // ranks, among the units that have steps, of those in the share
   PagedRecord record;
-  int held[kHeld];
   PagedPiece list[kList];
 
   struct Mine {            // of a thread: its units, and the width and the units with steps before them
     int u_begin, u_end, at, rank;
+    int tail;              // rows of unit share * kDealers + thread, if there is one
   };
-  __device__ __forceinline__ int rows_of(const PagedArgs& a, int u) const {
-    return a.n_units <= kHeld ? held[u] : paged_len(a, __ldcg(&a.state[u].x));
+  // Rows of a unit: held (a word's distance every 32, as a thread's run of units lies together), or read again.
+  __device__ __forceinline__ static int rows_of(const PagedArgs& a, const int* held, int u) {
+    return held ? held[u + (u >> 5)] : paged_len(a, __ldcg(&a.state[u].x));
   }
   // Pieces of ranks [from, from + kList) go to the list; from < 0: all, and the ranks of the first and last and the record
   // are noted (if there are more than kList, round() fills the list again).
-  __device__ __forceinline__ void fill(const PagedArgs& a, int window, int n_sink, const Mine& my, const PagedCut& cut, int share, int from) {
+  __device__ __forceinline__ void fill(const PagedArgs& a, int window, int n_sink, const Mine& my, const PagedCut& cut, int share, int from,
+                                       const int* held) {
     const int begin = cut.begin(share), end = cut.begin(share + 1);
     int r = my.rank, off = my.at;
 #pragma unroll 1
     for (int u = my.u_begin; u < my.u_end; ++u) {
-      const int len = rows_of(a, u), m = PagedSpan(len, window, n_sink).n;
+      const int len = rows_of(a, held, u), m = PagedSpan(len, window, n_sink).n;
       const int at = off + kPagedLead, lo = max(at, begin), hi = min(at + m, end);
       if (hi > lo) {
         // (divisions only for a unit that crosses the share's borders)
@@ -154,11 +156,11 @@ struct PagedDeal {
       r += m > 0;
     }
   }
-  __device__ __forceinline__ PagedCut start(const PagedArgs& a, int window, int n_sink, int share, Mine& my) {
+  __device__ __forceinline__ PagedCut start(const PagedArgs& a, int window, int n_sink, int share, Mine& my, int* held, bool copied_over) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    if (tid < kDealers && a.n_units <= kHeld)
+    if (tid < kDealers && held)
 #pragma unroll 4
-      for (int u = tid; u < a.n_units; u += kDealers) held[u] = paged_len(a, __ldcg(&a.state[u].x));
+      for (int u = tid; u < a.n_units; u += kDealers) held[u + (u >> 5)] = paged_len(a, __ldcg(&a.state[u].x));
     if (tid == 0) { first = 0; last = -1; record.parts = 0; }
     __syncthreads();
     my = Mine{};
@@ -169,7 +171,7 @@ struct PagedDeal {
       int width = 0, units = 0;
 #pragma unroll 1
       for (int u = my.u_begin; u < my.u_end; ++u) {
-        const int m = PagedSpan(rows_of(a, u), window, n_sink).n;
+        const int m = PagedSpan(rows_of(a, held, u), window, n_sink).n;
         width += m > 0 ? m + kPagedLead : 0;
         units += m > 0;
       }
@@ -195,7 +197,10 @@ struct PagedDeal {
     }
     const PagedCut cut(total, int(gridDim.x));
     if (tid == 0) record.steps = total - kPagedLead * units;
-    if (tid < kDealers) fill(a, window, n_sink, my, cut, share, -1);
+    if (tid < kDealers) fill(a, window, n_sink, my, cut, share, -1, held);
+    const int u = share * kDealers + tid;
+    if (tid < kDealers && u < a.n_units) my.tail = rows_of(a, held, u);
+    if (copied_over) ptx::fence_proxy_async_smem();
     __syncthreads();
     return cut;
   }
@@ -204,7 +209,7 @@ struct PagedDeal {
   __device__ __forceinline__ void round(const PagedArgs& a, int window, int n_sink, const Mine& my, const PagedCut& cut, int share, int rank0) {
     if (n_pieces() <= kList) return;
     __syncthreads();
-    if (threadIdx.x < kDealers) fill(a, window, n_sink, my, cut, share, first + rank0);
+    if (threadIdx.x < kDealers) fill(a, window, n_sink, my, cut, share, first + rank0, nullptr);
     __syncthreads();
   }
   __device__ __forceinline__ const PagedPiece& at(int rank0, int i) const { return list[(first + rank0 + i) & (kList - 1)]; }

@@ -143,6 +143,17 @@ def test_more_pieces_than_a_round_holds():
     Q.check(prm, q, c, Q.attend(prm, q, c, accumulate=True), 0, "bf16", before)
 
 
+@pytest.mark.parametrize("n,filled", [(148 * 140 + 5, 1.0), (50000, 0.3)])
+def test_units_by_the_ten_thousand(n, filled):
+    """Several rounds of pieces; more units than a share holds the lengths of, and than all threads together."""
+    prm = Q.params(n, 1, 1, 64, "bf16")
+    r = np.random.default_rng(n)
+    c = Q.make(prm, np.where(r.random(n) < filled, r.integers(1, 16, n), 0), 16, "bf16", 17)
+    before, q = Q.snapshot(c), query(prm, 8, "bf16")
+    Q.check(prm, q, c, Q.attend(prm, q, c), 0, "bf16")
+    Q.check(prm, q, c, Q.attend(prm, q, c, accumulate=True), 0, "bf16", before)
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_long_and_short_pieces_in_a_share(dtype):
     """Shares of 25 steps and more: pieces longer than the ring of stages, short ones in between."""
