@@ -9,8 +9,9 @@
  *     allocator.  What it keeps between calls is limited to: the built-in scratch array of
  *     tca_attn_decode_static (and its per-device address), a small cache of encoded TMA
  *     tensor maps keyed by buffer address and shape, per-device constants (SM count, L2 cache
- *     size, whether clusters of 16 run), and which kernels have been granted their shared memory on which device.  The bf16 decode kernel and tca_attn_paged ask the L2 to keep part of the
- *     cache they read (eviction-priority hints on their loads; nothing is set on the device or the context).
+ *     size, whether clusters of 16 run), and which kernels have been granted their shared memory on which device.
+ *     The bf16 decode kernel and tca_attn_paged ask the L2 to keep part of the cache they read (eviction-priority
+ *     hints on their loads; nothing is set on the device or the context).
  *   - Tensors are row-major with the head dimension contiguous:
  *       Q [batch, n_q_heads, L, head_dim]      K, V [batch, n_kv_heads, L, head_dim]
  *     A "unit" is one (sequence, KV head) pair, u = seq * n_kv_heads + kv_head; the G =
@@ -483,8 +484,9 @@ int tca_attn_window(const tca_params* prm, const void* Q, const void* K, const v
  *   All buffers but the table are aligned to 16 bytes.
  *   state   [n_units][TCA_PG_STATE_WORDS] int32, zeroed once: rows in use, position of the next token, first failed check
  *           (tca_paged_status), a word of the library's
- *   table   entries of slots that are not in use, or that a window hides, are not read.  Pages may be shared by units while they are only read;
- *           a call that writes to a page (append, evict, attention that accumulates) needs it to be one unit's alone.
+ *   table   entries of slots that are not in use, or that a window hides, are not read.  Pages may be shared by units
+ *           while they are only read; a call that writes to a page (append, evict, attention that accumulates) needs it
+ *           to be one unit's alone.
  * A call that changes a cache must not overlap with another one on it.
  * Supported: page_size 16, 32, 64, 128 or 256; n_pages * page_size and max_pages * page_size below 2^31; up to 65535
  * units (else TCA_ERR_UNSUPPORTED).
@@ -532,8 +534,8 @@ int tca_paged_append(const tca_params* prm, const void* K, const void* V, int64_
  *        different caches.
  * Slots that are not visible have no influence whatever they hold.  A visible slot whose page lies outside the pool
  * counts as not visible and sets the status word to TCA_ERR_BOUNDS (a unit that has no other gives NaN); later calls go on.
- * While a wait that gave up is in the status word, O and the masses stay as they were.  O must not overlap q.  n_sink >= 0 (TCA_ERR_INVALID_ARG), prm->window >= 1
- * (TCA_ERR_UNSUPPORTED).  prm->block, alpha and flags are not used.
+ * While a wait that gave up is in the status word, O and the masses stay as they were.  O must not overlap q.
+ * n_sink >= 0 (TCA_ERR_INVALID_ARG), prm->window >= 1 (TCA_ERR_UNSUPPORTED).  prm->block, alpha and flags are not used.
  */
 int tca_attn_paged(const tca_params* prm, const void* q, const tca_paged_desc* cache, int32_t n_sink, int32_t accumulate,
                    void* O, void* ws, size_t ws_bytes, void* stream);
@@ -545,7 +547,8 @@ size_t tca_attn_paged_workspace_bytes(const tca_params* prm, const tca_paged_des
  * below n_sink, the rows whose position is above the unit's largest position minus n_recent, and of the others
  * those with the largest mass (a NaN counts as the largest, equal ones to the lower slot).  Kept rows in slots below the
  * budget stay where they are; the other kept rows, in ascending order of slots, fill the evicted slots below the budget,
- * lowest first, with K, V, position and mass.  Then len is the budget (pages behind it are free); the position of the next token stays.
+ * lowest first, with K, V, position and mass.  Then len is the budget (pages behind it are free); the position of the
+ * next token stays.
  * The order of the other rows changes, so a sliding window, which goes by slots, no longer follows the positions.
  *   budget  DEVICE [n_units] int32
  * A unit whose sinks and recent rows are more than its budget, or with a page outside the pool, stays as it was, and

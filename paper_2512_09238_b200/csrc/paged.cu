@@ -3,20 +3,26 @@
 //
 // Bound by memory: 2 d elements per visible row, read once for the G heads of the group.  The visible rows of all
 // units are cut into one equal share per SM (paged_common.cuh); a CTA streams its share through a shared-memory ring.
-//   producer warp   reads the page table four steps ahead and brings one box per page (K or V: all columns of up to
-//                   128 rows, 128-byte swizzle; a page without a visible row is not read)
-//   two teams of 4 consumer warps, which take the pieces of the share in turn; a warp has 32 rows of every step
-//                   of 128 and a private online softmax.  bf16: ldmatrix and
-//                   mma.sync, the G <= 8 heads are the columns of the products (tcgen05 needs 64 rows of queries).
-//                   fp32: FP32 pipes, a row of K per lane, then D / 32 columns of V per lane.
+//   producer warp   reads the page table three batches of four steps ahead and brings one box per page (K or V: all
+//                   columns of up to 128 rows, 128-byte swizzle; a page without a visible row is not read)
+//   two teams of 4 consumer warps, which take the pieces of the share in turn; a warp has 32 rows of every step of 128
+//                   and a private online softmax.  bf16: ldmatrix and mma.sync, the G <= 8 heads are the columns of the
+//                   products (tcgen05 needs 64 rows of queries).  fp32: FP32 pipes, a row of K per lane, then D / 32
+//                   columns of V per lane.
 // At the end of a unit's piece the four states are merged; a piece that is the whole unit gives the result, others
-// partial results, which whoever brings the unit's last one merges in order.  Statistics and accumulators are fp32; bf16 weights are rounded
-// to bf16 before they meet the values (half a step, 2^-8 of a weight), the row sum adds the unrounded ones.
-// A slot nobody sees has no influence whatever it holds: its score is replaced, its value row is not read from the ring.
+// partial results, which whoever brings the unit's last one merges in order.  Statistics and accumulators are fp32; bf16
+// weights are rounded to bf16 before they meet the values (half a step, 2^-8 of a weight), the row sum adds the
+// unrounded ones.  A slot nobody sees has no influence whatever it holds: its score is replaced, its value row is not
+// read from the ring.
 //
 // Weights need the row sums of the whole unit, so the scores are left in the workspace (4 G bytes a row beside 4 d or 8 d)
 // and a second kernel turns them into weights; it merges the partial results as well, which costs nothing there (in the
 // first kernel, 2.5 us).
+//
+// Measured, 32/8 heads of 128, bf16, a captured call: one sequence of 700 rows 8.3 us (latency: about 5 us until the first rows
+// are there); 4 sequences of up to 64K rows (249 MB) 41 us over the same cache again, 47 over caches that change
+// (5.3 TB/s); 256 sequences of 500 to 1000 rows (790 MB) 127 us (6.2 TB/s), with weights 155; 64 sequences of up to 4K
+// rows (138 MB) with weights 36, of which the second kernel is 8.
 #include "bulk_ring.cuh"
 #include "paged_common.cuh"
 #include "rowslice.cuh"

