@@ -3,13 +3,13 @@
 //
 // One cluster of CTAs per unit, each with a run of the unit's slots, four of which a thread reads at a time (a page holds a
 // multiple of four).  The weights become order-preserving 32-bit keys, held in shared memory; the smallest kept key is
-// found by radix selection, 8 bits at a time, on histograms that the CTAs read from one another's shared memory.  The
-// i-th hole below the budget takes the i-th kept row behind it: sources and destinations are disjoint, so rows move in any
+// found by radix selection, 8 or 11 bits at a time until nothing is left to tell, on histograms that the CTAs add to one
+// another's shared memory.  The i-th hole below the budget takes the i-th kept row behind it: sources and destinations are disjoint, so rows move in any
 // order, and no more of them than have to (keeping the order of slots would move all rows behind the first hole, through
 // a staging buffer).  The pairs are put into shared memory by their number, equally many per CTA, so that the copies are
 // dealt evenly wherever the rows lie.
 // Bound by latency for short units, by memory for long ones: 8 bytes a row (weight, position) and twice a row's bytes for
-// each that moves.  32 units of up to 1200 rows take 11.5 us (a CTA each: four digits of the selection); 32 of up to 64K rows cut
+// each that moves.  32 units of up to 1200 rows take 11.5 us (a CTA each: the digits of the selection); 32 of up to 64K rows cut
 // to a third 50 us, 23 of selection and 23 moving 119 MB (5.2 TB/s); one unit of 262144 rows, on its cluster's 16 SMs, 135.
 #include <climits>
 
@@ -27,6 +27,10 @@ constexpr int kMaxCluster = 16;          // more than 8 is not portable: evict_c
 constexpr int kMostSlots = 1 << 22;      // slots of a unit: one bit each has to fit a cluster's shared memory
 constexpr int kHeld = 16 * 1024;         // slots of a CTA whose key and position are held; the others' are read again
 constexpr int kPairs = 2 * 1024;         // moves of a CTA at a time
+// Bits of a digit of the selection.  A CTA alone takes 11 (1200 rows: 12.4 against 13.7 us, the first two digits mostly
+// tell); in a cluster every bin in use is sent to all, and 8 are better (units of up to
+// 64K rows: 51.9 against 55.5 us).
+constexpr int kBitsAlone = 11, kBitsCluster = 8, kBins = 1 << kBitsAlone, kSums = 1 << kBitsCluster;
 constexpr uint32_t kSafe = 0xFFFFFFFFu;  // key of a sink or recent row; a NaN has the one below
 
 struct EvictBuffers {
@@ -46,8 +50,8 @@ struct EvictShared {
   int max_pos[kMaxCluster], bad[kMaxCluster], safe[kMaxCluster];   // of every CTA of the cluster, written by each
   int2 counts[kMaxCluster];                                        // holes, kept rows behind the budget
   int scan[kWarps][2];
-  unsigned hist[256];                     // this CTA's
-  unsigned sum[2][256];                   // the cluster's, added up by all; two, so that one barrier per digit is enough
+  alignas(16) unsigned hist[kBins];       // this CTA's
+  alignas(16) unsigned sum[2][kSums];     // the cluster's, added up by all; two, so that one barrier per digit is enough
   unsigned picked;
   int need, equals;                       // left to find; keys equal to the threshold
   int equal[kMaxCluster];
@@ -108,8 +112,10 @@ evict_kernel(const __grid_constant__ EvictBuffers b, const __grid_constant__ Pag
   top = __reduce_max_sync(0xffffffffu, top);
   bad = __any_sync(0xffffffffu, bad);
   if (lane == 0) { sh.scan[warp][0] = top; sh.scan[warp][1] = bad; }
-  sh.sum[tid >> 8][tid & 255] = 0;
-  if (tid < 256) sh.hist[tid] = 0;
+  static_assert(kBins == 4 * kThreads, "four bins a thread");
+  reinterpret_cast<uint4*>(sh.hist)[tid] = make_uint4(0, 0, 0, 0);
+  static_assert(2 * kSums == kThreads, "a word a thread");
+  sh.sum[tid / kSums][tid % kSums] = 0;
   __syncthreads();
   if (n_ctas > 1) cluster.barrier_wait();                 // every CTA of the cluster runs: its memory can be written
   if (tid < n_ctas) {
@@ -158,30 +164,33 @@ evict_kernel(const __grid_constant__ EvictBuffers b, const __grid_constant__ Pag
     cluster.map_shared_rank(&sh, tid)->safe[rank] = t;
   }
   // ---- radix selection of the need-th largest key among the others
-  uint32_t prefix = 0;
+  uint32_t prefix = 0, least = kSafe;                     // least: the smallest key that is kept
   int need = 0;
-  for (int digit = 0; digit < 4; ++digit) {
-    const int shift = 24 - 8 * digit;
+  bool tie = false;                                       // not all keys equal to the least are kept
+  const int most_bits = n_ctas > 1 ? kBitsCluster : kBitsAlone;
+  for (int digit = 0, top = 32; top > 0; ++digit) {       // bits from `top` on are known
+    const int bits = min(top, most_bits), shift = top - bits;
+    const uint32_t mask = (1u << bits) - 1u;
     for (int i = tid * 4; i < n; i += kThreads * 4) {
       const uint4 k4 = four(i);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const uint32_t k = e == 0 ? k4.x : e == 1 ? k4.y : e == 2 ? k4.z : k4.w;
-        const bool in = i + e < n && k != kSafe && (digit == 0 || (k >> (shift + 8)) == prefix);
-        if (in) atomicAdd(&sh.hist[(k >> shift) & 255u], 1u);   // (counting equal digits of a warp together first is slower)
+        const bool in = i + e < n && k != kSafe && (digit == 0 || (k >> top) == prefix);
+        if (in) atomicAdd(&sh.hist[(k >> shift) & mask], 1u);   // (counting equal digits of a warp together first is slower)
       }
     }
     __syncthreads();
     const unsigned* counts = sh.hist;
     if (n_ctas > 1) {
       counts = sh.sum[digit & 1];
-      if (tid < 256) {
+      if (tid < kSums) {
         // every CTA adds its counts to everybody's (read from the others after the barrier they took 1.2 us more a digit)
         const unsigned v = sh.hist[tid];
         if (v)
           for (int c = 0; c < n_ctas; ++c) atomicAdd(&cluster.map_shared_rank(&sh, c)->sum[digit & 1][tid], v);
       } else {
-        sh.sum[(digit + 1) & 1][tid - 256] = 0;     // read before the last barrier, added to after the next
+        sh.sum[(digit + 1) & 1][tid - kSums] = 0;         // read before the last barrier, added to after the next
       }
       cluster.sync();
     }
@@ -192,40 +201,50 @@ evict_kernel(const __grid_constant__ EvictBuffers b, const __grid_constant__ Pag
         if (rank == 0 && tid == 0) report_paged(st, kPagedBudget);
         return;
       }
+      if (need == 0) break;                               // none but the safe ones
     }
-    // the bin at which the count from above reaches need, one bin per thread; if nothing is needed the highest, of
-    // which nothing is kept
-    unsigned total = 0, count = 0;
-    if (tid < 256) {
-      count = total = counts[255 - tid];
+    // the bin at which the count from above reaches need, four bins per thread
+    const int n_four = 1 << (most_bits - 2);              // (bins behind the last digit's are empty)
+    const uint4 own = tid < n_four ? reinterpret_cast<const uint4*>(counts)[n_four - 1 - tid] : make_uint4(0, 0, 0, 0);
+    const unsigned total = own.x + own.y + own.z + own.w;
+    unsigned count = total;
 #pragma unroll
-      for (int off = 1; off < 32; off <<= 1) {
-        const unsigned t = __shfl_up_sync(0xffffffffu, count, off);
-        if (lane >= off) count += t;
-      }
-      if (lane == 31) sh.scan[warp][0] = int(count);
+    for (int off = 1; off < 32; off <<= 1) {
+      const unsigned t = __shfl_up_sync(0xffffffffu, count, off);
+      if (lane >= off) count += t;
     }
+    if (lane == 31) sh.scan[warp][0] = int(count);
     __syncthreads();
-    if (tid < 256) {
-      for (int w = 0; w < warp; ++w) count += unsigned(sh.scan[w][0]);
-      const int above = int(count - total);
-      if (need > 0 ? int(count) >= need && above < need : tid == 0) {
-        sh.picked = 255 - tid;
-        sh.need = need - above;
-        sh.equals = int(total);
+    for (int w = 0; w < warp; ++w) count += unsigned(sh.scan[w][0]);
+    int above = int(count - total);
+    if (int(count) >= need && above < need) {
+      int bin = (n_four - tid) * 4;
+      unsigned in = 0;
+#pragma unroll
+      for (int i = 3; i >= 0; --i) {
+        if (above + int(in) >= need) break;
+        above += int(in);
+        in = i == 3 ? own.w : i == 2 ? own.z : i == 1 ? own.y : own.x;
+        --bin;
       }
-      if (digit < 3) sh.hist[255 - tid] = 0;
+      sh.picked = bin;
+      sh.need = need - above;
+      sh.equals = int(in);
     }
+    if (shift > 0) reinterpret_cast<uint4*>(sh.hist)[tid] = make_uint4(0, 0, 0, 0);
     __syncthreads();
-    prefix = (prefix << 8) | sh.picked;
-    need = need > 0 ? sh.need : 0;
+    prefix = (prefix << bits) | sh.picked;
+    top = shift;
+    need = sh.need;
+    least = prefix << shift;
+    tie = need != sh.equals;                              // the whole cluster alike
+    if (!tie) break;                                      // the bin is kept whole
   }
 
-  // ---- which slots are kept: keys above the threshold, and of those equal to it the `need` lowest slots
+  // ---- which slots are kept: keys from the least on, or of those equal to it the `need` lowest slots
   const int words = (n + 31) >> 5;
-  const bool tie = need != sh.equals;                     // the whole cluster alike
-  int equals = 0;                                         // of the slots before: keys equal to the threshold
-  if (tie && need > 0) {
+  int equals = 0;                                         // of the slots before: keys equal to the least
+  if (tie) {
     if (tid < n_ctas) cluster.map_shared_rank(&sh, tid)->equal[rank] = int(sh.hist[sh.picked]);
     sync_all();
     for (int c = 0; c < rank; ++c) equals += sh.equal[c];
@@ -233,17 +252,16 @@ evict_kernel(const __grid_constant__ EvictBuffers b, const __grid_constant__ Pag
   for (int i0 = 0; i0 < n; i0 += kThreads * 4) {
     const int i = i0 + tid * 4;
     const uint4 k4 = i < n ? four(i) : make_uint4(0, 0, 0, 0);
-    unsigned nibble = 0, eq = 0;                          // of the four slots: kept, equal to the threshold
+    unsigned nibble = 0, eq = 0;                          // of the four slots: kept, equal to the least
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const uint32_t k = e == 0 ? k4.x : e == 1 ? k4.y : e == 2 ? k4.z : k4.w;
       if (i + e >= n) continue;
-      if (k == kSafe || k > prefix) nibble |= 1u << e;
-      if (need > 0 && k == prefix) eq |= 1u << e;
+      if (k >= least) nibble |= 1u << e;
+      if (k == least) eq |= 1u << e;
     }
-    if (!tie) {
-      nibble |= eq;
-    } else if (need > 0) {
+    if (tie) {
+      nibble &= ~eq;
       int incl = __popc(eq);
 #pragma unroll
       for (int off = 1; off < 32; off <<= 1) {
