@@ -204,7 +204,7 @@ __device__ __forceinline__ bool simt_flash(const Src& src, float scale_log2e, fl
     simt_group_sync(group);                // (P needs no more than a warp: a row's 16 threads are half of one)
     auto accumulate = [&](auto guarded) {
 #pragma unroll (RT == 4 ? 2 : 1)
-      for (int kk = 0; kk < kKeys; kk += 4) {
+      for (int kk = 0; kk < n_keys; kk += 4) {                       // (weights behind the tile's last key are 0)
         float4 p[RT];
 #pragma unroll
         for (int i = 0; i < RT; ++i) p[i] = *reinterpret_cast<const float4*>(sP + (ty * RT + i) * PST + kk);
