@@ -151,19 +151,24 @@ __device__ __forceinline__ bool simt_flash(const Src& src, float scale_log2e, fl
     for (int i = 0; i < RT; ++i)
 #pragma unroll
       for (int j = 0; j < KT; ++j) s[i][j] = 0.f;
+    auto score = [&](auto count) {         // the first count x 16 keys
+      constexpr int kCount = decltype(count)::value;
 #pragma unroll (RT == 4 ? 4 : 2)
-    for (int d = 0; d < D; d += 4) {
-      float4 q[RT], k[KT];
+      for (int d = 0; d < D; d += 4) {
+        float4 q[RT], k[kCount];
 #pragma unroll
-      for (int i = 0; i < RT; ++i) q[i] = *reinterpret_cast<const float4*>(sQ + (ty * RT + i) * ST + d);
+        for (int i = 0; i < RT; ++i) q[i] = *reinterpret_cast<const float4*>(sQ + (ty * RT + i) * ST + d);
 #pragma unroll
-      for (int j = 0; j < KT; ++j) k[j] = *reinterpret_cast<const float4*>(sK + (tx + 16 * j) * ST + d);
+        for (int j = 0; j < kCount; ++j) k[j] = *reinterpret_cast<const float4*>(sK + (tx + 16 * j) * ST + d);
 #pragma unroll
-      for (int i = 0; i < RT; ++i)
+        for (int i = 0; i < RT; ++i)
 #pragma unroll
-        for (int j = 0; j < KT; ++j)
-          s[i][j] = fmaf(q[i].w, k[j].w, fmaf(q[i].z, k[j].z, fmaf(q[i].y, k[j].y, fmaf(q[i].x, k[j].x, s[i][j]))));
-    }
+          for (int j = 0; j < kCount; ++j)
+            s[i][j] = fmaf(q[i].w, k[j].w, fmaf(q[i].z, k[j].z, fmaf(q[i].y, k[j].y, fmaf(q[i].x, k[j].x, s[i][j]))));
+      }
+    };
+    if (Src::kGap && src.keys(t) <= kKeys / 2) score(std::integral_constant<int, KT / 2>{});
+    else score(std::integral_constant<int, KT>{});
     simt_group_sync(group);                // K has been read
     load_k(t + 2);
     const bool masked = src.masked(t);
