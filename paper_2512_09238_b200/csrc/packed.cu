@@ -2,8 +2,8 @@
 // with every key retained), grouped query heads, strided buffers; tca_attn_window: the same with a sliding window
 // and sinks.  This file holds the entry points and the FP32-pipe kernel (fp32 inputs; bf16 with
 // TCA_FLAG_PREFILL_SIMT as a cross-check); bf16 runs on the tensor-core kernel of packed_tc.cu.
-// fp32, 8 heads of 64, prompts of up to 2048 tokens under 300 keys and 8 sinks: 68 us, 18 TFLOP/s, bound by the shared-memory pipe;
-// 384 keys a block of rows where 308 are seen.
+// fp32, 8 heads of 64, prompts of up to 2048 tokens under 300 keys and 8 sinks: 64 us, 19 TFLOP/s, bound by the shared-memory pipe;
+// up to 339 keys a block of 32 rows where 308 are seen.
 #include "flash_simt.cuh"
 #include "packed_common.cuh"
 

@@ -9,8 +9,8 @@
 // a staging buffer).  The pairs are put into shared memory by their number, equally many per CTA, so that the copies are
 // dealt evenly wherever the rows lie.
 // Bound by latency for short units, by memory for long ones: 8 bytes a row (weight, position) and twice a row's bytes for
-// each that moves.  32 units of up to 1200 rows take 11.5 us (a CTA each: the digits of the selection); 32 of up to 64K rows cut
-// to a third 50 us, 23 of selection and 23 moving 119 MB (5.2 TB/s); one unit of 262144 rows, on its cluster's 16 SMs, 135.
+// each that moves.  32 units of up to 1200 rows take 10 us (a CTA each); 32 of up to 64K rows cut to a third 48 us, 18 until the
+// moves are known and 23 moving 119 MB (5.2 TB/s); one unit of 262144 rows, on its cluster's 16 SMs, 104.
 #include <climits>
 
 #include <cooperative_groups.h>
