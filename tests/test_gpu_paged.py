@@ -412,6 +412,25 @@ def test_evict_cluster_shapes(n_units, length):
     evict_and_check_large(prm, c, 4, 100, np.full(n_units, length // 2))
 
 
+@pytest.mark.parametrize("length", [1500, 9000])
+@pytest.mark.parametrize("spread", [1, 40, 3000, 1 << 20])
+def test_evict_weights_that_differ_in_their_last_bits(length, spread):
+    """A CTA alone and a cluster; every digit of the selection has something to tell, or only the last one."""
+    prm = Q.params(4, 1, 1, 64, "bf16")
+    c = Q.make(prm, np.full(4, length) - np.arange(4), 32, "bf16", 48)
+    r = np.random.default_rng(spread)
+    bits = np.float32(0.75).view(np.int32) + r.integers(0, spread, c.mass.numel()).astype(np.int32)
+    c.mass.copy_(torch.from_numpy(bits.view(np.float32)).view(c.mass.shape))
+    evict_and_check_large(prm, c, 4, 0, [length // 3, 4, length - 5, length // 2])
+
+
+@pytest.mark.parametrize("length", [1500, 9000])
+def test_evict_leaves_exactly_what_has_to_stay(length):
+    prm = Q.params(2, 1, 1, 64, "bf16")
+    c = Q.make(prm, [length, length - 7], 32, "bf16", 49)
+    evict_and_check_large(prm, c, 10, 200, [210, 210])
+
+
 def evict_and_check_large(prm, c, n_sink, n_recent, budgets):
     """evict_and_check with a sort in place of the oracle's loops, and rows compared on the device."""
     lens, before = Q.lens_of(c), {n: getattr(c, n).clone() for n in ("k", "v", "pos", "mass")}
