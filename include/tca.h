@@ -468,8 +468,9 @@ int tca_cache_accept(const tca_params* prm, tca_cache_desc* cache, const void* k
  * Causal attention with a sliding window and a few first tokens that stay visible ("sinks"), for packed prompts:
  * row i of a sequence attends to its rows j <= i with i - j < prm->window or j < n_sink.  Everything else is
  * tca_attn_packed: buffers, strides, seq_start, empty sequences, rows of nobody, what a row does not see, flags, and
- * the workspace (TCA_OP_PACKED; the two calls may use the same one in turn).  With a window, or
- * sinks, of at least `rows` the result is bit for bit tca_attn_packed's.  The form for single tokens is tca_attn_paged.
+ * the workspace (TCA_OP_PACKED; the two calls may use the same one in turn).  A sequence of which
+ * the window or the sinks hide nothing (no longer than one of the two) gets bit for bit tca_attn_packed's result, whatever
+ * shares its buffers.  The form for single tokens is tca_attn_paged.
  * n_sink >= 0, else TCA_ERR_INVALID_ARG; prm->window >= 1, else TCA_ERR_UNSUPPORTED.
  */
 int tca_attn_window(const tca_params* prm, const void* Q, const void* K, const void* V, int64_t rows,

@@ -588,7 +588,11 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
         rescale(mx, it > 0);
         const float neg_m = (m_used == -INFINITY) ? 0.f : -m_used;
         const uint64_t neg_m2 = ptx::pack2(neg_m, neg_m);
+        // The row sum: two packed chains; of a masked tile one, in the order of the compact loop below, so that a row of
+        // which nothing is hidden has the same bits from sources of either kind (24 prompts of up to 2048 tokens under
+        // 512 keys 94.6 -> 95.9 us; a second body for items with hidden keys, which keep the packed chains, 98.5).
         uint64_t sum2[2] = {0ull, 0ull};
+        float sum = 0.f;
         // eight groups of 16 scores; a group's store is issued only after the next group's arithmetic, so it
         // never waits for exponentials still in flight
 #pragma unroll
@@ -599,7 +603,8 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
             float xl, xh;
             ptx::unpack2(ptx::fma2(ptx::pack2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])), scale2, neg_m2), xl, xh);
             const float el = ptx::fast_exp2(xl), eh = ptx::fast_exp2(xh);
-            sum2[j & 1] = ptx::add2(sum2[j & 1], ptx::pack2(el, eh));
+            if constexpr (kMasked) sum += el + eh;
+            else sum2[j & 1] = ptx::add2(sum2[j & 1], ptx::pack2(el, eh));
             v[j] = ptx::pack_bf16x2(el, eh);   // entry j is never read again (j <= 2j)
           }
           if (g == kTcPSplit + 1) {            // the first part was stored at least one group ago
@@ -609,10 +614,13 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
         }
         ptx::tmem_st8(s_addr + 56, &v[56]);
         announce(1);
-        float s0, s1, s2, s3;
-        ptx::unpack2(sum2[0], s0, s1);
-        ptx::unpack2(sum2[1], s2, s3);
-        l += (s0 + s1) + (s2 + s3);
+        if constexpr (!kMasked) {
+          float s0, s1, s2, s3;
+          ptx::unpack2(sum2[0], s0, s1);
+          ptx::unpack2(sum2[1], s2, s3);
+          sum = (s0 + s1) + (s2 + s3);
+        }
+        l += sum;
       };
 #pragma unroll 1
       for (; it < whole && ok; ++it) full_tile(std::false_type{}, src);

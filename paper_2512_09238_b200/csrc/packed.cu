@@ -209,7 +209,8 @@ extern "C" int tca_attn_packed(const tca_params* prm, const void* Q, const void*
 extern "C" int tca_attn_window(const tca_params* prm, const void* Q, const void* K, const void* V, int64_t rows,
                                const int64_t* seq_start, const int64_t* strides, int32_t n_sink, void* O, void* ws,
                                size_t ws_bytes, void* stream) {
-  // where nothing is hidden from anybody it is the other call
+  // Where nothing is hidden from anybody it is the other call.  Which prompts share the buffers decides that, so the two
+  // kernels take the keys of a prompt of which nothing is hidden in the same order: its bits are the same from either.
   if (prm && prm->window >= 1 && (prm->window >= rows || n_sink >= rows) && n_sink >= 0)
     return attn_packed<false>(prm, Q, K, V, rows, seq_start, strides, 0, O, ws, ws_bytes, stream);
   return attn_packed<true>(prm, Q, K, V, rows, seq_start, strides, n_sink, O, ws, ws_bytes, stream);
