@@ -1,0 +1,109 @@
+"""Shapes of the paged cache that need many rows or units: evictions of units whose slots do not all fit a CTA's shared memory,
+attention whose shares take several rounds of pieces."""
+import numpy as np
+import pytest
+import torch
+
+import paged_harness as Q
+import serving_harness as H
+from paper_2512_09238_b200 import binding as B
+
+pytestmark = pytest.mark.gpu
+HELD = 16 * 1024       # slots of a CTA whose weights and positions evict keeps in shared memory
+
+
+def query(prm, seed, dtype):
+    return H.randn(seed, (prm.batch, prm.n_q_heads, prm.head_dim), dtype, 1.5)
+
+
+# ------------------------------------------------------------------ eviction
+def kept_slots(mass, pos, budget, n_sink, n_recent):
+    """The definition by one sort: which slots of a unit are kept."""
+    slot = np.arange(len(mass))
+    safe = (slot < n_sink) | (pos.astype(np.int64) > int(pos.max()) - n_recent)
+    assert safe.sum() <= budget
+    weight = np.where(np.isnan(mass), np.inf, mass.astype(np.float64))
+    rank = np.lexsort((slot, -weight, ~np.isnan(mass), ~safe))
+    kept = np.zeros(len(mass), dtype=bool)
+    kept[rank[:budget]] = True
+    return kept
+
+
+def evict_and_check(prm, c, n_sink, n_recent, budgets):
+    lens, before = Q.lens_of(c), {n: getattr(c, n).clone() for n in ("k", "v", "pos", "mass")}
+    B.tca_paged_evict(prm, c, n_sink, n_recent, torch.tensor(np.asarray(budgets), dtype=torch.int32, device="cuda"))
+    assert B.tca_paged_status(c)[0] == B.TCA_OK
+    mass, pos = before["mass"].cpu().numpy().reshape(-1), before["pos"].cpu().numpy().reshape(-1)
+    to, frm = [], []
+    for u, n in enumerate(lens):
+        budget = int(budgets[u])
+        if n <= budget:
+            continue
+        rows = Q.pool_rows(c, u, np.arange(n))
+        kept = kept_slots(mass[rows], pos[rows], budget, n_sink, n_recent)
+        to.append(rows[:budget][~kept[:budget]])
+        frm.append(rows[budget:][kept[budget:]])
+    to, frm = (torch.from_numpy(np.concatenate(x)).cuda() for x in (to, frm))
+    for name, x in before.items():
+        flat = x.view(-1, prm.head_dim) if name in "kv" else x.view(-1)
+        flat[to] = flat[frm]
+        a, b = (t.view(torch.int32) if name == "mass" else t for t in (x, getattr(c, name)))
+        assert torch.equal(a, b), name
+    np.testing.assert_array_equal(Q.lens_of(c), np.minimum(lens, budgets))
+
+
+def weigh(c, seed, kind):
+    """Positions in no order; weights: "distinct", "ties" (few values) or "nans" (some of them NaN, in many ties)."""
+    r = np.random.default_rng(seed)
+    pos, mass = c.pos.cpu().numpy().reshape(-1), c.mass.cpu().numpy().reshape(-1)
+    for u, n in enumerate(Q.lens_of(c)):
+        n, rows = int(n), Q.pool_rows(c, u, np.arange(n))
+        pos[rows] = r.permutation(2 * n)[:n]
+        mass[rows] = r.permutation(n) * 0.25 + 1 if kind == "distinct" else r.integers(0, 5, n)
+        if kind == "nans":
+            mass[rows[r.random(n) < 0.3]] = np.nan
+    c.pos.copy_(torch.from_numpy(pos).view(c.pos.shape))
+    c.mass.copy_(torch.from_numpy(mass).view(c.mass.shape))
+
+
+@pytest.mark.parametrize("kind", ["distinct", "ties", "nans"])
+def test_evict_one_unit_of_more_slots_than_a_cluster_holds(kind):
+    """A cluster of 16 CTAs at most; every CTA reads the slots behind its first 16384 again at each pass."""
+    n = 16 * HELD + 16 * 700 + 3
+    prm = Q.params(1, 1, 1, 64, "bf16")
+    c = Q.make(prm, [n], 64, "bf16", 60)
+    weigh(c, 61, kind)
+    evict_and_check(prm, c, 5, 300, [n // 2 + 1])        # several rounds of moves
+    weigh(c, 62, kind)
+    evict_and_check(prm, c, 5, 300, [n // 7])
+
+
+@pytest.mark.parametrize("kind", ["distinct", "ties", "nans"])
+def test_evict_units_of_more_slots_than_a_cta_holds(kind):
+    """So many units that each has one CTA, a few of them longer than its shared memory."""
+    U = 2 * torch.cuda.get_device_properties(0).multi_processor_count + 4
+    lens = np.full(U, 5)
+    lens[[0, 7, U // 2, U - 1]] = [HELD, HELD + 1, 2 * HELD + 4099, HELD + 62]
+    prm = Q.params(U, 1, 1, 64, "f32")
+    c = Q.make(prm, lens, 32, "f32", 63)
+    weigh(c, 64, kind)
+    evict_and_check(prm, c, 3, 50, np.where(lens > 5, lens // 2 - 1, 5))
+
+
+# ------------------------------------------------------------------ attention
+@pytest.mark.parametrize("dtype,hq,d", [("bf16", 2, 64), ("bf16", 8, 128), ("f32", 1, 64), ("f32", 2, 64), ("f32", 5, 128)])
+def test_several_rounds_of_pieces_with_units_across_shares(dtype, hq, d):
+    """More than 128 pieces in every share (one round of the list), and units that run from one share into others."""
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    n = 140 * sms + 11
+    prm = Q.params(n, hq, 1, d, dtype)
+    r = np.random.default_rng(hq)
+    lens = r.integers(1, 16, n)
+    lens[r.permutation(n)[:6]] = [30000, 25000, 40001, 127, 2000, 33000]
+    c = Q.make(prm, lens, 16, dtype, 70)
+    q, ws = query(prm, 71, dtype), B.alloc_paged_workspace(prm, c, True)
+    o = Q.attend(prm, q, c, ws=ws)
+    Q.check(prm, q, c, o, 0, dtype)
+    before = Q.snapshot(c)
+    Q.check(prm, q, c, Q.attend(prm, q, c, accumulate=True, ws=ws), 0, dtype, before)
+    assert torch.equal(o, Q.attend(prm, q, c, ws=ws))
