@@ -26,6 +26,7 @@
 #include "bulk_ring.cuh"
 #include "paged_common.cuh"
 #include "rowslice.cuh"
+#include "team.cuh"
 #include "tensor_map.cuh"
 
 namespace tca {
@@ -442,7 +443,7 @@ paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
   uint8_t* query_buf = states + kTeams * Ring::kState;
   __shared__ BulkRing<kStages> ring;
   __shared__ PagedDeal<kTeams * kConsumers, kList> deal;
-  __shared__ int abort_word, merge_here[kTeams];
+  __shared__ int abort_word, goes_on[kTeams], merge_here[kTeams];
   __shared__ __align__(16) uint32_t zeros[4];
   __shared__ uint64_t query_full[Ring::kQueries];
   __shared__ int page_buf[kPageBatches + 1][32];
@@ -612,8 +613,8 @@ paged_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         }
         // ----------------------------------------------------------- the warps' states become the piece's
         rows.leave(state + tw * GT * state_row(D), s_m[team][tw], s_l[team][tw]);
-        team_sync(team);
-        if (!*abort_flag && !stops_call(found_status)) {
+        if (team_agrees(tid % kConsumers == 0, &goes_on[team], [&] { return !*abort_flag && !stops_call(found_status); },
+                        [&] { team_sync(team); })) {
           const size_t at = size_t(share + piece.u) * G;
           for (int j = tid % kConsumers * 4; j < G * D; j += kConsumers * 4) {
             const int g = j / D, d = j - g * D;
@@ -691,18 +692,19 @@ paged_join_kernel(int G, int n_shares, int weight_blocks, PagedWs ws, float* __r
   pdl_wait();
   pdl_launch_dependents();
   const int found_status = __ldcg(ws.status);
+  auto stopped = [&] { return __any_sync(0xffffffffu, stops_call(found_status)); };   // what follows needs whole warps
   if (int(blockIdx.x) >= weight_blocks) {
     const int at = (int(blockIdx.x) - weight_blocks) * kJoinWarps + warp, share = at / G, g = at - share * G;
     if (share >= n_shares) return;
     const int4 rec = __ldcg(reinterpret_cast<const int4*>(ws.records) + share);
-    if (stops_call(found_status)) return;
+    if (stopped()) return;
     if (rec.z > 0) merge_head<T, D>(ws, rec.y, rec.z, G, g, O + (size_t(rec.x) * G + g) * D);
     return;
   }
   // ---- weights
   const int warps = weight_blocks * kJoinWarps;
   const int total = __ldcg(&ws.records[0].steps);
-  if (stops_call(found_status)) return;
+  if (stopped()) return;
   const float inv_g = 1.f / float(G);
   int2 where, next_where, group[4];
   auto fetch = [&](int step) {               // the record of the step after this one is on its way during this one

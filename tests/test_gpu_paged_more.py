@@ -1,5 +1,6 @@
 """Shapes of the paged cache that need many rows or units: evictions of units whose slots do not all fit a CTA's shared memory,
-attention whose shares take several rounds of pieces."""
+attention whose shares take several rounds of pieces; a
+status word that changes under running calls."""
 import numpy as np
 import pytest
 import torch
@@ -107,3 +108,25 @@ def test_several_rounds_of_pieces_with_units_across_shares(dtype, hq, d):
     before = Q.snapshot(c)
     Q.check(prm, q, c, Q.attend(prm, q, c, accumulate=True, ws=ws), 0, dtype, before)
     assert torch.equal(o, Q.attend(prm, q, c, ws=ws))
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_a_status_word_that_changes_under_running_calls(accumulate):
+    """Somebody else sets and clears the status word all the time: every call still ends, writes nothing but its results, and
+    the zeroed workspace is as good as new."""
+    prm = Q.params(6, 8, 2, 128, "bf16")
+    c = Q.make(prm, [30000, 20, 700, 9000, 0, 1, 130, 260, 5000, 3, 64, 12000], 32, "bf16", 90)
+    ws, q = B.alloc_paged_workspace(prm, c, accumulate), query(prm, 91, "bf16")
+    good, before = Q.attend(prm, q, c, ws=ws), Q.snapshot(c)
+    words = [torch.zeros(1, dtype=torch.int32, device="cuda"), torch.ones(1, dtype=torch.int32, device="cuda")]
+    o, status, side = torch.empty_like(q), ws[:4].view(torch.int32), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for i in range(300):
+        B.tca_attn_paged(prm, q, c, 0, accumulate, o, ws)
+        with torch.cuda.stream(side):
+            for j in range(6):
+                status.copy_(words[j & 1])
+    torch.cuda.synchronize()
+    Q.same(before, Q.snapshot(c), ("mass",) if accumulate else ())
+    ws.zero_()
+    assert torch.equal(good, Q.attend(prm, q, c, ws=ws))
