@@ -126,6 +126,7 @@ append_rows_kernel(const __grid_constant__ AppendBuffers b, const __grid_constan
     __threadfence();
     const unsigned before = atomicAdd(count, 1u);
     if ((before & ~kFailed) == unsigned(seqs.first_cta[lo + 1] - seqs.first_cta[lo] - 1)) {
+      __threadfence();                    // the others' reads of the length come before what is written to it here
       if (!(before & kFailed)) {
         st->x = len + n_new;
         st->y = next + n_new;

@@ -1,6 +1,6 @@
 """Shapes of the paged cache that need many rows or units: evictions of units whose slots do not all fit a CTA's shared memory,
-attention whose shares take several rounds of pieces; a
-status word that changes under running calls."""
+attention whose shares take several rounds of pieces; a status word that changes under running calls; appends of many
+CTAs a unit."""
 import numpy as np
 import pytest
 import torch
@@ -130,3 +130,34 @@ def test_a_status_word_that_changes_under_running_calls(accumulate):
     Q.same(before, Q.snapshot(c), ("mass",) if accumulate else ())
     ws.zero_()
     assert torch.equal(good, Q.attend(prm, q, c, ws=ws))
+
+
+def test_append_with_many_ctas_a_unit_again_and_again():
+    """Up to 40 CTAs read a unit's length before the last of them moves it on; ten calls in a row, the same ones replayed."""
+    prm = Q.params(4, 3, 3, 64, "bf16")
+    new, again = np.array([5000, 129, 700, 2561]), 10
+    c = Q.make(prm, np.zeros(12), 64, "bf16", 95, room=int(new.max()) * 2 * again)
+    starts = np.concatenate([[0], np.cumsum(new)]).astype(np.int64)
+    rows = int(starts[-1])
+    k, v = (H.packed_buffer(96 + i, 3, rows, 64, "bf16", "tokens") for i in range(2))
+    calls = lambda: [B.tca_paged_append(prm, k, v, rows, starts, None, None, c) for _ in range(again)]  # noqa: E731
+    calls()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        calls()
+    g.replay()
+    torch.cuda.synchronize()
+    assert B.tca_paged_status(c)[0] == B.TCA_OK
+    state = c.state.cpu().numpy().reshape(4, 3, B.TCA_PG_STATE_WORDS)
+    for word in (B.TCA_PG_LEN, B.TCA_PG_NEXT):
+        np.testing.assert_array_equal(state[:, :, word], np.repeat(2 * again * new[:, None], 3, 1))
+    assert (state[:, :, 3] == 0).all()
+    for s, n in enumerate(new):
+        for h in range(3):
+            r = torch.from_numpy(Q.pool_rows(c, s * 3 + h, np.arange(2 * again * n))).cuda()
+            part = slice(int(starts[s]), int(starts[s + 1]))
+            for pool, x in ((c.k, k), (c.v, v)):
+                assert torch.equal(pool.view(-1, 64)[r].view(2 * again, int(n), 64), x[h, part].expand(2 * again, -1, -1))
+            assert torch.equal(c.pos.view(-1)[r].long().cpu(), torch.arange(2 * again * int(n)))
