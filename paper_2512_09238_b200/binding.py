@@ -632,7 +632,8 @@ class PagedCache:
     ``table``, ``state`` (rows, next position, first failed check, a word of the library's), ``pos`` and ``mass`` are
     device tensors; the last three lie in one buffer, ``meta``.  ``reserve`` and ``release`` keep a host copy of the table and a
     list of free pages, and upload the units that changed; a program with an allocator of its own writes ``table``
-    instead."""
+    instead.  They upload on ``stream``, or on torch's current one, and give pages to other units at once, so that
+    stream has to be the calls' over the cache, or ordered with it."""
 
     def __init__(self, prm: tca_params, n_pages: int, page_size: int, max_pages: int, device="cuda"):
         U = prm.batch * prm.n_kv_heads
@@ -660,7 +661,7 @@ class PagedCache:
         """It lies on device `here` and was made for this type and head size."""
         return self._kind == (here, dtype, d)
 
-    def reserve(self, rows: Sequence[int]) -> None:
+    def reserve(self, rows: Sequence[int], stream=None) -> None:
         """Every unit u gets the pages that rows[u] rows need, where it has fewer."""
         want = self._pages(rows)
         more = np.maximum(0, want - self.n_held)
@@ -672,9 +673,9 @@ class PagedCache:
             self.table_host[u, self.n_held[u]:want[u]] = self.free[-n:][::-1]
             del self.free[-n:]
             self.n_held[u] = want[u]
-        self._upload(changed)
+        self._upload(changed, stream)
 
-    def release(self, rows: Sequence[int]) -> None:
+    def release(self, rows: Sequence[int], stream=None) -> None:
         """Every unit u gives back the pages that rows[u] rows do not need (after an eviction to a budget, or with 0
         rows when its sequence ends; its state is the caller's to clear then)."""
         want = self._pages(rows)
@@ -683,7 +684,7 @@ class PagedCache:
             self.free.extend(self.table_host[u, want[u]:self.n_held[u]][::-1].tolist())
             self.table_host[u, want[u]:] = -1
             self.n_held[u] = want[u]
-        self._upload(changed)
+        self._upload(changed, stream)
 
     def _pages(self, rows) -> np.ndarray:
         rows = np.asarray(rows, dtype=np.int64)
@@ -691,10 +692,11 @@ class PagedCache:
             raise ValueError("rows must have one entry, not negative, per (sequence, KV head)")
         return -(-rows // self.page_size)
 
-    def _upload(self, units) -> None:
+    def _upload(self, units, stream) -> None:
         if len(units):
-            at = torch.from_numpy(np.ascontiguousarray(units)).to(self.table.device)
-            self.table[at] = torch.from_numpy(self.table_host[units]).to(self.table.device)
+            with torch.cuda.stream(stream):              # None: the current one
+                at = torch.from_numpy(np.ascontiguousarray(units)).to(self.table.device)
+                self.table[at] = torch.from_numpy(self.table_host[units]).to(self.table.device)
 
 
 def tca_calib_colmean(prm, Q, K, L, colmean, ws, stream=None) -> None:

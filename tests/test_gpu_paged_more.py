@@ -1,6 +1,6 @@
 """Shapes of the paged cache that need many rows or units: evictions of units whose slots do not all fit a CTA's shared memory,
 attention whose shares take several rounds of pieces; a status word that changes under running calls; appends of many
-CTAs a unit."""
+CTAs a unit; pages dealt on another stream."""
 import numpy as np
 import pytest
 import torch
@@ -161,3 +161,30 @@ def test_append_with_many_ctas_a_unit_again_and_again():
             for pool, x in ((c.k, k), (c.v, v)):
                 assert torch.equal(pool.view(-1, 64)[r].view(2 * again, int(n), 64), x[h, part].expand(2 * again, -1, -1))
             assert torch.equal(c.pos.view(-1)[r].long().cpu(), torch.arange(2 * again * int(n)))
+
+
+def test_pages_change_hands_on_the_stream_of_the_calls():
+    """A call that waits in its stream reads the pages it was given, although they are dealt anew behind it."""
+    prm = Q.params(2, 4, 2, 64, "bf16")
+    c = Q.make(prm, [300, 40, 500, 129], 32, "bf16", 97, max_pages=20, spare=0)
+    q, ws = query(prm, 98, "bf16"), B.alloc_paged_workspace(prm, c)
+    want, o, side = Q.attend(prm, q, c, ws=ws), torch.full_like(q, float("nan")), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(200_000_000)                   # 0.1 s
+    B.tca_attn_paged(prm, q, c, 0, False, o, ws, stream=side)
+    c.release([0, 0, 0, 0], stream=side)
+    assert (c.table_host == -1).all()
+    c.reserve([0, 600, 0, 1], stream=side)
+    with torch.cuda.stream(side):
+        c.state.zero_()
+    k, v = (H.randn(99 + i, (2, 2, 64), "bf16") for i in range(2))
+    torch.cuda.current_stream().synchronize()
+    c.reserve([1, 0, 1, 0], stream=side)
+    B.tca_paged_append(prm, k, v, 2, None, None, None, c, stream=side)
+    side.synchronize()
+    assert B.tca_ws_status(ws) == B.TCA_OK and B.tca_paged_status(c)[0] == B.TCA_OK
+    assert torch.equal(o, want)
+    np.testing.assert_array_equal(c.table.cpu().numpy(), c.table_host)
+    for u in range(4):
+        assert torch.equal(c.k.view(-1, 64)[Q.pool_rows(c, u, [0])[0]], k[u % 2, u // 2])
