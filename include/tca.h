@@ -533,6 +533,9 @@ int tca_paged_append(const tca_params* prm, const void* K, const void* V, int64_
  *   ws   DEVICE workspace of tca_attn_paged_workspace_bytes(prm, cache, accumulate) bytes, zeroed once after
  *        allocating; word 0 is the sticky status word.  Calls that share one must not overlap; they may be over
  *        different caches.
+ * The window goes by slots.  tca_paged_evict moves late rows into low slots, and nothing in the cache tells that it did: over
+ * a cache that is evicted from, a window that hides anything may hide recent rows and show old ones.  There the window is
+ * 2^31 - 1, and n_recent of the eviction is what keeps the recent rows.
  * Slots that are not visible have no influence whatever they hold.  A visible slot whose page lies outside the pool
  * counts as not visible and sets the status word to TCA_ERR_BOUNDS (a unit that has no other gives NaN); later calls go on.
  * While a wait that gave up is in the status word, O and the masses stay as they were.  O must not overlap q.
@@ -550,7 +553,8 @@ size_t tca_attn_paged_workspace_bytes(const tca_params* prm, const tca_paged_des
  * budget stay where they are; the other kept rows, in ascending order of slots, fill the evicted slots below the budget,
  * lowest first, with K, V, position and mass.  Then len is the budget (pages behind it are free); the position of the
  * next token stays.
- * The order of the other rows changes, so a sliding window, which goes by slots, no longer follows the positions.
+ * The order of the other rows changes, so the window of tca_attn_paged, which goes by slots, no longer follows the positions
+ * (see there).
  *   budget  DEVICE [n_units] int32
  * A unit whose sinks and recent rows are more than its budget, or with a page outside the pool, stays as it was, and
  * tca_paged_status says so.  n_sink, n_recent >= 0 (TCA_ERR_INVALID_ARG).

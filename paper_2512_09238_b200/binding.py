@@ -546,7 +546,7 @@ def alloc_paged_workspace(prm: tca_params, cache: "PagedCache", accumulate: bool
 
 
 def tca_attn_paged(prm, q, cache: "PagedCache", n_sink, accumulate, O, ws, stream=None) -> None:
-    """q, O [batch, n_q_heads, d], contiguous."""
+    """q, O [batch, n_q_heads, d], contiguous.  prm.window goes by slots: over a cache that is evicted from it is 2^31 - 1."""
     e, qs = _ELT.get(prm.dtype), (prm.batch, prm.n_q_heads, prm.head_dim)
     try:
         here = q.get_device()

@@ -1,6 +1,6 @@
 """Shapes of the paged cache that need many rows or units: evictions of units whose slots do not all fit a CTA's shared memory,
 attention whose shares take several rounds of pieces; a status word that changes under running calls; appends of many
-CTAs a unit; pages dealt on another stream."""
+CTAs a unit; pages dealt on another stream; a window over an evicted cache."""
 import numpy as np
 import pytest
 import torch
@@ -188,3 +188,18 @@ def test_pages_change_hands_on_the_stream_of_the_calls():
     np.testing.assert_array_equal(c.table.cpu().numpy(), c.table_host)
     for u in range(4):
         assert torch.equal(c.k.view(-1, 64)[Q.pool_rows(c, u, [0])[0]], k[u % 2, u // 2])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_window_over_an_evicted_cache_goes_by_slots(dtype):
+    """What stays visible are the last slots and the sinks, whatever positions their rows have; a window that hides nothing sees
+    every row that was kept."""
+    prm = Q.params(2, 4, 2, 64, dtype, window=20)
+    c = Q.make(prm, [300, 700, 41, 260], 32, dtype, 92)
+    B.tca_paged_evict(prm, c, 4, 30, torch.tensor([120, 200, 60, 90], dtype=torch.int32, device="cuda"))
+    assert B.tca_paged_status(c)[0] == B.TCA_OK and Q.lens_of(c).tolist() == [120, 200, 41, 90]
+    pos = c.pos.cpu().numpy().reshape(-1)
+    assert pos[Q.pool_rows(c, 1, np.arange(180))].max() >= 670       # recent rows lie where the window hides them
+    for p in (prm, Q.params(2, 4, 2, 64, dtype)):
+        q, before = query(prm, 93, dtype), Q.snapshot(c)
+        Q.check(p, q, c, Q.attend(p, q, c, 4, accumulate=True), 4, dtype, before)
