@@ -489,8 +489,9 @@ int tca_attn_window(const tca_params* prm, const void* Q, const void* K, const v
  *           while they are only read; a call that writes to a page (append, evict, attention that accumulates) needs it
  *           to be one unit's alone.
  * A call that changes a cache must not overlap with another one on it.
- * Supported: page_size 16, 32, 64, 128 or 256; n_pages * page_size and max_pages * page_size below 2^31; up to 65535
- * units (else TCA_ERR_UNSUPPORTED).
+ * Supported: page_size 16, 32, 64, 128 or 256; n_pages * page_size below 2^31, max_pages * page_size below 2^31 - 256; up
+ * to 65535 units; n_units * (max_pages * page_size / 128 + 3) below 2^31, as steps of 128 slots of all units are counted
+ * in 32 bits (else TCA_ERR_UNSUPPORTED).
  */
 typedef struct tca_paged_desc {
   void* k;              /* DEVICE [n_pages, page_size, head_dim]                        */
@@ -539,6 +540,9 @@ int tca_paged_append(const tca_params* prm, const void* K, const void* V, int64_
  * Slots that are not visible have no influence whatever they hold.  A visible slot whose page lies outside the pool
  * counts as not visible and sets the status word to TCA_ERR_BOUNDS (a unit that has no other gives NaN); later calls go on.
  * While a wait that gave up is in the status word, O and the masses stay as they were.  O must not overlap q.
+ * The softmax weights of bf16 inputs are rounded to bf16 before they meet the values, as in tca_attn_packed; sums,
+ * accumulators and masses are fp32.  How a unit's rows are split over CTAs follows from the lengths of all units, and the
+ * last bits of its result may too; the same state gives the same bits.
  * n_sink >= 0 (TCA_ERR_INVALID_ARG), prm->window >= 1 (TCA_ERR_UNSUPPORTED).  prm->block, alpha and flags are not used.
  */
 int tca_attn_paged(const tca_params* prm, const void* q, const tca_paged_desc* cache, int32_t n_sink, int32_t accumulate,
@@ -557,7 +561,8 @@ size_t tca_attn_paged_workspace_bytes(const tca_params* prm, const tca_paged_des
  * (see there).
  *   budget  DEVICE [n_units] int32
  * A unit whose sinks and recent rows are more than its budget, or with a page outside the pool, stays as it was, and
- * tca_paged_status says so.  n_sink, n_recent >= 0 (TCA_ERR_INVALID_ARG).
+ * tca_paged_status says so.  n_sink, n_recent >= 0 (TCA_ERR_INVALID_ARG); max_pages * page_size at most 2^22, a bit of
+ * shared memory each (TCA_ERR_UNSUPPORTED).
  */
 int tca_paged_evict(const tca_params* prm, tca_paged_desc* cache, int32_t n_sink, int32_t n_recent, const int32_t* budget,
                     void* stream);
