@@ -510,7 +510,8 @@ __device__ __forceinline__ void flash_tc(Source& src, uint8_t* smem, TcShared<ty
     const uint64_t scale2 = ptx::pack2(scale_log2e, scale_log2e);
     uint32_t tile_count = 0, item_count = 0;
     src.begin_row(row);
-    for (int k = 0; !*abort_flag && next_item(k); ++k) {
+    // (a vote, as another role may set the flag between two lanes' looks at it, and next_item() needs the whole warp)
+    for (int k = 0; !__any_sync(0xffffffffu, *abort_flag != 0) && next_item(k); ++k) {
       const int nt = src.tiles(kShared ? h : 0);
       const int mine = kShared ? nt : (nt - h + 1) / 2;      // tiles of this block / stream
       const int row_key = src.row_key(h);

@@ -1,5 +1,5 @@
-"""A team of threads whose branch holds barriers (csrc/team.cuh): it has to take the branch as one, whatever each of its threads
-would have found by asking for itself.  Runs the header's function on host threads; no kernel is launched."""
+"""Threads whose branch holds barriers or votes take it as one.  A team of warps (csrc/team.cuh) has to, whatever each of its
+threads would have found by asking for itself.  Runs the header's function on host threads; no kernel is launched."""
 import os
 import shutil
 import subprocess
@@ -99,3 +99,9 @@ def test_the_paged_kernel_asks_as_a_team():
     """The branch that holds the merge's barriers hangs on that one answer."""
     src = open(os.path.join(_build.CSRC, "paged.cu")).read()
     assert src.count("if (team_agrees(") == 1 and "if (!*abort_flag" not in src
+
+
+def test_the_mainloop_votes_on_the_abort_flag():
+    """The softmax warps of flash_tc.cuh leave their loop over items together: what is in it needs whole warps."""
+    src = open(os.path.join(_build.CSRC, "flash_tc.cuh")).read()
+    assert "!*abort_flag &&" not in src and "__any_sync(0xffffffffu, *abort_flag != 0)" in src
