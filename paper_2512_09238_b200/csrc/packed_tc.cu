@@ -10,7 +10,7 @@
 //
 // With a window the tiles are fewer and of two kinds (WindowTiles): 24 prompts of 0 to 2048 tokens under 512 keys and 16 sinks take
 // 96 us (items of 5 tiles: 17000 clocks, and 5000 for the end of one); 32768 tokens and two shorter prompts under 4096 keys
-// 1.78 to 1.88 ms (1.10 to 1.16 PFLOP/s).
+// 1.80 to 1.90 ms (1.09 to 1.15 PFLOP/s).
 #include "flash_tc.cuh"
 #include "packed_common.cuh"
 
